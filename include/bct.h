@@ -274,6 +274,108 @@ bct_status_t bct_stack_forward(bct_cache_t *const *caches, int32_t n_layers, con
                                void *scratch, size_t scratch_bytes, void *out, int64_t T, void *cuda_stream);
 
 /*
+ * Linear attention with a decay for each head: the update rule of the bounded cache with the key itself as the
+ * address.  Where UpdateKV adds softmax(wq_t . MK^T)^T . wv_t to a state of C slots, here a state of head_dim
+ * rows takes k_t^T . v_t and forgets at a rate of its own:
+ *     S_t = exp(log_decay[h]) * S_(t-1) + k_t^T v_t        o_g = scale * q_g . S_t      (the token sees its own write)
+ * per (sequence, kv-head), G = n_q_heads / n_kv_heads query heads reading each state.  The calls keep no handle:
+ * the state is the caller's, DEVICE float [B][Hkv][d][d], the key's features in its rows, the value's in its
+ * columns.
+ *   log_decay  DEVICE float [Hkv], 4-byte aligned: the logarithm of the decay, <= 0; 0 never forgets, minus infinity
+ *              keeps only the token itself.  A constant of the head: the backward forms no gradient for it.
+ * Outputs are rounded once to `dtype`; everything before that is fp32.  No atomics: the same call gives the same bits.
+ * No output may overlap an input or another output, except where stated (BCT_ERR_INVALID_ARG).
+ */
+typedef struct bct_linear_params {
+    int32_t batch;      /* B  >= 1 sequences */
+    int32_t n_q_heads;  /* Hq >= 1, a multiple of n_kv_heads */
+    int32_t n_kv_heads; /* Hkv >= 1 */
+    int32_t head_dim;   /* d in {64, 128}, of keys and values alike */
+    int32_t dtype;      /* BCT_F32 or BCT_BF16: q, k, v, out and their gradients; states are float */
+    float scale;        /* <= 0 selects 1/sqrt(head_dim) */
+} bct_linear_params_t;
+
+/* Bytes of scratch that bct_linear_forward (backward = 0) or bct_linear_backward (backward = 1) needs for T
+ * tokens: long calls of few heads are split over the tokens, and the states between the parts live there.  0 for
+ * many calls.  Depends on the arguments only. */
+bct_status_t bct_linear_scratch_bytes(const bct_linear_params_t *params, int64_t T, int32_t backward, size_t *bytes);
+
+/*
+ * One token per sequence.
+ *   q, out  DEVICE [B][Hq][d]     k, v  DEVICE [B][Hkv][d]
+ *   state, state_out   the state before and after; state_out may be `state` itself (exactly) or a buffer of its own
+ */
+bct_status_t bct_linear_step(const bct_linear_params_t *params, const void *q, const void *k, const void *v,
+                             const float *log_decay, const float *state, float *state_out, void *out,
+                             void *cuda_stream);
+
+/*
+ * T tokens per sequence, equal to T bct_linear_step calls within rounding, in chunks whose products are formed
+ * together.
+ *   q, out     DEVICE [B][T][Hq][d]      k, v  DEVICE [B][T][Hkv][d]
+ *   lens       DEVICE int32 [B] or NULL (all T): tokens of each sequence, 0..T (clamped); the rows behind them are
+ *              padding, which is not read into any result, and `out` is zero there
+ *   state      the state before the first token, or NULL (zeros)
+ *   state_out  the state after each sequence's last token, or NULL; may be `state` itself (exactly)
+ *   scratch    DEVICE, 256-byte aligned, bct_linear_scratch_bytes(params, T, 0); NULL where that is 0.  In use until
+ *              the stream has passed the call: calls that may overlap need a scratch each
+ */
+bct_status_t bct_linear_forward(const bct_linear_params_t *params, int64_t T, const void *q, const void *k,
+                                const void *v, const float *log_decay, const int32_t *lens, const float *state,
+                                float *state_out, void *out, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/*
+ * Backward of bct_linear_forward, from its inputs alone.  With do_t = dL/do_t (summing over the G heads of a group):
+ *     d_q_t = scale * S_t do_t                          S_t forward in time, from `state`
+ *     d_k_t = R_t v_t,  d_v_t = R_t^T k_t               R_t = exp(log_decay) R_(t+1) + scale * q_t^T do_t
+ *     d_state_in = exp(log_decay) * R_1
+ * where R_(len) + .. starts from d_state, the gradient of the state after the last token.
+ *   d_out      DEVICE [B][T][Hq][d]      q, k, v, lens, state   the forward call's (state NULL: zeros)
+ *   d_state    DEVICE float [B][Hkv][d][d], or NULL (zeros)
+ *   d_q        DEVICE [B][T][Hq][d]      d_k, d_v  DEVICE [B][T][Hkv][d], in `dtype`; zero in padding rows
+ *   d_state_in DEVICE float [B][Hkv][d][d], or NULL
+ *   scratch    as above, bct_linear_scratch_bytes(params, T, 1)
+ */
+bct_status_t bct_linear_backward(const bct_linear_params_t *params, int64_t T, const void *d_out, const void *q,
+                                 const void *k, const void *v, const float *log_decay, const int32_t *lens,
+                                 const float *state, const float *d_state, void *d_q, void *d_k, void *d_v,
+                                 float *d_state_in, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/*
+ * Norms of queries and keys for each head, and the rotation by the token's position in the same pass: what stands
+ * between bct_project_qkv and an attention step that knows positions.  For every head vector x of q and k
+ *     y = x / sqrt(mean(x^2) + eps) * w        out = y with its first rot_dim features turned in pairs:
+ *     (y_a, y_b) -> (y_a cos p f - y_b sin p f, y_a sin p f + y_b cos p f),   p the token's position, f = freq[i]
+ * with the pairs (i, i + rot_dim/2), or (2i, 2i + 1) with BCT_ROTATE_INTERLEAVED, i < rot_dim/2.
+ *   q, q_out   DEVICE [n_tokens][Hq][d]       k, k_out  DEVICE [n_tokens][Hkv][d], in `dtype`; q_out may be q itself
+ *              and k_out k itself (exactly), any other overlap is refused
+ *   w_q, w_k   DEVICE [d] in `dtype`, or NULL (ones)
+ *   positions  DEVICE int64 [n_tokens]        freq  DEVICE double [rot_dim/2], radians per position; the angle is
+ *              formed in double.  Both may be NULL with rot_dim = 0 (norm only)
+ *   rot_dim    0..head_dim, a multiple of 16 (BCT_ERR_UNSUPPORTED otherwise);  head_dim in {64, 128}
+ */
+#define BCT_ROTATE_INTERLEAVED 1u
+bct_status_t bct_norm_rotate(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                             const void *q, const void *k, const void *w_q, const void *w_k, float eps,
+                             const int64_t *positions, const double *freq, int32_t rot_dim, uint32_t flags, void *q_out,
+                             void *k_out, void *cuda_stream);
+
+/*
+ * Backward of bct_norm_rotate: d_q, d_k (in `dtype`; d_q may be d_q_out itself and d_k d_k_out itself) and the weights'
+ * gradients d_w_q, d_w_k (DEVICE float [d], summed over tokens and heads in a fixed order), each of which may be NULL.
+ *   q, k      the forward call's inputs, before the norm
+ *   scratch   DEVICE, 256-byte aligned, bct_norm_rotate_scratch_bytes bytes: the blocks' shares of d_w; not used, and may
+ *             be NULL, when both d_w_q and d_w_k are NULL.  Calls that may overlap need a scratch each
+ */
+bct_status_t bct_norm_rotate_scratch_bytes(int64_t n_tokens, int32_t head_dim, size_t *bytes);
+bct_status_t bct_norm_rotate_backward(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                      int32_t dtype, const void *d_q_out, const void *d_k_out, const void *q,
+                                      const void *k, const void *w_q, const void *w_k, float eps,
+                                      const int64_t *positions, const double *freq, int32_t rot_dim, uint32_t flags,
+                                      void *d_q, void *d_k, float *d_w_q, float *d_w_k, void *scratch,
+                                      size_t scratch_bytes, void *cuda_stream);
+
+/*
  * Host-buffer forms of bct_decode_step and bct_prefill_stream: the same shapes, but q, k, v and out are
  * HOST pointers.  The inputs are copied into the workspace's staging area (two sets, used
  * alternately, on a copy stream the handle owns, so that one call's copies overlap the

@@ -26,7 +26,10 @@ EXPORTS = (
     "bct_project_qkv", "bct_layer_scratch_bytes", "bct_layer_forward", "bct_update_kv",
     "bct_cache_status_clear", "bct_cache_rows_rewritten", "bct_selftest_timeout",
     "bct_update_kv_backward", "bct_stack_scratch_bytes", "bct_stack_forward",
+    "bct_linear_scratch_bytes", "bct_linear_step", "bct_linear_forward", "bct_linear_backward",
+    "bct_norm_rotate", "bct_norm_rotate_scratch_bytes", "bct_norm_rotate_backward",
 )
+ROTATE_INTERLEAVED = 1
 STATIC_STAGE_BYTES = 8 << 20
 
 
@@ -36,6 +39,13 @@ class BctParams(ctypes.Structure):
         ("head_dim", ctypes.c_int32), ("capacity", ctypes.c_int32), ("dtype", ctypes.c_int32),
         ("read_scale", ctypes.c_float), ("write_scale", ctypes.c_float), ("init_len", ctypes.c_int32),
         ("flags", ctypes.c_uint32), ("write_eps", ctypes.c_float), ("max_stream", ctypes.c_int32),
+    ]
+
+
+class BctLinearParams(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
     ]
 
 
@@ -89,6 +99,15 @@ def load() -> ctypes.CDLL:
     lib.bct_stack_scratch_bytes.argtypes = [ctypes.POINTER(vp), i32, i64, ctypes.POINTER(ctypes.c_size_t)]
     lib.bct_stack_forward.argtypes = [ctypes.POINTER(vp), i32, vp, i32, ctypes.POINTER(vp), ctypes.POINTER(vp),
                                       ctypes.POINTER(vp), vp, ctypes.c_size_t, vp, i64, vp]
+    pl, sz, f32, u32 = ctypes.POINTER(BctLinearParams), ctypes.c_size_t, ctypes.c_float, ctypes.c_uint32
+    lib.bct_linear_scratch_bytes.argtypes = [pl, i64, i32, ctypes.POINTER(sz)]
+    lib.bct_linear_step.argtypes = [pl, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.bct_linear_forward.argtypes = [pl, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bct_linear_backward.argtypes = [pl, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bct_norm_rotate.argtypes = [i64, i32, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, i32, u32, vp, vp, vp]
+    lib.bct_norm_rotate_scratch_bytes.argtypes = [i64, i32, ctypes.POINTER(sz)]
+    lib.bct_norm_rotate_backward.argtypes = [i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, f32, vp, vp, i32, u32,
+                                             vp, vp, vp, vp, vp, sz, vp]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -181,6 +200,198 @@ def stack_forward(caches, x, w_q, w_wq, w_wv, out=None, scratch=None, stream=Non
                                  arr([w.data_ptr() for w in w_wq]), arr([w.data_ptr() for w in w_wv]), scratch.data_ptr(),
                                  scratch.numel(), out.data_ptr(), T, _stream_ptr(stream)))
     return out
+
+
+def _operand(name, t, shape, dtype, device) -> None:
+    """The library sees pointers only: shape, type, place and layout are checked here."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s (got %s, %s, %s%s)" % (
+            name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", strided"))
+
+
+def _io_dtype(name, t) -> int:
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("%s must be float32 or bfloat16 (got %s)" % (name, t.dtype))
+    return BCT_BF16 if t.dtype == torch.bfloat16 else BCT_F32
+
+
+def _result(name, t, shape, dtype, device):
+    """The caller's buffer, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _operand(name, t, shape, dtype, device)
+    return t
+
+
+def _launch(device, stream, call, *args) -> None:
+    """The call on the tensors' device: on `stream`, or on that device's current stream."""
+    if device.index == torch.cuda.current_device():
+        _check(call(*args, _stream_ptr(stream)))
+        return
+    with torch.cuda.device(device):
+        _check(call(*args, _stream_ptr(stream)))
+
+
+def _scratch(need: int, scratch, device):
+    if scratch is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    if not scratch.is_cuda or scratch.device != device or not scratch.is_contiguous():
+        raise ValueError("scratch must be a contiguous tensor on %s" % device)
+    return scratch
+
+
+def _scratch_args(scratch):
+    return (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())
+
+
+def _linear_setup(q, k, v, log_decay, lead, scale):
+    """Checks the operands that every linear-attention call has; q ``[*lead, Hq, d]``, k and v ``[*lead, Hkv, d]``."""
+    if q.dim() != len(lead) + 2 or k.dim() != len(lead) + 2:
+        raise ValueError("q and k must have %d dimensions" % (len(lead) + 2))
+    Hq, Hkv, d = q.shape[-2], k.shape[-2], q.shape[-1]
+    dt = _io_dtype("q", q)
+    _operand("q", q, (*lead, Hq, d), q.dtype, q.device)
+    _operand("k", k, (*lead, Hkv, d), q.dtype, q.device)
+    _operand("v", v, (*lead, Hkv, d), q.dtype, q.device)
+    _operand("log_decay", log_decay, (Hkv,), torch.float32, q.device)
+    return BctLinearParams(lead[0], Hq, Hkv, d, dt, scale), (lead[0], Hkv, d, d)
+
+
+def linear_scratch_bytes(batch, T, n_q_heads, n_kv_heads, head_dim, dtype, *, backward=False) -> int:
+    """Scratch that linear_forward (or linear_backward) needs for these sizes."""
+    n = ctypes.c_size_t(0)
+    p = BctLinearParams(batch, n_q_heads, n_kv_heads, head_dim, _dtype_code(dtype), 0.0)
+    _check(load().bct_linear_scratch_bytes(ctypes.byref(p), T, int(backward), ctypes.byref(n)))
+    return n.value
+
+
+def linear_step(q, k, v, log_decay, state, scale=0.0, out=None, state_out=None, stream=None):
+    """Linear attention with a decay for each head, one token per sequence: ``S' = exp(log_decay) S + k^T v``,
+    ``out = scale q S'``.  q ``[B, Hq, d]``, k, v ``[B, Hkv, d]``, state ``[B, Hkv, d, d]`` float32.  state_out: where
+    S' goes; None updates `state` in place.  Returns (out, state after)."""
+    lib = load()
+    p, s_shape = _linear_setup(q, k, v, log_decay, q.shape[:1], scale)
+    _operand("state", state, s_shape, torch.float32, q.device)
+    out = _result("out", out, q.shape, q.dtype, q.device)
+    state_out = state if state_out is None else _result("state_out", state_out, s_shape, torch.float32, q.device)
+    _launch(q.device, stream, lib.bct_linear_step, ctypes.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+            log_decay.data_ptr(), state.data_ptr(), state_out.data_ptr(), out.data_ptr())
+    return out, state_out
+
+
+def linear_forward(q, k, v, log_decay, state=None, lens=None, scale=0.0, out=None, state_out=None, scratch=None,
+                   stream=None):
+    """T tokens per sequence: q ``[B, T, Hq, d]``, k, v ``[B, T, Hkv, d]``; state ``[B, Hkv, d, d]`` float32 or None
+    (zeros); lens int32 ``[B]`` or None: the valid tokens of each sequence of a padded batch.  Returns (out
+    ``[B, T, Hq, d]``, state after each sequence's last token); state_out may be `state`."""
+    lib = load()
+    p, s_shape = _linear_setup(q, k, v, log_decay, q.shape[:2], scale)
+    dev, T = q.device, q.shape[1]
+    if state is not None:
+        _operand("state", state, s_shape, torch.float32, dev)
+    if lens is not None:
+        _operand("lens", lens, q.shape[:1], torch.int32, dev)
+    out = _result("out", out, q.shape, q.dtype, dev)
+    state_out = _result("state_out", state_out, s_shape, torch.float32, dev)
+    need = ctypes.c_size_t(0)
+    _check(lib.bct_linear_scratch_bytes(ctypes.byref(p), T, 0, ctypes.byref(need)))
+    scratch = _scratch(need.value, scratch, dev)
+    _launch(dev, stream, lib.bct_linear_forward, ctypes.byref(p), T, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+            log_decay.data_ptr(), _ptr(lens), _ptr(state), state_out.data_ptr(), out.data_ptr(), *_scratch_args(scratch))
+    return out, state_out
+
+
+def linear_backward(d_out, q, k, v, log_decay, state=None, d_state=None, lens=None, scale=0.0, out=None, scratch=None,
+                    stream=None):
+    """Backward of linear_forward: d_out ``[B, T, Hq, d]`` and d_state ``[B, Hkv, d, d]`` float32 (the gradient of the
+    state after the last token, or None) -> (d_q, d_k, d_v in q's dtype, d_state_in float32).  out: that tuple, to
+    write into."""
+    lib = load()
+    p, s_shape = _linear_setup(q, k, v, log_decay, q.shape[:2], scale)
+    dev, T = q.device, q.shape[1]
+    _operand("d_out", d_out, q.shape, q.dtype, dev)
+    for name, t in (("state", state), ("d_state", d_state)):
+        if t is not None:
+            _operand(name, t, s_shape, torch.float32, dev)
+    if lens is not None:
+        _operand("lens", lens, q.shape[:1], torch.int32, dev)
+    given = (None,) * 4 if out is None else out
+    d_q = _result("d_q", given[0], q.shape, q.dtype, dev)
+    d_k = _result("d_k", given[1], k.shape, q.dtype, dev)
+    d_v = _result("d_v", given[2], v.shape, q.dtype, dev)
+    d_in = _result("d_state_in", given[3], s_shape, torch.float32, dev)
+    need = ctypes.c_size_t(0)
+    _check(lib.bct_linear_scratch_bytes(ctypes.byref(p), T, 1, ctypes.byref(need)))
+    scratch = _scratch(need.value, scratch, dev)
+    _launch(dev, stream, lib.bct_linear_backward, ctypes.byref(p), T, d_out.data_ptr(), q.data_ptr(), k.data_ptr(),
+            v.data_ptr(), log_decay.data_ptr(), _ptr(lens), _ptr(state), _ptr(d_state), d_q.data_ptr(), d_k.data_ptr(),
+            d_v.data_ptr(), d_in.data_ptr(), *_scratch_args(scratch))
+    return d_q, d_k, d_v, d_in
+
+
+def _norm_rotate_setup(q, k, w_q, w_k, positions, freq):
+    if q.dim() < 3 or k.dim() != q.dim():
+        raise ValueError("q and k must be [..., heads, head_dim] with at least one token dimension")
+    lead, d, dt, dev = tuple(q.shape[:-2]), q.shape[-1], _io_dtype("q", q), q.device
+    Hq, Hkv = q.shape[-2], k.shape[-2]
+    _operand("q", q, q.shape, q.dtype, dev)
+    _operand("k", k, (*lead, Hkv, d), q.dtype, dev)
+    for name, w in (("w_q", w_q), ("w_k", w_k)):
+        if w is not None:
+            _operand(name, w, (d,), q.dtype, dev)
+    rot = 0
+    if freq is not None:
+        rot = 2 * freq.numel()
+        _operand("freq", freq, (rot // 2,), torch.float64, dev)
+        if positions is None:
+            raise ValueError("positions are needed where freq is given")
+        _operand("positions", positions, lead, torch.int64, dev)
+    n = 1
+    for x in lead:
+        n *= x
+    return n, Hq, Hkv, d, dt, rot
+
+
+def norm_rotate(q, k, w_q, w_k, positions, freq, eps=1e-6, interleaved=False, out=None, stream=None):
+    """Norm of every head of q ``[..., Hq, d]`` and k ``[..., Hkv, d]`` with the weights w_q, w_k ``[d]`` (None: ones),
+    and the rotation of their first ``2 len(freq)`` features by ``positions * freq``: positions int64 ``[...]``, freq
+    float64, radians per position (None: norm only).  interleaved: neighbouring features are the pairs, instead of
+    those half the rotated part away.  out: (q, k) to write into, which may be the inputs.  Returns (q, k)."""
+    lib = load()
+    n, Hq, Hkv, d, dt, rot = _norm_rotate_setup(q, k, w_q, w_k, positions, freq)
+    q_out, k_out = (None, None) if out is None else out
+    q_out, k_out = _result("q_out", q_out, q.shape, q.dtype, q.device), _result("k_out", k_out, k.shape, q.dtype, q.device)
+    _launch(q.device, stream, lib.bct_norm_rotate, n, Hq, Hkv, d, dt, q.data_ptr(), k.data_ptr(), _ptr(w_q), _ptr(w_k), eps,
+            _ptr(positions) if rot else None, _ptr(freq) if rot else None, rot, ROTATE_INTERLEAVED if interleaved else 0,
+            q_out.data_ptr(), k_out.data_ptr())
+    return q_out, k_out
+
+
+def norm_rotate_backward(d_q_out, d_k_out, q, k, w_q, w_k, positions, freq, eps=1e-6, interleaved=False, want_d_w=True,
+                         out=None, scratch=None, stream=None):
+    """Backward of norm_rotate, given the gradients of its two results and its inputs -> (d_q, d_k in q's dtype, d_w_q,
+    d_w_k float32 or None).  out: that tuple, to write into (d_q may be d_q_out, d_k may be d_k_out)."""
+    lib = load()
+    n, Hq, Hkv, d, dt, rot = _norm_rotate_setup(q, k, w_q, w_k, positions, freq)
+    dev = q.device
+    _operand("d_q_out", d_q_out, q.shape, q.dtype, dev)
+    _operand("d_k_out", d_k_out, k.shape, q.dtype, dev)
+    given = (None,) * 4 if out is None else out
+    d_q = _result("d_q", given[0], q.shape, q.dtype, dev)
+    d_k = _result("d_k", given[1], k.shape, q.dtype, dev)
+    d_w_q = _result("d_w_q", given[2], (d,), torch.float32, dev) if want_d_w else None
+    d_w_k = _result("d_w_k", given[3], (d,), torch.float32, dev) if want_d_w else None
+    if want_d_w:
+        need = ctypes.c_size_t(0)
+        _check(lib.bct_norm_rotate_scratch_bytes(n, d, ctypes.byref(need)))
+        scratch = _scratch(need.value, scratch, dev)
+    else:
+        scratch = None
+    _launch(dev, stream, lib.bct_norm_rotate_backward, n, Hq, Hkv, d, dt, d_q_out.data_ptr(), d_k_out.data_ptr(),
+            q.data_ptr(), k.data_ptr(), _ptr(w_q), _ptr(w_k), eps, _ptr(positions) if rot else None,
+            _ptr(freq) if rot else None, rot, ROTATE_INTERLEAVED if interleaved else 0, d_q.data_ptr(), d_k.data_ptr(),
+            _ptr(d_w_q), _ptr(d_w_k), *_scratch_args(scratch))
+    return d_q, d_k, d_w_q, d_w_k
 
 
 class Cache:

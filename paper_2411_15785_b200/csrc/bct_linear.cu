@@ -1,0 +1,460 @@
+// Linear attention with a decay for each head on the CUDA cores: the single-token step, and the chunked scan
+// for the types and head sizes that the tensor-core kernel does not serve.
+//
+//     S_t = lambda S_{t-1} + k_t^T v_t        o_t = scale q_t S_t         lambda = exp(log_decay[h])
+//
+// The scan takes the tokens in chunks of 32: inside a chunk the products (a_i . b_j) are formed for all pairs
+// and weighted with lambda^|i-j|; what lies before the chunk comes out of the state, which is updated once per
+// chunk.  Everything is fp32; the powers of lambda are formed in double (33 of them per block).
+//
+// One block holds one (sequence, kv-head) unit and half of c's features: those columns of the state and of the
+// output depend on nothing in the other half, and only the 32 x 32 products are formed twice.  The state of the
+// block lives in registers (its update reads b and c from shared memory) and is copied to shared memory once per
+// chunk, where the next chunk's products with a read it.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "bct_device.cuh"
+#include "bct_internal.h"
+#include "bct_linear.h"
+
+namespace bct {
+namespace {
+
+constexpr int kCh = 32;         // tokens per chunk
+constexpr int kScanThreads = 256;
+
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p);
+template <>
+__device__ __forceinline__ float4 load4<float>(const float* p) {
+    return *reinterpret_cast<const float4*>(p);
+}
+template <>
+__device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p) {
+    const uint2 w = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                       __uint_as_float(w.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store4(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 x) {
+    *reinterpret_cast<uint2*>(p) =
+        make_uint2(Chunk<__nv_bfloat16>::pack2(x.x, x.y), Chunk<__nv_bfloat16>::pack2(x.z, x.w));
+}
+__device__ __forceinline__ float4 fma4(float s, float4 x, float4 acc) {
+    return make_float4(fmaf(s, x.x, acc.x), fmaf(s, x.y, acc.y), fmaf(s, x.z, acc.z), fmaf(s, x.w, acc.w));
+}
+__device__ __forceinline__ float4 mul4(float s, float4 x) { return make_float4(s * x.x, s * x.y, s * x.z, s * x.w); }
+__device__ __forceinline__ float dot4(float4 x, float4 y, float acc) {
+    return fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, acc))));
+}
+
+template <int D, int NC>
+struct ScanSmem {
+    float a[kCh][D + 4];    // rows 16 bytes apart modulo 128: neighbouring rows start in other banks
+    float b[kCh][D + 4];
+    float c[kCh][NC];
+    float p[kCh][kCh + 4];
+    float s[D][NC];
+    float pw[kCh + 1];      // lambda^n
+};
+
+// lambda^n, n = 0..kCh
+__device__ __forceinline__ void fill_powers(float* pw, float log_decay, int tid) {
+    if (tid <= kCh) pw[tid] = tid == 0 ? 1.f : (float)exp((double)tid * (double)log_decay);
+}
+
+template <typename T, int D, int NC, bool STATE_ONLY>
+__global__ void __launch_bounds__(kScanThreads, 2) linear_scan_kernel(const LinArgs args, const LinStates st) {
+    extern __shared__ __align__(16) unsigned char scan_smem_raw[];
+    ScanSmem<D, NC>& sm = *reinterpret_cast<ScanSmem<D, NC>*>(scan_smem_raw);
+    constexpr int kCG = NC / 4;                  // groups of four columns
+    constexpr int kRG = kScanThreads / kCG;      // groups of rows
+    constexpr int kOutRows = kCh / kRG;          // output rows of a thread
+    constexpr int kStateRows = D / kRG;          // state rows of a thread
+    static_assert(kOutRows >= 1 && kStateRows >= 1, "");
+
+    const int tid = threadIdx.x;
+    const int ncol = D / NC;
+    int idx = blockIdx.x;
+    const int col0 = (idx % ncol) * NC;
+    idx /= ncol;
+    const int seg = idx % args.nseg;
+    const int u = idx / args.nseg;
+    const int bi = u / args.Hkv, h = u - bi * args.Hkv;
+
+    const int which = STATE_ONLY ? (st.seg[0] == nullptr ? 1 : (int)blockIdx.y) : (int)blockIdx.y;
+    LinRole r = args.role[STATE_ONLY ? 0 : which];
+    if (STATE_ONLY) {
+        r.b = st.b[which];
+        r.c = st.c[which];
+        r.reverse = which;
+        r.Ga = 1;
+        r.Gb = st.G[which];
+        // the last segment in the order of the scan feeds no other
+        if (seg == (r.reverse ? 0 : args.nseg - 1)) return;
+    }
+    const T* ga = static_cast<const T*>(r.a);
+    const T* gb = static_cast<const T*>(r.b);
+    const T* gc = static_cast<const T*>(r.c);
+    T* go = static_cast<T*>(r.out);
+
+    const int len = args.lens ? min(max(args.lens[bi], 0), args.T) : args.T;
+    const int t_begin = seg * args.seg_len;
+    const int t_end = min(t_begin + args.seg_len, args.T);
+    const int v_end = min(t_end, len);           // valid tokens of the segment end here
+    const int n_chunks = v_end > t_begin ? (v_end - t_begin + kCh - 1) / kCh : 0;
+
+    fill_powers(sm.pw, args.log_decay[h], tid);
+
+    const int cg = tid % kCG, rg = tid / kCG;
+    const int cc = col0 + 4 * cg;                // this thread's four columns
+    float4 S[kStateRows];                        // rows rg * kStateRows ..
+#pragma unroll
+    for (int i = 0; i < kStateRows; ++i) S[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (!STATE_ONLY) {
+        const bool from_seg = args.nseg > 1;
+        const float* src = from_seg ? r.seg + ((size_t)u * args.nseg + seg) * D * D
+                                    : (r.state_in ? r.state_in + (size_t)u * D * D : nullptr);
+        const float mul = from_seg ? 1.f : r.in_mul;
+        if (src != nullptr) {
+#pragma unroll
+            for (int i = 0; i < kStateRows; ++i) {
+                const int k = rg * kStateRows + i;
+                if (!r.state_t) {
+                    S[i] = mul4(mul, *reinterpret_cast<const float4*>(src + (size_t)k * D + cc));
+                } else {
+                    S[i] = make_float4(mul * src[(size_t)cc * D + k], mul * src[(size_t)(cc + 1) * D + k],
+                                       mul * src[(size_t)(cc + 2) * D + k], mul * src[(size_t)(cc + 3) * D + k]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kStateRows; ++i)
+            *reinterpret_cast<float4*>(&sm.s[rg * kStateRows + i][4 * cg]) = S[i];
+    }
+
+    const int G = STATE_ONLY ? r.Gb : max(r.Ga, r.Gb);
+    const size_t a_row = (size_t)args.Hkv * r.Ga * D, b_row = (size_t)args.Hkv * r.Gb * D;  // elements per token
+    // 32 x D tile of head `head` from token t0; rows from nv on are zeros
+    auto load_tile = [&](float (*dst)[D + 4], const T* base, size_t row, int head, int t0, int nv) {
+        for (int i = tid; i < kCh * (D / 4); i += kScanThreads) {
+            const int tr = i / (D / 4), q4 = i - tr * (D / 4);
+            const float4 x = tr < nv ? load4(base + ((size_t)bi * args.T + t0 + tr) * row + (size_t)head * D + 4 * q4)
+                                     : make_float4(0.f, 0.f, 0.f, 0.f);
+            *reinterpret_cast<float4*>(&dst[tr][4 * q4]) = x;
+        }
+    };
+
+    float4 acc[kOutRows];
+    for (int n = 0; n < n_chunks; ++n) {
+        const int ch = r.reverse ? n_chunks - 1 - n : n;
+        const int t0 = t_begin + ch * kCh;
+        const int nv = min(kCh, v_end - t0);
+        for (int x = 0; x < G; ++x) {
+            __syncthreads();  // the item before has been read out of the tiles; the state is in place
+            const bool new_b = x == 0 || r.Gb > 1, new_a = x == 0 || r.Ga > 1;
+            if (!STATE_ONLY && new_a) load_tile(sm.a, ga, a_row, h * r.Ga + (r.Ga > 1 ? x : 0), t0, nv);
+            if (new_b) {
+                const int head = h * r.Gb + (r.Gb > 1 ? x : 0);
+                load_tile(sm.b, gb, b_row, head, t0, nv);
+                for (int i = tid; i < kCh * kCG; i += kScanThreads) {
+                    const int tr = i / kCG, q4 = i - tr * kCG;
+                    const float4 v = tr < nv ? load4(gc + ((size_t)bi * args.T + t0 + tr) * b_row + (size_t)head * D + col0 + 4 * q4)
+                                             : make_float4(0.f, 0.f, 0.f, 0.f);
+                    *reinterpret_cast<float4*>(&sm.c[tr][4 * q4]) = v;
+                }
+            }
+            __syncthreads();
+            if (!STATE_ONLY) {
+                {   // products of all pairs: this thread row i, columns j, j + 8, j + 16, j + 24
+                    const int i = tid >> 3, j = tid & 7;
+                    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+                    for (int kk = 0; kk < D; kk += 4) {
+                        const float4 av = *reinterpret_cast<const float4*>(&sm.a[i][kk]);
+#pragma unroll
+                        for (int m = 0; m < 4; ++m)
+                            s[m] = dot4(av, *reinterpret_cast<const float4*>(&sm.b[j + 8 * m][kk]), s[m]);
+                    }
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        const int jj = j + 8 * m;
+                        const int dist = r.reverse ? jj - i : i - jj;
+                        sm.p[i][jj] = dist >= 0 ? s[m] * sm.pw[dist] : 0.f;
+                    }
+                }
+                __syncthreads();
+                // the state's share, once per (chunk, head of a)
+                if (new_a) {
+                    float4 in[kOutRows];
+#pragma unroll
+                    for (int o = 0; o < kOutRows; ++o) in[o] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                    for (int kk = 0; kk < D; kk += 4) {
+                        float4 sv[4];
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) sv[m] = *reinterpret_cast<const float4*>(&sm.s[kk + m][4 * cg]);
+#pragma unroll
+                        for (int o = 0; o < kOutRows; ++o) {
+                            const float4 av = *reinterpret_cast<const float4*>(&sm.a[rg * kOutRows + o][kk]);
+                            in[o] = fma4(av.x, sv[0], fma4(av.y, sv[1], fma4(av.z, sv[2], fma4(av.w, sv[3], in[o]))));
+                        }
+                    }
+#pragma unroll
+                    for (int o = 0; o < kOutRows; ++o) {
+                        const int i = rg * kOutRows + o;
+                        const int e = r.reverse ? max(nv - 1 - i, 0) : i + 1;   // distance to the state's token
+                        acc[o] = mul4(sm.pw[e], in[o]);
+                    }
+                }
+#pragma unroll 4
+                for (int j = 0; j < kCh; ++j) {
+                    const float4 cv = *reinterpret_cast<const float4*>(&sm.c[j][4 * cg]);
+#pragma unroll
+                    for (int o = 0; o < kOutRows; ++o) acc[o] = fma4(sm.p[rg * kOutRows + o][j], cv, acc[o]);
+                }
+                if (r.Ga > 1 || x == G - 1) {
+                    const int head = h * r.Ga + (r.Ga > 1 ? x : 0);
+#pragma unroll
+                    for (int o = 0; o < kOutRows; ++o) {
+                        const int i = rg * kOutRows + o;
+                        if (i < nv)
+                            store4(go + ((size_t)bi * args.T + t0 + i) * a_row + (size_t)head * D + cc, mul4(r.scale, acc[o]));
+                    }
+                }
+            }
+            if (new_b) {
+                if (x == 0) {
+                    const float f = sm.pw[nv];
+#pragma unroll
+                    for (int i = 0; i < kStateRows; ++i) S[i] = mul4(f, S[i]);
+                }
+                for (int j = 0; j < nv; ++j) {
+                    const float w = sm.pw[r.reverse ? j + 1 : nv - 1 - j];
+                    const float4 cv = mul4(w, *reinterpret_cast<const float4*>(&sm.c[j][4 * cg]));
+#pragma unroll
+                    for (int i = 0; i < kStateRows; ++i) S[i] = fma4(sm.b[j][rg * kStateRows + i], cv, S[i]);
+                }
+            }
+            if (!STATE_ONLY && x == G - 1) {
+                __syncthreads();  // the state in shared memory has been read
+#pragma unroll
+                for (int i = 0; i < kStateRows; ++i)
+                    *reinterpret_cast<float4*>(&sm.s[rg * kStateRows + i][4 * cg]) = S[i];
+            }
+        }
+    }
+
+    if (STATE_ONLY) {   // into the slot of the segment that it feeds
+        float* dst = st.seg[which] + ((size_t)u * args.nseg + (r.reverse ? seg - 1 : seg + 1)) * D * D;
+#pragma unroll
+        for (int i = 0; i < kStateRows; ++i)
+            *reinterpret_cast<float4*>(dst + (size_t)(rg * kStateRows + i) * D + cc) = S[i];
+        return;
+    }
+    if (r.state_out != nullptr && seg == (r.reverse ? 0 : args.nseg - 1)) {
+        float* dst = r.state_out + (size_t)u * D * D;
+#pragma unroll
+        for (int i = 0; i < kStateRows; ++i) {
+            const int k = rg * kStateRows + i;
+            const float4 o = mul4(r.out_mul, S[i]);
+            if (!r.state_t) {
+                *reinterpret_cast<float4*>(dst + (size_t)k * D + cc) = o;
+            } else {
+                dst[(size_t)cc * D + k] = o.x;
+                dst[(size_t)(cc + 1) * D + k] = o.y;
+                dst[(size_t)(cc + 2) * D + k] = o.z;
+                dst[(size_t)(cc + 3) * D + k] = o.w;
+            }
+        }
+    }
+    // padding rows of this segment: zeros
+    const int pad0 = max(v_end, t_begin);
+    for (int t = pad0 + rg; t < t_end; t += kRG)
+        for (int x = 0; x < r.Ga; ++x)
+            store4(go + ((size_t)bi * args.T + t) * a_row + (size_t)(h * r.Ga + x) * D + cc, make_float4(0.f, 0.f, 0.f, 0.f));
+}
+
+// The state each segment starts from: slot s holds what the segment before it (in the order of the scan) adds;
+// the running sum decays by that segment's valid tokens.  One thread walks four elements over the segments.
+__global__ void __launch_bounds__(256) linear_combine_kernel(const LinArgs args, const LinStates st, int DD) {
+    const int dir = st.seg[0] == nullptr ? 1 : (int)blockIdx.z;
+    const int u = blockIdx.x;
+    const int e = (blockIdx.y * 256 + threadIdx.x) * 4;
+    if (e >= DD) return;
+    const int bi = u / args.Hkv, h = u - bi * args.Hkv;
+    const int len = args.lens ? min(max(args.lens[bi], 0), args.T) : args.T;
+    const double g = (double)args.log_decay[h];
+    float* base = st.seg[dir] + (size_t)u * args.nseg * DD + e;
+    float4 run = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (st.first[dir] != nullptr) run = mul4(st.in_mul[dir], *reinterpret_cast<const float4*>(st.first[dir] + (size_t)u * DD + e));
+    for (int n = 0; n < args.nseg; ++n) {
+        const int s = dir ? args.nseg - 1 - n : n;
+        float4* slot = reinterpret_cast<float4*>(base + (size_t)s * DD);
+        if (n > 0) {
+            const int prev = dir ? s + 1 : s - 1;
+            const int nv = min(max(len - prev * args.seg_len, 0), args.seg_len);
+            const float f = nv == 0 ? 1.f : (float)exp((double)nv * g);
+            const float4 add = *slot;
+            run = make_float4(fmaf(f, run.x, add.x), fmaf(f, run.y, add.y), fmaf(f, run.z, add.z), fmaf(f, run.w, add.w));
+        }
+        *slot = run;
+    }
+}
+
+// One token for every unit: S' = lambda S + k^T v, o_g = scale q_g S'.  Bound by the state's bytes (read and
+// written once).  A block holds 32 columns of one unit's state (128-byte row pieces): eight lanes per row, so
+// that a thread's rows are all asked for before the first is used, and four blocks share a unit, which fills the
+// machine from about forty units on.
+template <typename T, int D>
+__global__ void __launch_bounds__(128) linear_step_kernel(const T* __restrict__ q, const T* __restrict__ k,
+                                                          const T* __restrict__ v, const float* __restrict__ log_decay,
+                                                          const float* state, float* state_out, T* __restrict__ out,
+                                                          int Hkv, int G, float scale) {
+    constexpr int kRows = D / 16;   // state rows of a thread
+    constexpr int kGq = 8;          // query heads per round
+    __shared__ float sq[kGq][D];
+    __shared__ float sk[D];
+    __shared__ float red[4][kGq][32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int nb = D / 32;
+    const int u = blockIdx.x / nb, col0 = (blockIdx.x - u * nb) * 32;
+    const int h = u % Hkv;
+    const int cg = lane & 7;                     // four columns
+    const int r0 = warp * 4 + (lane >> 3);       // rows r0, r0 + 16, ...
+    const float* src = state + (size_t)u * D * D + col0 + 4 * cg;
+    float4 S[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) S[i] = *reinterpret_cast<const float4*>(src + (size_t)(r0 + 16 * i) * D);
+    const float4 vv = load4(v + (size_t)u * D + col0 + 4 * cg);
+    const float lam = expf(log_decay[h]);
+    for (int i = tid; i < D; i += 128) sk[i] = (float)k[(size_t)u * D + i];
+    for (int g0 = 0; g0 < G; g0 += kGq) {
+        const int ng = min(kGq, G - g0);
+        if (g0 > 0) __syncthreads();
+        for (int i = tid; i < ng * D; i += 128) sq[i / D][i % D] = (float)q[((size_t)u * G + g0) * D + i];
+        __syncthreads();
+        if (g0 == 0) {
+            float* dst = state_out + (size_t)u * D * D + col0 + 4 * cg;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                S[i] = fma4(sk[r0 + 16 * i], vv, mul4(lam, S[i]));
+                *reinterpret_cast<float4*>(dst + (size_t)(r0 + 16 * i) * D) = S[i];
+            }
+        }
+        for (int g = 0; g < ng; ++g) {
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) o = fma4(sq[g][r0 + 16 * i], S[i], o);
+#pragma unroll
+            for (int m = 8; m < 32; m <<= 1) {
+                o.x += __shfl_xor_sync(0xffffffffu, o.x, m);
+                o.y += __shfl_xor_sync(0xffffffffu, o.y, m);
+                o.z += __shfl_xor_sync(0xffffffffu, o.z, m);
+                o.w += __shfl_xor_sync(0xffffffffu, o.w, m);
+            }
+            if (lane < 8) *reinterpret_cast<float4*>(&red[warp][g][4 * lane]) = o;
+        }
+        __syncthreads();
+        for (int i = tid; i < ng * 32; i += 128) {
+            const int g = i >> 5, c = i & 31;
+            const float o = (red[0][g][c] + red[1][g][c]) + (red[2][g][c] + red[3][g][c]);
+            out[((size_t)u * G + g0 + g) * D + col0 + c] = (T)(scale * o);
+        }
+    }
+}
+
+template <typename T, int D, int NC, bool STATE_ONLY>
+cudaError_t launch_scan(const LinArgs& args, const LinStates& st, int grid_y, cudaStream_t stream) {
+    auto fn = linear_scan_kernel<T, D, NC, STATE_ONLY>;
+    const int smem = (int)sizeof(ScanSmem<D, NC>);
+    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)(args.B * args.Hkv * args.nseg * (D / NC)), (unsigned)grid_y);
+    fn<<<grid, kScanThreads, smem, stream>>>(args, st);
+    return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t scan_all(const LinArgs& args, const LinStates& st, cudaStream_t stream) {
+    constexpr int NC = D / 2;
+    if (args.nseg > 1) {
+        const int dirs = (st.seg[0] != nullptr) + (st.seg[1] != nullptr);
+        cudaError_t e = launch_scan<T, D, NC, true>(args, st, dirs, stream);
+        if (e == cudaSuccess) e = launch_linear_combine(D, args, st, stream);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_scan<T, D, NC, false>(args, st, args.n_roles, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_linear_combine(int D, const LinArgs& args, const LinStates& st, cudaStream_t stream) {
+    const int dirs = (st.seg[0] != nullptr) + (st.seg[1] != nullptr);
+    const dim3 grid((unsigned)(args.B * args.Hkv), (unsigned)((D * D / 4 + 255) / 256), (unsigned)dirs);
+    linear_combine_kernel<<<grid, 256, 0, stream>>>(args, st, D * D);
+    return cudaGetLastError();
+}
+
+LinPlan lin_plan(const bct_linear_params_t& p, int64_t T, int kind) {
+    LinPlan plan;
+    plan.tensor = false;
+    const int64_t blocks = (int64_t)p.batch * p.n_kv_heads * 2 * (kind == 1 ? 3 : 1);   // two column halves
+    const int64_t slots = 148 * 2;
+    const int64_t units128 = (T + 127) / 128;   // the token axis in steps of 128
+    // Rounds of blocks times the length of a segment; a split adds the pass over b and c that forms the segments'
+    // states (about half the work of the full one) and two launches (about two steps of 128 tokens).
+    int64_t best = 1;
+    double best_cost = 0;
+    for (int64_t n = 1; n <= units128 && n <= 64; ++n) {
+        const int64_t len = (units128 + n - 1) / n;
+        if ((units128 + len - 1) / len != n) continue;
+        const double rounds = (double)((blocks * n + slots - 1) / slots);
+        const double cost = rounds * (double)len * (n > 1 ? 1.5 : 1.0) + (n > 1 ? 2.0 : 0.0);
+        if (n == 1 || cost < best_cost) {
+            best = n;
+            best_cost = cost;
+        }
+    }
+    const int64_t len = (units128 + best - 1) / best;
+    plan.nseg = (int)best;
+    plan.seg_len = (int)(len * 128);
+    plan.seg_bytes = best > 1 ? (size_t)p.batch * p.n_kv_heads * best * p.head_dim * p.head_dim * sizeof(float) : 0;
+    return plan;
+}
+
+cudaError_t launch_linear_step(const bct_linear_params_t& p, const void* q, const void* k, const void* v,
+                               const float* log_decay, const float* state, float* state_out, void* out,
+                               cudaStream_t stream) {
+    const int G = p.n_q_heads / p.n_kv_heads;
+    const unsigned grid = (unsigned)(p.batch * p.n_kv_heads * (p.head_dim / 32));
+#define BCT_STEP(T, D)                                                                                               \
+    linear_step_kernel<T, D><<<grid, 128, 0, stream>>>(static_cast<const T*>(q), static_cast<const T*>(k),           \
+                                                       static_cast<const T*>(v), log_decay, state, state_out,        \
+                                                       static_cast<T*>(out), p.n_kv_heads, G, p.scale)
+    if (p.dtype == BCT_BF16) {
+        if (p.head_dim == 128)
+            BCT_STEP(__nv_bfloat16, 128);
+        else
+            BCT_STEP(__nv_bfloat16, 64);
+    } else {
+        if (p.head_dim == 128)
+            BCT_STEP(float, 128);
+        else
+            BCT_STEP(float, 64);
+    }
+#undef BCT_STEP
+    return cudaGetLastError();
+}
+
+cudaError_t launch_linear_scan(const bct_linear_params_t& p, const LinPlan& plan, const LinArgs& args,
+                               const LinStates& states, cudaStream_t stream) {
+    (void)plan;
+    if (p.dtype == BCT_BF16)
+        return p.head_dim == 128 ? scan_all<__nv_bfloat16, 128>(args, states, stream)
+                                 : scan_all<__nv_bfloat16, 64>(args, states, stream);
+    return p.head_dim == 128 ? scan_all<float, 128>(args, states, stream) : scan_all<float, 64>(args, states, stream);
+}
+
+}  // namespace bct
