@@ -919,16 +919,14 @@ bool make_plane_map(CUtensorMap* map, void* base, int U, int C) {
 
 // cuTensorMapEncodeTiled through the runtime's driver entry point lookup (no link against libcuda).
 TensorMapEncodeFn tensor_map_encode_fn() {
-    static TensorMapEncodeFn fn = nullptr;
-    static bool tried = false;
-    if (!tried) {
-        tried = true;
+    // (looked up by the first call, whichever thread makes it; the others wait for its answer)
+    static const TensorMapEncodeFn fn = [] {
         void* p = nullptr;
         cudaDriverEntryPointQueryResult qres;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
-            qres == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<TensorMapEncodeFn>(p);
-    }
+        const bool found = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
+                           qres == cudaDriverEntryPointSuccess;
+        return found ? reinterpret_cast<TensorMapEncodeFn>(p) : nullptr;
+    }();
     return fn;
 }
 

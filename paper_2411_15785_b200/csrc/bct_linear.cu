@@ -399,9 +399,10 @@ cudaError_t launch_linear_combine(int D, const LinArgs& args, const LinStates& s
 
 LinPlan lin_plan(const bct_linear_params_t& p, int64_t T, int kind) {
     LinPlan plan;
-    plan.tensor = false;
-    const int64_t blocks = (int64_t)p.batch * p.n_kv_heads * 2 * (kind == 1 ? 3 : 1);   // two column halves
-    const int64_t slots = 148 * 2;
+    plan.tensor = p.dtype == BCT_BF16 && p.head_dim == 128;
+    // blocks of one segment, and blocks the machine holds: on the CUDA cores two column halves, two blocks per SM
+    const int64_t blocks = (int64_t)p.batch * p.n_kv_heads * (kind == 1 ? 3 : 1) * (plan.tensor ? 1 : 2);
+    const int64_t slots = plan.tensor ? 148 : 148 * 2;
     const int64_t units128 = (T + 127) / 128;   // the token axis in steps of 128
     // Rounds of blocks times the length of a segment; a split adds the pass over b and c that forms the segments'
     // states (about half the work of the full one) and two launches (about two steps of 128 tokens).
@@ -450,7 +451,7 @@ cudaError_t launch_linear_step(const bct_linear_params_t& p, const void* q, cons
 
 cudaError_t launch_linear_scan(const bct_linear_params_t& p, const LinPlan& plan, const LinArgs& args,
                                const LinStates& states, cudaStream_t stream) {
-    (void)plan;
+    if (plan.tensor) return launch_linear_tc(args, states, stream);
     if (p.dtype == BCT_BF16)
         return p.head_dim == 128 ? scan_all<__nv_bfloat16, 128>(args, states, stream)
                                  : scan_all<__nv_bfloat16, 64>(args, states, stream);

@@ -1,5 +1,5 @@
 // Host-side internals of the linear-attention calls: the roles of one launch, the segment plan and the
-// launchers (bct_linear.cu: CUDA-core kernels).
+// launchers (bct_linear.cu: CUDA-core kernels, bct_linear_tc.cu: tensor-core kernel).
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -66,6 +66,8 @@ cudaError_t launch_linear_step(const bct_linear_params_t& p, const void* q, cons
 // The whole scan: with more than one segment the segments' own contributions, their running sums, then every role.
 cudaError_t launch_linear_scan(const bct_linear_params_t& p, const LinPlan& plan, const LinArgs& args,
                                const LinStates& states, cudaStream_t stream);
+// The same on the tensor path (bct_linear_tc.cu): bfloat16, head_dim 128.
+cudaError_t launch_linear_tc(const LinArgs& args, const LinStates& states, cudaStream_t stream);
 // Running sums over the segments, in the order of the scan.
 cudaError_t launch_linear_combine(int D, const LinArgs& args, const LinStates& states, cudaStream_t stream);
 
