@@ -7,24 +7,24 @@
 //     O     = A X + P C                             [i][feature of c]
 //     out_i = scale f_i O_i                         f_i = lambda^(distance of i to X's token)
 //     X    <- lambda^n X + (w o B)^T C              w_j = lambda^(distance of j to the new X's token)
-// all as tcgen05.mma with M = N = 128 and fp32 accumulators in tensor memory:
-//  - W's columns are reused for P (a tensor-memory operand) once its rows have been read.
-//  - The state is kept in fp32 in tensor memory, transposed (c's features in the lanes); what a chunk adds is formed
-//    beside it and added in registers, rounded to nearest.  Once per chunk it goes to shared memory in bfloat16, as an
-//    operand.
+// all as tcgen05.mma with M = 128 and fp32 accumulators in tensor memory.  What bounds it is the traffic of shared
+// memory (operands, tiles, results at 128 bytes a clock), so operands are kept in tensor memory where they can be:
+//  - W's columns are reused for P once its rows have been read.
+//  - B^T comes into tensor memory as a product with a 16 x 16 unit matrix, is multiplied with w there and split into two
+//    bfloat16 terms in place: 16 bits, as this library keeps the bounded cache's MV (what a token adds to the state is
+//    off by at most 2^-16 of it).  Weighted in shared memory it took 2300 clocks of traffic a chunk instead of 800.
+//  - The state accumulates in tensor memory, b's features in the lanes.  Once per chunk it is read, written to shared
+//    memory in bfloat16 as the operand X, and scaled.
 //  - f_i multiplies the whole row at the end instead of A's row, so A goes into both products as it is.  It is
 //    floored at 2^-40, which keeps P_ij in range: below that the state's share, as it is and as it is then taken,
 //    is under the rounding of what the row's own token adds.
-//  - w o B is split into two bfloat16 terms, 16 bits, as this library keeps the bounded cache's MV: what a token adds
-//    to the state is off by at most 2^-16 of it.  A third term made it exact to fp32 and cost 8 more products and half
-//    as much splitting again.
-//  - P and the state are each rounded to bfloat16 once where they enter a product with bfloat16 results.
-// Roles (27 warps): warps 0-7 turn W into P, warps 8-15 split w o B into a ring of 16-row steps, warps 16-23 keep the
-// state and write the outputs, over the A tile that has been read; warp 24 loads (TMA), warp 25 issues the products,
-// warp 26 stores (TMA).  The products of a chunk go out as W, A X, w o B C, P C: each waits for something that was
-// started at least one product earlier.  There is room for one tile of B and of C; their next tiles are brought into L2
-// two chunks ahead, so that the reload is short.  With more than one segment, the same kernel without A, W and P
-// forms what every segment adds.  Every wait is bounded; a timeout ends the work and fills the block's outputs with NaN.
+//  - P and X are each rounded to bfloat16 once, where they enter a product with bfloat16 results.
+// Roles (27 warps of 28): warp 0 issues the products, warp 1 loads (TMA), warp 2 stores (TMA); warps 4-11 turn W into P,
+// warps 12-19 weight and split B^T, warps 20-27 keep the state and write the outputs, over the A tile that has been read.
+// The products of a chunk go out as W, A X, w o B C, the next chunk's B^T, P C: each waits for something that was
+// started at least one product earlier.  With more than one
+// segment, the same kernel without A, W and P forms what every segment adds.  Every wait is bounded; a timeout ends the
+// work and fills the block's outputs with NaN.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -36,20 +36,15 @@
 namespace bct {
 namespace {
 
-constexpr int kLtThreads = 864;
+constexpr int kLtThreads = 896;
 constexpr int kLtCh = 128;                    // tokens per chunk
 constexpr int kLtHalf = 128 * 128;            // 64 columns (128 bytes) x 128 rows
 constexpr int kLtTile = 2 * kLtHalf;
-constexpr int kLtStep = 16;                   // rows of w o B per ring slot (one K step)
-constexpr int kLtTerms = 2;
-constexpr int kLtTermBytes = kLtStep * 256;   // two halves of 16 rows x 128 bytes
-constexpr int kLtSlotBytes = kLtTerms * kLtTermBytes;
-constexpr int kLtSlots = 7;
 // tensor-memory columns
 constexpr int kLtColW = 0;     // W, then P (bfloat16 pairs) in the first half of each of its 64-column halves
 constexpr int kLtColO = 128;
-constexpr int kLtColD = 256;   // what the chunk adds to the state, [feature of c][feature of b]
-constexpr int kLtColS = 384;   // the state
+constexpr int kLtColS = 256;   // the state [feature of b][feature of c]
+constexpr int kLtColT = 384;   // B^T [feature of b][j]; of every 16 columns 8 then hold the first terms, 8 the second
 
 struct LtArgs {
     CUtensorMap in[4];    // forward: q, k, v;  backward: d_out, q, k, v
@@ -61,31 +56,44 @@ struct LtArgs {
 };
 
 template <bool STATE_ONLY>
-struct LtSmem {
-    static constexpr int kBc = STATE_ONLY ? 2 : 1;     // buffers of B and of C
+struct LtSmem {   // two buffers of every tile; everything else is kept small enough for that
     static constexpr int b = 0;
-    static constexpr int c = b + kBc * kLtTile;
-    static constexpr int a = c + kBc * kLtTile;        // two buffers
-    static constexpr int x = a + (STATE_ONLY ? 0 : 2 * kLtTile);   // the state as an operand: rows = features of c
-    static constexpr int slots = x + (STATE_ONLY ? 0 : kLtTile);
-    static constexpr int bars = slots + kLtSlots * kLtSlotBytes;
-    static constexpr int pw = bars + 64 * 8;           // lambda^n, n = 0..128
-    static constexpr int pt = pw + 132 * 4;            // [256]: lambda^|j - i| at 127 + j - i, 0 where the mask is
-    // by the token's place in its chunk, for a full chunk and for the one that ends early:
-    static constexpr int pc = pt + 256 * 4;            // [32]: lambda^(31 - j), in reverse lambda^j
-    static constexpr int fo = pc + 32 * 4;           // [2][128] scale f_i
-    static constexpr int fi = fo + 256 * 4;            // [2][128] 1 / f_i
-    static constexpr int wb = fi + 256 * 4;            // [2][128] w_j, 0 behind the last valid token
-    static constexpr int total = wb + 256 * 4 + 1024;  // slack to align the base to 1024 bytes
+    static constexpr int c = b + 2 * kLtTile;
+    static constexpr int a = c + 2 * kLtTile;
+    static constexpr int x = a + (STATE_ONLY ? 0 : 2 * kLtTile);   // the state as an operand: rows = features of b
+    static constexpr int unit = x + (STATE_ONLY ? 0 : kLtTile);    // 16 x 16 unit matrix
+    static constexpr int bars = unit + 512;
+    static constexpr int pt = bars + 32 * 8;           // [256]: lambda^(i - j) at 127 + j - i, reverse lambda^(j - i); else 0
+    static constexpr int total = pt + 256 * 4 + 1024;  // slack to align the base to 1024 bytes
 };
 
-// D (+)= A B with A (bfloat16 pairs) in tensor memory
-__device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, bool accum) {
+// The products are issued by a whole warp, one lane of which is elected at each: descriptors and addresses then stay in
+// uniform registers.  A product of N = 128 takes 64 clocks; issued by one thread among 27 warps (a register move for
+// every word of its descriptors) it took 95 to 170.
+__device__ __forceinline__ void umma_warp(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accum) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accum)
+        : "memory");
+}
+// D (+)= A B with A (bfloat16 pairs) in tensor memory
+__device__ __forceinline__ void umma_warp_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, bool accum) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
         ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"((uint32_t)accum)
+        : "memory");
+}
+__device__ __forceinline__ void umma_commit_warp(uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
         : "memory");
 }
 __device__ __forceinline__ void tmem_st8u(uint32_t taddr, const uint32_t* r) {
@@ -99,34 +107,6 @@ __device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t* r) {
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
-}
-// 16 columns from each of two places, one wait.
-__device__ __forceinline__ void tmem_ld16_two(uint32_t ta, float* x, uint32_t tb, float* y) {
-    uint32_t a[16], b[16];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(a[4]), "=r"(a[5]), "=r"(a[6]), "=r"(a[7]), "=r"(a[8]),
-          "=r"(a[9]), "=r"(a[10]), "=r"(a[11]), "=r"(a[12]), "=r"(a[13]), "=r"(a[14]), "=r"(a[15])
-        : "r"(ta));
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]), "=r"(b[4]), "=r"(b[5]), "=r"(b[6]), "=r"(b[7]), "=r"(b[8]),
-          "=r"(b[9]), "=r"(b[10]), "=r"(b[11]), "=r"(b[12]), "=r"(b[13]), "=r"(b[14]), "=r"(b[15])
-        : "r"(tb));
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(a[0]), "+r"(a[1]), "+r"(a[2]), "+r"(a[3]), "+r"(a[4]), "+r"(a[5]), "+r"(a[6]), "+r"(a[7]),
-                   "+r"(a[8]), "+r"(a[9]), "+r"(a[10]), "+r"(a[11]), "+r"(a[12]), "+r"(a[13]), "+r"(a[14]), "+r"(a[15])
-                 :
-                 : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(b[0]), "+r"(b[1]), "+r"(b[2]), "+r"(b[3]), "+r"(b[4]), "+r"(b[5]), "+r"(b[6]), "+r"(b[7]),
-                   "+r"(b[8]), "+r"(b[9]), "+r"(b[10]), "+r"(b[11]), "+r"(b[12]), "+r"(b[13]), "+r"(b[14]), "+r"(b[15])
-                 :
-                 : "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(a[i]), y[i] = __uint_as_float(b[i]);
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, int x, int y, int z, int w, const void* src) {
@@ -162,12 +142,6 @@ __device__ __forceinline__ void lt_wait(uint64_t* bar, uint32_t parity, volatile
     if (!mbar_try_wait(bar, parity)) lt_wait_slow(bar, parity, abort_flag);
 }
 
-__device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int x, int y, int z, int w) {
-    asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];"
-                 ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(w)
-                 : "memory");
-}
-
 template <bool STATE_ONLY>
 __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_constant__ LtArgs args) {
     using L = LtSmem<STATE_ONLY>;
@@ -181,24 +155,19 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     uint64_t* empty_b = bars + 8;        // [2]
     uint64_t* full_c = bars + 10;        // [2]
     uint64_t* empty_c = bars + 12;       // [2]
-    uint64_t* slot_full = bars + 14;     // [kLtSlots], at most 8
-    uint64_t* slot_empty = bars + 22;    // [kLtSlots]
-    uint64_t* w_full = bars + 30;        // W complete
-    uint64_t* p_full = bars + 31;        // P in place, W read
-    uint64_t* o_full = bars + 33;
-    uint64_t* o_empty = bars + 34;
-    uint64_t* d_full = bars + 35;        // the chunk's addition to the state complete
-    uint64_t* d_empty = bars + 36;
-    uint64_t* x_full = bars + 37;        // the state operand in place
-    uint64_t* x_empty = bars + 38;       // the products with the state operand complete
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 40);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 41);
-    float* pw = reinterpret_cast<float*>(smem + L::pw);
+    uint64_t* clean = bars + 14;         // padding rows of B and C are zeros
+    uint64_t* b_full = bars + 15;        // B^T complete
+    uint64_t* t_full = bars + 16;        // [2] its terms in place, by halves of j
+    uint64_t* w_full = bars + 18;        // W complete
+    uint64_t* p_full = bars + 19;        // P in place
+    uint64_t* o_full = bars + 20;
+    uint64_t* o_empty = bars + 21;
+    uint64_t* s_full = bars + 22;        // the state holds the chunk
+    uint64_t* x_full = bars + 23;        // X in place, the state scaled
+    uint64_t* x_empty = bars + 24;       // the products with X complete
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 26);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 27);
     float* pt = reinterpret_cast<float*>(smem + L::pt);
-    float* pc = reinterpret_cast<float*>(smem + L::pc);
-    float* fo = reinterpret_cast<float*>(smem + L::fo);
-    float* fi = reinterpret_cast<float*>(smem + L::fi);
-    float* wb = reinterpret_cast<float*>(smem + L::wb);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const LinArgs& s = args.s;
@@ -223,54 +192,41 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     auto chunk_t0 = [&](int n) { return t_begin + (reverse ? n_chunks - 1 - n : n) * kLtCh; };
     auto chunk_nv = [&](int t0) { return min(kLtCh, v_end - t0); };
 
+    // The state is read in two rounds by the threads that keep it; here it is asked for into L2.
+    const float* state_src = nullptr;
+    if (!STATE_ONLY) state_src = s.nseg > 1 ? r.seg + ((size_t)u * s.nseg + seg) * 16384 : (r.state_in ? r.state_in + (size_t)u * 16384 : nullptr);
+    if (state_src != nullptr && tid < 512) asm volatile("prefetch.global.L2 [%0];" ::"l"(state_src + tid * 32));
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&full_a[i], 1);
             mbar_init(&empty_a[i], 1);
             mbar_init(&out_full[i], 8);
             mbar_init(&full_b[i], 1);
-            mbar_init(&empty_b[i], STATE_ONLY ? 8 : 9);   // the splitting warps, and the products with B
+            mbar_init(&empty_b[i], 1);
             mbar_init(&full_c[i], 1);
             mbar_init(&empty_c[i], 1);
+            mbar_init(&t_full[i], 4);
         }
-        for (int i = 0; i < kLtSlots; ++i) {
-            mbar_init(&slot_full[i], 4);
-            mbar_init(&slot_empty[i], 1);
-        }
+        mbar_init(clean, 8);
+        mbar_init(b_full, 1);
         mbar_init(w_full, 1);
         mbar_init(p_full, 8);
         mbar_init(o_full, 1);
         mbar_init(o_empty, 8);
-        mbar_init(d_full, 1);
-        mbar_init(d_empty, 8);
+        mbar_init(s_full, 1);
         mbar_init(x_full, 8);
         mbar_init(x_empty, 1);
         *abort_flag = 0;
         fence_mbar_init_cluster();
     }
-    if (warp == 25) tmem_alloc(tmem_slot, 512);
+    if (warp == 0) tmem_alloc(tmem_slot, 512);
     const float log_decay = s.log_decay[h];
-    for (int i = tid; i < 132; i += kLtThreads) {   // the powers in double, rounded once
-        const double g = (double)log_decay;
-        pw[i] = i == 0 ? 1.f : (float)exp(g * i);
-    }
-    for (int i = tid; i < 256; i += kLtThreads) {
-        const int t = i & 127, nv = i < 128 ? 128 : (n_chunks > 0 ? (v_end - t_begin - 1) % kLtCh + 1 : 1);
-        const int to_end = max(nv - 1 - t, 0), from_start = t + 1;
-        const double g = (double)log_decay;
-        const int ef = reverse ? to_end : from_start, ew = reverse ? from_start : to_end;
-        const float f = ef == 0 ? 1.f : fmaxf((float)exp(g * ef), 9.094947017729282e-13f);   // 2^-40
-        if (!STATE_ONLY) {
-            fo[i] = f * r.scale;
-            fi[i] = 1.f / f;
-        }
-        const int dist = reverse ? i - 127 : 127 - i;
-        pt[i] = dist < 0 ? 0.f : (dist == 0 ? 1.f : (float)exp(g * dist));
-        if (i < 32) {
-            const int e = reverse ? i : 31 - i;
-            pc[i] = e == 0 ? 1.f : (float)exp(g * e);
-        }
-        wb[i] = t >= nv ? 0.f : (ew == 0 ? 1.f : (float)exp(g * ew));
+    if (tid < 256) {   // the powers in double, rounded once
+        const int d = reverse ? tid - 127 : 127 - tid;
+        pt[tid] = d < 0 ? 0.f : (d == 0 ? 1.f : (float)exp((double)log_decay * d));
+    } else if (tid < 512) {
+        const int n = (tid - 256) >> 4, k = tid & 15;   // blocks of 8 rows x 16 bytes
+        reinterpret_cast<unsigned short*>(smem + L::unit)[(n >> 3) * 128 + (k >> 3) * 64 + (n & 7) * 8 + (k & 7)] = n == k ? 0x3f80 : 0;
     }
     fence_proxy_async_smem();
     tc_fence_before();
@@ -278,10 +234,24 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
+    // lambda^e, 0 <= e <= 128
+    auto lam = [&](int e) { return reverse ? pt[127 + e] : (e < 128 ? pt[127 - e] : pt[0] * pt[126]); };
+    // f of row i in a chunk of nv valid tokens
+    auto f_of = [&](int i, int nv) { return fmaxf(lam(reverse ? max(nv - 1 - i, 0) : i + 1), 9.094947017729282e-13f); };   // 2^-40
+    const int nv_last = n_chunks > 0 ? (v_end - t_begin - 1) % kLtCh + 1 : kLtCh;   // of the one chunk that may be shorter
 #define LT_WAIT(bar, parity) lt_wait(bar, (parity) & 1, abort_flag);
 
+// for a whole warp that goes on together
+#define LT_WAIT_WARP(bar, parity)    \
+    {                                \
+        LT_WAIT(bar, parity);        \
+        __syncwarp();                \
+    }
+
+    // (Loops are kept short where that costs nothing: 27 warps of six roles share the instruction caches, and straight-line
+    // code that is run once per chunk is fetched anew each time.)
     const int items = n_chunks * G;   // (chunk, head) in turn: head x of the side that has G of them
-    if (warp == 24) {
+    if (warp == 1) {
         // =========================== loads ===========================
         if (lane == 0) {
             auto load = [&](const CUtensorMap* map, int head, int t0, unsigned char* dst, uint64_t* bar) {
@@ -296,123 +266,128 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 load(map_a, h * Ga + (Ga > 1 ? x : 0), chunk_t0(n), smem + L::a + (na & 1) * kLtTile, &full_a[na & 1]);
             };
             auto load_b = [&](int it) {
-                const int n = it / G, x = it - n * G, nb = Gb > 1 ? it : n, st = nb % L::kBc;
+                const int n = it / G, x = it - n * G, nb = Gb > 1 ? it : n, st = nb & 1;
                 if (x > 0 && Gb == 1) return;
-                if (nb >= L::kBc) LT_WAIT(&empty_b[st], nb / L::kBc - 1);
+                if (nb > 1) LT_WAIT(&empty_b[st], (nb >> 1) - 1);
                 load(map_b, h * Gb + (Gb > 1 ? x : 0), chunk_t0(n), smem + L::b + st * kLtTile, &full_b[st]);
             };
             auto load_c = [&](int it) {
-                const int n = it / G, x = it - n * G, nb = Gb > 1 ? it : n, st = nb % L::kBc;
+                const int n = it / G, x = it - n * G, nb = Gb > 1 ? it : n, st = nb & 1;
                 if (x > 0 && Gb == 1) return;
-                if (nb >= L::kBc) LT_WAIT(&empty_c[st], nb / L::kBc - 1);
+                if (nb > 1) LT_WAIT(&empty_c[st], (nb >> 1) - 1);
                 load(map_c, h * Gb + (Gb > 1 ? x : 0), chunk_t0(n), smem + L::c + st * kLtTile, &full_c[st]);
             };
-            auto prefetch = [&](int it) {
-                const int n = it / G, x = it - n * G, t0 = chunk_t0(n);
-                if (!STATE_ONLY && (x == 0 || Ga > 1)) {
-                    tma_prefetch_4d(map_a, 0, h * Ga + (Ga > 1 ? x : 0), t0, bi);
-                    tma_prefetch_4d(map_a, 64, h * Ga + (Ga > 1 ? x : 0), t0, bi);
-                }
-                if (x == 0 || Gb > 1) {
-                    const int head = h * Gb + (Gb > 1 ? x : 0);
-                    tma_prefetch_4d(map_b, 0, head, t0, bi);
-                    tma_prefetch_4d(map_b, 64, head, t0, bi);
-                    tma_prefetch_4d(map_c, 0, head, t0, bi);
-                    tma_prefetch_4d(map_c, 64, head, t0, bi);
-                }
-            };
-            if (items > 0) {
-                load_b(0);
-                load_a(0);
-            }
-            if (items > 1) prefetch(1);
-            for (int it = 0; it < items; ++it) {   // in the order in which the tiles before them are free
+            for (int it = 0; it < items; ++it) {
+                load_b(it);
+                load_a(it);
                 load_c(it);
-                if (it + 2 < items) prefetch(it + 2);
-                if (it + 1 < items) {
-                    load_a(it + 1);
-                    load_b(it + 1);
-                }
             }
         }
         __syncwarp();
-    } else if (warp == 25) {
+    } else if (warp == 0) {
         // =========================== products ===========================
-        if (lane == 0) {
+        {
             constexpr uint32_t id_kk = instr_desc_mn(128, 128, false, false);
             constexpr uint32_t id_kn = instr_desc_mn(128, 128, false, true);
-            constexpr uint32_t id_nn = instr_desc_mn(128, 128, true, true);
-            const DescKind dk(smem_desc(0, 16, 1024)), dmn(smem_desc(0, kLtHalf, 1024)),
-                dslot(smem_desc(0, kLtStep * 128, 1024));
+            constexpr uint32_t id_t = instr_desc_mn(128, 16, true, false);
+            const DescKind dk(smem_desc(0, 16, 1024)), dmn(smem_desc(0, kLtHalf, 1024));
             const uint32_t a16 = desc_addr16(smem_u32(smem + L::a)), b16 = desc_addr16(smem_u32(smem + L::b)),
                            c16 = desc_addr16(smem_u32(smem + L::c)), x16 = desc_addr16(smem_u32(smem + L::x)),
-                           s16 = desc_addr16(smem_u32(smem + L::slots));
+                           u16 = desc_addr16(smem_u32(smem + L::unit));
+            // the unit matrix is not swizzled: blocks of 8 rows x 16 bytes, 128 bytes apart along k, 256 along its rows
+            const uint64_t unit = (smem_desc(0, 128, 256) & ~((uint64_t)7 << 61)) + u16;
             constexpr uint32_t t16 = kLtTile / 16, h16 = kLtHalf / 16;
-            // (Loops here and in the other roles are kept short: 27 warps of six roles share the instruction caches, and
-            // straight-line code that is run once per chunk is fetched anew each time.)
-            auto product_kk = [&](uint32_t d, uint32_t xa, uint32_t ya) {   // D = X Y^T, both with k along their rows
-#pragma unroll 1
-                for (int hf = 0; hf < 2; ++hf, xa += h16, ya += h16) {
+            int n_clean = 0;
+            const int n_short = nv_last == kLtCh ? -1 : (reverse ? 0 : n_chunks - 1);   // the chunk with padding rows
+            // B^T of the nb-th tile of B, which belongs to chunk n
+            auto transpose = [&](int nb, int n) {
+                const int sb = nb & 1;
+                LT_WAIT_WARP(&full_b[sb], nb >> 1);
+                if (n == n_short) LT_WAIT_WARP(clean, n_clean++);
+                tc_fence_after();
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) umma_bf16(d, dk.at(xa + 2 * kk), dk.at(ya + 2 * kk), id_kk, hf > 0 || kk > 0);
+                for (int kk = 0; kk < 8; kk += 2) {
+                    umma_warp(tmem + kLtColT + kk * 16, dmn.at(b16 + sb * t16 + kk * 128), unit, id_t, false);
+                    umma_warp(tmem + kLtColT + kk * 16 + 16, dmn.at(b16 + sb * t16 + kk * 128 + 128), unit, id_t, false);
                 }
+                umma_commit_warp(b_full);
+                if (STATE_ONLY) umma_commit_warp(&empty_b[sb]);
             };
-            int sl = 0;          // ring slot and the parity of its turn
-            uint32_t turn = 0;
+            if (items > 0) transpose(0, 0);
+            int n = 0, x = 0;
             for (int it = 0; it < items; ++it) {
-                const int n = it / G, x = it - n * G;
-                const int na = Ga > 1 ? it : n, nb = Gb > 1 ? it : n, sb = nb % L::kBc;
+                const int na = Ga > 1 ? it : n, nb = Gb > 1 ? it : n, sb = nb & 1;
                 const bool new_b = x == 0 || Gb > 1, new_a = x == 0 || Ga > 1, last = x == G - 1;
-                const uint32_t aa = a16 + (na & 1) * t16, ba = b16 + sb * t16, ca = c16 + sb * t16;
+                const uint32_t aa = a16 + (na & 1) * t16, ca = c16 + (nb & 1) * t16;
                 if (!STATE_ONLY) {
-                    LT_WAIT(&full_a[na & 1], na >> 1);
-                    LT_WAIT(&full_b[sb], nb / L::kBc);
+                    LT_WAIT_WARP(&full_a[na & 1], na >> 1);
+                    LT_WAIT_WARP(&full_b[sb], nb >> 1);
                     tc_fence_after();
-                    product_kk(tmem + kLtColW, aa, ba);
-                    umma_commit(w_full);
-                    if (Gb > 1 || last) umma_commit(&empty_b[sb]);
-                    if (new_a) {   // the state's share
-                        if (x == 0) LT_WAIT(x_full, n);
-                        if (na > 0) LT_WAIT(o_empty, na - 1);
-                        tc_fence_after();
-                        product_kk(tmem + kLtColO, aa, x16);
-                        if (Gb > 1 || last) umma_commit(x_empty);
-                    }
-                }
-                if (new_b) {   // the chunk's addition to the state
-                    if (x == 0 && n > 0) LT_WAIT(d_empty, n - 1);
-                    LT_WAIT(&full_c[sb], nb / L::kBc);
-#pragma unroll 1
-                    for (int st = 0; st < kLtCh / kLtStep; ++st) {
-                        LT_WAIT(&slot_full[sl], turn);
-                        tc_fence_after();
-                        const uint64_t cd = dmn.at(ca + st * 128);
-                        const uint32_t sa = s16 + sl * (kLtSlotBytes / 16);
+                    uint32_t xa = aa, ya = b16 + sb * t16;
 #pragma unroll
-                        for (int t = 0; t < kLtTerms; ++t)
-                            umma_bf16(tmem + kLtColD, cd, dslot.at(sa + t * (kLtTermBytes / 16)), id_nn, t > 0 || st > 0 || x > 0);
-                        umma_commit(&slot_empty[sl]);
-                        if (++sl == kLtSlots) sl = 0, turn ^= 1;
+                    for (int hf = 0; hf < 2; ++hf, xa += h16, ya += h16) {
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            umma_warp(tmem + kLtColW, dk.at(xa + 2 * kk), dk.at(ya + 2 * kk), id_kk, hf > 0 || kk > 0);
                     }
-                    if (Gb == 1 || last) umma_commit(d_full);
-                    if (STATE_ONLY) umma_commit(&empty_c[sb]);
+                    umma_commit_warp(w_full);
+                    if (Gb > 1 || last) umma_commit_warp(&empty_b[sb]);
+                }
+                if (x == 0) LT_WAIT_WARP(x_full, n);
+                if (!STATE_ONLY && new_a) {   // the state's share
+                    if (na > 0) LT_WAIT_WARP(o_empty, na - 1);
+                    tc_fence_after();
+                    uint32_t xa = aa;
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf, xa += h16) {
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            umma_warp(tmem + kLtColO, dk.at(xa + 2 * kk), dmn.at(x16 + hf * 512 + kk * 128), id_kn, hf > 0 || kk > 0);
+                    }
+                    if (Gb > 1 || last) umma_commit_warp(x_empty);
+                }
+                // the next tile of B comes with the next item, or with the first one of the next chunk
+                bool next = (Gb > 1 || last) && it + 1 < items;
+                const int nb1 = nb + 1, n1 = last ? n + 1 : n;
+                if (new_b) {   // the chunk's share of the state
+                    LT_WAIT_WARP(&full_c[nb & 1], nb >> 1);
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        LT_WAIT_WARP(&t_full[hf], nb);
+                        tc_fence_after();
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) {
+                            const uint64_t cd = dmn.at(ca + hf * 512 + kk * 128);
+                            umma_warp_ts(tmem + kLtColS, tmem + kLtColT + hf * 64 + kk * 16, cd, id_kn, true);
+                            umma_warp_ts(tmem + kLtColS, tmem + kLtColT + hf * 64 + kk * 16 + 8, cd, id_kn, true);
+                        }
+                    }
+                    if (Gb == 1 || last) umma_commit_warp(s_full);
+                    if (STATE_ONLY) umma_commit_warp(&empty_c[nb & 1]);
+                }
+                // the next tile's transposition before this item's last product, if the tile is there
+                if (next && (STATE_ONLY || __all_sync(0xffffffffu, mbar_try_wait(&full_b[nb1 & 1], (nb1 >> 1) & 1)))) {
+                    transpose(nb1, n1);
+                    next = false;
                 }
                 if (!STATE_ONLY) {
-                    LT_WAIT(p_full, it);
+                    LT_WAIT_WARP(p_full, it);
                     tc_fence_after();
-#pragma unroll 1
+#pragma unroll
                     for (int hf = 0; hf < 2; ++hf) {
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk)
-                            umma_bf16_ts(tmem + kLtColO, tmem + kLtColW + hf * 64 + kk * 8, dmn.at(ca + hf * 512 + kk * 128), id_kn, true);
+                            umma_warp_ts(tmem + kLtColO, tmem + kLtColW + hf * 64 + kk * 8, dmn.at(ca + hf * 512 + kk * 128), id_kn, true);
                     }
-                    if (Ga > 1 || last) umma_commit(o_full);
-                    if (Gb > 1 || last) umma_commit(&empty_c[sb]);
+                    if (Ga > 1 || last) umma_commit_warp(o_full);
+                    if (Gb > 1 || last) umma_commit_warp(&empty_c[nb & 1]);
                 }
+                if (next) transpose(nb1, n1);
+                if (++x == G) x = 0, ++n;
             }
         }
         __syncwarp();
-    } else if (warp == 26) {
+    } else if (warp == 2) {
         // =========================== stores ===========================
         if (!STATE_ONLY && lane == 0) {
             const CUtensorMap* map_o = &args.out[which];
@@ -432,16 +407,18 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             bulk_wait_all();
         }
         __syncwarp();
-    } else if (warp < 8) {
+    } else if (warp == 3) {   // (fills the first group of four)
+    } else if (warp < 12) {
         // =========================== W -> P: two threads per row i, 64 columns each ===========
         if (!STATE_ONLY) {
-            const int q = warp & 3, half = warp >> 2, i = q * 32 + lane;
+            const int q = warp & 3, half = (warp - 4) >> 2, i = q * 32 + lane;
             const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + kLtColW + half * 64;
             const float* pti = pt + 127 - i;
+            const float inv_full = 1.f / f_of(i, kLtCh), inv_last = 1.f / f_of(i, nv_last);
             int it = 0;
             for (int n = 0; n < n_chunks; ++n) {
                 const int nv = chunk_nv(chunk_t0(n));
-                const float inv_f = fi[(nv < kLtCh ? 128 : 0) + i];
+                const float inv_f = nv < kLtCh ? inv_last : inv_full;
                 for (int x = 0; x < G; ++x, ++it) {
                     LT_WAIT(w_full, it);
                     tc_fence_after();
@@ -461,10 +438,10 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                                     v[j] = w > 0.f ? v[j] * (w * inv_f) : 0.f;
                                 }
                             } else {         // a power for the row and the block, one for the column
-                                const float wr = pw[reverse ? cb * 32 - i : i - cb * 32 - 31] * inv_f;
+                                const float wr = lam(reverse ? cb * 32 - i - 1 : i - cb * 32 - 31) * inv_f;
 #pragma unroll
                                 for (int j = 0; j < 16; j += 4) {
-                                    const float4 wc = *reinterpret_cast<const float4*>(pc + (e & 1) * 16 + j);
+                                    const float4 wc = *reinterpret_cast<const float4*>(pt + (reverse ? 128 : 96) + (e & 1) * 16 + j);
                                     const float2 y = __fmul2_rn(__fmul2_rn(make_float2(v[j], v[j + 1]), make_float2(wc.x, wc.y)),
                                                                 make_float2(wr, wr));
                                     const float2 z = __fmul2_rn(__fmul2_rn(make_float2(v[j + 2], v[j + 3]), make_float2(wc.z, wc.w)),
@@ -489,148 +466,137 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 }
             }
         }
-    } else if (warp < 16) {
-        // =========================== w o B in three terms, 16 rows at a time ===========================
-        const int group = (warp - 8) >> 2, wt = tid & 127;   // two groups of four warps: even and odd steps
-        const int row = wt >> 3, c8 = wt & 7;
-        const int place = row * 128 + ((c8 ^ (row & 7)) * 16);
+    } else if (warp < 20) {
+        // =========================== w o B^T in two terms: two threads per feature of b, 64 tokens each ===========
+        const int q = warp & 3, half = (warp - 12) >> 2, wt = tid & 127;
+        const uint32_t t_col = tmem + ((uint32_t)(q * 32) << 16) + kLtColT + half * 64;
         int nb = 0;
         for (int n = 0; n < n_chunks; ++n) {
             const int nv = chunk_nv(chunk_t0(n));
+            const float* w = pt + (reverse ? 128 : kLtCh - nv) + half * 64;   // w_j = w[j], 0 behind the last valid token
+            const bool aligned = reverse || (nv & 3) == 0;
             for (int x = 0; x < Gb; ++x, ++nb) {
-                const int st = nb % L::kBc, use = nb / L::kBc;
-                const unsigned char* bt = smem + L::b + st * kLtTile;
-                LT_WAIT(&full_b[st], use);
-                if (nv < kLtCh && group == 0) {   // padding rows of C hold anything: zero, before the first product reads them
-                    LT_WAIT(&full_c[st], use);
+                if (nv < kLtCh) {   // padding rows hold anything: zeros in B (this half of the warps) and in C (the other)
+                    LT_WAIT(&full_b[(nb & 1)], (nb >> 1));
+                    LT_WAIT(&full_c[nb & 1], nb >> 1);
                     if (wt >= nv) {
-                        uint4* z = reinterpret_cast<uint4*>(smem + L::c + st * kLtTile + wt * 128);
+                        uint4* z = reinterpret_cast<uint4*>(smem + (half ? L::c + (nb & 1) * kLtTile : L::b + (nb & 1) * kLtTile) + wt * 128);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             z[j] = make_uint4(0, 0, 0, 0);
                             z[j + kLtHalf / 16] = make_uint4(0, 0, 0, 0);
                         }
                     }
-                }
-#pragma unroll 1
-                for (int t = group; t < kLtCh / kLtStep; t += 2) {
-                    const int ks = nb * (kLtCh / kLtStep) + t, sl = ks % kLtSlots;
-                    const int j = t * kLtStep + row;
-                    const float w = wb[(nv < kLtCh ? 128 : 0) + j];
-                    if (ks >= kLtSlots) LT_WAIT(&slot_empty[sl], ks / kLtSlots - 1);
-                    const unsigned char* src = bt + t * kLtStep * 128 + place;
-                    unsigned char* dst = smem + L::slots + sl * kLtSlotBytes + place;
-#pragma unroll 1
-                    for (int hf = 0; hf < 2; ++hf, src += kLtHalf, dst += kLtStep * 128) {
-                        uint4 raw = *reinterpret_cast<const uint4*>(src);
-                        if (j >= nv) raw = make_uint4(0, 0, 0, 0);   // (padding may hold NaN)
-                        const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
-                        uint32_t o[kLtTerms][4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float2 v = __fmul2_rn(make_float2(__uint_as_float(rw[e] << 16), __uint_as_float(rw[e] & 0xffff0000u)),
-                                                  make_float2(w, w));
-#pragma unroll
-                            for (int tm = 0; tm < kLtTerms; ++tm) {
-                                const uint32_t pk = Chunk<__nv_bfloat16>::pack2(v.x, v.y);
-                                o[tm][e] = pk;
-                                if (tm + 1 < kLtTerms)   // what the term leaves out, exactly
-                                    v = __fadd2_rn(v, make_float2(-__uint_as_float(pk << 16), -__uint_as_float(pk & 0xffff0000u)));
-                            }
-                        }
-#pragma unroll
-                        for (int tm = 0; tm < kLtTerms; ++tm)
-                            *reinterpret_cast<uint4*>(dst + tm * kLtTermBytes) = make_uint4(o[tm][0], o[tm][1], o[tm][2], o[tm][3]);
-                    }
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(&slot_full[sl]);
-                        if (t >= kLtCh / kLtStep - 2) mbar_arrive(&empty_b[st]);   // this group has read its rows of B
-                    }
+                    if (lane == 0) mbar_arrive(clean);
                 }
+                LT_WAIT(b_full, nb);
+                tc_fence_after();
+#pragma unroll 1
+                for (int e = 0; e < 4; ++e) {
+                    float v[16];
+                    tmem_ld16(t_col + e * 16, v);
+                    uint32_t o[16];
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4) {
+                        const float* wp = w + e * 16 + j;
+                        const float4 wj = aligned ? *reinterpret_cast<const float4*>(wp) : make_float4(wp[0], wp[1], wp[2], wp[3]);
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float2 y = __fmul2_rn(make_float2(v[j + 2 * k], v[j + 2 * k + 1]),
+                                                        k ? make_float2(wj.z, wj.w) : make_float2(wj.x, wj.y));
+                            const uint32_t hi = Chunk<__nv_bfloat16>::pack2(y.x, y.y);
+                            // what the first term leaves out, exactly
+                            const float2 z = __fadd2_rn(y, make_float2(-__uint_as_float(hi << 16), -__uint_as_float(hi & 0xffff0000u)));
+                            o[(j >> 1) + k] = hi;
+                            o[8 + (j >> 1) + k] = Chunk<__nv_bfloat16>::pack2(z.x, z.y);
+                        }
+                    }
+                    tmem_st16u(t_col + e * 16, o);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&t_full[half]);
             }
         }
     } else {
         // =========================== the state and the outputs ===========================
-        const int q = warp & 3, hs = (warp - 16) >> 2;   // lanes 32q.., columns 64 hs..
-        const int c = q * 32 + lane;                      // this thread's feature of c; of the outputs, its row
+        const int q = warp & 3, hs = (warp - 20) >> 2;   // lanes 32q.., columns 64 hs..
+        const int c = q * 32 + lane;                      // this thread's feature of b; of the outputs, its row
         const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
-        const uint32_t s_col = lane_base + kLtColS + hs * 64, d_col = lane_base + kLtColD + hs * 64;
+        const uint32_t s_col = lane_base + kLtColS + hs * 64;
         {
-            const bool from_seg = !STATE_ONLY && s.nseg > 1;
-            const float* src = STATE_ONLY ? nullptr
-                               : from_seg ? r.seg + ((size_t)u * s.nseg + seg) * 16384
-                                          : (r.state_in ? r.state_in + (size_t)u * 16384 : nullptr);
-            const float mul = from_seg || STATE_ONLY ? 1.f : r.in_mul;
+            const float* src = state_src;
+            const float mul = STATE_ONLY || s.nseg > 1 ? 1.f : r.in_mul;
 #pragma unroll 1
-            for (int k = 0; k < 4; ++k) {
-                float v[16];
+            for (int k = 0; k < 2; ++k) {
+                float v[32];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = 0.f;
+                for (int i = 0; i < 32; ++i) v[i] = 0.f;
                 if (src != nullptr) {
-                    if (!r.state_t) {
+                    if (r.state_t) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) v[i] = mul * src[(hs * 64 + k * 16 + i) * 128 + c];
+                        for (int i = 0; i < 32; ++i) v[i] = src[(hs * 64 + k * 32 + i) * 128 + c];
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float4 x = *reinterpret_cast<const float4*>(src + c * 128 + hs * 64 + k * 16 + 4 * i);
-                            v[4 * i] = mul * x.x, v[4 * i + 1] = mul * x.y, v[4 * i + 2] = mul * x.z, v[4 * i + 3] = mul * x.w;
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 x = *reinterpret_cast<const float4*>(src + c * 128 + hs * 64 + k * 32 + 4 * i);
+                            v[4 * i] = x.x, v[4 * i + 1] = x.y, v[4 * i + 2] = x.z, v[4 * i + 3] = x.w;
                         }
                     }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] *= mul;
                 }
-                tmem_st16u(s_col + k * 16, reinterpret_cast<const uint32_t*>(v));
+                tmem_st16u(s_col + k * 32, reinterpret_cast<const uint32_t*>(v));
+                tmem_st16u(s_col + k * 32 + 16, reinterpret_cast<const uint32_t*>(v + 16));
             }
             tmem_wait_st();
         }
         unsigned char* x_row = smem + L::x + hs * kLtHalf + c * 128;
-        // Before chunk n: take in what chunk n - 1 adds, and write the operand for chunk n's products.
+        // Before chunk n: the state as chunk n's operand, and scaled for what chunk n adds.
         auto turn = [&](int n) {
-            const bool add = n > 0, put = !STATE_ONLY && n < n_chunks;
-            const float f = add ? pw[chunk_nv(chunk_t0(n - 1))] : 1.f;
-            if (add) {
-                LT_WAIT(d_full, n - 1);
-                if (put) LT_WAIT(x_empty, n - 1);
+            const float f = lam(chunk_nv(chunk_t0(n)));
+            if (n > 0) {
+                LT_WAIT(s_full, n - 1);
+                if (!STATE_ONLY) LT_WAIT(x_empty, n - 1);
                 tc_fence_after();
             }
 #pragma unroll 1
             for (int k = 0; k < 4; ++k) {
-                float x[16], d[16];
-                tmem_ld16_two(s_col + k * 16, x, d_col + k * 16, d);
-                if (add) {
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float2 y = __ffma2_rn(make_float2(x[i], x[i + 1]), make_float2(f, f), make_float2(d[i], d[i + 1]));
-                        x[i] = y.x, x[i + 1] = y.y;
-                    }
-                    tmem_st16u(s_col + k * 16, reinterpret_cast<const uint32_t*>(x));
-                }
-                if (put) {
+                float x[16];
+                tmem_ld16(s_col + k * 16, x);
+                if (!STATE_ONLY) {
                     *reinterpret_cast<uint4*>(x_row + (((2 * k) ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(x);
                     *reinterpret_cast<uint4*>(x_row + (((2 * k + 1) ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(x + 8);
                 }
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float2 y = __fmul2_rn(make_float2(x[i], x[i + 1]), make_float2(f, f));
+                    x[i] = y.x, x[i + 1] = y.y;
+                }
+                tmem_st16u(s_col + k * 16, reinterpret_cast<const uint32_t*>(x));
             }
             tmem_wait_st();
-            if (put) fence_proxy_async_smem();
+            if (!STATE_ONLY) fence_proxy_async_smem();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) {
-                if (add) mbar_arrive(d_empty);
-                if (put) mbar_arrive(x_full);
-            }
+            if (lane == 0) mbar_arrive(x_full);
         };
+        const float f_full = STATE_ONLY ? 0.f : f_of(c, kLtCh) * r.scale, f_last = STATE_ONLY ? 0.f : f_of(c, nv_last) * r.scale;
         int na = 0;
         if (n_chunks > 0) turn(0);
         for (int n = 0; n < n_chunks; ++n) {
             if (STATE_ONLY) {
-                turn(n + 1);
+                if (n + 1 < n_chunks) turn(n + 1);
                 continue;
             }
             const int nv = chunk_nv(chunk_t0(n));
-            const float f = fo[(nv < kLtCh ? 128 : 0) + c];
+            const float f = nv < kLtCh ? f_last : f_full;
             for (int x = 0; x < Ga; ++x, ++na) {
-                if (x == Ga - 1) turn(n + 1);   // complete before the chunk's last output, and the next chunk's products wait for it
+                // (the state is complete before the chunk's last output, and the next chunk's products wait for it)
+                if (x == Ga - 1 && n + 1 < n_chunks) turn(n + 1);
                 LT_WAIT(o_full, na);
                 tc_fence_after();
                 unsigned char* dst = smem + L::a + (na & 1) * kLtTile + hs * kLtHalf + c * 128;
@@ -653,6 +619,10 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 if (lane == 0) mbar_arrive(&out_full[na & 1]);
             }
         }
+        if (n_chunks > 0) {
+            LT_WAIT(s_full, n_chunks - 1);
+            tc_fence_after();
+        }
         const float poison = *abort_flag ? __int_as_float(0x7fc00000) : 0.f;
         float* dst = nullptr;
         float mul = 1.f;
@@ -668,14 +638,17 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 float x[16];
                 tmem_ld16(s_col + k * 16, x);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) dst[(hs * 64 + k * 16 + i) * 128 + c] = x[i] * mul + poison;
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<float4*>(dst + c * 128 + hs * 64 + k * 16 + i) =
+                        make_float4(x[i] * mul + poison, x[i + 1] * mul + poison, x[i + 2] * mul + poison, x[i + 3] * mul + poison);
             }
         }
     }
 #undef LT_WAIT
+#undef LT_WAIT_WARP
     tc_fence_before();
     __syncthreads();
-    if (warp == 25) {
+    if (warp == 0) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
