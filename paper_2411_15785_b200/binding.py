@@ -7,6 +7,7 @@ There is no CPU fallback: ``load()`` raises when the library has not been built.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Tuple
 
@@ -202,41 +203,72 @@ def stack_forward(caches, x, w_q, w_wq, w_wv, out=None, scratch=None, stream=Non
     return out
 
 
-def _operand(name, t, shape, dtype, device) -> None:
-    """The library sees pointers only: shape, type, place and layout are checked here."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s (got %s, %s, %s%s)" % (
-            name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", strided"))
+def _operand(name, t, shape, dtype, dev) -> None:
+    """The library sees pointers only: shape, type, place (device index) and layout are checked here."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or dev < 0 or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on CUDA device %s (got %s, %s, %s%s)" % (
+            name, dtype, tuple(shape), dev if dev >= 0 else "0 or above", t.dtype, tuple(t.shape), t.device,
+            "" if t.is_contiguous() else ", strided"))
 
 
 def _io_dtype(name, t) -> int:
-    if t.dtype not in (torch.float32, torch.bfloat16):
+    if t.dtype is torch.bfloat16:
+        return BCT_BF16
+    if t.dtype is not torch.float32:
         raise ValueError("%s must be float32 or bfloat16 (got %s)" % (name, t.dtype))
-    return BCT_BF16 if t.dtype == torch.bfloat16 else BCT_F32
+    return BCT_F32
 
 
-def _result(name, t, shape, dtype, device):
-    """The caller's buffer, checked, or a new one."""
+def _result(name, t, like, shape, dtype, dev):
+    """The caller's buffer, checked, or a new one on the device of `like`."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    _operand(name, t, shape, dtype, device)
+        if like.dtype is dtype and like.shape == shape:
+            return torch.empty_like(like)
+        return like.new_empty(shape, dtype=dtype)
+    _operand(name, t, shape, dtype, dev)
     return t
 
 
-def _launch(device, stream, call, *args) -> None:
+def _raw_stream(dev: int) -> int:
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+# the same without building a Stream object (3 us of a call that takes 10), where this torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
+
+
+def _launch(dev, stream, call, *args) -> None:
     """The call on the tensors' device: on `stream`, or on that device's current stream."""
-    if device.index == torch.cuda.current_device():
-        _check(call(*args, _stream_ptr(stream)))
-        return
-    with torch.cuda.device(device):
-        _check(call(*args, _stream_ptr(stream)))
+    raw = _raw_stream(dev) if stream is None else stream.cuda_stream
+    if dev == torch.cuda.current_device():
+        st = call(*args, raw)
+    else:
+        with torch.cuda.device(dev):
+            st = call(*args, raw)
+    if st != BCT_OK:
+        _check(st)
 
 
-def _scratch(need: int, scratch, device):
+@functools.lru_cache(maxsize=256)
+def _linear_params(batch, n_q_heads, n_kv_heads, head_dim, dtype, scale):
+    """The parameter block of a call's sizes (never written to) and a reference to hand it over by."""
+    p = BctLinearParams(batch, n_q_heads, n_kv_heads, head_dim, dtype, scale)
+    return p, ctypes.byref(p)
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_scratch(batch, n_q_heads, n_kv_heads, head_dim, dtype, T, backward) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().bct_linear_scratch_bytes(_linear_params(batch, n_q_heads, n_kv_heads, head_dim, dtype, 0.0)[1], T,
+                                           backward, ctypes.byref(n)))
+    return n.value
+
+
+def _scratch(need: int, scratch, like, dev):
     if scratch is None:
-        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    if not scratch.is_cuda or scratch.device != device or not scratch.is_contiguous():
-        raise ValueError("scratch must be a contiguous tensor on %s" % device)
+        return like.new_empty(need, dtype=torch.uint8) if need else None
+    if scratch.get_device() != dev or not scratch.is_contiguous():
+        raise ValueError("scratch must be a contiguous tensor on CUDA device %d" % dev)
     return scratch
 
 
@@ -244,25 +276,24 @@ def _scratch_args(scratch):
     return (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())
 
 
-def _linear_setup(q, k, v, log_decay, lead, scale):
-    """Checks the operands that every linear-attention call has; q ``[*lead, Hq, d]``, k and v ``[*lead, Hkv, d]``."""
-    if q.dim() != len(lead) + 2 or k.dim() != len(lead) + 2:
-        raise ValueError("q and k must have %d dimensions" % (len(lead) + 2))
-    Hq, Hkv, d = q.shape[-2], k.shape[-2], q.shape[-1]
-    dt = _io_dtype("q", q)
-    _operand("q", q, (*lead, Hq, d), q.dtype, q.device)
-    _operand("k", k, (*lead, Hkv, d), q.dtype, q.device)
-    _operand("v", v, (*lead, Hkv, d), q.dtype, q.device)
-    _operand("log_decay", log_decay, (Hkv,), torch.float32, q.device)
-    return BctLinearParams(lead[0], Hq, Hkv, d, dt, scale), (lead[0], Hkv, d, d)
+def _linear_setup(q, k, v, log_decay, n_lead, scale):
+    """Checks the operands that every linear-attention call has: q ``[*lead, Hq, d]``, k and v ``[*lead, Hkv, d]``.
+    Returns the sizes, the parameters by reference, the state's shape and the device index."""
+    if q.dim() != n_lead + 2 or k.dim() != n_lead + 2:
+        raise ValueError("q and k must have %d dimensions" % (n_lead + 2))
+    dt, dev, sq, sk = _io_dtype("q", q), q.get_device(), q.shape, k.shape
+    want = (*sq[:-2], sk[-2], sq[-1])
+    _operand("q", q, sq, q.dtype, dev)
+    _operand("k", k, want, q.dtype, dev)
+    _operand("v", v, want, q.dtype, dev)
+    _operand("log_decay", log_decay, (sk[-2],), torch.float32, dev)
+    sizes = (sq[0], sq[-2], sk[-2], sq[-1], dt)
+    return sizes, _linear_params(*sizes, scale)[1], (sq[0], sk[-2], sq[-1], sq[-1]), dev
 
 
 def linear_scratch_bytes(batch, T, n_q_heads, n_kv_heads, head_dim, dtype, *, backward=False) -> int:
     """Scratch that linear_forward (or linear_backward) needs for these sizes."""
-    n = ctypes.c_size_t(0)
-    p = BctLinearParams(batch, n_q_heads, n_kv_heads, head_dim, _dtype_code(dtype), 0.0)
-    _check(load().bct_linear_scratch_bytes(ctypes.byref(p), T, int(backward), ctypes.byref(n)))
-    return n.value
+    return _linear_scratch(batch, n_q_heads, n_kv_heads, head_dim, _dtype_code(dtype), T, int(backward))
 
 
 def linear_step(q, k, v, log_decay, state, scale=0.0, out=None, state_out=None, stream=None):
@@ -270,11 +301,14 @@ def linear_step(q, k, v, log_decay, state, scale=0.0, out=None, state_out=None, 
     ``out = scale q S'``.  q ``[B, Hq, d]``, k, v ``[B, Hkv, d]``, state ``[B, Hkv, d, d]`` float32.  state_out: where
     S' goes; None updates `state` in place.  Returns (out, state after)."""
     lib = load()
-    p, s_shape = _linear_setup(q, k, v, log_decay, q.shape[:1], scale)
-    _operand("state", state, s_shape, torch.float32, q.device)
-    out = _result("out", out, q.shape, q.dtype, q.device)
-    state_out = state if state_out is None else _result("state_out", state_out, s_shape, torch.float32, q.device)
-    _launch(q.device, stream, lib.bct_linear_step, ctypes.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    _, p, s_shape, dev = _linear_setup(q, k, v, log_decay, 1, scale)
+    _operand("state", state, s_shape, torch.float32, dev)
+    out = _result("out", out, q, q.shape, q.dtype, dev)
+    if state_out is None:
+        state_out = state
+    else:
+        _operand("state_out", state_out, s_shape, torch.float32, dev)
+    _launch(dev, stream, lib.bct_linear_step, p, q.data_ptr(), k.data_ptr(), v.data_ptr(),
             log_decay.data_ptr(), state.data_ptr(), state_out.data_ptr(), out.data_ptr())
     return out, state_out
 
@@ -285,18 +319,16 @@ def linear_forward(q, k, v, log_decay, state=None, lens=None, scale=0.0, out=Non
     (zeros); lens int32 ``[B]`` or None: the valid tokens of each sequence of a padded batch.  Returns (out
     ``[B, T, Hq, d]``, state after each sequence's last token); state_out may be `state`."""
     lib = load()
-    p, s_shape = _linear_setup(q, k, v, log_decay, q.shape[:2], scale)
-    dev, T = q.device, q.shape[1]
+    sizes, p, s_shape, dev = _linear_setup(q, k, v, log_decay, 2, scale)
+    T = q.shape[1]
     if state is not None:
         _operand("state", state, s_shape, torch.float32, dev)
     if lens is not None:
         _operand("lens", lens, q.shape[:1], torch.int32, dev)
-    out = _result("out", out, q.shape, q.dtype, dev)
-    state_out = _result("state_out", state_out, s_shape, torch.float32, dev)
-    need = ctypes.c_size_t(0)
-    _check(lib.bct_linear_scratch_bytes(ctypes.byref(p), T, 0, ctypes.byref(need)))
-    scratch = _scratch(need.value, scratch, dev)
-    _launch(dev, stream, lib.bct_linear_forward, ctypes.byref(p), T, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    out = _result("out", out, q, q.shape, q.dtype, dev)
+    state_out = _result("state_out", state_out, q, s_shape, torch.float32, dev)
+    scratch = _scratch(_linear_scratch(*sizes, T, 0), scratch, q, dev)
+    _launch(dev, stream, lib.bct_linear_forward, p, T, q.data_ptr(), k.data_ptr(), v.data_ptr(),
             log_decay.data_ptr(), _ptr(lens), _ptr(state), state_out.data_ptr(), out.data_ptr(), *_scratch_args(scratch))
     return out, state_out
 
@@ -307,8 +339,8 @@ def linear_backward(d_out, q, k, v, log_decay, state=None, d_state=None, lens=No
     state after the last token, or None) -> (d_q, d_k, d_v in q's dtype, d_state_in float32).  out: that tuple, to
     write into."""
     lib = load()
-    p, s_shape = _linear_setup(q, k, v, log_decay, q.shape[:2], scale)
-    dev, T = q.device, q.shape[1]
+    sizes, p, s_shape, dev = _linear_setup(q, k, v, log_decay, 2, scale)
+    T = q.shape[1]
     _operand("d_out", d_out, q.shape, q.dtype, dev)
     for name, t in (("state", state), ("d_state", d_state)):
         if t is not None:
@@ -316,14 +348,12 @@ def linear_backward(d_out, q, k, v, log_decay, state=None, d_state=None, lens=No
     if lens is not None:
         _operand("lens", lens, q.shape[:1], torch.int32, dev)
     given = (None,) * 4 if out is None else out
-    d_q = _result("d_q", given[0], q.shape, q.dtype, dev)
-    d_k = _result("d_k", given[1], k.shape, q.dtype, dev)
-    d_v = _result("d_v", given[2], v.shape, q.dtype, dev)
-    d_in = _result("d_state_in", given[3], s_shape, torch.float32, dev)
-    need = ctypes.c_size_t(0)
-    _check(lib.bct_linear_scratch_bytes(ctypes.byref(p), T, 1, ctypes.byref(need)))
-    scratch = _scratch(need.value, scratch, dev)
-    _launch(dev, stream, lib.bct_linear_backward, ctypes.byref(p), T, d_out.data_ptr(), q.data_ptr(), k.data_ptr(),
+    d_q = _result("d_q", given[0], q, q.shape, q.dtype, dev)
+    d_k = _result("d_k", given[1], q, k.shape, q.dtype, dev)
+    d_v = _result("d_v", given[2], q, v.shape, q.dtype, dev)
+    d_in = _result("d_state_in", given[3], q, s_shape, torch.float32, dev)
+    scratch = _scratch(_linear_scratch(*sizes, T, 1), scratch, q, dev)
+    _launch(dev, stream, lib.bct_linear_backward, p, T, d_out.data_ptr(), q.data_ptr(), k.data_ptr(),
             v.data_ptr(), log_decay.data_ptr(), _ptr(lens), _ptr(state), _ptr(d_state), d_q.data_ptr(), d_k.data_ptr(),
             d_v.data_ptr(), d_in.data_ptr(), *_scratch_args(scratch))
     return d_q, d_k, d_v, d_in
@@ -332,7 +362,7 @@ def linear_backward(d_out, q, k, v, log_decay, state=None, d_state=None, lens=No
 def _norm_rotate_setup(q, k, w_q, w_k, positions, freq):
     if q.dim() < 3 or k.dim() != q.dim():
         raise ValueError("q and k must be [..., heads, head_dim] with at least one token dimension")
-    lead, d, dt, dev = tuple(q.shape[:-2]), q.shape[-1], _io_dtype("q", q), q.device
+    lead, d, dt, dev = tuple(q.shape[:-2]), q.shape[-1], _io_dtype("q", q), q.get_device()
     Hq, Hkv = q.shape[-2], k.shape[-2]
     _operand("q", q, q.shape, q.dtype, dev)
     _operand("k", k, (*lead, Hkv, d), q.dtype, dev)
@@ -359,9 +389,10 @@ def norm_rotate(q, k, w_q, w_k, positions, freq, eps=1e-6, interleaved=False, ou
     those half the rotated part away.  out: (q, k) to write into, which may be the inputs.  Returns (q, k)."""
     lib = load()
     n, Hq, Hkv, d, dt, rot = _norm_rotate_setup(q, k, w_q, w_k, positions, freq)
+    dev = q.get_device()
     q_out, k_out = (None, None) if out is None else out
-    q_out, k_out = _result("q_out", q_out, q.shape, q.dtype, q.device), _result("k_out", k_out, k.shape, q.dtype, q.device)
-    _launch(q.device, stream, lib.bct_norm_rotate, n, Hq, Hkv, d, dt, q.data_ptr(), k.data_ptr(), _ptr(w_q), _ptr(w_k), eps,
+    q_out, k_out = _result("q_out", q_out, q, q.shape, q.dtype, dev), _result("k_out", k_out, q, k.shape, q.dtype, dev)
+    _launch(dev, stream, lib.bct_norm_rotate, n, Hq, Hkv, d, dt, q.data_ptr(), k.data_ptr(), _ptr(w_q), _ptr(w_k), eps,
             _ptr(positions) if rot else None, _ptr(freq) if rot else None, rot, ROTATE_INTERLEAVED if interleaved else 0,
             q_out.data_ptr(), k_out.data_ptr())
     return q_out, k_out
@@ -373,18 +404,18 @@ def norm_rotate_backward(d_q_out, d_k_out, q, k, w_q, w_k, positions, freq, eps=
     d_w_k float32 or None).  out: that tuple, to write into (d_q may be d_q_out, d_k may be d_k_out)."""
     lib = load()
     n, Hq, Hkv, d, dt, rot = _norm_rotate_setup(q, k, w_q, w_k, positions, freq)
-    dev = q.device
+    dev = q.get_device()
     _operand("d_q_out", d_q_out, q.shape, q.dtype, dev)
     _operand("d_k_out", d_k_out, k.shape, q.dtype, dev)
     given = (None,) * 4 if out is None else out
-    d_q = _result("d_q", given[0], q.shape, q.dtype, dev)
-    d_k = _result("d_k", given[1], k.shape, q.dtype, dev)
-    d_w_q = _result("d_w_q", given[2], (d,), torch.float32, dev) if want_d_w else None
-    d_w_k = _result("d_w_k", given[3], (d,), torch.float32, dev) if want_d_w else None
+    d_q = _result("d_q", given[0], q, q.shape, q.dtype, dev)
+    d_k = _result("d_k", given[1], q, k.shape, q.dtype, dev)
+    d_w_q = _result("d_w_q", given[2], q, (d,), torch.float32, dev) if want_d_w else None
+    d_w_k = _result("d_w_k", given[3], q, (d,), torch.float32, dev) if want_d_w else None
     if want_d_w:
         need = ctypes.c_size_t(0)
         _check(lib.bct_norm_rotate_scratch_bytes(n, d, ctypes.byref(need)))
-        scratch = _scratch(need.value, scratch, dev)
+        scratch = _scratch(need.value, scratch, q, dev)
     else:
         scratch = None
     _launch(dev, stream, lib.bct_norm_rotate_backward, n, Hq, Hkv, d, dt, d_q_out.data_ptr(), d_k_out.data_ptr(),

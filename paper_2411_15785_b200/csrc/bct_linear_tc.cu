@@ -700,11 +700,13 @@ cudaError_t launch_linear_tc(const LinArgs& args, const LinStates& states, cudaS
     a.st = states;
     int n_in = 0;
     const void* base[4] = {};
+    int base_heads[4] = {};
     auto map_of = [&](const void* p, int heads) -> int {   // one map per tensor
         for (int i = 0; i < n_in; ++i)
-            if (base[i] == p) return i;
+            if (base[i] == p && base_heads[i] == heads) return i;
         if (n_in == 4 || !lt_map(&a.in[n_in], p, args.B, args.T, args.Hkv * heads)) return -1;
         base[n_in] = p;
+        base_heads[n_in] = heads;
         return n_in++;
     };
     for (int i = 0; i < args.n_roles; ++i) {

@@ -8,10 +8,13 @@
 // Everything between the load and the one rounding at the end is fp32; the angle is formed in double, in turns,
 // and only its fraction of a turn is handed to sincospi, so that far positions lose nothing.
 //
-// Bound by HBM: one load and one store per element (two loads and a store in the backward).  A lane holds 16
-// bytes of a head, so a head is 8, 16 or 32 neighbouring lanes, the mean is a few shuffles, and the partner of a
-// feature in the other half sits rot/2 features away in another lane at the same place (rot a multiple of 16).
-// A block takes a few tokens at a time and all their heads: the sines of a token are formed once for all of them.
+// Bound by HBM: one load and one store per element (two loads and a store in the backward).  A lane holds 16 bytes of
+// a head, so a head is 8, 16 or 32 neighbouring lanes, the mean is a few shuffles, and the partner of a feature in the
+// other half sits rot/2 features away in another lane at the same place (rot a multiple of 16).  A warp works alone on
+// the heads of one token (or on a share of them, when there are few tokens): it forms the token's sines once, in its
+// piece of shared memory, and the heads come as contiguous bulk copies into a ring of its own, three stages of 4 KiB.
+// 192 KiB in flight per SM is what it takes: with the loads in registers (48 KiB in flight) 32768 tokens of 32 + 8
+// heads of 128 took 150 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -23,7 +26,10 @@ namespace bct {
 namespace {
 
 constexpr int kNrThreads = 256;
-constexpr int kNrMaxTok = 8;    // tokens a block works on at a time, at most
+constexpr int kNrWarps = kNrThreads / 32;
+constexpr int kNrStages = 3;
+constexpr int kNrStageBytes = 4096;   // forward: 8 passes of heads; backward: 4, and their gradients
+constexpr int kNrSmem = kNrWarps * kNrStages * kNrStageBytes;
 
 struct NrArgs {
     const void* x[2];        // q, k
@@ -36,7 +42,7 @@ struct NrArgs {
     int64_t n_tokens;
     int H[2];
     int rot, interleaved;
-    int tok;                 // tokens per turn of a block
+    int parts;               // warps that share a token's heads
     float eps;
 };
 
@@ -45,132 +51,197 @@ __device__ __forceinline__ uint4 ldg16(const T* p) {
     return *reinterpret_cast<const uint4*>(p);
 }
 
-// sin and cos of the tokens' angles; a position is one double product away from its angle in turns
-__device__ __forceinline__ void fill_angles(float2 (*cs)[64], const NrArgs& a, int64_t t0, int nt) {
-    const int half = a.rot >> 1;
-    for (int i = threadIdx.x; i < nt * half; i += kNrThreads) {
-        const int t = i / half, f = i - t * half;
-        double turns = (double)a.positions[t0 + t] * (a.freq[f] * 0.15915494309189533577);
-        turns -= rint(turns);
-        float s, c;
-        sincospif(2.f * (float)turns, &s, &c);
-        cs[t][f] = make_float2(c, s);
-    }
-}
-
-// Turn this lane's features (kE of them from feature e0 on) by the angles in cs, or back when dir = -1.
-template <int kE>
-__device__ __forceinline__ void turn(float* x, const float2* cs, int e0, int rot, bool interleaved, float dir) {
-    if (interleaved) {
-#pragma unroll
-        for (int i = 0; i < kE; i += 2) {
-            if (e0 + i < rot) {
-                const float2 a = cs[(e0 + i) >> 1];
-                const float s = dir * a.y, u = x[i], v = x[i + 1];
-                x[i] = u * a.x - v * s;
-                x[i + 1] = u * s + v * a.x;
-            }
-        }
-        return;
-    }
-    const int half = rot >> 1, lane = threadIdx.x & 31;
-    const int hop = half / kE;                    // lanes between the two halves
-    const bool first = e0 < half, in = e0 < rot;
-    const int src = in ? (first ? lane + hop : lane - hop) : lane;
-#pragma unroll
-    for (int i = 0; i < kE; ++i) {
-        const float other = __shfl_sync(0xffffffffu, x[i], src & 31);
-        if (in) {
-            const float2 a = cs[first ? e0 + i : e0 + i - half];
-            const float s = first ? -dir * a.y : dir * a.y;
-            x[i] = fmaf(other, s, x[i] * a.x);
-        }
-    }
-}
-
-template <typename T, int D, bool BWD>
-__global__ void __launch_bounds__(kNrThreads) norm_rotate_kernel(const NrArgs a) {
+template <typename T, int D, bool BWD, bool INTER>
+__global__ void __launch_bounds__(kNrThreads, 2) norm_rotate_kernel(const NrArgs a) {
     constexpr int kE = Chunk<T>::kElems;          // features of a lane
     constexpr int kLanes = D / kE;                // lanes of a head
-    constexpr int kSlots = kNrThreads / kLanes;   // heads a block works on at a time
-    __shared__ float2 cs[kNrMaxTok][64];
-    const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
-    const int e0 = lane * kE;
-    const int H = a.H[0] + a.H[1];
+    constexpr int kHeads = 32 / kLanes;           // heads of a pass
+    constexpr int kP = kNrStageBytes / 512 / (BWD ? 2 : 1);   // passes of a stage
+    constexpr int kBatch = kHeads * kP;           // heads of a stage
+    constexpr int kHeadBytes = D * (int)sizeof(T);
+    extern __shared__ __align__(128) unsigned char nr_smem[];
+    __shared__ float2 cs_all[kNrWarps][64];
+    __shared__ uint64_t full_all[kNrWarps][kNrStages];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float2* cs = cs_all[warp];
+    uint64_t* full = full_all[warp];
+    unsigned char* ring = nr_smem + warp * (kNrStages * kNrStageBytes);
+    const int e0 = (lane % kLanes) * kE, hl = lane / kLanes;
+    const int half = a.rot >> 1;
+    const bool in = e0 < a.rot, first = e0 < half;
+    // where a feature's partner is: the next feature, or the same place of the lane half the rotated part away
+    const int partner = !in || INTER ? lane : (first ? lane + half / kE : lane - half / kE);
+    auto partner_of = [&](const float* x, int i) { return INTER ? x[i ^ 1] : __shfl_sync(0xffffffffu, x[i], partner); };
 
-    float w[2][kE];
+    // A warp's items: a token, or one of `parts` shares of it.  (With more than one part there are few tokens, so that
+    // items count below 2^31 either way.)  An item's heads come in batches, those of q, then those of k.
+    const int nbq = (a.H[0] + kBatch - 1) / kBatch, nb = nbq + (a.H[1] + kBatch - 1) / kBatch;
+    const int items = (int)(a.n_tokens * a.parts), stride = (int)gridDim.x * kNrWarps;
+    struct Cursor {
+        int item, t, batch;
+    };
+    auto start = [&](int item) {
+        Cursor c;
+        c.item = item;
+        c.t = a.parts == 1 ? item : item / a.parts;
+        c.batch = a.parts == 1 ? 0 : item - c.t * a.parts;
+        return c;
+    };
+    auto after = [&](const Cursor& c) {
+        Cursor n = c;
+        n.batch += a.parts;
+        return n.batch < nb ? n : start(c.item + stride);
+    };
+    if (lane == 0) {
+        for (int i = 0; i < kNrStages; ++i) mbar_init(&full[i], 1);
+        fence_mbar_init_cluster();
+    }
+    __syncwarp();
+    auto fetch = [&](const Cursor& c, int stage) {   // by one lane
+        const bool k = c.batch >= nbq;
+        const int H = k ? a.H[1] : a.H[0], h0 = (k ? c.batch - nbq : c.batch) * kBatch;
+        const uint32_t bytes = (uint32_t)min(kBatch, H - h0) * kHeadBytes;
+        const size_t off = ((size_t)c.t * H + h0) * kHeadBytes;
+        unsigned char* dst = ring + stage * kNrStageBytes;
+        mbar_arrive_expect_tx(&full[stage], BWD ? 2 * bytes : bytes);
+        bulk_load(dst, static_cast<const char*>(k ? a.x[1] : a.x[0]) + off, bytes, &full[stage]);
+        if (BWD) bulk_load(dst + kNrStageBytes / 2, static_cast<const char*>(k ? a.d[1] : a.d[0]) + off, bytes, &full[stage]);
+    };
+    Cursor cur = start((int)blockIdx.x * kNrWarps + warp), ahead = cur;
+    for (int i = 0; i < kNrStages; ++i) {
+        if (ahead.item < items) {
+            if (lane == 0) fetch(ahead, i);
+            ahead = after(ahead);
+        }
+    }
+
+    double fr[2];   // this lane's share of the frequencies, in turns per position
+#pragma unroll
+    for (int i = 0; i < 2; ++i) fr[i] = lane + 32 * i < half ? a.freq[lane + 32 * i] * 0.15915494309189533577 : 0.;
+    uint4 w_raw[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         if (a.w[s] != nullptr) {
-            Chunk<T>::unpack(ldg16(static_cast<const T*>(a.w[s]) + e0), w[s]);
+            w_raw[s] = ldg16(static_cast<const T*>(a.w[s]) + e0);
         } else {
+            float one[kE];
 #pragma unroll
-            for (int i = 0; i < kE; ++i) w[s][i] = 1.f;
+            for (int i = 0; i < kE; ++i) one[i] = 1.f;
+            w_raw[s] = Chunk<T>::pack(one);
         }
     }
     float dw[2][kE] = {};
+    int64_t pos = cur.item < items && half > 0 ? a.positions[cur.t] : 0;
+    int stage = 0;
+    uint32_t phase = 0;
 
-    const int64_t turns = (a.n_tokens + a.tok - 1) / a.tok;
-    for (int64_t tt = blockIdx.x; tt < turns; tt += gridDim.x) {
-        const int64_t t0 = tt * a.tok;
-        const int nt = (int)min((int64_t)a.tok, a.n_tokens - t0);
-        __syncthreads();
-        fill_angles(cs, a, t0, nt);
-        __syncthreads();
-        const int n = nt * H;
-        for (int i0 = 0; i0 < n; i0 += kSlots) {
-            const int i = min(i0 + slot, n - 1);      // (every lane takes part in the shuffles)
-            const bool valid = i0 + slot < n;
-            const int t = i / H, hh = i - t * H;
-            const int s = hh >= a.H[0];
-            const int h = s ? hh - a.H[0] : hh;
-            const size_t off = ((size_t)(t0 + t) * a.H[s] + h) * D + e0;
-            float x[kE];
-            Chunk<T>::unpack(ldg16(static_cast<const T*>(a.x[s]) + off), x);
-            float g[kE];
-            if (BWD) {
-                Chunk<T>::unpack(ldg16(static_cast<const T*>(a.d[s]) + off), g);
-                turn<kE>(g, cs[t], e0, a.rot, a.interleaved != 0, -1.f);
+    while (cur.item < items) {
+        const Cursor next_item = start(cur.item + stride);
+        const int64_t pos1 = next_item.item < items && half > 0 ? a.positions[next_item.t] : 0;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {   // sines of the token, formed once for all its heads
+            if (lane + 32 * i < half) {
+                double turns = (double)pos * fr[i];
+                turns -= rint(turns);
+                float sn, c;
+                sincospif(2.f * (float)turns, &sn, &c);
+                cs[lane + 32 * i] = make_float2(c, sn);
             }
-            float ss = 0.f;
-#pragma unroll
-            for (int j = 0; j < kE; ++j) ss = fmaf(x[j], x[j], ss);
-#pragma unroll
-            for (int m = kLanes / 2; m > 0; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
-            const float r = rsqrtf(ss * (1.f / D) + a.eps);
-            if (!BWD) {
-#pragma unroll
-                for (int j = 0; j < kE; ++j) x[j] = x[j] * r * (s ? w[1][j] : w[0][j]);
-                turn<kE>(x, cs[t], e0, a.rot, a.interleaved != 0, 1.f);
-            } else {
-                float dot = 0.f;
-#pragma unroll
-                for (int j = 0; j < kE; ++j) {
-                    x[j] *= r;
-                    const float gx = g[j] * x[j];
-                    if (valid) {
-                        dw[0][j] += s ? 0.f : gx;
-                        dw[1][j] += s ? gx : 0.f;
-                    }
-                    g[j] *= s ? w[1][j] : w[0][j];
-                    dot = fmaf(g[j], x[j], dot);
-                }
-#pragma unroll
-                for (int m = kLanes / 2; m > 0; m >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, m);
-                dot *= 1.f / D;
-#pragma unroll
-                for (int j = 0; j < kE; ++j) x[j] = r * (g[j] - x[j] * dot);
-            }
-            if (valid) *reinterpret_cast<uint4*>(static_cast<T*>(a.y[s]) + off) = Chunk<T>::pack(x);
         }
+        __syncwarp();
+        // The turn is one multiply-add per feature, x_i c_i + x_partner s_i with the partner's sign in s; features that
+        // are not turned have c = 1, s = 0.  Forward, the weights are in both.
+        float tc[kE], ts[kE];
+        int have = -1;
+        for (; cur.batch < nb; cur.batch += a.parts) {
+            const bool s = cur.batch >= nbq;
+            const int h0 = (s ? cur.batch - nbq : cur.batch) * kBatch, H = s ? a.H[1] : a.H[0];
+            float w[kE];
+            if (BWD || have != (int)s) Chunk<T>::unpack(s ? w_raw[1] : w_raw[0], w);
+            if (BWD ? have < 0 : have != (int)s) {
+                have = s;
+#pragma unroll
+                for (int i = 0; i < kE; ++i) {
+                    const int f = INTER ? (e0 + i) >> 1 : (first ? e0 + i : e0 + i - half);
+                    const float2 v = in ? cs[f] : make_float2(1.f, 0.f);
+                    const bool minus = (INTER ? (i & 1) == 0 : first) != BWD;
+                    tc[i] = v.x;
+                    ts[i] = minus ? -v.y : v.y;
+                }
+                if (!BWD) {
+#pragma unroll
+                    for (int i = 0; i < kE; ++i) {
+                        const float wp = partner_of(w, i);
+                        tc[i] *= w[i];
+                        ts[i] *= wp;
+                    }
+                }
+            }
+            const bool came = mbar_wait(&full[stage], phase);
+            __syncwarp();
+            const unsigned char* src = ring + stage * kNrStageBytes + lane * 16;
+            T* ys = static_cast<T*>(s ? a.y[1] : a.y[0]) + ((size_t)cur.t * H + h0 + hl) * D + e0;
+            const int passes = min(kP, (H - h0 + kHeads - 1) / kHeads);
+#pragma unroll 2
+            for (int p = 0; p < passes; ++p) {   // (lanes of heads past the last one work on what the stage held before)
+                float x[kE], g[kE];
+                Chunk<T>::unpack(*reinterpret_cast<const uint4*>(src + p * 512), x);
+                if (BWD) Chunk<T>::unpack(*reinterpret_cast<const uint4*>(src + kNrStageBytes / 2 + p * 512), g);
+                const bool valid = h0 + p * kHeads + hl < H;
+                float ss = 0.f;
+#pragma unroll
+                for (int j = 0; j < kE; ++j) ss = fmaf(x[j], x[j], ss);
+#pragma unroll
+                for (int m = kLanes / 2; m > 0; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+                float r = rsqrtf(ss * (1.f / D) + a.eps);
+                if (!came) r = __int_as_float(0x7fc00000);   // the copy never came: NaN, not old bytes
+                const float* v = BWD ? g : x;
+                float y[kE];
+#pragma unroll
+                for (int j = 0; j < kE; ++j) y[j] = fmaf(partner_of(v, j), ts[j], v[j] * tc[j]);
+                if (!BWD) {
+#pragma unroll
+                    for (int j = 0; j < kE; ++j) y[j] *= r;
+                } else {
+                    float dot = 0.f;
+#pragma unroll
+                    for (int j = 0; j < kE; ++j) {
+                        x[j] *= r;
+                        const float gx = valid ? y[j] * x[j] : 0.f;
+                        if (!s)
+                            dw[0][j] += gx;
+                        else
+                            dw[1][j] += gx;
+                        y[j] *= w[j];
+                        dot = fmaf(y[j], x[j], dot);
+                    }
+#pragma unroll
+                    for (int m = kLanes / 2; m > 0; m >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, m);
+                    dot *= 1.f / D;
+#pragma unroll
+                    for (int j = 0; j < kE; ++j) y[j] = r * (y[j] - x[j] * dot);
+                }
+                if (valid) *reinterpret_cast<uint4*>(ys + (size_t)p * kHeads * D) = Chunk<T>::pack(y);
+            }
+            __syncwarp();   // the stage has been read
+            if (ahead.item < items) {
+                if (lane == 0) fetch(ahead, stage);
+                ahead = after(ahead);
+            }
+            if (++stage == kNrStages) stage = 0, phase ^= 1;
+        }
+        cur = next_item;
+        pos = pos1;
     }
-    if (BWD && a.partial != nullptr) {   // this block's share of dL/dw: its slots summed in order
+    if (BWD && a.partial != nullptr) {   // this block's share of dL/dw: its lanes' sums in a fixed order
         __shared__ float red[kNrThreads * kE];
+        constexpr int kSlots = kNrThreads / kLanes;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < kE; ++j) red[slot * D + e0 + j] = dw[s][j];
+            for (int j = 0; j < kE; ++j) red[(threadIdx.x / kLanes) * D + e0 + j] = dw[s][j];
             __syncthreads();
             for (int e = threadIdx.x; e < D; e += kNrThreads) {
                 float sum = 0.f;
@@ -197,30 +268,38 @@ __global__ void __launch_bounds__(1024) norm_rotate_dw_kernel(const float* parti
     }
 }
 
-int nr_tokens_per_turn(int64_t n_tokens) {
-    // one token per block while that leaves SMs without work, more beyond (the sines of a turn fill the block)
-    return n_tokens >= 148 * 4 * 4 ? 4 : 1;
+// Warps that share a token's heads: enough for about eight warps per SM in all, at most one to a batch.
+int nr_parts(int64_t n_tokens, int Hq, int Hkv, int D, int dtype) {
+    const int heads = kNrStageBytes / (D * (dtype == BCT_BF16 ? 2 : 4));   // of a batch
+    const int most = (Hq + heads - 1) / heads + (Hkv + heads - 1) / heads;
+    const int64_t parts = (148 * 8 + n_tokens - 1) / n_tokens;
+    return (int)(parts > most ? most : parts);
 }
 
-int nr_grid(int64_t n_tokens, int tok, int per_sm) {
-    const int64_t turns = (n_tokens + tok - 1) / tok;
-    return (int)(turns < 148 * per_sm ? turns : 148 * per_sm);
+int nr_grid(int64_t n_tokens, int parts, int per_sm) {
+    const int64_t blocks = (n_tokens * parts + kNrWarps - 1) / kNrWarps;
+    return (int)(blocks < 148 * per_sm ? blocks : 148 * per_sm);
 }
 
+template <typename T, int D, bool BWD, bool INTER>
+cudaError_t nr_launch_kernel(const NrArgs& a, int grid, cudaStream_t stream) {
+    auto fn = norm_rotate_kernel<T, D, BWD, INTER>;
+    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, kNrSmem);
+    if (e != cudaSuccess) return e;
+    fn<<<grid, kNrThreads, kNrSmem, stream>>>(a);
+    return cudaGetLastError();
+}
+template <bool BWD, bool INTER>
+cudaError_t nr_launch_as(const NrArgs& a, int D, int dtype, int grid, cudaStream_t stream) {
+    if (dtype == BCT_BF16)
+        return D == 128 ? nr_launch_kernel<__nv_bfloat16, 128, BWD, INTER>(a, grid, stream)
+                        : nr_launch_kernel<__nv_bfloat16, 64, BWD, INTER>(a, grid, stream);
+    return D == 128 ? nr_launch_kernel<float, 128, BWD, INTER>(a, grid, stream)
+                    : nr_launch_kernel<float, 64, BWD, INTER>(a, grid, stream);
+}
 template <bool BWD>
 cudaError_t nr_launch(const NrArgs& a, int D, int dtype, int grid, cudaStream_t stream) {
-    if (dtype == BCT_BF16) {
-        if (D == 128)
-            norm_rotate_kernel<__nv_bfloat16, 128, BWD><<<grid, kNrThreads, 0, stream>>>(a);
-        else
-            norm_rotate_kernel<__nv_bfloat16, 64, BWD><<<grid, kNrThreads, 0, stream>>>(a);
-    } else {
-        if (D == 128)
-            norm_rotate_kernel<float, 128, BWD><<<grid, kNrThreads, 0, stream>>>(a);
-        else
-            norm_rotate_kernel<float, 64, BWD><<<grid, kNrThreads, 0, stream>>>(a);
-    }
-    return cudaGetLastError();
+    return a.interleaved ? nr_launch_as<BWD, true>(a, D, dtype, grid, stream) : nr_launch_as<BWD, false>(a, D, dtype, grid, stream);
 }
 
 }  // namespace
@@ -238,12 +317,13 @@ cudaError_t launch_norm_rotate(int64_t n_tokens, int Hq, int Hkv, int D, int dty
     a.H[0] = Hq, a.H[1] = Hkv;
     a.rot = rot;
     a.interleaved = interleaved;
-    a.tok = nr_tokens_per_turn(n_tokens);
+    a.parts = nr_parts(n_tokens, Hq, Hkv, D, dtype);
     a.eps = eps;
-    return nr_launch<false>(a, D, dtype, nr_grid(n_tokens, a.tok, 8), stream);
+    return nr_launch<false>(a, D, dtype, nr_grid(n_tokens, a.parts, 2), stream);
 }
 
-int norm_rotate_bwd_blocks(int64_t n_tokens) { return nr_grid(n_tokens, nr_tokens_per_turn(n_tokens), 4); }
+// The backward keeps one warp to a token: a block's share of d_w costs as much however little it has summed.
+int norm_rotate_bwd_blocks(int64_t n_tokens) { return nr_grid(n_tokens, 1, 2); }
 
 cudaError_t launch_norm_rotate_bwd(int64_t n_tokens, int Hq, int Hkv, int D, int dtype, const void* d_q_out,
                                    const void* d_k_out, const void* q, const void* k, const void* w_q, const void* w_k,
@@ -262,7 +342,7 @@ cudaError_t launch_norm_rotate_bwd(int64_t n_tokens, int Hq, int Hkv, int D, int
     a.H[0] = Hq, a.H[1] = Hkv;
     a.rot = rot;
     a.interleaved = interleaved;
-    a.tok = nr_tokens_per_turn(n_tokens);
+    a.parts = 1;
     a.eps = eps;
     const int grid = norm_rotate_bwd_blocks(n_tokens);
     cudaError_t e = nr_launch<true>(a, D, dtype, grid, stream);
