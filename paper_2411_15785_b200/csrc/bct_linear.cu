@@ -1,5 +1,5 @@
-// Linear attention with a decay for each head on the CUDA cores: the single-token step, and the chunked scan
-// for the types and head sizes that the tensor-core kernel does not serve.
+// Linear attention with a decay for each head on the CUDA cores: the single-token step, and the chunked scan in
+// float (bfloat16 is the tensor-core kernel's).
 //
 //     S_t = lambda S_{t-1} + k_t^T v_t        o_t = scale q_t S_t         lambda = exp(log_decay[h])
 //
@@ -7,16 +7,19 @@
 // and weighted with lambda^|i-j|; what lies before the chunk comes out of the state, which is updated once per
 // chunk.  Everything is fp32; the powers of lambda are formed in double (33 of them per block).
 //
-// One block holds one (sequence, kv-head) unit and half of c's features: those columns of the state and of the
-// output depend on nothing in the other half, and only the 32 x 32 products are formed twice.  The state of the
-// block lives in registers (its update reads b and c from shared memory) and is copied to shared memory once per
-// chunk, where the next chunk's products with a read it.
+// One block holds one (sequence, kv-head) unit, one segment of the tokens and 32 of c's features: those columns of the
+// state and of the output depend on nothing in the others, and only the 32 x 32 products are formed again for each 32.
+// That trades an eighth more multiplications (head_dim 128) for four times the blocks, which is what the small calls
+// in float want.  The state of the block lives in registers (its update reads b and c from shared memory) and is copied
+// to shared memory once per chunk, where the next chunk's products with a read it; the next tiles come by
+// asynchronous copies while this chunk is worked on.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include "bct_device.cuh"
 #include "bct_internal.h"
 #include "bct_linear.h"
+#include "bct_tc.cuh"
 
 namespace bct {
 namespace {
@@ -24,22 +27,16 @@ namespace {
 constexpr int kCh = 32;         // tokens per chunk
 constexpr int kScanThreads = 256;
 
-template <typename T>
-__device__ __forceinline__ float4 load4(const T* p);
-template <>
-__device__ __forceinline__ float4 load4<float>(const float* p) {
-    return *reinterpret_cast<const float4*>(p);
-}
-template <>
-__device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p) {
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
     const uint2 w = *reinterpret_cast<const uint2*>(p);
     return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
                        __uint_as_float(w.y & 0xffff0000u));
 }
 __device__ __forceinline__ void store4(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 x) {
-    *reinterpret_cast<uint2*>(p) =
-        make_uint2(Chunk<__nv_bfloat16>::pack2(x.x, x.y), Chunk<__nv_bfloat16>::pack2(x.z, x.w));
+// 16 bytes into shared memory, asynchronously; zeros where `on` is false (nothing is read then)
+__device__ __forceinline__ void copy16(float* dst, const float* src, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ float4 fma4(float s, float4 x, float4 acc) {
     return make_float4(fmaf(s, x.x, acc.x), fmaf(s, x.y, acc.y), fmaf(s, x.z, acc.z), fmaf(s, x.w, acc.w));
@@ -49,14 +46,16 @@ __device__ __forceinline__ float dot4(float4 x, float4 y, float acc) {
     return fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, acc))));
 }
 
-template <int D, int NC>
+constexpr int kNc = 32;         // columns of a block
+
+template <int D>
 struct ScanSmem {
-    float a[kCh][D + 4];    // rows 16 bytes apart modulo 128: neighbouring rows start in other banks
-    float b[kCh][D + 4];
-    float c[kCh][NC];
+    float a[2][kCh][D + 4];    // two buffers; rows 16 bytes apart modulo 128: neighbouring rows start in other banks
+    float b[2][kCh][D + 4];
+    float c[2][kCh][kNc];
     float p[kCh][kCh + 4];
-    float s[D][NC];
-    float pw[kCh + 1];      // lambda^n
+    float s[D][kNc];
+    float pw[kCh + 1];         // lambda^n
 };
 
 // lambda^n, n = 0..kCh
@@ -64,47 +63,65 @@ __device__ __forceinline__ void fill_powers(float* pw, float log_decay, int tid)
     if (tid <= kCh) pw[tid] = tid == 0 ? 1.f : (float)exp((double)tid * (double)log_decay);
 }
 
-template <typename T, int D, int NC, bool STATE_ONLY>
-__global__ void __launch_bounds__(kScanThreads, 2) linear_scan_kernel(const LinArgs args, const LinStates st) {
+template <int D, bool STATE_ONLY>
+__global__ void __launch_bounds__(kScanThreads, 2) linear_scan_kernel(const __grid_constant__ LinArgs args, const __grid_constant__ LinStates st) {
     extern __shared__ __align__(16) unsigned char scan_smem_raw[];
-    ScanSmem<D, NC>& sm = *reinterpret_cast<ScanSmem<D, NC>*>(scan_smem_raw);
-    constexpr int kCG = NC / 4;                  // groups of four columns
-    constexpr int kRG = kScanThreads / kCG;      // groups of rows
-    constexpr int kOutRows = kCh / kRG;          // output rows of a thread
+    ScanSmem<D>& sm = *reinterpret_cast<ScanSmem<D>*>(scan_smem_raw);
+    constexpr int kCG = kNc / 4;                 // groups of four columns
+    constexpr int kRG = kScanThreads / kCG;      // groups of rows: one output row each
     constexpr int kStateRows = D / kRG;          // state rows of a thread
-    static_assert(kOutRows >= 1 && kStateRows >= 1, "");
+    static_assert(kRG == kCh && (kStateRows == 2 || kStateRows == 4), "");
 
     const int tid = threadIdx.x;
-    const int ncol = D / NC;
+    const int ncol = D / kNc;
     int idx = blockIdx.x;
-    const int col0 = (idx % ncol) * NC;
+    const int col0 = (idx % ncol) * kNc;
     idx /= ncol;
     const int seg = idx % args.nseg;
     const int u = idx / args.nseg;
     const int bi = u / args.Hkv, h = u - bi * args.Hkv;
 
     const int which = STATE_ONLY ? (st.seg[0] == nullptr ? 1 : (int)blockIdx.y) : (int)blockIdx.y;
-    LinRole r = args.role[STATE_ONLY ? 0 : which];
-    if (STATE_ONLY) {
-        r.b = st.b[which];
-        r.c = st.c[which];
-        r.reverse = which;
-        r.Ga = 1;
-        r.Gb = st.G[which];
-        // the last segment in the order of the scan feeds no other
-        if (seg == (r.reverse ? 0 : args.nseg - 1)) return;
-    }
-    const T* ga = static_cast<const T*>(r.a);
-    const T* gb = static_cast<const T*>(r.b);
-    const T* gc = static_cast<const T*>(r.c);
-    T* go = static_cast<T*>(r.out);
+    const LinRole& r = args.role[STATE_ONLY ? 0 : which];
+    const int reverse = STATE_ONLY ? which : r.reverse;
+    const int Ga = STATE_ONLY ? 1 : r.Ga, Gb = STATE_ONLY ? st.G[which] : r.Gb;
+    // the last segment in the order of the scan feeds no other
+    if (STATE_ONLY && seg == (reverse ? 0 : args.nseg - 1)) return;
+    const float* ga = static_cast<const float*>(r.a);
+    const float* gb = static_cast<const float*>(STATE_ONLY ? st.b[which] : r.b);
+    const float* gc = static_cast<const float*>(STATE_ONLY ? st.c[which] : r.c);
+    float* go = static_cast<float*>(r.out);
 
     const int len = args.lens ? min(max(args.lens[bi], 0), args.T) : args.T;
     const int t_begin = seg * args.seg_len;
     const int t_end = min(t_begin + args.seg_len, args.T);
     const int v_end = min(t_end, len);           // valid tokens of the segment end here
     const int n_chunks = v_end > t_begin ? (v_end - t_begin + kCh - 1) / kCh : 0;
+    const int G = STATE_ONLY ? Gb : max(Ga, Gb), items = n_chunks * G;
+    const size_t a_row = (size_t)args.Hkv * Ga * D, b_row = (size_t)args.Hkv * Gb * D;  // elements per token
+    auto chunk_t0 = [&](int n) { return t_begin + (reverse ? n_chunks - 1 - n : n) * kCh; };
 
+    // the tiles of item `it` (chunk it / G, head it % G): into the buffer of its tile count; rows behind the last valid
+    // token are zeros
+    auto fetch = [&](int it) {
+        const int n = it / G, x = it - n * G, t0 = chunk_t0(n), nv = min(kCh, v_end - t0);
+        const int na = Ga > 1 ? it : n, nb = Gb > 1 ? it : n;
+        const bool new_b = x == 0 || Gb > 1, new_a = !STATE_ONLY && (x == 0 || Ga > 1);
+        const size_t tok = (size_t)bi * args.T + t0;
+        for (int i = tid; i < kCh * (D / 4); i += kScanThreads) {
+            const int tr = i / (D / 4), q4 = i - tr * (D / 4);
+            const size_t row = tok + min(tr, nv - 1);
+            if (new_a) copy16(&sm.a[na & 1][tr][4 * q4], ga + row * a_row + (size_t)(h * Ga + (Ga > 1 ? x : 0)) * D + 4 * q4, tr < nv);
+            if (new_b) copy16(&sm.b[nb & 1][tr][4 * q4], gb + row * b_row + (size_t)(h * Gb + (Gb > 1 ? x : 0)) * D + 4 * q4, tr < nv);
+        }
+        if (new_b) {
+            const int tr = tid / kCG, q4 = tid - tr * kCG;
+            const size_t row = tok + min(tr, nv - 1);
+            copy16(&sm.c[nb & 1][tr][4 * q4], gc + row * b_row + (size_t)(h * Gb + (Gb > 1 ? x : 0)) * D + col0 + 4 * q4, tr < nv);
+        }
+        cp_async_commit();
+    };
+    if (items > 0) fetch(0);
     fill_powers(sm.pw, args.log_decay[h], tid);
 
     const int cg = tid % kCG, rg = tid / kCG;
@@ -134,126 +151,83 @@ __global__ void __launch_bounds__(kScanThreads, 2) linear_scan_kernel(const LinA
             *reinterpret_cast<float4*>(&sm.s[rg * kStateRows + i][4 * cg]) = S[i];
     }
 
-    const int G = STATE_ONLY ? r.Gb : max(r.Ga, r.Gb);
-    const size_t a_row = (size_t)args.Hkv * r.Ga * D, b_row = (size_t)args.Hkv * r.Gb * D;  // elements per token
-    // 32 x D tile of head `head` from token t0; rows from nv on are zeros
-    auto load_tile = [&](float (*dst)[D + 4], const T* base, size_t row, int head, int t0, int nv) {
-        for (int i = tid; i < kCh * (D / 4); i += kScanThreads) {
-            const int tr = i / (D / 4), q4 = i - tr * (D / 4);
-            const float4 x = tr < nv ? load4(base + ((size_t)bi * args.T + t0 + tr) * row + (size_t)head * D + 4 * q4)
-                                     : make_float4(0.f, 0.f, 0.f, 0.f);
-            *reinterpret_cast<float4*>(&dst[tr][4 * q4]) = x;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int it = 0; it < items; ++it) {
+        const int n = it / G, x = it - n * G;
+        const int t0 = chunk_t0(n), nv = min(kCh, v_end - t0);
+        const int na = Ga > 1 ? it : n, nb = Gb > 1 ? it : n;
+        const bool new_b = x == 0 || Gb > 1, new_a = x == 0 || Ga > 1;
+        cp_async_wait_all();
+        __syncthreads();  // this item's tiles are here, the item before has been read, the state is in place
+        if (it + 1 < items) fetch(it + 1);
+        float (*ta)[D + 4] = sm.a[na & 1], (*tb)[D + 4] = sm.b[nb & 1], (*tc)[kNc] = sm.c[nb & 1];
+        if (!STATE_ONLY) {
+            {   // products of all pairs: this thread row i, columns j, j + 8, j + 16, j + 24
+                const int i = tid >> 3, j = tid & 7;
+                float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+                for (int kk = 0; kk < D; kk += 4) {
+                    const float4 av = *reinterpret_cast<const float4*>(&ta[i][kk]);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) s[m] = dot4(av, *reinterpret_cast<const float4*>(&tb[j + 8 * m][kk]), s[m]);
+                }
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const int jj = j + 8 * m;
+                    const int dist = reverse ? jj - i : i - jj;
+                    sm.p[i][jj] = dist >= 0 ? s[m] * sm.pw[dist] : 0.f;
+                }
+            }
+            // the state's share, once per (chunk, head of a); this thread's output row is rg
+            if (new_a) {
+                float4 in = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                for (int kk = 0; kk < D; kk += 4) {
+                    const float4 av = *reinterpret_cast<const float4*>(&ta[rg][kk]);
+                    in = fma4(av.x, *reinterpret_cast<const float4*>(&sm.s[kk][4 * cg]), in);
+                    in = fma4(av.y, *reinterpret_cast<const float4*>(&sm.s[kk + 1][4 * cg]), in);
+                    in = fma4(av.z, *reinterpret_cast<const float4*>(&sm.s[kk + 2][4 * cg]), in);
+                    in = fma4(av.w, *reinterpret_cast<const float4*>(&sm.s[kk + 3][4 * cg]), in);
+                }
+                acc = mul4(sm.pw[reverse ? max(nv - 1 - rg, 0) : rg + 1], in);   // the distance to the state's token
+            }
+            __syncwarp();     // a warp's rows of P are its own: rows 4 w .. 4 w + 3, as its output rows are
+#pragma unroll 8
+            for (int j = 0; j < kCh; ++j) acc = fma4(sm.p[rg][j], *reinterpret_cast<const float4*>(&tc[j][4 * cg]), acc);
+            if ((Ga > 1 || x == G - 1) && rg < nv)
+                store4(go + ((size_t)bi * args.T + t0 + rg) * a_row + (size_t)(h * Ga + (Ga > 1 ? x : 0)) * D + cc, mul4(r.scale, acc));
+            __syncwarp();     // P has been read
         }
-    };
-
-    float4 acc[kOutRows];
-    for (int n = 0; n < n_chunks; ++n) {
-        const int ch = r.reverse ? n_chunks - 1 - n : n;
-        const int t0 = t_begin + ch * kCh;
-        const int nv = min(kCh, v_end - t0);
-        for (int x = 0; x < G; ++x) {
-            __syncthreads();  // the item before has been read out of the tiles; the state is in place
-            const bool new_b = x == 0 || r.Gb > 1, new_a = x == 0 || r.Ga > 1;
-            if (!STATE_ONLY && new_a) load_tile(sm.a, ga, a_row, h * r.Ga + (r.Ga > 1 ? x : 0), t0, nv);
-            if (new_b) {
-                const int head = h * r.Gb + (r.Gb > 1 ? x : 0);
-                load_tile(sm.b, gb, b_row, head, t0, nv);
-                for (int i = tid; i < kCh * kCG; i += kScanThreads) {
-                    const int tr = i / kCG, q4 = i - tr * kCG;
-                    const float4 v = tr < nv ? load4(gc + ((size_t)bi * args.T + t0 + tr) * b_row + (size_t)head * D + col0 + 4 * q4)
-                                             : make_float4(0.f, 0.f, 0.f, 0.f);
-                    *reinterpret_cast<float4*>(&sm.c[tr][4 * q4]) = v;
-                }
+        if (new_b) {
+            if (x == 0) {
+                const float f = sm.pw[nv];
+#pragma unroll
+                for (int i = 0; i < kStateRows; ++i) S[i] = mul4(f, S[i]);
             }
-            __syncthreads();
-            if (!STATE_ONLY) {
-                {   // products of all pairs: this thread row i, columns j, j + 8, j + 16, j + 24
-                    const int i = tid >> 3, j = tid & 7;
-                    float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-                    for (int kk = 0; kk < D; kk += 4) {
-                        const float4 av = *reinterpret_cast<const float4*>(&sm.a[i][kk]);
+            for (int j = 0; j < nv; ++j) {
+                const float w = sm.pw[reverse ? j + 1 : nv - 1 - j];
+                const float4 cv = mul4(w, *reinterpret_cast<const float4*>(&tc[j][4 * cg]));
 #pragma unroll
-                        for (int m = 0; m < 4; ++m)
-                            s[m] = dot4(av, *reinterpret_cast<const float4*>(&sm.b[j + 8 * m][kk]), s[m]);
-                    }
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        const int jj = j + 8 * m;
-                        const int dist = r.reverse ? jj - i : i - jj;
-                        sm.p[i][jj] = dist >= 0 ? s[m] * sm.pw[dist] : 0.f;
-                    }
-                }
-                __syncthreads();
-                // the state's share, once per (chunk, head of a)
-                if (new_a) {
-                    float4 in[kOutRows];
-#pragma unroll
-                    for (int o = 0; o < kOutRows; ++o) in[o] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                    for (int kk = 0; kk < D; kk += 4) {
-                        float4 sv[4];
-#pragma unroll
-                        for (int m = 0; m < 4; ++m) sv[m] = *reinterpret_cast<const float4*>(&sm.s[kk + m][4 * cg]);
-#pragma unroll
-                        for (int o = 0; o < kOutRows; ++o) {
-                            const float4 av = *reinterpret_cast<const float4*>(&sm.a[rg * kOutRows + o][kk]);
-                            in[o] = fma4(av.x, sv[0], fma4(av.y, sv[1], fma4(av.z, sv[2], fma4(av.w, sv[3], in[o]))));
-                        }
-                    }
-#pragma unroll
-                    for (int o = 0; o < kOutRows; ++o) {
-                        const int i = rg * kOutRows + o;
-                        const int e = r.reverse ? max(nv - 1 - i, 0) : i + 1;   // distance to the state's token
-                        acc[o] = mul4(sm.pw[e], in[o]);
-                    }
-                }
-#pragma unroll 4
-                for (int j = 0; j < kCh; ++j) {
-                    const float4 cv = *reinterpret_cast<const float4*>(&sm.c[j][4 * cg]);
-#pragma unroll
-                    for (int o = 0; o < kOutRows; ++o) acc[o] = fma4(sm.p[rg * kOutRows + o][j], cv, acc[o]);
-                }
-                if (r.Ga > 1 || x == G - 1) {
-                    const int head = h * r.Ga + (r.Ga > 1 ? x : 0);
-#pragma unroll
-                    for (int o = 0; o < kOutRows; ++o) {
-                        const int i = rg * kOutRows + o;
-                        if (i < nv)
-                            store4(go + ((size_t)bi * args.T + t0 + i) * a_row + (size_t)head * D + cc, mul4(r.scale, acc[o]));
-                    }
-                }
+                for (int i = 0; i < kStateRows; ++i) S[i] = fma4(tb[j][rg * kStateRows + i], cv, S[i]);
             }
-            if (new_b) {
-                if (x == 0) {
-                    const float f = sm.pw[nv];
+        }
+        if (!STATE_ONLY && x == G - 1) {
+            __syncthreads();  // the state in shared memory has been read
 #pragma unroll
-                    for (int i = 0; i < kStateRows; ++i) S[i] = mul4(f, S[i]);
-                }
-                for (int j = 0; j < nv; ++j) {
-                    const float w = sm.pw[r.reverse ? j + 1 : nv - 1 - j];
-                    const float4 cv = mul4(w, *reinterpret_cast<const float4*>(&sm.c[j][4 * cg]));
-#pragma unroll
-                    for (int i = 0; i < kStateRows; ++i) S[i] = fma4(sm.b[j][rg * kStateRows + i], cv, S[i]);
-                }
-            }
-            if (!STATE_ONLY && x == G - 1) {
-                __syncthreads();  // the state in shared memory has been read
-#pragma unroll
-                for (int i = 0; i < kStateRows; ++i)
-                    *reinterpret_cast<float4*>(&sm.s[rg * kStateRows + i][4 * cg]) = S[i];
-            }
+            for (int i = 0; i < kStateRows; ++i)
+                *reinterpret_cast<float4*>(&sm.s[rg * kStateRows + i][4 * cg]) = S[i];
         }
     }
 
     if (STATE_ONLY) {   // into the slot of the segment that it feeds
-        float* dst = st.seg[which] + ((size_t)u * args.nseg + (r.reverse ? seg - 1 : seg + 1)) * D * D;
+        float* dst = st.seg[which] + ((size_t)u * args.nseg + (reverse ? seg - 1 : seg + 1)) * D * D;
 #pragma unroll
         for (int i = 0; i < kStateRows; ++i)
             *reinterpret_cast<float4*>(dst + (size_t)(rg * kStateRows + i) * D + cc) = S[i];
         return;
     }
-    if (r.state_out != nullptr && seg == (r.reverse ? 0 : args.nseg - 1)) {
+    if (r.state_out != nullptr && seg == (reverse ? 0 : args.nseg - 1)) {
         float* dst = r.state_out + (size_t)u * D * D;
 #pragma unroll
         for (int i = 0; i < kStateRows; ++i) {
@@ -272,8 +246,8 @@ __global__ void __launch_bounds__(kScanThreads, 2) linear_scan_kernel(const LinA
     // padding rows of this segment: zeros
     const int pad0 = max(v_end, t_begin);
     for (int t = pad0 + rg; t < t_end; t += kRG)
-        for (int x = 0; x < r.Ga; ++x)
-            store4(go + ((size_t)bi * args.T + t) * a_row + (size_t)(h * r.Ga + x) * D + cc, make_float4(0.f, 0.f, 0.f, 0.f));
+        for (int x = 0; x < Ga; ++x)
+            store4(go + ((size_t)bi * args.T + t) * a_row + (size_t)(h * Ga + x) * D + cc, make_float4(0.f, 0.f, 0.f, 0.f));
 }
 
 // The state each segment starts from: slot s holds what the segment before it (in the order of the scan) adds;
@@ -365,27 +339,26 @@ __global__ void __launch_bounds__(128) linear_step_kernel(const T* __restrict__ 
     }
 }
 
-template <typename T, int D, int NC, bool STATE_ONLY>
+template <int D, bool STATE_ONLY>
 cudaError_t launch_scan(const LinArgs& args, const LinStates& st, int grid_y, cudaStream_t stream) {
-    auto fn = linear_scan_kernel<T, D, NC, STATE_ONLY>;
-    const int smem = (int)sizeof(ScanSmem<D, NC>);
+    auto fn = linear_scan_kernel<D, STATE_ONLY>;
+    const int smem = (int)sizeof(ScanSmem<D>);
     cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)(args.B * args.Hkv * args.nseg * (D / NC)), (unsigned)grid_y);
+    const dim3 grid((unsigned)(args.B * args.Hkv * args.nseg * (D / kNc)), (unsigned)grid_y);
     fn<<<grid, kScanThreads, smem, stream>>>(args, st);
     return cudaGetLastError();
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t scan_all(const LinArgs& args, const LinStates& st, cudaStream_t stream) {
-    constexpr int NC = D / 2;
     if (args.nseg > 1) {
         const int dirs = (st.seg[0] != nullptr) + (st.seg[1] != nullptr);
-        cudaError_t e = launch_scan<T, D, NC, true>(args, st, dirs, stream);
+        cudaError_t e = launch_scan<D, true>(args, st, dirs, stream);
         if (e == cudaSuccess) e = launch_linear_combine(D, args, st, stream);
         if (e != cudaSuccess) return e;
     }
-    return launch_scan<T, D, NC, false>(args, st, args.n_roles, stream);
+    return launch_scan<D, false>(args, st, args.n_roles, stream);
 }
 
 }  // namespace
@@ -399,28 +372,35 @@ cudaError_t launch_linear_combine(int D, const LinArgs& args, const LinStates& s
 
 LinPlan lin_plan(const bct_linear_params_t& p, int64_t T, int kind) {
     LinPlan plan;
-    plan.tensor = p.dtype == BCT_BF16 && p.head_dim == 128;
-    // blocks of one segment, and blocks the machine holds: on the CUDA cores two column halves, two blocks per SM
-    const int64_t blocks = (int64_t)p.batch * p.n_kv_heads * (kind == 1 ? 3 : 1) * (plan.tensor ? 1 : 2);
-    const int64_t slots = plan.tensor ? 148 : 148 * 2;
-    const int64_t units128 = (T + 127) / 128;   // the token axis in steps of 128
-    // Rounds of blocks times the length of a segment; a split adds the pass over b and c that forms the segments'
-    // states (about half the work of the full one) and two launches (about two steps of 128 tokens).
+    plan.tensor = p.dtype == BCT_BF16;
+    // Blocks of one segment, blocks that the machine holds, and the tokens that segments are multiples of.
+    const int64_t ncol = plan.tensor ? 1 : p.head_dim / kNc;
+    const int64_t units = (int64_t)p.batch * p.n_kv_heads * ncol, roles = kind == 1 ? 3 : 1, dirs = kind == 1 ? 2 : 1;
+    const int64_t slots = plan.tensor ? 148 : 148 * 2, step = plan.tensor ? 128 : kCh;
+    const int64_t steps = (T + step - 1) / step;
+    const double G = p.n_q_heads / p.n_kv_heads;
+    // A block's time in units of one (chunk, head) of the full scan; a block starts in `start` of them.  A split adds the
+    // pass that forms the segments' states (per chunk and head of k about half of the full one's) and two launches.
+    const double start = plan.tensor ? 3.0 : 1.0, part = plan.tensor ? 0.6 : 0.4, launches = plan.tensor ? 1.5 : 2.0;
     int64_t best = 1;
     double best_cost = 0;
-    for (int64_t n = 1; n <= units128 && n <= 64; ++n) {
-        const int64_t len = (units128 + n - 1) / n;
-        if ((units128 + len - 1) / len != n) continue;
-        const double rounds = (double)((blocks * n + slots - 1) / slots);
-        const double cost = rounds * (double)len * (n > 1 ? 1.5 : 1.0) + (n > 1 ? 2.0 : 0.0);
+    for (int64_t n = 1; n <= steps && n <= 64; ++n) {
+        const int64_t len = (steps + n - 1) / n;
+        if ((steps + len - 1) / len != n) continue;
+        const double rounds = (double)((units * roles * n + slots - 1) / slots);
+        double cost = rounds * ((double)len * G + start);
+        if (n > 1) {
+            const double before = (double)((units * dirs * (n - 1) + slots - 1) / slots);
+            cost += before * ((double)len * (kind == 1 ? G : 1.0) * part + start) + launches;
+        }
         if (n == 1 || cost < best_cost) {
             best = n;
             best_cost = cost;
         }
     }
-    const int64_t len = (units128 + best - 1) / best;
+    const int64_t len = (steps + best - 1) / best;
     plan.nseg = (int)best;
-    plan.seg_len = (int)(len * 128);
+    plan.seg_len = (int)(len * step);
     plan.seg_bytes = best > 1 ? (size_t)p.batch * p.n_kv_heads * best * p.head_dim * p.head_dim * sizeof(float) : 0;
     return plan;
 }
@@ -451,11 +431,8 @@ cudaError_t launch_linear_step(const bct_linear_params_t& p, const void* q, cons
 
 cudaError_t launch_linear_scan(const bct_linear_params_t& p, const LinPlan& plan, const LinArgs& args,
                                const LinStates& states, cudaStream_t stream) {
-    if (plan.tensor) return launch_linear_tc(args, states, stream);
-    if (p.dtype == BCT_BF16)
-        return p.head_dim == 128 ? scan_all<__nv_bfloat16, 128>(args, states, stream)
-                                 : scan_all<__nv_bfloat16, 64>(args, states, stream);
-    return p.head_dim == 128 ? scan_all<float, 128>(args, states, stream) : scan_all<float, 64>(args, states, stream);
+    if (plan.tensor) return launch_linear_tc(p.head_dim, args, states, stream);
+    return p.head_dim == 128 ? scan_all<128>(args, states, stream) : scan_all<64>(args, states, stream);
 }
 
 }  // namespace bct

@@ -37,7 +37,7 @@ struct LinArgs {
     const int* lens;         // [B] or NULL
     int n_roles;
     int B, Hkv, T;
-    int nseg, seg_len;       // segments of the token axis, tokens per segment (a multiple of 128)
+    int nseg, seg_len;       // segments of the token axis, tokens per segment (a multiple of the chunk)
 };
 
 // The states that the segments start from: for each direction (0 forward in time, 1 reverse) what the
@@ -66,8 +66,8 @@ cudaError_t launch_linear_step(const bct_linear_params_t& p, const void* q, cons
 // The whole scan: with more than one segment the segments' own contributions, their running sums, then every role.
 cudaError_t launch_linear_scan(const bct_linear_params_t& p, const LinPlan& plan, const LinArgs& args,
                                const LinStates& states, cudaStream_t stream);
-// The same on the tensor path (bct_linear_tc.cu): bfloat16, head_dim 128.
-cudaError_t launch_linear_tc(const LinArgs& args, const LinStates& states, cudaStream_t stream);
+// The same on the tensor path (bct_linear_tc.cu): bfloat16.
+cudaError_t launch_linear_tc(int D, const LinArgs& args, const LinStates& states, cudaStream_t stream);
 // Running sums over the segments, in the order of the scan.
 cudaError_t launch_linear_combine(int D, const LinArgs& args, const LinStates& states, cudaStream_t stream);
 

@@ -1,5 +1,4 @@
-// Linear attention with a decay for each head on the sm_100a tensor path: the chunked scan for bfloat16 and
-// head_dim 128 (the forward, and the three scans of the backward; bct_linear.h names the roles a, b, c).
+// Linear attention with a decay for each head on the sm_100a tensor path: the chunked scan for bfloat16 (the forward, and the three scans of the backward; bct_linear.h names the roles a, b, c).
 //
 // Per (sequence, kv-head) unit and chunk of 128 tokens, X being the state outside the chunk:
 //     W     = A B^T                                 products of all pairs   [i][j]
@@ -7,7 +6,7 @@
 //     O     = A X + P C                             [i][feature of c]
 //     out_i = scale f_i O_i                         f_i = lambda^(distance of i to X's token)
 //     X    <- lambda^n X + (w o B)^T C              w_j = lambda^(distance of j to the new X's token)
-// all as tcgen05.mma with M = 128 and fp32 accumulators in tensor memory.  What bounds it is the traffic of shared
+// all as tcgen05.mma with M = 128 and N = 128 (64 columns of results with head_dim 64) and fp32 accumulators in tensor memory.  What bounds it is the traffic of shared
 // memory (operands, tiles, results at 128 bytes a clock), so operands are kept in tensor memory where they can be:
 //  - W's columns are reused for P once its rows have been read.
 //  - B^T comes into tensor memory as a product with a 16 x 16 unit matrix, is multiplied with w there and split into two
@@ -39,7 +38,6 @@ namespace {
 constexpr int kLtThreads = 896;
 constexpr int kLtCh = 128;                    // tokens per chunk
 constexpr int kLtHalf = 128 * 128;            // 64 columns (128 bytes) x 128 rows
-constexpr int kLtTile = 2 * kLtHalf;
 // tensor-memory columns
 constexpr int kLtColW = 0;     // W, then P (bfloat16 pairs) in the first half of each of its 64-column halves
 constexpr int kLtColO = 128;
@@ -55,13 +53,14 @@ struct LtArgs {
     int st_map_b[2], st_map_c[2];
 };
 
-template <bool STATE_ONLY>
+template <int D, bool STATE_ONLY>
 struct LtSmem {   // two buffers of every tile; everything else is kept small enough for that
+    static constexpr int kLtTile = D / 64 * kLtHalf;   // bytes of a tile
     static constexpr int b = 0;
     static constexpr int c = b + 2 * kLtTile;
     static constexpr int a = c + 2 * kLtTile;
     static constexpr int x = a + (STATE_ONLY ? 0 : 2 * kLtTile);   // the state as an operand: rows = features of b
-    static constexpr int unit = x + (STATE_ONLY ? 0 : kLtTile);    // 16 x 16 unit matrix
+    static constexpr int unit = x + (STATE_ONLY ? 0 : D * D * 2);  // 16 x 16 unit matrix
     static constexpr int bars = unit + 512;
     static constexpr int pt = bars + 32 * 8;           // [256]: lambda^(i - j) at 127 + j - i, reverse lambda^(j - i); else 0
     static constexpr int total = pt + 256 * 4 + 1024;  // slack to align the base to 1024 bytes
@@ -142,9 +141,10 @@ __device__ __forceinline__ void lt_wait(uint64_t* bar, uint32_t parity, volatile
     if (!mbar_try_wait(bar, parity)) lt_wait_slow(bar, parity, abort_flag);
 }
 
-template <bool STATE_ONLY>
+template <int D, bool STATE_ONLY>
 __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_constant__ LtArgs args) {
-    using L = LtSmem<STATE_ONLY>;
+    using L = LtSmem<D, STATE_ONLY>;
+    constexpr int kLtTile = L::kLtTile, kHalves = D / 64;
     extern __shared__ unsigned char lt_smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(lt_smem_raw) + 1023) & ~uintptr_t(1023));
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bars);
@@ -194,8 +194,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
 
     // The state is read in two rounds by the threads that keep it; here it is asked for into L2.
     const float* state_src = nullptr;
-    if (!STATE_ONLY) state_src = s.nseg > 1 ? r.seg + ((size_t)u * s.nseg + seg) * 16384 : (r.state_in ? r.state_in + (size_t)u * 16384 : nullptr);
-    if (state_src != nullptr && tid < 512) asm volatile("prefetch.global.L2 [%0];" ::"l"(state_src + tid * 32));
+    if (!STATE_ONLY) state_src = s.nseg > 1 ? r.seg + ((size_t)u * s.nseg + seg) * (D * D) : (r.state_in ? r.state_in + (size_t)u * (D * D) : nullptr);
+    if (state_src != nullptr && tid < D * D / 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(state_src + tid * 32));
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&full_a[i], 1);
@@ -256,8 +256,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         if (lane == 0) {
             auto load = [&](const CUtensorMap* map, int head, int t0, unsigned char* dst, uint64_t* bar) {
                 mbar_arrive_expect_tx(bar, kLtTile);
-                tma_load_4d(dst, map, 0, head, t0, bi, bar);
-                tma_load_4d(dst + kLtHalf, map, 64, head, t0, bi, bar);
+                for (int hf = 0; hf < kHalves; ++hf) tma_load_4d(dst + hf * kLtHalf, map, hf * 64, head, t0, bi, bar);
             };
             auto load_a = [&](int it) {
                 const int n = it / G, x = it - n * G, na = Ga > 1 ? it : n;
@@ -288,7 +287,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         // =========================== products ===========================
         {
             constexpr uint32_t id_kk = instr_desc_mn(128, 128, false, false);
-            constexpr uint32_t id_kn = instr_desc_mn(128, 128, false, true);
+            constexpr uint32_t id_kn = instr_desc_mn(128, D, false, true);
             constexpr uint32_t id_t = instr_desc_mn(128, 16, true, false);
             const DescKind dk(smem_desc(0, 16, 1024)), dmn(smem_desc(0, kLtHalf, 1024));
             const uint32_t a16 = desc_addr16(smem_u32(smem + L::a)), b16 = desc_addr16(smem_u32(smem + L::b)),
@@ -299,7 +298,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             constexpr uint32_t t16 = kLtTile / 16, h16 = kLtHalf / 16;
             int n_clean = 0;
             const int n_short = nv_last == kLtCh ? -1 : (reverse ? 0 : n_chunks - 1);   // the chunk with padding rows
-            // B^T of the nb-th tile of B, which belongs to chunk n
+            // B^T of the nb-th tile of B, which belongs to chunk n.  (With head_dim 64 the upper 64 rows of this product, and
+            // of the state's, come from what lies behind the tile; nothing reads them.)
             auto transpose = [&](int nb, int n) {
                 const int sb = nb & 1;
                 LT_WAIT_WARP(&full_b[sb], nb >> 1);
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     tc_fence_after();
                     uint32_t xa = aa, ya = b16 + sb * t16;
 #pragma unroll
-                    for (int hf = 0; hf < 2; ++hf, xa += h16, ya += h16) {
+                    for (int hf = 0; hf < kHalves; ++hf, xa += h16, ya += h16) {
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk)
                             umma_warp(tmem + kLtColW, dk.at(xa + 2 * kk), dk.at(ya + 2 * kk), id_kk, hf > 0 || kk > 0);
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     tc_fence_after();
                     uint32_t xa = aa;
 #pragma unroll
-                    for (int hf = 0; hf < 2; ++hf, xa += h16) {
+                    for (int hf = 0; hf < kHalves; ++hf, xa += h16) {
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk)
                             umma_warp(tmem + kLtColO, dk.at(xa + 2 * kk), dmn.at(x16 + hf * 512 + kk * 128), id_kn, hf > 0 || kk > 0);
@@ -397,8 +397,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 for (int x = 0; x < Ga; ++x, ++na) {
                     const unsigned char* src = smem + L::a + (na & 1) * kLtTile;
                     LT_WAIT(&out_full[na & 1], na >> 1);
-                    tma_store_4d(map_o, 0, h * Ga + x, t0, bi, src);
-                    tma_store_4d(map_o, 64, h * Ga + x, t0, bi, src + kLtHalf);
+                    for (int hf = 0; hf < kHalves; ++hf) tma_store_4d(map_o, hf * 64, h * Ga + x, t0, bi, src + hf * kLtHalf);
                     bulk_commit();
                     bulk_wait_read();
                     mbar_arrive(&empty_a[na & 1]);
@@ -482,10 +481,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     if (wt >= nv) {
                         uint4* z = reinterpret_cast<uint4*>(smem + (half ? L::c + (nb & 1) * kLtTile : L::b + (nb & 1) * kLtTile) + wt * 128);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            z[j] = make_uint4(0, 0, 0, 0);
-                            z[j + kLtHalf / 16] = make_uint4(0, 0, 0, 0);
-                        }
+                        for (int j = 0; j < 8 * kHalves; ++j) z[(j & 7) + (j >> 3) * (kLtHalf / 16)] = make_uint4(0, 0, 0, 0);
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
@@ -494,7 +490,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 LT_WAIT(b_full, nb);
                 tc_fence_after();
 #pragma unroll 1
-                for (int e = 0; e < 4; ++e) {
+                for (int e = q * 32 < D ? 0 : 4; e < 4; ++e) {   // (lanes without a feature only take part in the barriers)
                     float v[16];
                     tmem_ld16(t_col + e * 16, v);
                     uint32_t o[16];
@@ -526,23 +522,25 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         const int q = warp & 3, hs = (warp - 20) >> 2;   // lanes 32q.., columns 64 hs..
         const int c = q * 32 + lane;                      // this thread's feature of b; of the outputs, its row
         const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
-        const uint32_t s_col = lane_base + kLtColS + hs * 64;
-        {
+        constexpr int kCols = D / 2;                      // columns of a thread, from hs * kCols on
+        const bool has_row = q * 32 < D;                  // (head_dim 64: half of the lanes hold no row of the state)
+        const uint32_t s_col = lane_base + kLtColS + hs * kCols;
+        if (has_row) {
             const float* src = state_src;
             const float mul = STATE_ONLY || s.nseg > 1 ? 1.f : r.in_mul;
 #pragma unroll 1
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < kCols / 32; ++k) {
                 float v[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = 0.f;
                 if (src != nullptr) {
                     if (r.state_t) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = src[(hs * 64 + k * 32 + i) * 128 + c];
+                        for (int i = 0; i < 32; ++i) v[i] = src[(hs * kCols + k * 32 + i) * D + c];
                     } else {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            const float4 x = *reinterpret_cast<const float4*>(src + c * 128 + hs * 64 + k * 32 + 4 * i);
+                            const float4 x = *reinterpret_cast<const float4*>(src + c * D + hs * kCols + k * 32 + 4 * i);
                             v[4 * i] = x.x, v[4 * i + 1] = x.y, v[4 * i + 2] = x.z, v[4 * i + 3] = x.w;
                         }
                     }
@@ -554,7 +552,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             }
             tmem_wait_st();
         }
-        unsigned char* x_row = smem + L::x + hs * kLtHalf + c * 128;
+        unsigned char* x_row = smem + L::x + (hs * kCols / 64) * (D * 128) + c * 128;
+        constexpr int kPiece = kHalves == 2 ? 0 : 4;      // 16-byte pieces of a 128-byte row before hs = 1's
         // Before chunk n: the state as chunk n's operand, and scaled for what chunk n adds.
         auto turn = [&](int n) {
             const float f = lam(chunk_nv(chunk_t0(n)));
@@ -564,12 +563,13 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 tc_fence_after();
             }
 #pragma unroll 1
-            for (int k = 0; k < 4; ++k) {
+            for (int k = has_row ? 0 : kCols / 16; k < kCols / 16; ++k) {
                 float x[16];
                 tmem_ld16(s_col + k * 16, x);
                 if (!STATE_ONLY) {
-                    *reinterpret_cast<uint4*>(x_row + (((2 * k) ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(x);
-                    *reinterpret_cast<uint4*>(x_row + (((2 * k + 1) ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(x + 8);
+                    const int pc = hs * kPiece + 2 * k;
+                    *reinterpret_cast<uint4*>(x_row + ((pc ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(x);
+                    *reinterpret_cast<uint4*>(x_row + (((pc + 1) ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(x + 8);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) {
@@ -599,20 +599,21 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 if (x == Ga - 1 && n + 1 < n_chunks) turn(n + 1);
                 LT_WAIT(o_full, na);
                 tc_fence_after();
-                unsigned char* dst = smem + L::a + (na & 1) * kLtTile + hs * kLtHalf + c * 128;
+                unsigned char* dst = smem + L::a + (na & 1) * kLtTile + (hs * kCols / 64) * kLtHalf + c * 128;
 #pragma unroll 1
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < kCols / 16; ++k) {
                     float o[16];
-                    tmem_ld16(lane_base + kLtColO + hs * 64 + k * 16, o);
-                    if (k == 3) {
+                    tmem_ld16(lane_base + kLtColO + hs * kCols + k * 16, o);
+                    if (k == kCols / 16 - 1) {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(o_empty);
                     }
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[i] = c < nv ? o[i] * f : 0.f;   // padding rows: zeros
-                    *reinterpret_cast<uint4*>(dst + (((2 * k) ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(o);
-                    *reinterpret_cast<uint4*>(dst + (((2 * k + 1) ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(o + 8);
+                    const int pc = hs * kPiece + 2 * k;
+                    *reinterpret_cast<uint4*>(dst + ((pc ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(o);
+                    *reinterpret_cast<uint4*>(dst + (((pc + 1) ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(o + 8);
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -627,19 +628,19 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         float* dst = nullptr;
         float mul = 1.f;
         if (STATE_ONLY) {   // into the slot of the segment that it feeds, key's features in the rows
-            dst = args.st.seg[which] + ((size_t)u * s.nseg + (reverse ? seg - 1 : seg + 1)) * 16384;
+            dst = args.st.seg[which] + ((size_t)u * s.nseg + (reverse ? seg - 1 : seg + 1)) * (D * D);
         } else if (r.state_out != nullptr && seg == (reverse ? 0 : s.nseg - 1)) {
-            dst = r.state_out + (size_t)u * 16384;   // (never transposed)
+            dst = r.state_out + (size_t)u * (D * D);   // (never transposed)
             mul = r.out_mul;
         }
-        if (dst != nullptr) {
+        if (dst != nullptr && has_row) {
 #pragma unroll 1
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < kCols / 16; ++k) {
                 float x[16];
                 tmem_ld16(s_col + k * 16, x);
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
-                    *reinterpret_cast<float4*>(dst + c * 128 + hs * 64 + k * 16 + i) =
+                    *reinterpret_cast<float4*>(dst + c * D + hs * kCols + k * 16 + i) =
                         make_float4(x[i] * mul + poison, x[i + 1] * mul + poison, x[i + 2] * mul + poison, x[i + 3] * mul + poison);
             }
         }
@@ -657,22 +658,24 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         const int first = bad ? t_begin : t_begin + n_chunks * kLtCh;
         const uint32_t fill = bad ? 0x7fc07fc0u : 0u;
         char* out = static_cast<char*>(r.out);
-        for (int i = tid; (long long)first + i / 16 < t_end; i += kLtThreads) {
-            const size_t row = (size_t)bi * s.T + first + i / 16;
+        constexpr int kRow = D * 2 / 16;   // 16-byte pieces of a row
+        for (int i = tid; (long long)first + i / kRow < t_end; i += kLtThreads) {
+            const size_t row = (size_t)bi * s.T + first + i / kRow;
             for (int x = 0; x < Ga; ++x)
-                reinterpret_cast<uint4*>(out + (row * s.Hkv * Ga + (size_t)h * Ga + x) * 256)[i & 15] =
+                reinterpret_cast<uint4*>(out + (row * s.Hkv * Ga + (size_t)h * Ga + x) * (D * 2))[i % kRow] =
                     make_uint4(fill, fill, fill, fill);
         }
     }
 }
 
-// [B][T][H][128] bfloat16 as (feature, head, token, sequence); one box is 64 features of one head for 128 tokens;
+// [B][T][H][D] bfloat16 as (feature, head, token, sequence); one box is 64 features of one head for 128 tokens;
 // tokens past T read as zeros and are not written.
-bool lt_map(CUtensorMap* map, const void* base, int B, int T, int H) {
+bool lt_map(CUtensorMap* map, const void* base, int B, int T, int H, int D) {
     TensorMapEncodeFn fn = tensor_map_encode_fn();
     if (fn == nullptr) return false;
-    const cuuint64_t dims[4] = {128, (cuuint64_t)H, (cuuint64_t)T, (cuuint64_t)B};
-    const cuuint64_t strides[3] = {256, (cuuint64_t)H * 256, (cuuint64_t)T * H * 256};
+    const cuuint64_t row = (cuuint64_t)D * 2;
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)H, (cuuint64_t)T, (cuuint64_t)B};
+    const cuuint64_t strides[3] = {row, (cuuint64_t)H * row, (cuuint64_t)T * H * row};
     const cuuint32_t box[4] = {64, 1, (cuuint32_t)kLtCh, 1};
     const cuuint32_t estr[4] = {1, 1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
@@ -680,11 +683,11 @@ bool lt_map(CUtensorMap* map, const void* base, int B, int T, int H) {
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool STATE_ONLY>
+template <int D, bool STATE_ONLY>
 cudaError_t lt_launch(const LtArgs& a, int grid_y, cudaStream_t stream) {
-    auto fn = linear_tc_kernel<STATE_ONLY>;
-    const int smem = LtSmem<STATE_ONLY>::total;
-    static_assert(LtSmem<STATE_ONLY>::total <= 232448, "shared memory of a block");
+    auto fn = linear_tc_kernel<D, STATE_ONLY>;
+    const int smem = LtSmem<D, STATE_ONLY>::total;
+    static_assert(LtSmem<D, STATE_ONLY>::total <= 232448, "shared memory of a block");
     cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)(a.s.B * a.s.Hkv * a.s.nseg), (unsigned)grid_y);
@@ -692,9 +695,8 @@ cudaError_t lt_launch(const LtArgs& a, int grid_y, cudaStream_t stream) {
     return cudaGetLastError();
 }
 
-}  // namespace
-
-cudaError_t launch_linear_tc(const LinArgs& args, const LinStates& states, cudaStream_t stream) {
+template <int D>
+cudaError_t launch_all(const LinArgs& args, const LinStates& states, cudaStream_t stream) {
     LtArgs a;
     a.s = args;
     a.st = states;
@@ -704,7 +706,7 @@ cudaError_t launch_linear_tc(const LinArgs& args, const LinStates& states, cudaS
     auto map_of = [&](const void* p, int heads) -> int {   // one map per tensor
         for (int i = 0; i < n_in; ++i)
             if (base[i] == p && base_heads[i] == heads) return i;
-        if (n_in == 4 || !lt_map(&a.in[n_in], p, args.B, args.T, args.Hkv * heads)) return -1;
+        if (n_in == 4 || !lt_map(&a.in[n_in], p, args.B, args.T, args.Hkv * heads, D)) return -1;
         base[n_in] = p;
         base_heads[n_in] = heads;
         return n_in++;
@@ -715,7 +717,7 @@ cudaError_t launch_linear_tc(const LinArgs& args, const LinStates& states, cudaS
         a.map_b[i] = map_of(r.b, r.Gb);
         a.map_c[i] = map_of(r.c, r.Gb);
         if (a.map_a[i] < 0 || a.map_b[i] < 0 || a.map_c[i] < 0) return cudaErrorInvalidValue;
-        if (!lt_map(&a.out[i], r.out, args.B, args.T, args.Hkv * r.Ga)) return cudaErrorInvalidValue;
+        if (!lt_map(&a.out[i], r.out, args.B, args.T, args.Hkv * r.Ga, D)) return cudaErrorInvalidValue;
     }
     if (args.nseg > 1) {
         for (int d = 0; d < 2; ++d) {
@@ -725,11 +727,17 @@ cudaError_t launch_linear_tc(const LinArgs& args, const LinStates& states, cudaS
             if (a.st_map_b[d] < 0 || a.st_map_c[d] < 0) return cudaErrorInvalidValue;
         }
         const int dirs = (states.seg[0] != nullptr) + (states.seg[1] != nullptr);
-        cudaError_t e = lt_launch<true>(a, dirs, stream);
-        if (e == cudaSuccess) e = launch_linear_combine(128, args, states, stream);
+        cudaError_t e = lt_launch<D, true>(a, dirs, stream);
+        if (e == cudaSuccess) e = launch_linear_combine(D, args, states, stream);
         if (e != cudaSuccess) return e;
     }
-    return lt_launch<false>(a, args.n_roles, stream);
+    return lt_launch<D, false>(a, args.n_roles, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_linear_tc(int D, const LinArgs& args, const LinStates& states, cudaStream_t stream) {
+    return D == 128 ? launch_all<128>(args, states, stream) : launch_all<64>(args, states, stream);
 }
 
 }  // namespace bct
