@@ -260,20 +260,28 @@ __global__ void __launch_bounds__(256) linear_combine_kernel(const LinArgs args,
     const int bi = u / args.Hkv, h = u - bi * args.Hkv;
     const int len = args.lens ? min(max(args.lens[bi], 0), args.T) : args.T;
     const double g = (double)args.log_decay[h];
+    const float f_whole = (float)exp((double)args.seg_len * g);
     float* base = st.seg[dir] + (size_t)u * args.nseg * DD + e;
     float4 run = make_float4(0.f, 0.f, 0.f, 0.f);
     if (st.first[dir] != nullptr) run = mul4(st.in_mul[dir], *reinterpret_cast<const float4*>(st.first[dir] + (size_t)u * DD + e));
-    for (int n = 0; n < args.nseg; ++n) {
-        const int s = dir ? args.nseg - 1 - n : n;
-        float4* slot = reinterpret_cast<float4*>(base + (size_t)s * DD);
-        if (n > 0) {
-            const int prev = dir ? s + 1 : s - 1;
+    const int step = dir ? -1 : 1, s0 = dir ? args.nseg - 1 : 0;   // segments in the order of the scan
+    *reinterpret_cast<float4*>(base + (size_t)s0 * DD) = run;
+    constexpr int kAhead = 8;   // what the next segments add is asked for together: the walk is a chain of additions, not of loads
+    for (int n0 = 1; n0 < args.nseg; n0 += kAhead) {
+        float4 add[kAhead];
+        const int m = min(kAhead, args.nseg - n0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (i < m) add[i] = *reinterpret_cast<const float4*>(base + (size_t)(s0 + step * (n0 + i)) * DD);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (i >= m) break;
+            const int s = s0 + step * (n0 + i), prev = s - step;
             const int nv = min(max(len - prev * args.seg_len, 0), args.seg_len);
-            const float f = nv == 0 ? 1.f : (float)exp((double)nv * g);
-            const float4 add = *slot;
-            run = make_float4(fmaf(f, run.x, add.x), fmaf(f, run.y, add.y), fmaf(f, run.z, add.z), fmaf(f, run.w, add.w));
+            const float f = nv == 0 ? 1.f : (nv == args.seg_len ? f_whole : (float)exp((double)nv * g));
+            run = make_float4(fmaf(f, run.x, add[i].x), fmaf(f, run.y, add[i].y), fmaf(f, run.z, add[i].z), fmaf(f, run.w, add[i].w));
+            *reinterpret_cast<float4*>(base + (size_t)s * DD) = run;
         }
-        *slot = run;
     }
 }
 
@@ -375,7 +383,8 @@ LinPlan lin_plan(const bct_linear_params_t& p, int64_t T, int kind) {
     plan.tensor = p.dtype == BCT_BF16;
     // Blocks of one segment, blocks that the machine holds, and the tokens that segments are multiples of.
     const int64_t ncol = plan.tensor ? 1 : p.head_dim / kNc;
-    const int64_t units = (int64_t)p.batch * p.n_kv_heads * ncol, roles = kind == 1 ? 3 : 1, dirs = kind == 1 ? 2 : 1;
+    const int64_t roles = kind == 1 ? 3 : (kind == 3 ? 2 : 1), dirs = kind == 1 ? 2 : 1;
+    const int64_t units = (int64_t)p.batch * p.n_kv_heads * ncol;
     const int64_t slots = plan.tensor ? 148 : 148 * 2, step = plan.tensor ? 128 : kCh;
     const int64_t steps = (T + step - 1) / step;
     const double G = p.n_q_heads / p.n_kv_heads;
@@ -391,7 +400,7 @@ LinPlan lin_plan(const bct_linear_params_t& p, int64_t T, int kind) {
         double cost = rounds * ((double)len * G + start);
         if (n > 1) {
             const double before = (double)((units * dirs * (n - 1) + slots - 1) / slots);
-            cost += before * ((double)len * (kind == 1 ? G : 1.0) * part + start) + launches;
+            cost += before * ((double)len * (kind == 1 || kind == 3 ? G : 1.0) * part + start) + launches;
         }
         if (n == 1 || cost < best_cost) {
             best = n;

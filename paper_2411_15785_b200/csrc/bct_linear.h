@@ -57,7 +57,8 @@ struct LinPlan {
     bool tensor;       // the tensor-core kernel serves the call
 };
 
-// kind: 0 forward, 1 backward.  Depends on the sizes only (a B200's 148 SMs are assumed).
+// One launch over the roles of `kind`: 0 forward, 1 backward (all three), 2 its d_q alone, 3 its d_k and d_v.  Depends on
+// the sizes only (a B200's 148 SMs are assumed).
 LinPlan lin_plan(const bct_linear_params_t& p, int64_t T, int kind);
 
 cudaError_t launch_linear_step(const bct_linear_params_t& p, const void* q, const void* k, const void* v,
@@ -67,6 +68,7 @@ cudaError_t launch_linear_step(const bct_linear_params_t& p, const void* q, cons
 cudaError_t launch_linear_scan(const bct_linear_params_t& p, const LinPlan& plan, const LinArgs& args,
                                const LinStates& states, cudaStream_t stream);
 // The same on the tensor path (bct_linear_tc.cu): bfloat16.
+// A launch has several heads on A's side in every role or in none.
 cudaError_t launch_linear_tc(int D, const LinArgs& args, const LinStates& states, cudaStream_t stream);
 // Running sums over the segments, in the order of the scan.
 cudaError_t launch_linear_combine(int D, const LinArgs& args, const LinStates& states, cudaStream_t stream);

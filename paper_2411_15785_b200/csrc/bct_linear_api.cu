@@ -98,6 +98,14 @@ bct_status_t check_scratch(const void* scratch, size_t bytes, size_t need) {
         return fail(BCT_ERR_INVALID_ARG, "scratch must be 256-byte aligned and hold %zu bytes (got %zu)", need, bytes);
     return BCT_OK;
 }
+// One launch serves roles that all have several heads on A's side, or none: the backward of shared heads takes two.
+bool two_launches(const bct_linear_params_t& p) { return p.dtype == BCT_BF16 && p.n_q_heads > p.n_kv_heads; }
+size_t scratch_need(const bct_linear_params_t& p, int64_t T, bool backward) {
+    if (!backward) return round256(bct::lin_plan(p, T, 0).seg_bytes);
+    if (!two_launches(p)) return 2 * round256(bct::lin_plan(p, T, 1).seg_bytes);
+    const size_t a = round256(bct::lin_plan(p, T, 2).seg_bytes), b = round256(bct::lin_plan(p, T, 3).seg_bytes);
+    return a > b ? a : b;   // one after the other, in the same place
+}
 bct_status_t check_lens(const int32_t* lens) {
     if (!aligned(lens, 4)) return fail(BCT_ERR_INVALID_ARG, "lens must be 4-byte aligned");
     return BCT_OK;
@@ -118,8 +126,7 @@ bct_status_t bct_linear_scratch_bytes(const bct_linear_params_t* params, int64_t
     if (st == BCT_OK) st = check_tokens(p, T);
     if (st != BCT_OK) return st;
     if (bytes == nullptr) return fail(BCT_ERR_INVALID_ARG, "bytes is NULL");
-    const bct::LinPlan plan = bct::lin_plan(p, T, backward ? 1 : 0);
-    *bytes = (backward ? 2 : 1) * round256(plan.seg_bytes);
+    *bytes = scratch_need(p, T, backward != 0);
     return BCT_OK;
 }
 
@@ -150,7 +157,7 @@ bct_status_t bct_linear_forward(const bct_linear_params_t* params, int64_t T, co
     if (st != BCT_OK) return st;
     const Sizes s = sizes_of(p, T);
     const bct::LinPlan plan = bct::lin_plan(p, T, 0);
-    const size_t need = round256(plan.seg_bytes);
+    const size_t need = scratch_need(p, T, false);
     if ((st = check_scratch(scratch, scratch_bytes, need)) != BCT_OK) return st;
     const Span in[] = {{"q", q, s.q, false}, {"k", k, s.kv, false}, {"v", v, s.kv, false}, {"state", state, s.state, true}};
     const Span outs[] = {{"out", out, s.q, false}, {"state_out", state_out, s.state, true}, {"scratch", need ? scratch : nullptr, need, true}};
@@ -184,8 +191,7 @@ bct_status_t bct_linear_backward(const bct_linear_params_t* params, int64_t T, c
     if (st == BCT_OK) st = check_lens(lens);
     if (st != BCT_OK) return st;
     const Sizes s = sizes_of(p, T);
-    const bct::LinPlan plan = bct::lin_plan(p, T, 1);
-    const size_t need = 2 * round256(plan.seg_bytes);
+    const size_t need = scratch_need(p, T, true);
     if ((st = check_scratch(scratch, scratch_bytes, need)) != BCT_OK) return st;
     const Span in[] = {{"d_out", d_out, s.q, false}, {"q", q, s.q, false},          {"k", k, s.kv, false},
                        {"v", v, s.kv, false},        {"state", state, s.state, true}, {"d_state", d_state, s.state, true}};
@@ -199,25 +205,33 @@ bct_status_t bct_linear_backward(const bct_linear_params_t* params, int64_t T, c
     if ((st = check_overlap(in, 6, outs, 5, in_place)) != BCT_OK) return st;
 
     const int G = p.n_q_heads / p.n_kv_heads;
-    bct::LinArgs a = {};
-    a.log_decay = log_decay;
-    a.lens = lens;
-    a.n_roles = 3;
-    a.B = p.batch, a.Hkv = p.n_kv_heads, a.T = (int)T;
-    a.nseg = plan.nseg, a.seg_len = plan.seg_len;
-    float* seg0 = plan.nseg > 1 ? static_cast<float*>(scratch) : nullptr;
-    float* seg1 = plan.nseg > 1 ? reinterpret_cast<float*>(static_cast<char*>(scratch) + round256(plan.seg_bytes)) : nullptr;
     // In reverse the state is carried without the scale that q has in it: R = sum lambda^.. q^T do, times `scale`
     // where it is used, so what comes in is divided by it and what goes out multiplied.
     const float inv = 1.f / p.scale;
-    a.role[0] = {d_out, v, k, d_q, state, nullptr, seg0, G, 1, 0, 1, p.scale, 1.f, 1.f};
-    a.role[1] = {v, d_out, q, d_k, d_state, nullptr, seg1, 1, G, 1, 1, p.scale, inv, 1.f};
-    a.role[2] = {k, q, d_out, d_v, d_state, d_state_in, seg1, 1, G, 1, 0, p.scale, inv, p.scale};
-    bct::LinStates states = {};
-    states.b[0] = k, states.c[0] = v, states.seg[0] = seg0, states.first[0] = state, states.in_mul[0] = 1.f, states.G[0] = 1;
-    states.b[1] = q, states.c[1] = d_out, states.seg[1] = seg1, states.first[1] = d_state, states.in_mul[1] = inv, states.G[1] = G;
-    const cudaError_t e = bct::launch_linear_scan(p, plan, a, states, static_cast<cudaStream_t>(cuda_stream));
-    return e == cudaSuccess ? BCT_OK : fail_cuda("linear backward launch", e);
+    const bool two = two_launches(p);
+    for (int launch = 0; launch < (two ? 2 : 1); ++launch) {
+        const int kind = two ? 2 + launch : 1;
+        const bct::LinPlan plan = bct::lin_plan(p, T, kind);
+        float* seg = static_cast<float*>(scratch);      // forward in time, then in reverse
+        float* seg0 = plan.nseg > 1 && kind != 3 ? seg : nullptr;
+        if (seg0 != nullptr) seg += round256(plan.seg_bytes) / sizeof(float);
+        float* seg1 = plan.nseg > 1 && kind != 2 ? seg : nullptr;
+        const bct::LinRole roles[3] = {{d_out, v, k, d_q, state, nullptr, seg0, G, 1, 0, 1, p.scale, 1.f, 1.f},
+                                       {v, d_out, q, d_k, d_state, nullptr, seg1, 1, G, 1, 1, p.scale, inv, 1.f},
+                                       {k, q, d_out, d_v, d_state, d_state_in, seg1, 1, G, 1, 0, p.scale, inv, p.scale}};
+        bct::LinArgs a = {};
+        a.log_decay = log_decay;
+        a.lens = lens;
+        a.B = p.batch, a.Hkv = p.n_kv_heads, a.T = (int)T;
+        a.nseg = plan.nseg, a.seg_len = plan.seg_len;
+            for (int i = kind == 3 ? 1 : 0; i < (kind == 2 ? 1 : 3); ++i) a.role[a.n_roles++] = roles[i];
+        bct::LinStates states = {};
+        states.b[0] = k, states.c[0] = v, states.seg[0] = seg0, states.first[0] = state, states.in_mul[0] = 1.f, states.G[0] = 1;
+        states.b[1] = q, states.c[1] = d_out, states.seg[1] = seg1, states.first[1] = d_state, states.in_mul[1] = inv, states.G[1] = G;
+        const cudaError_t e = bct::launch_linear_scan(p, plan, a, states, static_cast<cudaStream_t>(cuda_stream));
+        if (e != cudaSuccess) return fail_cuda("linear backward launch", e);
+    }
+    return BCT_OK;
 }
 
 }  // extern "C"

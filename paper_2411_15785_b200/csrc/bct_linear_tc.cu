@@ -42,7 +42,8 @@ constexpr int kLtHalf = 128 * 128;            // 64 columns (128 bytes) x 128 ro
 constexpr int kLtColW = 0;     // W, then P (bfloat16 pairs) in the first half of each of its 64-column halves
 constexpr int kLtColO = 128;
 constexpr int kLtColS = 256;   // the state [feature of b][feature of c]
-constexpr int kLtColT = 384;   // B^T [feature of b][j]; of every 16 columns 8 then hold the first terms, 8 the second
+constexpr int kLtColT = 384;   // B^T [feature of b][j]; of every 16 columns 8 then hold the first terms, 8 the second.
+                               // With several heads of A to a state also every other head's W and P
 
 struct LtArgs {
     CUtensorMap in[4];    // forward: q, k, v;  backward: d_out, q, k, v
@@ -141,32 +142,33 @@ __device__ __forceinline__ void lt_wait(uint64_t* bar, uint32_t parity, volatile
     if (!mbar_try_wait(bar, parity)) lt_wait_slow(bar, parity, abort_flag);
 }
 
-template <int D, bool STATE_ONLY>
+// MULTI_A: every role has several heads on A's side (and one on B's).
+template <int D, bool STATE_ONLY, bool MULTI_A>
 __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_constant__ LtArgs args) {
     using L = LtSmem<D, STATE_ONLY>;
     constexpr int kLtTile = L::kLtTile, kHalves = D / 64;
     extern __shared__ unsigned char lt_smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(lt_smem_raw) + 1023) & ~uintptr_t(1023));
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bars);
-    uint64_t* full_a = bars;             // [2]
-    uint64_t* empty_a = bars + 2;        // [2] the output that took A's place has been read out
-    uint64_t* out_full = bars + 4;       // [2] the output is in A's place
-    uint64_t* full_b = bars + 6;         // [2]
-    uint64_t* empty_b = bars + 8;        // [2]
-    uint64_t* full_c = bars + 10;        // [2]
-    uint64_t* empty_c = bars + 12;       // [2]
-    uint64_t* clean = bars + 14;         // padding rows of B and C are zeros
-    uint64_t* b_full = bars + 15;        // B^T complete
-    uint64_t* t_full = bars + 16;        // [2] its terms in place, by halves of j
-    uint64_t* w_full = bars + 18;        // W complete
-    uint64_t* p_full = bars + 19;        // P in place
-    uint64_t* o_full = bars + 20;
-    uint64_t* o_empty = bars + 21;
-    uint64_t* s_full = bars + 22;        // the state holds the chunk
-    uint64_t* x_full = bars + 23;        // X in place, the state scaled
-    uint64_t* x_empty = bars + 24;       // the products with X complete
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 26);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 27);
+    uint64_t* full_a = bars;             // [3]
+    uint64_t* empty_a = bars + 3;        // [3] the output that took A's place has been read out
+    uint64_t* out_full = bars + 6;       // [3] the output is in A's place
+    uint64_t* full_b = bars + 9;         // [2]
+    uint64_t* empty_b = bars + 11;       // [2]
+    uint64_t* full_c = bars + 13;        // [2]
+    uint64_t* empty_c = bars + 15;       // [2]
+    uint64_t* clean = bars + 17;         // padding rows of B and C are zeros
+    uint64_t* b_full = bars + 18;        // B^T complete
+    uint64_t* t_full = bars + 19;        // [2] its terms in place, by halves of j
+    uint64_t* w_full = bars + 21;        // [2] W complete, by items in turn
+    uint64_t* p_full = bars + 23;        // [2] P in place
+    uint64_t* o_full = bars + 25;
+    uint64_t* o_empty = bars + 26;
+    uint64_t* s_full = bars + 27;        // the state holds the chunk
+    uint64_t* x_full = bars + 28;        // X in place, the state scaled
+    uint64_t* x_empty = bars + 29;       // the products with X complete
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 30);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 31);
     float* pt = reinterpret_cast<float*>(smem + L::pt);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -177,7 +179,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     const int which = STATE_ONLY ? (args.st.seg[0] == nullptr ? 1 : (int)blockIdx.y) : (int)blockIdx.y;
     const LinRole& r = s.role[STATE_ONLY ? 0 : which];
     const int reverse = STATE_ONLY ? which : r.reverse;
-    const int Ga = STATE_ONLY ? 1 : r.Ga, Gb = STATE_ONLY ? args.st.G[which] : r.Gb;
+    const int Ga = MULTI_A ? r.Ga : 1, Gb = MULTI_A ? 1 : (STATE_ONLY ? args.st.G[which] : r.Gb);
     if (STATE_ONLY && seg == (reverse ? 0 : s.nseg - 1)) return;   // feeds no other segment
     const CUtensorMap* map_a = &args.in[STATE_ONLY ? 0 : args.map_a[which]];
     const CUtensorMap* map_b = &args.in[STATE_ONLY ? args.st_map_b[which] : args.map_b[which]];
@@ -188,7 +190,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     const int t_end = min(t_begin + s.seg_len, s.T);
     const int v_end = min(t_end, len);
     const int n_chunks = v_end > t_begin ? (v_end - t_begin + kLtCh - 1) / kLtCh : 0;
-    const int G = Ga > Gb ? Ga : Gb;
+    const int G = MULTI_A ? Ga : Gb;
     auto chunk_t0 = [&](int n) { return t_begin + (reverse ? n_chunks - 1 - n : n) * kLtCh; };
     auto chunk_nv = [&](int t0) { return min(kLtCh, v_end - t0); };
 
@@ -197,20 +199,22 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     if (!STATE_ONLY) state_src = s.nseg > 1 ? r.seg + ((size_t)u * s.nseg + seg) * (D * D) : (r.state_in ? r.state_in + (size_t)u * (D * D) : nullptr);
     if (state_src != nullptr && tid < D * D / 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(state_src + tid * 32));
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 3; ++i) {
             mbar_init(&full_a[i], 1);
             mbar_init(&empty_a[i], 1);
             mbar_init(&out_full[i], 8);
+        }
+        for (int i = 0; i < 2; ++i) {
             mbar_init(&full_b[i], 1);
             mbar_init(&empty_b[i], 1);
             mbar_init(&full_c[i], 1);
             mbar_init(&empty_c[i], 1);
             mbar_init(&t_full[i], 4);
+            mbar_init(&w_full[i], 1);
+            mbar_init(&p_full[i], 8);
         }
         mbar_init(clean, 8);
         mbar_init(b_full, 1);
-        mbar_init(w_full, 1);
-        mbar_init(p_full, 8);
         mbar_init(o_full, 1);
         mbar_init(o_empty, 8);
         mbar_init(s_full, 1);
@@ -248,9 +252,20 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         __syncwarp();                \
     }
 
-    // (Loops are kept short where that costs nothing: 27 warps of six roles share the instruction caches, and straight-line
+    // (Loops are kept short where that costs nothing: 26 warps of six roles share the instruction caches, and straight-line
     // code that is run once per chunk is fetched anew each time.)
     const int items = n_chunks * G;   // (chunk, head) in turn: head x of the side that has G of them
+    // Buffers: two of every tile; with several heads on A's side, whose tiles then turn over fastest, B's second one is a
+    // third of A's.
+    constexpr int n_a = !STATE_ONLY && MULTI_A ? 3 : 2, n_b = !STATE_ONLY && MULTI_A ? 1 : 2;
+    struct Ring {   // a place in a ring of buffers and the parity of its turn
+        int s = 0;
+        uint32_t turn = 0;
+        __device__ __forceinline__ void next(int n) {
+            if (++s == n) s = 0, turn ^= 1;
+        }
+    };
+    auto a_at = [&](int st) { return st < 2 ? L::a + st * kLtTile : L::b + kLtTile; };
     if (warp == 1) {
         // =========================== loads ===========================
         if (lane == 0) {
@@ -258,160 +273,200 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 mbar_arrive_expect_tx(bar, kLtTile);
                 for (int hf = 0; hf < kHalves; ++hf) tma_load_4d(dst + hf * kLtHalf, map, hf * 64, head, t0, bi, bar);
             };
-            auto load_a = [&](int it) {
-                const int n = it / G, x = it - n * G, na = Ga > 1 ? it : n;
-                if (STATE_ONLY || (x > 0 && Ga == 1)) return;
-                if (na > 1) LT_WAIT(&empty_a[na & 1], (na >> 1) - 1);
-                load(map_a, h * Ga + (Ga > 1 ? x : 0), chunk_t0(n), smem + L::a + (na & 1) * kLtTile, &full_a[na & 1]);
-            };
-            auto load_b = [&](int it) {
-                const int n = it / G, x = it - n * G, nb = Gb > 1 ? it : n, st = nb & 1;
-                if (x > 0 && Gb == 1) return;
-                if (nb > 1) LT_WAIT(&empty_b[st], (nb >> 1) - 1);
-                load(map_b, h * Gb + (Gb > 1 ? x : 0), chunk_t0(n), smem + L::b + st * kLtTile, &full_b[st]);
-            };
-            auto load_c = [&](int it) {
-                const int n = it / G, x = it - n * G, nb = Gb > 1 ? it : n, st = nb & 1;
-                if (x > 0 && Gb == 1) return;
-                if (nb > 1) LT_WAIT(&empty_c[st], (nb >> 1) - 1);
-                load(map_c, h * Gb + (Gb > 1 ? x : 0), chunk_t0(n), smem + L::c + st * kLtTile, &full_c[st]);
-            };
-            for (int it = 0; it < items; ++it) {
-                load_b(it);
-                load_a(it);
-                load_c(it);
+            Ring ra, rb, rc;
+            for (int n = 0; n < n_chunks; ++n) {
+                const int t0 = chunk_t0(n);
+                for (int x = 0; x < G; ++x) {
+                    const bool new_b = x == 0 || Gb > 1, new_a = !STATE_ONLY && (x == 0 || Ga > 1);
+                    const int hb = h * Gb + (Gb > 1 ? x : 0);
+                    if (new_b) {
+                        LT_WAIT(&empty_b[rb.s], rb.turn ^ 1);
+                        load(map_b, hb, t0, smem + L::b + rb.s * kLtTile, &full_b[rb.s]);
+                        rb.next(n_b);
+                    }
+                    if (new_a) {
+                        LT_WAIT(&empty_a[ra.s], ra.turn ^ 1);
+                        load(map_a, h * Ga + (Ga > 1 ? x : 0), t0, smem + a_at(ra.s), &full_a[ra.s]);
+                        ra.next(n_a);
+                    }
+                    if (new_b) {
+                        LT_WAIT(&empty_c[rc.s], rc.turn ^ 1);
+                        load(map_c, hb, t0, smem + L::c + rc.s * kLtTile, &full_c[rc.s]);
+                        rc.next(2);
+                    }
+                }
             }
         }
         __syncwarp();
     } else if (warp == 0) {
         // =========================== products ===========================
-        {
-            constexpr uint32_t id_kk = instr_desc_mn(128, 128, false, false);
-            constexpr uint32_t id_kn = instr_desc_mn(128, D, false, true);
-            constexpr uint32_t id_t = instr_desc_mn(128, 16, true, false);
-            const DescKind dk(smem_desc(0, 16, 1024)), dmn(smem_desc(0, kLtHalf, 1024));
-            const uint32_t a16 = desc_addr16(smem_u32(smem + L::a)), b16 = desc_addr16(smem_u32(smem + L::b)),
-                           c16 = desc_addr16(smem_u32(smem + L::c)), x16 = desc_addr16(smem_u32(smem + L::x)),
-                           u16 = desc_addr16(smem_u32(smem + L::unit));
-            // the unit matrix is not swizzled: blocks of 8 rows x 16 bytes, 128 bytes apart along k, 256 along its rows
-            const uint64_t unit = (smem_desc(0, 128, 256) & ~((uint64_t)7 << 61)) + u16;
-            constexpr uint32_t t16 = kLtTile / 16, h16 = kLtHalf / 16;
-            int n_clean = 0;
-            const int n_short = nv_last == kLtCh ? -1 : (reverse ? 0 : n_chunks - 1);   // the chunk with padding rows
-            // B^T of the nb-th tile of B, which belongs to chunk n.  (With head_dim 64 the upper 64 rows of this product, and
-            // of the state's, come from what lies behind the tile; nothing reads them.)
-            auto transpose = [&](int nb, int n) {
-                const int sb = nb & 1;
-                LT_WAIT_WARP(&full_b[sb], nb >> 1);
-                if (n == n_short) LT_WAIT_WARP(clean, n_clean++);
+        constexpr uint32_t id_kk = instr_desc_mn(128, 128, false, false);
+        constexpr uint32_t id_kn = instr_desc_mn(128, D, false, true);
+        constexpr uint32_t id_t = instr_desc_mn(128, 16, true, false);
+        const DescKind dk(smem_desc(0, 16, 1024)), dmn(smem_desc(0, kLtHalf, 1024));
+        const uint32_t base16 = desc_addr16(smem_u32(smem)), x16 = base16 + L::x / 16;
+        // the unit matrix is not swizzled: blocks of 8 rows x 16 bytes, 128 bytes apart along k, 256 along its rows
+        const uint64_t unit = (smem_desc(0, 128, 256) & ~((uint64_t)7 << 61)) + base16 + L::unit / 16;
+        constexpr uint32_t h16 = kLtHalf / 16;
+        const int n_short = nv_last == kLtCh ? -1 : (reverse ? 0 : n_chunks - 1);   // the chunk with padding rows
+        int n_clean = 0;
+        Ring ra, rb, rt, rc;   // A and B as W takes them, B as its transposition does, C
+        uint32_t a_w = 0, b_w = 0, c_now = 0;
+        int c_slot = 0;
+        // B^T of the next tile of B, which belongs to chunk n.  (With head_dim 64 the upper 64 rows of this product, and
+        // of the state's, come from what lies behind the tile; nothing reads them.)
+        auto transpose = [&](int n) {
+            LT_WAIT_WARP(&full_b[rt.s], rt.turn);
+            if (n == n_short) LT_WAIT_WARP(clean, n_clean++);
+            tc_fence_after();
+            const uint32_t ba = base16 + (L::b + rt.s * kLtTile) / 16;
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) umma_warp(tmem + kLtColT + kk * 16, dmn.at(ba + kk * 128), unit, id_t, false);
+            umma_commit_warp(b_full);
+            if (STATE_ONLY) umma_commit_warp(&empty_b[rt.s]);
+            rt.next(n_b);
+        };
+        // With several heads on A's side every other one's W goes where B^T was, which is free from the chunk's share of
+        // the state until the next chunk: the next head's W then does not wait for this one's P.
+        auto w_col = [&](int x) { return MULTI_A && (x & 1) ? kLtColT : kLtColW; };
+        auto w_products = [&](int it, int x) {
+            if (x == 0 || Ga > 1) {
+                LT_WAIT_WARP(&full_a[ra.s], ra.turn);
+                a_w = base16 + a_at(ra.s) / 16;
+                ra.next(n_a);
+            }
+            const bool new_b = x == 0 || Gb > 1;
+            if (new_b) {
+                LT_WAIT_WARP(&full_b[rb.s], rb.turn);
+                b_w = rb.s;
+                rb.next(n_b);
+            }
+            tc_fence_after();
+            const uint32_t col = tmem + w_col(x), ba = base16 + (L::b + b_w * kLtTile) / 16;
+#pragma unroll
+            for (int hf = 0; hf < kHalves; ++hf) {
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                    umma_warp(col, dk.at(a_w + hf * h16 + 2 * kk), dk.at(ba + hf * h16 + 2 * kk), id_kk, hf > 0 || kk > 0);
+            }
+            umma_commit_warp(&w_full[it & 1]);
+            if (Gb > 1 || x == G - 1) umma_commit_warp(&empty_b[b_w]);
+        };
+        if (items > 0) transpose(0);
+        bool w_ahead = false;
+        int n = 0, x = 0, na = 0, nb = 0;
+        for (int it = 0; it < items; ++it) {
+            const bool new_b = x == 0 || Gb > 1, new_a = x == 0 || Ga > 1, last = x == G - 1, more = it + 1 < items;
+            const int n1 = last ? n + 1 : n, x1 = last ? 0 : x + 1;      // the next item
+            if (!STATE_ONLY && !w_ahead) w_products(it, x);
+            w_ahead = false;
+            if (x == 0) LT_WAIT_WARP(x_full, n);
+            if (!STATE_ONLY && new_a) {   // the state's share
+                if (na > 0) LT_WAIT_WARP(o_empty, na - 1);
                 tc_fence_after();
 #pragma unroll
-                for (int kk = 0; kk < 8; kk += 2) {
-                    umma_warp(tmem + kLtColT + kk * 16, dmn.at(b16 + sb * t16 + kk * 128), unit, id_t, false);
-                    umma_warp(tmem + kLtColT + kk * 16 + 16, dmn.at(b16 + sb * t16 + kk * 128 + 128), unit, id_t, false);
+                for (int hf = 0; hf < kHalves; ++hf) {
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)
+                        umma_warp(tmem + kLtColO, dk.at(a_w + hf * h16 + 2 * kk), dmn.at(x16 + hf * 512 + kk * 128), id_kn, hf > 0 || kk > 0);
                 }
-                umma_commit_warp(b_full);
-                if (STATE_ONLY) umma_commit_warp(&empty_b[sb]);
-            };
-            if (items > 0) transpose(0, 0);
-            int n = 0, x = 0;
-            for (int it = 0; it < items; ++it) {
-                const int na = Ga > 1 ? it : n, nb = Gb > 1 ? it : n, sb = nb & 1;
-                const bool new_b = x == 0 || Gb > 1, new_a = x == 0 || Ga > 1, last = x == G - 1;
-                const uint32_t aa = a16 + (na & 1) * t16, ca = c16 + (nb & 1) * t16;
-                if (!STATE_ONLY) {
-                    LT_WAIT_WARP(&full_a[na & 1], na >> 1);
-                    LT_WAIT_WARP(&full_b[sb], nb >> 1);
-                    tc_fence_after();
-                    uint32_t xa = aa, ya = b16 + sb * t16;
-#pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf, xa += h16, ya += h16) {
-#pragma unroll
-                        for (int kk = 0; kk < 4; ++kk)
-                            umma_warp(tmem + kLtColW, dk.at(xa + 2 * kk), dk.at(ya + 2 * kk), id_kk, hf > 0 || kk > 0);
-                    }
-                    umma_commit_warp(w_full);
-                    if (Gb > 1 || last) umma_commit_warp(&empty_b[sb]);
-                }
-                if (x == 0) LT_WAIT_WARP(x_full, n);
-                if (!STATE_ONLY && new_a) {   // the state's share
-                    if (na > 0) LT_WAIT_WARP(o_empty, na - 1);
-                    tc_fence_after();
-                    uint32_t xa = aa;
-#pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf, xa += h16) {
-#pragma unroll
-                        for (int kk = 0; kk < 4; ++kk)
-                            umma_warp(tmem + kLtColO, dk.at(xa + 2 * kk), dmn.at(x16 + hf * 512 + kk * 128), id_kn, hf > 0 || kk > 0);
-                    }
-                    if (Gb > 1 || last) umma_commit_warp(x_empty);
-                }
-                // the next tile of B comes with the next item, or with the first one of the next chunk
-                bool next = (Gb > 1 || last) && it + 1 < items;
-                const int nb1 = nb + 1, n1 = last ? n + 1 : n;
-                if (new_b) {   // the chunk's share of the state
-                    LT_WAIT_WARP(&full_c[nb & 1], nb >> 1);
+                if (Gb > 1 || last) umma_commit_warp(x_empty);
+            }
+            if (new_b) {
+                LT_WAIT_WARP(&full_c[rc.s], rc.turn);
+                c_now = base16 + (L::c + rc.s * kLtTile) / 16;
+                c_slot = rc.s;
+                rc.next(2);
+            }
+            bool add = new_b, put = !STATE_ONLY;     // the chunk's share of the state; this item's last product
+            bool next_b = (Gb > 1 || last) && more;  // the next item, or the next chunk's first one, brings a tile of B
+            while (add || put || next_b) {
+                // with several heads of A, P may well be there before B^T has been weighted
+                if (add && !(put && MULTI_A && __all_sync(0xffffffffu, mbar_try_wait(&p_full[it & 1], (it >> 1) & 1)))) {
 #pragma unroll
                     for (int hf = 0; hf < 2; ++hf) {
                         LT_WAIT_WARP(&t_full[hf], nb);
                         tc_fence_after();
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk) {
-                            const uint64_t cd = dmn.at(ca + hf * 512 + kk * 128);
+                            const uint64_t cd = dmn.at(c_now + hf * 512 + kk * 128);
                             umma_warp_ts(tmem + kLtColS, tmem + kLtColT + hf * 64 + kk * 16, cd, id_kn, true);
                             umma_warp_ts(tmem + kLtColS, tmem + kLtColT + hf * 64 + kk * 16 + 8, cd, id_kn, true);
                         }
                     }
                     if (Gb == 1 || last) umma_commit_warp(s_full);
-                    if (STATE_ONLY) umma_commit_warp(&empty_c[nb & 1]);
+                    if (STATE_ONLY) umma_commit_warp(&empty_c[c_slot]);
+                    add = false;
+                    continue;
                 }
-                // the next tile's transposition before this item's last product, if the tile is there
-                if (next && (STATE_ONLY || __all_sync(0xffffffffu, mbar_try_wait(&full_b[nb1 & 1], (nb1 >> 1) & 1)))) {
-                    transpose(nb1, n1);
-                    next = false;
+                // the next tile's transposition before this item's last product, if the tile is there and its place free
+                if (next_b && !add && (!put || (w_col(x) != kLtColT && __all_sync(0xffffffffu, mbar_try_wait(&full_b[rt.s], rt.turn))))) {
+                    transpose(n1);
+                    next_b = false;
+                    continue;
                 }
-                if (!STATE_ONLY) {
-                    LT_WAIT_WARP(p_full, it);
+                // and the next item's W, if it has a place of its own
+                if (MULTI_A && put && more && !add && !w_ahead && w_col(x1) != w_col(x) &&
+                    __all_sync(0xffffffffu, mbar_try_wait(&full_a[ra.s], ra.turn) &&
+                                                (x1 != 0 || mbar_try_wait(&full_b[rb.s], rb.turn)))) {
+                    w_products(it + 1, x1);
+                    w_ahead = true;
+                }
+                if (put) {
+                    LT_WAIT_WARP(&p_full[it & 1], it >> 1);
                     tc_fence_after();
 #pragma unroll
                     for (int hf = 0; hf < 2; ++hf) {
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk)
-                            umma_warp_ts(tmem + kLtColO, tmem + kLtColW + hf * 64 + kk * 8, dmn.at(ca + hf * 512 + kk * 128), id_kn, true);
+                            umma_warp_ts(tmem + kLtColO, tmem + w_col(x) + hf * 64 + kk * 8, dmn.at(c_now + hf * 512 + kk * 128), id_kn, true);
                     }
                     if (Ga > 1 || last) umma_commit_warp(o_full);
-                    if (Gb > 1 || last) umma_commit_warp(&empty_c[nb & 1]);
+                    if (Gb > 1 || last) umma_commit_warp(&empty_c[c_slot]);
+                    put = false;
                 }
-                if (next) transpose(nb1, n1);
-                if (++x == G) x = 0, ++n;
             }
+            na += new_a;
+            nb += new_b;
+            x = x1;
+            n = n1;
         }
         __syncwarp();
     } else if (warp == 2) {
         // =========================== stores ===========================
         if (!STATE_ONLY && lane == 0) {
             const CUtensorMap* map_o = &args.out[which];
-            int na = 0;
+            Ring ra;
             for (int n = 0; n < n_chunks; ++n) {
                 const int t0 = chunk_t0(n);
-                for (int x = 0; x < Ga; ++x, ++na) {
-                    const unsigned char* src = smem + L::a + (na & 1) * kLtTile;
-                    LT_WAIT(&out_full[na & 1], na >> 1);
+                for (int x = 0; x < Ga; ++x) {
+                    const unsigned char* src = smem + a_at(ra.s);
+                    LT_WAIT(&out_full[ra.s], ra.turn);
                     for (int hf = 0; hf < kHalves; ++hf) tma_store_4d(map_o, hf * 64, h * Ga + x, t0, bi, src + hf * kLtHalf);
                     bulk_commit();
                     bulk_wait_read();
-                    mbar_arrive(&empty_a[na & 1]);
+                    mbar_arrive(&empty_a[ra.s]);
+                    ra.next(n_a);
                 }
             }
             bulk_wait_all();
         }
         __syncwarp();
-    } else if (warp == 3) {   // (fills the first group of four)
+    } else if (warp == 3) {
+        // =========================== padding rows behind the last chunk ===========================
+        if (!STATE_ONLY) {
+            constexpr int kRow = D * 2 / 16;   // 16-byte pieces of a row
+            char* out = static_cast<char*>(r.out) + ((size_t)bi * s.T * s.Hkv + h) * Ga * (D * 2);
+            const long long end = (long long)t_end * kRow;
+            for (long long i = (long long)(t_begin + n_chunks * kLtCh) * kRow + lane; i < end; i += 32)
+                for (int x = 0; x < Ga; ++x)
+                    reinterpret_cast<uint4*>(out + ((size_t)(i / kRow) * s.Hkv * Ga + x) * (D * 2))[i % kRow] = make_uint4(0, 0, 0, 0);
+        }
     } else if (warp < 12) {
         // =========================== W -> P: two threads per row i, 64 columns each ===========
         if (!STATE_ONLY) {
             const int q = warp & 3, half = (warp - 4) >> 2, i = q * 32 + lane;
-            const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + kLtColW + half * 64;
+            const uint32_t lane_w = tmem + ((uint32_t)(q * 32) << 16) + half * 64;
             const float* pti = pt + 127 - i;
             const float inv_full = 1.f / f_of(i, kLtCh), inv_last = 1.f / f_of(i, nv_last);
             int it = 0;
@@ -419,7 +474,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 const int nv = chunk_nv(chunk_t0(n));
                 const float inv_f = nv < kLtCh ? inv_last : inv_full;
                 for (int x = 0; x < G; ++x, ++it) {
-                    LT_WAIT(w_full, it);
+                    const uint32_t lane_base = lane_w + (MULTI_A && (x & 1) ? kLtColT : kLtColW);
+                    LT_WAIT(&w_full[it & 1], it >> 1);
                     tc_fence_after();
 #pragma unroll 1
                     for (int e = 0; e < 4; ++e) {   // 16 columns; P takes the place of columns read before
@@ -461,7 +517,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     tmem_wait_st();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(p_full);
+                    if (lane == 0) mbar_arrive(&p_full[it & 1]);
                 }
             }
         }
@@ -470,16 +526,17 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         const int q = warp & 3, half = (warp - 12) >> 2, wt = tid & 127;
         const uint32_t t_col = tmem + ((uint32_t)(q * 32) << 16) + kLtColT + half * 64;
         int nb = 0;
+        Ring rb;
         for (int n = 0; n < n_chunks; ++n) {
             const int nv = chunk_nv(chunk_t0(n));
             const float* w = pt + (reverse ? 128 : kLtCh - nv) + half * 64;   // w_j = w[j], 0 behind the last valid token
             const bool aligned = reverse || (nv & 3) == 0;
             for (int x = 0; x < Gb; ++x, ++nb) {
                 if (nv < kLtCh) {   // padding rows hold anything: zeros in B (this half of the warps) and in C (the other)
-                    LT_WAIT(&full_b[(nb & 1)], (nb >> 1));
+                    LT_WAIT(&full_b[rb.s], rb.turn);
                     LT_WAIT(&full_c[nb & 1], nb >> 1);
                     if (wt >= nv) {
-                        uint4* z = reinterpret_cast<uint4*>(smem + (half ? L::c + (nb & 1) * kLtTile : L::b + (nb & 1) * kLtTile) + wt * 128);
+                        uint4* z = reinterpret_cast<uint4*>(smem + (half ? L::c + (nb & 1) * kLtTile : L::b + rb.s * kLtTile) + wt * 128);
 #pragma unroll
                         for (int j = 0; j < 8 * kHalves; ++j) z[(j & 7) + (j >> 3) * (kLtHalf / 16)] = make_uint4(0, 0, 0, 0);
                     }
@@ -515,6 +572,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&t_full[half]);
+                rb.next(n_b);
             }
         }
     } else {
@@ -525,35 +583,50 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         constexpr int kCols = D / 2;                      // columns of a thread, from hs * kCols on
         const bool has_row = q * 32 < D;                  // (head_dim 64: half of the lanes hold no row of the state)
         const uint32_t s_col = lane_base + kLtColS + hs * kCols;
+        unsigned char* x_row = smem + L::x + (hs * kCols / 64) * (D * 128) + c * 128;
+        constexpr int kPiece = kHalves == 2 ? 0 : 4;      // 16-byte pieces of a 128-byte row before hs = 1's
+        // The state passes through X's place, kVia columns at a time, and every warp keeps to the bytes of X that it writes
+        // itself (another warp may be a step ahead): piece `piece` of the warp's row `row`.
+        constexpr int kVia = D / 4;
+        auto via = [&](int row, int piece) { return x_row + (row - lane) * 128 + (((hs * kPiece + piece) ^ (row & 7)) * 16); };
         if (has_row) {
             const float* src = state_src;
             const float mul = STATE_ONLY || s.nseg > 1 ? 1.f : r.in_mul;
 #pragma unroll 1
-            for (int k = 0; k < kCols / 32; ++k) {
-                float v[32];
+            for (int k = 0; k < kCols / kVia; ++k) {
+                float v[kVia];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = 0.f;
-                if (src != nullptr) {
+                for (int i = 0; i < kVia; ++i) v[i] = 0.f;
+                if (!STATE_ONLY && src != nullptr) {
                     if (r.state_t) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = src[(hs * kCols + k * 32 + i) * D + c];
+                        for (int i = 0; i < kVia; ++i) v[i] = src[(hs * kCols + k * kVia + i) * D + c];
                     } else {
+                        // A thread's row is D * 4 bytes from its neighbour's: read so, the loads held up the whole SM's
+                        // shared-memory pipe for 10 us.  Whole lines come into shared memory, then every thread its row.
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 x = *reinterpret_cast<const float4*>(src + c * D + hs * kCols + k * 32 + 4 * i);
+                        for (int i = 0; i < kVia / 4; ++i) {
+                            const int row = i * (128 / kVia) + lane / (kVia / 4), piece = lane % (kVia / 4);
+                            cp_async16(via(row, piece), src + (q * 32 + row) * D + hs * kCols + k * kVia + piece * 4);
+                        }
+                        cp_async_commit();
+                        cp_async_wait_all();
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < kVia / 4; ++i) {
+                            const float4 x = *reinterpret_cast<const float4*>(via(lane, i));
                             v[4 * i] = x.x, v[4 * i + 1] = x.y, v[4 * i + 2] = x.z, v[4 * i + 3] = x.w;
                         }
+                        __syncwarp();
                     }
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] *= mul;
+                    for (int i = 0; i < kVia; ++i) v[i] *= mul;
                 }
-                tmem_st16u(s_col + k * 32, reinterpret_cast<const uint32_t*>(v));
-                tmem_st16u(s_col + k * 32 + 16, reinterpret_cast<const uint32_t*>(v + 16));
+#pragma unroll
+                for (int i = 0; i < kVia; i += 16) tmem_st16u(s_col + k * kVia + i, reinterpret_cast<const uint32_t*>(v + i));
             }
             tmem_wait_st();
         }
-        unsigned char* x_row = smem + L::x + (hs * kCols / 64) * (D * 128) + c * 128;
-        constexpr int kPiece = kHalves == 2 ? 0 : 4;      // 16-byte pieces of a 128-byte row before hs = 1's
         // Before chunk n: the state as chunk n's operand, and scaled for what chunk n adds.
         auto turn = [&](int n) {
             const float f = lam(chunk_nv(chunk_t0(n)));
@@ -586,6 +659,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         };
         const float f_full = STATE_ONLY ? 0.f : f_of(c, kLtCh) * r.scale, f_last = STATE_ONLY ? 0.f : f_of(c, nv_last) * r.scale;
         int na = 0;
+        Ring ra;
         if (n_chunks > 0) turn(0);
         for (int n = 0; n < n_chunks; ++n) {
             if (STATE_ONLY) {
@@ -599,7 +673,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 if (x == Ga - 1 && n + 1 < n_chunks) turn(n + 1);
                 LT_WAIT(o_full, na);
                 tc_fence_after();
-                unsigned char* dst = smem + L::a + (na & 1) * kLtTile + (hs * kCols / 64) * kLtHalf + c * 128;
+                unsigned char* dst = smem + a_at(ra.s) + (hs * kCols / 64) * kLtHalf + c * 128;
 #pragma unroll 1
                 for (int k = 0; k < kCols / 16; ++k) {
                     float o[16];
@@ -617,7 +691,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&out_full[na & 1]);
+                if (lane == 0) mbar_arrive(&out_full[ra.s]);
+                ra.next(n_a);
             }
         }
         if (n_chunks > 0) {
@@ -639,9 +714,24 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 float x[16];
                 tmem_ld16(s_col + k * 16, x);
 #pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    *reinterpret_cast<float4*>(dst + c * D + hs * kCols + k * 16 + i) =
-                        make_float4(x[i] * mul + poison, x[i + 1] * mul + poison, x[i + 2] * mul + poison, x[i + 3] * mul + poison);
+                for (int i = 0; i < 16; ++i) x[i] = x[i] * mul + poison;
+                if (STATE_ONLY) {   // (no X there, and nothing beside this)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        *reinterpret_cast<float4*>(dst + c * D + hs * kCols + k * 16 + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                } else {            // whole lines again, 16 columns at a time
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<float4*>(via(lane, i)) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int row = i * 8 + lane / 4, piece = lane % 4;
+                        *reinterpret_cast<float4*>(dst + (q * 32 + row) * D + hs * kCols + k * 16 + piece * 4) =
+                            *reinterpret_cast<const float4*>(via(row, piece));
+                    }
+                    __syncwarp();
+                }
             }
         }
     }
@@ -653,18 +743,14 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
-    if (!STATE_ONLY) {   // padding rows behind the last chunk: zeros; after a timeout everything is NaN
-        const bool bad = *abort_flag != 0;
-        const int first = bad ? t_begin : t_begin + n_chunks * kLtCh;
-        const uint32_t fill = bad ? 0x7fc07fc0u : 0u;
-        char* out = static_cast<char*>(r.out);
-        constexpr int kRow = D * 2 / 16;   // 16-byte pieces of a row
-        for (int i = tid; (long long)first + i / kRow < t_end; i += kLtThreads) {
-            const size_t row = (size_t)bi * s.T + first + i / kRow;
+    if (!STATE_ONLY && *abort_flag != 0) {   // after a timeout everything is NaN
+        constexpr int kRow = D * 2 / 16;
+        char* out = static_cast<char*>(r.out) + ((size_t)bi * s.T * s.Hkv + h) * Ga * (D * 2);
+        const long long end = (long long)t_end * kRow;
+        for (long long i = (long long)t_begin * kRow + tid; i < end; i += kLtThreads)
             for (int x = 0; x < Ga; ++x)
-                reinterpret_cast<uint4*>(out + (row * s.Hkv * Ga + (size_t)h * Ga + x) * (D * 2))[i % kRow] =
-                    make_uint4(fill, fill, fill, fill);
-        }
+                reinterpret_cast<uint4*>(out + ((size_t)(i / kRow) * s.Hkv * Ga + x) * (D * 2))[i % kRow] =
+                    make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
     }
 }
 
@@ -683,9 +769,9 @@ bool lt_map(CUtensorMap* map, const void* base, int B, int T, int H, int D) {
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool STATE_ONLY>
+template <int D, bool STATE_ONLY, bool MULTI_A>
 cudaError_t lt_launch(const LtArgs& a, int grid_y, cudaStream_t stream) {
-    auto fn = linear_tc_kernel<D, STATE_ONLY>;
+    auto fn = linear_tc_kernel<D, STATE_ONLY, MULTI_A>;
     const int smem = LtSmem<D, STATE_ONLY>::total;
     static_assert(LtSmem<D, STATE_ONLY>::total <= 232448, "shared memory of a block");
     cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -695,7 +781,7 @@ cudaError_t lt_launch(const LtArgs& a, int grid_y, cudaStream_t stream) {
     return cudaGetLastError();
 }
 
-template <int D>
+template <int D, bool MULTI_A>
 cudaError_t launch_all(const LinArgs& args, const LinStates& states, cudaStream_t stream) {
     LtArgs a;
     a.s = args;
@@ -727,17 +813,19 @@ cudaError_t launch_all(const LinArgs& args, const LinStates& states, cudaStream_
             if (a.st_map_b[d] < 0 || a.st_map_c[d] < 0) return cudaErrorInvalidValue;
         }
         const int dirs = (states.seg[0] != nullptr) + (states.seg[1] != nullptr);
-        cudaError_t e = lt_launch<D, true>(a, dirs, stream);
+        cudaError_t e = lt_launch<D, true, false>(a, dirs, stream);
         if (e == cudaSuccess) e = launch_linear_combine(D, args, states, stream);
         if (e != cudaSuccess) return e;
     }
-    return lt_launch<D, false>(a, args.n_roles, stream);
+    return lt_launch<D, false, MULTI_A>(a, args.n_roles, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_linear_tc(int D, const LinArgs& args, const LinStates& states, cudaStream_t stream) {
-    return D == 128 ? launch_all<128>(args, states, stream) : launch_all<64>(args, states, stream);
+    if (args.role[0].Ga > 1)   // (in every role then)
+        return D == 128 ? launch_all<128, true>(args, states, stream) : launch_all<64, true>(args, states, stream);
+    return D == 128 ? launch_all<128, false>(args, states, stream) : launch_all<64, false>(args, states, stream);
 }
 
 }  // namespace bct
