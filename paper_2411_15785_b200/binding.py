@@ -211,14 +211,6 @@ def _operand(name, t, shape, dtype, dev) -> None:
             "" if t.is_contiguous() else ", strided"))
 
 
-def _io_dtype(name, t) -> int:
-    if t.dtype is torch.bfloat16:
-        return BCT_BF16
-    if t.dtype is not torch.float32:
-        raise ValueError("%s must be float32 or bfloat16 (got %s)" % (name, t.dtype))
-    return BCT_F32
-
-
 def _result(name, t, like, shape, dtype, dev):
     """The caller's buffer, checked, or a new one on the device of `like`."""
     if t is None:
@@ -276,19 +268,33 @@ def _scratch_args(scratch):
     return (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())
 
 
+@functools.lru_cache(maxsize=1024)
+def _linear_sizes(q_shape, k_shape, dtype, n_lead, scale):
+    """What follows from the shapes alone: (sizes, parameters by reference, k's shape, the decays', the state's)."""
+    if len(q_shape) != n_lead + 2 or len(k_shape) != n_lead + 2:
+        raise ValueError("q and k must have %d dimensions" % (n_lead + 2))
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("q must be float32 or bfloat16 (got %s)" % dtype)
+    Hkv, d = k_shape[-2], q_shape[-1]
+    sizes = (q_shape[0], q_shape[-2], Hkv, d, BCT_BF16 if dtype is torch.bfloat16 else BCT_F32)
+    return (sizes, _linear_params(*sizes, scale)[1], torch.Size((*q_shape[:-2], Hkv, d)), torch.Size((Hkv,)),
+            torch.Size((q_shape[0], Hkv, d, d)))
+
+
 def _linear_setup(q, k, v, log_decay, n_lead, scale):
     """Checks the operands that every linear-attention call has: q ``[*lead, Hq, d]``, k and v ``[*lead, Hkv, d]``.
     Returns the sizes, the parameters by reference, the state's shape and the device index."""
-    if q.dim() != n_lead + 2 or k.dim() != n_lead + 2:
-        raise ValueError("q and k must have %d dimensions" % (n_lead + 2))
-    dt, dev, sq, sk = _io_dtype("q", q), q.get_device(), q.shape, k.shape
-    want = (*sq[:-2], sk[-2], sq[-1])
-    _operand("q", q, sq, q.dtype, dev)
-    _operand("k", k, want, q.dtype, dev)
-    _operand("v", v, want, q.dtype, dev)
-    _operand("log_decay", log_decay, (sk[-2],), torch.float32, dev)
-    sizes = (sq[0], sq[-2], sk[-2], sq[-1], dt)
-    return sizes, _linear_params(*sizes, scale)[1], (sq[0], sk[-2], sq[-1], sq[-1]), dev
+    dt, dev = q.dtype, q.get_device()
+    sizes, p, kv, hk, s_shape = _linear_sizes(q.shape, k.shape, dt, n_lead, scale)
+    if not (dev >= 0 and k.shape == kv and v.shape == kv and k.dtype is dt and v.dtype is dt and log_decay.shape == hk
+            and log_decay.dtype is torch.float32 and k.get_device() == dev and v.get_device() == dev
+            and log_decay.get_device() == dev and q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
+            and log_decay.is_contiguous()):
+        _operand("q", q, q.shape, dt, dev)      # one of these says what it is
+        _operand("k", k, kv, dt, dev)
+        _operand("v", v, kv, dt, dev)
+        _operand("log_decay", log_decay, hk, torch.float32, dev)
+    return sizes, p, s_shape, dev
 
 
 def linear_scratch_bytes(batch, T, n_q_heads, n_kv_heads, head_dim, dtype, *, backward=False) -> int:
@@ -303,7 +309,7 @@ def linear_step(q, k, v, log_decay, state, scale=0.0, out=None, state_out=None, 
     lib = load()
     _, p, s_shape, dev = _linear_setup(q, k, v, log_decay, 1, scale)
     _operand("state", state, s_shape, torch.float32, dev)
-    out = _result("out", out, q, q.shape, q.dtype, dev)
+    out = torch.empty_like(q) if out is None else _result("out", out, q, q.shape, q.dtype, dev)
     if state_out is None:
         state_out = state
     else:
@@ -325,8 +331,11 @@ def linear_forward(q, k, v, log_decay, state=None, lens=None, scale=0.0, out=Non
         _operand("state", state, s_shape, torch.float32, dev)
     if lens is not None:
         _operand("lens", lens, q.shape[:1], torch.int32, dev)
-    out = _result("out", out, q, q.shape, q.dtype, dev)
-    state_out = _result("state_out", state_out, q, s_shape, torch.float32, dev)
+    out = torch.empty_like(q) if out is None else _result("out", out, q, q.shape, q.dtype, dev)
+    if state_out is None:
+        state_out = q.new_empty(s_shape, dtype=torch.float32) if state is None else torch.empty_like(state)
+    else:
+        _operand("state_out", state_out, s_shape, torch.float32, dev)
     scratch = _scratch(_linear_scratch(*sizes, T, 0), scratch, q, dev)
     _launch(dev, stream, lib.bct_linear_forward, p, T, q.data_ptr(), k.data_ptr(), v.data_ptr(),
             log_decay.data_ptr(), _ptr(lens), _ptr(state), state_out.data_ptr(), out.data_ptr(), *_scratch_args(scratch))
@@ -359,27 +368,41 @@ def linear_backward(d_out, q, k, v, log_decay, state=None, d_state=None, lens=No
     return d_q, d_k, d_v, d_in
 
 
-def _norm_rotate_setup(q, k, w_q, w_k, positions, freq):
-    if q.dim() < 3 or k.dim() != q.dim():
+@functools.lru_cache(maxsize=1024)
+def _norm_rotate_sizes(q_shape, k_shape, dtype, half):
+    """What follows from the shapes alone: (tokens, Hq, Hkv, d, dtype code, rotated features), k's shape, the tokens'."""
+    if len(q_shape) < 3 or len(k_shape) != len(q_shape):
         raise ValueError("q and k must be [..., heads, head_dim] with at least one token dimension")
-    lead, d, dt, dev = tuple(q.shape[:-2]), q.shape[-1], _io_dtype("q", q), q.get_device()
-    Hq, Hkv = q.shape[-2], k.shape[-2]
-    _operand("q", q, q.shape, q.dtype, dev)
-    _operand("k", k, (*lead, Hkv, d), q.dtype, dev)
-    for name, w in (("w_q", w_q), ("w_k", w_k)):
-        if w is not None:
-            _operand(name, w, (d,), q.dtype, dev)
-    rot = 0
-    if freq is not None:
-        rot = 2 * freq.numel()
-        _operand("freq", freq, (rot // 2,), torch.float64, dev)
-        if positions is None:
-            raise ValueError("positions are needed where freq is given")
-        _operand("positions", positions, lead, torch.int64, dev)
-    n = 1
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("q must be float32 or bfloat16 (got %s)" % dtype)
+    lead, d, n = q_shape[:-2], q_shape[-1], 1
     for x in lead:
         n *= x
-    return n, Hq, Hkv, d, dt, rot
+    sizes = (n, q_shape[-2], k_shape[-2], d, BCT_BF16 if dtype is torch.bfloat16 else BCT_F32, 2 * half)
+    return sizes, torch.Size((*lead, k_shape[-2], d)), torch.Size(lead), torch.Size((d,))
+
+
+def _norm_rotate_setup(q, k, w_q, w_k, positions, freq):
+    dt, dev = q.dtype, q.get_device()
+    half = 0 if freq is None else freq.numel()
+    sizes, ks, lead, wd = _norm_rotate_sizes(q.shape, k.shape, dt, half)
+    if half and positions is None:
+        raise ValueError("positions are needed where freq is given")
+    if not (dev >= 0 and k.shape == ks and k.dtype is dt and k.get_device() == dev and q.is_contiguous() and k.is_contiguous()
+            and (w_q is None or (w_q.shape == wd and w_q.dtype is dt and w_q.get_device() == dev and w_q.is_contiguous()))
+            and (w_k is None or (w_k.shape == wd and w_k.dtype is dt and w_k.get_device() == dev and w_k.is_contiguous()))
+            and (not half or (positions.shape == lead and positions.dtype is torch.int64 and positions.get_device() == dev
+                              and positions.is_contiguous() and freq.dim() == 1 and freq.dtype is torch.float64
+                              and freq.get_device() == dev and freq.is_contiguous()))):
+        _operand("q", q, q.shape, dt, dev)      # one of these says what it is
+        _operand("k", k, ks, dt, dev)
+        for name, w in (("w_q", w_q), ("w_k", w_k)):
+            if w is not None:
+                _operand(name, w, wd, dt, dev)
+        if half:
+            _operand("freq", freq, (half,), torch.float64, dev)
+            _operand("positions", positions, lead, torch.int64, dev)
+    return sizes
 
 
 def norm_rotate(q, k, w_q, w_k, positions, freq, eps=1e-6, interleaved=False, out=None, stream=None):
@@ -390,8 +413,12 @@ def norm_rotate(q, k, w_q, w_k, positions, freq, eps=1e-6, interleaved=False, ou
     lib = load()
     n, Hq, Hkv, d, dt, rot = _norm_rotate_setup(q, k, w_q, w_k, positions, freq)
     dev = q.get_device()
-    q_out, k_out = (None, None) if out is None else out
-    q_out, k_out = _result("q_out", q_out, q, q.shape, q.dtype, dev), _result("k_out", k_out, q, k.shape, q.dtype, dev)
+    if out is None:
+        q_out, k_out = torch.empty_like(q), torch.empty_like(k)
+    else:
+        q_out, k_out = out
+        _operand("q_out", q_out, q.shape, q.dtype, dev)
+        _operand("k_out", k_out, k.shape, q.dtype, dev)
     _launch(dev, stream, lib.bct_norm_rotate, n, Hq, Hkv, d, dt, q.data_ptr(), k.data_ptr(), _ptr(w_q), _ptr(w_k), eps,
             _ptr(positions) if rot else None, _ptr(freq) if rot else None, rot, ROTATE_INTERLEAVED if interleaved else 0,
             q_out.data_ptr(), k_out.data_ptr())

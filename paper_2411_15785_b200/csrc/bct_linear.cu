@@ -351,7 +351,8 @@ template <int D, bool STATE_ONLY>
 cudaError_t launch_scan(const LinArgs& args, const LinStates& st, int grid_y, cudaStream_t stream) {
     auto fn = linear_scan_kernel<D, STATE_ONLY>;
     const int smem = (int)sizeof(ScanSmem<D>);
-    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static std::atomic<unsigned long long> allowed{0};
+    cudaError_t e = allow_smem(reinterpret_cast<const void*>(fn), smem, allowed);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)(args.B * args.Hkv * args.nseg * (D / kNc)), (unsigned)grid_y);
     fn<<<grid, kScanThreads, smem, stream>>>(args, st);

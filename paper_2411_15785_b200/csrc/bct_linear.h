@@ -4,9 +4,23 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/bct.h"
 
 namespace bct {
+
+// Dynamic shared memory beyond 48 KiB has to be allowed once per kernel and device; `done` is the kernel's own record of
+// the devices where it has been (a microsecond of every call otherwise).
+inline cudaError_t allow_smem(const void* fn, int bytes, std::atomic<unsigned long long>& done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1)) return cudaSuccess;
+    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+    return e;
+}
 
 // One scan over the tokens of every (sequence, kv-head) unit.  All three passes of the backward have the
 // forward's form, with other tensors in the three roles:

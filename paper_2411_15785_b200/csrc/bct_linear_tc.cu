@@ -774,7 +774,8 @@ cudaError_t lt_launch(const LtArgs& a, int grid_y, cudaStream_t stream) {
     auto fn = linear_tc_kernel<D, STATE_ONLY, MULTI_A>;
     const int smem = LtSmem<D, STATE_ONLY>::total;
     static_assert(LtSmem<D, STATE_ONLY>::total <= 232448, "shared memory of a block");
-    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static std::atomic<unsigned long long> allowed{0};
+    cudaError_t e = allow_smem(reinterpret_cast<const void*>(fn), smem, allowed);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)(a.s.B * a.s.Hkv * a.s.nseg), (unsigned)grid_y);
     fn<<<grid, kLtThreads, smem, stream>>>(a);

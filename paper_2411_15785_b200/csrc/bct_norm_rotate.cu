@@ -284,7 +284,8 @@ int nr_grid(int64_t n_tokens, int parts, int per_sm) {
 template <typename T, int D, bool BWD, bool INTER>
 cudaError_t nr_launch_kernel(const NrArgs& a, int grid, cudaStream_t stream) {
     auto fn = norm_rotate_kernel<T, D, BWD, INTER>;
-    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, kNrSmem);
+    static std::atomic<unsigned long long> allowed{0};
+    cudaError_t e = allow_smem(reinterpret_cast<const void*>(fn), kNrSmem, allowed);
     if (e != cudaSuccess) return e;
     fn<<<grid, kNrThreads, kNrSmem, stream>>>(a);
     return cudaGetLastError();
