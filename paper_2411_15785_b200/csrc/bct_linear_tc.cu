@@ -55,11 +55,12 @@ struct LtArgs {
 };
 
 template <int D, bool STATE_ONLY>
-struct LtSmem {   // two buffers of every tile; everything else is kept small enough for that
+struct LtSmem {   // two buffers of every tile (three without A); everything else is kept small enough for that
     static constexpr int kLtTile = D / 64 * kLtHalf;   // bytes of a tile
+    static constexpr int kBc = STATE_ONLY ? 3 : 2;     // buffers of B and of C
     static constexpr int b = 0;
-    static constexpr int c = b + 2 * kLtTile;
-    static constexpr int a = c + 2 * kLtTile;
+    static constexpr int c = b + kBc * kLtTile;
+    static constexpr int a = c + kBc * kLtTile;
     static constexpr int x = a + (STATE_ONLY ? 0 : 2 * kLtTile);   // the state as an operand: rows = features of b
     static constexpr int unit = x + (STATE_ONLY ? 0 : D * D * 2);  // 16 x 16 unit matrix
     static constexpr int bars = unit + 512;
@@ -153,13 +154,13 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     uint64_t* full_a = bars;             // [3]
     uint64_t* empty_a = bars + 3;        // [3] the output that took A's place has been read out
     uint64_t* out_full = bars + 6;       // [3] the output is in A's place
-    uint64_t* full_b = bars + 9;         // [2]
-    uint64_t* empty_b = bars + 11;       // [2]
+    uint64_t* full_b = STATE_ONLY ? bars : bars + 9;        // [2] (without A: [3], in the place of the three above)
+    uint64_t* empty_b = STATE_ONLY ? bars + 3 : bars + 11;
     uint64_t* full_c = bars + 13;        // [2]
-    uint64_t* empty_c = bars + 15;       // [2]
+    uint64_t* empty_c = STATE_ONLY ? bars + 6 : bars + 15;
     uint64_t* clean = bars + 17;         // padding rows of B and C are zeros
     uint64_t* b_full = bars + 18;        // B^T complete
-    uint64_t* t_full = bars + 19;        // [2] its terms in place, by halves of j
+    uint64_t* t_full = bars + 19;        // its terms in place
     uint64_t* w_full = bars + 21;        // [2] W complete, by items in turn
     uint64_t* p_full = bars + 23;        // [2] P in place
     uint64_t* o_full = bars + 25;
@@ -202,19 +203,21 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         for (int i = 0; i < 3; ++i) {
             mbar_init(&full_a[i], 1);
             mbar_init(&empty_a[i], 1);
-            mbar_init(&out_full[i], 8);
+            mbar_init(&out_full[i], STATE_ONLY ? 1 : 8);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&full_b[i], 1);
-            mbar_init(&empty_b[i], 1);
-            mbar_init(&full_c[i], 1);
-            mbar_init(&empty_c[i], 1);
-            mbar_init(&t_full[i], 4);
+            if (!STATE_ONLY) {
+                mbar_init(&full_b[i], 1);
+                mbar_init(&empty_b[i], 1);
+                mbar_init(&full_c[i], 1);
+                mbar_init(&empty_c[i], 1);
+            }
             mbar_init(&w_full[i], 1);
             mbar_init(&p_full[i], 8);
         }
         mbar_init(clean, 8);
         mbar_init(b_full, 1);
+        mbar_init(t_full, 8);
         mbar_init(o_full, 1);
         mbar_init(o_empty, 8);
         mbar_init(s_full, 1);
@@ -252,12 +255,19 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         __syncwarp();                \
     }
 
+    // Where the nb-th tile of B is transposed, and its barriers.  Where nothing but the state is formed, W's place and
+    // barriers make a second one: the next tile is transposed while this one's terms are formed.
+    auto t_place = [&](int nb) { return STATE_ONLY && (nb & 1) ? kLtColW : kLtColT; };
+    auto bt_full = [&](int nb) { return STATE_ONLY ? &w_full[nb & 1] : b_full; };
+    auto terms_full = [&](int nb) { return STATE_ONLY ? &p_full[nb & 1] : t_full; };
+    auto bt_turn = [&](int nb) { return STATE_ONLY ? nb >> 1 : nb; };
+
     // (Loops are kept short where that costs nothing: 26 warps of six roles share the instruction caches, and straight-line
     // code that is run once per chunk is fetched anew each time.)
     const int items = n_chunks * G;   // (chunk, head) in turn: head x of the side that has G of them
     // Buffers: two of every tile; with several heads on A's side, whose tiles then turn over fastest, B's second one is a
     // third of A's.
-    constexpr int n_a = !STATE_ONLY && MULTI_A ? 3 : 2, n_b = !STATE_ONLY && MULTI_A ? 1 : 2;
+    constexpr int n_a = MULTI_A ? 3 : 2, n_b = MULTI_A ? 1 : L::kBc;
     struct Ring {   // a place in a ring of buffers and the parity of its turn
         int s = 0;
         uint32_t turn = 0;
@@ -269,9 +279,12 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     if (warp == 1) {
         // =========================== loads ===========================
         if (lane == 0) {
+            auto copy = [&](const CUtensorMap* map, int head, int t0, unsigned char* dst, uint64_t* bar) {
+                for (int hf = 0; hf < kHalves; ++hf) tma_load_4d(dst + hf * kLtHalf, map, hf * 64, head, t0, bi, bar);
+            };
             auto load = [&](const CUtensorMap* map, int head, int t0, unsigned char* dst, uint64_t* bar) {
                 mbar_arrive_expect_tx(bar, kLtTile);
-                for (int hf = 0; hf < kHalves; ++hf) tma_load_4d(dst + hf * kLtHalf, map, hf * 64, head, t0, bi, bar);
+                copy(map, head, t0, dst, bar);
             };
             Ring ra, rb, rc;
             for (int n = 0; n < n_chunks; ++n) {
@@ -279,6 +292,21 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 for (int x = 0; x < G; ++x) {
                     const bool new_b = x == 0 || Gb > 1, new_a = !STATE_ONLY && (x == 0 || Ga > 1);
                     const int hb = h * Gb + (Gb > 1 ? x : 0);
+                    if (!MULTI_A) {   // one barrier for B and C: every wait costs the warp that issues the products
+                        uint64_t* full = &full_b[rb.s];
+                        LT_WAIT(&empty_b[rb.s], rb.turn ^ 1);
+                        mbar_arrive_expect_tx(full, 2 * kLtTile);
+                        copy(map_b, hb, t0, smem + L::b + rb.s * kLtTile, full);
+                        LT_WAIT(&empty_c[rb.s], rb.turn ^ 1);
+                        copy(map_c, hb, t0, smem + L::c + rb.s * kLtTile, full);
+                        rb.next(n_b);
+                        if (new_a) {   // (A's buffer is the last to be free: the output goes out of it)
+                            LT_WAIT(&empty_a[ra.s], ra.turn ^ 1);
+                            load(map_a, h, t0, smem + L::a + ra.s * kLtTile, &full_a[ra.s]);
+                            ra.next(n_a);
+                        }
+                        continue;
+                    }
                     if (new_b) {
                         LT_WAIT(&empty_b[rb.s], rb.turn ^ 1);
                         load(map_b, hb, t0, smem + L::b + rb.s * kLtTile, &full_b[rb.s]);
@@ -309,7 +337,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         const uint64_t unit = (smem_desc(0, 128, 256) & ~((uint64_t)7 << 61)) + base16 + L::unit / 16;
         constexpr uint32_t h16 = kLtHalf / 16;
         const int n_short = nv_last == kLtCh ? -1 : (reverse ? 0 : n_chunks - 1);   // the chunk with padding rows
-        int n_clean = 0;
+        int n_clean = 0, n_t = 0;   // padded tiles, and tiles of B transposed so far
         Ring ra, rb, rt, rc;   // A and B as W takes them, B as its transposition does, C
         uint32_t a_w = 0, b_w = 0, c_now = 0;
         int c_slot = 0;
@@ -321,8 +349,9 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             tc_fence_after();
             const uint32_t ba = base16 + (L::b + rt.s * kLtTile) / 16;
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk) umma_warp(tmem + kLtColT + kk * 16, dmn.at(ba + kk * 128), unit, id_t, false);
-            umma_commit_warp(b_full);
+            for (int kk = 0; kk < 8; ++kk) umma_warp(tmem + t_place(n_t) + kk * 16, dmn.at(ba + kk * 128), unit, id_t, false);
+            umma_commit_warp(bt_full(n_t));
+            ++n_t;
             if (STATE_ONLY) umma_commit_warp(&empty_b[rt.s]);
             rt.next(n_b);
         };
@@ -352,7 +381,84 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             umma_commit_warp(&w_full[it & 1]);
             if (Gb > 1 || x == G - 1) umma_commit_warp(&empty_b[b_w]);
         };
+        auto state_products = [&](int nb, uint32_t ca) {
+            LT_WAIT_WARP(terms_full(nb), bt_turn(nb));
+            tc_fence_after();
+            const uint32_t ta = tmem + t_place(nb);
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) {
+                const uint64_t cd = dmn.at(ca + kk * 128);
+                umma_warp_ts(tmem + kLtColS, ta + kk * 16, cd, id_kn, true);
+                umma_warp_ts(tmem + kLtColS, ta + kk * 16 + 8, cd, id_kn, true);
+            }
+        };
         if (items > 0) transpose(0);
+        if constexpr (!MULTI_A) {
+            // An item's C has come with its B, which has been transposed.
+            int na = 0, x = 0;
+            for (int n = 0, it = 0; it < items; ++it) {
+                const bool last = x == G - 1;
+                const uint32_t ba = base16 + (L::b + rc.s * kLtTile) / 16, ca = base16 + (L::c + rc.s * kLtTile) / 16;
+                const uint32_t aa = base16 + (L::a + (n & 1) * kLtTile) / 16;
+                const int bc = rc.s;
+                rc.next(n_b);
+                if (STATE_ONLY) {
+                    bool next = it + 1 < items;
+                    if (next && __all_sync(0xffffffffu, mbar_try_wait(&full_b[rt.s], rt.turn))) {
+                        transpose(last ? n + 1 : n);
+                        next = false;
+                    }
+                    if (x == 0) LT_WAIT_WARP(x_full, n);
+                    state_products(it, ca);
+                    umma_commit_warp(&empty_c[bc]);
+                    if (last) umma_commit_warp(s_full);
+                    if (next) transpose(last ? n + 1 : n);
+                } else {
+                    if (x == 0) {
+                        LT_WAIT_WARP(&full_a[n & 1], n >> 1);
+                        tc_fence_after();
+                    }
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t o = (kk >> 2) * h16 + (kk & 3) * 2;
+                        umma_warp(tmem + kLtColW, dk.at(aa + o), dk.at(ba + o), id_kk, kk > 0);
+                    }
+                    umma_commit_warp(&w_full[it & 1]);
+                    umma_commit_warp(&empty_b[bc]);
+                    if (x == 0) {   // the state's share.  (X of chunk n is in place before the output of chunk n - 1 is read.)
+                        if (na > 0)
+                            LT_WAIT_WARP(o_empty, na - 1)
+                        else
+                            LT_WAIT_WARP(x_full, 0)
+                        ++na;
+                        tc_fence_after();
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk)
+                            umma_warp(tmem + kLtColO, dk.at(aa + (kk >> 2) * h16 + (kk & 3) * 2), dmn.at(x16 + kk * 128), id_kn, kk > 0);
+                    }
+                    state_products(it, ca);
+                    if (last) umma_commit_warp(s_full);
+                    // the next tile's transposition before this item's last product, if its tiles are there
+                    bool next = it + 1 < items;
+                    if (next && __all_sync(0xffffffffu, mbar_try_wait(&full_b[rt.s], rt.turn))) {
+                        transpose(last ? n + 1 : n);
+                        next = false;
+                    }
+                    LT_WAIT_WARP(&p_full[it & 1], it >> 1);
+                    tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        umma_warp_ts(tmem + kLtColO, tmem + kLtColW + (kk >> 2) * 64 + (kk & 3) * 8, dmn.at(ca + kk * 128), id_kn, true);
+                    if (last) umma_commit_warp(o_full);
+                    umma_commit_warp(&empty_c[bc]);
+                    if (next) transpose(last ? n + 1 : n);
+                }
+                if (last)
+                    x = 0, ++n;
+                else
+                    ++x;
+            }
+        } else {
         bool w_ahead = false;
         int n = 0, x = 0, na = 0, nb = 0;
         for (int it = 0; it < items; ++it) {
@@ -383,17 +489,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             while (add || put || next_b) {
                 // with several heads of A, P may well be there before B^T has been weighted
                 if (add && !(put && MULTI_A && __all_sync(0xffffffffu, mbar_try_wait(&p_full[it & 1], (it >> 1) & 1)))) {
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {
-                        LT_WAIT_WARP(&t_full[hf], nb);
-                        tc_fence_after();
-#pragma unroll
-                        for (int kk = 0; kk < 4; ++kk) {
-                            const uint64_t cd = dmn.at(c_now + hf * 512 + kk * 128);
-                            umma_warp_ts(tmem + kLtColS, tmem + kLtColT + hf * 64 + kk * 16, cd, id_kn, true);
-                            umma_warp_ts(tmem + kLtColS, tmem + kLtColT + hf * 64 + kk * 16 + 8, cd, id_kn, true);
-                        }
-                    }
+                    state_products(nb, c_now);
                     if (Gb == 1 || last) umma_commit_warp(s_full);
                     if (STATE_ONLY) umma_commit_warp(&empty_c[c_slot]);
                     add = false;
@@ -430,6 +526,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             nb += new_b;
             x = x1;
             n = n1;
+        }
         }
         __syncwarp();
     } else if (warp == 2) {
@@ -524,7 +621,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     } else if (warp < 20) {
         // =========================== w o B^T in two terms: two threads per feature of b, 64 tokens each ===========
         const int q = warp & 3, half = (warp - 12) >> 2, wt = tid & 127;
-        const uint32_t t_col = tmem + ((uint32_t)(q * 32) << 16) + kLtColT + half * 64;
+        const uint32_t lane_half = tmem + ((uint32_t)(q * 32) << 16) + half * 64;
         int nb = 0;
         Ring rb;
         for (int n = 0; n < n_chunks; ++n) {
@@ -534,9 +631,9 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             for (int x = 0; x < Gb; ++x, ++nb) {
                 if (nv < kLtCh) {   // padding rows hold anything: zeros in B (this half of the warps) and in C (the other)
                     LT_WAIT(&full_b[rb.s], rb.turn);
-                    LT_WAIT(&full_c[nb & 1], nb >> 1);
+                    if (MULTI_A) LT_WAIT(&full_c[nb & 1], nb >> 1);
                     if (wt >= nv) {
-                        uint4* z = reinterpret_cast<uint4*>(smem + (half ? L::c + (nb & 1) * kLtTile : L::b + rb.s * kLtTile) + wt * 128);
+                        uint4* z = reinterpret_cast<uint4*>(smem + (half ? L::c + (MULTI_A ? nb & 1 : rb.s) * kLtTile : L::b + rb.s * kLtTile) + wt * 128);
 #pragma unroll
                         for (int j = 0; j < 8 * kHalves; ++j) z[(j & 7) + (j >> 3) * (kLtHalf / 16)] = make_uint4(0, 0, 0, 0);
                     }
@@ -544,7 +641,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     __syncwarp();
                     if (lane == 0) mbar_arrive(clean);
                 }
-                LT_WAIT(b_full, nb);
+                LT_WAIT(bt_full(nb), bt_turn(nb));
+                const uint32_t t_col = lane_half + t_place(nb);
                 tc_fence_after();
 #pragma unroll 1
                 for (int e = q * 32 < D ? 0 : 4; e < 4; ++e) {   // (lanes without a feature only take part in the barriers)
@@ -571,7 +669,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&t_full[half]);
+                if (lane == 0) mbar_arrive(terms_full(nb));
                 rb.next(n_b);
             }
         }
@@ -632,7 +730,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             const float f = lam(chunk_nv(chunk_t0(n)));
             if (n > 0) {
                 LT_WAIT(s_full, n - 1);
-                if (!STATE_ONLY) LT_WAIT(x_empty, n - 1);
+                if (MULTI_A) LT_WAIT(x_empty, n - 1);   // (otherwise the state's products are the later ones)
                 tc_fence_after();
             }
 #pragma unroll 1
