@@ -51,6 +51,21 @@ __device__ __forceinline__ uint4 ldg16(const T* p) {
     return *reinterpret_cast<const uint4*>(p);
 }
 
+// 16 bytes as pairs of floats, and back
+__device__ __forceinline__ void unpack2(const uint4& w, float2 (&x)[4]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+}
+__device__ __forceinline__ void unpack2(const uint4& w, float2 (&x)[2]) {
+    x[0] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+    x[1] = make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack2s(const float2* x) {
+    return Chunk<T>::pack(reinterpret_cast<const float*>(x));
+}
+
 template <typename T, int D, bool BWD, bool INTER>
 __global__ void __launch_bounds__(kNrThreads, 2) norm_rotate_kernel(const NrArgs a) {
     constexpr int kE = Chunk<T>::kElems;          // features of a lane
@@ -71,7 +86,10 @@ __global__ void __launch_bounds__(kNrThreads, 2) norm_rotate_kernel(const NrArgs
     const bool in = e0 < a.rot, first = e0 < half;
     // where a feature's partner is: the next feature, or the same place of the lane half the rotated part away
     const int partner = !in || INTER ? lane : (first ? lane + half / kE : lane - half / kE);
-    auto partner_of = [&](const float* x, int i) { return INTER ? x[i ^ 1] : __shfl_sync(0xffffffffu, x[i], partner); };
+    auto partners_of = [&](float2 x) {
+        return INTER ? make_float2(x.y, x.x)
+                     : make_float2(__shfl_sync(0xffffffffu, x.x, partner), __shfl_sync(0xffffffffu, x.y, partner));
+    };
 
     // A warp's items: a token, or one of `parts` shares of it.  (With more than one part there are few tokens, so that
     // items count below 2^31 either way.)  An item's heads come in batches, those of q, then those of k.
@@ -130,7 +148,7 @@ __global__ void __launch_bounds__(kNrThreads, 2) norm_rotate_kernel(const NrArgs
             w_raw[s] = Chunk<T>::pack(one);
         }
     }
-    float dw[2][kE] = {};
+    float2 dw[2][kE / 2] = {};
     int64_t pos = cur.item < items && half > 0 ? a.positions[cur.t] : 0;
     int stage = 0;
     uint32_t phase = 0;
@@ -151,30 +169,27 @@ __global__ void __launch_bounds__(kNrThreads, 2) norm_rotate_kernel(const NrArgs
         }
         __syncwarp();
         // The turn is one multiply-add per feature, x_i c_i + x_partner s_i with the partner's sign in s; features that
-        // are not turned have c = 1, s = 0.  Forward, the weights are in both.
-        float tc[kE], ts[kE];
+        // are not turned have c = 1, s = 0.  Forward, the weights are in both.  (Two features to an instruction throughout:
+        // the backward is bound by the issue of instructions.)
+        float2 tc[kE / 2], ts[kE / 2];
         int have = -1;
         for (; cur.batch < nb; cur.batch += a.parts) {
             const bool s = cur.batch >= nbq;
             const int h0 = (s ? cur.batch - nbq : cur.batch) * kBatch, H = s ? a.H[1] : a.H[0];
-            float w[kE];
-            if (BWD || have != (int)s) Chunk<T>::unpack(s ? w_raw[1] : w_raw[0], w);
+            float2 w[kE / 2];
+            if (BWD || have != (int)s) unpack2(s ? w_raw[1] : w_raw[0], w);
             if (BWD ? have < 0 : have != (int)s) {
                 have = s;
 #pragma unroll
-                for (int i = 0; i < kE; ++i) {
-                    const int f = INTER ? (e0 + i) >> 1 : (first ? e0 + i : e0 + i - half);
-                    const float2 v = in ? cs[f] : make_float2(1.f, 0.f);
-                    const bool minus = (INTER ? (i & 1) == 0 : first) != BWD;
-                    tc[i] = v.x;
-                    ts[i] = minus ? -v.y : v.y;
-                }
-                if (!BWD) {
-#pragma unroll
-                    for (int i = 0; i < kE; ++i) {
-                        const float wp = partner_of(w, i);
-                        tc[i] *= w[i];
-                        ts[i] *= wp;
+                for (int i = 0; i < kE / 2; ++i) {
+                    const int f = first || INTER ? e0 + 2 * i : e0 + 2 * i - half;
+                    const float2 u = in ? cs[INTER ? f >> 1 : f] : make_float2(1.f, 0.f);
+                    const float2 v = INTER ? u : (in ? cs[f + 1] : make_float2(1.f, 0.f));
+                    tc[i] = make_float2(u.x, v.x);
+                    ts[i] = make_float2((INTER || first) != BWD ? -u.y : u.y, (!INTER && first) != BWD ? -v.y : v.y);
+                    if (!BWD) {
+                        tc[i] = __fmul2_rn(tc[i], w[i]);
+                        ts[i] = __fmul2_rn(ts[i], partners_of(w[i]));
                     }
                 }
             }
@@ -184,45 +199,46 @@ __global__ void __launch_bounds__(kNrThreads, 2) norm_rotate_kernel(const NrArgs
             T* ys = static_cast<T*>(s ? a.y[1] : a.y[0]) + ((size_t)cur.t * H + h0 + hl) * D + e0;
             const int passes = min(kP, (H - h0 + kHeads - 1) / kHeads);
 #pragma unroll 2
-            for (int p = 0; p < passes; ++p) {   // (lanes of heads past the last one work on what the stage held before)
-                float x[kE], g[kE];
-                Chunk<T>::unpack(*reinterpret_cast<const uint4*>(src + p * 512), x);
-                if (BWD) Chunk<T>::unpack(*reinterpret_cast<const uint4*>(src + kNrStageBytes / 2 + p * 512), g);
+            for (int p = 0; p < passes; ++p) {   // (lanes of heads past the last one work on zeros)
                 const bool valid = h0 + p * kHeads + hl < H;
-                float ss = 0.f;
+                float2 x[kE / 2], g[kE / 2], y[kE / 2];
+                unpack2(valid ? *reinterpret_cast<const uint4*>(src + p * 512) : make_uint4(0, 0, 0, 0), x);
+                if (BWD) unpack2(valid ? *reinterpret_cast<const uint4*>(src + kNrStageBytes / 2 + p * 512) : make_uint4(0, 0, 0, 0), g);
+                float2 ss2 = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int j = 0; j < kE; ++j) ss = fmaf(x[j], x[j], ss);
+                for (int j = 0; j < kE / 2; ++j) ss2 = __ffma2_rn(x[j], x[j], ss2);
+                float ss = ss2.x + ss2.y;
 #pragma unroll
                 for (int m = kLanes / 2; m > 0; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
                 float r = rsqrtf(ss * (1.f / D) + a.eps);
                 if (!came) r = __int_as_float(0x7fc00000);   // the copy never came: NaN, not old bytes
-                const float* v = BWD ? g : x;
-                float y[kE];
+                const float2 rr = make_float2(r, r);
+                const float2* v = BWD ? g : x;
 #pragma unroll
-                for (int j = 0; j < kE; ++j) y[j] = fmaf(partner_of(v, j), ts[j], v[j] * tc[j]);
+                for (int j = 0; j < kE / 2; ++j) y[j] = __ffma2_rn(partners_of(v[j]), ts[j], __fmul2_rn(v[j], tc[j]));
                 if (!BWD) {
 #pragma unroll
-                    for (int j = 0; j < kE; ++j) y[j] *= r;
+                    for (int j = 0; j < kE / 2; ++j) y[j] = __fmul2_rn(y[j], rr);
                 } else {
-                    float dot = 0.f;
+                    float2 d2 = make_float2(0.f, 0.f);
 #pragma unroll
-                    for (int j = 0; j < kE; ++j) {
-                        x[j] *= r;
-                        const float gx = valid ? y[j] * x[j] : 0.f;
+                    for (int j = 0; j < kE / 2; ++j) {
+                        x[j] = __fmul2_rn(x[j], rr);
                         if (!s)
-                            dw[0][j] += gx;
+                            dw[0][j] = __ffma2_rn(y[j], x[j], dw[0][j]);
                         else
-                            dw[1][j] += gx;
-                        y[j] *= w[j];
-                        dot = fmaf(y[j], x[j], dot);
+                            dw[1][j] = __ffma2_rn(y[j], x[j], dw[1][j]);
+                        y[j] = __fmul2_rn(y[j], w[j]);
+                        d2 = __ffma2_rn(y[j], x[j], d2);
                     }
+                    float dot = d2.x + d2.y;
 #pragma unroll
                     for (int m = kLanes / 2; m > 0; m >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, m);
-                    dot *= 1.f / D;
+                    dot *= -(1.f / D);
 #pragma unroll
-                    for (int j = 0; j < kE; ++j) y[j] = r * (y[j] - x[j] * dot);
+                    for (int j = 0; j < kE / 2; ++j) y[j] = __fmul2_rn(rr, __ffma2_rn(x[j], make_float2(dot, dot), y[j]));
                 }
-                if (valid) *reinterpret_cast<uint4*>(ys + (size_t)p * kHeads * D) = Chunk<T>::pack(y);
+                if (valid) *reinterpret_cast<uint4*>(ys + (size_t)p * kHeads * D) = pack2s<T>(y);
             }
             __syncwarp();   // the stage has been read
             if (ahead.item < items) {
@@ -241,7 +257,7 @@ __global__ void __launch_bounds__(kNrThreads, 2) norm_rotate_kernel(const NrArgs
         for (int s = 0; s < 2; ++s) {
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < kE; ++j) red[(threadIdx.x / kLanes) * D + e0 + j] = dw[s][j];
+            for (int j = 0; j < kE / 2; ++j) *reinterpret_cast<float2*>(&red[(threadIdx.x / kLanes) * D + e0 + 2 * j]) = dw[s][j];
             __syncthreads();
             for (int e = threadIdx.x; e < D; e += kNrThreads) {
                 float sum = 0.f;
