@@ -42,8 +42,9 @@ constexpr int kLtHalf = 128 * 128;            // 64 columns (128 bytes) x 128 ro
 constexpr int kLtColW = 0;     // W, then P (bfloat16 pairs) in the first half of each of its 64-column halves
 constexpr int kLtColO = 128;
 constexpr int kLtColS = 256;   // the state [feature of b][feature of c]
-constexpr int kLtColT = 384;   // B^T [feature of b][j]; of every 16 columns 8 then hold the first terms, 8 the second.
-                               // With several heads of A to a state also every other head's W and P
+constexpr int kLtColT = 384;   // B^T [feature of b][j] of half a tile, 64 columns; of every 16 of them 8 then hold the first
+                               // terms, 8 the second, and 32 columns behind them the third.  With several heads of A to a
+                               // state also every other head's W and P
 
 struct LtArgs {
     CUtensorMap in[4];    // forward: q, k, v;  backward: d_out, q, k, v
@@ -255,12 +256,12 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         __syncwarp();                \
     }
 
-    // Where the nb-th tile of B is transposed, and its barriers.  Where nothing but the state is formed, W's place and
-    // barriers make a second one: the next tile is transposed while this one's terms are formed.
-    auto t_place = [&](int nb) { return STATE_ONLY && (nb & 1) ? kLtColW : kLtColT; };
-    auto bt_full = [&](int nb) { return STATE_ONLY ? &w_full[nb & 1] : b_full; };
-    auto terms_full = [&](int nb) { return STATE_ONLY ? &p_full[nb & 1] : t_full; };
-    auto bt_turn = [&](int nb) { return STATE_ONLY ? nb >> 1 : nb; };
+    // Where the hb-th half tile of B is transposed, and its barriers.  Where nothing but the state is formed, W's place and
+    // barriers make a second one: the next half is transposed while this one's terms are formed.
+    auto t_place = [&](int hb) { return STATE_ONLY && (hb & 1) ? kLtColW : kLtColT; };
+    auto bt_full = [&](int hb) { return STATE_ONLY ? &w_full[hb & 1] : b_full; };
+    auto terms_full = [&](int hb) { return STATE_ONLY ? &p_full[hb & 1] : t_full; };
+    auto bt_turn = [&](int hb) { return STATE_ONLY ? hb >> 1 : hb; };
 
     // (Loops are kept short where that costs nothing: 26 warps of six roles share the instruction caches, and straight-line
     // code that is run once per chunk is fetched anew each time.)
@@ -337,23 +338,28 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         const uint64_t unit = (smem_desc(0, 128, 256) & ~((uint64_t)7 << 61)) + base16 + L::unit / 16;
         constexpr uint32_t h16 = kLtHalf / 16;
         const int n_short = nv_last == kLtCh ? -1 : (reverse ? 0 : n_chunks - 1);   // the chunk with padding rows
-        int n_clean = 0, n_t = 0;   // padded tiles, and tiles of B transposed so far
+        int n_clean = 0, n_t = 0;   // padded tiles, and half tiles of B transposed so far
         Ring ra, rb, rt, rc;   // A and B as W takes them, B as its transposition does, C
         uint32_t a_w = 0, b_w = 0, c_now = 0;
         int c_slot = 0;
-        // B^T of the next tile of B, which belongs to chunk n.  (With head_dim 64 the upper 64 rows of this product, and
+        // B^T of the next half tile of B, which belongs to chunk n.  (With head_dim 64 the upper 64 rows of this product, and
         // of the state's, come from what lies behind the tile; nothing reads them.)
         auto transpose = [&](int n) {
-            LT_WAIT_WARP(&full_b[rt.s], rt.turn);
-            if (n == n_short) LT_WAIT_WARP(clean, n_clean++);
+            const int half = n_t & 1;
+            if (half == 0) {
+                LT_WAIT_WARP(&full_b[rt.s], rt.turn);
+                if (n == n_short) LT_WAIT_WARP(clean, n_clean++);
+            }
             tc_fence_after();
-            const uint32_t ba = base16 + (L::b + rt.s * kLtTile) / 16;
+            const uint32_t ba = base16 + (L::b + rt.s * kLtTile) / 16 + half * 512, place = tmem + t_place(n_t);
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk) umma_warp(tmem + t_place(n_t) + kk * 16, dmn.at(ba + kk * 128), unit, id_t, false);
+            for (int kk = 0; kk < 4; ++kk) umma_warp(place + kk * 16, dmn.at(ba + kk * 128), unit, id_t, false);
             umma_commit_warp(bt_full(n_t));
+            if (half == 1) {
+                if (!MULTI_A) umma_commit_warp(&empty_b[rt.s]);   // (the products of W are before this)
+                rt.next(n_b);
+            }
             ++n_t;
-            if (STATE_ONLY) umma_commit_warp(&empty_b[rt.s]);
-            rt.next(n_b);
         };
         // With several heads on A's side every other one's W goes where B^T was, which is free from the chunk's share of
         // the state until the next chunk: the next head's W then does not wait for this one's P.
@@ -381,15 +387,16 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             umma_commit_warp(&w_full[it & 1]);
             if (Gb > 1 || x == G - 1) umma_commit_warp(&empty_b[b_w]);
         };
-        auto state_products = [&](int nb, uint32_t ca) {
-            LT_WAIT_WARP(terms_full(nb), bt_turn(nb));
+        auto state_products = [&](int hb, uint32_t ca) {   // half a tile's share of the state
+            LT_WAIT_WARP(terms_full(hb), bt_turn(hb));
             tc_fence_after();
-            const uint32_t ta = tmem + t_place(nb);
+            const uint32_t ta = tmem + t_place(hb);
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk) {
-                const uint64_t cd = dmn.at(ca + kk * 128);
+            for (int kk = 0; kk < 4; ++kk) {
+                const uint64_t cd = dmn.at(ca + (hb & 1) * 512 + kk * 128);
                 umma_warp_ts(tmem + kLtColS, ta + kk * 16, cd, id_kn, true);
                 umma_warp_ts(tmem + kLtColS, ta + kk * 16 + 8, cd, id_kn, true);
+                umma_warp_ts(tmem + kLtColS, ta + 64 + kk * 8, cd, id_kn, true);
             }
         };
         if (items > 0) transpose(0);
@@ -402,17 +409,20 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 const uint32_t aa = base16 + (L::a + (n & 1) * kLtTile) / 16;
                 const int bc = rc.s;
                 rc.next(n_b);
+                const int n1 = last ? n + 1 : n;
+                bool next = it + 1 < items;
                 if (STATE_ONLY) {
-                    bool next = it + 1 < items;
+                    transpose(n);             // the second half
+                    if (x == 0) LT_WAIT_WARP(x_full, n);
+                    state_products(2 * it, ca);
                     if (next && __all_sync(0xffffffffu, mbar_try_wait(&full_b[rt.s], rt.turn))) {
-                        transpose(last ? n + 1 : n);
+                        transpose(n1);
                         next = false;
                     }
-                    if (x == 0) LT_WAIT_WARP(x_full, n);
-                    state_products(it, ca);
+                    state_products(2 * it + 1, ca);
                     umma_commit_warp(&empty_c[bc]);
                     if (last) umma_commit_warp(s_full);
-                    if (next) transpose(last ? n + 1 : n);
+                    if (next) transpose(n1);
                 } else {
                     if (x == 0) {
                         LT_WAIT_WARP(&full_a[n & 1], n >> 1);
@@ -424,24 +434,22 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                         umma_warp(tmem + kLtColW, dk.at(aa + o), dk.at(ba + o), id_kk, kk > 0);
                     }
                     umma_commit_warp(&w_full[it & 1]);
-                    umma_commit_warp(&empty_b[bc]);
-                    if (x == 0) {   // the state's share.  (X of chunk n is in place before the output of chunk n - 1 is read.)
-                        if (na > 0)
-                            LT_WAIT_WARP(o_empty, na - 1)
-                        else
-                            LT_WAIT_WARP(x_full, 0)
+                    if (x == 0) LT_WAIT_WARP(x_full, n);
+                    state_products(2 * it, ca);
+                    transpose(n);             // the second half
+                    if (x == 0) {             // the state's share
+                        if (na > 0) LT_WAIT_WARP(o_empty, na - 1);
                         ++na;
                         tc_fence_after();
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk)
                             umma_warp(tmem + kLtColO, dk.at(aa + (kk >> 2) * h16 + (kk & 3) * 2), dmn.at(x16 + kk * 128), id_kn, kk > 0);
                     }
-                    state_products(it, ca);
+                    state_products(2 * it + 1, ca);
                     if (last) umma_commit_warp(s_full);
-                    // the next tile's transposition before this item's last product, if its tiles are there
-                    bool next = it + 1 < items;
+                    // the next tile's first half before this item's last product, if the tile is there
                     if (next && __all_sync(0xffffffffu, mbar_try_wait(&full_b[rt.s], rt.turn))) {
-                        transpose(last ? n + 1 : n);
+                        transpose(n1);
                         next = false;
                     }
                     LT_WAIT_WARP(&p_full[it & 1], it >> 1);
@@ -451,7 +459,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                         umma_warp_ts(tmem + kLtColO, tmem + kLtColW + (kk >> 2) * 64 + (kk & 3) * 8, dmn.at(ca + kk * 128), id_kn, true);
                     if (last) umma_commit_warp(o_full);
                     umma_commit_warp(&empty_c[bc]);
-                    if (next) transpose(last ? n + 1 : n);
+                    if (next) transpose(n1);
                 }
                 if (last)
                     x = 0, ++n;
@@ -464,10 +472,10 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         for (int it = 0; it < items; ++it) {
             const bool new_b = x == 0 || Gb > 1, new_a = x == 0 || Ga > 1, last = x == G - 1, more = it + 1 < items;
             const int n1 = last ? n + 1 : n, x1 = last ? 0 : x + 1;      // the next item
-            if (!STATE_ONLY && !w_ahead) w_products(it, x);
+            if (!w_ahead) w_products(it, x);
             w_ahead = false;
             if (x == 0) LT_WAIT_WARP(x_full, n);
-            if (!STATE_ONLY && new_a) {   // the state's share
+            if (new_a) {   // the state's share
                 if (na > 0) LT_WAIT_WARP(o_empty, na - 1);
                 tc_fence_after();
 #pragma unroll
@@ -484,15 +492,17 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 c_slot = rc.s;
                 rc.next(2);
             }
-            bool add = new_b, put = !STATE_ONLY;     // the chunk's share of the state; this item's last product
+            int add = new_b ? 2 : 0;                 // halves of the chunk's share of the state
+            bool put = true;                         // this item's last product
             bool next_b = (Gb > 1 || last) && more;  // the next item, or the next chunk's first one, brings a tile of B
             while (add || put || next_b) {
                 // with several heads of A, P may well be there before B^T has been weighted
-                if (add && !(put && MULTI_A && __all_sync(0xffffffffu, mbar_try_wait(&p_full[it & 1], (it >> 1) & 1)))) {
-                    state_products(nb, c_now);
-                    if (Gb == 1 || last) umma_commit_warp(s_full);
-                    if (STATE_ONLY) umma_commit_warp(&empty_c[c_slot]);
-                    add = false;
+                if (add && !(put && __all_sync(0xffffffffu, mbar_try_wait(&p_full[it & 1], (it >> 1) & 1)))) {
+                    state_products(2 * nb + 2 - add, c_now);
+                    if (--add == 1)
+                        transpose(n);   // the second half
+                    else
+                        umma_commit_warp(s_full);
                     continue;
                 }
                 // the next tile's transposition before this item's last product, if the tile is there and its place free
@@ -502,7 +512,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     continue;
                 }
                 // and the next item's W, if it has a place of its own
-                if (MULTI_A && put && more && !add && !w_ahead && w_col(x1) != w_col(x) &&
+                if (put && more && !add && !w_ahead && w_col(x1) != w_col(x) &&
                     __all_sync(0xffffffffu, mbar_try_wait(&full_a[ra.s], ra.turn) &&
                                                 (x1 != 0 || mbar_try_wait(&full_b[rb.s], rb.turn)))) {
                     w_products(it + 1, x1);
@@ -619,21 +629,21 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             }
         }
     } else if (warp < 20) {
-        // =========================== w o B^T in two terms: two threads per feature of b, 64 tokens each ===========
-        const int q = warp & 3, half = (warp - 12) >> 2, wt = tid & 127;
-        const uint32_t lane_half = tmem + ((uint32_t)(q * 32) << 16) + half * 64;
+        // =========================== w o B^T in three terms: two threads per feature of b ===========
+        const int q = warp & 3, part = (warp - 12) >> 2, wt = tid & 127;
+        const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
         int nb = 0;
         Ring rb;
         for (int n = 0; n < n_chunks; ++n) {
             const int nv = chunk_nv(chunk_t0(n));
-            const float* w = pt + (reverse ? 128 : kLtCh - nv) + half * 64;   // w_j = w[j], 0 behind the last valid token
+            const float* w = pt + (reverse ? 128 : kLtCh - nv);   // w_j = w[j], 0 behind the last valid token
             const bool aligned = reverse || (nv & 3) == 0;
             for (int x = 0; x < Gb; ++x, ++nb) {
                 if (nv < kLtCh) {   // padding rows hold anything: zeros in B (this half of the warps) and in C (the other)
                     LT_WAIT(&full_b[rb.s], rb.turn);
                     if (MULTI_A) LT_WAIT(&full_c[nb & 1], nb >> 1);
                     if (wt >= nv) {
-                        uint4* z = reinterpret_cast<uint4*>(smem + (half ? L::c + (MULTI_A ? nb & 1 : rb.s) * kLtTile : L::b + rb.s * kLtTile) + wt * 128);
+                        uint4* z = reinterpret_cast<uint4*>(smem + (part ? L::c + (MULTI_A ? nb & 1 : rb.s) * kLtTile : L::b + rb.s * kLtTile) + wt * 128);
 #pragma unroll
                         for (int j = 0; j < 8 * kHalves; ++j) z[(j & 7) + (j >> 3) * (kLtHalf / 16)] = make_uint4(0, 0, 0, 0);
                     }
@@ -641,35 +651,42 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     __syncwarp();
                     if (lane == 0) mbar_arrive(clean);
                 }
-                LT_WAIT(bt_full(nb), bt_turn(nb));
-                const uint32_t t_col = lane_half + t_place(nb);
-                tc_fence_after();
 #pragma unroll 1
-                for (int e = q * 32 < D ? 0 : 4; e < 4; ++e) {   // (lanes without a feature only take part in the barriers)
-                    float v[16];
-                    tmem_ld16(t_col + e * 16, v);
-                    uint32_t o[16];
+                for (int hb = 2 * nb; hb < 2 * nb + 2; ++hb) {
+                    LT_WAIT(bt_full(hb), bt_turn(hb));
+                    tc_fence_after();
+                    const uint32_t place = lane_base + t_place(hb), t_col = place + part * 32;
+                    const float* wh = w + (hb & 1) * 64 + part * 32;
+#pragma unroll 1
+                    for (int e = q * 32 < D ? 0 : 2; e < 2; ++e) {   // (lanes without a feature only take part in the barriers)
+                        float v[16];
+                        tmem_ld16(t_col + e * 16, v);
+                        uint32_t o[16], o3[8];
 #pragma unroll
-                    for (int j = 0; j < 16; j += 4) {
-                        const float* wp = w + e * 16 + j;
-                        const float4 wj = aligned ? *reinterpret_cast<const float4*>(wp) : make_float4(wp[0], wp[1], wp[2], wp[3]);
+                        for (int j = 0; j < 16; j += 4) {
+                            const float* wp = wh + e * 16 + j;
+                            const float4 wj = aligned ? *reinterpret_cast<const float4*>(wp) : make_float4(wp[0], wp[1], wp[2], wp[3]);
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const float2 y = __fmul2_rn(make_float2(v[j + 2 * k], v[j + 2 * k + 1]),
-                                                        k ? make_float2(wj.z, wj.w) : make_float2(wj.x, wj.y));
-                            const uint32_t hi = Chunk<__nv_bfloat16>::pack2(y.x, y.y);
-                            // what the first term leaves out, exactly
-                            const float2 z = __fadd2_rn(y, make_float2(-__uint_as_float(hi << 16), -__uint_as_float(hi & 0xffff0000u)));
-                            o[(j >> 1) + k] = hi;
-                            o[8 + (j >> 1) + k] = Chunk<__nv_bfloat16>::pack2(z.x, z.y);
+                            for (int k = 0; k < 2; ++k) {
+                                float2 y = __fmul2_rn(make_float2(v[j + 2 * k], v[j + 2 * k + 1]),
+                                                      k ? make_float2(wj.z, wj.w) : make_float2(wj.x, wj.y));
+#pragma unroll
+                                for (int t = 0; t < 3; ++t) {
+                                    const uint32_t term = Chunk<__nv_bfloat16>::pack2(y.x, y.y);
+                                    (t < 2 ? o[8 * t + (j >> 1) + k] : o3[(j >> 1) + k]) = term;
+                                    // what the term leaves out, exactly
+                                    y = __fadd2_rn(y, make_float2(-__uint_as_float(term << 16), -__uint_as_float(term & 0xffff0000u)));
+                                }
+                            }
                         }
+                        tmem_st16u(t_col + e * 16, o);
+                        tmem_st8u(place + 64 + part * 16 + e * 8, o3);
                     }
-                    tmem_st16u(t_col + e * 16, o);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(terms_full(hb));
                 }
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(terms_full(nb));
                 rb.next(n_b);
             }
         }
