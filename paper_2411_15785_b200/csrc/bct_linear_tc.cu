@@ -1,4 +1,5 @@
-// Linear attention with a decay for each head on the sm_100a tensor path: the chunked scan for bfloat16 (the forward, and the three scans of the backward; bct_linear.h names the roles a, b, c).
+// Linear attention with a decay for each head on the sm_100a tensor path: the chunked scan for bfloat16 (the forward, and
+// the three scans of the backward; bct_linear.h names the roles a, b, c).
 //
 // Per (sequence, kv-head) unit and chunk of 128 tokens, X being the state outside the chunk:
 //     W     = A B^T                                 products of all pairs   [i][j]
@@ -6,22 +7,25 @@
 //     O     = A X + P C                             [i][feature of c]
 //     out_i = scale f_i O_i                         f_i = lambda^(distance of i to X's token)
 //     X    <- lambda^n X + (w o B)^T C              w_j = lambda^(distance of j to the new X's token)
-// all as tcgen05.mma with M = 128 and N = 128 (64 columns of results with head_dim 64) and fp32 accumulators in tensor memory.  What bounds it is the traffic of shared
-// memory (operands, tiles, results at 128 bytes a clock), so operands are kept in tensor memory where they can be:
+// all as tcgen05.mma with M = 128 and N = 128 (64 columns of results with head_dim 64) and fp32 accumulators in tensor
+// memory.  What bounds it is the traffic of shared memory (operands, tiles, results at 128 bytes a clock: some 4400 of a
+// chunk's 6400 clocks), so operands are kept in tensor memory where they can be:
 //  - W's columns are reused for P once its rows have been read.
-//  - B^T comes into tensor memory as a product with a 16 x 16 unit matrix, is multiplied with w there and split into two
-//    bfloat16 terms in place: 16 bits, as this library keeps the bounded cache's MV (what a token adds to the state is
-//    off by at most 2^-16 of it).  Weighted in shared memory it took 2300 clocks of traffic a chunk instead of 800.
+//  - B^T comes into tensor memory as a product with a 16 x 16 unit matrix, is multiplied with w there and split into
+//    three bfloat16 terms in place: 24 bits, so that the fp32 state is as good as one of fp32 sums.  (Two terms leave
+//    2.8e-6 of it; they took 220 instead of 249 us for 8 x 4096 tokens of 32 heads.)  Weighted in shared memory it took
+//    2300 clocks of traffic a chunk instead of 800.
 //  - The state accumulates in tensor memory, b's features in the lanes.  Once per chunk it is read, written to shared
 //    memory in bfloat16 as the operand X, and scaled.
 //  - f_i multiplies the whole row at the end instead of A's row, so A goes into both products as it is.  It is
 //    floored at 2^-40, which keeps P_ij in range: below that the state's share, as it is and as it is then taken,
 //    is under the rounding of what the row's own token adds.
 //  - P and X are each rounded to bfloat16 once, where they enter a product with bfloat16 results.
-// Roles (27 warps of 28): warp 0 issues the products, warp 1 loads (TMA), warp 2 stores (TMA); warps 4-11 turn W into P,
-// warps 12-19 weight and split B^T, warps 20-27 keep the state and write the outputs, over the A tile that has been read.
-// The products of a chunk go out as W, A X, w o B C, the next chunk's B^T, P C: each waits for something that was
-// started at least one product earlier.  With more than one
+// Roles: warp 0 issues the products of the outputs (W, A X, P C), warp 3 those of the state (B^T and its terms with C, a
+// quarter tile at a time; one warp for both waited for one while the other was ready, 300 instead of 249 us), warp 1 loads
+// (TMA), warp 2 stores (TMA); warps 4-11 turn W into P, warps 12-19 weight and split B^T, warps 20-27 keep the state and
+// write the outputs, over the A tile that has been read.  With several heads of A to a state, whose W and P also use the
+// place of B^T, warp 0 issues everything: W, A X, the state's products while P is formed, P C.  With more than one
 // segment, the same kernel without A, W and P forms what every segment adds.  Every wait is bounded; a timeout ends the
 // work and fills the block's outputs with NaN.
 #include <cuda.h>
@@ -42,9 +46,9 @@ constexpr int kLtHalf = 128 * 128;            // 64 columns (128 bytes) x 128 ro
 constexpr int kLtColW = 0;     // W, then P (bfloat16 pairs) in the first half of each of its 64-column halves
 constexpr int kLtColO = 128;
 constexpr int kLtColS = 256;   // the state [feature of b][feature of c]
-constexpr int kLtColT = 384;   // B^T [feature of b][j] of half a tile, 64 columns; of every 16 of them 8 then hold the first
-                               // terms, 8 the second, and 32 columns behind them the third.  With several heads of A to a
-                               // state also every other head's W and P
+constexpr int kLtColT = 384;   // two places of 64 columns for B^T [feature of b][j] of a quarter tile, 32 columns; of every
+                               // 16 of them 8 then hold the first terms, 8 the second, and 16 columns behind them the third.
+                               // With several heads of A to a state also every other head's W and P
 
 struct LtArgs {
     CUtensorMap in[4];    // forward: q, k, v;  backward: d_out, q, k, v
@@ -65,30 +69,81 @@ struct LtSmem {   // two buffers of every tile (three without A); everything els
     static constexpr int x = a + (STATE_ONLY ? 0 : 2 * kLtTile);   // the state as an operand: rows = features of b
     static constexpr int unit = x + (STATE_ONLY ? 0 : D * D * 2);  // 16 x 16 unit matrix
     static constexpr int bars = unit + 512;
-    static constexpr int pt = bars + 32 * 8;           // [256]: lambda^(i - j) at 127 + j - i, reverse lambda^(j - i); else 0
+    static constexpr int pt = bars + 38 * 8;           // [256]: lambda^(i - j) at 127 + j - i, reverse lambda^(j - i); else 0
     static constexpr int total = pt + 256 * 4 + 1024;  // slack to align the base to 1024 bytes
 };
 
-// The products are issued by a whole warp, one lane of which is elected at each: descriptors and addresses then stay in
-// uniform registers.  A product of N = 128 takes 64 clocks; issued by one thread among 27 warps (a register move for
-// every word of its descriptors) it took 95 to 170.
-__device__ __forceinline__ void umma_warp(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accum) {
+// The products are issued by a whole warp, one lane of which is elected: descriptors and addresses then stay in uniform
+// registers.  A product of N = 128 takes 64 clocks; issued by one thread among 27 warps (a register move for every word of
+// its descriptors) it took 95 to 170.  Several go out under one election.
+#define LT_UMMA "tcgen05.mma.cta_group::1.kind::f16 "
+// D (+)= A B over four steps of 16, whose descriptors are DA and DB apart
+template <int DA, int DB>
+__device__ __forceinline__ void umma4_warp(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accum) {
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
         "elect.sync _|q, 0xffffffff;\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accum)
+        "@q " LT_UMMA "[%0], %1, %2, %3, p;\n\t"
+        "setp.eq.b32 p, 0, 0;\n\t"
+        "add.s64 a, %1, %5;\n\tadd.s64 b, %2, %6;\n\t"
+        "@q " LT_UMMA "[%0], a, b, %3, p;\n\t"
+        "add.s64 a, %1, %7;\n\tadd.s64 b, %2, %8;\n\t"
+        "@q " LT_UMMA "[%0], a, b, %3, p;\n\t"
+        "add.s64 a, %1, %9;\n\tadd.s64 b, %2, %10;\n\t"
+        "@q " LT_UMMA "[%0], a, b, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accum),
+          "n"(DA), "n"(DB), "n"(2 * DA), "n"(2 * DB), "n"(3 * DA), "n"(3 * DB)
         : "memory");
 }
-// D (+)= A B with A (bfloat16 pairs) in tensor memory
-__device__ __forceinline__ void umma_warp_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, bool accum) {
+// D += A B over four steps with A (bfloat16 pairs, 8 columns a step) in tensor memory
+template <int DB>
+__device__ __forceinline__ void umma4_warp_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc) {
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
+        "{\n\t.reg .pred p, q;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\t"
+        "setp.eq.b32 p, 0, 0;\n\t"
         "elect.sync _|q, 0xffffffff;\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"((uint32_t)accum)
+        "@q " LT_UMMA "[%0], [%1], %2, %3, p;\n\t"
+        "add.s32 a, %1, 8;\n\tadd.s64 b, %2, %4;\n\t"
+        "@q " LT_UMMA "[%0], [a], b, %3, p;\n\t"
+        "add.s32 a, %1, 16;\n\tadd.s64 b, %2, %5;\n\t"
+        "@q " LT_UMMA "[%0], [a], b, %3, p;\n\t"
+        "add.s32 a, %1, 24;\n\tadd.s64 b, %2, %6;\n\t"
+        "@q " LT_UMMA "[%0], [a], b, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "n"(DB), "n"(2 * DB), "n"(3 * DB)
+        : "memory");
+}
+// D += (the three terms of a quarter tile) C: two steps of 16 tokens, 128 apart in C's descriptor
+__device__ __forceinline__ void umma_terms_warp(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\t"
+        "setp.eq.b32 p, 0, 0;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q " LT_UMMA "[%0], [%1], %2, %3, p;\n\t"
+        "add.s32 a, %1, 8;\n\t"
+        "@q " LT_UMMA "[%0], [a], %2, %3, p;\n\t"
+        "add.s32 a, %1, 32;\n\t"
+        "@q " LT_UMMA "[%0], [a], %2, %3, p;\n\t"
+        "add.s32 a, %1, 16;\n\tadd.s64 b, %2, 128;\n\t"
+        "@q " LT_UMMA "[%0], [a], b, %3, p;\n\t"
+        "add.s32 a, %1, 24;\n\t"
+        "@q " LT_UMMA "[%0], [a], b, %3, p;\n\t"
+        "add.s32 a, %1, 40;\n\t"
+        "@q " LT_UMMA "[%0], [a], b, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc)
+        : "memory");
+}
+// A quarter of B^T: two steps of 16 tokens, 128 apart in B's descriptor and 16 columns in the result
+__device__ __forceinline__ void umma_transpose_warp(uint32_t tmem_d, uint64_t adesc, uint64_t unit, uint32_t idesc, uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b32 d;\n\t.reg .b64 a;\n\t"
+        "setp.ne.b32 p, 0, 0;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q " LT_UMMA "[%0], %1, %2, %3, p;\n\t"
+        "add.s32 d, %0, 16;\n\tadd.s64 a, %1, 128;\n\t"
+        "@q " LT_UMMA "[d], a, %2, %3, p;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(unit), "r"(idesc), "r"(smem_u32(bar))
         : "memory");
 }
 __device__ __forceinline__ void umma_commit_warp(uint64_t* bar) {
@@ -144,6 +199,19 @@ __device__ __forceinline__ void lt_wait(uint64_t* bar, uint32_t parity, volatile
     if (!mbar_try_wait(bar, parity)) lt_wait_slow(bar, parity, abort_flag);
 }
 
+// One look at a barrier, without a wait.
+__device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok;
+}
+
 // MULTI_A: every role has several heads on A's side (and one on B's).
 template <int D, bool STATE_ONLY, bool MULTI_A>
 __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_constant__ LtArgs args) {
@@ -160,17 +228,17 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     uint64_t* full_c = bars + 13;        // [2]
     uint64_t* empty_c = STATE_ONLY ? bars + 6 : bars + 15;
     uint64_t* clean = bars + 17;         // padding rows of B and C are zeros
-    uint64_t* b_full = bars + 18;        // B^T complete
-    uint64_t* t_full = bars + 19;        // its terms in place
-    uint64_t* w_full = bars + 21;        // [2] W complete, by items in turn
-    uint64_t* p_full = bars + 23;        // [2] P in place
-    uint64_t* o_full = bars + 25;
-    uint64_t* o_empty = bars + 26;
-    uint64_t* s_full = bars + 27;        // the state holds the chunk
-    uint64_t* x_full = bars + 28;        // X in place, the state scaled
-    uint64_t* x_empty = bars + 29;       // the products with X complete
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 30);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 31);
+    uint64_t* bt_full = bars + 18;       // [4] a quarter of B^T complete, by places
+    uint64_t* terms_full = bars + 22;    // [4] its terms in place
+    uint64_t* w_full = bars + 26;        // [2] W complete, by items in turn
+    uint64_t* p_full = bars + 28;        // [2] P in place
+    uint64_t* o_full = bars + 30;
+    uint64_t* o_empty = bars + 31;
+    uint64_t* s_full = bars + 32;        // the state holds the chunk
+    uint64_t* x_full = bars + 33;        // X in place, the state scaled
+    uint64_t* x_empty = bars + 34;       // the products with X complete
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 35);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 36);
     float* pt = reinterpret_cast<float*>(smem + L::pt);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -209,16 +277,18 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         for (int i = 0; i < 2; ++i) {
             if (!STATE_ONLY) {
                 mbar_init(&full_b[i], 1);
-                mbar_init(&empty_b[i], 1);
+                mbar_init(&empty_b[i], MULTI_A ? 1 : 2);   // (two warps issue products that read it)
                 mbar_init(&full_c[i], 1);
-                mbar_init(&empty_c[i], 1);
+                mbar_init(&empty_c[i], MULTI_A ? 1 : 2);
             }
             mbar_init(&w_full[i], 1);
             mbar_init(&p_full[i], 8);
         }
         mbar_init(clean, 8);
-        mbar_init(b_full, 1);
-        mbar_init(t_full, 8);
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&bt_full[i], 1);
+            mbar_init(&terms_full[i], 8);
+        }
         mbar_init(o_full, 1);
         mbar_init(o_empty, 8);
         mbar_init(s_full, 1);
@@ -256,14 +326,13 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         __syncwarp();                \
     }
 
-    // Where the hb-th half tile of B is transposed, and its barriers.  Where nothing but the state is formed, W's place and
-    // barriers make a second one: the next half is transposed while this one's terms are formed.
-    auto t_place = [&](int hb) { return STATE_ONLY && (hb & 1) ? kLtColW : kLtColT; };
-    auto bt_full = [&](int hb) { return STATE_ONLY ? &w_full[hb & 1] : b_full; };
-    auto terms_full = [&](int hb) { return STATE_ONLY ? &p_full[hb & 1] : t_full; };
-    auto bt_turn = [&](int hb) { return STATE_ONLY ? hb >> 1 : hb; };
+    // Where the qb-th quarter tile of B is transposed.  (All four quarters' terms at once have no room beside W, O and the
+    // state; in two halves that took turns in one place the state waited for them, 6450 clocks a chunk.)  Where nothing but
+    // the state is formed, W's place makes two more.
+    constexpr int kPlaces = STATE_ONLY ? 4 : 2;
+    auto t_place = [&](int qb) { return (STATE_ONLY && (qb & 2) ? kLtColW : kLtColT) + (qb & 1) * 64; };
 
-    // (Loops are kept short where that costs nothing: 26 warps of six roles share the instruction caches, and straight-line
+    // (Loops are kept short where that costs nothing: 28 warps of seven roles share the instruction caches, and straight-line
     // code that is run once per chunk is fetched anew each time.)
     const int items = n_chunks * G;   // (chunk, head) in turn: head x of the side that has G of them
     // Buffers: two of every tile; with several heads on A's side, whose tiles then turn over fastest, B's second one is a
@@ -327,7 +396,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             }
         }
         __syncwarp();
-    } else if (warp == 0) {
+    } else if (warp == 0 || (!MULTI_A && !STATE_ONLY && warp == 3)) {
         // =========================== products ===========================
         constexpr uint32_t id_kk = instr_desc_mn(128, 128, false, false);
         constexpr uint32_t id_kn = instr_desc_mn(128, D, false, true);
@@ -338,25 +407,23 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         const uint64_t unit = (smem_desc(0, 128, 256) & ~((uint64_t)7 << 61)) + base16 + L::unit / 16;
         constexpr uint32_t h16 = kLtHalf / 16;
         const int n_short = nv_last == kLtCh ? -1 : (reverse ? 0 : n_chunks - 1);   // the chunk with padding rows
-        int n_clean = 0, n_t = 0;   // padded tiles, and half tiles of B transposed so far
+        int n_clean = 0, n_t = 0;   // padded tiles, and quarter tiles of B transposed so far
         Ring ra, rb, rt, rc;   // A and B as W takes them, B as its transposition does, C
         uint32_t a_w = 0, b_w = 0, c_now = 0;
         int c_slot = 0;
-        // B^T of the next half tile of B, which belongs to chunk n.  (With head_dim 64 the upper 64 rows of this product, and
-        // of the state's, come from what lies behind the tile; nothing reads them.)
+        // B^T of the next quarter tile of B, which belongs to chunk n.  (With head_dim 64 the upper 64 rows of this product,
+        // and of the state's, come from what lies behind the tile; nothing reads them.)
         auto transpose = [&](int n) {
-            const int half = n_t & 1;
-            if (half == 0) {
+            const int quarter = n_t & 3;
+            if (quarter == 0) {
                 LT_WAIT_WARP(&full_b[rt.s], rt.turn);
                 if (n == n_short) LT_WAIT_WARP(clean, n_clean++);
             }
             tc_fence_after();
-            const uint32_t ba = base16 + (L::b + rt.s * kLtTile) / 16 + half * 512, place = tmem + t_place(n_t);
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) umma_warp(place + kk * 16, dmn.at(ba + kk * 128), unit, id_t, false);
-            umma_commit_warp(bt_full(n_t));
-            if (half == 1) {
-                if (!MULTI_A) umma_commit_warp(&empty_b[rt.s]);   // (the products of W are before this)
+            const uint32_t ba = base16 + (L::b + rt.s * kLtTile) / 16 + quarter * 256, place = tmem + t_place(n_t);
+            umma_transpose_warp(place, dmn.at(ba), unit, id_t, &bt_full[n_t % kPlaces]);
+            if (quarter == 3) {
+                if (!MULTI_A) umma_commit_warp(&empty_b[rt.s]);
                 rt.next(n_b);
             }
             ++n_t;
@@ -379,96 +446,78 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             tc_fence_after();
             const uint32_t col = tmem + w_col(x), ba = base16 + (L::b + b_w * kLtTile) / 16;
 #pragma unroll
-            for (int hf = 0; hf < kHalves; ++hf) {
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                    umma_warp(col, dk.at(a_w + hf * h16 + 2 * kk), dk.at(ba + hf * h16 + 2 * kk), id_kk, hf > 0 || kk > 0);
-            }
+            for (int hf = 0; hf < kHalves; ++hf) umma4_warp<2, 2>(col, dk.at(a_w + hf * h16), dk.at(ba + hf * h16), id_kk, hf > 0);
             umma_commit_warp(&w_full[it & 1]);
             if (Gb > 1 || x == G - 1) umma_commit_warp(&empty_b[b_w]);
         };
-        auto state_products = [&](int hb, uint32_t ca) {   // half a tile's share of the state
-            LT_WAIT_WARP(terms_full(hb), bt_turn(hb));
+        auto state_products = [&](int qb, uint32_t ca) {   // a quarter tile's share of the state
+            LT_WAIT_WARP(&terms_full[qb % kPlaces], qb / kPlaces);
             tc_fence_after();
-            const uint32_t ta = tmem + t_place(hb);
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-                const uint64_t cd = dmn.at(ca + (hb & 1) * 512 + kk * 128);
-                umma_warp_ts(tmem + kLtColS, ta + kk * 16, cd, id_kn, true);
-                umma_warp_ts(tmem + kLtColS, ta + kk * 16 + 8, cd, id_kn, true);
-                umma_warp_ts(tmem + kLtColS, ta + 64 + kk * 8, cd, id_kn, true);
-            }
+            umma_terms_warp(tmem + kLtColS, tmem + t_place(qb), dmn.at(ca + (qb & 3) * 256), id_kn);
         };
-        if (items > 0) transpose(0);
-        if constexpr (!MULTI_A) {
-            // An item's C has come with its B, which has been transposed.
-            int na = 0, x = 0;
+        auto ready = [&](uint64_t* bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_test_wait(bar, parity & 1)); };
+        if (!MULTI_A && (STATE_ONLY || warp == 3)) {
+            // The state: quarters are transposed as far ahead of their products as there are places.  (An item's C has come
+            // with its B.)
+            int x = 0, xt = 0, nt = 0;   // xt, nt: of the next tile to be transposed
             for (int n = 0, it = 0; it < items; ++it) {
-                const bool last = x == G - 1;
-                const uint32_t ba = base16 + (L::b + rc.s * kLtTile) / 16, ca = base16 + (L::c + rc.s * kLtTile) / 16;
-                const uint32_t aa = base16 + (L::a + (n & 1) * kLtTile) / 16;
-                const int bc = rc.s;
+                const uint32_t ca = base16 + (L::c + rc.s * kLtTile) / 16;
+#pragma unroll 1
+                for (int qb = 4 * it; qb < 4 * it + 4; ++qb) {
+                    while (n_t < 4 * items && n_t < qb + kPlaces && (n_t <= qb || (n_t & 3) != 0 || ready(&full_b[rt.s], rt.turn))) {
+                        transpose(nt);
+                        if ((n_t & 3) == 0 && ++xt == G) xt = 0, ++nt;
+                    }
+                    if (qb == 4 * it && x == 0) LT_WAIT_WARP(x_full, n);
+                    state_products(qb, ca);
+                }
+                umma_commit_warp(&empty_c[rc.s]);
                 rc.next(n_b);
-                const int n1 = last ? n + 1 : n;
-                bool next = it + 1 < items;
-                if (STATE_ONLY) {
-                    transpose(n);             // the second half
-                    if (x == 0) LT_WAIT_WARP(x_full, n);
-                    state_products(2 * it, ca);
-                    if (next && __all_sync(0xffffffffu, mbar_try_wait(&full_b[rt.s], rt.turn))) {
-                        transpose(n1);
-                        next = false;
-                    }
-                    state_products(2 * it + 1, ca);
-                    umma_commit_warp(&empty_c[bc]);
-                    if (last) umma_commit_warp(s_full);
-                    if (next) transpose(n1);
-                } else {
-                    if (x == 0) {
-                        LT_WAIT_WARP(&full_a[n & 1], n >> 1);
-                        tc_fence_after();
-                    }
+                if (++x == G) {
+                    umma_commit_warp(s_full);
+                    x = 0, ++n;
+                }
+            }
+        } else if constexpr (!MULTI_A) {
+            // The outputs.
+            int x = 0;
+            for (int n = 0, it = 0; it < items; ++it) {
+                const uint32_t aa = base16 + (L::a + (n & 1) * kLtTile) / 16, ba = base16 + (L::b + rb.s * kLtTile) / 16;
+                const uint32_t ca = base16 + (L::c + rb.s * kLtTile) / 16;
+                LT_WAIT_WARP(&full_b[rb.s], rb.turn);
+                if (x == 0) LT_WAIT_WARP(&full_a[n & 1], n >> 1);
+                tc_fence_after();
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) {
-                        const uint32_t o = (kk >> 2) * h16 + (kk & 3) * 2;
-                        umma_warp(tmem + kLtColW, dk.at(aa + o), dk.at(ba + o), id_kk, kk > 0);
-                    }
-                    umma_commit_warp(&w_full[it & 1]);
-                    if (x == 0) LT_WAIT_WARP(x_full, n);
-                    state_products(2 * it, ca);
-                    transpose(n);             // the second half
-                    if (x == 0) {             // the state's share
-                        if (na > 0) LT_WAIT_WARP(o_empty, na - 1);
-                        ++na;
-                        tc_fence_after();
-#pragma unroll
-                        for (int kk = 0; kk < D / 16; ++kk)
-                            umma_warp(tmem + kLtColO, dk.at(aa + (kk >> 2) * h16 + (kk & 3) * 2), dmn.at(x16 + kk * 128), id_kn, kk > 0);
-                    }
-                    state_products(2 * it + 1, ca);
-                    if (last) umma_commit_warp(s_full);
-                    // the next tile's first half before this item's last product, if the tile is there
-                    if (next && __all_sync(0xffffffffu, mbar_try_wait(&full_b[rt.s], rt.turn))) {
-                        transpose(n1);
-                        next = false;
-                    }
-                    LT_WAIT_WARP(&p_full[it & 1], it >> 1);
+                for (int hf = 0; hf < kHalves; ++hf)
+                    umma4_warp<2, 2>(tmem + kLtColW, dk.at(aa + hf * h16), dk.at(ba + hf * h16), id_kk, hf > 0);
+                umma_commit_warp(&w_full[it & 1]);
+                umma_commit_warp(&empty_b[rb.s]);
+                if (x == 0) {             // the state's share
+                    LT_WAIT_WARP(x_full, n);
+                    if (n > 0) LT_WAIT_WARP(o_empty, n - 1);
                     tc_fence_after();
 #pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)
-                        umma_warp_ts(tmem + kLtColO, tmem + kLtColW + (kk >> 2) * 64 + (kk & 3) * 8, dmn.at(ca + kk * 128), id_kn, true);
-                    if (last) umma_commit_warp(o_full);
-                    umma_commit_warp(&empty_c[bc]);
-                    if (next) transpose(n1);
+                    for (int hf = 0; hf < kHalves; ++hf)
+                        umma4_warp<2, 128>(tmem + kLtColO, dk.at(aa + hf * h16), dmn.at(x16 + hf * 512), id_kn, hf > 0);
+                    umma_commit_warp(x_empty);
                 }
-                if (last)
+                if (n == n_short) LT_WAIT_WARP(clean, n_clean++);
+                LT_WAIT_WARP(&p_full[it & 1], it >> 1);
+                tc_fence_after();
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+                    umma4_warp_ts<128>(tmem + kLtColO, tmem + kLtColW + hf * 64, dmn.at(ca + hf * 512), id_kn);
+                umma_commit_warp(&empty_c[rb.s]);
+                rb.next(n_b);
+                if (++x == G) {
+                    umma_commit_warp(o_full);
                     x = 0, ++n;
-                else
-                    ++x;
+                }
             }
         } else {
         bool w_ahead = false;
         int n = 0, x = 0, na = 0, nb = 0;
+        if (items > 0) transpose(0), transpose(0);
         for (int it = 0; it < items; ++it) {
             const bool new_b = x == 0 || Gb > 1, new_a = x == 0 || Ga > 1, last = x == G - 1, more = it + 1 < items;
             const int n1 = last ? n + 1 : n, x1 = last ? 0 : x + 1;      // the next item
@@ -479,11 +528,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 if (na > 0) LT_WAIT_WARP(o_empty, na - 1);
                 tc_fence_after();
 #pragma unroll
-                for (int hf = 0; hf < kHalves; ++hf) {
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)
-                        umma_warp(tmem + kLtColO, dk.at(a_w + hf * h16 + 2 * kk), dmn.at(x16 + hf * 512 + kk * 128), id_kn, hf > 0 || kk > 0);
-                }
+                for (int hf = 0; hf < kHalves; ++hf)
+                    umma4_warp<2, 128>(tmem + kLtColO, dk.at(a_w + hf * h16), dmn.at(x16 + hf * 512), id_kn, hf > 0);
                 if (Gb > 1 || last) umma_commit_warp(x_empty);
             }
             if (new_b) {
@@ -492,23 +538,21 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 c_slot = rc.s;
                 rc.next(2);
             }
-            int add = new_b ? 2 : 0;                 // halves of the chunk's share of the state
+            int add = new_b ? 4 : 0;                 // quarters of the chunk's share of the state
             bool put = true;                         // this item's last product
-            bool next_b = (Gb > 1 || last) && more;  // the next item, or the next chunk's first one, brings a tile of B
+            int next_b = (Gb > 1 || last) && more ? 2 : 0;   // quarters of B that the next chunk's first item begins with
             while (add || put || next_b) {
                 // with several heads of A, P may well be there before B^T has been weighted
-                if (add && !(put && __all_sync(0xffffffffu, mbar_try_wait(&p_full[it & 1], (it >> 1) & 1)))) {
-                    state_products(2 * nb + 2 - add, c_now);
-                    if (--add == 1)
-                        transpose(n);   // the second half
-                    else
-                        umma_commit_warp(s_full);
+                if (add && !(put && ready(&p_full[it & 1], it >> 1))) {
+                    state_products(4 * nb + 4 - add, c_now);
+                    if (--add >= 2) transpose(n);   // the third and the fourth
+                    if (add == 0) umma_commit_warp(s_full);
                     continue;
                 }
                 // the next tile's transposition before this item's last product, if the tile is there and its place free
-                if (next_b && !add && (!put || (w_col(x) != kLtColT && __all_sync(0xffffffffu, mbar_try_wait(&full_b[rt.s], rt.turn))))) {
+                if (next_b && !add && (!put || (w_col(x) != kLtColT && ((n_t & 3) != 0 || ready(&full_b[rt.s], rt.turn))))) {
                     transpose(n1);
-                    next_b = false;
+                    --next_b;
                     continue;
                 }
                 // and the next item's W, if it has a place of its own
@@ -522,11 +566,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     LT_WAIT_WARP(&p_full[it & 1], it >> 1);
                     tc_fence_after();
 #pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {
-#pragma unroll
-                        for (int kk = 0; kk < 4; ++kk)
-                            umma_warp_ts(tmem + kLtColO, tmem + w_col(x) + hf * 64 + kk * 8, dmn.at(c_now + hf * 512 + kk * 128), id_kn, true);
-                    }
+                    for (int hf = 0; hf < 2; ++hf)
+                        umma4_warp_ts<128>(tmem + kLtColO, tmem + w_col(x) + hf * 64, dmn.at(c_now + hf * 512), id_kn);
                     if (Ga > 1 || last) umma_commit_warp(o_full);
                     if (Gb > 1 || last) umma_commit_warp(&empty_c[c_slot]);
                     put = false;
@@ -539,9 +580,9 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         }
         }
         __syncwarp();
-    } else if (warp == 2) {
+    } else if (warp < 4) {
         // =========================== stores ===========================
-        if (!STATE_ONLY && lane == 0) {
+        if (!STATE_ONLY && warp == 2 && lane == 0) {
             const CUtensorMap* map_o = &args.out[which];
             Ring ra;
             for (int n = 0; n < n_chunks; ++n) {
@@ -559,16 +600,6 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             bulk_wait_all();
         }
         __syncwarp();
-    } else if (warp == 3) {
-        // =========================== padding rows behind the last chunk ===========================
-        if (!STATE_ONLY) {
-            constexpr int kRow = D * 2 / 16;   // 16-byte pieces of a row
-            char* out = static_cast<char*>(r.out) + ((size_t)bi * s.T * s.Hkv + h) * Ga * (D * 2);
-            const long long end = (long long)t_end * kRow;
-            for (long long i = (long long)(t_begin + n_chunks * kLtCh) * kRow + lane; i < end; i += 32)
-                for (int x = 0; x < Ga; ++x)
-                    reinterpret_cast<uint4*>(out + ((size_t)(i / kRow) * s.Hkv * Ga + x) * (D * 2))[i % kRow] = make_uint4(0, 0, 0, 0);
-        }
     } else if (warp < 12) {
         // =========================== W -> P: two threads per row i, 64 columns each ===========
         if (!STATE_ONLY) {
@@ -627,6 +658,13 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     if (lane == 0) mbar_arrive(&p_full[it & 1]);
                 }
             }
+            // padding rows behind the last chunk
+            constexpr int kRow = D * 2 / 16;   // 16-byte pieces of a row
+            char* out = static_cast<char*>(r.out) + ((size_t)bi * s.T * s.Hkv + h) * Ga * (D * 2);
+            const long long end = (long long)t_end * kRow;
+            for (long long j = (long long)(t_begin + n_chunks * kLtCh) * kRow + tid - 128; j < end; j += 256)
+                for (int x = 0; x < Ga; ++x)
+                    reinterpret_cast<uint4*>(out + ((size_t)(j / kRow) * s.Hkv * Ga + x) * (D * 2))[j % kRow] = make_uint4(0, 0, 0, 0);
         }
     } else if (warp < 20) {
         // =========================== w o B^T in three terms: two threads per feature of b ===========
@@ -652,20 +690,19 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     if (lane == 0) mbar_arrive(clean);
                 }
 #pragma unroll 1
-                for (int hb = 2 * nb; hb < 2 * nb + 2; ++hb) {
-                    LT_WAIT(bt_full(hb), bt_turn(hb));
+                for (int qb = 4 * nb; qb < 4 * nb + 4; ++qb) {
+                    LT_WAIT(&bt_full[qb % kPlaces], qb / kPlaces);
                     tc_fence_after();
-                    const uint32_t place = lane_base + t_place(hb), t_col = place + part * 32;
-                    const float* wh = w + (hb & 1) * 64 + part * 32;
-#pragma unroll 1
-                    for (int e = q * 32 < D ? 0 : 2; e < 2; ++e) {   // (lanes without a feature only take part in the barriers)
+                    const uint32_t place = lane_base + t_place(qb), t_col = place + part * 16;
+                    const float* wp = w + (qb & 3) * 32 + part * 16;
+                    if (q * 32 < D) {   // (lanes without a feature only take part in the barriers)
                         float v[16];
-                        tmem_ld16(t_col + e * 16, v);
+                        tmem_ld16(t_col, v);
                         uint32_t o[16], o3[8];
 #pragma unroll
                         for (int j = 0; j < 16; j += 4) {
-                            const float* wp = wh + e * 16 + j;
-                            const float4 wj = aligned ? *reinterpret_cast<const float4*>(wp) : make_float4(wp[0], wp[1], wp[2], wp[3]);
+                            const float4 wj = aligned ? *reinterpret_cast<const float4*>(wp + j)
+                                                      : make_float4(wp[j], wp[j + 1], wp[j + 2], wp[j + 3]);
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
                                 float2 y = __fmul2_rn(make_float2(v[j + 2 * k], v[j + 2 * k + 1]),
@@ -675,17 +712,18 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                                     const uint32_t term = Chunk<__nv_bfloat16>::pack2(y.x, y.y);
                                     (t < 2 ? o[8 * t + (j >> 1) + k] : o3[(j >> 1) + k]) = term;
                                     // what the term leaves out, exactly
-                                    y = __fadd2_rn(y, make_float2(-__uint_as_float(term << 16), -__uint_as_float(term & 0xffff0000u)));
+                                    y = __ffma2_rn(make_float2(__uint_as_float(term << 16), __uint_as_float(term & 0xffff0000u)),
+                                                   make_float2(-1.f, -1.f), y);
                                 }
                             }
                         }
-                        tmem_st16u(t_col + e * 16, o);
-                        tmem_st8u(place + 64 + part * 16 + e * 8, o3);
+                        tmem_st16u(t_col, o);
+                        tmem_st8u(place + 32 + part * 8, o3);
+                        tmem_wait_st();
                     }
-                    tmem_wait_st();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(terms_full(hb));
+                    if (lane == 0) mbar_arrive(&terms_full[qb % kPlaces]);
                 }
                 rb.next(n_b);
             }
@@ -747,7 +785,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             const float f = lam(chunk_nv(chunk_t0(n)));
             if (n > 0) {
                 LT_WAIT(s_full, n - 1);
-                if (MULTI_A) LT_WAIT(x_empty, n - 1);   // (otherwise the state's products are the later ones)
+                if (!STATE_ONLY) LT_WAIT(x_empty, n - 1);
                 tc_fence_after();
             }
 #pragma unroll 1
@@ -784,8 +822,11 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             const int nv = chunk_nv(chunk_t0(n));
             const float f = nv < kLtCh ? f_last : f_full;
             for (int x = 0; x < Ga; ++x, ++na) {
-                // (the state is complete before the chunk's last output, and the next chunk's products wait for it)
-                if (x == Ga - 1 && n + 1 < n_chunks) turn(n + 1);
+                // The chunk's last output and the state's turn: what is complete first goes first.  (The output has to leave
+                // A's place before the tile after the next can be loaded; the next chunk's products wait for the state.)
+                const bool turns = x == Ga - 1 && n + 1 < n_chunks;
+                const bool out_first = !turns || __all_sync(0xffffffffu, mbar_test_wait(o_full, na & 1));
+                if (!out_first) turn(n + 1);
                 LT_WAIT(o_full, na);
                 tc_fence_after();
                 unsigned char* dst = smem + a_at(ra.s) + (hs * kCols / 64) * kLtHalf + c * 128;
@@ -799,15 +840,21 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                         if (lane == 0) mbar_arrive(o_empty);
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[i] = c < nv ? o[i] * f : 0.f;   // padding rows: zeros
+                    for (int i = 0; i < 16; i += 2) {
+                        const float2 y = __fmul2_rn(make_float2(o[i], o[i + 1]), make_float2(f, f));
+                        o[i] = y.x, o[i + 1] = y.y;
+                    }
+                    uint4 lo = Chunk<__nv_bfloat16>::pack(o), hi = Chunk<__nv_bfloat16>::pack(o + 8);
+                    if (c >= nv) lo = hi = make_uint4(0, 0, 0, 0);   // padding rows
                     const int pc = hs * kPiece + 2 * k;
-                    *reinterpret_cast<uint4*>(dst + ((pc ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(o);
-                    *reinterpret_cast<uint4*>(dst + (((pc + 1) ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(o + 8);
+                    *reinterpret_cast<uint4*>(dst + ((pc ^ (c & 7)) * 16)) = lo;
+                    *reinterpret_cast<uint4*>(dst + (((pc + 1) ^ (c & 7)) * 16)) = hi;
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&out_full[ra.s]);
                 ra.next(n_a);
+                if (turns && out_first) turn(n + 1);
             }
         }
         if (n_chunks > 0) {
