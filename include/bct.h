@@ -283,7 +283,13 @@ bct_status_t bct_stack_forward(bct_cache_t *const *caches, int32_t n_layers, con
  * columns.
  *   log_decay  DEVICE float [Hkv], 4-byte aligned: the logarithm of the decay, <= 0; 0 never forgets, minus infinity
  *              keeps only the token itself.  A constant of the head: the backward forms no gradient for it.
- * Outputs are rounded once to `dtype`; everything before that is fp32.  No atomics: the same call gives the same bits.
+ * Roundings.  BCT_F32, and the step in either type: fp32 throughout, one rounding to `dtype`.  Prompts and their
+ * backward in BCT_BF16 run on the tensor cores: the products of pairs (q_t . k_s and their like, weighted with the
+ * decay) and the state where it enters a product are each rounded to bfloat16 once, sums are fp32, and `out` and the
+ * gradients are rounded once; the float states (state_out, d_state_in) are fp32 sums of unrounded products.
+ * No atomics: the same call gives the same bits.  A NaN or an infinity in a token that counts may also reach the
+ * results of up to 127 tokens before it (of those after it, in the backward), as 0 * infinity; one in a padding row
+ * reaches nothing.
  * No output may overlap an input or another output, except where stated (BCT_ERR_INVALID_ARG).
  */
 typedef struct bct_linear_params {

@@ -18,8 +18,7 @@
 //  - The state accumulates in tensor memory, b's features in the lanes.  Once per chunk it is read, written to shared
 //    memory in bfloat16 as the operand X, and scaled.
 //  - f_i multiplies the whole row at the end instead of A's row, so A goes into both products as it is.  It is
-//    floored at 2^-40, which keeps P_ij in range: below that the state's share, as it is and as it is then taken,
-//    is under the rounding of what the row's own token adds.
+//    floored at 2^-64, which keeps P_ij in range (2^64 W_ij) and is off by 2^-64 of the state's share at most.
 //  - P and X are each rounded to bfloat16 once, where they enter a product with bfloat16 results.
 // Roles: warp 0 issues the products of the outputs (W, A X, P C), warp 3 those of the state (B^T and its terms with C, a
 // quarter tile at a time; one warp for both waited for one while the other was ready, 300 instead of 249 us), warp 1 loads
@@ -315,7 +314,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     // lambda^e, 0 <= e <= 128
     auto lam = [&](int e) { return reverse ? pt[127 + e] : (e < 128 ? pt[127 - e] : pt[0] * pt[126]); };
     // f of row i in a chunk of nv valid tokens
-    auto f_of = [&](int i, int nv) { return fmaxf(lam(reverse ? max(nv - 1 - i, 0) : i + 1), 9.094947017729282e-13f); };   // 2^-40
+    auto f_of = [&](int i, int nv) { return fmaxf(lam(reverse ? max(nv - 1 - i, 0) : i + 1), 5.421010862427522e-20f); };   // 2^-64
     const int nv_last = n_chunks > 0 ? (v_end - t_begin - 1) % kLtCh + 1 : kLtCh;   // of the one chunk that may be shorter
 #define LT_WAIT(bar, parity) lt_wait(bar, (parity) & 1, abort_flag);
 

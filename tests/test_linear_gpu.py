@@ -355,3 +355,32 @@ def test_the_path_from_tokens_to_outputs_and_back():
                           (ro.detach(), *grads)):
         err = float((a.double() - b).square().mean().sqrt() / b.square().mean().sqrt())
         assert err <= tol, (name, err)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(2, 2, 128), (8, 2, 128), (2, 2, 64), (6, 2, 64)])
+def test_float_states_of_a_bfloat16_call_are_float_sums(Hq, Hkv, d):
+    # 16 tokens are one step of a tensor-core sum for each part a product is split into: at most four of them, each cut
+    # off (not rounded) at 2^-23 of the partial sum, and a decay's power, one rounding of 2^-24, in front.
+    q, k, v, ld, S = _inputs(3, 16, Hq, Hkv, d, "bf16", 59, decay=-0.11)
+    _, S1 = B.linear_forward(q, k, v, ld)
+    _, ref = R.linear_forward(q, k, v, ld)
+    _, mag = R.linear_forward(q.abs(), k.abs(), v.abs(), ld)
+    assert bool(((S1.double() - ref).abs() <= 4.5 * 2.0 ** -23 * mag).all())
+    do = torch.randn(q.shape, generator=torch.Generator(device="cuda").manual_seed(60), device="cuda").to(q.dtype)
+    got = B.linear_backward(do, q, k, v, ld)[3]
+    ref = R.linear_backward(do, q, k, v, ld)[3]
+    mag = R.linear_backward(do.abs(), q.abs(), k.abs(), v.abs(), ld)[3]
+    G = Hq // Hkv       # the heads of a group follow one another in the sum; one product with the scale behind it
+    assert bool(((got.double() - ref).abs() <= (4 * G + 1.5) * 2.0 ** -23 * mag).all())
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(2, 2), (4, 2)])
+def test_a_large_state_under_a_strong_decay(Hq, Hkv):
+    # the state is 2^40 times what the tokens add and gone after a few of them: nothing of it may stay
+    q, k, v, ld, S = _inputs(1, 130, Hq, Hkv, 128, "bf16", 61, decay=-2.0)
+    S = S * 2.0 ** 40
+    out, S1 = B.linear_forward(q, k, v, ld, state=S)
+    ref, rS = R.linear_forward(q, k, v, ld, S)
+    mag, mS = R.linear_forward(q.abs(), k.abs(), v.abs(), ld, S.abs())
+    _check("out", out[:, 40:], ref[:, 40:], mag[:, 40:], "bf16", 128 + 130 + 64, tensor=True)
+    _check("state", S1, rS, mS, "f32", 128 + 130 + 64)
