@@ -615,25 +615,25 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     LT_WAIT(&w_full[it & 1], it >> 1);
                     tc_fence_after();
 #pragma unroll 1
-                    for (int e = 0; e < 4; ++e) {   // 16 columns; P takes the place of columns read before
-                        const int j0 = half * 64 + e * 16, cb = j0 >> 5;
-                        float v[16];
+                    for (int e = 0; e < 2; ++e) {   // 32 columns; P takes the place of columns read before
+                        const int cb = half * 2 + e, j0 = cb * 32;
+                        float v[32];
                         if (reverse ? cb < q : cb > q) {   // the mask leaves nothing
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] = 0.f;
+                            for (int j = 0; j < 32; ++j) v[j] = 0.f;
                         } else {
-                            tmem_ld16(lane_base + e * 16, v);
+                            tmem_ld32(lane_base + e * 32, v);
                             if (cb == q) {   // the mask's edge runs through this block
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) {
+                                for (int j = 0; j < 32; ++j) {
                                     const float w = pti[j0 + j];
                                     v[j] = w > 0.f ? v[j] * (w * inv_f) : 0.f;
                                 }
                             } else {         // a power for the row and the block, one for the column
-                                const float wr = lam(reverse ? cb * 32 - i - 1 : i - cb * 32 - 31) * inv_f;
+                                const float wr = lam(reverse ? j0 - i - 1 : i - j0 - 31) * inv_f;
 #pragma unroll
-                                for (int j = 0; j < 16; j += 4) {
-                                    const float4 wc = *reinterpret_cast<const float4*>(pt + (reverse ? 128 : 96) + (e & 1) * 16 + j);
+                                for (int j = 0; j < 32; j += 4) {
+                                    const float4 wc = *reinterpret_cast<const float4*>(pt + (reverse ? 128 : 96) + j);
                                     const float2 y = __fmul2_rn(__fmul2_rn(make_float2(v[j], v[j + 1]), make_float2(wc.x, wc.y)),
                                                                 make_float2(wr, wr));
                                     const float2 z = __fmul2_rn(__fmul2_rn(make_float2(v[j + 2], v[j + 3]), make_float2(wc.z, wc.w)),
@@ -643,13 +643,16 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                             }
                             if (nv < kLtCh) {   // products with padding rows, which hold anything
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) v[j] = j0 + j < nv ? v[j] : 0.f;
+                                for (int j = 0; j < 32; ++j) v[j] = j0 + j < nv ? v[j] : 0.f;
                             }
                         }
-                        uint32_t pk[8];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) pk[j] = Chunk<__nv_bfloat16>::pack2(v[2 * j], v[2 * j + 1]);
-                        tmem_st8u(lane_base + e * 8, pk);
+                        for (int hf = 0; hf < 2; ++hf) {
+                            uint32_t pk[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) pk[j] = Chunk<__nv_bfloat16>::pack2(v[16 * hf + 2 * j], v[16 * hf + 2 * j + 1]);
+                            tmem_st8u(lane_base + e * 16 + hf * 8, pk);
+                        }
                     }
                     tmem_wait_st();
                     tc_fence_before();
