@@ -229,9 +229,18 @@ def _raw_stream(dev: int) -> int:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
 
 
-def _launch(dev, stream, call, *args) -> None:
-    """The call on the tensors' device: on `stream`, or on that device's current stream."""
-    raw = _raw_stream(dev) if stream is None else stream.cuda_stream
+def _on_stream(stream, call, *args):
+    """`call` with `stream` as the current one: what it allocates (results, scratch) then belongs to that stream, and
+    freeing it cannot hand it to work of another stream that runs beside the call's kernels."""
+    if stream.device.index != args[0].get_device():
+        raise ValueError("stream is on %s, the tensors are on %s" % (stream.device, args[0].device))
+    with torch.cuda.stream(stream):
+        return call(*args)
+
+
+def _launch(dev, call, *args) -> None:
+    """The call on the tensors' device and that device's current stream."""
+    raw = _raw_stream(dev)
     if dev == torch.cuda.current_device():
         st = call(*args, raw)
     else:
@@ -306,6 +315,8 @@ def linear_step(q, k, v, log_decay, state, scale=0.0, out=None, state_out=None, 
     """Linear attention with a decay for each head, one token per sequence: ``S' = exp(log_decay) S + k^T v``,
     ``out = scale q S'``.  q ``[B, Hq, d]``, k, v ``[B, Hkv, d]``, state ``[B, Hkv, d, d]`` float32.  state_out: where
     S' goes; None updates `state` in place.  Returns (out, state after)."""
+    if stream is not None:
+        return _on_stream(stream, linear_step, q, k, v, log_decay, state, scale, out, state_out)
     lib = load()
     _, p, s_shape, dev = _linear_setup(q, k, v, log_decay, 1, scale)
     _operand("state", state, s_shape, torch.float32, dev)
@@ -314,7 +325,7 @@ def linear_step(q, k, v, log_decay, state, scale=0.0, out=None, state_out=None, 
         state_out = state
     else:
         _operand("state_out", state_out, s_shape, torch.float32, dev)
-    _launch(dev, stream, lib.bct_linear_step, p, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    _launch(dev, lib.bct_linear_step, p, q.data_ptr(), k.data_ptr(), v.data_ptr(),
             log_decay.data_ptr(), state.data_ptr(), state_out.data_ptr(), out.data_ptr())
     return out, state_out
 
@@ -324,6 +335,8 @@ def linear_forward(q, k, v, log_decay, state=None, lens=None, scale=0.0, out=Non
     """T tokens per sequence: q ``[B, T, Hq, d]``, k, v ``[B, T, Hkv, d]``; state ``[B, Hkv, d, d]`` float32 or None
     (zeros); lens int32 ``[B]`` or None: the valid tokens of each sequence of a padded batch.  Returns (out
     ``[B, T, Hq, d]``, state after each sequence's last token); state_out may be `state`."""
+    if stream is not None:
+        return _on_stream(stream, linear_forward, q, k, v, log_decay, state, lens, scale, out, state_out, scratch)
     lib = load()
     sizes, p, s_shape, dev = _linear_setup(q, k, v, log_decay, 2, scale)
     T = q.shape[1]
@@ -337,7 +350,7 @@ def linear_forward(q, k, v, log_decay, state=None, lens=None, scale=0.0, out=Non
     else:
         _operand("state_out", state_out, s_shape, torch.float32, dev)
     scratch = _scratch(_linear_scratch(*sizes, T, 0), scratch, q, dev)
-    _launch(dev, stream, lib.bct_linear_forward, p, T, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    _launch(dev, lib.bct_linear_forward, p, T, q.data_ptr(), k.data_ptr(), v.data_ptr(),
             log_decay.data_ptr(), _ptr(lens), _ptr(state), state_out.data_ptr(), out.data_ptr(), *_scratch_args(scratch))
     return out, state_out
 
@@ -347,6 +360,8 @@ def linear_backward(d_out, q, k, v, log_decay, state=None, d_state=None, lens=No
     """Backward of linear_forward: d_out ``[B, T, Hq, d]`` and d_state ``[B, Hkv, d, d]`` float32 (the gradient of the
     state after the last token, or None) -> (d_q, d_k, d_v in q's dtype, d_state_in float32).  out: that tuple, to
     write into."""
+    if stream is not None:
+        return _on_stream(stream, linear_backward, d_out, q, k, v, log_decay, state, d_state, lens, scale, out, scratch)
     lib = load()
     sizes, p, s_shape, dev = _linear_setup(q, k, v, log_decay, 2, scale)
     T = q.shape[1]
@@ -362,7 +377,7 @@ def linear_backward(d_out, q, k, v, log_decay, state=None, d_state=None, lens=No
     d_v = _result("d_v", given[2], q, v.shape, q.dtype, dev)
     d_in = _result("d_state_in", given[3], q, s_shape, torch.float32, dev)
     scratch = _scratch(_linear_scratch(*sizes, T, 1), scratch, q, dev)
-    _launch(dev, stream, lib.bct_linear_backward, p, T, d_out.data_ptr(), q.data_ptr(), k.data_ptr(),
+    _launch(dev, lib.bct_linear_backward, p, T, d_out.data_ptr(), q.data_ptr(), k.data_ptr(),
             v.data_ptr(), log_decay.data_ptr(), _ptr(lens), _ptr(state), _ptr(d_state), d_q.data_ptr(), d_k.data_ptr(),
             d_v.data_ptr(), d_in.data_ptr(), *_scratch_args(scratch))
     return d_q, d_k, d_v, d_in
@@ -410,6 +425,8 @@ def norm_rotate(q, k, w_q, w_k, positions, freq, eps=1e-6, interleaved=False, ou
     and the rotation of their first ``2 len(freq)`` features by ``positions * freq``: positions int64 ``[...]``, freq
     float64, radians per position (None: norm only).  interleaved: neighbouring features are the pairs, instead of
     those half the rotated part away.  out: (q, k) to write into, which may be the inputs.  Returns (q, k)."""
+    if stream is not None:
+        return _on_stream(stream, norm_rotate, q, k, w_q, w_k, positions, freq, eps, interleaved, out)
     lib = load()
     n, Hq, Hkv, d, dt, rot = _norm_rotate_setup(q, k, w_q, w_k, positions, freq)
     dev = q.get_device()
@@ -419,7 +436,7 @@ def norm_rotate(q, k, w_q, w_k, positions, freq, eps=1e-6, interleaved=False, ou
         q_out, k_out = out
         _operand("q_out", q_out, q.shape, q.dtype, dev)
         _operand("k_out", k_out, k.shape, q.dtype, dev)
-    _launch(dev, stream, lib.bct_norm_rotate, n, Hq, Hkv, d, dt, q.data_ptr(), k.data_ptr(), _ptr(w_q), _ptr(w_k), eps,
+    _launch(dev, lib.bct_norm_rotate, n, Hq, Hkv, d, dt, q.data_ptr(), k.data_ptr(), _ptr(w_q), _ptr(w_k), eps,
             _ptr(positions) if rot else None, _ptr(freq) if rot else None, rot, ROTATE_INTERLEAVED if interleaved else 0,
             q_out.data_ptr(), k_out.data_ptr())
     return q_out, k_out
@@ -429,6 +446,9 @@ def norm_rotate_backward(d_q_out, d_k_out, q, k, w_q, w_k, positions, freq, eps=
                          out=None, scratch=None, stream=None):
     """Backward of norm_rotate, given the gradients of its two results and its inputs -> (d_q, d_k in q's dtype, d_w_q,
     d_w_k float32 or None).  out: that tuple, to write into (d_q may be d_q_out, d_k may be d_k_out)."""
+    if stream is not None:
+        return _on_stream(stream, norm_rotate_backward, d_q_out, d_k_out, q, k, w_q, w_k, positions, freq, eps, interleaved,
+                          want_d_w, out, scratch)
     lib = load()
     n, Hq, Hkv, d, dt, rot = _norm_rotate_setup(q, k, w_q, w_k, positions, freq)
     dev = q.get_device()
@@ -445,7 +465,7 @@ def norm_rotate_backward(d_q_out, d_k_out, q, k, w_q, w_k, positions, freq, eps=
         scratch = _scratch(need.value, scratch, q, dev)
     else:
         scratch = None
-    _launch(dev, stream, lib.bct_norm_rotate_backward, n, Hq, Hkv, d, dt, d_q_out.data_ptr(), d_k_out.data_ptr(),
+    _launch(dev, lib.bct_norm_rotate_backward, n, Hq, Hkv, d, dt, d_q_out.data_ptr(), d_k_out.data_ptr(),
             q.data_ptr(), k.data_ptr(), _ptr(w_q), _ptr(w_k), eps, _ptr(positions) if rot else None,
             _ptr(freq) if rot else None, rot, ROTATE_INTERLEAVED if interleaved else 0, d_q.data_ptr(), d_k.data_ptr(),
             _ptr(d_w_q), _ptr(d_w_k), *_scratch_args(scratch))

@@ -36,7 +36,7 @@ bool overlap(const Span& x, const Span& y) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
     return x.p != nullptr && y.p != nullptr && x.bytes > 0 && y.bytes > 0 && a < b + y.bytes && b < a + x.bytes;
 }
-bct_status_t check_spans(const Span* s, int n) {
+bct_status_t check_spans(const Span* s, int n) {   // the operands that kernels read and write 16 bytes at a time
     for (int i = 0; i < n; ++i) {
         if (s[i].p == nullptr && !s[i].may_be_null) return fail(BCT_ERR_INVALID_ARG, "%s must not be NULL", s[i].name);
         if (!aligned(s[i].p, 16)) return fail(BCT_ERR_INVALID_ARG, "%s must be 16-byte aligned", s[i].name);
@@ -69,6 +69,7 @@ bct_status_t resolve(const bct_linear_params_t* in, bct_linear_params_t* p) {
         return fail(BCT_ERR_UNSUPPORTED, "head_dim %d: this library has kernels for 64 and 128", p->head_dim);
     if ((long long)p->batch * p->n_kv_heads > (1LL << 20) || p->n_q_heads > (1 << 16))
         return fail(BCT_ERR_INVALID_ARG, "batch * n_kv_heads or n_q_heads too large");
+    if (std::isnan(p->scale)) return fail(BCT_ERR_INVALID_ARG, "scale is not a number");
     if (!(p->scale > 0.f)) p->scale = 1.0f / std::sqrt((float)p->head_dim);
     if (!std::isfinite(p->scale) || !std::isfinite(1.f / p->scale))
         return fail(BCT_ERR_INVALID_ARG, "scale must be finite, and its reciprocal too");
@@ -77,7 +78,7 @@ bct_status_t resolve(const bct_linear_params_t* in, bct_linear_params_t* p) {
 
 // Sizes of one call's tensors.
 struct Sizes {
-    size_t q, kv, state;
+    size_t q, kv, state, decay, lens;
 };
 Sizes sizes_of(const bct_linear_params_t& p, int64_t T) {
     const size_t eb = p.dtype == BCT_F32 ? 4 : 2;
@@ -85,6 +86,8 @@ Sizes sizes_of(const bct_linear_params_t& p, int64_t T) {
     s.q = (size_t)p.batch * (size_t)T * p.n_q_heads * p.head_dim * eb;
     s.kv = (size_t)p.batch * (size_t)T * p.n_kv_heads * p.head_dim * eb;
     s.state = (size_t)p.batch * p.n_kv_heads * p.head_dim * p.head_dim * sizeof(float);
+    s.decay = (size_t)p.n_kv_heads * sizeof(float);
+    s.lens = (size_t)p.batch * sizeof(int32_t);
     return s;
 }
 bct_status_t check_tokens(const bct_linear_params_t& p, int64_t T) {
@@ -137,11 +140,12 @@ bct_status_t bct_linear_step(const bct_linear_params_t* params, const void* q, c
     if (st == BCT_OK) st = check_decay(log_decay);
     if (st != BCT_OK) return st;
     const Sizes s = sizes_of(p, 1);
-    const Span in[] = {{"q", q, s.q, false}, {"k", k, s.kv, false}, {"v", v, s.kv, false}, {"state", state, s.state, false}};
+    const Span in[] = {{"q", q, s.q, false}, {"k", k, s.kv, false}, {"v", v, s.kv, false}, {"state", state, s.state, false},
+                       {"log_decay", log_decay, s.decay, false}};
     const Span outs[] = {{"out", out, s.q, false}, {"state_out", state_out, s.state, false}};
     const int in_place[] = {-1, 3};
     if ((st = check_spans(in, 4)) != BCT_OK || (st = check_spans(outs, 2)) != BCT_OK) return st;
-    if ((st = check_overlap(in, 4, outs, 2, in_place)) != BCT_OK) return st;
+    if ((st = check_overlap(in, 5, outs, 2, in_place)) != BCT_OK) return st;
     const cudaError_t e = bct::launch_linear_step(p, q, k, v, log_decay, state, state_out, out, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? BCT_OK : fail_cuda("linear step launch", e);
 }
@@ -159,11 +163,12 @@ bct_status_t bct_linear_forward(const bct_linear_params_t* params, int64_t T, co
     const bct::LinPlan plan = bct::lin_plan(p, T, 0);
     const size_t need = scratch_need(p, T, false);
     if ((st = check_scratch(scratch, scratch_bytes, need)) != BCT_OK) return st;
-    const Span in[] = {{"q", q, s.q, false}, {"k", k, s.kv, false}, {"v", v, s.kv, false}, {"state", state, s.state, true}};
+    const Span in[] = {{"q", q, s.q, false}, {"k", k, s.kv, false}, {"v", v, s.kv, false}, {"state", state, s.state, true},
+                       {"log_decay", log_decay, s.decay, false}, {"lens", lens, s.lens, true}};
     const Span outs[] = {{"out", out, s.q, false}, {"state_out", state_out, s.state, true}, {"scratch", need ? scratch : nullptr, need, true}};
     const int in_place[] = {-1, 3, -1};
     if ((st = check_spans(in, 4)) != BCT_OK || (st = check_spans(outs, 3)) != BCT_OK) return st;
-    if ((st = check_overlap(in, 4, outs, 3, in_place)) != BCT_OK) return st;
+    if ((st = check_overlap(in, 6, outs, 3, in_place)) != BCT_OK) return st;
 
     const int G = p.n_q_heads / p.n_kv_heads;
     bct::LinArgs a = {};
@@ -194,7 +199,8 @@ bct_status_t bct_linear_backward(const bct_linear_params_t* params, int64_t T, c
     const size_t need = scratch_need(p, T, true);
     if ((st = check_scratch(scratch, scratch_bytes, need)) != BCT_OK) return st;
     const Span in[] = {{"d_out", d_out, s.q, false}, {"q", q, s.q, false},          {"k", k, s.kv, false},
-                       {"v", v, s.kv, false},        {"state", state, s.state, true}, {"d_state", d_state, s.state, true}};
+                       {"v", v, s.kv, false},        {"state", state, s.state, true}, {"d_state", d_state, s.state, true},
+                       {"log_decay", log_decay, s.decay, false}, {"lens", lens, s.lens, true}};
     const Span outs[] = {{"d_q", d_q, s.q, false},
                          {"d_k", d_k, s.kv, false},
                          {"d_v", d_v, s.kv, false},
@@ -202,7 +208,7 @@ bct_status_t bct_linear_backward(const bct_linear_params_t* params, int64_t T, c
                          {"scratch", need ? scratch : nullptr, need, true}};
     const int in_place[] = {-1, -1, -1, -1, -1};
     if ((st = check_spans(in, 6)) != BCT_OK || (st = check_spans(outs, 5)) != BCT_OK) return st;
-    if ((st = check_overlap(in, 6, outs, 5, in_place)) != BCT_OK) return st;
+    if ((st = check_overlap(in, 8, outs, 5, in_place)) != BCT_OK) return st;
 
     const int G = p.n_q_heads / p.n_kv_heads;
     // In reverse the state is carried without the scale that q has in it: R = sum lambda^.. q^T do, times `scale`
@@ -224,7 +230,7 @@ bct_status_t bct_linear_backward(const bct_linear_params_t* params, int64_t T, c
         a.lens = lens;
         a.B = p.batch, a.Hkv = p.n_kv_heads, a.T = (int)T;
         a.nseg = plan.nseg, a.seg_len = plan.seg_len;
-            for (int i = kind == 3 ? 1 : 0; i < (kind == 2 ? 1 : 3); ++i) a.role[a.n_roles++] = roles[i];
+        for (int i = kind == 3 ? 1 : 0; i < (kind == 2 ? 1 : 3); ++i) a.role[a.n_roles++] = roles[i];
         bct::LinStates states = {};
         states.b[0] = k, states.c[0] = v, states.seg[0] = seg0, states.first[0] = state, states.in_mul[0] = 1.f, states.G[0] = 1;
         states.b[1] = q, states.c[1] = d_out, states.seg[1] = seg1, states.first[1] = d_state, states.in_mul[1] = inv, states.G[1] = G;
@@ -274,11 +280,13 @@ bct_status_t bct_norm_rotate(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_h
     bct_status_t st = check_norm_rotate(n_tokens, n_q_heads, n_kv_heads, head_dim, dtype, eps, positions, freq, rot_dim,
                                         flags, &qb, &kb, &wb);
     if (st != BCT_OK) return st;
-    const Span in[] = {{"q", q, qb, false}, {"k", k, kb, false}, {"w_q", w_q, wb, true}, {"w_k", w_k, wb, true}};
+    const Span in[] = {{"q", q, qb, false}, {"k", k, kb, false}, {"w_q", w_q, wb, true}, {"w_k", w_k, wb, true},
+                       {"positions", rot_dim ? positions : nullptr, (size_t)n_tokens * 8, true},
+                       {"freq", rot_dim ? freq : nullptr, (size_t)rot_dim * 4, true}};
     const Span outs[] = {{"q_out", q_out, qb, false}, {"k_out", k_out, kb, false}};
     const int in_place[] = {0, 1};
     if ((st = check_spans(in, 4)) != BCT_OK || (st = check_spans(outs, 2)) != BCT_OK) return st;
-    if ((st = check_overlap(in, 4, outs, 2, in_place)) != BCT_OK) return st;
+    if ((st = check_overlap(in, 6, outs, 2, in_place)) != BCT_OK) return st;
     const cudaError_t e = bct::launch_norm_rotate(n_tokens, n_q_heads, n_kv_heads, head_dim, dtype, q, k, w_q, w_k, eps,
                                                   positions, freq, rot_dim, (flags & BCT_ROTATE_INTERLEAVED) != 0, q_out,
                                                   k_out, static_cast<cudaStream_t>(cuda_stream));
@@ -308,7 +316,9 @@ bct_status_t bct_norm_rotate_backward(int64_t n_tokens, int32_t n_q_heads, int32
         if (st != BCT_OK) return st;
     }
     const Span in[] = {{"d_q_out", d_q_out, qb, false}, {"d_k_out", d_k_out, kb, false}, {"q", q, qb, false},
-                       {"k", k, kb, false},             {"w_q", w_q, wb, true},          {"w_k", w_k, wb, true}};
+                       {"k", k, kb, false},             {"w_q", w_q, wb, true},          {"w_k", w_k, wb, true},
+                       {"positions", rot_dim ? positions : nullptr, (size_t)n_tokens * 8, true},
+                       {"freq", rot_dim ? freq : nullptr, (size_t)rot_dim * 4, true}};
     const size_t fw = (size_t)head_dim * sizeof(float);
     const Span outs[] = {{"d_q", d_q, qb, false},
                          {"d_k", d_k, kb, false},
@@ -317,7 +327,7 @@ bct_status_t bct_norm_rotate_backward(int64_t n_tokens, int32_t n_q_heads, int32
                          {"scratch", need ? scratch : nullptr, need, true}};
     const int in_place[] = {0, 1, -1, -1, -1};
     if ((st = check_spans(in, 6)) != BCT_OK || (st = check_spans(outs, 5)) != BCT_OK) return st;
-    if ((st = check_overlap(in, 6, outs, 5, in_place)) != BCT_OK) return st;
+    if ((st = check_overlap(in, 8, outs, 5, in_place)) != BCT_OK) return st;
     const cudaError_t e = bct::launch_norm_rotate_bwd(
         n_tokens, n_q_heads, n_kv_heads, head_dim, dtype, d_q_out, d_k_out, q, k, w_q, w_k, eps, positions, freq, rot_dim,
         (flags & BCT_ROTATE_INTERLEAVED) != 0, d_q, d_k, d_w_q, d_w_k, static_cast<float*>(need ? scratch : nullptr),

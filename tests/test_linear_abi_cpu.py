@@ -167,3 +167,20 @@ def test_the_binding_refuses_tensors_the_library_cannot_see_the_layout_of():
         B.norm_rotate(q, k, None, None, None, None)
     with pytest.raises(ValueError):
         B.linear_step(q.half(), k.half(), k.half(), g, s)
+
+
+def test_results_over_decays_lengths_positions_or_frequencies_are_refused(lib):
+    p = _p()
+    assert _step(lib, p, out=A[3] - 16) == B.BCT_ERR_INVALID_ARG and "log_decay" in B.last_error()
+    assert _fwd(lib, p, state_out=A[3] - 256) == B.BCT_ERR_INVALID_ARG and "log_decay" in B.last_error()
+    assert _fwd(lib, p, lens=A[6] + 16) == B.BCT_ERR_INVALID_ARG and "lens" in B.last_error()
+    assert _bwd(lib, p, lens=A[9] + 4) == B.BCT_ERR_INVALID_ARG and "lens" in B.last_error()
+    assert _bwd(lib, p, d_k=A[4] - 64) == B.BCT_ERR_INVALID_ARG and "log_decay" in B.last_error()
+    assert _nr(lib, k_out=A[4] + 48) == B.BCT_ERR_INVALID_ARG and "positions" in B.last_error()
+    assert _nrb(lib, d_q=A[5] + 496) == B.BCT_ERR_INVALID_ARG and "freq" in B.last_error()
+
+
+def test_a_scale_that_is_not_a_number_is_refused(lib):
+    p = _p(scale=float("nan"))
+    assert _step(lib, p) == B.BCT_ERR_INVALID_ARG and "scale" in B.last_error()
+    assert _fwd(lib, p) == B.BCT_ERR_INVALID_ARG and _bwd(lib, p) == B.BCT_ERR_INVALID_ARG

@@ -384,3 +384,27 @@ def test_a_large_state_under_a_strong_decay(Hq, Hkv):
     mag, mS = R.linear_forward(q.abs(), k.abs(), v.abs(), ld, S.abs())
     _check("out", out[:, 40:], ref[:, 40:], mag[:, 40:], "bf16", 128 + 130 + 64, tensor=True)
     _check("state", S1, rS, mS, "f32", 128 + 130 + 64)
+
+
+def test_a_stream_argument_owns_what_the_call_allocates():
+    # the stream is kept busy, and the current stream takes and overwrites all memory that the call could have let go
+    q, k, v, ld, S = _inputs(1, 1500, 2, 2, 128, "bf16", 67)
+    need = B.linear_scratch_bytes(1, 1500, 2, 2, 128, torch.bfloat16)
+    assert need > 0
+    do = torch.randn_like(q.float()).to(q.dtype)
+    want, wantb = B.linear_forward(q, k, v, ld, state=S), B.linear_backward(do, q, k, v, ld, state=S)
+    w = torch.ones(128, device="cuda", dtype=torch.bfloat16)
+    pos, freq = torch.arange(1500, device="cuda")[None], torch.linspace(1.0, 0.01, 64, device="cuda", dtype=torch.float64)
+    wantn = B.norm_rotate_backward(q, k, q, k, w, w, pos, freq)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+    got = B.linear_forward(q, k, v, ld, state=S, stream=s)
+    gotb = B.linear_backward(do, q, k, v, ld, state=S, stream=s)
+    gotn = B.norm_rotate_backward(q, k, q, k, w, w, pos, freq, stream=s)
+    held = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (need, 2 * need, need, 1 << 20, 1 << 21) for _ in range(3)]
+    torch.cuda.synchronize()
+    for a, b in ((got, want), (gotb, wantb), (gotn, wantn)):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    del held
