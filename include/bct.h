@@ -287,8 +287,7 @@ bct_status_t bct_stack_forward(bct_cache_t *const *caches, int32_t n_layers, con
  * backward in BCT_BF16 run on the tensor cores: the products of pairs (q_t . k_s and their like, weighted with the
  * decay) and the state where it enters a product are each rounded to bfloat16 once, sums are fp32, and `out` and the
  * gradients are rounded once; the float states (state_out, d_state_in) are the tensor cores' fp32 sums of unrounded
- * products, off by less than 1e-6 of them (root mean square); with G > 1 heads to a state d_state_in adds up G times as
- * many, each cut off at fp32: 0.7e-6 G.
+ * products, off by less than 1e-6 of them (root mean square).
  * No atomics: the same call gives the same bits.  A NaN or an infinity in a token that counts may also reach the
  * results of up to 127 tokens before it (of those after it, in the backward), as 0 * infinity; one in a padding row
  * reaches nothing.
@@ -341,7 +340,7 @@ bct_status_t bct_linear_forward(const bct_linear_params_t *params, int64_t T, co
  *   d_out      DEVICE [B][T][Hq][d]      q, k, v, lens, state   the forward call's (state NULL: zeros)
  *   d_state    DEVICE float [B][Hkv][d][d], or NULL (zeros)
  *   d_q        DEVICE [B][T][Hq][d]      d_k, d_v  DEVICE [B][T][Hkv][d], in `dtype`; zero in padding rows
- *   d_state_in DEVICE float [B][Hkv][d][d], or NULL
+ *   d_state_in DEVICE float [B][Hkv][d][d], or NULL: with G > 1 in BCT_BF16 it costs a pass of its own over q and d_out
  *   scratch    as above, bct_linear_scratch_bytes(params, T, 1)
  */
 bct_status_t bct_linear_backward(const bct_linear_params_t *params, int64_t T, const void *d_out, const void *q,

@@ -356,12 +356,13 @@ def linear_forward(q, k, v, log_decay, state=None, lens=None, scale=0.0, out=Non
 
 
 def linear_backward(d_out, q, k, v, log_decay, state=None, d_state=None, lens=None, scale=0.0, out=None, scratch=None,
-                    stream=None):
+                    stream=None, want_d_state=True):
     """Backward of linear_forward: d_out ``[B, T, Hq, d]`` and d_state ``[B, Hkv, d, d]`` float32 (the gradient of the
-    state after the last token, or None) -> (d_q, d_k, d_v in q's dtype, d_state_in float32).  out: that tuple, to
-    write into."""
+    state after the last token, or None) -> (d_q, d_k, d_v in q's dtype, d_state_in float32 or None).  out: that tuple,
+    to write into."""
     if stream is not None:
-        return _on_stream(stream, linear_backward, d_out, q, k, v, log_decay, state, d_state, lens, scale, out, scratch)
+        return _on_stream(stream, linear_backward, d_out, q, k, v, log_decay, state, d_state, lens, scale, out, scratch,
+                          None, want_d_state)
     lib = load()
     sizes, p, s_shape, dev = _linear_setup(q, k, v, log_decay, 2, scale)
     T = q.shape[1]
@@ -375,11 +376,11 @@ def linear_backward(d_out, q, k, v, log_decay, state=None, d_state=None, lens=No
     d_q = _result("d_q", given[0], q, q.shape, q.dtype, dev)
     d_k = _result("d_k", given[1], q, k.shape, q.dtype, dev)
     d_v = _result("d_v", given[2], q, v.shape, q.dtype, dev)
-    d_in = _result("d_state_in", given[3], q, s_shape, torch.float32, dev)
+    d_in = _result("d_state_in", given[3], q, s_shape, torch.float32, dev) if want_d_state else None
     scratch = _scratch(_linear_scratch(*sizes, T, 1), scratch, q, dev)
     _launch(dev, lib.bct_linear_backward, p, T, d_out.data_ptr(), q.data_ptr(), k.data_ptr(),
             v.data_ptr(), log_decay.data_ptr(), _ptr(lens), _ptr(state), _ptr(d_state), d_q.data_ptr(), d_k.data_ptr(),
-            d_v.data_ptr(), d_in.data_ptr(), *_scratch_args(scratch))
+            d_v.data_ptr(), _ptr(d_in), *_scratch_args(scratch))
     return d_q, d_k, d_v, d_in
 
 

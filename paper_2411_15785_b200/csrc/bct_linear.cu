@@ -286,6 +286,33 @@ __global__ void __launch_bounds__(256) linear_combine_kernel(const LinArgs args,
     }
 }
 
+// What every segment adds comes by head (slot s of a head: what segment s adds): the running sum in reverse over the
+// segments and, in each, over the heads that share the state, in fp32 and in a fixed order.  Slot s of `seg`, where there
+// is one, gets what segment s starts from, `last` what comes out of the first token.
+__global__ void __launch_bounds__(256) linear_combine_heads_kernel(const LinArgs args, const LinStates st, int DD) {
+    const int u = blockIdx.x;
+    const int e = (blockIdx.y * 256 + threadIdx.x) * 4;
+    if (e >= DD) return;
+    const int bi = u / args.Hkv, h = u - bi * args.Hkv;
+    const int len = args.lens ? min(max(args.lens[bi], 0), args.T) : args.T;
+    const double g = (double)args.log_decay[h];
+    const float* add = st.by_head + (size_t)u * st.heads * args.nseg * DD + e;
+    float4 run = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (st.first[1] != nullptr) run = mul4(st.in_mul[1], *reinterpret_cast<const float4*>(st.first[1] + (size_t)u * DD + e));
+    for (int s = args.nseg - 1; s >= 0; --s) {
+        if (st.seg[1] != nullptr) *reinterpret_cast<float4*>(st.seg[1] + ((size_t)u * args.nseg + s) * DD + e) = run;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int x = 0; x < st.heads; ++x) {
+            const float4 y = *reinterpret_cast<const float4*>(add + ((size_t)x * args.nseg + s) * DD);
+            sum = make_float4(sum.x + y.x, sum.y + y.y, sum.z + y.z, sum.w + y.w);
+        }
+        const int nv = min(max(len - s * args.seg_len, 0), args.seg_len);
+        run = fma4(nv == 0 ? 1.f : (float)exp((double)nv * g), run, sum);
+    }
+    *reinterpret_cast<float4*>(st.last + (size_t)u * DD + e) = mul4(st.last_mul, run);
+}
+
 // One token for every unit: S' = lambda S + k^T v, o_g = scale q_g S'.  Bound by the state's bytes (read and
 // written once).  A block holds 32 columns of one unit's state (128-byte row pieces): eight lanes per row, so
 // that a thread's rows are all asked for before the first is used, and four blocks share a unit, which fills the
@@ -378,6 +405,12 @@ cudaError_t launch_linear_combine(int D, const LinArgs& args, const LinStates& s
     const int dirs = (st.seg[0] != nullptr) + (st.seg[1] != nullptr);
     const dim3 grid((unsigned)(args.B * args.Hkv), (unsigned)((D * D / 4 + 255) / 256), (unsigned)dirs);
     linear_combine_kernel<<<grid, 256, 0, stream>>>(args, st, D * D);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_linear_combine_heads(int D, const LinArgs& args, const LinStates& st, cudaStream_t stream) {
+    const dim3 grid((unsigned)(args.B * args.Hkv), (unsigned)((D * D / 4 + 255) / 256));
+    linear_combine_heads_kernel<<<grid, 256, 0, stream>>>(args, st, D * D);
     return cudaGetLastError();
 }
 

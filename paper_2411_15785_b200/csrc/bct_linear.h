@@ -63,6 +63,12 @@ struct LinStates {
     const float* first[2];    // the state before the first segment, or NULL
     float in_mul[2];
     int G[2];
+    // Not NULL (tensor path, reverse direction alone, G > 1): what every segment adds is formed by head, [B][Hkv * heads]
+    // [nseg][D][D], and summed over the heads on the way; the state after the scan then goes to `last`, times last_mul.
+    float* by_head;
+    int heads;
+    float* last;
+    float last_mul;
 };
 
 struct LinPlan {
@@ -86,6 +92,8 @@ cudaError_t launch_linear_scan(const bct_linear_params_t& p, const LinPlan& plan
 cudaError_t launch_linear_tc(int D, const LinArgs& args, const LinStates& states, cudaStream_t stream);
 // Running sums over the segments, in the order of the scan.
 cudaError_t launch_linear_combine(int D, const LinArgs& args, const LinStates& states, cudaStream_t stream);
+// The same over segments and heads (states.by_head).
+cudaError_t launch_linear_combine_heads(int D, const LinArgs& args, const LinStates& states, cudaStream_t stream);
 
 cudaError_t launch_norm_rotate(int64_t n_tokens, int Hq, int Hkv, int D, int dtype, const void* q, const void* k,
                                const void* w_q, const void* w_k, float eps, const int64_t* positions, const double* freq,

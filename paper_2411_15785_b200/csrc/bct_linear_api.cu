@@ -103,10 +103,15 @@ bct_status_t check_scratch(const void* scratch, size_t bytes, size_t need) {
 }
 // One launch serves roles that all have several heads on A's side, or none: the backward of shared heads takes two.
 bool two_launches(const bct_linear_params_t& p) { return p.dtype == BCT_BF16 && p.n_q_heads > p.n_kv_heads; }
+// What every segment adds to the state in reverse, by head.
+size_t by_head_bytes(const bct_linear_params_t& p, const bct::LinPlan& plan) {
+    return round256((size_t)p.batch * p.n_q_heads * plan.nseg * p.head_dim * p.head_dim * sizeof(float));
+}
 size_t scratch_need(const bct_linear_params_t& p, int64_t T, bool backward) {
     if (!backward) return round256(bct::lin_plan(p, T, 0).seg_bytes);
     if (!two_launches(p)) return 2 * round256(bct::lin_plan(p, T, 1).seg_bytes);
-    const size_t a = round256(bct::lin_plan(p, T, 2).seg_bytes), b = round256(bct::lin_plan(p, T, 3).seg_bytes);
+    const bct::LinPlan last = bct::lin_plan(p, T, 3);
+    const size_t a = round256(bct::lin_plan(p, T, 2).seg_bytes), b = round256(last.seg_bytes) + by_head_bytes(p, last);
     return a > b ? a : b;   // one after the other, in the same place
 }
 bct_status_t check_lens(const int32_t* lens) {
@@ -222,9 +227,11 @@ bct_status_t bct_linear_backward(const bct_linear_params_t* params, int64_t T, c
         float* seg0 = plan.nseg > 1 && kind != 3 ? seg : nullptr;
         if (seg0 != nullptr) seg += round256(plan.seg_bytes) / sizeof(float);
         float* seg1 = plan.nseg > 1 && kind != 2 ? seg : nullptr;
+        if (seg1 != nullptr) seg += round256(plan.seg_bytes) / sizeof(float);
+        float* by_head = kind == 3 && d_state_in != nullptr ? seg : nullptr;
         const bct::LinRole roles[3] = {{d_out, v, k, d_q, state, nullptr, seg0, G, 1, 0, 1, p.scale, 1.f, 1.f},
                                        {v, d_out, q, d_k, d_state, nullptr, seg1, 1, G, 1, 1, p.scale, inv, 1.f},
-                                       {k, q, d_out, d_v, d_state, d_state_in, seg1, 1, G, 1, 0, p.scale, inv, p.scale}};
+                                       {k, q, d_out, d_v, d_state, by_head ? nullptr : d_state_in, seg1, 1, G, 1, 0, p.scale, inv, p.scale}};
         bct::LinArgs a = {};
         a.log_decay = log_decay;
         a.lens = lens;
@@ -234,6 +241,7 @@ bct_status_t bct_linear_backward(const bct_linear_params_t* params, int64_t T, c
         bct::LinStates states = {};
         states.b[0] = k, states.c[0] = v, states.seg[0] = seg0, states.first[0] = state, states.in_mul[0] = 1.f, states.G[0] = 1;
         states.b[1] = q, states.c[1] = d_out, states.seg[1] = seg1, states.first[1] = d_state, states.in_mul[1] = inv, states.G[1] = G;
+        states.by_head = by_head, states.heads = G, states.last = d_state_in, states.last_mul = p.scale;
         const cudaError_t e = bct::launch_linear_scan(p, plan, a, states, static_cast<cudaStream_t>(cuda_stream));
         if (e != cudaSuccess) return fail_cuda("linear backward launch", e);
     }

@@ -255,7 +255,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     const LinRole& r = s.role[STATE_ONLY ? 0 : which];
     const int reverse = STATE_ONLY ? which : r.reverse;
     const int Ga = MULTI_A ? r.Ga : 1, Gb = MULTI_A ? 1 : (STATE_ONLY ? args.st.G[which] : r.Gb);
-    if (STATE_ONLY && seg == (reverse ? 0 : s.nseg - 1)) return;   // feeds no other segment
+    const bool by_head = STATE_ONLY && args.st.by_head != nullptr;   // (s.Hkv counts the heads of b then)
+    if (STATE_ONLY && !by_head && seg == (reverse ? 0 : s.nseg - 1)) return;   // feeds no other segment
     const CUtensorMap* map_a = &args.in[STATE_ONLY ? 0 : args.map_a[which]];
     const CUtensorMap* map_b = &args.in[STATE_ONLY ? args.st_map_b[which] : args.map_b[which]];
     const CUtensorMap* map_c = &args.in[STATE_ONLY ? args.st_map_c[which] : args.map_c[which]];
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         fence_mbar_init_cluster();
     }
     if (warp == 0) tmem_alloc(tmem_slot, 512);
-    const float log_decay = s.log_decay[h];
+    const float log_decay = s.log_decay[by_head ? h / args.st.heads : h];
     if (tid < 256) {   // the powers in double, rounded once
         const int d = reverse ? tid - 127 : 127 - tid;
         pt[tid] = d < 0 ? 0.f : (d == 0 ? 1.f : (float)exp((double)log_decay * d));
@@ -877,8 +878,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         const float poison = *abort_flag ? __int_as_float(0x7fc00000) : 0.f;
         float* dst = nullptr;
         float mul = 1.f;
-        if (STATE_ONLY) {   // into the slot of the segment that it feeds, key's features in the rows
-            dst = args.st.seg[which] + ((size_t)u * s.nseg + (reverse ? seg - 1 : seg + 1)) * (D * D);
+        if (STATE_ONLY) {   // into the slot of the segment that it feeds (by head: its own), key's features in the rows
+            dst = args.st.seg[which] + ((size_t)u * s.nseg + (by_head ? seg : (reverse ? seg - 1 : seg + 1))) * (D * D);
         } else if (r.state_out != nullptr && seg == (reverse ? 0 : s.nseg - 1)) {
             dst = r.state_out + (size_t)u * (D * D);   // (never transposed)
             mul = r.out_mul;
@@ -981,7 +982,20 @@ cudaError_t launch_all(const LinArgs& args, const LinStates& states, cudaStream_
         if (a.map_a[i] < 0 || a.map_b[i] < 0 || a.map_c[i] < 0) return cudaErrorInvalidValue;
         if (!lt_map(&a.out[i], r.out, args.B, args.T, args.Hkv * r.Ga, D)) return cudaErrorInvalidValue;
     }
-    if (args.nseg > 1) {
+    if (states.by_head != nullptr) {
+        // A state that G heads add to, G tiles to a chunk, would be off by G times what the cutting off of the tensor
+        // cores' sums leaves (2.6e-6 with four heads); by head it is as exact as with one.
+        a.st_map_b[1] = map_of(states.b[1], states.heads);
+        a.st_map_c[1] = map_of(states.c[1], states.heads);
+        if (a.st_map_b[1] < 0 || a.st_map_c[1] < 0) return cudaErrorInvalidValue;
+        LtArgs x = a;
+        x.s.Hkv = args.Hkv * states.heads;
+        x.st.G[1] = 1;
+        x.st.seg[0] = nullptr, x.st.seg[1] = states.by_head;
+        cudaError_t e = lt_launch<D, true, false>(x, 1, stream);
+        if (e == cudaSuccess) e = launch_linear_combine_heads(D, args, states, stream);
+        if (e != cudaSuccess) return e;
+    } else if (args.nseg > 1) {
         for (int d = 0; d < 2; ++d) {
             if (states.seg[d] == nullptr) continue;
             a.st_map_b[d] = map_of(states.b[d], states.G[d]);

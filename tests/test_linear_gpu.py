@@ -408,3 +408,41 @@ def test_a_stream_argument_owns_what_the_call_allocates():
     for a, b in ((got, want), (gotb, wantb), (gotn, wantn)):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
     del held
+
+
+@pytest.mark.parametrize("Bt,T,Hq,Hkv,d,lens", [(2, 300, 8, 2, 128, None), (1, 1500, 16, 2, 128, None), (1, 700, 15, 1, 64, None),
+                                                (3, 400, 6, 2, 64, [400, 0, 129]), (40, 130, 8, 4, 128, None), (1, 1, 2, 1, 128, None)])
+def test_the_state_gradient_of_shared_heads_is_as_exact_as_one_heads(Bt, T, Hq, Hkv, d, lens):
+    # A head's share is cut off at most 2^-23 of what it has come to at each of 3 * 8 steps of a chunk.  The tokens enter
+    # in the order of their weights, so with these decays the sums of the squares of what has come to be is at most the
+    # last's; chunks before decay.  In root mean square that is below 24 * 2^-24 of the state, whatever the heads.
+    q, k, v, ld, S = _inputs(Bt, T, Hq, Hkv, d, "bf16", 71)
+    g = torch.Generator(device="cuda").manual_seed(72)
+    do = torch.randn(q.shape, generator=g, device="cuda").to(q.dtype)
+    dS = torch.randn((Bt, Hkv, d, d), generator=g, device="cuda")
+    lt = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    lam, G = torch.exp(ld.double())[:, None, None], Hq // Hkv
+    for first in (None, dS):
+        got = B.linear_backward(do, q, k, v, ld, state=S, d_state=first, lens=lt)
+        for b in range(Bt):
+            ref = torch.zeros((Hkv, d, d), dtype=torch.float64, device="cuda") if first is None else dS[b].double().clone()
+            for t in reversed(range(T if lens is None else lens[b])):
+                x, y = (z[b, t].double().view(Hkv, G, d) for z in (q, do))
+                ref = lam * (ref + d ** -0.5 * torch.einsum("hgi,hgj->hij", x, y))
+            err = float((got[3][b].double() - ref).norm())
+            assert err <= 24 * 2.0 ** -24 * float(ref.norm()), (b, err / float(ref.norm()))
+        again = B.linear_backward(do, q, k, v, ld, state=S, d_state=first, lens=lt)
+        assert all(torch.equal(x, y) for x, y in zip(got, again))
+
+
+@pytest.mark.parametrize("Hq,Hkv,dtype", [(4, 2, "bf16"), (2, 2, "bf16"), (4, 2, "f32")])
+def test_backward_without_the_state_gradient(Hq, Hkv, dtype):
+    q, k, v, ld, S = _inputs(1, 700, Hq, Hkv, 128, dtype, 73)
+    with_it = B.linear_backward(q, q, k, v, ld, state=S, d_state=S)
+    without = B.linear_backward(q, q, k, v, ld, state=S, d_state=S, want_d_state=False)
+    assert without[3] is None
+    n = 128 + 700 * (Hq // Hkv) + 64
+    ref, mag = R.linear_backward(q, q, k, v, ld, S, S), _magnitudes(q, q, k, v, ld, S, S, None)
+    for name, x, y, r, m in zip(("d_q", "d_k", "d_v"), without, with_it, ref, mag):
+        _check(name, x, r, m, dtype, n, tensor=True)
+        _check(name, y, r, m, dtype, n, tensor=True)
