@@ -29,7 +29,7 @@
 // work and fills the block's outputs with NaN.
 //
 // Measured: 8 x 4096 tokens of 32 heads of 128 (1.11 GB) 239 us at full clock, 4.6 TB/s, 0.71 of the copy rate; the
-// backward of 4 x 4096 (three scans) 349 us; 16384 tokens of one sequence, 32 heads over 8 states, 124 us (state pass 24,
+// backward of 4 x 4096 (three scans) 349 us; 16384 tokens of one sequence, 32 heads over 8 states, 122 us (state pass 22,
 // segments' states 5, outputs 95).  A chunk takes some 6400 clocks, of which the state's chain (its products 4600, the
 // turn 1600) is the longest; the tensor cores are busy 47 % and the issue slots 50 % of the time.
 #include <cuda.h>
@@ -237,6 +237,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     uint64_t* terms_full = bars + 22;    // [4] its terms in place
     uint64_t* w_full = bars + 26;        // [2] W complete, by items in turn
     uint64_t* p_full = bars + 28;        // [2] P in place
+    uint64_t* kv_done = w_full;          // [4] without W and P: a quarter's products with C complete, by places
     uint64_t* o_full = bars + 30;
     uint64_t* o_empty = bars + 31;
     uint64_t* s_full = bars + 32;        // the state holds the chunk
@@ -288,7 +289,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 mbar_init(&empty_c[i], MULTI_A ? 1 : 2);
             }
             mbar_init(&w_full[i], 1);
-            mbar_init(&p_full[i], 8);
+            mbar_init(&p_full[i], STATE_ONLY ? 1 : 8);
         }
         mbar_init(clean, 8);
         for (int i = 0; i < 4; ++i) {
@@ -402,7 +403,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             }
         }
         __syncwarp();
-    } else if (warp == 0 || (!MULTI_A && !STATE_ONLY && warp == 3)) {
+    } else if (warp == 0 || (!MULTI_A && warp == 3)) {
         // =========================== products ===========================
         constexpr uint32_t id_kk = instr_desc_mn(128, 128, false, false);
         constexpr uint32_t id_kn = instr_desc_mn(128, D, false, true);
@@ -467,7 +468,35 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             umma_terms_warp(tmem + kLtColS, tmem + t_place(qb), dmn.at(ca + first_of(qb & 3)), step_t, id_kn);
         };
         auto ready = [&](uint64_t* bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_test_wait(bar, parity & 1)); };
-        if (!MULTI_A && (STATE_ONLY || warp == 3)) {
+        if constexpr (STATE_ONLY) {
+            // (An item's C has come with its B.)  One warp transposes, up to four quarters ahead, the other adds to the state:
+            // with both in one, 5200 instead of 4200 clocks a chunk went by in issuing them in turn.  (What is left is the chain
+            // of the products and the turn; the idle warps of W and P beside those that weight B^T changed nothing.)
+            int x = 0;
+            if (warp == 3) {
+                for (int n = 0, qb = 0; qb < 4 * items; ++qb) {
+                    if (qb >= kPlaces) LT_WAIT_WARP(&kv_done[qb % kPlaces], qb / kPlaces - 1);
+                    transpose(n);
+                    if ((qb & 3) == 3 && ++x == G) x = 0, ++n;
+                }
+            } else {
+                for (int n = 0, it = 0; it < items; ++it) {
+                    const uint32_t ca = base16 + (L::c + rc.s * kLtTile) / 16;
+                    if (x == 0) LT_WAIT_WARP(x_full, n);
+#pragma unroll 1
+                    for (int qb = 4 * it; qb < 4 * it + 4; ++qb) {
+                        state_products(qb, ca);
+                        umma_commit_warp(&kv_done[qb % kPlaces]);
+                    }
+                    umma_commit_warp(&empty_c[rc.s]);
+                    rc.next(n_b);
+                    if (++x == G) {
+                        umma_commit_warp(s_full);
+                        x = 0, ++n;
+                    }
+                }
+            }
+        } else if (!MULTI_A && warp == 3) {
             // The state: quarters are transposed as far ahead of their products as there are places.  (An item's C has come
             // with its B.)
             int x = 0, xt = 0, nt = 0;   // xt, nt: of the next tile to be transposed
