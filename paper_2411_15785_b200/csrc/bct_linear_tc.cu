@@ -31,7 +31,7 @@
 // Measured: 8 x 4096 tokens of 32 heads of 128 (1.11 GB) 239 us at full clock, 4.6 TB/s, 0.71 of the copy rate; the
 // backward of 4 x 4096 (three scans) 349 us; 16384 tokens of one sequence, 32 heads over 8 states, 122 us (state pass 22,
 // segments' states 5, outputs 95).  A chunk takes some 6400 clocks, of which the state's chain (its products 4600, the
-// turn 1600) is the longest; the tensor cores are busy 47 % and the issue slots 50 % of the time.
+// turn 1600) is the longest; the tensor cores are busy 45 % and the issue slots 49 % of the time.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
