@@ -232,7 +232,10 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     uint64_t* empty_b = STATE_ONLY ? bars + 3 : bars + 11;
     uint64_t* full_c = bars + 13;        // [2]
     uint64_t* empty_c = STATE_ONLY ? bars + 6 : bars + 15;
-    uint64_t* clean = bars + 17;         // padding rows of B and C are zeros
+    // padding rows of B and C are zeros, by padded tiles in turn: [2].  Two warps look at it and only one of them paces the
+    // warps that arrive, so that one barrier could go through two phases between two looks of the other warp, which would
+    // then wait for good; a phase that is two tiles on needs a buffer that both have given back.
+    auto clean = [&](int n) { return bars + (n & 1 ? 37 : 17); };
     uint64_t* bt_full = bars + 18;       // [4] a quarter of B^T complete, by places
     uint64_t* terms_full = bars + 22;    // [4] its terms in place
     uint64_t* w_full = bars + 26;        // [2] W complete, by items in turn
@@ -291,7 +294,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             mbar_init(&w_full[i], 1);
             mbar_init(&p_full[i], STATE_ONLY ? 1 : 8);
         }
-        mbar_init(clean, 8);
+        mbar_init(clean(0), 8);
+        mbar_init(clean(1), 8);
         for (int i = 0; i < 4; ++i) {
             mbar_init(&bt_full[i], 1);
             mbar_init(&terms_full[i], 8);
@@ -331,6 +335,12 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     {                                \
         LT_WAIT(bar, parity);        \
         __syncwarp();                \
+    }
+// for padded tile n, and n counted on
+#define LT_WAIT_CLEAN(n)                     \
+    {                                        \
+        LT_WAIT_WARP(clean(n), (n) >> 1);    \
+        ++(n);                               \
     }
 
     // Where the qb-th quarter tile of B is transposed.  (All four quarters' terms at once have no room beside W, O and the
@@ -429,7 +439,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             const int quarter = n_t & 3;
             if (quarter == 0) {
                 LT_WAIT_WARP(&full_b[rt.s], rt.turn);
-                if (n == n_short) LT_WAIT_WARP(clean, n_clean++);
+                if (n == n_short) LT_WAIT_CLEAN(n_clean);
             }
             tc_fence_after();
             const uint32_t ba = base16 + (L::b + rt.s * kLtTile) / 16 + first_of(quarter);
@@ -541,7 +551,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                         umma4_warp<2, 128>(tmem + kLtColO, dk.at(aa + hf * h16), dmn.at(x16 + hf * 512), id_kn, hf > 0);
                     umma_commit_warp(x_empty);
                 }
-                if (n == n_short) LT_WAIT_WARP(clean, n_clean++);
+                if (n == n_short) LT_WAIT_CLEAN(n_clean);
                 LT_WAIT_WARP(&p_full[it & 1], it >> 1);
                 tc_fence_after();
 #pragma unroll
@@ -713,7 +723,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         // =========================== w o B^T in three terms: two threads per feature of b ===========
         const int q = warp & 3, part = (warp - 12) >> 2, wt = tid & 127;
         const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
-        int nb = 0;
+        int nb = 0, n_clean = 0;
         Ring rb;
         for (int n = 0; n < n_chunks; ++n) {
             const int nv = chunk_nv(chunk_t0(n));
@@ -730,7 +740,8 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(clean);
+                    if (lane == 0) mbar_arrive(clean(n_clean));
+                    ++n_clean;
                 }
 #pragma unroll 1
                 for (int qb = 4 * nb; qb < 4 * nb + 4; ++qb) {
@@ -942,6 +953,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
     }
 #undef LT_WAIT
 #undef LT_WAIT_WARP
+#undef LT_WAIT_CLEAN
     tc_fence_before();
     __syncthreads();
     if (warp == 0) {

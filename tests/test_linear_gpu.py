@@ -446,3 +446,18 @@ def test_backward_without_the_state_gradient(Hq, Hkv, dtype):
     for name, x, y, r, m in zip(("d_q", "d_k", "d_v"), without, with_it, ref, mag):
         _check(name, x, r, m, dtype, n, tensor=True)
         _check(name, y, r, m, dtype, n, tensor=True)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(4, 2, 128), (6, 2, 128), (10, 2, 64), (16, 1, 128)])
+@pytest.mark.parametrize("T", [1, 60, 129, 250])
+def test_reverse_scans_of_shared_heads_that_begin_with_a_padded_chunk(Hq, Hkv, d, T):
+    # every head of the group brings a tile of its own whose padding rows are zeroed: against the formula, and the same bits
+    # each time while every SM runs such a scan
+    _backward_case(2, T, Hq, Hkv, d, "bf16", 79 + T)
+    q, k, v, ld, S = _inputs(80, T, Hq, Hkv, d, "bf16", 83)
+    lens = torch.randint(0, T + 1, (80,), generator=torch.Generator().manual_seed(T), dtype=torch.int32).cuda()
+    first = B.linear_backward(q, q, k, v, ld, state=S, d_state=S, lens=lens)
+    assert all(torch.isfinite(x.float()).all() for x in first)
+    for _ in range(20):
+        again = B.linear_backward(q, q, k, v, ld, state=S, d_state=S, lens=lens)
+        assert all(torch.equal(x, y) for x, y in zip(first, again))
