@@ -213,6 +213,7 @@ __global__ void __launch_bounds__(kNrThreads, 2) norm_rotate_kernel(const NrArgs
 #pragma unroll
                 for (int m = kLanes / 2; m > 0; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
                 float r = rsqrtf(ss * (1.f / D) + a.eps);
+                if (BWD && !valid) r = 0.f;   // (with eps = 0 their r is infinite, and 0 r not 0: it would enter dw)
                 if (!came) r = __int_as_float(0x7fc00000);   // the copy never came: NaN, not old bytes
                 const float2 rr = make_float2(r, r);
                 const float2* v = BWD ? g : x;

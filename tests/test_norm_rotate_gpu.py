@@ -185,3 +185,31 @@ def test_rotated_queries_and_keys_go_into_the_bounded_cache():
     ref = (torch.softmax(s, -1) @ vf).transpose(1, 2)
     assert float((out.double() - ref).abs().max()) <= 2e-2
     cache.destroy()
+
+
+@pytest.mark.parametrize("N,Hq,Hkv,d,dtype", [(1, 1, 1, 128, "bf16"), (50, 3, 1, 128, "bf16"), (700, 7, 5, 128, "bf16"), (33, 2, 1, 64, "bf16"),
+                                              (2500, 7, 3, 64, "bf16"), (90, 3, 1, 64, "f32"), (20, 5, 1, 128, "f32"), (60, 8, 4, 64, "bf16")])
+@pytest.mark.parametrize("inter", [False, True])
+def test_without_eps_whatever_the_number_of_heads(N, Hq, Hkv, d, dtype, inter):
+    # no vector is zero, so nothing is divided by zero; the bounds are those of the tests above
+    q, k, wq, wk, pos, freq = _inputs(N, Hq, Hkv, d, dtype, d, 5000, 43 + N)
+    g = torch.Generator(device="cuda").manual_seed(N)
+    dq, dk = (torch.randn(x.shape, generator=g, device="cuda").to(x.dtype) for x in (q, k))
+    out = B.norm_rotate(q, k, wq, wk, pos, freq, eps=0.0, interleaved=inter)
+    got = B.norm_rotate_backward(dq, dk, q, k, wq, wk, pos, freq, eps=0.0, interleaved=inter)
+    for x, w, dy, y, dx, dw in ((q, wq, dq, out[0], got[0], got[2]), (k, wk, dk, out[1], got[1], got[3])):
+        lx, lw = x.double().requires_grad_(), w.double().requires_grad_()
+        ref = R.norm_rotate(lx, lw, pos, freq, 0.0, inter)
+        rx, rw = torch.autograd.grad((ref * dy.double()).sum(), (lx, lw))
+        ref = ref.detach()
+        half = 2.0 ** -8 if dtype == "bf16" else 0
+        m = _pair_size(R.norm_rotate(x, w, None, None, 0.0, inter), d, inter)
+        assert bool(((y.double() - ref).abs() <= 64 * 2.0 ** -24 * m + half * ref.abs()).all())
+        r = 1 / torch.sqrt(x.double().square().mean(-1, keepdim=True))
+        xh = (x.double() * r).abs()
+        gg = _pair_size(dy.double(), d, inter)
+        n = gg * w.double().abs()
+        mag = r * (n + xh * (n * xh).mean(-1, keepdim=True))
+        assert bool(((dx.double() - rx).abs() <= 96 * 2.0 ** -24 * mag + half * rx.abs()).all())
+        mw = (gg * xh).sum((0, 1))
+        assert bool(((dw.double() - rw).abs() <= (N * x.shape[1] + 64) * 2.0 ** -24 * mw).all())
