@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 import os
 from typing import Optional, Tuple
 
@@ -294,7 +295,8 @@ def _linear_setup(q, k, v, log_decay, n_lead, scale):
     """Checks the operands that every linear-attention call has: q ``[*lead, Hq, d]``, k and v ``[*lead, Hkv, d]``.
     Returns the sizes, the parameters by reference, the state's shape and the device index."""
     dt, dev = q.dtype, q.get_device()
-    sizes, p, kv, hk, s_shape = _linear_sizes(q.shape, k.shape, dt, n_lead, scale)
+    # (float(): the sizes are kept under what they follow from, and a tensor or an array may have changed since)
+    sizes, p, kv, hk, s_shape = _linear_sizes(q.shape, k.shape, dt, n_lead, float(scale))
     if not (dev >= 0 and k.shape == kv and v.shape == kv and k.dtype is dt and v.dtype is dt and log_decay.shape == hk
             and log_decay.dtype is torch.float32 and k.get_device() == dev and v.get_device() == dev
             and log_decay.get_device() == dev and q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
@@ -308,6 +310,7 @@ def _linear_setup(q, k, v, log_decay, n_lead, scale):
 
 def linear_scratch_bytes(batch, T, n_q_heads, n_kv_heads, head_dim, dtype, *, backward=False) -> int:
     """Scratch that linear_forward (or linear_backward) needs for these sizes."""
+    batch, T, n_q_heads, n_kv_heads, head_dim = map(operator.index, (batch, T, n_q_heads, n_kv_heads, head_dim))
     return _linear_scratch(batch, n_q_heads, n_kv_heads, head_dim, _dtype_code(dtype), T, int(backward))
 
 

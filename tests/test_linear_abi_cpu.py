@@ -1,5 +1,7 @@
 """Host-side checks of the linear-attention and norm/rotation calls: sizes, refusals, all before a device is touched."""
 import ctypes
+import gc
+import weakref
 
 import pytest
 import torch
@@ -184,3 +186,33 @@ def test_a_scale_that_is_not_a_number_is_refused(lib):
     p = _p(scale=float("nan"))
     assert _step(lib, p) == B.BCT_ERR_INVALID_ARG and "scale" in B.last_error()
     assert _fwd(lib, p) == B.BCT_ERR_INVALID_ARG and _bwd(lib, p) == B.BCT_ERR_INVALID_ARG
+
+
+def test_a_scale_is_read_at_every_call_and_not_kept():
+    # (the call is refused, the tensors being on the CPU, but only after its sizes and its scale have been looked at)
+    q, k, g, s = torch.zeros(2, 4, 64), torch.zeros(2, 2, 64), torch.zeros(2), torch.zeros(2, 2, 64, 64)
+    scale = torch.tensor(0.5)
+    kept = weakref.ref(scale)
+    with pytest.raises(ValueError):
+        B.linear_step(q, k, k, g, s, scale=scale)
+    scale.mul_(2)
+    sizes = [_scale_of(q, k, x) for x in (scale, 1.0, 0.5)]
+    assert sizes == [1.0, 1.0, 0.5]
+    del scale
+    gc.collect()
+    assert kept() is None
+    n = torch.tensor(2)
+    a = B.linear_scratch_bytes(n, 16384, 8, 2, 128, torch.bfloat16)
+    n.fill_(1)
+    assert B.linear_scratch_bytes(n, 16384, 8, 2, 128, torch.bfloat16) == B.linear_scratch_bytes(1, 16384, 8, 2, 128, torch.bfloat16)
+    assert a == B.linear_scratch_bytes(2, 16384, 8, 2, 128, torch.bfloat16)
+
+
+def _scale_of(q, k, scale):
+    """The scale that a call with these arguments hands to the library."""
+    seen = []
+    with pytest.MonkeyPatch.context() as m:
+        m.setattr(B, "_operand", lambda *a: None)
+        m.setattr(B, "_launch", lambda dev, call, p, *a: seen.append(p._obj.scale))
+        B.linear_step(q, k, k, torch.zeros(2), torch.zeros(2, 2, 64, 64), scale=scale)
+    return seen[0]
