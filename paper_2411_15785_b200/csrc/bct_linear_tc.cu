@@ -46,6 +46,7 @@ namespace {
 constexpr int kLtThreads = 896;
 constexpr int kLtCh = 128;                    // tokens per chunk
 constexpr int kLtHalf = 128 * 128;            // 64 columns (128 bytes) x 128 rows
+constexpr float kLtHuge = 8.507059173023462e37f;   // 2^126
 // tensor-memory columns
 constexpr int kLtColW = 0;     // W, then P (bfloat16 pairs) in the first half of each of its 64-column halves
 constexpr int kLtColO = 128;
@@ -117,14 +118,16 @@ __device__ __forceinline__ void umma4_warp_ts(uint32_t tmem_d, uint32_t tmem_a, 
         ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "n"(DB), "n"(2 * DB), "n"(3 * DB)
         : "memory");
 }
-// D += (the three terms of a quarter tile) C: two steps of 16 tokens, `step` apart in C's descriptor, the small terms first
-__device__ __forceinline__ void umma_terms_warp(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, int64_t step, uint32_t idesc) {
+// D (+)= (the three terms of a quarter tile) C: two steps of 16 tokens, `step` apart in C's descriptor, the small terms first
+__device__ __forceinline__ void umma_terms_warp(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, int64_t step, uint32_t idesc,
+                                                bool accum) {
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\t"
+        "{\n\t.reg .pred p, q, c;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\t"
         "setp.eq.b32 p, 0, 0;\n\t"
+        "setp.ne.b32 c, %5, 0;\n\t"
         "elect.sync _|q, 0xffffffff;\n\t"
         "add.s32 a, %1, 32;\n\t"
-        "@q " LT_UMMA "[%0], [a], %2, %3, p;\n\t"
+        "@q " LT_UMMA "[%0], [a], %2, %3, c;\n\t"
         "add.s32 a, %1, 8;\n\t"
         "@q " LT_UMMA "[%0], [a], %2, %3, p;\n\t"
         "@q " LT_UMMA "[%0], [%1], %2, %3, p;\n\t"
@@ -134,7 +137,7 @@ __device__ __forceinline__ void umma_terms_warp(uint32_t tmem_d, uint32_t tmem_a
         "@q " LT_UMMA "[%0], [a], b, %3, p;\n\t"
         "add.s32 a, %1, 16;\n\t"
         "@q " LT_UMMA "[%0], [a], b, %3, p;\n\t}"
-        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "l"(step)
+        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "l"(step), "r"((uint32_t)accum)
         : "memory");
 }
 // A quarter of B^T: two steps of 16 tokens, `step` apart in B's descriptor and 16 columns in the result
@@ -175,6 +178,13 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, int x, int 
     asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%1, %2, %3, %4}], [%5];"
                  ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(src))
                  : "memory");
+}
+
+// eight bfloat16 numbers as pairs of floats
+__device__ __forceinline__ void unpack4(const uint4& w, float2 (&x)[4]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
 }
 
 // Bounded wait.  try_wait is given a suspend time, since most of the warps wait here at any time and every poll takes an
@@ -472,10 +482,10 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             umma_commit_warp(&w_full[it & 1]);
             if (Gb > 1 || x == G - 1) umma_commit_warp(&empty_b[b_w]);
         };
-        auto state_products = [&](int qb, uint32_t ca) {   // a quarter tile's share of the state
+        auto state_products = [&](int qb, uint32_t ca, bool accum = true) {   // a quarter tile's share of the state
             LT_WAIT_WARP(&terms_full[qb % kPlaces], qb / kPlaces);
             tc_fence_after();
-            umma_terms_warp(tmem + kLtColS, tmem + t_place(qb), dmn.at(ca + first_of(qb & 3)), step_t, id_kn);
+            umma_terms_warp(tmem + kLtColS, tmem + t_place(qb), dmn.at(ca + first_of(qb & 3)), step_t, id_kn, accum);
         };
         auto ready = [&](uint64_t* bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_test_wait(bar, parity & 1)); };
         if constexpr (STATE_ONLY) {
@@ -495,7 +505,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     if (x == 0) LT_WAIT_WARP(x_full, n);
 #pragma unroll 1
                     for (int qb = 4 * it; qb < 4 * it + 4; ++qb) {
-                        state_products(qb, ca);
+                        state_products(qb, ca, x > 0 || (qb & 3) > 0);
                         umma_commit_warp(&kv_done[qb % kPlaces]);
                     }
                     umma_commit_warp(&empty_c[rc.s]);
@@ -790,6 +800,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         constexpr int kCols = D / 2;                      // columns of a thread, from hs * kCols on
         const bool has_row = q * 32 < D;                  // (head_dim 64: half of the lanes hold no row of the state)
         const uint32_t s_col = lane_base + kLtColS + hs * kCols;
+        const uint32_t keep_col = lane_base + (STATE_ONLY ? kLtColO : kLtColS) + hs * kCols;   // where the state is at the end
         unsigned char* x_row = smem + L::x + (hs * kCols / 64) * (D * 128) + c * 128;
         constexpr int kPiece = kHalves == 2 ? 0 : 4;      // 16-byte pieces of a 128-byte row before hs = 1's
         // The state passes through X's place, kVia columns at a time, and every warp keeps to the bytes of X that it writes
@@ -830,10 +841,48 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                     for (int i = 0; i < kVia; ++i) v[i] *= mul;
                 }
 #pragma unroll
-                for (int i = 0; i < kVia; i += 16) tmem_st16u(s_col + k * kVia + i, reinterpret_cast<const uint32_t*>(v + i));
+                for (int i = 0; i < kVia; i += 16) tmem_st16u(keep_col + k * kVia + i, reinterpret_cast<const uint32_t*>(v + i));
             }
             tmem_wait_st();
         }
+        // The tensor cores cut their sums off towards zero, 24 times a chunk, so that a state that stays under their sum loses
+        // some 5e-7 of itself with every chunk and, a decay of L a chunk being made good by what comes, 5e-7 / (1 - L) in all:
+        // 1.2e-5 after 4096 tokens without a decay to speak of.  Where that would matter (L > 1/4, more than a chunk) the state
+        // is kept in two parts: X, the operand, and under the sum only what X leaves out, 2^-8 of it at most; X times the decay
+        // is added at the turn, with rounding.  That makes a turn 1000 clocks longer (8 x 4096 tokens of 32 heads, all of
+        // them slow: 271 instead of 240 us).  Without X there is room for the state beside the sum, for every decay.
+        const bool by_parts = !STATE_ONLY && n_chunks > 1 && lam(kLtCh) > 0.25f;
+        auto x_at = [&](int piece) { return reinterpret_cast<uint4*>(x_row + (((hs * kPiece + piece) ^ (c & 7)) * 16)); };
+        if (by_parts && has_row) {   // X holds nothing yet
+#pragma unroll
+            for (int i = 0; i < kCols / 8; ++i) *x_at(i) = make_uint4(0, 0, 0, 0);
+        }
+        // The state, times g, and the last chunk's share.
+        auto add_share = [&](float g) {
+#pragma unroll 1
+            for (int k = 0; k < kCols / 16; ++k) {
+                float x[16], y[16];
+                tmem_ld16(s_col + k * 16, x);
+                if (STATE_ONLY) {
+                    tmem_ld16(keep_col + k * 16, y);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float2 hi[4];
+                        unpack4(*x_at(2 * k + e), hi);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[8 * e + 2 * i] = hi[i].x, y[8 * e + 2 * i + 1] = hi[i].y;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float2 z = __ffma2_rn(make_float2(y[i], y[i + 1]), make_float2(g, g), make_float2(x[i], x[i + 1]));
+                    x[i] = z.x, x[i + 1] = z.y;
+                }
+                tmem_st16u(keep_col + k * 16, reinterpret_cast<const uint32_t*>(x));
+            }
+            tmem_wait_st();
+        };
         // Before chunk n: the state as chunk n's operand, and scaled for what chunk n adds.
         auto turn = [&](int n) {
             const float f = lam(chunk_nv(chunk_t0(n)));
@@ -842,21 +891,46 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
                 if (!STATE_ONLY) LT_WAIT(x_empty, n - 1);
                 tc_fence_after();
             }
+            if (STATE_ONLY) {
+                if (n > 0 && has_row) add_share(lam(chunk_nv(chunk_t0(n - 1))));
+            } else if (by_parts) {
+                const float g = n > 0 ? lam(chunk_nv(chunk_t0(n - 1))) : 1.f;
 #pragma unroll 1
-            for (int k = has_row ? 0 : kCols / 16; k < kCols / 16; ++k) {
-                float x[16];
-                tmem_ld16(s_col + k * 16, x);
-                if (!STATE_ONLY) {
-                    const int pc = hs * kPiece + 2 * k;
-                    *reinterpret_cast<uint4*>(x_row + ((pc ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(x);
-                    *reinterpret_cast<uint4*>(x_row + (((pc + 1) ^ (c & 7)) * 16)) = Chunk<__nv_bfloat16>::pack(x + 8);
-                }
+                for (int k = has_row ? 0 : kCols / 8; k < kCols / 8; ++k) {
+                    float x[8];
+                    float2 hi[4];
+                    tmem_ld8(s_col + k * 8, x);
+                    unpack4(*x_at(k), hi);
 #pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float2 y = __fmul2_rn(make_float2(x[i], x[i + 1]), make_float2(f, f));
-                    x[i] = y.x, x[i + 1] = y.y;
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 y = __ffma2_rn(hi[i], make_float2(g, g), make_float2(x[2 * i], x[2 * i + 1]));
+                        x[2 * i] = y.x, x[2 * i + 1] = y.y;
+                    }
+                    const uint4 p = Chunk<__nv_bfloat16>::pack(x);
+                    *x_at(k) = p;
+                    unpack4(p, hi);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 y = __fmul2_rn(__ffma2_rn(hi[i], make_float2(-1.f, -1.f), make_float2(x[2 * i], x[2 * i + 1])), make_float2(f, f));
+                        // (what an infinity leaves out of itself is no number; a finite one leaves it as it is)
+                        x[2 * i] = fmaxf(y.x, -kLtHuge), x[2 * i + 1] = fmaxf(y.y, -kLtHuge);
+                    }
+                    tmem_st8u(s_col + k * 8, reinterpret_cast<const uint32_t*>(x));
                 }
-                tmem_st16u(s_col + k * 16, reinterpret_cast<const uint32_t*>(x));
+            } else {
+#pragma unroll 1
+                for (int k = has_row ? 0 : kCols / 16; k < kCols / 16; ++k) {
+                    float x[16];
+                    tmem_ld16(s_col + k * 16, x);
+                    *x_at(2 * k) = Chunk<__nv_bfloat16>::pack(x);
+                    *x_at(2 * k + 1) = Chunk<__nv_bfloat16>::pack(x + 8);
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        const float2 y = __fmul2_rn(make_float2(x[i], x[i + 1]), make_float2(f, f));
+                        x[i] = y.x, x[i + 1] = y.y;
+                    }
+                    tmem_st16u(s_col + k * 16, reinterpret_cast<const uint32_t*>(x));
+                }
             }
             tmem_wait_st();
             if (!STATE_ONLY) fence_proxy_async_smem();
@@ -914,6 +988,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         if (n_chunks > 0) {
             LT_WAIT(s_full, n_chunks - 1);
             tc_fence_after();
+            if ((STATE_ONLY || by_parts) && has_row) add_share(lam(chunk_nv(chunk_t0(n_chunks - 1))));
         }
         const float poison = *abort_flag ? __int_as_float(0x7fc00000) : 0.f;
         float* dst = nullptr;
@@ -928,7 +1003,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
 #pragma unroll 1
             for (int k = 0; k < kCols / 16; ++k) {
                 float x[16];
-                tmem_ld16(s_col + k * 16, x);
+                tmem_ld16(keep_col + k * 16, x);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[i] = x[i] * mul + poison;
                 if (STATE_ONLY) {   // (no X there, and nothing beside this)

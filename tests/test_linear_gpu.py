@@ -461,3 +461,60 @@ def test_reverse_scans_of_shared_heads_that_begin_with_a_padded_chunk(Hq, Hkv, d
     for _ in range(20):
         again = B.linear_backward(q, q, k, v, ld, state=S, d_state=S, lens=lens)
         assert all(torch.equal(x, y) for x, y in zip(first, again))
+
+
+def _slow_state(b, c, log_decay, first, reverse):
+    """sum_t lambda^(T-1-t) b_t^T c_t + lambda^T first, or lambda^(t+1) in reverse; b, c [T, H, d] -> [H, d, d], float64."""
+    T = b.shape[0]
+    t = torch.arange(T, device=b.device, dtype=torch.float64)
+    w = torch.exp(f64(log_decay)[None, :] * (t + 1 if reverse else T - 1 - t)[:, None])
+    S = torch.einsum("thi,thj->hij", b.double() * w[:, :, None], c.double())
+    return S if first is None else S + torch.exp(T * f64(log_decay))[:, None, None] * first.double()
+
+
+def f64(x):
+    return x.double()
+
+
+@pytest.mark.parametrize("Bt,T,Hq,Hkv,d,split", [(5, 4096, 32, 32, 128, False), (5, 2000, 32, 32, 64, False), (20, 4096, 16, 8, 128, True),
+                                                 (1, 40000, 2, 2, 128, True)])
+@pytest.mark.parametrize("decay", [0.0, -1e-4, -1e-3, -0.0107, -0.0109, -0.03])
+def test_float_states_of_long_slow_sequences(Bt, T, Hq, Hkv, d, split, decay):
+    # What the header says of them: off by less than 1e-6 in root mean square, whatever is kept and however long.  In a chunk
+    # of 128 tokens 24 sums are cut off, by 2^-24 / 1.39 of what has come to be on average, which grows as the root of the
+    # tokens: 24 * 2/3 * 2^-24 / 1.39 = 0.69e-6 of the chunk's share.  The chunks' shares are added with rounding: n chunks
+    # add n roundings of 2^-24 / sqrt(3) at most of a sum that grows as the root of n, sqrt(n/2) 2^-24 / sqrt(3), which is
+    # 0.14e-6 for 32 chunks.  (The last three decays are about where a chunk leaves a quarter of the state: one that stays under
+    # the sums loses 24 * 2^-24 / 1.39 of half of it on average, as the sum grows, and 1 / (1 - 1/4) of that in all: 0.69e-6.)
+    assert (B.linear_scratch_bytes(Bt, T, Hq, Hkv, d, torch.bfloat16) > 0) == split
+    q, k, v, ld, S = _inputs(Bt, T, Hq, Hkv, d, "bf16", 89, decay=decay)
+    do = torch.randn(q.shape, generator=torch.Generator(device="cuda").manual_seed(90), device="cuda").to(q.dtype)
+    for first in (None, S):
+        got = B.linear_forward(q, k, v, ld, state=first)[1]
+        back = B.linear_backward(do, q, k, v, ld, d_state=first)[3]
+        G = Hq // Hkv
+        for b in {0, Bt - 1}:
+            ref = _slow_state(k[b], v[b], ld, None if first is None else first[b], False)
+            err = float((got[b].double() - ref).norm() / ref.norm())
+            assert err <= 1e-6, ("state", first is None, err)
+            ref = d ** -0.5 * _slow_state(q[b], do[b], ld.repeat_interleave(G), None, True).view(Hkv, G, d, d).sum(1)
+            if first is not None:
+                ref = ref + torch.exp(T * f64(ld))[:, None, None] * first[b].double()
+            err = float((back[b].double() - ref).norm() / ref.norm())
+            assert err <= 1e-6, ("d_state_in", first is None, err)
+
+
+@pytest.mark.parametrize("decay", [0.0, -1e-4, -0.05])
+@pytest.mark.parametrize("Hq,d", [(2, 128), (4, 128), (2, 64)])
+@pytest.mark.parametrize("inf", [float("inf"), float("-inf")])
+def test_an_infinity_in_the_state_stays_where_it_is(Hq, d, decay, inf):
+    q, k, v, ld, S = _inputs(80, 400, Hq, 2, d, "bf16", 97, decay=decay)   # (enough heads that a call is not split)
+    S[0, 1, 3, 5] = inf
+    out, S1 = B.linear_forward(q, k, v, ld, state=S)
+    want = torch.isinf(S)
+    assert torch.equal(torch.isinf(S1), want) and float(S1[0, 1, 3, 5]) == inf and not bool(torch.isnan(S1).any())
+    G = Hq // 2
+    sees = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+    sees[0, :, G:, 5] = q[0, :, G:, 3] != 0
+    assert torch.equal(torch.isinf(out), sees)
+    assert torch.equal(torch.sign(out[sees].float()), torch.sign(q[0, :, G:, 3][sees[0, :, G:, 5]].float()) * (1 if inf > 0 else -1))
