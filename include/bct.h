@@ -302,9 +302,10 @@ typedef struct bct_linear_params {
     float scale;        /* <= 0 selects 1/sqrt(head_dim) */
 } bct_linear_params_t;
 
-/* Bytes of scratch that bct_linear_forward (backward = 0) or bct_linear_backward (backward = 1) needs for T
- * tokens: long calls of few heads are split over the tokens, and the states between the parts live there.  0 for
- * many calls.  Depends on the arguments only. */
+/* Bytes of scratch that bct_linear_forward (backward = 0), bct_linear_backward (backward = 1) or the latter with
+ * d_state_in NULL (backward = 2) needs for T tokens: long calls of few heads are split over the tokens, and the states
+ * between the parts live there, with 1, G > 1 and BCT_BF16 also what each query head adds to d_state_in.  0 for many
+ * calls.  Depends on the arguments only. */
 bct_status_t bct_linear_scratch_bytes(const bct_linear_params_t *params, int64_t T, int32_t backward, size_t *bytes);
 
 /*
@@ -341,7 +342,7 @@ bct_status_t bct_linear_forward(const bct_linear_params_t *params, int64_t T, co
  *   d_state    DEVICE float [B][Hkv][d][d], or NULL (zeros)
  *   d_q        DEVICE [B][T][Hq][d]      d_k, d_v  DEVICE [B][T][Hkv][d], in `dtype`; zero in padding rows
  *   d_state_in DEVICE float [B][Hkv][d][d], or NULL: with G > 1 in BCT_BF16 it costs a pass of its own over q and d_out
- *   scratch    as above, bct_linear_scratch_bytes(params, T, 1)
+ *   scratch    as above, bct_linear_scratch_bytes(params, T, 1), or (params, T, 2) where d_state_in is NULL
  */
 bct_status_t bct_linear_backward(const bct_linear_params_t *params, int64_t T, const void *d_out, const void *q,
                                  const void *k, const void *v, const float *log_decay, const int32_t *lens,

@@ -308,10 +308,11 @@ def _linear_setup(q, k, v, log_decay, n_lead, scale):
     return sizes, p, s_shape, dev
 
 
-def linear_scratch_bytes(batch, T, n_q_heads, n_kv_heads, head_dim, dtype, *, backward=False) -> int:
-    """Scratch that linear_forward (or linear_backward) needs for these sizes."""
+def linear_scratch_bytes(batch, T, n_q_heads, n_kv_heads, head_dim, dtype, *, backward=False, want_d_state=True) -> int:
+    """Scratch that linear_forward (or linear_backward, with or without the state's gradient) needs for these sizes."""
     batch, T, n_q_heads, n_kv_heads, head_dim = map(operator.index, (batch, T, n_q_heads, n_kv_heads, head_dim))
-    return _linear_scratch(batch, n_q_heads, n_kv_heads, head_dim, _dtype_code(dtype), T, int(backward))
+    return _linear_scratch(batch, n_q_heads, n_kv_heads, head_dim, _dtype_code(dtype), T,
+                           0 if not backward else (1 if want_d_state else 2))
 
 
 def linear_step(q, k, v, log_decay, state, scale=0.0, out=None, state_out=None, stream=None):
@@ -380,7 +381,7 @@ def linear_backward(d_out, q, k, v, log_decay, state=None, d_state=None, lens=No
     d_k = _result("d_k", given[1], q, k.shape, q.dtype, dev)
     d_v = _result("d_v", given[2], q, v.shape, q.dtype, dev)
     d_in = _result("d_state_in", given[3], q, s_shape, torch.float32, dev) if want_d_state else None
-    scratch = _scratch(_linear_scratch(*sizes, T, 1), scratch, q, dev)
+    scratch = _scratch(_linear_scratch(*sizes, T, 1 if want_d_state else 2), scratch, q, dev)
     _launch(dev, lib.bct_linear_backward, p, T, d_out.data_ptr(), q.data_ptr(), k.data_ptr(),
             v.data_ptr(), log_decay.data_ptr(), _ptr(lens), _ptr(state), _ptr(d_state), d_q.data_ptr(), d_k.data_ptr(),
             d_v.data_ptr(), _ptr(d_in), *_scratch_args(scratch))

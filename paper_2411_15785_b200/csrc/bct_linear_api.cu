@@ -107,11 +107,13 @@ bool two_launches(const bct_linear_params_t& p) { return p.dtype == BCT_BF16 && 
 size_t by_head_bytes(const bct_linear_params_t& p, const bct::LinPlan& plan) {
     return round256((size_t)p.batch * p.n_q_heads * plan.nseg * p.head_dim * p.head_dim * sizeof(float));
 }
-size_t scratch_need(const bct_linear_params_t& p, int64_t T, bool backward) {
-    if (!backward) return round256(bct::lin_plan(p, T, 0).seg_bytes);
+// kind: 0 the forward, 1 the backward, 2 the backward without d_state_in
+size_t scratch_need(const bct_linear_params_t& p, int64_t T, int kind) {
+    if (kind == 0) return round256(bct::lin_plan(p, T, 0).seg_bytes);
     if (!two_launches(p)) return 2 * round256(bct::lin_plan(p, T, 1).seg_bytes);
     const bct::LinPlan last = bct::lin_plan(p, T, 3);
-    const size_t a = round256(bct::lin_plan(p, T, 2).seg_bytes), b = round256(last.seg_bytes) + by_head_bytes(p, last);
+    const size_t a = round256(bct::lin_plan(p, T, 2).seg_bytes);
+    const size_t b = round256(last.seg_bytes) + (kind == 2 ? 0 : by_head_bytes(p, last));
     return a > b ? a : b;   // one after the other, in the same place
 }
 bct_status_t check_lens(const int32_t* lens) {
@@ -134,7 +136,7 @@ bct_status_t bct_linear_scratch_bytes(const bct_linear_params_t* params, int64_t
     if (st == BCT_OK) st = check_tokens(p, T);
     if (st != BCT_OK) return st;
     if (bytes == nullptr) return fail(BCT_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = scratch_need(p, T, backward != 0);
+    *bytes = scratch_need(p, T, backward == 0 ? 0 : (backward == 2 ? 2 : 1));
     return BCT_OK;
 }
 
@@ -166,7 +168,7 @@ bct_status_t bct_linear_forward(const bct_linear_params_t* params, int64_t T, co
     if (st != BCT_OK) return st;
     const Sizes s = sizes_of(p, T);
     const bct::LinPlan plan = bct::lin_plan(p, T, 0);
-    const size_t need = scratch_need(p, T, false);
+    const size_t need = scratch_need(p, T, 0);
     if ((st = check_scratch(scratch, scratch_bytes, need)) != BCT_OK) return st;
     const Span in[] = {{"q", q, s.q, false}, {"k", k, s.kv, false}, {"v", v, s.kv, false}, {"state", state, s.state, true},
                        {"log_decay", log_decay, s.decay, false}, {"lens", lens, s.lens, true}};
@@ -201,7 +203,7 @@ bct_status_t bct_linear_backward(const bct_linear_params_t* params, int64_t T, c
     if (st == BCT_OK) st = check_lens(lens);
     if (st != BCT_OK) return st;
     const Sizes s = sizes_of(p, T);
-    const size_t need = scratch_need(p, T, true);
+    const size_t need = scratch_need(p, T, d_state_in != nullptr ? 1 : 2);
     if ((st = check_scratch(scratch, scratch_bytes, need)) != BCT_OK) return st;
     const Span in[] = {{"d_out", d_out, s.q, false}, {"q", q, s.q, false},          {"k", k, s.kv, false},
                        {"v", v, s.kv, false},        {"state", state, s.state, true}, {"d_state", d_state, s.state, true},

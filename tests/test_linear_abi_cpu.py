@@ -216,3 +216,26 @@ def _scale_of(q, k, scale):
         m.setattr(B, "_launch", lambda dev, call, p, *a: seen.append(p._obj.scale))
         B.linear_step(q, k, k, torch.zeros(2), torch.zeros(2, 2, 64, 64), scale=scale)
     return seen[0]
+
+
+def test_a_backward_without_the_state_gradient_needs_no_room_for_it(lib):
+    p = _p(batch=8, Hq=32, Hkv=8)
+    n = ctypes.c_size_t(0)
+    need = []
+    for kind in (1, 2):
+        assert lib.bct_linear_scratch_bytes(ctypes.byref(p), 4096, kind, ctypes.byref(n)) == B.BCT_OK
+        need.append(n.value)
+    # every query head's share of d_state_in; the launch of d_q, before it, uses the same place for less
+    assert need[0] >= 8 * 32 * 128 * 128 * 4 > need[1]
+    bf, f32 = torch.bfloat16, torch.float32
+    assert B.linear_scratch_bytes(8, 4096, 32, 8, 128, bf, backward=True) == need[0]
+    assert B.linear_scratch_bytes(8, 4096, 32, 8, 128, bf, backward=True, want_d_state=False) == need[1]
+    for Hq, dt in ((8, bf), (32, f32)):                    # elsewhere it is no room of its own
+        assert B.linear_scratch_bytes(1, 16384, Hq, 8, 128, dt, backward=True) == \
+            B.linear_scratch_bytes(1, 16384, Hq, 8, 128, dt, backward=True, want_d_state=False)
+    # no more is asked for than that (the refused overlap says that the scratch was taken), and no less
+    assert _bwd(lib, p, T=4096, d_in=None, n=need[1], d_q=A[0]) == B.BCT_ERR_INVALID_ARG and "overlaps" in B.last_error()
+    assert _bwd(lib, p, T=4096, n=need[1]) == B.BCT_ERR_INVALID_ARG and "scratch" in B.last_error()
+    few = _p(batch=1, Hq=32, Hkv=8)
+    assert lib.bct_linear_scratch_bytes(ctypes.byref(few), 16384, 2, ctypes.byref(n)) == B.BCT_OK and n.value > 0
+    assert _bwd(lib, few, T=16384, d_in=None, n=n.value - 1) == B.BCT_ERR_INVALID_ARG and "scratch" in B.last_error()

@@ -518,3 +518,14 @@ def test_an_infinity_in_the_state_stays_where_it_is(Hq, d, decay, inf):
     sees[0, :, G:, 5] = q[0, :, G:, 3] != 0
     assert torch.equal(torch.isinf(out), sees)
     assert torch.equal(torch.sign(out[sees].float()), torch.sign(q[0, :, G:, 3][sees[0, :, G:, 5]].float()) * (1 if inf > 0 else -1))
+
+
+@pytest.mark.parametrize("Bt,T,Hq,Hkv,d", [(1, 3000, 8, 2, 128), (2, 700, 6, 2, 64), (40, 200, 8, 4, 128)])
+def test_backward_without_the_state_gradient_keeps_to_its_scratch(Bt, T, Hq, Hkv, d):
+    q, k, v, ld, S = _inputs(Bt, T, Hq, Hkv, d, "bf16", 101)
+    need = B.linear_scratch_bytes(Bt, T, Hq, Hkv, d, torch.bfloat16, backward=True, want_d_state=False)
+    want = B.linear_backward(q, q, k, v, ld, state=S, d_state=S, want_d_state=False)
+    raw = torch.full((need + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
+    got = B.linear_backward(q, q, k, v, ld, state=S, d_state=S, want_d_state=False, scratch=raw[4096:4096 + need])
+    assert got[3] is None and all(torch.equal(x, y) for x, y in zip(got[:3], want[:3]))
+    assert bool((raw[:4096] == 0xA5).all()) and bool((raw[-4096:] == 0xA5).all())
