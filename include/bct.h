@@ -286,8 +286,13 @@ bct_status_t bct_stack_forward(bct_cache_t *const *caches, int32_t n_layers, con
  * Roundings.  BCT_F32, and the step in either type: fp32 throughout, one rounding to `dtype`.  Prompts and their
  * backward in BCT_BF16 run on the tensor cores: the products of pairs (q_t . k_s and their like, weighted with the
  * decay) and the state where it enters a product are each rounded to bfloat16 once, sums are fp32, and `out` and the
- * gradients are rounded once; the float states (state_out, d_state_in) are the tensor cores' fp32 sums of unrounded
- * products, off by less than 1e-6 of them (root mean square).
+ * gradients are rounded once; the float states (state_out, d_state_in) are fp32 sums of unrounded products, off by less
+ * than 1e-6 of them (root mean square) for every decay and length.
+ * Range.  BCT_F32 and the step have fp32's.  Prompts and their backward in BCT_BF16 carry the results of a token, until
+ * the last product, as multiples of exp(log_decay)^n or 2^-64, whichever is larger, n <= 128 being the token's distance
+ * from the end of the chunk before it (in reverse, from the start of the one behind it).  Under a strong decay the
+ * products of pairs and the results without `scale` therefore have to stay below 2^63, 9e18 (beyond, infinities), and a
+ * state whose share has decayed below 2^-64 is still seen with 2^-64.  d_state / scale has to be in fp32's range.
  * No atomics: the same call gives the same bits.  A NaN or an infinity in a token that counts may also reach the
  * results of up to 127 tokens before it (of those after it, in the backward), as 0 * infinity; one in a padding row
  * reaches nothing.
@@ -295,8 +300,8 @@ bct_status_t bct_stack_forward(bct_cache_t *const *caches, int32_t n_layers, con
  */
 typedef struct bct_linear_params {
     int32_t batch;      /* B  >= 1 sequences */
-    int32_t n_q_heads;  /* Hq >= 1, a multiple of n_kv_heads */
-    int32_t n_kv_heads; /* Hkv >= 1 */
+    int32_t n_q_heads;  /* Hq in 1..65536, a multiple of n_kv_heads */
+    int32_t n_kv_heads; /* Hkv >= 1, B * Hkv <= 2^20 */
     int32_t head_dim;   /* d in {64, 128}, of keys and values alike */
     int32_t dtype;      /* BCT_F32 or BCT_BF16: q, k, v, out and their gradients; states are float */
     float scale;        /* <= 0 selects 1/sqrt(head_dim) */

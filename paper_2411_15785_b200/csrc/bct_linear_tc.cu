@@ -18,7 +18,9 @@
 //  - The state accumulates in tensor memory, b's features in the lanes.  Once per chunk it is read, written to shared
 //    memory in bfloat16 as the operand X, and scaled.
 //  - f_i multiplies the whole row at the end instead of A's row, so A goes into both products as it is.  It is
-//    floored at 2^-64, which keeps P_ij in range (2^64 W_ij) and is off by 2^-64 of the state's share at most.
+//    floored at 2^-64.  That is off by 2^-64 of the state's share at most, and leaves W and the results a range of 2^63: O
+//    is up to 2^64 times too large.  (Both come out of the one accumulator that A X and P C share, so that a floor divides
+//    fp32's range between them; at 2^-40 a state 2^40 times what the tokens add stayed visible under a strong decay.)
 //  - P and X are each rounded to bfloat16 once, where they enter a product with bfloat16 results.
 // Roles: warp 0 issues the products of the outputs (W, A X, P C), warp 3 those of the state (B^T and its terms with C, a
 // quarter tile at a time; one warp for both waited for one while the other was ready, 300 instead of 249 us), warp 1 loads

@@ -529,3 +529,26 @@ def test_backward_without_the_state_gradient_keeps_to_its_scratch(Bt, T, Hq, Hkv
     got = B.linear_backward(q, q, k, v, ld, state=S, d_state=S, want_d_state=False, scratch=raw[4096:4096 + need])
     assert got[3] is None and all(torch.equal(x, y) for x, y in zip(got[:3], want[:3]))
     assert bool((raw[:4096] == 0xA5).all()) and bool((raw[-4096:] == 0xA5).all())
+
+
+@pytest.mark.parametrize("Hq,d", [(2, 128), (4, 128), (2, 64)])
+@pytest.mark.parametrize("decay", [-0.3, -1.0, -9.0, float("-inf")])
+def test_large_tokens_under_a_strong_decay(Hq, d, decay):
+    # up to the stated range: results without the scale below 2^63
+    q, k, v, ld, S = _inputs(2, 200, Hq, 2, d, "bf16", 103, decay=decay)
+    do = torch.randn(q.shape, generator=torch.Generator(device="cuda").manual_seed(104), device="cuda").to(q.dtype)
+    q, k, v, do, S = q * 2.0 ** 17, k * 2.0 ** 17, v * 2.0 ** 20, do * 2.0 ** 17, S * 2.0 ** 40
+    out, S1 = B.linear_forward(q, k, v, ld, state=S)
+    ref, rS = R.linear_forward(q, k, v, ld, S)
+    mag, mS = R.linear_forward(q.abs(), k.abs(), v.abs(), ld, S.abs())
+    assert 2.0 ** 55 < float(ref.abs().max()) * d ** 0.5 < 2.0 ** 63
+    n = d + 200 * (Hq // 2) + 64
+    _check("out", out, ref, mag, "bf16", n, tensor=True)
+    _check("state", S1, rS, mS, "f32", n)
+    dS = S * 2.0 ** -20        # (v has 2^20 more than do)
+    got = B.linear_backward(do, q, k, v, ld, state=S, d_state=dS)
+    ref, mag = R.linear_backward(do, q, k, v, ld, S, dS), _magnitudes(do, q, k, v, ld, S, dS, None)
+    for name, x, y, m in zip(("d_q", "d_k", "d_v"), got, ref, mag):
+        assert float(y.abs().max()) * d ** 0.5 < 2.0 ** 63
+        _check(name, x, y, m, "bf16", n, tensor=True)
+    _check("d_state_in", got[3], ref[3], mag[3], "f32", n)
