@@ -809,6 +809,11 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         // itself (another warp may be a step ahead): piece `piece` of the warp's row `row`.
         constexpr int kVia = D / 4;
         auto via = [&](int row, int piece) { return x_row + (row - lane) * 128 + (((hs * kPiece + piece) ^ (row & 7)) * 16); };
+        float* dst = nullptr;   // where the state goes
+        if (STATE_ONLY)         // into the slot of the segment that it feeds (by head: its own), key's features in the rows
+            dst = args.st.seg[which] + ((size_t)u * s.nseg + (by_head ? seg : (reverse ? seg - 1 : seg + 1))) * (D * D);
+        else if (r.state_out != nullptr && seg == (reverse ? 0 : s.nseg - 1))
+            dst = r.state_out + (size_t)u * (D * D);   // (never transposed)
         if (has_row) {
             const float* src = state_src;
             const float mul = STATE_ONLY || s.nseg > 1 ? 1.f : r.in_mul;
@@ -847,13 +852,15 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
             }
             tmem_wait_st();
         }
-        // The tensor cores cut their sums off towards zero, 24 times a chunk, so that a state that stays under their sum loses
-        // some 5e-7 of itself with every chunk and, a decay of L a chunk being made good by what comes, 5e-7 / (1 - L) in all:
-        // 1.2e-5 after 4096 tokens without a decay to speak of.  Where that would matter (L > 1/4, more than a chunk) the state
-        // is kept in two parts: X, the operand, and under the sum only what X leaves out, 2^-8 of it at most; X times the decay
-        // is added at the turn, with rounding.  That makes a turn 1000 clocks longer (8 x 4096 tokens of 32 heads, all of
-        // them slow: 271 instead of 240 us).  Without X there is room for the state beside the sum, for every decay.
-        const bool by_parts = !STATE_ONLY && n_chunks > 1 && lam(kLtCh) > 0.25f;
+        // The tensor cores cut their sums off towards zero, three times for 16 tokens, so that a state that stays under their
+        // sum loses some 4e-7 of itself with every chunk and, a chunk leaving a share of L of it, 4e-7 / (1 - L) in all:
+        // 1.2e-5 after 4096 tokens without a decay to speak of, in one call or in many.  Where that would be seen in a float
+        // state (L > 1/4 over a chunk, or over the tokens of a shorter call) the state is kept in two parts: X, the operand,
+        // and under the sum only what X leaves out, 2^-8 of it at most; X times the decay is added at the turn, with
+        // rounding.  That makes a turn 1000 clocks longer (8 x 4096 tokens of 32 heads, all of them slow: 271 instead of
+        // 240 us), so a scan whose state is only seen in bfloat16 does it from 64 chunks on, where the loss comes to a
+        // hundredth of that rounding.  Without X there is room for the state beside the sum, for every decay.
+        const bool by_parts = !STATE_ONLY && lam(n_chunks > 1 ? kLtCh : nv_last) > 0.25f && (dst != nullptr || n_chunks > 64);
         auto x_at = [&](int piece) { return reinterpret_cast<uint4*>(x_row + (((hs * kPiece + piece) ^ (c & 7)) * 16)); };
         if (by_parts && has_row) {   // X holds nothing yet
 #pragma unroll
@@ -990,17 +997,9 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         if (n_chunks > 0) {
             LT_WAIT(s_full, n_chunks - 1);
             tc_fence_after();
-            if ((STATE_ONLY || by_parts) && has_row) add_share(lam(chunk_nv(chunk_t0(n_chunks - 1))));
+            if ((STATE_ONLY || by_parts) && has_row && dst != nullptr) add_share(lam(chunk_nv(chunk_t0(n_chunks - 1))));
         }
-        const float poison = *abort_flag ? __int_as_float(0x7fc00000) : 0.f;
-        float* dst = nullptr;
-        float mul = 1.f;
-        if (STATE_ONLY) {   // into the slot of the segment that it feeds (by head: its own), key's features in the rows
-            dst = args.st.seg[which] + ((size_t)u * s.nseg + (by_head ? seg : (reverse ? seg - 1 : seg + 1))) * (D * D);
-        } else if (r.state_out != nullptr && seg == (reverse ? 0 : s.nseg - 1)) {
-            dst = r.state_out + (size_t)u * (D * D);   // (never transposed)
-            mul = r.out_mul;
-        }
+        const float poison = *abort_flag ? __int_as_float(0x7fc00000) : 0.f, mul = STATE_ONLY ? 1.f : r.out_mul;
         if (dst != nullptr && has_row) {
 #pragma unroll 1
             for (int k = 0; k < kCols / 16; ++k) {

@@ -552,3 +552,17 @@ def test_large_tokens_under_a_strong_decay(Hq, d, decay):
         assert float(y.abs().max()) * d ** 0.5 < 2.0 ** 63
         _check(name, x, y, m, "bf16", n, tensor=True)
     _check("d_state_in", got[3], ref[3], mag[3], "f32", n)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(16, 16, 128), (8, 4, 128), (4, 4, 64)])
+@pytest.mark.parametrize("T,calls,decay", [(100, 60, -1e-4), (128, 40, -1e-3), (16, 300, -1e-4), (1, 300, -0.01), (200, 20, -1e-4)])
+def test_float_states_handed_from_call_to_call(Hq, Hkv, d, T, calls, decay):
+    # a prompt in pieces: what a call leaves in the state must not add up over the calls (the bound is that of one call; the
+    # calls' roundings are n = `calls` of 2^-24 / sqrt(3) at most of a sum that grows as the root of n: below 0.43e-6)
+    q, k, v, ld, S = _inputs(1, T * calls, Hq, Hkv, d, "bf16", 107, decay=decay)
+    cur = S
+    for i in range(calls):
+        x = [y[:, i * T:(i + 1) * T].contiguous() for y in (q, k, v)]
+        cur = B.linear_forward(*x, ld, state=cur)[1]
+    ref = _slow_state(k[0], v[0], ld, S[0], False)
+    assert float((cur[0].double() - ref).norm() / ref.norm()) <= 1e-6
