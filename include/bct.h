@@ -366,6 +366,8 @@ bct_status_t bct_linear_backward(const bct_linear_params_t *params, int64_t T, c
  *   positions  DEVICE int64 [n_tokens]        freq  DEVICE double [rot_dim/2], radians per position; the angle is
  *              formed in double.  Both may be NULL with rot_dim = 0 (norm only)
  *   rot_dim    0..head_dim, a multiple of 16 (BCT_ERR_UNSUPPORTED otherwise);  head_dim in {64, 128}
+ *   eps        >= 0.  mean(x^2) is formed in fp32, so |x| has to stay below 1e18, and above 1e-18 where eps is 0; a
+ *              vector of zeros with eps = 0 is 0 / 0
  */
 #define BCT_ROTATE_INTERLEAVED 1u
 bct_status_t bct_norm_rotate(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,

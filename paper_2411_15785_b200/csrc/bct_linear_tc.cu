@@ -16,7 +16,8 @@
 //    2.8e-6 of it; they took 220 instead of 249 us for 8 x 4096 tokens of 32 heads.)  Weighted in shared memory it took
 //    2300 clocks of traffic a chunk instead of 800.
 //  - The state accumulates in tensor memory, b's features in the lanes.  Once per chunk it is read, written to shared
-//    memory in bfloat16 as the operand X, and scaled.
+//    memory in bfloat16 as the operand X, and scaled.  Where a slow decay would let the sums' cut-off show in a float
+//    state, only what X leaves out stays in tensor memory (by_parts, below).
 //  - f_i multiplies the whole row at the end instead of A's row, so A goes into both products as it is.  It is
 //    floored at 2^-64.  That is off by 2^-64 of the state's share at most, and leaves W and the results a range of 2^63: O
 //    is up to 2^64 times too large.  (Both come out of the one accumulator that A X and P C share, so that a floor divides
@@ -30,10 +31,14 @@
 // segment, the same kernel without A, W and P forms what every segment adds.  Every wait is bounded; a timeout ends the
 // work and fills the block's outputs with NaN.
 //
-// Measured: 8 x 4096 tokens of 32 heads of 128 (1.11 GB) 239 us at full clock, 4.6 TB/s, 0.71 of the copy rate; the
-// backward of 4 x 4096 (three scans) 349 us; 16384 tokens of one sequence, 32 heads over 8 states, 122 us (state pass 22,
-// segments' states 5, outputs 95).  A chunk takes some 6400 clocks, of which the state's chain (its products 4600, the
-// turn 1600) is the longest; the tensor cores are busy 45 % and the issue slots 49 % of the time.
+// Measured, decays spread over the heads from exp(-0.84) to exp(-0.004): 8 x 4096 tokens of 32 heads of 128 (1.11 GB)
+// 259 us at full clock, 4.3 TB/s, 0.66 of the copy rate (244 before the slow quarter of the heads kept their states in two
+// parts); the backward of 4 x 4096 (three scans) 372 us; 16384 tokens of one sequence, 32 heads over 8 states, 127 us (state
+// pass 25, segments' states 5, outputs 88 to 97).  With one head to a state a chunk takes some 6400 clocks, of which the
+// state's chain (its products 4600, the turn 1600, 1000 more in two parts) is the longest; the tensor cores are busy 44 %
+// and the issue slots 49 % of the time.  With four heads of A to a state the state is formed once for four of them, and a
+// (chunk, head) still takes 5100 to 5700 clocks: the warps that form P are busy 1300 of them, those that write outputs 1200,
+// the tensor cores 2000; warp 0, which issues everything, waits for 1200 and is in its own loop for the rest.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -858,7 +863,7 @@ __global__ void __launch_bounds__(kLtThreads, 1) linear_tc_kernel(const __grid_c
         // state (L > 1/4 over a chunk, or over the tokens of a shorter call) the state is kept in two parts: X, the operand,
         // and under the sum only what X leaves out, 2^-8 of it at most; X times the decay is added at the turn, with
         // rounding.  That makes a turn 1000 clocks longer (8 x 4096 tokens of 32 heads, all of them slow: 271 instead of
-        // 240 us), so a scan whose state is only seen in bfloat16 does it from 64 chunks on, where the loss comes to a
+        // 244 us), so a scan whose state is only seen in bfloat16 does it from 64 chunks on, where the loss comes to a
         // hundredth of that rounding.  Without X there is room for the state beside the sum, for every decay.
         const bool by_parts = !STATE_ONLY && lam(n_chunks > 1 ? kLtCh : nv_last) > 0.25f && (dst != nullptr || n_chunks > 64);
         auto x_at = [&](int piece) { return reinterpret_cast<uint4*>(x_row + (((hs * kPiece + piece) ^ (c & 7)) * 16)); };

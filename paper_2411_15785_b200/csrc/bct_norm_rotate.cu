@@ -14,8 +14,8 @@
 // the heads of one token (or on a share of them, when there are few tokens): it forms the token's sines once, in its
 // piece of shared memory, and the heads come as contiguous bulk copies into a ring of its own, three stages of 4 KiB.
 // 192 KiB in flight per SM is what it takes: with the loads in registers (48 KiB in flight) 32768 tokens of 32 + 8
-// heads of 128 took 150 us.  Measured: those (671 MB) 111 us back to back, 6.0 TB/s, 0.92 of the copy rate, 122 us with
-// other calls between; the backward of 16384 tokens of 32 + 32 heads (805 MB) 147 and 156 us, where instructions are 60 %
+// heads of 128 took 150 us.  Measured: those (671 MB) 112 us back to back, 6.0 TB/s, 0.92 of the copy rate, 123 us with
+// other calls between; the backward of 16384 tokens of 32 + 32 heads (805 MB) 150 and 160 us, where instructions are 60 %
 // of the issue slots.  Three blocks of 64 KiB (four stages of 2 KiB a warp, 80 registers) instead of two of 96: 124 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
