@@ -391,6 +391,77 @@ bct_status_t bct_norm_rotate_backward(int64_t n_tokens, int32_t n_q_heads, int32
                                       size_t scratch_bytes, void *cuda_stream);
 
 /*
+ * A cache of predefined capacity held in 8 bits, which throws out the slots that attention has used least: the other way
+ * to keep a bounded cache than the update rule above, which rewrites its values.  The calls keep no handle: the cache is
+ * the caller's memory, described by a struct of sizes and DEVICE pointers (16-byte aligned, contiguous, no two
+ * overlapping).  A zeroed `state` is an empty cache; the other planes need no initial values.
+ *
+ * Codes.  The key of slot j is k[j] * k_scale[j / 32], its value v[j] * v_scale[j / 32] (fp32).  A block of 32 slots that holds
+ * nothing takes the scale amax / 127 (rounded to fp32; at least 2^-126) of what is written into it, amax being its largest
+ * magnitude.  A block that holds something keeps its scale s while amax <= 127.5 s; otherwise s is multiplied by the
+ * smallest power of two with which that holds, and the codes it keeps are divided by it.  Codes are rounded to the nearest,
+ * ties to the even one, and limited to -127..127.  So a value is off by half a step when it is written, and by less than
+ * one step of its block's scale at any time (a slot that an eviction moves is rounded once more, as a new one).  A NaN or an
+ * infinity makes its block's scale a NaN, and every output that sees the block, until the block is written anew.
+ */
+#define BCT_QCACHE_BLOCK 32
+typedef struct bct_qcache {
+    int32_t batch;      /* B  >= 1 sequences */
+    int32_t n_kv_heads; /* Hkv >= 1, B * Hkv <= 2^20 */
+    int32_t head_dim;   /* d in {64, 128} */
+    int32_t capacity;   /* C in 1..2^24 slots */
+    int8_t *k, *v;      /* [B][Hkv][C][d] */
+    float *k_scale, *v_scale; /* [B][Hkv][ceil(C / 32)] */
+    float *weight;      /* [B][Hkv][C]: what attention has given the slot so far */
+    int32_t *position;  /* [B][Hkv][C]: the number of the slot's token in its sequence, from 0 */
+    int32_t *state;     /* [3][B]: slots held (0..C, of every head of the sequence alike), tokens seen, a word of the
+                           library's own that is zero between calls */
+} bct_qcache_t;
+
+/*
+ * Append T tokens per sequence behind the slots held, with weight 0 and the positions that follow the tokens seen.
+ *   k, v   DEVICE [B][T][Hkv][d] in `dtype` (BCT_F32 or BCT_BF16)
+ *   lens   DEVICE int32 [B] or NULL (all T): valid tokens of each sequence, 0..T (clamped); the others are padding, which
+ *          is not read
+ * Tokens that find no slot free are dropped, and neither held nor seen: make room first (bct_qcache_evict).
+ */
+bct_status_t bct_qcache_append(const bct_qcache_t *cache, int64_t T, int32_t dtype, const void *k, const void *v,
+                               const int32_t *lens, void *cuda_stream);
+
+/*
+ * Softmax attention of the last T tokens appended to each sequence over what its cache holds: token i of n sees the first
+ * held - n + i + 1 slots (so the call goes behind the append of these tokens, before an eviction moves slots).
+ *     s = scale q . k_j        p = softmax_j(s), or softmax_j(cap tanh(s / cap)) with cap = score_cap > 0
+ *     out = sum_j p_j v_j      weight_j += p_j, summed over the tokens and the query heads, if `accumulate`
+ *   q, out  DEVICE [B][T][Hq][d] in `dtype`; heads h*G .. h*G+G-1 read kv-head h, G = Hq / Hkv; Hq in 1..65536
+ *   lens    as above: n of each sequence.  Rows behind them are not read, add nothing, and their `out` is zero; so is that of
+ *           a row that sees no slot
+ *   scale   <= 0 selects 1/sqrt(head_dim)
+ *   scratch DEVICE, 256-byte aligned, bct_qcache_attend_scratch_bytes bytes.  In use until the stream has passed the call:
+ *           calls that may overlap need a scratch each
+ * Roundings.  fp32 sums and softmax.  BCT_BF16: exact products of queries and codes, probabilities rounded to 11 bits where
+ * they multiply values, one rounding of `out`.  BCT_F32: queries and probabilities rounded to 22 bits or more.  Where they
+ * multiply values, probabilities below 2^-39 of the row's largest are 0.  The weights are fp32 sums in either.  No atomics: the same call gives the same bits.
+ */
+bct_status_t bct_qcache_attend_scratch_bytes(const bct_qcache_t *cache, int64_t T, int32_t n_q_heads, int32_t dtype,
+                                             int32_t accumulate, size_t *bytes);
+bct_status_t bct_qcache_attend(const bct_qcache_t *cache, int64_t T, int32_t n_q_heads, int32_t dtype, const void *q,
+                               const int32_t *lens, float scale, float score_cap, int32_t accumulate, void *out,
+                               void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/*
+ * Evict from every cache that holds more than `keep` slots all but `keep`, head by head: those of the least weight go, of
+ * equal weights the lower slots first, but none of the last `recent` tokens (position >= tokens seen - recent).  The slots
+ * that stay behind the new end move, in their order, into the places before it that have become free, in theirs; no other
+ * slot moves.  A NaN counts as more weight than any number.
+ *   keep    0..capacity          recent  0..keep
+ *   scratch DEVICE, 256-byte aligned, bct_qcache_evict_scratch_bytes bytes (0, and NULL, with keep = capacity); as above
+ */
+bct_status_t bct_qcache_evict_scratch_bytes(const bct_qcache_t *cache, int32_t keep, size_t *bytes);
+bct_status_t bct_qcache_evict(const bct_qcache_t *cache, int32_t keep, int32_t recent, void *scratch, size_t scratch_bytes,
+                              void *cuda_stream);
+
+/*
  * Host-buffer forms of bct_decode_step and bct_prefill_stream: the same shapes, but q, k, v and out are
  * HOST pointers.  The inputs are copied into the workspace's staging area (two sets, used
  * alternately, on a copy stream the handle owns, so that one call's copies overlap the

@@ -30,8 +30,11 @@ EXPORTS = (
     "bct_update_kv_backward", "bct_stack_scratch_bytes", "bct_stack_forward",
     "bct_linear_scratch_bytes", "bct_linear_step", "bct_linear_forward", "bct_linear_backward",
     "bct_norm_rotate", "bct_norm_rotate_scratch_bytes", "bct_norm_rotate_backward",
+    "bct_qcache_append", "bct_qcache_attend_scratch_bytes", "bct_qcache_attend",
+    "bct_qcache_evict_scratch_bytes", "bct_qcache_evict",
 )
 ROTATE_INTERLEAVED = 1
+QCACHE_BLOCK = 32   # slots of an 8-bit cache that share a scale
 STATIC_STAGE_BYTES = 8 << 20
 
 
@@ -55,6 +58,14 @@ class BctError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__("bct status %d: %s" % (status, message))
         self.status = status
+
+
+class BctQcache(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("capacity", ctypes.c_int32),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p), ("position", ctypes.c_void_p), ("state", ctypes.c_void_p),
+    ]
 
 
 _lib = None
@@ -110,6 +121,12 @@ def load() -> ctypes.CDLL:
     lib.bct_norm_rotate_scratch_bytes.argtypes = [i64, i32, ctypes.POINTER(sz)]
     lib.bct_norm_rotate_backward.argtypes = [i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, f32, vp, vp, i32, u32,
                                              vp, vp, vp, vp, vp, sz, vp]
+    pq = ctypes.POINTER(BctQcache)
+    lib.bct_qcache_append.argtypes = [pq, i64, i32, vp, vp, vp, vp]
+    lib.bct_qcache_attend_scratch_bytes.argtypes = [pq, i64, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.bct_qcache_attend.argtypes = [pq, i64, i32, i32, vp, vp, f32, f32, i32, vp, vp, sz, vp]
+    lib.bct_qcache_evict_scratch_bytes.argtypes = [pq, i32, ctypes.POINTER(sz)]
+    lib.bct_qcache_evict.argtypes = [pq, i32, i32, vp, sz, vp]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -475,6 +492,104 @@ def norm_rotate_backward(d_q_out, d_k_out, q, k, w_q, w_k, positions, freq, eps=
             _ptr(freq) if rot else None, rot, ROTATE_INTERLEAVED if interleaved else 0, d_q.data_ptr(), d_k.data_ptr(),
             _ptr(d_w_q), _ptr(d_w_k), *_scratch_args(scratch))
     return d_q, d_k, d_w_q, d_w_k
+
+
+class QuantCache:
+    """A cache of predefined capacity in 8 bits, with a scale per block of 32 slots and head, which throws out the slots
+    that attention has used least.  Its planes are ordinary tensors:
+
+    ``k``, ``v`` int8 ``[B, Hkv, C, d]``; ``k_scale``, ``v_scale`` float32 ``[B, Hkv, ceil(C / 32)]``; ``weight`` float32 and
+    ``position`` int32 ``[B, Hkv, C]``; ``state`` int32 ``[3, B]``: the slots held, the tokens seen, a word of the library's.
+
+    planes: that tuple, in this order, to go on with a cache that exists; None makes an empty one.  Calls on one cache
+    belong on one stream, or on streams that wait for one another.
+    """
+
+    def __init__(self, batch, n_kv_heads, head_dim, capacity, device="cuda", planes=None):
+        self.B, self.Hkv, self.d, self.C = map(operator.index, (batch, n_kv_heads, head_dim, capacity))
+        lib = load()
+        slots, blocks = (self.B, self.Hkv, self.C), (self.B, self.Hkv, -(-self.C // QCACHE_BLOCK))
+        kinds = (("k", (*slots, self.d), torch.int8), ("v", (*slots, self.d), torch.int8), ("k_scale", blocks, torch.float32),
+                 ("v_scale", blocks, torch.float32), ("weight", slots, torch.float32), ("position", slots, torch.int32),
+                 ("state", (3, self.B), torch.int32))
+        need = ctypes.c_size_t(0)     # refuses sizes that the library does not have, before memory is taken
+        _check(lib.bct_qcache_evict_scratch_bytes(ctypes.byref(BctQcache(self.B, self.Hkv, self.d, self.C)), 0, ctypes.byref(need)))
+        if planes is None:
+            planes = [torch.zeros(shape, dtype=dt, device=device) for _, shape, dt in kinds]
+            if not planes[0].is_cuda:
+                raise ValueError("device must be a CUDA device (got %s)" % planes[0].device)
+        elif len(planes) != len(kinds):
+            raise ValueError("planes must be (%s)" % ", ".join(name for name, _, _ in kinds))
+        self.dev = planes[0].get_device()
+        for (name, shape, dt), t in zip(kinds, planes):
+            _operand(name, t, torch.Size(shape), dt, self.dev)
+        self.k, self.v, self.k_scale, self.v_scale, self.weight, self.position, self.state = planes
+        self._planes = tuple(planes)   # the library has their addresses
+        self._c = BctQcache(self.B, self.Hkv, self.d, self.C, *(t.data_ptr() for t in planes))
+        self._p = ctypes.byref(self._c)
+        self._need = {}
+
+    @property
+    def held(self) -> torch.Tensor:
+        """Slots held by each sequence, int32 ``[B]`` on the device."""
+        return self.state[0]
+
+    @property
+    def seen(self) -> torch.Tensor:
+        """Tokens appended to each sequence so far, int32 ``[B]`` on the device."""
+        return self.state[1]
+
+    def _tokens(self, name, x, heads, lens):
+        """Checks x ``[B, T, heads, d]`` and lens; returns (T, dtype code)."""
+        if x.dim() != 4 or x.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("%s must be float32 or bfloat16 [B, T, heads, head_dim] (got %s, %s)" % (name, x.dtype, tuple(x.shape)))
+        _operand(name, x, torch.Size((self.B, x.shape[1], heads, self.d)), x.dtype, self.dev)
+        if lens is not None:
+            _operand("lens", lens, torch.Size((self.B,)), torch.int32, self.dev)
+        return x.shape[1], BCT_BF16 if x.dtype is torch.bfloat16 else BCT_F32
+
+    def append(self, k, v, lens=None, stream=None) -> None:
+        """k, v ``[B, T, Hkv, d]`` float32 or bfloat16 go behind the slots held; lens int32 ``[B]`` or None (all T): the
+        valid tokens of each sequence of a padded batch.  Tokens that find no slot free are dropped: evict first."""
+        if stream is not None:
+            return _on_stream(stream, lambda k_: self.append(k_, v, lens), k)
+        T, dt = self._tokens("k", k, self.Hkv, lens)
+        _operand("v", v, k.shape, k.dtype, self.dev)
+        _launch(self.dev, load().bct_qcache_append, self._p, T, dt, k.data_ptr(), v.data_ptr(), _ptr(lens))
+
+    def attend(self, q, lens=None, scale=0.0, score_cap=0.0, accumulate=True, out=None, scratch=None, stream=None):
+        """Attention of the last T tokens appended to each sequence, q ``[B, T, Hq, d]``, each over the slots up to its
+        own; lens as in append.  scale <= 0: 1/sqrt(d).  score_cap > 0: scores are ``score_cap tanh(s / score_cap)``.
+        accumulate: adds what each slot was given to ``weight``.  Returns out ``[B, T, Hq, d]``."""
+        if stream is not None:
+            return _on_stream(stream, lambda q_: self.attend(q_, lens, scale, score_cap, accumulate, out, scratch), q)
+        Hq = q.shape[2] if q.dim() == 4 else 0
+        T, dt = self._tokens("q", q, Hq, lens)
+        out = torch.empty_like(q) if out is None else _result("out", out, q, q.shape, q.dtype, self.dev)
+        key = (T, Hq, dt, bool(accumulate))
+        need = self._need.get(key)
+        if need is None:
+            n = ctypes.c_size_t(0)
+            _check(load().bct_qcache_attend_scratch_bytes(self._p, T, Hq, dt, key[3], ctypes.byref(n)))
+            need = self._need[key] = n.value
+        scratch = _scratch(need, scratch, q, self.dev)
+        _launch(self.dev, load().bct_qcache_attend, self._p, T, Hq, dt, q.data_ptr(), _ptr(lens), scale, score_cap, key[3],
+                out.data_ptr(), *_scratch_args(scratch))
+        return out
+
+    def evict(self, keep, recent=0, scratch=None, stream=None) -> None:
+        """Every head of every sequence that holds more than `keep` slots gives up those of the least ``weight``, but none
+        of the last `recent` tokens; slots behind the new end move into the places that have become free."""
+        if stream is not None:
+            return _on_stream(stream, lambda k_: self.evict(keep, recent, scratch), self.k)
+        keep, recent = operator.index(keep), operator.index(recent)
+        need = self._need.get(keep)
+        if need is None:
+            n = ctypes.c_size_t(0)
+            _check(load().bct_qcache_evict_scratch_bytes(self._p, keep, ctypes.byref(n)))
+            need = self._need[keep] = n.value
+        scratch = _scratch(need, scratch, self.k, self.dev)
+        _launch(self.dev, load().bct_qcache_evict, self._p, keep, recent, *_scratch_args(scratch))
 
 
 class Cache:

@@ -1,0 +1,704 @@
+// Attention over the 8-bit cache, few rows to a unit: decode steps and drafted tokens (bct_qcache_prompt.cu has prompts).
+//
+// Per (sequence, kv-head) unit, with its R = T G rows q_r and slots j < sees_r:
+//     s_rj = scale q_r . k_j  (cap tanh(s / cap) where the call says so)      p_rj = exp(s_rj - max_j s_rj)
+//     o_r  = sum_j p_rj v_j / sum_j p_rj                                       weight_j += sum_r p_rj / sum_j p_rj
+//
+// Bound by HBM: 2 d bytes of codes per slot, which every row of the unit shares.  A warp works alone on blocks of 32 slots
+// (the block of a scale), which come by 16-byte asynchronous copies into a ring of its own; the blocks of all units, in
+// their order, are dealt to the warps in equal runs, whatever the sequences' lengths.  What a warp has of a unit that
+// others share (at most two such per warp) goes to scratch and is joined by qc_join_kernel, which then gives each slot its
+// weight from the stored scores (4 R bytes a slot written and read, against 2 d for reading the keys again).
+//
+// Products are mma.sync m16n8k16 with the slots in M and eight rows in N: rows are few, and an 8-bit code has to be
+// turned into 16 bits in registers on its way in any case, so there is nothing for tcgen05 to read from shared memory; the
+// tensor cores are idle most of the time here.  Codes become fp16 exactly (two instructions for a pair: the byte under the
+// exponent of 1024, less 1152).  A query is scaled by a power of two to below 2^15 and is fp16 as it is if it is bfloat16
+// (terms below 2^-39 of the row's largest apart); a float query is two such terms.  Scores are thus exact products with
+// fp32 sums.  The probabilities enter the second product as fp16 times 2^15 (2^-12 of each, below 2^-39 of the largest 0),
+// for float results as two terms (2^-23).  Each block's V product starts from zero and is added with the block's scale in
+// fp32, so scales may differ by any factor.
+//
+// Fragments need no shuffling of codes: the order of features in the first product's sum, and of slots in the second's, is
+// free.  Lane (g, t) = (lane / 4, lane % 4) reads for slot 8 (g / 2) + 4 (g % 2) + i, i < 4, the features 16 t .. 16 t + 15
+// (and 64 + 16 t ..), and for the slots 8 t + i, 8 t + 4 + i the features 16 g .. 16 g + 15 of V; what it computes for the
+// former is, transposed 8 x 8 at a time by movmatrix, the other operand of the latter.  16-byte chunks of a slot are stored
+// at chunk ^ x(slot), with which both readings are free of bank conflicts.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "bct_device.cuh"
+#include "bct_internal.h"
+#include "bct_qcache.h"
+#include "bct_tc.cuh"
+
+namespace bct {
+namespace {
+
+constexpr int kQaWarps = 8;
+constexpr int kQaThreads = kQaWarps * 32;
+constexpr int kQaStages = 3;
+constexpr int kQaScored = kQcScoredRows;
+constexpr int kQjThreads = 256;
+constexpr int kQjSlots = 1024;        // slots of a CTA of the joining kernel
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kPScale = 32768.f;    // of a probability on its way into fp16
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
+// a pair of bytes of `w` (each a code + 128), chosen by `sel`, as fp16
+__device__ __forceinline__ uint32_t pair_of(uint32_t w, uint32_t sel) {
+    const uint32_t u = prmt(w, 0x64646464u, sel);
+    const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t half2_bits(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 half2_floats(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void* src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Where the 16-byte chunk of a slot stands in its block's tile.
+template <int D>
+__device__ __forceinline__ int tile_at(int slot, int chunk) {
+    const int x = (((slot >> 3) & 3) << 1) ^ (((slot >> 2) & 1) << 2);
+    if constexpr (D == 128) return slot * 128 + ((chunk ^ x) << 4);
+    else return (slot >> 1) * 128 + (((((slot & 1) << 2) | chunk) ^ x) << 4);
+}
+
+// upto[thread]: the blocks of the sequences up to the end of its share of them, `chunk_out` sequences.  Returns all blocks.
+__device__ __forceinline__ int64_t count_blocks(const QcAttend& a, int64_t* upto, int* chunk_out) {
+    const int chunk = (a.c.B + blockDim.x - 1) / blockDim.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int64_t x = 0;
+    for (int i = 0; i < chunk; ++i) {
+        const int b = tid * chunk + i;
+        if (b < a.c.B) x += (min(max(a.c.state[b], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    __shared__ int64_t warps[32];
+    if (lane == 31) warps[warp] = x;
+    __syncthreads();
+    for (int i = 0; i < warp; ++i) x += warps[i];
+    upto[tid] = x;
+    __syncthreads();
+    *chunk_out = chunk;
+    return upto[blockDim.x - 1];
+}
+// The warp whose run has block x of `total` in all, of n runs (n <= total).
+__device__ __forceinline__ int run_of(int64_t x, int64_t total, int n) { return (int)(((x + 1) * n - 1) / total); }
+
+// What a row sees: rows of a unit are (token, head), token-major.
+struct Sees {
+    int held, n, G;   // slots held, valid tokens
+    int64_t R;
+    __device__ __forceinline__ int operator()(int64_t r) const {
+        const int64_t i = r / G;
+        return r < R && i < n ? max(held - n + (int)i + 1, 0) : 0;
+    }
+};
+__device__ __forceinline__ Sees sees_of(const QcAttend& a, int b) {
+    Sees s;
+    s.held = min(max(a.c.state[b], 0), a.c.C);
+    s.n = (int)(a.lens == nullptr ? a.T : min((int64_t)max(a.lens[b], 0), a.T));
+    s.G = a.G;
+    s.R = a.R;
+    return s;
+}
+template <typename T>
+__device__ __forceinline__ const T* row_of(const QcAttend& a, const void* base, int b, int h, int64_t r) {
+    const int64_t i = r / a.G;
+    const int64_t head = (int64_t)h * a.G + (r - i * a.G);
+    return static_cast<const T*>(base) + (((int64_t)b * a.T + i) * ((int64_t)a.c.Hkv * a.G) + head) * a.c.D;
+}
+
+// The queries of eight rows as fragments: lane (g, t) has row g.  `mul`: what the row was divided by.
+template <typename T, int D, int TERMS>
+__device__ __forceinline__ void load_queries(const T* row, bool real, uint32_t (&f)[TERMS][D / 16][2], float* mul) {
+    const int t = threadIdx.x & 3;
+    float x[D / 4];
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+        constexpr int kE = Chunk<T>::kElems;
+#pragma unroll
+        for (int i = 0; i < 16 / kE; ++i) {
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (real) w = *reinterpret_cast<const uint4*>(row + 64 * j + 16 * t + i * kE);
+            Chunk<T>::unpack(w, x + 16 * j + i * kE);
+        }
+    }
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 4; ++i) top = fmaxf(top, fabsf(x[i]));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    // 2^(14 - exponent of the largest), from 2^-113 to 2^126; rows of zeros, infinities or NaN as they are
+    const int e = (int)(__float_as_uint(top) >> 23) - 127;
+    const int up = e > -127 && e < 128 ? min(14 - e, 126) : 0;
+    const float by = __uint_as_float((uint32_t)(up + 127) << 23);
+    *mul = __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const float u = x[4 * ks + 2 * p] * by, v = x[4 * ks + 2 * p + 1] * by;
+            f[0][ks][p] = half2_bits(u, v);
+            if constexpr (TERMS == 2) {
+                const float2 b = half2_floats(f[0][ks][p]);
+                f[1][ks][p] = half2_bits(u - b.x, v - b.y);
+            }
+        }
+    }
+}
+
+// The codes of a block's keys as fragments: [i][word] pairs, i the lane's slots, word four features.
+template <int D>
+__device__ __forceinline__ void load_keys(const unsigned char* tile, int g, int t, uint32_t (&w)[4][D / 16]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int slot = 8 * (g >> 1) + 4 * (g & 1) + i;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+            const uint4 u = *reinterpret_cast<const uint4*>(tile + tile_at<D>(slot, t + 4 * j));
+            w[i][4 * j] = u.x ^ 0x80808080u, w[i][4 * j + 1] = u.y ^ 0x80808080u;
+            w[i][4 * j + 2] = u.z ^ 0x80808080u, w[i][4 * j + 3] = u.w ^ 0x80808080u;
+        }
+    }
+}
+
+// Products of a block's keys with eight rows: s[mt][..] for the slots i = 2 mt (c0, c1: rows 2t, 2t + 1), 2 mt + 1 (c2, c3).
+template <int D, int TERMS, int NT>
+__device__ __forceinline__ void score_products(const uint32_t (&w)[4][D / 16], const uint32_t (&q)[NT][TERMS][D / 16][2],
+                                               float (&s)[NT][2][4]) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[nt][i >> 2][i & 3] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            const uint32_t u = w[2 * mt][ks], v = w[2 * mt + 1][ks];
+            const uint32_t a0 = pair_of(u, 0x4140), a1 = pair_of(v, 0x4140), a2 = pair_of(u, 0x4342), a3 = pair_of(v, 0x4342);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int term = 0; term < TERMS; ++term)
+                    mma16816(s[nt][mt], a0, a1, a2, a3, q[nt][term][ks][0], q[nt][term][ks][1]);
+        }
+    }
+}
+
+// Scores in powers of two from products: `mul` has the block's scale and the row's.
+__device__ __forceinline__ float score_of(float dot, float mul, float cap) {
+    const float s = dot * mul;
+    return cap > 0.f ? cap * kLog2e * tanhf(s) : s;
+}
+// what a row's products are multiplied with, besides the block's scale
+__device__ __forceinline__ float row_factor(const QcAttend& a, float mul) {
+    return a.cap > 0.f ? mul * (a.scale / a.cap) : mul * (a.scale * kLog2e);
+}
+
+template <typename T, int D, int NT, int TERMS>
+__global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend a) {
+    constexpr int kTile = kQcBlock * D;
+    constexpr int kMt = D / 16;                    // tiles of 16 features
+    constexpr int kRows = 8 * NT;
+    extern __shared__ __align__(128) unsigned char qa_smem[];
+    __shared__ int64_t upto[kQaThreads];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    unsigned char* ring = qa_smem + warp * (kQaStages * 2 * kTile);
+    const uint32_t ring32 = smem_u32(ring);
+
+    int chunk;
+    const int64_t per_seq = (int64_t)a.c.Hkv * a.n_groups;
+    const int64_t total = count_blocks(a, upto, &chunk) * per_seq;
+    if (total == 0) return;
+    const int n_runs = (int)min((int64_t)a.n_warps, total);
+    const int run = warp * gridDim.x + blockIdx.x;
+    if (run >= n_runs) return;
+    int64_t x = total * run / n_runs;
+    const int64_t end = total * (run + 1) / n_runs;
+
+    // where the run begins: its sequence, then the unit and row group within
+    int b;
+    int64_t before;       // blocks of the sequences before b, times per_seq
+    {
+        int lo = 0, hi = kQaThreads - 1;           // first thread's share that ends behind x
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (upto[mid] * per_seq > x) hi = mid; else lo = mid + 1;
+        }
+        b = lo * chunk;
+        before = (lo ? upto[lo - 1] : 0) * per_seq;
+        for (;;) {
+            const int64_t nb = (min(max(a.c.state[b], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
+            if (before + nb * per_seq > x) break;
+            before += nb * per_seq;
+            ++b;
+        }
+    }
+    int nb = (min(max(a.c.state[b], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
+    int64_t unit_in = (x - before) / nb;           // h * n_groups + group
+    int blk = (int)((x - before) - unit_in * nb);
+
+    while (x < end) {
+        const int h = (int)(unit_in / a.n_groups);
+        const int64_t group = unit_in - h * a.n_groups;
+        const int64_t unit = (int64_t)b * a.c.Hkv + h, r0 = group * kRows;
+        const int first = blk, last = (int)min((int64_t)nb, first + (end - x));   // this piece's blocks
+        const Sees sees = sees_of(a, b);
+        const int8_t* kp = a.c.codes[0] + (size_t)unit * a.c.C * D;
+        const int8_t* vp = a.c.codes[1] + (size_t)unit * a.c.C * D;
+        const float* ksp = a.c.scale[0] + (size_t)unit * a.c.NB;
+        const float* vsp = a.c.scale[1] + (size_t)unit * a.c.NB;
+
+        // rows 2t, 2t + 1 of each tile of eight are this lane's in the scores and outputs, row g in the queries
+        uint32_t q[NT][TERMS][D / 16][2];
+        float mul[NT][2];
+        int lim[NT][2];
+        int lim_max = 0, lim_min = 0x7fffffff;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int64_t r = r0 + nt * 8 + g;
+            float m;
+            load_queries<T, D, TERMS>(row_of<T>(a, a.q, b, h, r < a.R ? r : 0), r < a.R && sees(r) > 0, q[nt], &m);
+            m = row_factor(a, m);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                mul[nt][e] = __shfl_sync(0xffffffffu, m, (2 * t + e) * 4);
+                lim[nt][e] = sees(r0 + nt * 8 + 2 * t + e);
+                lim_max = max(lim_max, lim[nt][e]);
+                lim_min = min(lim_min, lim[nt][e]);
+            }
+        }
+        lim_max = __reduce_max_sync(0xffffffffu, lim_max);
+        lim_min = __reduce_min_sync(0xffffffffu, lim_min);
+        const int stop = min(last, (lim_max + kQcBlock - 1) / kQcBlock);   // blocks behind it are hidden from all rows
+
+        auto fetch = [&](int blk_, int stage) {
+            if (blk_ < stop) {
+                const uint32_t dst = ring32 + stage * 2 * kTile;
+                constexpr int kChunks = D / 16, kPer = 32 / kChunks;   // chunks of a slot, slots of an instruction
+                const int c = lane % kChunks;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const int8_t* src = p ? vp : kp;
+#pragma unroll
+                    for (int i = 0; i < kQcBlock / kPer; ++i) {
+                        const int s = i * kPer + lane / kChunks, slot = blk_ * kQcBlock + s;
+                        const bool real = slot < lim_max;
+                        cp_async16_zfill(dst + p * kTile + tile_at<D>(s, c), src + (size_t)(real ? slot : 0) * D + c * 16, real);
+                    }
+                }
+            }
+            cp_async_commit();
+        };
+
+        float o[NT][kMt][4], m_run[NT][2], l_run[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int i = 0; i < kMt * 4; ++i) o[nt][i >> 2][i & 3] = 0.f;
+            m_run[nt][0] = m_run[nt][1] = -INFINITY;
+            l_run[nt][0] = l_run[nt][1] = 0.f;
+        }
+#pragma unroll
+        for (int s = 0; s < kQaStages - 1; ++s) fetch(first + s, s);
+        int stage = 0;
+        for (int i = first; i < stop; ++i) {
+            const float ks = ksp[i], vs = vsp[i];
+            cp_async_wait<kQaStages - 2>();
+            __syncwarp();
+            {
+                int to = stage + kQaStages - 1;
+                fetch(i + kQaStages - 1, to >= kQaStages ? to - kQaStages : to);
+            }
+            const unsigned char* tile = ring + stage * 2 * kTile;
+            if (++stage == kQaStages) stage = 0;
+
+            float s[NT][2][4];
+            {
+                uint32_t w[4][D / 16];
+                load_keys<D>(tile, g, t, w);
+                score_products<D, TERMS, NT>(w, q, s);
+            }
+            const int slot0 = i * kQcBlock + 8 * (g >> 1) + 4 * (g & 1);
+            const bool all = (i + 1) * kQcBlock <= lim_min;
+            uint32_t pf[NT][TERMS][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float& v = s[nt][j >> 1][2 * (j & 1) + e];
+                        v = score_of(v, ks * mul[nt][e], a.cap);
+                        if (!all && slot0 + j >= lim[nt][e]) v = -INFINITY;
+                        top[e] = fmaxf(top[e], v);
+                    }
+                if (a.scores != nullptr && r0 + nt * 8 + 2 * t < a.R) {
+                    float* to = a.scores + ((size_t)unit * a.c.C + slot0) * a.R2 + r0 + nt * 8 + 2 * t;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (slot0 + j >= lim_max) break;
+                        const float* v = &s[nt][j >> 1][2 * (j & 1)];
+                        if (a.R2 == 1) to[j] = v[0];
+                        else *reinterpret_cast<float2*>(to + (size_t)j * a.R2) = make_float2(v[0], v[1]);
+                    }
+                }
+                bool higher = false;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int o_ = 4; o_ < 32; o_ <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], o_));
+                    higher |= top[e] > m_run[nt][e];
+                }
+                if (__any_sync(0xffffffffu, higher)) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float m = fmaxf(m_run[nt][e], top[e]);
+                        const float by = m == -INFINITY ? 1.f : ex2(m_run[nt][e] - m);
+                        m_run[nt][e] = m;
+                        l_run[nt][e] *= by;
+#pragma unroll
+                        for (int f = 0; f < kMt; ++f) o[nt][f][e] *= by, o[nt][f][2 + e] *= by;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float p[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float m = m_run[nt][e] == -INFINITY ? 0.f : m_run[nt][e];
+                        p[e] = ex2(s[nt][j >> 1][2 * (j & 1) + e] - m);
+                        l_run[nt][e] += p[e];
+                        p[e] *= kPScale;
+                    }
+                    const uint32_t hi = half2_bits(p[0], p[1]);
+                    pf[nt][0][j] = transposed(hi);
+                    if constexpr (TERMS == 2) {
+                        const float2 b2 = half2_floats(hi);
+                        pf[nt][1][j] = transposed(half2_bits(p[0] - b2.x, p[1] - b2.y));
+                    }
+                }
+            }
+
+            // V: for the slots 8 t + i (e = 0) and 8 t + 4 + i (e = 1) the lane's D / 8 features, 16 or 8 from 16 g or 8 g on
+            const unsigned char* vt = tile + kTile;
+            const float vmul = vs * (1.f / kPScale);
+#pragma unroll
+            for (int half = 0; half < D / 64; ++half) {       // 8 bytes of each slot at a time
+                uint2 w[2][4];
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int slot = 8 * t + 4 * e + j;
+                        const int at = D == 128 ? tile_at<D>(slot, g) + 8 * half : tile_at<D>(slot, g >> 1) + 8 * (g & 1);
+                        w[e][j] = *reinterpret_cast<const uint2*>(vt + at);
+                    }
+#pragma unroll
+                for (int wd = 0; wd < 2; ++wd) {
+                    uint32_t lo[4], hi[4];            // slots 8t + j and 8t + 4 + j, two features
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t u = (wd ? w[0][j].y : w[0][j].x) ^ 0x80808080u, v = (wd ? w[1][j].y : w[1][j].x) ^ 0x80808080u;
+                        lo[j] = prmt(u, v, 0x5140);
+                        hi[j] = prmt(u, v, 0x7362);
+                    }
+#pragma unroll
+                    for (int hm = 0; hm < 2; ++hm) {
+                        const int f = half * 4 + wd * 2 + hm;   // features 2 f, 2 f + 1 of the lane's
+                        uint32_t A[4][2];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t u = hm ? hi[j] : lo[j];
+                            A[j][0] = pair_of(u, 0x4140);
+                            A[j][1] = pair_of(u, 0x4342);
+                        }
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+                                for (int k2 = 0; k2 < 2; ++k2)
+                                    mma16816(acc, A[2 * k2][0], A[2 * k2][1], A[2 * k2 + 1][0], A[2 * k2 + 1][1],
+                                             pf[nt][term][2 * k2], pf[nt][term][2 * k2 + 1]);
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) o[nt][f][c] = fmaf(acc[c], vmul, o[nt][f][c]);
+                        }
+                    }
+                }
+            }
+            __syncwarp();   // the stage may be filled again
+        }
+        cp_async_wait<0>();
+        __syncwarp();
+
+        // the piece's sums; a whole unit is done, a part goes to scratch
+        const bool whole = first == 0 && last == nb;
+        const int64_t slot_no = first == 0 ? 2 * (int64_t)run + 1 : 2 * (int64_t)run;
+        constexpr int kE = D / 8;     // features of a lane
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float l = l_run[nt][e];
+#pragma unroll
+                for (int o_ = 4; o_ < 32; o_ <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o_);
+                const int row = nt * 8 + 2 * t + e;
+                const int64_t r = r0 + row;
+                if (r >= a.R) continue;
+                if (whole) {
+                    const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+                    T* to = const_cast<T*>(row_of<T>(a, a.out, b, h, r)) + g * kE;
+                    float y[kE];
+#pragma unroll
+                    for (int f = 0; f < kMt; ++f) y[2 * f] = o[nt][f][e] * inv, y[2 * f + 1] = o[nt][f][2 + e] * inv;
+#pragma unroll
+                    for (int c = 0; c < kE / Chunk<T>::kElems; ++c)
+                        *reinterpret_cast<uint4*>(to + c * Chunk<T>::kElems) = Chunk<T>::pack(y + c * Chunk<T>::kElems);
+                    if (g == 0) a.ml[unit * a.R + r] = make_float2(m_run[nt][e], inv);
+                } else {
+                    float* to = a.part_o + (slot_no * kRows + row) * D + g * kE;
+#pragma unroll
+                    for (int f = 0; f < kMt; f += 2)
+                        *reinterpret_cast<float4*>(to + 2 * f) = make_float4(o[nt][f][e], o[nt][f][2 + e], o[nt][f + 1][e], o[nt][f + 1][2 + e]);
+                    if (g == 0) a.part_ml[slot_no * kRows + row] = make_float2(m_run[nt][e], l);
+                }
+            }
+
+        x += last - first;
+        blk = 0;
+        if (last == nb && x < end) {
+            if (++unit_in == per_seq) {
+                unit_in = 0;
+                do ++b, nb = (min(max(a.c.state[b], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
+                while (nb == 0);
+            }
+        }
+    }
+}
+
+// Joins what several warps have of a unit, writes the zeros of rows that see nothing in an empty cache, and adds the
+// weights from the stored scores.  A CTA per unit and kQjSlots of its slots (per unit and 8 rows of it, where there are no
+// scores); the rows that a unit's CTAs join are shared out among them.
+template <typename T, int D>
+__global__ void __launch_bounds__(kQjThreads) qc_join_kernel(const QcAttend a, int ctas, int group_rows) {
+    __shared__ float2 row_ml[kQaScored];           // where there are scores
+    __shared__ int row_sees[kQaScored];
+    __shared__ int64_t upto[kQjThreads];
+    const int64_t unit = blockIdx.x / ctas;
+    const int part = (int)(blockIdx.x - unit * ctas);
+    const int b = (int)(unit / a.c.Hkv), h = (int)(unit - (int64_t)b * a.c.Hkv), tid = threadIdx.x;
+    const Sees sees = sees_of(a, b);
+    const int nb = (sees.held + kQcBlock - 1) / kQcBlock;
+    int chunk;
+    const int64_t per_seq = (int64_t)a.c.Hkv * a.n_groups;
+    const int64_t total = count_blocks(a, upto, &chunk) * per_seq;
+    const int n_runs = (int)min((int64_t)a.n_warps, total);
+    int64_t before = b / chunk ? upto[b / chunk - 1] : 0;
+    for (int i = b / chunk * chunk; i < b; ++i) before += (min(max(a.c.state[i], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
+    before = before * per_seq + (int64_t)h * a.n_groups * nb;
+
+    // which warps have a row group: [first, last]
+    auto runs = [&](int64_t group, int* first, int* last) {
+        *first = run_of(before + group * nb, total, n_runs);
+        *last = run_of(before + (group + 1) * nb - 1, total, n_runs);
+    };
+    // maximum and 1 / sum of a row; the parts' places are 2 first + 1, then 2 run
+    auto join = [&](int64_t r, int first, int last) {
+        const int64_t row = r % group_rows;
+        float m = -INFINITY, l = 0.f;
+        for (int i = first; i <= last; ++i) {
+            const float2 p = a.part_ml[(2 * (int64_t)i + (i == first)) * group_rows + row];
+            const float top = fmaxf(m, p.x);
+            if (top == -INFINITY) {
+                l += p.y;      // (0, or a NaN)
+                continue;
+            }
+            l = l * ex2(m - top) + p.y * ex2(p.x - top);
+            m = top;
+        }
+        return make_float2(m, l > 0.f ? 1.f / l : (l == l ? 0.f : l));
+    };
+
+    const bool scored = a.scores != nullptr;
+    if (scored) {
+        for (int r = tid; r < a.R; r += kQjThreads) {
+            float2 v = make_float2(-INFINITY, 0.f);
+            if (nb > 0) {
+                int first, last;
+                runs(r / group_rows, &first, &last);
+                v = first == last ? a.ml[unit * a.R + r] : join(r, first, last);
+            }
+            row_ml[r] = v;
+            row_sees[r] = v.y == 0.f ? 0 : sees(r);
+        }
+        __syncthreads();
+    }
+    // outputs: 32 threads and more to a row
+    constexpr int kPer = kQjThreads / (D / 4);     // rows at a time
+    const int64_t step = scored ? (int64_t)ctas * kPer : kPer;
+    const int64_t r_end = scored ? a.R : min(a.R, (int64_t)(part + 1) * 8);
+    for (int64_t r = (scored ? (int64_t)part * kPer : (int64_t)part * 8) + tid / (D / 4); r < r_end; r += step) {
+        const int f = tid % (D / 4) * 4;
+        int first = 0, last = 0;
+        if (nb > 0) runs(r / group_rows, &first, &last);
+        if (nb > 0 && first == last) continue;
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (nb > 0) {
+            const float2 ml = scored ? row_ml[r] : join(r, first, last);
+            for (int i = first; i <= last; ++i) {
+                const int64_t at = (2 * (int64_t)i + (i == first)) * group_rows + r % group_rows;
+                const float m = a.part_ml[at].x;
+                const float by = m == -INFINITY ? 0.f : ex2(m - ml.x) * ml.y;
+                const float4 o = *reinterpret_cast<const float4*>(a.part_o + at * D + f);
+                y.x = fmaf(o.x, by, y.x), y.y = fmaf(o.y, by, y.y), y.z = fmaf(o.z, by, y.z), y.w = fmaf(o.w, by, y.w);
+            }
+            if (ml.y != ml.y) y = make_float4(ml.y, ml.y, ml.y, ml.y);
+            if (!scored && f == 0) a.ml[unit * a.R + r] = ml;
+        } else if (!scored && f == 0) {
+            a.ml[unit * a.R + r] = make_float2(-INFINITY, 0.f);
+        }
+        T* to = const_cast<T*>(row_of<T>(a, a.out, b, h, r)) + f;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = y;
+        else *reinterpret_cast<uint2*>(to) = make_uint2(Chunk<T>::pack2(y.x, y.y), Chunk<T>::pack2(y.z, y.w));
+    }
+    if (!scored) return;
+    for (int j = part * kQjSlots + tid; j < min((part + 1) * kQjSlots, sees.n > 0 ? sees.held : 0); j += kQjThreads) {
+        const float* s = a.scores + ((size_t)unit * a.c.C + j) * a.R2;
+        float w = 0.f;
+        for (int r = 0; r < a.R; ++r)
+            if (j < row_sees[r]) w += ex2(s[r] - row_ml[r].x) * row_ml[r].y;
+        a.c.weight[(size_t)unit * a.c.C + j] += w;
+    }
+}
+
+// The weights from the keys again, for calls with many rows: a warp per block of slots goes through the rows that see it.
+template <typename T, int D, int TERMS>
+__global__ void __launch_bounds__(kQaThreads) qc_weights_kernel(const QcAttend a) {
+    __shared__ __align__(128) unsigned char tiles[kQaWarps][kQcBlock * D];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int per_unit = (a.c.NB + kQaWarps - 1) / kQaWarps;
+    const int64_t unit = blockIdx.x / per_unit;
+    const int blk = (int)(blockIdx.x - unit * per_unit) * kQaWarps + warp;
+    const int b = (int)(unit / a.c.Hkv), h = (int)(unit - (int64_t)b * a.c.Hkv);
+    const Sees sees = sees_of(a, b);
+    const int slot0 = blk * kQcBlock;
+    if (slot0 >= sees.held || sees.n == 0) return;
+    unsigned char* tile = tiles[warp];
+    {
+        const int8_t* kp = a.c.codes[0] + (size_t)unit * a.c.C * D;
+        constexpr int kChunks = D / 16, kPer = 32 / kChunks;
+        const int c = lane % kChunks;
+#pragma unroll
+        for (int i = 0; i < kQcBlock / kPer; ++i) {
+            const int s = i * kPer + lane / kChunks;
+            const bool real = slot0 + s < sees.held;
+            cp_async16_zfill(smem_u32(tile + tile_at<D>(s, c)), kp + (size_t)(real ? slot0 + s : 0) * D + c * 16, real);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        __syncwarp();
+    }
+    const float ks = a.c.scale[0][(size_t)unit * a.c.NB + blk];
+    uint32_t w[4][D / 16];
+    load_keys<D>(tile, g, t, w);
+    // the first token that sees the block's first slot
+    const int i0 = max(0, slot0 - (sees.held - sees.n));
+    const int mine = slot0 + 8 * (g >> 1) + 4 * (g & 1);
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int64_t r0 = (int64_t)i0 * a.G / 8 * 8; r0 < (int64_t)sees.n * a.G; r0 += 8) {
+        uint32_t q[1][TERMS][D / 16][2];
+        float m;
+        const int64_t r = r0 + g;
+        load_queries<T, D, TERMS>(row_of<T>(a, a.q, b, h, r < a.R ? r : 0), r < a.R, q[0], &m);
+        m = row_factor(a, m);
+        float s[1][2][4];
+        score_products<D, TERMS, 1>(w, q, s);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float mul = __shfl_sync(0xffffffffu, m, (2 * t + e) * 4) * ks;
+            const int64_t re = r0 + 2 * t + e;
+            const int lim = sees(re);
+            const float2 ml = re < a.R ? a.ml[unit * a.R + re] : make_float2(0.f, 0.f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (mine + j < lim && ml.y != 0.f) sum[j] += ex2(score_of(s[0][j >> 1][2 * (j & 1) + e], mul, a.cap) - ml.x) * ml.y;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
+        sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
+        if (t == 0 && mine + j < sees.held) a.c.weight[(size_t)unit * a.c.C + mine + j] += sum[j];
+    }
+}
+
+template <typename T, int D, int NT, int TERMS>
+cudaError_t attend_with(const QcAttend& a, cudaStream_t s) {
+    constexpr int smem = kQaWarps * kQaStages * 2 * kQcBlock * D;
+    cudaError_t e = cudaFuncSetAttribute(qc_attend_kernel<T, D, NT, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    qc_attend_kernel<T, D, NT, TERMS><<<(a.n_warps + kQaWarps - 1) / kQaWarps, kQaThreads, smem, s>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename T, int D, int TERMS>
+cudaError_t attend_of(const QcAttend& a, const QcPlan& p, cudaStream_t s) {
+    cudaError_t e = cudaErrorInvalidValue;
+    if (p.tiles == 1) e = attend_with<T, D, 1, TERMS>(a, s);
+    else if (p.tiles == 2) e = attend_with<T, D, 2, TERMS>(a, s);
+    else if constexpr (TERMS == 1) e = attend_with<T, D, 3, TERMS>(a, s);
+    if (e != cudaSuccess) return e;
+    const int64_t units = (int64_t)a.c.B * a.c.Hkv;
+    const int64_t ctas = p.by_scores ? (a.c.C + kQjSlots - 1) / kQjSlots : (a.R + 7) / 8;
+    qc_join_kernel<T, D><<<(unsigned)(units * ctas), kQjThreads, 0, s>>>(a, (int)ctas, p.rows);
+    if ((e = cudaGetLastError()) != cudaSuccess || a.accumulate == 0 || p.by_scores) return e;
+    const int64_t per_unit = (a.c.NB + kQaWarps - 1) / kQaWarps;
+    qc_weights_kernel<T, D, TERMS><<<(unsigned)(units * per_unit), kQaThreads, 0, s>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+int qc_attend_max_warps() { return 148 * kQaWarps; }
+
+cudaError_t qc_attend(const QcAttend& a, const QcPlan& p, int dtype, cudaStream_t s) {
+    if (dtype == BCT_BF16)
+        return a.c.D == 128 ? attend_of<__nv_bfloat16, 128, 1>(a, p, s) : attend_of<__nv_bfloat16, 64, 1>(a, p, s);
+    return a.c.D == 128 ? attend_of<float, 128, 2>(a, p, s) : attend_of<float, 64, 2>(a, p, s);
+}
+
+}  // namespace bct
