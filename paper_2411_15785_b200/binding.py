@@ -507,7 +507,7 @@ class QuantCache:
 
     def __init__(self, batch, n_kv_heads, head_dim, capacity, device="cuda", planes=None):
         self.B, self.Hkv, self.d, self.C = map(operator.index, (batch, n_kv_heads, head_dim, capacity))
-        lib = load()
+        lib = self._lib = load()
         slots, blocks = (self.B, self.Hkv, self.C), (self.B, self.Hkv, -(-self.C // QCACHE_BLOCK))
         kinds = (("k", (*slots, self.d), torch.int8), ("v", (*slots, self.d), torch.int8), ("k_scale", blocks, torch.float32),
                  ("v_scale", blocks, torch.float32), ("weight", slots, torch.float32), ("position", slots, torch.int32),
@@ -527,7 +527,7 @@ class QuantCache:
         self._planes = tuple(planes)   # the library has their addresses
         self._c = BctQcache(self.B, self.Hkv, self.d, self.C, *(t.data_ptr() for t in planes))
         self._p = ctypes.byref(self._c)
-        self._need = {}
+        self._known = {}              # sizes of calls, by the shapes that they follow from
 
     @property
     def held(self) -> torch.Tensor:
@@ -539,23 +539,32 @@ class QuantCache:
         """Tokens appended to each sequence so far, int32 ``[B]`` on the device."""
         return self.state[1]
 
-    def _tokens(self, name, x, heads, lens):
-        """Checks x ``[B, T, heads, d]`` and lens; returns (T, dtype code)."""
+    def _sizes(self, name, x, heads):
+        """(T, dtype code) of x ``[B, T, heads, d]``."""
         if x.dim() != 4 or x.dtype not in (torch.float32, torch.bfloat16):
             raise ValueError("%s must be float32 or bfloat16 [B, T, heads, head_dim] (got %s, %s)" % (name, x.dtype, tuple(x.shape)))
         _operand(name, x, torch.Size((self.B, x.shape[1], heads, self.d)), x.dtype, self.dev)
-        if lens is not None:
-            _operand("lens", lens, torch.Size((self.B,)), torch.int32, self.dev)
         return x.shape[1], BCT_BF16 if x.dtype is torch.bfloat16 else BCT_F32
+
+    def _lens(self, lens):
+        _operand("lens", lens, torch.Size((self.B,)), torch.int32, self.dev)
+        return lens.data_ptr()
 
     def append(self, k, v, lens=None, stream=None) -> None:
         """k, v ``[B, T, Hkv, d]`` float32 or bfloat16 go behind the slots held; lens int32 ``[B]`` or None (all T): the
         valid tokens of each sequence of a padded batch.  Tokens that find no slot free are dropped: evict first."""
         if stream is not None:
             return _on_stream(stream, lambda k_: self.append(k_, v, lens), k)
-        T, dt = self._tokens("k", k, self.Hkv, lens)
-        _operand("v", v, k.shape, k.dtype, self.dev)
-        _launch(self.dev, load().bct_qcache_append, self._p, T, dt, k.data_ptr(), v.data_ptr(), _ptr(lens))
+        dt, shape = k.dtype, k.shape
+        sizes = self._known.get((shape, dt))     # what follows from the shape alone
+        if sizes is None:
+            sizes = self._known[shape, dt] = self._sizes("k", k, self.Hkv)
+        if not (k.get_device() == self.dev and v.get_device() == self.dev and v.shape == shape and v.dtype is dt
+                and k.is_contiguous() and v.is_contiguous()):
+            _operand("k", k, shape, dt, self.dev)      # one of these says what it is
+            _operand("v", v, shape, dt, self.dev)
+        _launch(self.dev, self._lib.bct_qcache_append, self._p, *sizes, k.data_ptr(), v.data_ptr(),
+                None if lens is None else self._lens(lens))
 
     def attend(self, q, lens=None, scale=0.0, score_cap=0.0, accumulate=True, out=None, scratch=None, stream=None):
         """Attention of the last T tokens appended to each sequence, q ``[B, T, Hq, d]``, each over the slots up to its
@@ -563,18 +572,25 @@ class QuantCache:
         accumulate: adds what each slot was given to ``weight``.  Returns out ``[B, T, Hq, d]``."""
         if stream is not None:
             return _on_stream(stream, lambda q_: self.attend(q_, lens, scale, score_cap, accumulate, out, scratch), q)
-        Hq = q.shape[2] if q.dim() == 4 else 0
-        T, dt = self._tokens("q", q, Hq, lens)
-        out = torch.empty_like(q) if out is None else _result("out", out, q, q.shape, q.dtype, self.dev)
-        key = (T, Hq, dt, bool(accumulate))
-        need = self._need.get(key)
-        if need is None:
+        accumulate = 1 if accumulate else 0
+        key = (q.shape, q.dtype, accumulate)
+        known = self._known.get(key)
+        if known is None:
+            Hq = q.shape[2] if q.dim() == 4 else 0
+            T, dt = self._sizes("q", q, Hq)
             n = ctypes.c_size_t(0)
-            _check(load().bct_qcache_attend_scratch_bytes(self._p, T, Hq, dt, key[3], ctypes.byref(n)))
-            need = self._need[key] = n.value
+            _check(self._lib.bct_qcache_attend_scratch_bytes(self._p, T, Hq, dt, accumulate, ctypes.byref(n)))
+            known = self._known[key] = T, Hq, dt, n.value
+        T, Hq, dt, need = known
+        if q.get_device() != self.dev or not q.is_contiguous():
+            _operand("q", q, q.shape, q.dtype, self.dev)
+        if out is None:
+            out = torch.empty_like(q)
+        else:
+            _operand("out", out, q.shape, q.dtype, self.dev)
         scratch = _scratch(need, scratch, q, self.dev)
-        _launch(self.dev, load().bct_qcache_attend, self._p, T, Hq, dt, q.data_ptr(), _ptr(lens), scale, score_cap, key[3],
-                out.data_ptr(), *_scratch_args(scratch))
+        _launch(self.dev, self._lib.bct_qcache_attend, self._p, T, Hq, dt, q.data_ptr(),
+                None if lens is None else self._lens(lens), scale, score_cap, accumulate, out.data_ptr(), *_scratch_args(scratch))
         return out
 
     def evict(self, keep, recent=0, scratch=None, stream=None) -> None:
@@ -583,13 +599,13 @@ class QuantCache:
         if stream is not None:
             return _on_stream(stream, lambda k_: self.evict(keep, recent, scratch), self.k)
         keep, recent = operator.index(keep), operator.index(recent)
-        need = self._need.get(keep)
+        need = self._known.get(keep)
         if need is None:
             n = ctypes.c_size_t(0)
-            _check(load().bct_qcache_evict_scratch_bytes(self._p, keep, ctypes.byref(n)))
-            need = self._need[keep] = n.value
+            _check(self._lib.bct_qcache_evict_scratch_bytes(self._p, keep, ctypes.byref(n)))
+            need = self._known[keep] = n.value
         scratch = _scratch(need, scratch, self.k, self.dev)
-        _launch(self.dev, load().bct_qcache_evict, self._p, keep, recent, *_scratch_args(scratch))
+        _launch(self.dev, self._lib.bct_qcache_evict, self._p, keep, recent, *_scratch_args(scratch))
 
 
 class Cache:

@@ -60,21 +60,32 @@ struct QcAttend {
     int n_warps;           // warps that share the blocks of all units
     float* part_o;         // [2 n_warps][rows of a group][d]: what a warp has of a unit that it shares with others
     float2* part_ml;       // [2 n_warps][rows of a group]: running maximum (in powers of two) and sum
+    int2* spans;           // [units][row groups]: the first and last warp that have blocks of them
     float2* ml;            // [units][R]: maximum, 1 / sum
     float* scores;         // [units][C][R2], powers of two; NULL where the weights are formed from the keys again
     int R2;                // R, rounded up to an even number where it is not 1
 };
+// The tensor path's share of such a call (bct_qcache_prompt.cu).
+struct QcPrompt {
+    int tiles;             // of 256 rows, per unit
+    int splits;            // CTAs that share the slots of a tile of rows
+    uint16_t* q16;         // [units][R][d]: queries as fp16, and what their products are multiplied with; NULL without weights
+    float* q_factor;       // [units][R]
+};
 // Which kernels serve a call, and its scratch: offsets into the caller's buffer, by the arguments alone.
 struct QcPlan {
-    int rows;              // rows of a group
+    bool prompt;           // the tensor path: bfloat16, more than kQcScoredRows rows
+    QcPrompt pr;
+    int rows;              // otherwise: rows of a group
     int tiles;             // of 8 rows each
     bool by_scores;        // the weights come from stored scores
     int n_warps;
     int64_t n_groups;
     int R2;
-    size_t part_o, part_ml, ml, scores, total;
+    size_t part_o, part_ml, spans, ml, scores, q16, q_factor, total;
 };
 cudaError_t qc_attend(const QcAttend& a, const QcPlan& p, int dtype, cudaStream_t s);
+cudaError_t qc_prompt(const QcAttend& a, const QcPrompt& pr, cudaStream_t s);
 int qc_attend_max_warps();
 
 }  // namespace bct

@@ -31,6 +31,8 @@
 #include "bct_device.cuh"
 #include "bct_internal.h"
 #include "bct_qcache.h"
+#include "bct_qcache.cuh"
+#include "bct_qcache_math.cuh"
 #include "bct_tc.cuh"
 
 namespace bct {
@@ -42,26 +44,8 @@ constexpr int kQaStages = 3;
 constexpr int kQaScored = kQcScoredRows;
 constexpr int kQjThreads = 256;
 constexpr int kQjSlots = 1024;        // slots of a CTA of the joining kernel
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kPScale = 32768.f;    // of a probability on its way into fp16
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
-// a pair of bytes of `w` (each a code + 128), chosen by `sel`, as fp16
-__device__ __forceinline__ uint32_t pair_of(uint32_t w, uint32_t sel) {
-    const uint32_t u = prmt(w, 0x64646464u, sel);
-    const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x6480)));
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t half2_bits(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ float2 half2_floats(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -72,9 +56,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     uint32_t y;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
-}
-__device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void* src, bool real) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() {
@@ -115,30 +96,6 @@ __device__ __forceinline__ int64_t count_blocks(const QcAttend& a, int64_t* upto
 // The warp whose run has block x of `total` in all, of n runs (n <= total).
 __device__ __forceinline__ int run_of(int64_t x, int64_t total, int n) { return (int)(((x + 1) * n - 1) / total); }
 
-// What a row sees: rows of a unit are (token, head), token-major.
-struct Sees {
-    int held, n, G;   // slots held, valid tokens
-    int64_t R;
-    __device__ __forceinline__ int operator()(int64_t r) const {
-        const int64_t i = r / G;
-        return r < R && i < n ? max(held - n + (int)i + 1, 0) : 0;
-    }
-};
-__device__ __forceinline__ Sees sees_of(const QcAttend& a, int b) {
-    Sees s;
-    s.held = min(max(a.c.state[b], 0), a.c.C);
-    s.n = (int)(a.lens == nullptr ? a.T : min((int64_t)max(a.lens[b], 0), a.T));
-    s.G = a.G;
-    s.R = a.R;
-    return s;
-}
-template <typename T>
-__device__ __forceinline__ const T* row_of(const QcAttend& a, const void* base, int b, int h, int64_t r) {
-    const int64_t i = r / a.G;
-    const int64_t head = (int64_t)h * a.G + (r - i * a.G);
-    return static_cast<const T*>(base) + (((int64_t)b * a.T + i) * ((int64_t)a.c.Hkv * a.G) + head) * a.c.D;
-}
-
 // The queries of eight rows as fragments: lane (g, t) has row g.  `mul`: what the row was divided by.
 template <typename T, int D, int TERMS>
 __device__ __forceinline__ void load_queries(const T* row, bool real, uint32_t (&f)[TERMS][D / 16][2], float* mul) {
@@ -159,11 +116,8 @@ __device__ __forceinline__ void load_queries(const T* row, bool real, uint32_t (
     for (int i = 0; i < D / 4; ++i) top = fmaxf(top, fabsf(x[i]));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    // 2^(14 - exponent of the largest), from 2^-113 to 2^126; rows of zeros, infinities or NaN as they are
-    const int e = (int)(__float_as_uint(top) >> 23) - 127;
-    const int up = e > -127 && e < 128 ? min(14 - e, 126) : 0;
-    const float by = __uint_as_float((uint32_t)(up + 127) << 23);
-    *mul = __uint_as_float((uint32_t)(127 - up) << 23);
+    float by;
+    row_scale(top, &by, mul);
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
 #pragma unroll
@@ -217,15 +171,15 @@ __device__ __forceinline__ void score_products(const uint32_t (&w)[4][D / 16], c
 }
 
 // Scores in powers of two from products: `mul` has the block's scale and the row's.
-__device__ __forceinline__ float score_of(float dot, float mul, float cap) {
-    const float s = dot * mul;
-    return cap > 0.f ? cap * kLog2e * tanhf(s) : s;
+__device__ __forceinline__ void to_scores(float (&s)[2][4], float mul0, float mul1, float cap) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] *= i & 1 ? mul1 : mul0;
+    if (cap > 0.f) {
+        const float to = cap * kLog2e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = to * tanh1(s[i >> 2][i & 3]);
+    }
 }
-// what a row's products are multiplied with, besides the block's scale
-__device__ __forceinline__ float row_factor(const QcAttend& a, float mul) {
-    return a.cap > 0.f ? mul * (a.scale / a.cap) : mul * (a.scale * kLog2e);
-}
-
 template <typename T, int D, int NT, int TERMS>
 __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend a) {
     constexpr int kTile = kQcBlock * D;
@@ -237,6 +191,8 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
     unsigned char* ring = qa_smem + warp * (kQaStages * 2 * kTile);
     const uint32_t ring32 = smem_u32(ring);
 
+    pdl_wait();
+    pdl_open();
     int chunk;
     const int64_t per_seq = (int64_t)a.c.Hkv * a.n_groups;
     const int64_t total = count_blocks(a, upto, &chunk) * per_seq;
@@ -356,12 +312,12 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float top[2] = {-INFINITY, -INFINITY};
+                to_scores(s[nt], ks * mul[nt][0], ks * mul[nt][1], a.cap);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         float& v = s[nt][j >> 1][2 * (j & 1) + e];
-                        v = score_of(v, ks * mul[nt][e], a.cap);
                         if (!all && slot0 + j >= lim[nt][e]) v = -INFINITY;
                         top[e] = fmaxf(top[e], v);
                     }
@@ -467,6 +423,8 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
 
         // the piece's sums; a whole unit is done, a part goes to scratch
         const bool whole = first == 0 && last == nb;
+        if (first == 0 && lane == 0)    // for who joins them: the first and last run that have blocks of these rows
+            a.spans[unit * a.n_groups + group] = make_int2(run, whole ? run : run_of(x + nb - 1, total, n_runs));
         const int64_t slot_no = first == 0 ? 2 * (int64_t)run + 1 : 2 * (int64_t)run;
         constexpr int kE = D / 8;     // features of a lane
 #pragma unroll
@@ -510,169 +468,207 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
     }
 }
 
-// Joins what several warps have of a unit, writes the zeros of rows that see nothing in an empty cache, and adds the
-// weights from the stored scores.  A CTA per unit and kQjSlots of its slots (per unit and 8 rows of it, where there are no
-// scores); the rows that a unit's CTAs join are shared out among them.
-template <typename T, int D>
+// Joins what several warps have of a unit, writes the zeros of an empty cache's rows, and adds the weights from the stored
+// scores (SCORED).  A CTA per unit and kQjSlots of its slots, or, without scores, per unit and 8 of its rows; the rows that
+// a unit's CTAs join are shared out among them, and a row's parts, up to two for each warp that the call has, among the
+// CTA's threads.
+template <typename T, int D, bool SCORED>
 __global__ void __launch_bounds__(kQjThreads) qc_join_kernel(const QcAttend a, int ctas, int group_rows) {
-    __shared__ float2 row_ml[kQaScored];           // where there are scores
-    __shared__ int row_sees[kQaScored];
-    __shared__ int64_t upto[kQjThreads];
-    const int64_t unit = blockIdx.x / ctas;
+    constexpr int kLanes = D / 4, kSlices = kQjThreads / kLanes;   // four features of a lane; slices of a row's parts
+    constexpr int kEach = kQjSlots / kQjThreads;
+    __shared__ float2 row_ml[SCORED ? kQaScored : 1];
+    __shared__ int row_sees[SCORED ? kQaScored : 1];
+    __shared__ float4 sums[kSlices][kLanes];
+    const unsigned unit = blockIdx.x / (unsigned)ctas;
     const int part = (int)(blockIdx.x - unit * ctas);
-    const int b = (int)(unit / a.c.Hkv), h = (int)(unit - (int64_t)b * a.c.Hkv), tid = threadIdx.x;
+    const int b = (int)(unit / (unsigned)a.c.Hkv), h = (int)unit - b * a.c.Hkv, tid = threadIdx.x;
+    const int lane = tid & 31, warp = tid >> 5;
+    pdl_wait();
+    pdl_open();
     const Sees sees = sees_of(a, b);
     const int nb = (sees.held + kQcBlock - 1) / kQcBlock;
-    int chunk;
-    const int64_t per_seq = (int64_t)a.c.Hkv * a.n_groups;
-    const int64_t total = count_blocks(a, upto, &chunk) * per_seq;
-    const int n_runs = (int)min((int64_t)a.n_warps, total);
-    int64_t before = b / chunk ? upto[b / chunk - 1] : 0;
-    for (int i = b / chunk * chunk; i < b; ++i) before += (min(max(a.c.state[i], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
-    before = before * per_seq + (int64_t)h * a.n_groups * nb;
+    const int slot0 = part * kQjSlots + tid, end = sees.n > 0 ? min((part + 1) * kQjSlots, sees.held) : 0;
+    float* weight = a.c.weight + (size_t)unit * a.c.C;
+    const float* scores = a.scores + (size_t)unit * a.c.C * a.R2;
+    // (on their way while the rows' sums are formed)
+    float before[kEach], single[kEach];
+    if constexpr (SCORED) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = slot0 + i * kQjThreads;
+            before[i] = j < end ? weight[j] : 0.f;
+            single[i] = j < end && a.R2 == 1 ? scores[j] : 0.f;
+        }
+    }
 
-    // which warps have a row group: [first, last]
-    auto runs = [&](int64_t group, int* first, int* last) {
-        *first = run_of(before + group * nb, total, n_runs);
-        *last = run_of(before + (group + 1) * nb - 1, total, n_runs);
-    };
-    // maximum and 1 / sum of a row; the parts' places are 2 first + 1, then 2 run
-    auto join = [&](int64_t r, int first, int last) {
-        const int64_t row = r % group_rows;
+    // the runs that have a row's group; where its parts are: 2 first + 1, then 2 run
+    auto span_of = [&](int64_t r) { return nb > 0 ? a.spans[unit * a.n_groups + r / group_rows] : make_int2(0, 0); };
+    auto place = [&](int64_t r, int run, int first) { return (2 * (int64_t)run + (run == first)) * group_rows + r % group_rows; };
+    // maximum and 1 / sum of a row, by a warp
+    auto join = [&](int64_t r, int2 span) {
+        if (nb == 0) return make_float2(-INFINITY, 0.f);
+        if (span.x == span.y) return a.ml[(size_t)unit * a.R + r];
         float m = -INFINITY, l = 0.f;
-        for (int i = first; i <= last; ++i) {
-            const float2 p = a.part_ml[(2 * (int64_t)i + (i == first)) * group_rows + row];
+        for (int i = span.x + lane; i <= span.y; i += 32) {
+            const float2 p = a.part_ml[place(r, i, span.x)];
             const float top = fmaxf(m, p.x);
-            if (top == -INFINITY) {
-                l += p.y;      // (0, or a NaN)
-                continue;
-            }
-            l = l * ex2(m - top) + p.y * ex2(p.x - top);
+            l = top == -INFINITY ? l + p.y : l * ex2(m - top) + p.y * ex2(p.x - top);   // (p.y is 0, or a NaN)
             m = top;
         }
-        return make_float2(m, l > 0.f ? 1.f / l : (l == l ? 0.f : l));
+        const float top = warp_max(m);
+        l = warp_sum(top == -INFINITY ? l : l * ex2(m - top));
+        return make_float2(top, l > 0.f ? 1.f / l : (l == l ? 0.f : l));
     };
 
-    const bool scored = a.scores != nullptr;
-    if (scored) {
-        for (int r = tid; r < a.R; r += kQjThreads) {
-            float2 v = make_float2(-INFINITY, 0.f);
-            if (nb > 0) {
-                int first, last;
-                runs(r / group_rows, &first, &last);
-                v = first == last ? a.ml[unit * a.R + r] : join(r, first, last);
+    if constexpr (SCORED) {                        // every row's, for the weights (R <= kQaScored)
+        for (int r = warp; r < (int)a.R; r += kQjThreads / 32) {
+            const float2 v = join(r, span_of(r));
+            if (lane == 0) {
+                row_ml[r] = v;
+                row_sees[r] = v.y == 0.f ? 0 : sees(r);
             }
-            row_ml[r] = v;
-            row_sees[r] = v.y == 0.f ? 0 : sees(r);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = slot0 + i * kQjThreads;
+            if (j >= end) break;
+            float w = 0.f;
+            if (a.R2 == 1) {
+                if (j < row_sees[0]) w = ex2(single[i] - row_ml[0].x) * row_ml[0].y;
+            } else {
+                const float2* s = reinterpret_cast<const float2*>(scores + (size_t)j * a.R2);
+#pragma unroll 4
+                for (int r = 0; r < (int)a.R; r += 2) {
+                    const float2 v = s[r / 2];
+                    if (j < row_sees[r]) w += ex2(v.x - row_ml[r].x) * row_ml[r].y;
+                    if (r + 1 < (int)a.R && j < row_sees[r + 1]) w += ex2(v.y - row_ml[r + 1].x) * row_ml[r + 1].y;
+                }
+            }
+            weight[j] = before[i] + w;
+        }
+    }
+    const int64_t r_step = SCORED ? ctas : 1, r_end = SCORED ? a.R : min(a.R, (int64_t)(part + 1) * 8);
+    for (int64_t r = SCORED ? part : (int64_t)part * 8; r < r_end; r += r_step) {
+        const int2 span = span_of(r);
+        if (nb > 0 && span.x == span.y) continue;              // whole: its warp wrote it
+        float2 ml;
+        if constexpr (SCORED) {
+            ml = row_ml[r];
+        } else {
+            if (warp == 0) {
+                ml = join(r, span);
+                if (lane == 0) row_ml[0] = a.ml[(size_t)unit * a.R + r] = ml;
+            }
+            __syncthreads();
+            ml = row_ml[0];
+        }
+        const int slice = tid / kLanes, f = tid % kLanes;
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (nb > 0) {
+#pragma unroll 4
+            for (int i = span.x + slice; i <= span.y; i += kSlices) {
+                const int64_t at = place(r, i, span.x);
+                const float m = a.part_ml[at].x;
+                const float by = m == -INFINITY ? 0.f : ex2(m - ml.x) * ml.y;
+                const float4 o = *reinterpret_cast<const float4*>(a.part_o + at * D + 4 * f);
+                y.x = fmaf(o.x, by, y.x), y.y = fmaf(o.y, by, y.y), y.z = fmaf(o.z, by, y.z), y.w = fmaf(o.w, by, y.w);
+            }
+        }
+        sums[slice][f] = y;
+        __syncthreads();
+        if (slice == 0) {
+#pragma unroll
+            for (int i = 1; i < kSlices; ++i) {
+                const float4 o = sums[i][f];
+                y.x += o.x, y.y += o.y, y.z += o.z, y.w += o.w;
+            }
+            if (ml.y != ml.y) y = make_float4(ml.y, ml.y, ml.y, ml.y);
+            T* to = const_cast<T*>(row_of<T>(a, a.out, b, h, r)) + 4 * f;
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = y;
+            else *reinterpret_cast<uint2*>(to) = make_uint2(Chunk<T>::pack2(y.x, y.y), Chunk<T>::pack2(y.z, y.w));
         }
         __syncthreads();
     }
-    // outputs: 32 threads and more to a row
-    constexpr int kPer = kQjThreads / (D / 4);     // rows at a time
-    const int64_t step = scored ? (int64_t)ctas * kPer : kPer;
-    const int64_t r_end = scored ? a.R : min(a.R, (int64_t)(part + 1) * 8);
-    for (int64_t r = (scored ? (int64_t)part * kPer : (int64_t)part * 8) + tid / (D / 4); r < r_end; r += step) {
-        const int f = tid % (D / 4) * 4;
-        int first = 0, last = 0;
-        if (nb > 0) runs(r / group_rows, &first, &last);
-        if (nb > 0 && first == last) continue;
-        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (nb > 0) {
-            const float2 ml = scored ? row_ml[r] : join(r, first, last);
-            for (int i = first; i <= last; ++i) {
-                const int64_t at = (2 * (int64_t)i + (i == first)) * group_rows + r % group_rows;
-                const float m = a.part_ml[at].x;
-                const float by = m == -INFINITY ? 0.f : ex2(m - ml.x) * ml.y;
-                const float4 o = *reinterpret_cast<const float4*>(a.part_o + at * D + f);
-                y.x = fmaf(o.x, by, y.x), y.y = fmaf(o.y, by, y.y), y.z = fmaf(o.z, by, y.z), y.w = fmaf(o.w, by, y.w);
-            }
-            if (ml.y != ml.y) y = make_float4(ml.y, ml.y, ml.y, ml.y);
-            if (!scored && f == 0) a.ml[unit * a.R + r] = ml;
-        } else if (!scored && f == 0) {
-            a.ml[unit * a.R + r] = make_float2(-INFINITY, 0.f);
-        }
-        T* to = const_cast<T*>(row_of<T>(a, a.out, b, h, r)) + f;
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = y;
-        else *reinterpret_cast<uint2*>(to) = make_uint2(Chunk<T>::pack2(y.x, y.y), Chunk<T>::pack2(y.z, y.w));
-    }
-    if (!scored) return;
-    for (int j = part * kQjSlots + tid; j < min((part + 1) * kQjSlots, sees.n > 0 ? sees.held : 0); j += kQjThreads) {
-        const float* s = a.scores + ((size_t)unit * a.c.C + j) * a.R2;
-        float w = 0.f;
-        for (int r = 0; r < a.R; ++r)
-            if (j < row_sees[r]) w += ex2(s[r] - row_ml[r].x) * row_ml[r].y;
-        a.c.weight[(size_t)unit * a.c.C + j] += w;
-    }
 }
 
-// The weights from the keys again, for calls with many rows: a warp per block of slots goes through the rows that see it.
+// The weights from the keys again, for calls with many rows: a CTA per block of slots, whose warps share the rows that see
+// it and add up in their order.
 template <typename T, int D, int TERMS>
 __global__ void __launch_bounds__(kQaThreads) qc_weights_kernel(const QcAttend a) {
-    __shared__ __align__(128) unsigned char tiles[kQaWarps][kQcBlock * D];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int per_unit = (a.c.NB + kQaWarps - 1) / kQaWarps;
-    const int64_t unit = blockIdx.x / per_unit;
-    const int blk = (int)(blockIdx.x - unit * per_unit) * kQaWarps + warp;
-    const int b = (int)(unit / a.c.Hkv), h = (int)(unit - (int64_t)b * a.c.Hkv);
+    __shared__ __align__(128) unsigned char tile[kQcBlock * D];
+    __shared__ float sums[kQaWarps][kQcBlock];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const unsigned unit = blockIdx.x / (unsigned)a.c.NB;
+    const int blk = (int)(blockIdx.x - unit * a.c.NB);
+    const int b = (int)(unit / (unsigned)a.c.Hkv), h = (int)unit - b * a.c.Hkv;
+    pdl_wait();
     const Sees sees = sees_of(a, b);
     const int slot0 = blk * kQcBlock;
     if (slot0 >= sees.held || sees.n == 0) return;
-    unsigned char* tile = tiles[warp];
     {
         const int8_t* kp = a.c.codes[0] + (size_t)unit * a.c.C * D;
-        constexpr int kChunks = D / 16, kPer = 32 / kChunks;
-        const int c = lane % kChunks;
-#pragma unroll
-        for (int i = 0; i < kQcBlock / kPer; ++i) {
-            const int s = i * kPer + lane / kChunks;
+        constexpr int kChunks = D / 16;
+        if (tid < kQcBlock * kChunks) {
+            const int s = tid / kChunks, c = tid % kChunks;
             const bool real = slot0 + s < sees.held;
             cp_async16_zfill(smem_u32(tile + tile_at<D>(s, c)), kp + (size_t)(real ? slot0 + s : 0) * D + c * 16, real);
         }
         cp_async_commit();
         cp_async_wait<0>();
-        __syncwarp();
+        __syncthreads();
     }
     const float ks = a.c.scale[0][(size_t)unit * a.c.NB + blk];
     uint32_t w[4][D / 16];
     load_keys<D>(tile, g, t, w);
     // the first token that sees the block's first slot
     const int i0 = max(0, slot0 - (sees.held - sees.n));
-    const int mine = slot0 + 8 * (g >> 1) + 4 * (g & 1);
+    const int mine = 8 * (g >> 1) + 4 * (g & 1);
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t r0 = (int64_t)i0 * a.G / 8 * 8; r0 < (int64_t)sees.n * a.G; r0 += 8) {
+    for (int64_t r0 = (int64_t)i0 * a.G / 8 * 8 + warp * 8; r0 < (int64_t)sees.n * a.G; r0 += 8 * kQaWarps) {
         uint32_t q[1][TERMS][D / 16][2];
         float m;
         const int64_t r = r0 + g;
         load_queries<T, D, TERMS>(row_of<T>(a, a.q, b, h, r < a.R ? r : 0), r < a.R, q[0], &m);
         m = row_factor(a, m);
-        float s[1][2][4];
-        score_products<D, TERMS, 1>(w, q, s);
+        float2 ml[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const float mul = __shfl_sync(0xffffffffu, m, (2 * t + e) * 4) * ks;
             const int64_t re = r0 + 2 * t + e;
-            const int lim = sees(re);
-            const float2 ml = re < a.R ? a.ml[unit * a.R + re] : make_float2(0.f, 0.f);
+            ml[e] = re < a.R ? a.ml[(size_t)unit * a.R + re] : make_float2(0.f, 0.f);
+        }
+        float s[1][2][4];
+        score_products<D, TERMS, 1>(w, q, s);
+        to_scores(s[0], __shfl_sync(0xffffffffu, m, 8 * t) * ks, __shfl_sync(0xffffffffu, m, 8 * t + 4) * ks, a.cap);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int lim = sees(r0 + 2 * t + e);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (mine + j < lim && ml.y != 0.f) sum[j] += ex2(score_of(s[0][j >> 1][2 * (j & 1) + e], mul, a.cap) - ml.x) * ml.y;
+                if (slot0 + mine + j < lim && ml[e].y != 0.f) sum[j] += ex2(s[0][j >> 1][2 * (j & 1) + e] - ml[e].x) * ml[e].y;
         }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
         sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
-        if (t == 0 && mine + j < sees.held) a.c.weight[(size_t)unit * a.c.C + mine + j] += sum[j];
+        if (t == 0) sums[warp][mine + j] = sum[j];
+    }
+    __syncthreads();
+    if (tid < kQcBlock && slot0 + tid < sees.held) {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < kQaWarps; ++i) x += sums[i][tid];
+        a.c.weight[(size_t)unit * a.c.C + slot0 + tid] += x;
     }
 }
 
 template <typename T, int D, int NT, int TERMS>
 cudaError_t attend_with(const QcAttend& a, cudaStream_t s) {
     constexpr int smem = kQaWarps * kQaStages * 2 * kQcBlock * D;
-    cudaError_t e = cudaFuncSetAttribute(qc_attend_kernel<T, D, NT, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-    qc_attend_kernel<T, D, NT, TERMS><<<(a.n_warps + kQaWarps - 1) / kQaWarps, kQaThreads, smem, s>>>(a);
-    return cudaGetLastError();
+    static std::atomic<uint64_t> done{0};
+    if (const cudaError_t e = allow_smem(qc_attend_kernel<T, D, NT, TERMS>, smem, &done)) return e;
+    return pdl_launch(qc_attend_kernel<T, D, NT, TERMS>, (a.n_warps + kQaWarps - 1) / kQaWarps, kQaThreads, smem, s, a);
 }
 
 template <typename T, int D, int TERMS>
@@ -683,12 +679,14 @@ cudaError_t attend_of(const QcAttend& a, const QcPlan& p, cudaStream_t s) {
     else if constexpr (TERMS == 1) e = attend_with<T, D, 3, TERMS>(a, s);
     if (e != cudaSuccess) return e;
     const int64_t units = (int64_t)a.c.B * a.c.Hkv;
-    const int64_t ctas = p.by_scores ? (a.c.C + kQjSlots - 1) / kQjSlots : (a.R + 7) / 8;
-    qc_join_kernel<T, D><<<(unsigned)(units * ctas), kQjThreads, 0, s>>>(a, (int)ctas, p.rows);
-    if ((e = cudaGetLastError()) != cudaSuccess || a.accumulate == 0 || p.by_scores) return e;
-    const int64_t per_unit = (a.c.NB + kQaWarps - 1) / kQaWarps;
-    qc_weights_kernel<T, D, TERMS><<<(unsigned)(units * per_unit), kQaThreads, 0, s>>>(a);
-    return cudaGetLastError();
+    const int ctas = (int)(p.by_scores ? (a.c.C + kQjSlots - 1) / kQjSlots : (a.R + 7) / 8);
+    e = p.by_scores ? pdl_launch(qc_join_kernel<T, D, true>, (unsigned)(units * ctas), kQjThreads, 0, s, a, ctas, p.rows)
+                    : pdl_launch(qc_join_kernel<T, D, false>, (unsigned)(units * ctas), kQjThreads, 0, s, a, ctas, p.rows);
+    if constexpr (TERMS == 2) {   // (many bfloat16 rows are the tensor path's)
+        if (e == cudaSuccess && a.accumulate != 0 && !p.by_scores)
+            e = pdl_launch(qc_weights_kernel<T, D, TERMS>, (unsigned)(units * a.c.NB), kQaThreads, 0, s, a);
+    }
+    return e;
 }
 
 }  // namespace

@@ -1,0 +1,86 @@
+// What the attention kernels of the 8-bit cache share on the device: what a row is and sees, codes and queries as fp16,
+// scores.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "bct_device.cuh"
+#include "bct_qcache.h"
+
+namespace bct {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
+// a pair of bytes of `w` (each a code + 128), chosen by `sel`, as fp16
+__device__ __forceinline__ uint32_t pair_of(uint32_t w, uint32_t sel) {
+    const uint32_t u = prmt(w, 0x64646464u, sel);
+    const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t half2_bits(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 half2_floats(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
+__device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void* src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+// What a row sees: rows of a unit are (token, head), token-major.
+struct Sees {
+    int held, n, G;   // slots held, valid tokens
+    int64_t R;
+    __device__ __forceinline__ int operator()(int64_t r) const {
+        const int64_t i = r / G;
+        return r < R && i < n ? max(held - n + (int)i + 1, 0) : 0;
+    }
+};
+__device__ __forceinline__ Sees sees_of(const QcAttend& a, int b) {
+    Sees s;
+    s.held = min(max(a.c.state[b], 0), a.c.C);
+    s.n = (int)(a.lens == nullptr ? a.T : min((int64_t)max(a.lens[b], 0), a.T));
+    s.G = a.G;
+    s.R = a.R;
+    return s;
+}
+template <typename T>
+__device__ __forceinline__ const T* row_of(const QcAttend& a, const void* base, int b, int h, int64_t r) {
+    const int64_t i = r / a.G;
+    const int64_t head = (int64_t)h * a.G + (r - i * a.G);
+    return static_cast<const T*>(base) + (((int64_t)b * a.T + i) * ((int64_t)a.c.Hkv * a.G) + head) * a.c.D;
+}
+
+// The power of two that brings a row whose largest magnitude is `top` into [2^14, 2^15), from 2^-113 to 2^126, and its
+// inverse; rows of zeros, infinities or NaN are left as they are.
+__device__ __forceinline__ void row_scale(float top, float* by, float* back) {
+    const int e = (int)(__float_as_uint(top) >> 23) - 127;
+    const int up = e > -127 && e < 128 ? min(14 - e, 126) : 0;
+    *by = __uint_as_float((uint32_t)(up + 127) << 23);
+    *back = __uint_as_float((uint32_t)(127 - up) << 23);
+}
+// what a row's products are multiplied with, besides the block's scale
+__device__ __forceinline__ float row_factor(const QcAttend& a, float mul) {
+    return a.cap > 0.f ? mul * (a.scale / a.cap) : mul * (a.scale * kLog2e);
+}
+
+// tanh: the fifth convergent of Lambert's continued fraction x / (1 + x^2 / (3 + x^2 / (5 + ..))), off by x^10 / 9.8e6 of
+// itself, up to 1; (e - 1) / (e + 1) with e = exp(2 |x|) beyond, where nothing cancels.  Scores are rarely that close to
+// the cap, so that most warps take one side.
+__device__ __forceinline__ float tanh1(float x) {
+    const float y = x * x;
+    float n = x * fmaf(y, y + 105.f, 945.f), d = fmaf(y, fmaf(y, 15.f, 420.f), 945.f);
+    if (y > 1.f) {
+        const float e = ex2(fminf(fabsf(x), 16.f) * (2.f * kLog2e));
+        n = copysignf(e - 1.f, x);
+        d = e + 1.f;
+    }
+    return __fdividef(n, d);
+}
+
+}  // namespace bct

@@ -1,0 +1,736 @@
+// Attention over the 8-bit cache on the sm_100a tensor path: bfloat16 calls with many rows to a unit (prompts).
+//
+// The formulas are those of bct_qcache_attend.cu; a unit's rows are its (token, head) pairs, token-major.  A CTA has 256 of
+// them, two tiles of 128, and goes through the slots that they see, 128 at a time:
+//     S = Q K^T  (M = 128 rows, N = 128 slots)     P = exp2(S - m), fp16, into S's place     O += P V  (N = d)
+// as tcgen05.mma with fp32 accumulators in tensor memory; P is read from there.  Warps 0-3 and 4-7 form P of the two
+// tiles, a row to a thread; warps 8-11 turn codes into fp16 operands (exactly), which both tiles use; warp 12 issues the
+// products, so that one tile's products run while the other's P is formed.
+//  - A query is fp16 after a power of two that brings its row below 2^15, which is exact (terms below 2^-39 of the row's
+//    largest apart), and codes are fp16 exactly: scores are exact products with fp32 sums.
+//  - The running maximum m moves only when a score passes it by 2^6: P is 2^9 p, below 2^15, and O is rarely scaled.
+//  - The blocks' value scales multiply P, relative to one that follows the loudest block of a tile (vref below), so that one
+//    product covers four blocks; the accumulators are in units of it.
+// With few rows the slots are dealt to several CTAs, whose results qc_prompt_join_kernel joins.  The weights come from a
+// second pass in the transposed form, S^T = K Q^T with the slots in the lanes: with each row's maximum and sum known, a
+// thread adds up exp2(S - m) / sum over the rows, in their order, without atomics.
+//
+// Every wait is bounded; a timeout ends the work and fills what the CTA writes with NaN.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "bct_device.cuh"
+#include "bct_internal.h"
+#include "bct_qcache.h"
+#include "bct_qcache.cuh"
+#include "bct_qcache_math.cuh"
+#include "bct_tc.cuh"
+
+namespace bct {
+namespace {
+
+constexpr int kQpRows = 256;                 // rows of a CTA
+constexpr int kQpSlots = 128;                // slots of a tile
+constexpr int kQpThreads = 13 * 32;
+constexpr int kQpHalf = 128 * 128;           // bytes of 128 rows x 64 fp16 columns
+constexpr float kQpPScale = 512.f;           // 2^9
+constexpr float kQpSlack = 6.f;              // m may be passed by as many powers of two
+
+#define QP_UMMA "tcgen05.mma.cta_group::1.kind::f16 "
+// D (+)= A B over four steps of 16, both K-major (32 bytes a step)
+__device__ __forceinline__ void umma4_kk(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accum) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q " QP_UMMA "[%0], %1, %2, %3, p;\n\t"
+        "setp.eq.b32 p, 0, 0;\n\t"
+        "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t"
+        "@q " QP_UMMA "[%0], a, b, %3, p;\n\t"
+        "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t"
+        "@q " QP_UMMA "[%0], a, b, %3, p;\n\t"
+        "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t"
+        "@q " QP_UMMA "[%0], a, b, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accum)
+        : "memory");
+}
+// D (+)= A B over four steps with A (fp16 pairs, 8 columns a step) in tensor memory, B MN-major (16 rows of 128 bytes a step)
+__device__ __forceinline__ void umma4_tm(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, bool accum) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q " QP_UMMA "[%0], [%1], %2, %3, p;\n\t"
+        "setp.eq.b32 p, 0, 0;\n\t"
+        "add.s32 a, %1, 8;\n\tadd.s64 b, %2, 128;\n\t"
+        "@q " QP_UMMA "[%0], [a], b, %3, p;\n\t"
+        "add.s32 a, %1, 16;\n\tadd.s64 b, %2, 256;\n\t"
+        "@q " QP_UMMA "[%0], [a], b, %3, p;\n\t"
+        "add.s32 a, %1, 24;\n\tadd.s64 b, %2, 384;\n\t"
+        "@q " QP_UMMA "[%0], [a], b, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"((uint32_t)accum)
+        : "memory");
+}
+__device__ __forceinline__ void commit_warp(uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
+        : "memory");
+}
+// fp16 x fp16 -> fp32
+__host__ __device__ constexpr uint32_t idesc_f16(uint32_t M, uint32_t N, bool b_mn_major) {
+    return instr_desc_mn(M, N, false, b_mn_major) & ~((7u << 7) | (7u << 10));
+}
+__device__ __forceinline__ void tmem_ld32_raw(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+// until loads are complete; names the destination so that no use of it moves ahead
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                   "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                   "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+                 :
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    tmem_st16(taddr, r);
+    tmem_st16(taddr + 16, r + 16);
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// two floats to an instruction
+__device__ __forceinline__ uint64_t f2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 f2_of(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// A bounded wait of a warp.
+__device__ __forceinline__ void qp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    if (!mbar_wait_abortable(bar, parity & 1, abort_flag)) *abort_flag = 1;
+    __syncwarp();
+}
+// Where 16-byte chunk c (8 fp16 columns) of a row stands in an operand tile: halves of 64 columns, 128-byte swizzle.
+__device__ __forceinline__ int operand_at(int row, int c) { return (c >> 3) * kQpHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4); }
+
+// 128 threads turn a tile of codes into an fp16 operand: raw[i] are the 16-byte pieces of this thread.
+template <int D>
+struct Codes {
+    static constexpr int kPer = D / 16;            // 16-byte pieces of a slot
+    static constexpr int kRaw = kPer;              // pieces of a thread: 128 slots x kPer / 128
+    uint4 raw[kRaw];
+    __device__ __forceinline__ void load(const int8_t* unit, int slot0, int end, int t) {
+#pragma unroll
+        for (int i = 0; i < kRaw; ++i) {
+            const int slot = slot0 + i * (128 / kPer) + t / kPer;
+            raw[i] = make_uint4(0, 0, 0, 0);
+            if (slot < end) raw[i] = *reinterpret_cast<const uint4*>(unit + (size_t)slot * D + (t % kPer) * 16);
+        }
+    }
+    __device__ __forceinline__ void store(unsigned char* tile, int t) const {
+#pragma unroll
+        for (int i = 0; i < kRaw; ++i) {
+            const int row = i * (128 / kPer) + t / kPer, c = t % kPer * 2;
+            const uint32_t w[4] = {raw[i].x ^ 0x80808080u, raw[i].y ^ 0x80808080u, raw[i].z ^ 0x80808080u, raw[i].w ^ 0x80808080u};
+            uint4 o[2];
+            o[0] = make_uint4(pair_of(w[0], 0x4140), pair_of(w[0], 0x4342), pair_of(w[1], 0x4140), pair_of(w[1], 0x4342));
+            o[1] = make_uint4(pair_of(w[2], 0x4140), pair_of(w[2], 0x4342), pair_of(w[3], 0x4140), pair_of(w[3], 0x4342));
+            // (the lanes of the second half of a row begin with the other chunk: no two lanes at the same banks)
+            const bool second = (c >> 3) != 0;
+            *reinterpret_cast<uint4*>(tile + operand_at(row, c + second)) = second ? o[1] : o[0];
+            *reinterpret_cast<uint4*>(tile + operand_at(row, c + !second)) = second ? o[0] : o[1];
+        }
+    }
+};
+
+template <int D>
+struct QpSmem {
+    static constexpr int kTile = D / 64 * kQpHalf;    // an operand tile of 128 rows
+    static constexpr int q = 0;                       // two
+    static constexpr int k = q + 2 * kTile;           // two stages
+    static constexpr int v = k + 2 * kTile;           // two stages
+    static constexpr int bars = v + 2 * kTile;
+    static constexpr int total = bars + 256 + 1024;   // (1024 to align the base)
+};
+
+template <int D, bool CAP>
+__global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend a, const QcPrompt pr) {
+    using L = QpSmem<D>;
+    extern __shared__ unsigned char qp_smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(qp_smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bars);
+    uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6;   // [2] by stages
+    uint64_t *s_full = bars + 8, *p_full = bars + 10, *o_full = bars + 12;                   // [2] by tiles of rows
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 14);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 15);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    // (unit, rows, split): the rows that see most come first
+    const unsigned units = (unsigned)(a.c.B * a.c.Hkv);
+    unsigned idx = blockIdx.x;
+    const unsigned split = idx % pr.splits;
+    idx /= pr.splits;
+    const unsigned unit = idx % units;
+    const int64_t r0 = (int64_t)(pr.tiles - 1 - (int)(idx / units)) * kQpRows;
+    const int b = (int)(unit / a.c.Hkv), h = (int)(unit - b * a.c.Hkv);
+    pdl_wait();
+    const Sees sees = sees_of(a, b);
+    const int64_t valid = (int64_t)sees.n * a.G;                        // rows of valid tokens
+    const int rows = (int)max((int64_t)0, min((int64_t)kQpRows, valid - r0));
+    const int lim_max = rows > 0 ? sees(r0 + rows - 1) : 0, lim_min = rows > 0 ? sees(r0) : 0;
+    const int all_tiles = (lim_max + kQpSlots - 1) / kQpSlots;
+    const int lo = (int)((int64_t)all_tiles * split / pr.splits), hi = (int)((int64_t)all_tiles * (split + 1) / pr.splits);
+    const int N = hi - lo, subs = rows > 128 ? 2 : 1;
+    const int8_t* kp = a.c.codes[0] + (size_t)unit * a.c.C * D;
+    const int8_t* vp = a.c.codes[1] + (size_t)unit * a.c.C * D;
+
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&k_full[i], 4);
+            mbar_init(&k_empty[i], 1);
+            mbar_init(&v_full[i], 4);
+            mbar_init(&v_empty[i], 1);
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_full[i], 4);
+            mbar_init(&o_full[i], 1);
+        }
+        *abort_flag = 0;
+        fence_mbar_init_cluster();
+    }
+    if (warp == 12) tmem_alloc(tmem_slot, 512);
+
+    const int sub = warp >> 2;                                          // of warps 0-7: the tile of rows
+    const int my_row = (warp & 3) * 32 + lane;
+    const int64_t r = r0 + sub * 128 + my_row;
+    float factor = 0.f;                                                 // what the row's products are multiplied with
+    int lim = 0;
+    if (warp < 8) {
+        const bool real = r < valid;
+        lim = real ? sees(r) : 0;
+        // the row, as an operand and for the pass that forms the weights
+        const __nv_bfloat16* src = row_of<__nv_bfloat16>(a, a.q, b, h, real ? r : 0);
+        uint4 w[D / 8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            w[i] = real ? reinterpret_cast<const uint4*>(src)[i] : make_uint4(0, 0, 0, 0);
+            const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max(top, max((u[j] << 16) & 0x7fffffffu, u[j] & 0x7fff0000u));
+        }
+        float by;
+        row_scale(__uint_as_float(top), &by, &factor);
+        factor = row_factor(a, factor);
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            float x[8];
+            Chunk<__nv_bfloat16>::unpack(w[i], x);
+            const uint4 o = make_uint4(half2_bits(x[0] * by, x[1] * by), half2_bits(x[2] * by, x[3] * by),
+                                       half2_bits(x[4] * by, x[5] * by), half2_bits(x[6] * by, x[7] * by));
+            *reinterpret_cast<uint4*>(smem + L::q + sub * L::kTile + operand_at(my_row, i)) = o;
+            if (pr.q16 != nullptr && split == 0 && real) *reinterpret_cast<uint4*>(pr.q16 + ((size_t)unit * a.R + r) * D + i * 8) = o;
+        }
+        if (pr.q16 != nullptr && split == 0 && real) pr.q_factor[(size_t)unit * a.R + r] = factor;
+    }
+    fence_proxy_async_smem();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_open();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 12) {
+        // =========================== products ===========================
+        constexpr uint32_t id_s = idesc_f16(128, 128, false), id_o = idesc_f16(128, D, true);
+        const DescKind dk(smem_desc(0, 16, 1024)), dmn(smem_desc(0, kQpHalf, 1024));
+        const uint32_t base16 = desc_addr16(smem_u32(smem));
+        auto scores = [&](int n, int g) {
+            const uint32_t qa = base16 + (L::q + g * L::kTile) / 16, ka = base16 + (L::k + (n & 1) * L::kTile) / 16;
+#pragma unroll
+            for (int hf = 0; hf < D / 64; ++hf)
+                umma4_kk(tmem + g * 128, dk.at(qa + hf * (kQpHalf / 16)), dk.at(ka + hf * (kQpHalf / 16)), id_s, hf > 0);
+            commit_warp(&s_full[g]);
+            if (g == subs - 1) commit_warp(&k_empty[n & 1]);
+        };
+        if (N > 0) {
+            qp_wait(&k_full[0], 0, abort_flag);
+            tc_fence_after();
+            for (int g = 0; g < subs; ++g) scores(0, g);
+        }
+        for (int n = 0; n < N; ++n) {
+            const uint32_t va = base16 + (L::v + (n & 1) * L::kTile) / 16;
+            for (int g = 0; g < subs; ++g) {
+                if (g == 0) qp_wait(&v_full[n & 1], n >> 1, abort_flag);
+                qp_wait(&p_full[g], n, abort_flag);
+                tc_fence_after();
+                umma4_tm(tmem + 256 + g * D, tmem + g * 128, dmn.at(va), id_o, n > 0);
+                umma4_tm(tmem + 256 + g * D, tmem + g * 128 + 32, dmn.at(va + 512), id_o, true);
+                commit_warp(&o_full[g]);
+                if (g == subs - 1) commit_warp(&v_empty[n & 1]);
+                if (n + 1 < N) {
+                    if (g == 0) {
+                        qp_wait(&k_full[(n + 1) & 1], (n + 1) >> 1, abort_flag);
+                        tc_fence_after();
+                    }
+                    scores(n + 1, g);      // (after the product that reads P from its place)
+                }
+            }
+        }
+    } else if (warp >= 8) {
+        // =========================== codes to operands ===========================
+        const int t = tid - 256;
+        Codes<D> k, v;
+        if (N > 0) {
+            k.load(kp, lo * kQpSlots, lim_max, t);
+            v.load(vp, lo * kQpSlots, lim_max, t);
+        }
+        for (int n = 0; n < N; ++n) {
+            const int st = n & 1;
+            if (n >= 2) qp_wait(&k_empty[st], (n >> 1) - 1, abort_flag);
+            k.store(smem + L::k + st * L::kTile, t);
+            if (n + 1 < N) k.load(kp, (lo + n + 1) * kQpSlots, lim_max, t);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&k_full[st]);
+            if (n >= 2) qp_wait(&v_empty[st], (n >> 1) - 1, abort_flag);
+            v.store(smem + L::v + st * L::kTile, t);
+            if (n + 1 < N) v.load(vp, (lo + n + 1) * kQpSlots, lim_max, t);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&v_full[st]);
+        }
+    } else {
+        // =========================== softmax ===========================
+        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);      // (32 lanes further in bits 16 and up)
+        const uint32_t s_col = lanes + sub * 128, o_col = lanes + 256 + sub * D;
+        const float* ksp = a.c.scale[0] + (size_t)unit * a.c.NB;
+        const float* vsp = a.c.scale[1] + (size_t)unit * a.c.NB;
+        const int blocks = (lim_max + kQcBlock - 1) / kQcBlock;
+        float m = -INFINITY, vref = 0.f, vmost = 0.f;
+        uint64_t l2[2] = {0, 0};
+        if (sub < subs) {
+            for (int n = 0; n < N; ++n) {
+                const int slot0 = (lo + n) * kQpSlots;
+                float ks[4], vs[4], vt = 0.f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int blk = slot0 / kQcBlock + c;
+                    ks[c] = blk < blocks ? ksp[blk] * factor : 0.f;
+                    vs[c] = blk < blocks ? vsp[blk] : 0.f;
+                    vt = fmaxf(vt, vs[c]);
+                }
+                // the scale that the values are relative to follows the loudest block, not below 2^-60 of the loudest so far
+                float by_v = 1.f;
+                vmost = fmaxf(vmost, vt);
+                if (vt > vref || vt < vref * 0.015625f) {
+                    const float to = fmaxf(vt, vmost * 8.67361738e-19f);
+                    if (vref > 0.f && to > 0.f) by_v = vref / to;
+                    if (to > 0.f) vref = to;
+                }
+                const float inv_v = vref > 0.f ? kQpPScale / vref : 0.f;
+                const bool masked = slot0 + kQpSlots > lim_min;
+                qp_wait(&s_full[sub], n, abort_flag);
+                tc_fence_after();
+
+                float top = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t x[32];
+                    tmem_ld32_raw(s_col + 32 * c, x);
+                    tmem_wait_ld(x);
+                    float most = -INFINITY;
+                    if (masked) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) most = fmaxf(most, slot0 + 32 * c + j < lim ? __uint_as_float(x[j]) : -INFINITY);
+                        if (slot0 + 32 * c >= lim) most = -INFINITY;
+                        else most *= ks[c];
+                    } else {
+                        float part[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) part[j & 3] = fmaxf(part[j & 3], __uint_as_float(x[j]));
+                        most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * ks[c];
+                    }
+                    top = fmaxf(top, most);
+                }
+                if constexpr (CAP) top = top == -INFINITY ? top : a.cap * kLog2e * tanh1(top);
+                float by = by_v;
+                if (top > m + kQpSlack || (m == -INFINITY && top > m)) {
+                    const float keep = ex2(m - top);           // (0 the first time)
+                    by *= keep;
+                    l2[0] = mul2(l2[0], f2(keep, keep));
+                    l2[1] = mul2(l2[1], f2(keep, keep));
+                    m = top;
+                }
+                if (n > 0 && __any_sync(0xffffffffu, by != 1.f)) {
+                    qp_wait(&o_full[sub], n - 1, abort_flag);
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t x[32];
+                        tmem_ld32_raw(o_col + c, x);
+                        tmem_wait_ld(x);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * by);
+                        tmem_st32(o_col + c, x);
+                    }
+                }
+                const float m0 = m == -INFINITY ? 0.f : m;
+                const uint64_t nm = f2(-m0, -m0);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t x[32], p[16];
+                    tmem_ld32_raw(s_col + 32 * c, x);
+                    tmem_wait_ld(x);
+                    const uint64_t k2 = f2(ks[c], ks[c]), v2 = f2(vs[c] * inv_v, vs[c] * inv_v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        uint64_t s = f2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
+                        if constexpr (CAP) {
+                            const float2 y = f2_of(mul2(s, k2));
+                            const float cl = a.cap * kLog2e;
+                            s = fma2(f2(tanh1(y.x), tanh1(y.y)), f2(cl, cl), nm);
+                        } else {
+                            s = fma2(s, k2, nm);
+                        }
+                        float2 e = f2_of(s);
+                        e.x = ex2(e.x);
+                        e.y = ex2(e.y);
+                        float2 y;
+                        if (masked) {                        // hidden slots give nothing, whatever their scales are
+                            const int left = lim - (slot0 + 32 * c + 2 * j);
+                            if (left < 1) e.x = 0.f;
+                            if (left < 2) e.y = 0.f;
+                            y = f2_of(mul2(f2(e.x, e.y), v2));
+                            if (left < 1) y.x = 0.f;
+                            if (left < 2) y.y = 0.f;
+                        } else {
+                            y = f2_of(mul2(f2(e.x, e.y), v2));
+                        }
+                        l2[j & 1] = add2(l2[j & 1], f2(e.x, e.y));
+                        p[j] = half2_bits(y.x, y.y);
+                    }
+                    tmem_st16(s_col + 16 * c, p);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[sub]);
+            }
+        }
+        // results: the accumulators are in units of vref / 2^9
+        if (N > 0 && sub < subs) {
+            qp_wait(&o_full[sub], N - 1, abort_flag);
+            tc_fence_after();
+        }
+        const float2 la = f2_of(add2(l2[0], l2[1]));
+        float l = la.x + la.y;
+        if (lim == 0) l = 0.f;                                // (a padding row in a tile that others see through)
+        if (*abort_flag) l = __uint_as_float(0x7fffffffu);
+        float mul = vref * (1.f / kQpPScale);
+        const bool there = r < a.R, mine = N > 0 && sub < subs;
+        const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+        if (pr.splits == 1) mul = l == l ? mul * inv : l;
+        const int64_t at = ((int64_t)unit * a.R + r) * pr.splits + split;
+        __nv_bfloat16* to = const_cast<__nv_bfloat16*>(row_of<__nv_bfloat16>(a, a.out, b, h, there ? r : 0));
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+            uint32_t x[32];
+            if (mine) {                                       // (the whole warp)
+                tmem_ld32_raw(o_col + c, x);
+                tmem_wait_ld(x);
+            }
+            float y[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) y[j] = mine && (l != 0.f) ? __uint_as_float(x[j]) * mul : 0.f;
+            if (there && pr.splits == 1) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) *reinterpret_cast<uint4*>(to + c + j) = Chunk<__nv_bfloat16>::pack(y + j);
+            } else if (there) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 4)
+                    *reinterpret_cast<float4*>(a.part_o + at * D + c + j) = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
+            }
+            __syncwarp();
+        }
+        if (there) {
+            if (pr.splits == 1) a.ml[(size_t)unit * a.R + r] = make_float2(m, inv);
+            else a.part_ml[at] = make_float2(m, l);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 12) tmem_dealloc(tmem, 512);
+}
+
+// Joins the splits of a row: a warp to a row.
+template <int D>
+__global__ void __launch_bounds__(256) qc_prompt_join_kernel(const QcAttend a, const QcPrompt pr) {
+    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), rows = (int64_t)a.c.B * a.c.Hkv * a.R;
+    const int lane = threadIdx.x & 31;
+    pdl_wait();
+    pdl_open();
+    if (row >= rows) return;
+    const int64_t unit = row / a.R, r = row - unit * a.R;
+    const float2* ml = a.part_ml + row * pr.splits;
+    float m = -INFINITY, l = 0.f;
+    for (int i = 0; i < pr.splits; ++i) m = fmaxf(m, ml[i].x);
+    for (int i = 0; i < pr.splits; ++i) l += m == -INFINITY ? ml[i].y : ml[i].y * ex2(ml[i].x - m);
+    const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+    constexpr int kN = D / 32;
+    float y[kN] = {};
+    for (int i = 0; i < pr.splits; ++i) {
+        const float by = ml[i].x == -INFINITY ? 0.f : ex2(ml[i].x - m) * inv;
+#pragma unroll
+        for (int j = 0; j < kN; ++j) y[j] = fmaf(a.part_o[(row * pr.splits + i) * D + lane * kN + j], by, y[j]);
+    }
+    const int b = (int)(unit / a.c.Hkv), h = (int)(unit - (int64_t)b * a.c.Hkv);
+    __nv_bfloat16* to = const_cast<__nv_bfloat16*>(row_of<__nv_bfloat16>(a, a.out, b, h, r)) + lane * kN;
+#pragma unroll
+    for (int j = 0; j < kN; j += 2)
+        *reinterpret_cast<uint32_t*>(to + j) = l == l ? Chunk<__nv_bfloat16>::pack2(y[j], y[j + 1]) : 0x7fff7fffu;
+    if (lane == 0) a.ml[row] = make_float2(m, inv);
+}
+
+// ---- the weights ------------------------------------------------------------------------------------------------
+constexpr int kQwtThreads = 13 * 32;
+template <int D>
+struct QwtSmem {
+    static constexpr int kTile = D / 64 * kQpHalf;
+    static constexpr int k = 0;
+    static constexpr int q = k + kTile;               // two stages
+    static constexpr int rows = q + 2 * kTile;        // two stages of 64 x {factor, factor, -log, -log} by pairs of rows, and limits
+    static constexpr int kRowBytes = 128 * 8 + 128 * 4;
+    static constexpr int bars = rows + 2 * kRowBytes;
+    static constexpr int total = bars + 128 + 1024;
+};
+
+template <int D, bool CAP>
+__global__ void __launch_bounds__(kQwtThreads, 2) qc_prompt_weights_kernel(const QcAttend a, const QcPrompt pr) {
+    using L = QwtSmem<D>;
+    extern __shared__ unsigned char qp_smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(qp_smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bars);
+    uint64_t *q_full = bars, *q_empty = bars + 2, *s_full = bars + 4, *s_empty = bars + 6;   // [2]
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 8);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 9);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const unsigned units = (unsigned)(a.c.B * a.c.Hkv);
+    const unsigned unit = blockIdx.x % units;
+    const int slot0 = (int)(blockIdx.x / units) * kQpSlots;             // the slots that most rows see come first
+    const int b = (int)(unit / a.c.Hkv), h = (int)(unit - b * a.c.Hkv);
+    pdl_wait();
+    const Sees sees = sees_of(a, b);
+    if (slot0 >= sees.held || sees.n == 0) return;
+    const int64_t valid = (int64_t)sees.n * a.G;
+    const int i0 = max(0, slot0 - (sees.held - sees.n));                // the first token that sees the first slot
+    const int64_t first = (int64_t)i0 * a.G / 128 * 128;
+    const int N = (int)((valid - first + 127) / 128);
+
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], 4);
+            mbar_init(&q_empty[i], 5);                                  // the products and the four warps that read the rows' terms
+            mbar_init(&s_full[i], 1);
+            mbar_init(&s_empty[i], 4);
+        }
+        *abort_flag = 0;
+        fence_mbar_init_cluster();
+    }
+    if (warp == 12) tmem_alloc(tmem_slot, 256);
+    if (warp >= 8 && warp < 12) {
+        Codes<D> k;
+        k.load(a.c.codes[0] + (size_t)unit * a.c.C * D, slot0, sees.held, tid - 256);
+        k.store(smem + L::k, tid - 256);
+    }
+    fence_proxy_async_smem();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    float sum = 0.f;
+
+    if (warp == 12) {
+        constexpr uint32_t id_s = idesc_f16(128, 128, false);
+        const DescKind dk(smem_desc(0, 16, 1024));
+        const uint32_t base16 = desc_addr16(smem_u32(smem));
+        for (int n = 0; n < N; ++n) {
+            const int st = n & 1;
+            qp_wait(&q_full[st], n >> 1, abort_flag);
+            if (n >= 2) qp_wait(&s_empty[st], (n >> 1) - 1, abort_flag);
+            tc_fence_after();
+            const uint32_t ka = base16 + L::k / 16, qa = base16 + (L::q + st * L::kTile) / 16;
+#pragma unroll
+            for (int hf = 0; hf < D / 64; ++hf)
+                umma4_kk(tmem + st * 128, dk.at(ka + hf * (kQpHalf / 16)), dk.at(qa + hf * (kQpHalf / 16)), id_s, hf > 0);
+            commit_warp(&s_full[st]);
+            commit_warp(&q_empty[st]);
+        }
+    } else if (warp >= 8) {
+        // =========================== queries and their rows' terms ===========================
+        const int t = tid - 256;
+        constexpr int kChunks = D / 8;                                  // 16-byte pieces of a row
+        for (int n = 0; n <= N; ++n) {
+            if (n < N) {
+                const int st = n & 1;
+                if (n >= 2) qp_wait(&q_empty[st], (n >> 1) - 1, abort_flag);
+                unsigned char* tile = smem + L::q + st * L::kTile;
+                const int64_t r0 = first + (int64_t)n * 128;
+#pragma unroll
+                for (int i = 0; i < kChunks; ++i) {
+                    const int row = i * (128 / kChunks) + t / kChunks, c = t % kChunks;
+                    const bool real = r0 + row < valid;
+                    cp_async16_zfill(smem_u32(tile + operand_at(row, c)),
+                                     pr.q16 + ((size_t)unit * a.R + (real ? r0 + row : 0)) * D + c * 8, real);
+                }
+                cp_async_commit();
+                // a thread's row: rows that add nothing have the logarithm infinity
+                const int64_t r = r0 + t;
+                float f = 0.f, nl = -INFINITY;
+                int lim = 0;
+                if (r < valid) {
+                    const float2 ml = a.ml[(size_t)unit * a.R + r];
+                    f = pr.q_factor[(size_t)unit * a.R + r];
+                    lim = sees(r);
+                    if (ml.y != 0.f) nl = __log2f(ml.y) - ml.x;
+                }
+                float* rows = reinterpret_cast<float*>(smem + L::rows + st * L::kRowBytes);
+                rows[(t >> 1) * 4 + (t & 1)] = f;
+                rows[(t >> 1) * 4 + 2 + (t & 1)] = nl;
+                reinterpret_cast<int*>(rows + 256)[t] = lim;
+            }
+            if (n > 0) {
+                if (n < N) cp_async_wait_but_one();
+                else cp_async_wait_all();
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&q_full[(n - 1) & 1]);
+            }
+        }
+    } else {
+        // =========================== a slot to a thread; warps 0-3 and 4-7 take the row tiles in turn ===========================
+        const int g = warp >> 2, my = (warp & 3) * 32 + lane, slot = slot0 + my;
+        const int blk = slot / kQcBlock;
+        const float ks = slot < sees.held ? a.c.scale[0][(size_t)unit * a.c.NB + blk] : 0.f;
+        const uint64_t k2 = f2(ks, ks);
+        const uint32_t s_col = tmem + ((uint32_t)(warp & 3) << 21) + g * 128;
+        uint64_t acc[2] = {0, 0};
+        for (int n = g; n < N; n += 2) {
+            const float* rows = reinterpret_cast<const float*>(smem + L::rows + g * L::kRowBytes);
+            const int* lims = reinterpret_cast<const int*>(rows + 256);
+            const bool masked = slot0 + kQpSlots > sees(first + (int64_t)n * 128);
+            qp_wait(&q_full[g], n >> 1, abort_flag);                    // (the rows' terms)
+            qp_wait(&s_full[g], n >> 1, abort_flag);
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t x[32];
+                tmem_ld32_raw(s_col + 32 * c, x);
+                tmem_wait_ld(x);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float4 t = *reinterpret_cast<const float4*>(rows + (16 * c + j) * 4);
+                    uint64_t s = mul2(f2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), k2);
+                    if constexpr (CAP) {
+                        const float2 y = f2_of(mul2(s, f2(t.x, t.y)));
+                        const float cl = a.cap * kLog2e;
+                        s = fma2(f2(tanh1(y.x), tanh1(y.y)), f2(cl, cl), f2(t.z, t.w));
+                    } else {
+                        s = fma2(s, f2(t.x, t.y), f2(t.z, t.w));
+                    }
+                    float2 e = f2_of(s);
+                    e.x = ex2(e.x);
+                    e.y = ex2(e.y);
+                    if (masked) {
+                        if (slot >= lims[32 * c + 2 * j]) e.x = 0.f;
+                        if (slot >= lims[32 * c + 2 * j + 1]) e.y = 0.f;
+                    }
+                    acc[j & 1] = add2(acc[j & 1], f2(e.x, e.y));
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&s_empty[g]);
+                mbar_arrive(&q_empty[g]);
+            }
+        }
+        const float2 x = f2_of(add2(acc[0], acc[1]));
+        sum = x.x + x.y;
+    }
+    tc_fence_before();
+    __syncthreads();
+    float* share = reinterpret_cast<float*>(smem + L::rows);
+    if (warp >= 4 && warp < 8) share[tid - 128] = sum;
+    __syncthreads();
+    if (warp < 4 && slot0 + tid < sees.held) {
+        sum += share[tid];
+        if (*abort_flag) sum = __uint_as_float(0x7fffffffu);
+        a.c.weight[(size_t)unit * a.c.C + slot0 + tid] += sum;
+    }
+    if (warp == 12) tmem_dealloc(tmem, 256);
+}
+
+template <int D, bool CAP>
+cudaError_t prompt_with(const QcAttend& a, const QcPrompt& pr, cudaStream_t s) {
+    static std::atomic<uint64_t> done[2];
+    const int64_t units = (int64_t)a.c.B * a.c.Hkv;
+    cudaError_t e = allow_smem(qc_prompt_kernel<D, CAP>, QpSmem<D>::total, &done[0]);
+    if (e != cudaSuccess) return e;
+    e = pdl_launch(qc_prompt_kernel<D, CAP>, (unsigned)(units * pr.tiles * pr.splits), kQpThreads, QpSmem<D>::total, s, a, pr);
+    if (e != cudaSuccess) return e;
+    if (pr.splits > 1 && (e = pdl_launch(qc_prompt_join_kernel<D>, (unsigned)((units * a.R + 7) / 8), 256, 0, s, a, pr)) != cudaSuccess)
+        return e;
+    if (!a.accumulate) return cudaSuccess;
+    if ((e = allow_smem(qc_prompt_weights_kernel<D, CAP>, QwtSmem<D>::total, &done[1])) != cudaSuccess) return e;
+    return pdl_launch(qc_prompt_weights_kernel<D, CAP>, (unsigned)(units * ((a.c.C + kQpSlots - 1) / kQpSlots)), kQwtThreads,
+                      QwtSmem<D>::total, s, a, pr);
+}
+
+}  // namespace
+
+cudaError_t qc_prompt(const QcAttend& a, const QcPrompt& pr, cudaStream_t s) {
+    if (a.c.D == 128) return a.cap > 0.f ? prompt_with<128, true>(a, pr, s) : prompt_with<128, false>(a, pr, s);
+    return a.cap > 0.f ? prompt_with<64, true>(a, pr, s) : prompt_with<64, false>(a, pr, s);
+}
+
+}  // namespace bct

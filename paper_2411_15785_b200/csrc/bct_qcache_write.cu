@@ -17,6 +17,7 @@
 #include "bct_device.cuh"
 #include "bct_internal.h"
 #include "bct_qcache.h"
+#include "bct_qcache.cuh"
 
 namespace bct {
 namespace {
@@ -27,60 +28,97 @@ constexpr int kQwRows = kQcBlock / 4;
 // round((x + lo) / s) in -127..127, ties to the even code; |lo| is at most half an ulp of x.  q is off by one at most
 // where x / s is next to a half; r = x - q s is exact there (multiples of s's ulp, or of half of it where q is 0 or 1,
 // below s), and so are the differences from half a step that decide.
-__device__ __forceinline__ float code_of(float x, float lo, float s, float inv) {
+__device__ __forceinline__ int exact_code(float x, float lo, float s, float inv) {
     float q = rintf(x * inv);
     const float r = fmaf(-q, s, x), half = 0.5f * s;
     const bool odd = (static_cast<int>(q) & 1) != 0;
     const float up = (r - half) + lo, down = (r + half) + lo;
     if (up > 0.f || (up == 0.f && odd)) q += 1.f;
     else if (down < 0.f || (down == 0.f && odd)) q -= 1.f;
-    return fminf(fmaxf(q, -127.f), 127.f);
+    return static_cast<int>(fminf(fmaxf(q, -127.f), 127.f));
+}
+template <int N>
+__device__ __forceinline__ uint32_t packed(const uint32_t (&u)[N]) {   // the low bytes
+    if constexpr (N == 4) return __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
+    else return __byte_perm(u[0], u[1], 0x0040) & 0xffffu;
+}
+// N codes as the bytes of a word.  Adding 1.5 2^23 rounds x / s to an integer, whose low byte is the code; *far is the
+// largest distance from it: only next to a half can it be the wrong one (x inv is off by 127.5 2^-24 = 7.6e-6 at most).
+template <int N>
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[N], float inv, float* far) {
+    constexpr float kMagic = 12582912.f;
+    uint32_t u[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float m = fmaf(x[i], inv, kMagic);
+        u[i] = __float_as_uint(m);
+        *far = fmaxf(*far, fabsf(fmaf(x[i], inv, kMagic - m)));
+    }
+    return packed(u);
+}
+template <int N>
+__device__ __forceinline__ uint32_t exact_codes(const float (&x)[N], const float (&lo)[N], float s, float inv) {
+    uint32_t u[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) u[i] = (uint32_t)exact_code(x[i], lo[i], s, inv);
+    return packed(u);
+}
+constexpr float kNextToHalf = 0.49999f;
+// N codes divided by a power of two, ties to the even one
+template <int N>
+__device__ __forceinline__ uint32_t shrunk(uint32_t w, float by) {
+    uint32_t out = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) out |= (uint32_t)(uint8_t)(int8_t)(int)rintf((float)(int8_t)(w >> (8 * i)) * by) << (8 * i);
+    return out;
 }
 
-// The scale of a block that takes values up to amax, and the factor by which the codes it holds are multiplied.
-__device__ __forceinline__ float grown(float s, double amax, bool fresh, float* shrink) {
+// The scale of a block that takes values up to amax, and the factor by which the codes it holds are multiplied.  64 bits
+// only where they decide: in a block that starts afresh from products of codes and scales, and where a scale grows.
+template <typename F>
+__device__ __forceinline__ float grown(float s, F amax, bool fresh, float* shrink) {
     *shrink = 1.f;
-    if (fresh || s == 0.f)
-        return amax > 0. ? fmaxf((float)(amax / 127.), 1.17549435e-38f) : (float)amax;   // (a NaN stays one)
+    if (fresh || s == 0.f) return amax > F(0) ? fmaxf((float)(amax / F(127)), 1.17549435e-38f) : (float)amax;   // (a NaN stays one)
+    if ((float)amax < 127.4f * s) return s;
     const double top = 127.5 * (double)s;
-    if (!(amax > top)) return amax == amax ? s : (float)amax;
+    if (!((double)amax > top)) return amax == amax ? s : (float)amax;
     int e;
-    const double m = frexp(amax / top, &e);
+    const double m = frexp((double)amax / top, &e);
     if (!(m > 0.5)) --e;
     *shrink = ldexpf(1.f, -e);
     return ldexpf(s, e);
 }
 
+// N features of a lane, as loaded
 template <typename T, int N>
-struct Row;   // N features of a lane
-template <int N>
-struct Row<float, N> {
-    float x[N];
-    __device__ __forceinline__ void load(const float* p) {
-        if constexpr (N == 4) {
-            const float4 w = *reinterpret_cast<const float4*>(p);
-            x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w;
-        } else {
-            const float2 w = *reinterpret_cast<const float2*>(p);
-            x[0] = w.x, x[1] = w.y;
-        }
-    }
-};
-template <int N>
-struct Row<__nv_bfloat16, N> {
-    float x[N];
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
-        uint32_t w[N / 2];
-        if constexpr (N == 4) {
+struct Row {
+    static constexpr int kWords = N * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (kWords == 4) {
+            const uint4 u = *reinterpret_cast<const uint4*>(p);
+            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+        } else if constexpr (kWords == 2) {
             const uint2 u = *reinterpret_cast<const uint2*>(p);
             w[0] = u.x, w[1] = u.y;
         } else {
             w[0] = *reinterpret_cast<const uint32_t*>(p);
         }
+    }
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ void values(float (&x)[N]) const {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = __uint_as_float(w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
         }
     }
 };
@@ -92,43 +130,38 @@ __device__ __forceinline__ uint32_t load_codes(const int8_t* p) {
     else return *reinterpret_cast<const uint16_t*>(p);
 }
 template <int N>
-__device__ __forceinline__ void store_codes(int8_t* p, const float* c) {
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) w |= (uint32_t)(uint8_t)(int8_t)(int)c[i] << (8 * i);
+__device__ __forceinline__ void store_codes(int8_t* p, uint32_t w) {
     if constexpr (N == 4) *reinterpret_cast<uint32_t*>(p) = w;
     else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w;
 }
 __device__ __forceinline__ float code_at(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
 
-// Largest magnitude of a plane's four warps (64 bits: a code times a scale has 31); a NaN or an infinity in any of them
-// makes it a NaN.
-__device__ __forceinline__ double plane_amax(double mine, bool odd_one, double (*share)[4], int plane, int part) {
+// The larger one, or a NaN if either is one; an infinity becomes one at the end.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+// Largest magnitude of a plane's four warps; a NaN or an infinity in any of them makes it a NaN.
+__device__ __forceinline__ float plane_amax(float mine, float (*share)[4], int plane, int part) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mine = fmax(mine, __shfl_xor_sync(0xffffffffu, mine, o));
-    if (__any_sync(0xffffffffu, odd_one)) mine = nan("");
+    for (int o = 16; o > 0; o >>= 1) mine = max_nan(mine, __shfl_xor_sync(0xffffffffu, mine, o));
     if ((threadIdx.x & 31) == 0) share[plane][part] = mine;
     __syncthreads();
-    double amax = 0.;
-    bool is_nan = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const double m = share[plane][i];
-        is_nan |= m != m;
-        amax = fmax(amax, m);
-    }
-    return is_nan ? nan("") : amax;
+    const float amax = max_nan(max_nan(share[plane][0], share[plane][1]), max_nan(share[plane][2], share[plane][3]));
+    return amax <= 3.402823466e38f ? amax : __uint_as_float(0x7fffffffu);
 }
-__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) <= 3.402823466e38f); }
 
 // ---- append -----------------------------------------------------------------------------------------------------
 // A CTA per (sequence, head, block of the cache that the new tokens may touch).  The last CTA of a sequence moves its
 // length on: all of them have read it by then.
 template <typename T, int D>
-__global__ void __launch_bounds__(kQwThreads) qc_append_kernel(const QcAppend a) {
+__global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? 6 : 4) qc_append_kernel(const QcAppend a) {
     constexpr int kN = D / 32;
-    __shared__ double share[2][4];
-    const int w = blockIdx.x % a.W, unit = blockIdx.x / a.W, b = unit / a.c.Hkv, h = unit - b * a.c.Hkv;
+    __shared__ float share[2][4];
+    pdl_wait();
+    // the heads of a block of tokens run side by side: they stand side by side in memory
+    const int h = blockIdx.x % a.c.Hkv, bw = blockIdx.x / a.c.Hkv, w = bw % a.W, b = bw / a.W, unit = b * a.c.Hkv + h;
     const int C = a.c.C;
     const int held = min(max(a.c.state[b], 0), C), seen = a.c.state[a.c.B + b];
     const int64_t want = a.lens == nullptr ? a.T : min((int64_t)max(a.lens[b], 0), a.T);
@@ -141,38 +174,58 @@ __global__ void __launch_bounds__(kQwThreads) qc_append_kernel(const QcAppend a)
         float* scale = a.c.scale[plane] + (size_t)unit * a.c.NB + blk;
         const T* x = static_cast<const T*>(a.x[plane]);
         Row<T, kN> row[kQwRows];
-        float top = 0.f;
-        bool odd_one = false;
 #pragma unroll
         for (int i = 0; i < kQwRows; ++i) {
             const int slot = lo + part * kQwRows + i;
-            if (slot < first || slot >= last) continue;
-            row[i].load(x + (((size_t)b * a.T + (slot - held)) * a.c.Hkv + h) * D + lane * kN);
-#pragma unroll
-            for (int j = 0; j < kN; ++j) {
-                top = fmaxf(top, fabsf(row[i].x[j]));
-                odd_one |= not_finite(row[i].x[j]);
-            }
+            if (slot >= first && slot < last) row[i].load(x + (((size_t)b * a.T + (slot - held)) * a.c.Hkv + h) * D + lane * kN);
+            else row[i].clear();
         }
         const float old = *scale;
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < kQwRows; ++i) {
+            float y[kN];
+            row[i].values(y);
+#pragma unroll
+            for (int j = 0; j < kN; ++j) top = max_nan(top, fabsf(y[j]));
+        }
         // (all have read the old scale when its barrier lets them go)
-        const double amax = plane_amax(top, odd_one, share, plane, part);
+        const float amax = plane_amax(top, share, plane, part);
         float shrink;
         const float s = grown(old, amax, first == lo, &shrink), inv = s > 0.f ? 1.f / s : 0.f;
+        unsigned again = 0;                                 // rows with a value next to a half
 #pragma unroll
         for (int i = 0; i < kQwRows; ++i) {
             const int slot = lo + part * kQwRows + i;
-            int8_t* p = codes + (size_t)slot * D + lane * kN;
-            float c[kN];
-            if (slot >= first && slot < last) {
+            float y[kN], far = 0.f;
+            row[i].values(y);
+            const uint32_t c = s > 0.f ? codes_of(y, inv, &far) : 0;
+            if (far > kNextToHalf) again |= 1u << i;
+            if (slot >= first && slot < last) store_codes<kN>(codes + (size_t)slot * D + lane * kN, c);
+        }
+#pragma unroll 1
+        for (; again != 0; again &= again - 1) {
+            const int slot = lo + part * kQwRows + __ffs(again) - 1;
+            if (slot < first || slot >= last || !(s > 0.f)) continue;
+            Row<T, kN> one;
+            one.load(x + (((size_t)b * a.T + (slot - held)) * a.c.Hkv + h) * D + lane * kN);
+            float y[kN];
+            one.values(y);
+            const float none[kN] = {};
+            store_codes<kN>(codes + (size_t)slot * D + lane * kN, exact_codes(y, none, s, inv));
+        }
+        if (shrink != 1.f) {                                // (what stands behind the new end too: a block's codes have one scale)
+            uint32_t held_codes[kQwRows];
 #pragma unroll
-                for (int j = 0; j < kN; ++j) c[j] = s > 0.f ? code_of(row[i].x[j], 0.f, s, inv) : 0.f;
-                store_codes<kN>(p, c);
-            } else if (slot < first && shrink != 1.f) {
-                const uint32_t word = load_codes<kN>(p);
+            for (int i = 0; i < kQwRows; ++i) {
+                const int slot = lo + part * kQwRows + i;
+                if (slot < C && (slot < first || slot >= last)) held_codes[i] = load_codes<kN>(codes + (size_t)slot * D + lane * kN);
+            }
 #pragma unroll
-                for (int j = 0; j < kN; ++j) c[j] = rintf(code_at(word, j) * shrink);
-                store_codes<kN>(p, c);
+            for (int i = 0; i < kQwRows; ++i) {
+                const int slot = lo + part * kQwRows + i;
+                if (slot < C && (slot < first || slot >= last))
+                    store_codes<kN>(codes + (size_t)slot * D + lane * kN, shrunk<kN>(held_codes[i], shrink));
             }
         }
         if (part == 0 && lane == 0) *scale = s;
@@ -184,9 +237,8 @@ __global__ void __launch_bounds__(kQwThreads) qc_append_kernel(const QcAppend a)
             }
         }
     }
-    __syncthreads();   // (all of this CTA have read the sequence's state)
+    __syncthreads();   // all of this CTA have read the sequence's state (have it: their branches went by it)
     if (threadIdx.x == 0) {
-        __threadfence();
         int* done = reinterpret_cast<int*>(a.c.state + 2 * a.c.B + b);
         if (atomicAdd(done, 1) == a.W * a.c.Hkv - 1) {
             a.c.state[b] = held + n;
@@ -197,8 +249,6 @@ __global__ void __launch_bounds__(kQwThreads) qc_append_kernel(const QcAppend a)
 }
 
 // ---- eviction ---------------------------------------------------------------------------------------------------
-constexpr int kQsThreads = 1024;
-constexpr int kQsWarps = kQsThreads / 32;
 constexpr int kQsBins = 2048;          // 11 bits of a key at a time
 constexpr int kQsKeys = 40960;         // keys that are kept in shared memory; those behind are formed anew
 
@@ -209,39 +259,39 @@ __device__ __forceinline__ uint32_t worth_key(float w, bool stays) {
     return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
 }
 
-// Inclusive sum over the CTA's threads in order, and the total.  share: kQsWarps + 1 words.
-__device__ __forceinline__ int cta_scan(int x, int* share, int* total) {
+// Sum of the words of the warps before this thread's, and of all.  share: two sets of 32 words, used in turn, so that one
+// barrier is enough; `x` is the same in all of a warp.
+template <int WARPS>
+__device__ __forceinline__ uint32_t warps_before(uint32_t x, uint32_t (*share)[32], int* turn, uint32_t* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t* s = share[*turn];
+    *turn ^= 1;
+    if (lane == 0) s[warp] = x;
+    __syncthreads();
+    uint32_t y = lane < WARPS ? s[lane] : 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
+    for (int o = 1; o < WARPS; o <<= 1) {
+        const uint32_t z = __shfl_up_sync(0xffffffffu, y, o);
+        if (lane >= o) y += z;
     }
-    __syncthreads();
-    if (lane == 31) share[warp] = x;
-    __syncthreads();
-    if (warp == 0) {
-        int y = share[lane];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int z = __shfl_up_sync(0xffffffffu, y, o);
-            if (lane >= o) y += z;
-        }
-        share[lane] = y;
-    }
-    __syncthreads();
-    *total = share[kQsWarps - 1];
-    return x + (warp ? share[warp - 1] : 0);
+    *total = __shfl_sync(0xffffffffu, y, WARPS - 1);
+    const uint32_t before = __shfl_sync(0xffffffffu, y, warp ? warp - 1 : 0);
+    return warp ? before : 0;
 }
 
-// A CTA per unit finds the n least keys: 11 + 11 + 10 bits of the n-th one, by counting; then one pass in the slots'
-// order, in which a warp is a block, lists the blocks with holes and the slots that move.
-__global__ void __launch_bounds__(kQsThreads) qc_select_kernel(const QcEvict a) {
+// A CTA per unit finds the n least keys: 11 + 11 + 10 bits of the n-th one, by counting (one slot alone: the least pair
+// of key and slot); then one pass in the slots' order, in which a warp is a block, lists the blocks with holes and the
+// slots that move.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) qc_select_kernel(const QcEvict a) {
+    constexpr int kWarps = THREADS / 32, kBinsEach = kQsBins / THREADS;
     extern __shared__ uint32_t keys[];
     __shared__ int bins[kQsBins];
-    __shared__ int share[kQsWarps + 1];
-    __shared__ int found[2];
-    const int unit = blockIdx.x, b = unit / a.c.Hkv, C = a.c.C, tid = threadIdx.x, lane = tid & 31;
+    __shared__ uint32_t share[2][32];
+    __shared__ unsigned long long least[kWarps];
+    __shared__ int found[3];
+    const int unit = blockIdx.x, b = unit / a.c.Hkv, C = a.c.C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_wait();
     const int held = min(max(a.c.state[b], 0), C), from = a.c.state[a.c.B + b] - a.recent;
     const int n = held - a.keep;
     if (n <= 0) {
@@ -250,134 +300,214 @@ __global__ void __launch_bounds__(kQsThreads) qc_select_kernel(const QcEvict a) 
     }
     const float* weight = a.c.weight + (size_t)unit * C;
     const int32_t* position = a.c.position + (size_t)unit * C;
+    int4* blocks = a.blocks + (size_t)unit * a.max_blocks;
+    int32_t* movers = a.movers + (size_t)unit * a.max_moves;
+    if (tid < 2 && a.keep < C) a.cut_scale[2 * unit + tid] = a.c.scale[tid][(size_t)unit * a.c.NB + a.keep / kQcBlock];
+
+    if (n == 1) {
+        unsigned long long best = ~0ull;
+#pragma unroll 4
+        for (int j = tid; j < held; j += THREADS) {
+            const unsigned long long k = ((unsigned long long)worth_key(weight[j], position[j] >= from) << 32) | (unsigned)j;
+            best = k < best ? k : best;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const unsigned long long k = __shfl_xor_sync(0xffffffffu, best, o);
+            best = k < best ? k : best;
+        }
+        if (lane == 0) least[warp] = best;
+        __syncthreads();
+        if (tid != 0) return;
+        for (int i = 1; i < kWarps; ++i) best = least[i] < best ? least[i] : best;
+        const int j = (int)(unsigned)best;
+        const bool moves = j < a.keep;         // or the slot behind the new end is itself the one
+        if (moves) {
+            movers[0] = held - 1;
+            blocks[0] = make_int4(j / kQcBlock, 0, (int)(1u << (j % kQcBlock)), 0);
+        }
+        a.n_out[unit] = 1;
+        a.n_blocks[unit] = moves;
+        return;
+    }
+
     const int kept_keys = min(held, kQsKeys);
-    for (int j = tid; j < kept_keys; j += kQsThreads) keys[j] = worth_key(weight[j], position[j] >= from);
+#pragma unroll 4
+    for (int j = tid; j < kept_keys; j += THREADS) keys[j] = worth_key(weight[j], position[j] >= from);
     auto key_at = [&](int j) { return j < kQsKeys ? keys[j] : worth_key(weight[j], position[j] >= from); };
 
-    uint32_t prefix = 0, mask = 0;
-    int left = n;                          // of the keys that share the prefix, so many go
-#pragma unroll
+    uint32_t prefix = 0, mask = 0, total;
+    int left = n, turn = 0;                // of the keys that share the prefix, so many go
+    bool ties = false;                     // and others with the very same key stay
+#pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
-        bins[tid] = bins[tid + kQsThreads] = 0;
+#pragma unroll
+        for (int i = 0; i < kBinsEach; ++i) bins[tid + i * THREADS] = 0;
         __syncthreads();
-        for (int j = tid; j < held; j += kQsThreads) {
+        for (int j = tid; j < held; j += THREADS) {
             const uint32_t k = key_at(j);
             if ((k & mask) == prefix) atomicAdd(&bins[(k >> shift) & ((1u << width) - 1)], 1);
         }
         __syncthreads();
-        const int c0 = bins[2 * tid], c1 = bins[2 * tid + 1];
-        int total;
-        const int upto = cta_scan(c0 + c1, share, &total), before = upto - c0 - c1;
+        int mine[kBinsEach], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kBinsEach; ++i) sum += mine[i] = bins[kBinsEach * tid + i];
+        int upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        upto += (int)warps_before<kWarps>((uint32_t)__shfl_sync(0xffffffffu, upto, 31), share, &turn, &total);
+        int before = upto - sum;
         if (before < left && left <= upto) {
-            const bool second = left > before + c0;
-            found[0] = 2 * tid + second;
-            found[1] = left - before - (second ? c0 : 0);
+#pragma unroll
+            for (int i = 0; i < kBinsEach; ++i) {
+                if (before < left && left <= before + mine[i]) {
+                    found[0] = kBinsEach * tid + i;
+                    found[1] = left - before;
+                    found[2] = mine[i];
+                }
+                before += mine[i];
+            }
         }
         __syncthreads();
         prefix |= (uint32_t)found[0] << shift;
         left = found[1];
+        ties = found[2] != left;
         mask |= ((1u << width) - 1) << shift;
         __syncthreads();
     }
 
-    int4* blocks = a.blocks + (size_t)unit * a.max_blocks;
-    int32_t* movers = a.movers + (size_t)unit * a.max_moves;
-    int ties = 0, n_holes = 0, n_movers = 0, n_blocks = 0;
-    for (int base = 0; base < held; base += kQsThreads) {
+    int tied = 0, n_holes = 0, n_movers = 0, n_blocks = 0;
+    const unsigned below = (1u << lane) - 1u;
+    for (int base = 0; base < held; base += THREADS) {
         const int j = base + tid;
         const uint32_t k = j < held ? key_at(j) : 0xffffffffu;
         const bool tie = j < held && k == prefix;
-        int total;
-        const int tie_no = ties + cta_scan(tie, share, &total) - 1;
-        ties += total;
-        const bool out = j < held && (k < prefix || (tie && tie_no < left));
-        const bool hole = out && j < a.keep, mover = !out && j >= a.keep && j < held;
-        // what comes before, of both kinds: a slot is one of them at most
-        const int no = cta_scan(hole ? 1 : mover ? 1 << 16 : 0, share, &total);
-        if (mover) movers[n_movers + (no >> 16) - 1] = j;
-        const unsigned holes = __ballot_sync(0xffffffffu, hole);
-        const int hole_no = n_holes + (__shfl_sync(0xffffffffu, no, 31) & 0xffff) - __popc(holes);
-        n_holes += total & 0xffff;
-        n_movers += total >> 16;
-        const int blk_no = n_blocks + cta_scan(lane == 0 && holes != 0, share, &total) - 1;
-        if (lane == 0 && holes != 0) blocks[blk_no] = make_int4(j / kQcBlock, hole_no, (int)holes, 0);
-        n_blocks += total;
+        bool out = j < held && k <= prefix;
+        if (ties) {                        // the lower slots go
+            const unsigned t = __ballot_sync(0xffffffffu, tie);
+            const int no = tied + (int)warps_before<kWarps>(__popc(t), share, &turn, &total) + __popc(t & below);
+            if (tie) out = no < left;
+            tied += (int)total;
+        }
+        const unsigned holes = __ballot_sync(0xffffffffu, out && j < a.keep);
+        const unsigned moves = __ballot_sync(0xffffffffu, !out && j >= a.keep && j < held);
+        // of all warps, up to 1024 of each, 32 blocks
+        const uint32_t before = warps_before<kWarps>(__popc(holes) | (__popc(moves) << 11) | ((holes != 0) << 22), share, &turn, &total);
+        if ((moves >> lane) & 1) movers[n_movers + ((before >> 11) & 0x7ff) + __popc(moves & below)] = j;
+        if (lane == 0 && holes != 0)
+            blocks[n_blocks + (before >> 22)] = make_int4(j / kQcBlock, n_holes + (int)(before & 0x7ff), (int)holes, 0);
+        n_holes += total & 0x7ff;
+        n_movers += (total >> 11) & 0x7ff;
+        n_blocks += total >> 22;
     }
-    if (tid < 2 && a.keep < C) a.cut_scale[2 * unit + tid] = a.c.scale[tid][(size_t)unit * a.c.NB + a.keep / kQcBlock];
     if (tid == 0) {
         a.n_out[unit] = n;
         a.n_blocks[unit] = n_blocks;
     }
 }
 
-// A CTA per block with holes: the slots that move in come with the codes and scale of where they were.
+// A warp per block with holes and plane: the slots that move in come with the codes and scale of where they were, eight
+// rows in flight.  (Four warps to a block, as an append has, would be idle where a block has a few holes.)
+constexpr int kQmRows = 8;
 template <int D>
-__global__ void __launch_bounds__(kQwThreads) qc_move_kernel(const QcEvict a, int ctas) {
+__global__ void __launch_bounds__(kQwThreads) qc_move_kernel(const QcEvict a, int per_unit) {
     constexpr int kN = D / 32;
-    __shared__ double share[2][4];
-    const int no = blockIdx.x % ctas, unit = blockIdx.x / ctas, C = a.c.C;
-    if (no == 0 && unit % a.c.Hkv == 0 && threadIdx.x == 0 && a.n_out[unit] > 0) a.c.state[unit / a.c.Hkv] = a.keep;
-    if (no >= a.n_blocks[unit]) return;
-    const int4 e = a.blocks[(size_t)unit * a.max_blocks + no];
+    const int lane = threadIdx.x & 31, plane = (threadIdx.x >> 5) & 1, C = a.c.C;
+    const int64_t item = (int64_t)blockIdx.x * (kQwThreads / 64) + (threadIdx.x >> 6);
+    const int unit = (int)(item / per_unit), no = (int)(item - (int64_t)unit * per_unit);
+    if (unit >= a.c.B * a.c.Hkv) return;
+    pdl_wait();
+    const int n_blocks = a.n_blocks[unit];
+    const int4 e = a.max_blocks > 0 ? a.blocks[(size_t)unit * a.max_blocks + no] : make_int4(0, 0, 0, 0);
+    if (no == 0 && plane == 0 && unit % a.c.Hkv == 0 && lane == 0 && a.n_out[unit] > 0) a.c.state[unit / a.c.Hkv] = a.keep;
+    if (no >= n_blocks) return;
     const int lo = e.x * kQcBlock;
     const unsigned holes = (unsigned)e.z;
-    const int32_t* movers = a.movers + (size_t)unit * a.max_moves + e.y;
-    const int plane = threadIdx.x >> 7, part = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
-    int8_t* codes = a.c.codes[plane] + (size_t)unit * C * D;
+    const int count = __popc(holes);
+    int8_t* codes = a.c.codes[plane] + (size_t)unit * C * D + lane * kN;
     float* scales = a.c.scale[plane] + (size_t)unit * a.c.NB;
-    // (the block that the new end cuts takes slots in and gives some away: its scale is the one before)
-    auto scale_of = [&](int src) { return src / kQcBlock == a.keep / kQcBlock ? a.cut_scale[2 * unit + plane] : scales[src / kQcBlock]; };
     const int kept = min(kQcBlock, a.keep - lo);
-    const bool fresh = holes == (kept == kQcBlock ? 0xffffffffu : (1u << kept) - 1u);
+    const unsigned all = kept == kQcBlock ? 0xffffffffu : (1u << kept) - 1u;
+    const bool fresh = holes == all;
 
-    uint32_t word[kQwRows];
-    float from[kQwRows];
-    double amax = 0.;
-    bool odd_one = false;
-#pragma unroll
-    for (int i = 0; i < kQwRows; ++i) {
-        const int at = part * kQwRows + i;
-        if (!((holes >> at) & 1)) continue;
-        const int src = movers[__popc(holes & ((1u << at) - 1u))];
-        from[i] = scale_of(src);
-        word[i] = load_codes<kN>(codes + (size_t)src * D + lane * kN);
-        float top = 0.f;
-#pragma unroll
-        for (int j = 0; j < kN; ++j) top = fmaxf(top, fabsf(code_at(word[i], j)));
-        amax = fmax(amax, (double)top * (double)from[i]);
-        odd_one |= not_finite(from[i]);
-    }
+    // lane i: the i-th hole, the slot that moves there and its scale (the block that the new end cuts takes slots in and
+    // gives some away: its scale is the one before)
+    const int src = lane < count ? a.movers[(size_t)unit * a.max_moves + e.y + lane] : 0;
+    int dst = lo;
+    for (unsigned m = holes, i = 0; m != 0; m &= m - 1, ++i)
+        if (i == (unsigned)lane) dst = lo + __ffs(m) - 1;
     const float old = scales[e.x];
-    amax = plane_amax(amax, odd_one, share, plane, part);
+    uint32_t word[kQmRows];
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int i = 0; i < kQmRows; ++i)
+            if (i0 + i < count) word[i] = load_codes<kN>(codes + (size_t)__shfl_sync(0xffffffffu, src, i0 + i) * D);
+    };
+    load(0);
+    float from = 0.f;
+    if (lane < count) from = src / kQcBlock == a.keep / kQcBlock ? a.cut_scale[2 * unit + plane] : scales[src / kQcBlock];
+    double amax = 0.;
+    for (int i0 = 0;;) {
+        // row by row: the largest |code| times its scale, exact in 64 bits
+#pragma unroll
+        for (int i = 0; i < kQmRows; ++i) {
+            if (i0 + i < count) {
+                int top = 0;
+#pragma unroll
+                for (int j = 0; j < kN; ++j) top = max(top, abs((int)(int8_t)(word[i] >> (8 * j))));
+                amax = fmax(amax, (double)top * (double)__shfl_sync(0xffffffffu, from, i0 + i));
+            }
+        }
+        if ((i0 += kQmRows) >= count) break;
+        load(i0);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) amax = fmax(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if (__any_sync(0xffffffffu, !(fabsf(from) <= 3.402823466e38f))) amax = nan("");
     float shrink;
     const float s = grown(old, amax, fresh, &shrink), inv = s > 0.f ? 1.f / s : 0.f;
+    if (count > kQmRows) load(0);
+    for (int i0 = 0;;) {
 #pragma unroll
-    for (int i = 0; i < kQwRows; ++i) {
-        const int at = part * kQwRows + i, slot = lo + at;
-        if (at >= kept) continue;
-        int8_t* p = codes + (size_t)slot * D + lane * kN;
-        float c[kN];
-        if ((holes >> at) & 1) {
+        for (int i = 0; i < kQmRows; ++i) {
+            if (i0 + i < count) {
+                const float f = __shfl_sync(0xffffffffu, from, i0 + i);
+                const int to = __shfl_sync(0xffffffffu, dst, i0 + i);
+                float x[kN], rest[kN], far = 0.f;
 #pragma unroll
-            for (int j = 0; j < kN; ++j) {
-                const float code = code_at(word[i], j), x = code * from[i];
-                c[j] = s > 0.f ? code_of(x, fmaf(code, from[i], -x), s, inv) : 0.f;
+                for (int j = 0; j < kN; ++j) {
+                    const float code = code_at(word[i], j);
+                    x[j] = code * f;
+                    rest[j] = fmaf(code, f, -x[j]);
+                }
+                uint32_t c = s > 0.f ? codes_of(x, inv, &far) : 0;
+                if (far > kNextToHalf && s > 0.f) c = exact_codes(x, rest, s, inv);
+                store_codes<kN>(codes + (size_t)to * D, c);
             }
-            store_codes<kN>(p, c);
-        } else if (shrink != 1.f) {
-            const uint32_t held = load_codes<kN>(p);
+        }
+        if ((i0 += kQmRows) >= count) break;
+        load(i0);
+    }
+    if (shrink != 1.f) {
+        const unsigned stay = all & ~holes;
+        for (int i0 = 0; i0 < kept; i0 += kQmRows) {
 #pragma unroll
-            for (int j = 0; j < kN; ++j) c[j] = rintf(code_at(held, j) * shrink);
-            store_codes<kN>(p, c);
+            for (int i = 0; i < kQmRows; ++i)
+                if ((stay >> (i0 + i)) & 1) word[i] = load_codes<kN>(codes + (size_t)(lo + i0 + i) * D);
+#pragma unroll
+            for (int i = 0; i < kQmRows; ++i)
+                if ((stay >> (i0 + i)) & 1) store_codes<kN>(codes + (size_t)(lo + i0 + i) * D, shrunk<kN>(word[i], shrink));
         }
     }
-    if (part == 0 && lane == 0) scales[e.x] = s;
-    if (plane == 0 && part == 0 && ((holes >> lane) & 1)) {
-        const int src = movers[__popc(holes & ((1u << lane) - 1u))];
+    if (lane == 0) scales[e.x] = s;
+    if (plane == 0 && lane < count) {
         const size_t u = (size_t)unit * C;
-        a.c.weight[u + lo + lane] = a.c.weight[u + src];
-        a.c.position[u + lo + lane] = a.c.position[u + src];
+        a.c.weight[u + dst] = a.c.weight[u + src];
+        a.c.position[u + dst] = a.c.position[u + src];
     }
 }
 
@@ -385,28 +515,27 @@ __global__ void __launch_bounds__(kQwThreads) qc_move_kernel(const QcEvict a, in
 
 cudaError_t qc_append(const QcAppend& a, int dtype, cudaStream_t s) {
     const unsigned grid = (unsigned)((int64_t)a.c.B * a.c.Hkv * a.W);
-    if (dtype == BCT_BF16) {
-        if (a.c.D == 128) qc_append_kernel<__nv_bfloat16, 128><<<grid, kQwThreads, 0, s>>>(a);
-        else qc_append_kernel<__nv_bfloat16, 64><<<grid, kQwThreads, 0, s>>>(a);
-    } else {
-        if (a.c.D == 128) qc_append_kernel<float, 128><<<grid, kQwThreads, 0, s>>>(a);
-        else qc_append_kernel<float, 64><<<grid, kQwThreads, 0, s>>>(a);
-    }
-    return cudaGetLastError();
+    if (dtype == BCT_BF16)
+        return a.c.D == 128 ? pdl_launch(qc_append_kernel<__nv_bfloat16, 128>, grid, kQwThreads, 0, s, a)
+                            : pdl_launch(qc_append_kernel<__nv_bfloat16, 64>, grid, kQwThreads, 0, s, a);
+    return a.c.D == 128 ? pdl_launch(qc_append_kernel<float, 128>, grid, kQwThreads, 0, s, a)
+                        : pdl_launch(qc_append_kernel<float, 64>, grid, kQwThreads, 0, s, a);
 }
 
 cudaError_t qc_evict(const QcEvict& a, cudaStream_t s) {
     const int units = a.c.B * a.c.Hkv;
+    // many units fill the SMs with small CTAs, whose barriers cost less; few units need their threads
+    const bool small = units >= 296;
+    const auto kernel = small ? qc_select_kernel<256> : qc_select_kernel<1024>;
     const int smem = (a.c.C < kQsKeys ? a.c.C : kQsKeys) * 4;
-    cudaError_t e = cudaFuncSetAttribute(qc_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kQsKeys * 4);
-    if (e != cudaSuccess) return e;
-    qc_select_kernel<<<units, kQsThreads, smem, s>>>(a);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    const int ctas = a.max_blocks > 0 ? a.max_blocks : 1;
-    const unsigned grid = (unsigned)((int64_t)units * ctas);
-    if (a.c.D == 128) qc_move_kernel<128><<<grid, kQwThreads, 0, s>>>(a, ctas);
-    else qc_move_kernel<64><<<grid, kQwThreads, 0, s>>>(a, ctas);
-    return cudaGetLastError();
+    cudaError_t e;
+    static std::atomic<uint64_t> done[2];
+    if (smem > 32768 && (e = allow_smem(kernel, kQsKeys * 4, &done[small])) != cudaSuccess) return e;
+    if ((e = pdl_launch(kernel, units, small ? 256 : 1024, smem, s, a)) != cudaSuccess) return e;
+    const int per_unit = a.max_blocks > 0 ? a.max_blocks : 1;
+    const unsigned grid = (unsigned)(((int64_t)units * per_unit + kQwThreads / 64 - 1) / (kQwThreads / 64));
+    return a.c.D == 128 ? pdl_launch(qc_move_kernel<128>, grid, kQwThreads, 0, s, a, per_unit)
+                        : pdl_launch(qc_move_kernel<64>, grid, kQwThreads, 0, s, a, per_unit);
 }
 
 }  // namespace bct
