@@ -176,8 +176,20 @@ __device__ __forceinline__ void to_scores(float (&s)[2][4], float mul0, float mu
     for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] *= i & 1 ? mul1 : mul0;
     if (cap > 0.f) {
         const float to = cap * kLog2e;
+        float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = to * tanh1(s[i >> 2][i & 3]);
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(s[i >> 2][i & 3]));
+        if (__any_sync(0xffffffffu, top > 1.f)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = to * tanh_any(s[i >> 2][i & 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const float2 y = f2_of(mul2(tanh_near2(f2(s[i >> 2][i & 3], s[i >> 2][(i & 3) + 1])), f2(to, to)));
+                s[i >> 2][i & 3] = y.x;
+                s[i >> 2][(i & 3) + 1] = y.y;
+            }
+        }
     }
 }
 template <typename T, int D, int NT, int TERMS>

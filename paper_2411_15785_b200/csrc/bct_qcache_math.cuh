@@ -69,10 +69,37 @@ __device__ __forceinline__ float row_factor(const QcAttend& a, float mul) {
     return a.cap > 0.f ? mul * (a.scale / a.cap) : mul * (a.scale * kLog2e);
 }
 
-// tanh: the fifth convergent of Lambert's continued fraction x / (1 + x^2 / (3 + x^2 / (5 + ..))), off by x^10 / 9.8e6 of
-// itself, up to 1; (e - 1) / (e + 1) with e = exp(2 |x|) beyond, where nothing cancels.  Scores are rarely that close to
-// the cap, so that most warps take one side.
-__device__ __forceinline__ float tanh1(float x) {
+// two floats to an instruction
+__device__ __forceinline__ uint64_t f2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 f2_of(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// tanh: up to 1 the fifth convergent of Lambert's continued fraction x / (1 + x^2 / (3 + x^2 / (5 + ..))), off by
+// x^10 / 9.8e6 of itself; beyond, (e - 1) / (e + 1) with e = exp(2 |x|), where nothing cancels.  Scores are rarely that
+// close to the cap, so that warps ask once for many of them (near: all are up to 1) and take two at a time.
+__device__ __forceinline__ float tanh_any(float x) {
     const float y = x * x;
     float n = x * fmaf(y, y + 105.f, 945.f), d = fmaf(y, fmaf(y, 15.f, 420.f), 945.f);
     if (y > 1.f) {
@@ -81,6 +108,12 @@ __device__ __forceinline__ float tanh1(float x) {
         d = e + 1.f;
     }
     return __fdividef(n, d);
+}
+__device__ __forceinline__ uint64_t tanh_near2(uint64_t x) {
+    const uint64_t y = mul2(x, x);
+    const uint64_t n = mul2(x, fma2(y, add2(y, f2(105.f, 105.f)), f2(945.f, 945.f)));
+    const float2 d = f2_of(fma2(y, fma2(y, f2(15.f, 15.f), f2(420.f, 420.f)), f2(945.f, 945.f)));
+    return mul2(n, f2(__fdividef(1.f, d.x), __fdividef(1.f, d.y)));
 }
 
 }  // namespace bct

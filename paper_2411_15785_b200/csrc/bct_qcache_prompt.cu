@@ -4,7 +4,7 @@
 // them, two tiles of 128, and goes through the slots that they see, 128 at a time:
 //     S = Q K^T  (M = 128 rows, N = 128 slots)     P = exp2(S - m), fp16, into S's place     O += P V  (N = d)
 // as tcgen05.mma with fp32 accumulators in tensor memory; P is read from there.  Warps 0-3 and 4-7 form P of the two
-// tiles, a row to a thread; warps 8-11 turn codes into fp16 operands (exactly), which both tiles use; warp 12 issues the
+// tiles, a row to a thread; warps 8-10 turn codes into fp16 operands (exactly), which both tiles use; warp 11 issues the
 // products, so that one tile's products run while the other's P is formed.
 //  - A query is fp16 after a power of two that brings its row below 2^15, which is exact (terms below 2^-39 of the row's
 //    largest apart), and codes are fp16 exactly: scores are exact products with fp32 sums.
@@ -20,6 +20,8 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "bct_device.cuh"
 #include "bct_internal.h"
 #include "bct_qcache.h"
@@ -32,7 +34,8 @@ namespace {
 
 constexpr int kQpRows = 256;                 // rows of a CTA
 constexpr int kQpSlots = 128;                // slots of a tile
-constexpr int kQpThreads = 13 * 32;
+constexpr int kQpThreads = 12 * 32;         // (three warps to a quarter of an SM: 168 registers, a row of S stays in them)
+constexpr int kQpMakers = 96;               // threads that turn codes into operands
 constexpr int kQpHalf = 128 * 128;           // bytes of 128 rows x 64 fp16 columns
 constexpr float kQpPScale = 512.f;           // 2^9
 constexpr float kQpSlack = 6.f;              // m may be passed by as many powers of two
@@ -105,6 +108,23 @@ __device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[32]) {
                  :
                  : "memory");
 }
+// The 128 columns of this thread's lane, 32 at a time: use(c, x) for c = 0..3, the next ones on their way meanwhile.  (A
+// loop: with all of it unrolled, masks and caps in every copy, the kernels missed the instruction cache and took twice as
+// long.)
+template <typename F>
+__device__ __forceinline__ void by_chunks(uint32_t taddr, F use) {
+    uint32_t x[32], y[32];
+    tmem_ld32_raw(taddr, x);
+#pragma unroll 1
+    for (int c = 0; c < 4; c += 2) {
+        tmem_wait_ld(x);
+        tmem_ld32_raw(taddr + 32 * c + 32, y);
+        use(c, x);
+        tmem_wait_ld(y);
+        if (c == 0) tmem_ld32_raw(taddr + 64, x);
+        use(c + 1, y);
+    }
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -118,31 +138,34 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// two floats to an instruction
-__device__ __forceinline__ uint64_t f2(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
+// tanh of 32 numbers, some of them beyond 1 (rare: out of the way, through local memory)
+__device__ __noinline__ void tanh_far(uint64_t* s) {
+#pragma unroll 1
+    for (int j = 0; j < 16; ++j) {
+        const float2 y = f2_of(s[j]);
+        s[j] = f2(tanh_any(y.x), tanh_any(y.y));
+    }
 }
-__device__ __forceinline__ float2 f2_of(uint64_t v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
+// The capped scores of 32 products that have their factors, in powers of two, less something: cl tanh(s) + less[j].
+template <typename F>
+__device__ __forceinline__ void capped(uint64_t (&s)[16], uint64_t cl, F less) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const float2 y = f2_of(s[j]);
+        top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
+    }
+    if (__any_sync(0xffffffffu, top > 1.f)) {
+        uint64_t far[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) far[j] = s[j];
+        tanh_far(far);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = fma2(far[j], cl, less(j));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = fma2(tanh_near2(s[j]), cl, less(j));
+    }
 }
 
 // A bounded wait of a warp.
@@ -153,32 +176,36 @@ __device__ __forceinline__ void qp_wait(uint64_t* bar, uint32_t parity, volatile
 // Where 16-byte chunk c (8 fp16 columns) of a row stands in an operand tile: halves of 64 columns, 128-byte swizzle.
 __device__ __forceinline__ int operand_at(int row, int c) { return (c >> 3) * kQpHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4); }
 
-// 128 threads turn a tile of codes into an fp16 operand: raw[i] are the 16-byte pieces of this thread.
+// kQpMakers threads turn a tile of codes into an fp16 operand: raw[i] are the 16-byte pieces of a thread.
 template <int D>
 struct Codes {
-    static constexpr int kPer = D / 16;            // 16-byte pieces of a slot
-    static constexpr int kRaw = kPer;              // pieces of a thread: 128 slots x kPer / 128
+    static constexpr int kPer = D / 16, kAll = 128 * kPer;              // 16-byte pieces of a slot, of the tile
+    static constexpr int kRaw = (kAll + kQpMakers - 1) / kQpMakers;
     uint4 raw[kRaw];
     __device__ __forceinline__ void load(const int8_t* unit, int slot0, int end, int t) {
+        const int8_t* from = unit + (size_t)slot0 * D;
+        const int most = min(128, end - slot0) * kPer;
 #pragma unroll
         for (int i = 0; i < kRaw; ++i) {
-            const int slot = slot0 + i * (128 / kPer) + t / kPer;
+            const int piece = i * kQpMakers + t;
             raw[i] = make_uint4(0, 0, 0, 0);
-            if (slot < end) raw[i] = *reinterpret_cast<const uint4*>(unit + (size_t)slot * D + (t % kPer) * 16);
+            if (piece < most) raw[i] = *reinterpret_cast<const uint4*>(from + piece * 16);
         }
     }
     __device__ __forceinline__ void store(unsigned char* tile, int t) const {
 #pragma unroll
         for (int i = 0; i < kRaw; ++i) {
-            const int row = i * (128 / kPer) + t / kPer, c = t % kPer * 2;
+            const int piece = i * kQpMakers + t, row = piece / kPer, c = piece % kPer * 2;
             const uint32_t w[4] = {raw[i].x ^ 0x80808080u, raw[i].y ^ 0x80808080u, raw[i].z ^ 0x80808080u, raw[i].w ^ 0x80808080u};
             uint4 o[2];
             o[0] = make_uint4(pair_of(w[0], 0x4140), pair_of(w[0], 0x4342), pair_of(w[1], 0x4140), pair_of(w[1], 0x4342));
             o[1] = make_uint4(pair_of(w[2], 0x4140), pair_of(w[2], 0x4342), pair_of(w[3], 0x4140), pair_of(w[3], 0x4342));
             // (the lanes of the second half of a row begin with the other chunk: no two lanes at the same banks)
             const bool second = (c >> 3) != 0;
-            *reinterpret_cast<uint4*>(tile + operand_at(row, c + second)) = second ? o[1] : o[0];
-            *reinterpret_cast<uint4*>(tile + operand_at(row, c + !second)) = second ? o[0] : o[1];
+            if (piece < kAll) {
+                *reinterpret_cast<uint4*>(tile + operand_at(row, c + second)) = second ? o[1] : o[0];
+                *reinterpret_cast<uint4*>(tile + operand_at(row, c + !second)) = second ? o[0] : o[1];
+            }
         }
     }
 };
@@ -226,9 +253,9 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&k_full[i], 4);
+            mbar_init(&k_full[i], kQpMakers / 32);
             mbar_init(&k_empty[i], 1);
-            mbar_init(&v_full[i], 4);
+            mbar_init(&v_full[i], kQpMakers / 32);
             mbar_init(&v_empty[i], 1);
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 4);
@@ -237,7 +264,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
         *abort_flag = 0;
         fence_mbar_init_cluster();
     }
-    if (warp == 12) tmem_alloc(tmem_slot, 512);
+    if (warp == 11) tmem_alloc(tmem_slot, 512);
 
     const int sub = warp >> 2;                                          // of warps 0-7: the tile of rows
     const int my_row = (warp & 3) * 32 + lane;
@@ -279,7 +306,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
     pdl_open();
     const uint32_t tmem = *tmem_slot;
 
-    if (warp == 12) {
+    if (warp == 11) {
         // =========================== products ===========================
         constexpr uint32_t id_s = idesc_f16(128, 128, false), id_o = idesc_f16(128, D, true);
         const DescKind dk(smem_desc(0, 16, 1024)), dmn(smem_desc(0, kQpHalf, 1024));
@@ -351,14 +378,11 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
         if (sub < subs) {
             for (int n = 0; n < N; ++n) {
                 const int slot0 = (lo + n) * kQpSlots;
-                float ks[4], vs[4], vt = 0.f;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int blk = slot0 / kQcBlock + c;
-                    ks[c] = blk < blocks ? ksp[blk] * factor : 0.f;
-                    vs[c] = blk < blocks ? vsp[blk] : 0.f;
-                    vt = fmaxf(vt, vs[c]);
-                }
+                // lane c (of four) has the scales of the tile's block c
+                const int blk = slot0 / kQcBlock + (lane & 3);
+                const float ks = blk < blocks ? ksp[blk] : 0.f, vs = blk < blocks ? vsp[blk] : 0.f;
+                float vt = fmaxf(vs, __shfl_xor_sync(0xffffffffu, vs, 1));
+                vt = fmaxf(0.f, fmaxf(vt, __shfl_xor_sync(0xffffffffu, vt, 2)));
                 // the scale that the values are relative to follows the loudest block, not below 2^-60 of the loudest so far
                 float by_v = 1.f;
                 vmost = fmaxf(vmost, vt);
@@ -373,26 +397,19 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
                 tc_fence_after();
 
                 float top = -INFINITY;
+                auto most_of = [&](auto hide, int c, const uint32_t (&x)[32]) {
+                    const float k = __shfl_sync(0xffffffffu, ks, c) * factor;
+                    const int see = lim - (slot0 + 32 * c);   // slots of this block that the row sees
+                    float part[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t x[32];
-                    tmem_ld32_raw(s_col + 32 * c, x);
-                    tmem_wait_ld(x);
-                    float most = -INFINITY;
-                    if (masked) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) most = fmaxf(most, slot0 + 32 * c + j < lim ? __uint_as_float(x[j]) : -INFINITY);
-                        if (slot0 + 32 * c >= lim) most = -INFINITY;
-                        else most *= ks[c];
-                    } else {
-                        float part[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) part[j & 3] = fmaxf(part[j & 3], __uint_as_float(x[j]));
-                        most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * ks[c];
-                    }
-                    top = fmaxf(top, most);
-                }
-                if constexpr (CAP) top = top == -INFINITY ? top : a.cap * kLog2e * tanh1(top);
+                    for (int j = 0; j < 32; ++j)
+                        part[j & 3] = fmaxf(part[j & 3], decltype(hide)::value && j >= see ? -INFINITY : __uint_as_float(x[j]));
+                    const float most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * k;
+                    if (!decltype(hide)::value || see > 0) top = fmaxf(top, most);
+                };
+                if (masked) by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { most_of(std::true_type(), c, x); });
+                else by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { most_of(std::false_type(), c, x); });
+                if constexpr (CAP) top = top == -INFINITY ? top : a.cap * kLog2e * tanh_any(top);
                 float by = by_v;
                 if (top > m + kQpSlack || (m == -INFINITY && top > m)) {
                     const float keep = ex2(m - top);           // (0 the first time)
@@ -415,42 +432,43 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
                     }
                 }
                 const float m0 = m == -INFINITY ? 0.f : m;
-                const uint64_t nm = f2(-m0, -m0);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t x[32], p[16];
-                    tmem_ld32_raw(s_col + 32 * c, x);
-                    tmem_wait_ld(x);
-                    const uint64_t k2 = f2(ks[c], ks[c]), v2 = f2(vs[c] * inv_v, vs[c] * inv_v);
+                const uint64_t nm = f2(-m0, -m0), cl = f2(a.cap * kLog2e, a.cap * kLog2e);
+                auto form = [&](auto hide, int c, const uint32_t (&x)[32]) {
+                    constexpr bool kHide = decltype(hide)::value;
+                    const float k = __shfl_sync(0xffffffffu, ks, c) * factor, v = __shfl_sync(0xffffffffu, vs, c) * inv_v;
+                    const uint64_t k2 = f2(k, k), v2 = f2(v, v);
+                    const int see = lim - (slot0 + 32 * c);
+                    uint64_t s[16];
+                    uint32_t p[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        uint64_t s = f2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
-                        if constexpr (CAP) {
-                            const float2 y = f2_of(mul2(s, k2));
-                            const float cl = a.cap * kLog2e;
-                            s = fma2(f2(tanh1(y.x), tanh1(y.y)), f2(cl, cl), nm);
-                        } else {
-                            s = fma2(s, k2, nm);
-                        }
-                        float2 e = f2_of(s);
+                        s[j] = f2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
+                        s[j] = CAP ? mul2(s[j], k2) : fma2(s[j], k2, nm);
+                    }
+                    if constexpr (CAP) capped(s, cl, [&](int) { return nm; });
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float2 e = f2_of(s[j]);
                         e.x = ex2(e.x);
                         e.y = ex2(e.y);
-                        float2 y;
-                        if (masked) {                        // hidden slots give nothing, whatever their scales are
-                            const int left = lim - (slot0 + 32 * c + 2 * j);
-                            if (left < 1) e.x = 0.f;
-                            if (left < 2) e.y = 0.f;
-                            y = f2_of(mul2(f2(e.x, e.y), v2));
-                            if (left < 1) y.x = 0.f;
-                            if (left < 2) y.y = 0.f;
-                        } else {
-                            y = f2_of(mul2(f2(e.x, e.y), v2));
+                        if (kHide) {                          // hidden slots give nothing,
+                            if (2 * j >= see) e.x = 0.f;
+                            if (2 * j + 1 >= see) e.y = 0.f;
                         }
-                        l2[j & 1] = add2(l2[j & 1], f2(e.x, e.y));
+                        const uint64_t e2 = f2(e.x, e.y);
+                        l2[j & 1] = add2(l2[j & 1], e2);
+                        float2 y = f2_of(mul2(e2, v2));
+                        if (kHide) {                          // whatever their scales are
+                            if (2 * j >= see) y.x = 0.f;
+                            if (2 * j + 1 >= see) y.y = 0.f;
+                        }
                         p[j] = half2_bits(y.x, y.y);
                     }
                     tmem_st16(s_col + 16 * c, p);
-                }
+                };
+                // (P of 32 slots goes into 16 columns of what has been read: by_chunks is 32 ahead at most)
+                if (masked) by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { form(std::true_type(), c, x); });
+                else by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { form(std::false_type(), c, x); });
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -499,7 +517,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) tmem_dealloc(tmem, 512);
+    if (warp == 11) tmem_dealloc(tmem, 512);
 }
 
 // Joins the splits of a row: a warp to a row.
@@ -532,27 +550,28 @@ __global__ void __launch_bounds__(256) qc_prompt_join_kernel(const QcAttend a, c
 }
 
 // ---- the weights ------------------------------------------------------------------------------------------------
-constexpr int kQwtThreads = 13 * 32;
+constexpr int kQwtStages = 4;                          // of query tiles, and of products in tensor memory
 template <int D>
 struct QwtSmem {
     static constexpr int kTile = D / 64 * kQpHalf;
     static constexpr int k = 0;
-    static constexpr int q = k + kTile;               // two stages
-    static constexpr int rows = q + 2 * kTile;        // two stages of 64 x {factor, factor, -log, -log} by pairs of rows, and limits
+    static constexpr int q = k + kTile;
+    static constexpr int rows = q + kQwtStages * kTile;   // 64 x {factor, factor, -log, -log} by pairs of rows, and limits
     static constexpr int kRowBytes = 128 * 8 + 128 * 4;
-    static constexpr int bars = rows + 2 * kRowBytes;
-    static constexpr int total = bars + 128 + 1024;
+    static constexpr int bars = rows + kQwtStages * kRowBytes;
+    static constexpr int total = bars + 256 + 1024;
 };
 
 template <int D, bool CAP>
-__global__ void __launch_bounds__(kQwtThreads, 2) qc_prompt_weights_kernel(const QcAttend a, const QcPrompt pr) {
+__global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_weights_kernel(const QcAttend a, const QcPrompt pr) {
     using L = QwtSmem<D>;
+    constexpr int kSt = kQwtStages;
     extern __shared__ unsigned char qp_smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(qp_smem_raw) + 1023) & ~uintptr_t(1023));
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bars);
-    uint64_t *q_full = bars, *q_empty = bars + 2, *s_full = bars + 4, *s_empty = bars + 6;   // [2]
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 8);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 9);
+    uint64_t *q_full = bars, *q_empty = bars + kSt, *s_full = bars + 2 * kSt, *s_empty = bars + 3 * kSt;   // [kSt]
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 4 * kSt);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * kSt + 1);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const unsigned units = (unsigned)(a.c.B * a.c.Hkv);
     const unsigned unit = blockIdx.x % units;
@@ -567,8 +586,8 @@ __global__ void __launch_bounds__(kQwtThreads, 2) qc_prompt_weights_kernel(const
     const int N = (int)((valid - first + 127) / 128);
 
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&q_full[i], 4);
+        for (int i = 0; i < kSt; ++i) {
+            mbar_init(&q_full[i], kQpMakers / 32);
             mbar_init(&q_empty[i], 5);                                  // the products and the four warps that read the rows' terms
             mbar_init(&s_full[i], 1);
             mbar_init(&s_empty[i], 4);
@@ -576,8 +595,8 @@ __global__ void __launch_bounds__(kQwtThreads, 2) qc_prompt_weights_kernel(const
         *abort_flag = 0;
         fence_mbar_init_cluster();
     }
-    if (warp == 12) tmem_alloc(tmem_slot, 256);
-    if (warp >= 8 && warp < 12) {
+    if (warp == 11) tmem_alloc(tmem_slot, 512);
+    if (warp >= 8 && warp < 11) {
         Codes<D> k;
         k.load(a.c.codes[0] + (size_t)unit * a.c.C * D, slot0, sees.held, tid - 256);
         k.store(smem + L::k, tid - 256);
@@ -589,14 +608,14 @@ __global__ void __launch_bounds__(kQwtThreads, 2) qc_prompt_weights_kernel(const
     const uint32_t tmem = *tmem_slot;
     float sum = 0.f;
 
-    if (warp == 12) {
+    if (warp == 11) {
         constexpr uint32_t id_s = idesc_f16(128, 128, false);
         const DescKind dk(smem_desc(0, 16, 1024));
         const uint32_t base16 = desc_addr16(smem_u32(smem));
         for (int n = 0; n < N; ++n) {
-            const int st = n & 1;
-            qp_wait(&q_full[st], n >> 1, abort_flag);
-            if (n >= 2) qp_wait(&s_empty[st], (n >> 1) - 1, abort_flag);
+            const int st = n % kSt;
+            qp_wait(&q_full[st], n / kSt, abort_flag);
+            if (n >= kSt) qp_wait(&s_empty[st], n / kSt - 1, abort_flag);
             tc_fence_after();
             const uint32_t ka = base16 + L::k / 16, qa = base16 + (L::q + st * L::kTile) / 16;
 #pragma unroll
@@ -608,42 +627,44 @@ __global__ void __launch_bounds__(kQwtThreads, 2) qc_prompt_weights_kernel(const
     } else if (warp >= 8) {
         // =========================== queries and their rows' terms ===========================
         const int t = tid - 256;
-        constexpr int kChunks = D / 8;                                  // 16-byte pieces of a row
-        for (int n = 0; n <= N; ++n) {
+        constexpr int kChunks = D / 8, kAll = 128 * kChunks;            // 16-byte pieces of a row, of a tile
+        constexpr int kAhead = 2;                                       // tiles on their way
+        for (int n = 0; n < N + kAhead; ++n) {
             if (n < N) {
-                const int st = n & 1;
-                if (n >= 2) qp_wait(&q_empty[st], (n >> 1) - 1, abort_flag);
+                const int st = n % kSt;
+                if (n >= kSt) qp_wait(&q_empty[st], n / kSt - 1, abort_flag);
                 unsigned char* tile = smem + L::q + st * L::kTile;
                 const int64_t r0 = first + (int64_t)n * 128;
-#pragma unroll
-                for (int i = 0; i < kChunks; ++i) {
-                    const int row = i * (128 / kChunks) + t / kChunks, c = t % kChunks;
-                    const bool real = r0 + row < valid;
-                    cp_async16_zfill(smem_u32(tile + operand_at(row, c)),
-                                     pr.q16 + ((size_t)unit * a.R + (real ? r0 + row : 0)) * D + c * 8, real);
+                const uint16_t* from = pr.q16 + ((size_t)unit * a.R + r0) * D;
+                const int most = (int)min((int64_t)128, valid - r0) * kChunks;
+#pragma unroll 4
+                for (int piece = t; piece < kAll; piece += kQpMakers) {
+                    const bool real = piece < most;
+                    cp_async16_zfill(smem_u32(tile + operand_at(piece / kChunks, piece % kChunks)), from + (real ? piece * 8 : 0), real);
                 }
-                cp_async_commit();
-                // a thread's row: rows that add nothing have the logarithm infinity
-                const int64_t r = r0 + t;
-                float f = 0.f, nl = -INFINITY;
-                int lim = 0;
-                if (r < valid) {
-                    const float2 ml = a.ml[(size_t)unit * a.R + r];
-                    f = pr.q_factor[(size_t)unit * a.R + r];
-                    lim = sees(r);
-                    if (ml.y != 0.f) nl = __log2f(ml.y) - ml.x;
-                }
+                // the rows' terms; rows that add nothing have the logarithm infinity
                 float* rows = reinterpret_cast<float*>(smem + L::rows + st * L::kRowBytes);
-                rows[(t >> 1) * 4 + (t & 1)] = f;
-                rows[(t >> 1) * 4 + 2 + (t & 1)] = nl;
-                reinterpret_cast<int*>(rows + 256)[t] = lim;
+                for (int i = t; i < 128; i += kQpMakers) {
+                    const int64_t r = r0 + i;
+                    float f = 0.f, nl = -INFINITY;
+                    int lim = 0;
+                    if (r < valid) {
+                        const float2 ml = a.ml[(size_t)unit * a.R + r];
+                        f = pr.q_factor[(size_t)unit * a.R + r];
+                        lim = sees(r);
+                        if (ml.y != 0.f) nl = __log2f(ml.y) - ml.x;
+                    }
+                    rows[(i >> 1) * 4 + (i & 1)] = f;
+                    rows[(i >> 1) * 4 + 2 + (i & 1)] = nl;
+                    reinterpret_cast<int*>(rows + 256)[i] = lim;
+                }
             }
-            if (n > 0) {
-                if (n < N) cp_async_wait_but_one();
-                else cp_async_wait_all();
+            cp_async_commit();
+            if (n >= kAhead) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&q_full[(n - 1) & 1]);
+                if (lane == 0) mbar_arrive(&q_full[(n - kAhead) % kSt]);
             }
         }
     } else {
@@ -651,48 +672,50 @@ __global__ void __launch_bounds__(kQwtThreads, 2) qc_prompt_weights_kernel(const
         const int g = warp >> 2, my = (warp & 3) * 32 + lane, slot = slot0 + my;
         const int blk = slot / kQcBlock;
         const float ks = slot < sees.held ? a.c.scale[0][(size_t)unit * a.c.NB + blk] : 0.f;
-        const uint64_t k2 = f2(ks, ks);
-        const uint32_t s_col = tmem + ((uint32_t)(warp & 3) << 21) + g * 128;
+        const uint64_t k2 = f2(ks, ks), cl = f2(a.cap * kLog2e, a.cap * kLog2e);
         uint64_t acc[2] = {0, 0};
         for (int n = g; n < N; n += 2) {
-            const float* rows = reinterpret_cast<const float*>(smem + L::rows + g * L::kRowBytes);
+            const int st = n % kSt;
+            const float* rows = reinterpret_cast<const float*>(smem + L::rows + st * L::kRowBytes);
             const int* lims = reinterpret_cast<const int*>(rows + 256);
             const bool masked = slot0 + kQpSlots > sees(first + (int64_t)n * 128);
-            qp_wait(&q_full[g], n >> 1, abort_flag);                    // (the rows' terms)
-            qp_wait(&s_full[g], n >> 1, abort_flag);
+            qp_wait(&q_full[st], n / kSt, abort_flag);                  // (the rows' terms)
+            qp_wait(&s_full[st], n / kSt, abort_flag);
             tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t x[32];
-                tmem_ld32_raw(s_col + 32 * c, x);
-                tmem_wait_ld(x);
+            auto add = [&](auto hide, int c, const uint32_t (&x)[32]) {
+                uint64_t s[16];
+                const float* row = rows + 64 * c;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float4 t = *reinterpret_cast<const float4*>(rows + (16 * c + j) * 4);
-                    uint64_t s = mul2(f2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), k2);
-                    if constexpr (CAP) {
-                        const float2 y = f2_of(mul2(s, f2(t.x, t.y)));
-                        const float cl = a.cap * kLog2e;
-                        s = fma2(f2(tanh1(y.x), tanh1(y.y)), f2(cl, cl), f2(t.z, t.w));
-                    } else {
-                        s = fma2(s, f2(t.x, t.y), f2(t.z, t.w));
-                    }
-                    float2 e = f2_of(s);
+                    const float4 t = *reinterpret_cast<const float4*>(row + 4 * j);
+                    s[j] = mul2(f2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), k2);
+                    s[j] = CAP ? mul2(s[j], f2(t.x, t.y)) : fma2(s[j], f2(t.x, t.y), f2(t.z, t.w));
+                }
+                if constexpr (CAP)
+                    capped(s, cl, [&](int j) {
+                        const float2 t = *reinterpret_cast<const float2*>(row + 4 * j + 2);
+                        return f2(t.x, t.y);
+                    });
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    float2 e = f2_of(s[j]);
                     e.x = ex2(e.x);
                     e.y = ex2(e.y);
-                    if (masked) {
+                    if (decltype(hide)::value) {
                         if (slot >= lims[32 * c + 2 * j]) e.x = 0.f;
                         if (slot >= lims[32 * c + 2 * j + 1]) e.y = 0.f;
                     }
                     acc[j & 1] = add2(acc[j & 1], f2(e.x, e.y));
                 }
-            }
+            };
+            const uint32_t s_col = tmem + ((uint32_t)(warp & 3) << 21) + st * 128;
+            if (masked) by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { add(std::true_type(), c, x); });
+            else by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { add(std::false_type(), c, x); });
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&s_empty[g]);
-                mbar_arrive(&q_empty[g]);
-            }
+            if (lane == 0) mbar_arrive(&s_empty[st]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_empty[st]);
         }
         const float2 x = f2_of(add2(acc[0], acc[1]));
         sum = x.x + x.y;
@@ -707,7 +730,7 @@ __global__ void __launch_bounds__(kQwtThreads, 2) qc_prompt_weights_kernel(const
         if (*abort_flag) sum = __uint_as_float(0x7fffffffu);
         a.c.weight[(size_t)unit * a.c.C + slot0 + tid] += sum;
     }
-    if (warp == 12) tmem_dealloc(tmem, 256);
+    if (warp == 11) tmem_dealloc(tmem, 512);
 }
 
 template <int D, bool CAP>
@@ -722,7 +745,7 @@ cudaError_t prompt_with(const QcAttend& a, const QcPrompt& pr, cudaStream_t s) {
         return e;
     if (!a.accumulate) return cudaSuccess;
     if ((e = allow_smem(qc_prompt_weights_kernel<D, CAP>, QwtSmem<D>::total, &done[1])) != cudaSuccess) return e;
-    return pdl_launch(qc_prompt_weights_kernel<D, CAP>, (unsigned)(units * ((a.c.C + kQpSlots - 1) / kQpSlots)), kQwtThreads,
+    return pdl_launch(qc_prompt_weights_kernel<D, CAP>, (unsigned)(units * ((a.c.C + kQpSlots - 1) / kQpSlots)), kQpThreads,
                       QwtSmem<D>::total, s, a, pr);
 }
 
