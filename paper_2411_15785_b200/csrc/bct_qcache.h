@@ -69,8 +69,8 @@ struct QcAttend {
 struct QcPrompt {
     int tiles;             // of 256 rows, per unit
     int splits;            // CTAs that share the slots of a tile of rows
-    uint16_t* q16;         // [units][R][d]: queries as fp16, and what their products are multiplied with; NULL without weights
-    float* q_factor;       // [units][R]
+    unsigned char* q_tiles;   // [units][2 tiles] of 128 rows: queries as operands; NULL without weights
+    unsigned char* records;   // their rows' terms
 };
 // Which kernels serve a call, and its scratch: offsets into the caller's buffer, by the arguments alone.
 struct QcPlan {
@@ -82,7 +82,7 @@ struct QcPlan {
     int n_warps;
     int64_t n_groups;
     int R2;
-    size_t part_o, part_ml, spans, ml, scores, q16, q_factor, total;
+    size_t part_o, part_ml, spans, ml, scores, q_tiles, records, total;
 };
 cudaError_t qc_attend(const QcAttend& a, const QcPlan& p, int dtype, cudaStream_t s);
 cudaError_t qc_prompt(const QcAttend& a, const QcPrompt& pr, cudaStream_t s);

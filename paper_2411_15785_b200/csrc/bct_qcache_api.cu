@@ -103,13 +103,13 @@ bct_status_t plan_attend(const QcView& v, int64_t T, int32_t n_q_heads, int32_t 
     if (n_q_heads < 1 || n_q_heads > (1 << 16) || n_q_heads % v.Hkv != 0)
         return fail(BCT_ERR_INVALID_ARG, "n_q_heads (%d) must be a multiple of n_kv_heads (%d) in 1..65536", n_q_heads, v.Hkv);
     const int64_t R = T * (n_q_heads / v.Hkv), units = (int64_t)v.B * v.Hkv;
+    if (!grid_fits(units, std::max<int64_t>(v.NB, R))) return fail(BCT_ERR_INVALID_ARG, "batch, heads and T too large for one call");
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };
     *p = bct::QcPlan{};
     p->prompt = dtype == BCT_BF16 && R > bct::kQcScoredRows;
     if (p->prompt) {
         const int64_t tiles = (R + 255) / 256;
-        if (!grid_fits(units, std::max<int64_t>(v.NB, R))) return fail(BCT_ERR_INVALID_ARG, "batch, heads and T too large for one call");
         // a CTA per SM, but four tiles of 128 slots to each at least
         p->pr.tiles = (int)tiles;
         p->pr.splits = (int)std::max<int64_t>(1, std::min<int64_t>(148 / (units * tiles), v.C / 512));
@@ -117,10 +117,9 @@ bct_status_t plan_attend(const QcView& v, int64_t T, int32_t n_q_heads, int32_t 
             p->part_o = take((size_t)units * R * p->pr.splits * v.D * 4);
             p->part_ml = take((size_t)units * R * p->pr.splits * 8);
         }
-        p->ml = take((size_t)units * R * 8);
         if (accumulate) {
-            p->q16 = take((size_t)units * R * v.D * 2);
-            p->q_factor = take((size_t)units * R * 4);
+            p->q_tiles = take((size_t)units * tiles * 256 * v.D * 2);
+            p->records = take((size_t)units * tiles * 2 * 1536);
         }
         p->total = at;
         return BCT_OK;
@@ -132,8 +131,6 @@ bct_status_t plan_attend(const QcView& v, int64_t T, int32_t n_q_heads, int32_t 
     p->by_scores = accumulate != 0 && R <= bct::kQcScoredRows;
     p->n_warps = (int)std::min<int64_t>(bct::qc_attend_max_warps(), units * p->n_groups * v.NB);
     p->R2 = R == 1 ? 1 : (int)((std::min<int64_t>(R, bct::kQcScoredRows) + 1) / 2 * 2);
-    if (!grid_fits(units, std::max<int64_t>(v.NB, (R + 7) / 8)))
-        return fail(BCT_ERR_INVALID_ARG, "batch, heads and T too large for one call");
     p->part_o = take((size_t)2 * p->n_warps * p->rows * v.D * 4);
     p->part_ml = take((size_t)2 * p->n_warps * p->rows * 8);
     p->spans = take((size_t)units * p->n_groups * 8);
@@ -237,8 +234,8 @@ extern "C" bct_status_t bct_qcache_attend(const bct_qcache_t* cache, int64_t T, 
     cudaError_t e;
     if (p.prompt) {
         if (accumulate != 0) {
-            p.pr.q16 = reinterpret_cast<uint16_t*>(base + p.q16);
-            p.pr.q_factor = reinterpret_cast<float*>(base + p.q_factor);
+            p.pr.q_tiles = base + p.q_tiles;
+            p.pr.records = base + p.records;
         }
         e = bct::qc_prompt(a, p.pr, static_cast<cudaStream_t>(cuda_stream));
     } else {

@@ -184,11 +184,7 @@ __device__ __forceinline__ void to_scores(float (&s)[2][4], float mul0, float mu
             for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = to * tanh_any(s[i >> 2][i & 3]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const float2 y = f2_of(mul2(tanh_near2(f2(s[i >> 2][i & 3], s[i >> 2][(i & 3) + 1])), f2(to, to)));
-                s[i >> 2][i & 3] = y.x;
-                s[i >> 2][(i & 3) + 1] = y.y;
-            }
+            for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = to * tanh_near(s[i >> 2][i & 3]);
         }
     }
 }

@@ -35,10 +35,11 @@ __device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void* src, 
 // What a row sees: rows of a unit are (token, head), token-major.
 struct Sees {
     int held, n, G;   // slots held, valid tokens
-    int64_t R;
+    int64_t R;        // (below 2^31)
     __device__ __forceinline__ int operator()(int64_t r) const {
-        const int64_t i = r / G;
-        return r < R && i < n ? max(held - n + (int)i + 1, 0) : 0;
+        if (r >= R) return 0;
+        const int i = (int)((unsigned)r / (unsigned)G);
+        return i < n ? max(held - n + i + 1, 0) : 0;
     }
 };
 __device__ __forceinline__ Sees sees_of(const QcAttend& a, int b) {
@@ -51,8 +52,7 @@ __device__ __forceinline__ Sees sees_of(const QcAttend& a, int b) {
 }
 template <typename T>
 __device__ __forceinline__ const T* row_of(const QcAttend& a, const void* base, int b, int h, int64_t r) {
-    const int64_t i = r / a.G;
-    const int64_t head = (int64_t)h * a.G + (r - i * a.G);
+    const unsigned i = (unsigned)r / (unsigned)a.G, head = (unsigned)h * a.G + ((unsigned)r - i * a.G);
     return static_cast<const T*>(base) + (((int64_t)b * a.T + i) * ((int64_t)a.c.Hkv * a.G) + head) * a.c.D;
 }
 
@@ -69,51 +69,28 @@ __device__ __forceinline__ float row_factor(const QcAttend& a, float mul) {
     return a.cap > 0.f ? mul * (a.scale / a.cap) : mul * (a.scale * kLog2e);
 }
 
-// two floats to an instruction
-__device__ __forceinline__ uint64_t f2(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float2 f2_of(uint64_t v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
 }
 
-// tanh: up to 1 the fifth convergent of Lambert's continued fraction x / (1 + x^2 / (3 + x^2 / (5 + ..))), off by
-// x^10 / 9.8e6 of itself; beyond, (e - 1) / (e + 1) with e = exp(2 |x|), where nothing cancels.  Scores are rarely that
-// close to the cap, so that warps ask once for many of them (near: all are up to 1) and take two at a time.
-__device__ __forceinline__ float tanh_any(float x) {
+// tanh.  Up to 1, x times a polynomial in x^2 whose largest relative error is least (5e-8; fitted to tanh(x) / x by weighted
+// least squares; with its roundings 1.6e-7); beyond, (e - 1) / (e + 1) with e = exp(2 |x|), where nothing cancels.  Scores are
+// rarely that close to the cap, so that warps ask once for many of them whether all are up to 1.
+__device__ __forceinline__ float tanh_near(float x) {
     const float y = x * x;
-    float n = x * fmaf(y, y + 105.f, 945.f), d = fmaf(y, fmaf(y, 15.f, 420.f), 945.f);
-    if (y > 1.f) {
-        const float e = ex2(fminf(fabsf(x), 16.f) * (2.f * kLog2e));
-        n = copysignf(e - 1.f, x);
-        d = e + 1.f;
-    }
-    return __fdividef(n, d);
+    float p = fmaf(y, 0.001041022245772183f, -0.006203378085047007f);
+    p = fmaf(y, p, 0.020289979875087738f);
+    p = fmaf(y, p, -0.05345702916383743f);
+    p = fmaf(y, p, 0.13325203955173492f);
+    p = fmaf(y, p, -0.33332839608192444f);
+    return x * fmaf(y, p, 0.9999999403953552f);
 }
-__device__ __forceinline__ uint64_t tanh_near2(uint64_t x) {
-    const uint64_t y = mul2(x, x);
-    const uint64_t n = mul2(x, fma2(y, add2(y, f2(105.f, 105.f)), f2(945.f, 945.f)));
-    const float2 d = f2_of(fma2(y, fma2(y, f2(15.f, 15.f), f2(420.f, 420.f)), f2(945.f, 945.f)));
-    return mul2(n, f2(__fdividef(1.f, d.x), __fdividef(1.f, d.y)));
+__device__ __forceinline__ float tanh_any(float x) {
+    if (!(fabsf(x) > 1.f)) return tanh_near(x);   // (a NaN too)
+    const float e = ex2(fminf(fabsf(x), 16.f) * (2.f * kLog2e));
+    return copysignf(__fdividef(e - 1.f, e + 1.f), x);
 }
 
 }  // namespace bct

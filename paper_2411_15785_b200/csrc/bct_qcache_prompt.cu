@@ -139,74 +139,129 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // tanh of 32 numbers, some of them beyond 1 (rare: out of the way, through local memory)
-__device__ __noinline__ void tanh_far(uint64_t* s) {
+__device__ __noinline__ void tanh_far(float* s) {
 #pragma unroll 1
-    for (int j = 0; j < 16; ++j) {
-        const float2 y = f2_of(s[j]);
-        s[j] = f2(tanh_any(y.x), tanh_any(y.y));
-    }
+    for (int j = 0; j < 32; ++j) s[j] = tanh_any(s[j]);
 }
-// The capped scores of 32 products that have their factors, in powers of two, less something: cl tanh(s) + less[j].
-template <typename F>
-__device__ __forceinline__ void capped(uint64_t (&s)[16], uint64_t cl, F less) {
+// tanh of 32 scores that have their factors
+__device__ __forceinline__ void tanh32(float (&s)[32]) {
     float top = 0.f;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const float2 y = f2_of(s[j]);
-        top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
-    }
+    for (int j = 0; j < 32; j += 2) top = max3(top, fabsf(s[j]), fabsf(s[j + 1]));
     if (__any_sync(0xffffffffu, top > 1.f)) {
-        uint64_t far[16];
+        float far[32];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) far[j] = s[j];
+        for (int j = 0; j < 32; ++j) far[j] = s[j];
         tanh_far(far);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = fma2(far[j], cl, less(j));
+        for (int j = 0; j < 32; ++j) s[j] = far[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = fma2(tanh_near2(s[j]), cl, less(j));
+        for (int j = 0; j < 32; ++j) s[j] = tanh_near(s[j]);
     }
 }
 
-// A bounded wait of a warp.
+// A bounded wait of a warp: two seconds of the global timer, a thousandth of that once a wait has failed.  try_wait is given
+// a suspend time: warps wait here most of the time, and every poll takes issue slots from those that work.
+__device__ __noinline__ void qp_wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    const unsigned long long limit = *abort_flag ? 2000000ull : 2000000000ull;
+    for (;;) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (ok) return;
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+        if (t - t0 > limit) {
+            *abort_flag = 1;
+            return;
+        }
+    }
+}
 __device__ __forceinline__ void qp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    if (!mbar_wait_abortable(bar, parity & 1, abort_flag)) *abort_flag = 1;
+    if (!mbar_try_wait(bar, parity & 1)) qp_wait_slow(bar, parity & 1, abort_flag);
     __syncwarp();
 }
 // Where 16-byte chunk c (8 fp16 columns) of a row stands in an operand tile: halves of 64 columns, 128-byte swizzle.
 __device__ __forceinline__ int operand_at(int row, int c) { return (c >> 3) * kQpHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4); }
 
-// kQpMakers threads turn a tile of codes into an fp16 operand: raw[i] are the 16-byte pieces of a thread.
-template <int D>
+// THREADS threads turn a tile of codes into an fp16 operand: raw[i] are the 16-byte pieces of a thread.  Its rows are
+// multiples of four apart, so that their swizzles are two, and all addresses constants away from two.
+template <int D, int THREADS>
 struct Codes {
     static constexpr int kPer = D / 16, kAll = 128 * kPer;              // 16-byte pieces of a slot, of the tile
-    static constexpr int kRaw = (kAll + kQpMakers - 1) / kQpMakers;
+    static constexpr int kRaw = (kAll + THREADS - 1) / THREADS, kStep = THREADS / kPer;
+    static_assert(THREADS % kPer == 0 && kStep % 4 == 0, "a thread's rows are multiples of four apart");
     uint4 raw[kRaw];
     __device__ __forceinline__ void load(const int8_t* unit, int slot0, int end, int t) {
-        const int8_t* from = unit + (size_t)slot0 * D;
-        const int most = min(128, end - slot0) * kPer;
+        const uint4* from = reinterpret_cast<const uint4*>(unit + (size_t)slot0 * D) + t;
+        const int most = (end - slot0) * kPer - t;
+        if ((end - slot0) >= 128) {
 #pragma unroll
-        for (int i = 0; i < kRaw; ++i) {
-            const int piece = i * kQpMakers + t;
-            raw[i] = make_uint4(0, 0, 0, 0);
-            if (piece < most) raw[i] = *reinterpret_cast<const uint4*>(from + piece * 16);
+            for (int i = 0; i < kRaw; ++i)
+                if ((i + 1) * THREADS <= kAll || i * THREADS + t < kAll) raw[i] = from[i * THREADS];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRaw; ++i) raw[i] = i * THREADS < most ? from[i * THREADS] : make_uint4(0, 0, 0, 0);
         }
     }
     __device__ __forceinline__ void store(unsigned char* tile, int t) const {
+        const int row = t / kPer, c = t % kPer * 2;
+        // (the lanes of the second half of a row begin with the other chunk: no two lanes at the same banks)
+        const bool second = (c >> 3) != 0;
+        unsigned char* const to[2] = {tile + operand_at(row, c + second), tile + operand_at(row, c + !second)};
+        unsigned char* const to4[2] = {tile + operand_at(row ^ 4, c + second) + (row - (row ^ 4)) * 128,
+                                       tile + operand_at(row ^ 4, c + !second) + (row - (row ^ 4)) * 128};
 #pragma unroll
         for (int i = 0; i < kRaw; ++i) {
-            const int piece = i * kQpMakers + t, row = piece / kPer, c = piece % kPer * 2;
-            const uint32_t w[4] = {raw[i].x ^ 0x80808080u, raw[i].y ^ 0x80808080u, raw[i].z ^ 0x80808080u, raw[i].w ^ 0x80808080u};
-            uint4 o[2];
-            o[0] = make_uint4(pair_of(w[0], 0x4140), pair_of(w[0], 0x4342), pair_of(w[1], 0x4140), pair_of(w[1], 0x4342));
-            o[1] = make_uint4(pair_of(w[2], 0x4140), pair_of(w[2], 0x4342), pair_of(w[3], 0x4140), pair_of(w[3], 0x4342));
-            // (the lanes of the second half of a row begin with the other chunk: no two lanes at the same banks)
-            const bool second = (c >> 3) != 0;
-            if (piece < kAll) {
-                *reinterpret_cast<uint4*>(tile + operand_at(row, c + second)) = second ? o[1] : o[0];
-                *reinterpret_cast<uint4*>(tile + operand_at(row, c + !second)) = second ? o[0] : o[1];
-            }
+            if ((i + 1) * THREADS > kAll && i * THREADS + t >= kAll) break;
+            const uint32_t w[4] = {(second ? raw[i].z : raw[i].x) ^ 0x80808080u, (second ? raw[i].w : raw[i].y) ^ 0x80808080u,
+                                   (second ? raw[i].x : raw[i].z) ^ 0x80808080u, (second ? raw[i].y : raw[i].w) ^ 0x80808080u};
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                *reinterpret_cast<uint4*>(((kStep * i) & 4 ? to4[k] : to[k]) + kStep * i * 128) =
+                    make_uint4(pair_of(w[2 * k], 0x4140), pair_of(w[2 * k], 0x4342), pair_of(w[2 * k + 1], 0x4140),
+                               pair_of(w[2 * k + 1], 0x4342));
         }
+    }
+};
+
+// For the pass that forms the weights, of each tile of 128 rows: the queries as that operand, and a record of the rows'
+// terms: {factor, factor, -log, -log} for each pair of rows (what the row's products are multiplied with; the logarithm of
+// its sum of powers of two, infinity for a row that adds nothing), then how many slots each row sees.
+constexpr int kQpRecord = 128 * 8 + 128 * 4;
+__device__ __forceinline__ float* terms_of(const QcPrompt& pr, size_t tile, int row) {
+    return reinterpret_cast<float*>(pr.records + tile * kQpRecord) + (row >> 1) * 4 + (row & 1);
+}
+__device__ __forceinline__ int* limits_of(const QcPrompt& pr, size_t tile) {
+    return reinterpret_cast<int*>(pr.records + tile * kQpRecord + 1024);
+}
+
+// Where rows stand in q and out, `step` rows on at a time.
+struct RowWalk {
+    int64_t at, token_step, head_step;
+    int head, G, heads_on;
+    __device__ __forceinline__ RowWalk(const QcAttend& a, int b, int h, int64_t r, int step) {
+        const unsigned i = (unsigned)r / (unsigned)a.G;
+        const int64_t token = (int64_t)a.c.Hkv * a.G * a.c.D;
+        G = a.G;
+        head = (int)((unsigned)r - i * a.G);
+        at = ((int64_t)b * a.T + i) * token + (int64_t)(h * a.G + head) * a.c.D;
+        const int tokens_on = step / G;
+        heads_on = step - tokens_on * G;
+        head_step = tokens_on * token + (int64_t)heads_on * a.c.D;
+        token_step = token - (int64_t)G * a.c.D;       // a token on, and the heads of a group back
+    }
+    __device__ __forceinline__ void next() {
+        head += heads_on;
+        at += head_step;
+        if (head >= G) head -= G, at += token_step;
     }
 };
 
@@ -269,35 +324,48 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
     const int sub = warp >> 2;                                          // of warps 0-7: the tile of rows
     const int my_row = (warp & 3) * 32 + lane;
     const int64_t r = r0 + sub * 128 + my_row;
+    const size_t tile128 = ((size_t)unit * pr.tiles + (size_t)(r0 / kQpRows)) * 2 + sub;
+    const bool keep_q = pr.q_tiles != nullptr && split == 0;            // for the pass that forms the weights
     float factor = 0.f;                                                 // what the row's products are multiplied with
     int lim = 0;
     if (warp < 8) {
-        const bool real = r < valid;
-        lim = real ? sees(r) : 0;
-        // the row, as an operand and for the pass that forms the weights
-        const __nv_bfloat16* src = row_of<__nv_bfloat16>(a, a.q, b, h, real ? r : 0);
-        uint4 w[D / 8];
-        uint32_t top = 0;
+        // The warp's rows, as an operand: kLanes lanes to a row, 16 bytes each.
+        constexpr int kLanes = D / 8, kEach = 32 / kLanes, kTurns = 32 / kEach;
+        const int part = lane % kLanes;
+        uint4 w[kTurns];
+        RowWalk walk(a, b, h, r - lane + lane / kLanes, kEach);
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-            w[i] = real ? reinterpret_cast<const uint4*>(src)[i] : make_uint4(0, 0, 0, 0);
-            const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top = max(top, max((u[j] << 16) & 0x7fffffffu, u[j] & 0x7fff0000u));
+        for (int i = 0; i < kTurns; ++i) {
+            w[i] = make_uint4(0, 0, 0, 0);
+            if (r - lane + i * kEach + lane / kLanes < valid)
+                w[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + walk.at + 8 * part);
+            walk.next();
         }
-        float by;
-        row_scale(__uint_as_float(top), &by, &factor);
-        factor = row_factor(a, factor);
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-            float x[8];
+        for (int i = 0; i < kTurns; ++i) {
+            // (magnitudes in their order as 16-bit integers, two at a time)
+            uint32_t two = __vmaxu2(__vmaxu2(w[i].x & 0x7fff7fffu, w[i].y & 0x7fff7fffu), __vmaxu2(w[i].z & 0x7fff7fffu, w[i].w & 0x7fff7fffu));
+#pragma unroll
+            for (int o = 1; o < kLanes; o <<= 1) two = __vmaxu2(two, __shfl_xor_sync(0xffffffffu, two, o));
+            float by, back, x[8];
+            row_scale(__uint_as_float(max(two << 16, two & 0xffff0000u)), &by, &back);
             Chunk<__nv_bfloat16>::unpack(w[i], x);
             const uint4 o = make_uint4(half2_bits(x[0] * by, x[1] * by), half2_bits(x[2] * by, x[3] * by),
                                        half2_bits(x[4] * by, x[5] * by), half2_bits(x[6] * by, x[7] * by));
-            *reinterpret_cast<uint4*>(smem + L::q + sub * L::kTile + operand_at(my_row, i)) = o;
-            if (pr.q16 != nullptr && split == 0 && real) *reinterpret_cast<uint4*>(pr.q16 + ((size_t)unit * a.R + r) * D + i * 8) = o;
+            const int at = operand_at((warp & 3) * 32 + i * kEach + lane / kLanes, part);
+            *reinterpret_cast<uint4*>(smem + L::q + sub * L::kTile + at) = o;
+            if (keep_q) *reinterpret_cast<uint4*>(pr.q_tiles + tile128 * L::kTile + at) = o;
+            back = __shfl_sync(0xffffffffu, back, lane % kEach * kLanes);
+            if (i == lane / kEach) factor = row_factor(a, back);
         }
-        if (pr.q16 != nullptr && split == 0 && real) pr.q_factor[(size_t)unit * a.R + r] = factor;
+        const bool real = r < valid;
+        lim = real ? sees(r) : 0;
+        if (keep_q) {
+            float* terms = terms_of(pr, tile128, my_row);
+            terms[0] = real ? factor : 0.f;
+            terms[2] = -INFINITY;
+            limits_of(pr, tile128)[my_row] = lim;
+        }
     }
     fence_proxy_async_smem();
     tc_fence_before();
@@ -346,7 +414,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
     } else if (warp >= 8) {
         // =========================== codes to operands ===========================
         const int t = tid - 256;
-        Codes<D> k, v;
+        Codes<D, kQpMakers> k, v;
         if (N > 0) {
             k.load(kp, lo * kQpSlots, lim_max, t);
             v.load(vp, lo * kQpSlots, lim_max, t);
@@ -374,48 +442,62 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
         const float* vsp = a.c.scale[1] + (size_t)unit * a.c.NB;
         const int blocks = (lim_max + kQcBlock - 1) / kQcBlock;
         float m = -INFINITY, vref = 0.f, vmost = 0.f;
-        uint64_t l2[2] = {0, 0};
+        const float cap = a.cap * kLog2e;
+        float l = 0.f;
+        // lane c (of four) has the scales of a tile's block c, a tile ahead
+        float ks_next = 0.f, vs_next = 0.f;
+        auto load_scales = [&](int n) {
+            const int blk = (lo + n) * (kQpSlots / kQcBlock) + (lane & 3);
+            ks_next = vs_next = 0.f;
+            if (n < N && blk < blocks) ks_next = ksp[blk], vs_next = vsp[blk];
+        };
+        load_scales(0);
         if (sub < subs) {
-            for (int n = 0; n < N; ++n) {
+            auto tile = [&](int n, auto hide) {               // hide: some row does not see all of it
+                constexpr bool kHide = decltype(hide)::value;
                 const int slot0 = (lo + n) * kQpSlots;
-                // lane c (of four) has the scales of the tile's block c
-                const int blk = slot0 / kQcBlock + (lane & 3);
-                const float ks = blk < blocks ? ksp[blk] : 0.f, vs = blk < blocks ? vsp[blk] : 0.f;
+                const float ks = ks_next, vs = vs_next;
+                load_scales(n + 1);
                 float vt = fmaxf(vs, __shfl_xor_sync(0xffffffffu, vs, 1));
                 vt = fmaxf(0.f, fmaxf(vt, __shfl_xor_sync(0xffffffffu, vt, 2)));
-                // the scale that the values are relative to follows the loudest block, not below 2^-60 of the loudest so far
+                // the scale that the values are relative to follows the loudest block (some way above it, so that it moves
+                // rarely), not below 2^-60 of the loudest so far
                 float by_v = 1.f;
                 vmost = fmaxf(vmost, vt);
-                if (vt > vref || vt < vref * 0.015625f) {
-                    const float to = fmaxf(vt, vmost * 8.67361738e-19f);
+                if (vt > vref || vt < vref * 0.00390625f) {
+                    const float to = 4.f * fmaxf(vt, vmost * 8.67361738e-19f);
                     if (vref > 0.f && to > 0.f) by_v = vref / to;
                     if (to > 0.f) vref = to;
                 }
-                const float inv_v = vref > 0.f ? kQpPScale / vref : 0.f;
-                const bool masked = slot0 + kQpSlots > lim_min;
+                // P's factor of the lane's block, as a power of two and inverted; a block of zeros has any
+                const float v_rel = vs == 0.f ? kQpPScale : max_nan(__fdividef(vs, vref > 0.f ? vref : 1.f), 8.67361738e-19f) * kQpPScale;
+                const float v_log = __log2f(v_rel), v_inv = __fdividef(1.f, v_rel);
                 qp_wait(&s_full[sub], n, abort_flag);
                 tc_fence_after();
 
                 float top = -INFINITY;
-                auto most_of = [&](auto hide, int c, const uint32_t (&x)[32]) {
+                by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) {
                     const float k = __shfl_sync(0xffffffffu, ks, c) * factor;
                     const int see = lim - (slot0 + 32 * c);   // slots of this block that the row sees
-                    float part[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    float part[2] = {-INFINITY, -INFINITY};
+                    if constexpr (kHide) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        part[j & 3] = fmaxf(part[j & 3], decltype(hide)::value && j >= see ? -INFINITY : __uint_as_float(x[j]));
-                    const float most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * k;
-                    if (!decltype(hide)::value || see > 0) top = fmaxf(top, most);
-                };
-                if (masked) by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { most_of(std::true_type(), c, x); });
-                else by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { most_of(std::false_type(), c, x); });
-                if constexpr (CAP) top = top == -INFINITY ? top : a.cap * kLog2e * tanh_any(top);
+                        for (int j = 0; j < 32; ++j) part[j & 1] = fmaxf(part[j & 1], j < see ? __uint_as_float(x[j]) : -INFINITY);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            part[0] = max3(part[0], __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
+                            part[1] = max3(part[1], __uint_as_float(x[j + 2]), __uint_as_float(x[j + 3]));
+                        }
+                    }
+                    if (!kHide || see > 0) top = fmaxf(top, fmaxf(part[0], part[1]) * k);
+                });
+                if constexpr (CAP) top = top == -INFINITY ? top : cap * tanh_any(top);
                 float by = by_v;
                 if (top > m + kQpSlack || (m == -INFINITY && top > m)) {
                     const float keep = ex2(m - top);           // (0 the first time)
                     by *= keep;
-                    l2[0] = mul2(l2[0], f2(keep, keep));
-                    l2[1] = mul2(l2[1], f2(keep, keep));
+                    l *= keep;
                     m = top;
                 }
                 if (n > 0 && __any_sync(0xffffffffu, by != 1.f)) {
@@ -432,56 +514,49 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
                     }
                 }
                 const float m0 = m == -INFINITY ? 0.f : m;
-                const uint64_t nm = f2(-m0, -m0), cl = f2(a.cap * kLog2e, a.cap * kLog2e);
-                auto form = [&](auto hide, int c, const uint32_t (&x)[32]) {
-                    constexpr bool kHide = decltype(hide)::value;
-                    const float k = __shfl_sync(0xffffffffu, ks, c) * factor, v = __shfl_sync(0xffffffffu, vs, c) * inv_v;
-                    const uint64_t k2 = f2(k, k), v2 = f2(v, v);
+                // (P of 32 slots goes into 16 columns of what has been read: by_chunks is 32 ahead at most)
+                by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) {
+                    const float k = __shfl_sync(0xffffffffu, ks, c) * factor;
+                    const float bias = __shfl_sync(0xffffffffu, v_log, c) - m0, v_back = __shfl_sync(0xffffffffu, v_inv, c);
                     const int see = lim - (slot0 + 32 * c);
-                    uint64_t s[16];
+                    float e[32], sum[4] = {0.f, 0.f, 0.f, 0.f};
                     uint32_t p[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        s[j] = f2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
-                        s[j] = CAP ? mul2(s[j], k2) : fma2(s[j], k2, nm);
-                    }
-                    if constexpr (CAP) capped(s, cl, [&](int) { return nm; });
+                    for (int j = 0; j < 32; ++j) e[j] = CAP ? __uint_as_float(x[j]) * k : fmaf(__uint_as_float(x[j]), k, bias);
+                    if constexpr (CAP) {
+                        tanh32(e);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        float2 e = f2_of(s[j]);
-                        e.x = ex2(e.x);
-                        e.y = ex2(e.y);
-                        if (kHide) {                          // hidden slots give nothing,
-                            if (2 * j >= see) e.x = 0.f;
-                            if (2 * j + 1 >= see) e.y = 0.f;
-                        }
-                        const uint64_t e2 = f2(e.x, e.y);
-                        l2[j & 1] = add2(l2[j & 1], e2);
-                        float2 y = f2_of(mul2(e2, v2));
-                        if (kHide) {                          // whatever their scales are
-                            if (2 * j >= see) y.x = 0.f;
-                            if (2 * j + 1 >= see) y.y = 0.f;
-                        }
-                        p[j] = half2_bits(y.x, y.y);
+                        for (int j = 0; j < 32; ++j) e[j] = fmaf(e[j], cap, bias);
                     }
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) e[j] = ex2(e[j]);
+                    if constexpr (kHide) {                    // hidden slots give nothing, whatever their scales
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) e[j] = j < see ? e[j] : 0.f;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[j & 3] += e[j];
+                    if (!kHide || see > 0) l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), v_back, l);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) p[j] = half2_bits(e[2 * j], e[2 * j + 1]);
                     tmem_st16(s_col + 16 * c, p);
-                };
-                // (P of 32 slots goes into 16 columns of what has been read: by_chunks is 32 ahead at most)
-                if (masked) by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { form(std::true_type(), c, x); });
-                else by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { form(std::false_type(), c, x); });
+                });
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&p_full[sub]);
-            }
+            };
+            const int seen = min(max(lim_min / kQpSlots - lo, 0), N);   // tiles that every row sees
+#pragma unroll 1
+            for (int n = 0; n < seen; ++n) tile(n, std::false_type());
+#pragma unroll 1
+            for (int n = seen; n < N; ++n) tile(n, std::true_type());
         }
         // results: the accumulators are in units of vref / 2^9
         if (N > 0 && sub < subs) {
             qp_wait(&o_full[sub], N - 1, abort_flag);
             tc_fence_after();
         }
-        const float2 la = f2_of(add2(l2[0], l2[1]));
-        float l = la.x + la.y;
         if (lim == 0) l = 0.f;                                // (a padding row in a tile that others see through)
         if (*abort_flag) l = __uint_as_float(0x7fffffffu);
         float mul = vref * (1.f / kQpPScale);
@@ -489,7 +564,8 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
         const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
         if (pr.splits == 1) mul = l == l ? mul * inv : l;
         const int64_t at = ((int64_t)unit * a.R + r) * pr.splits + split;
-        __nv_bfloat16* to = const_cast<__nv_bfloat16*>(row_of<__nv_bfloat16>(a, a.out, b, h, there ? r : 0));
+        // (through the warp's part of the queries' tile, which is free by now, so that rows are written in one piece)
+        unsigned char* stage = smem + L::q + sub * L::kTile + (warp & 3) * (32 * D * 2);
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
             uint32_t x[32];
@@ -500,9 +576,10 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
             float y[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) y[j] = mine && (l != 0.f) ? __uint_as_float(x[j]) * mul : 0.f;
-            if (there && pr.splits == 1) {
+            if (pr.splits == 1) {
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) *reinterpret_cast<uint4*>(to + c + j) = Chunk<__nv_bfloat16>::pack(y + j);
+                for (int j = 0; j < 32; j += 8)
+                    *reinterpret_cast<uint4*>(stage + lane * (D * 2) + ((((c + j) >> 3) ^ (lane & 7)) << 4)) = Chunk<__nv_bfloat16>::pack(y + j);
             } else if (there) {
 #pragma unroll
                 for (int j = 0; j < 32; j += 4)
@@ -510,9 +587,20 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
             }
             __syncwarp();
         }
+        if (pr.splits == 1) {
+            constexpr int kLanes = D / 8, kEach = 32 / kLanes;
+            RowWalk walk(a, b, h, r - lane + lane / kLanes, kEach);
+#pragma unroll 4
+            for (int i = 0; i < 32; i += kEach) {
+                const int row = i + lane / kLanes, part = lane % kLanes;
+                const uint4 v = *reinterpret_cast<const uint4*>(stage + row * (D * 2) + ((part ^ (row & 7)) << 4));
+                if (r - lane + row < a.R) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + walk.at + 8 * part) = v;
+                walk.next();
+            }
+        }
         if (there) {
-            if (pr.splits == 1) a.ml[(size_t)unit * a.R + r] = make_float2(m, inv);
-            else a.part_ml[at] = make_float2(m, l);
+            if (pr.splits > 1) a.part_ml[at] = make_float2(m, l);
+            else if (keep_q && inv != 0.f) terms_of(pr, tile128, my_row)[2] = log2f(inv) - m;
         }
     }
     tc_fence_before();
@@ -546,24 +634,25 @@ __global__ void __launch_bounds__(256) qc_prompt_join_kernel(const QcAttend a, c
 #pragma unroll
     for (int j = 0; j < kN; j += 2)
         *reinterpret_cast<uint32_t*>(to + j) = l == l ? Chunk<__nv_bfloat16>::pack2(y[j], y[j + 1]) : 0x7fff7fffu;
-    if (lane == 0) a.ml[row] = make_float2(m, inv);
+    if (lane == 0 && pr.q_tiles != nullptr && inv != 0.f)
+        terms_of(pr, ((size_t)unit * pr.tiles + (size_t)(r / kQpRows)) * 2 + (size_t)(r % kQpRows) / 128, (int)(r % 128))[2] = log2f(inv) - m;
 }
 
 // ---- the weights ------------------------------------------------------------------------------------------------
 constexpr int kQwtStages = 4;                          // of query tiles, and of products in tensor memory
+constexpr int kQwtThreads = 10 * 32;                   // eight warps that add up, one that loads, one for the products
 template <int D>
 struct QwtSmem {
     static constexpr int kTile = D / 64 * kQpHalf;
     static constexpr int k = 0;
     static constexpr int q = k + kTile;
-    static constexpr int rows = q + kQwtStages * kTile;   // 64 x {factor, factor, -log, -log} by pairs of rows, and limits
-    static constexpr int kRowBytes = 128 * 8 + 128 * 4;
-    static constexpr int bars = rows + kQwtStages * kRowBytes;
+    static constexpr int rows = q + kQwtStages * kTile;   // the rows' records
+    static constexpr int bars = rows + kQwtStages * kQpRecord;
     static constexpr int total = bars + 256 + 1024;
 };
 
 template <int D, bool CAP>
-__global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_weights_kernel(const QcAttend a, const QcPrompt pr) {
+__global__ void __launch_bounds__(kQwtThreads, 1) qc_prompt_weights_kernel(const QcAttend a, const QcPrompt pr) {
     using L = QwtSmem<D>;
     constexpr int kSt = kQwtStages;
     extern __shared__ unsigned char qp_smem_raw[];
@@ -587,7 +676,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_weights_kernel(const 
 
     if (tid == 0) {
         for (int i = 0; i < kSt; ++i) {
-            mbar_init(&q_full[i], kQpMakers / 32);
+            mbar_init(&q_full[i], 1);
             mbar_init(&q_empty[i], 5);                                  // the products and the four warps that read the rows' terms
             mbar_init(&s_full[i], 1);
             mbar_init(&s_empty[i], 4);
@@ -595,11 +684,11 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_weights_kernel(const 
         *abort_flag = 0;
         fence_mbar_init_cluster();
     }
-    if (warp == 11) tmem_alloc(tmem_slot, 512);
-    if (warp >= 8 && warp < 11) {
-        Codes<D> k;
-        k.load(a.c.codes[0] + (size_t)unit * a.c.C * D, slot0, sees.held, tid - 256);
-        k.store(smem + L::k, tid - 256);
+    if (warp == 9) tmem_alloc(tmem_slot, 512);
+    if (warp < 8) {
+        Codes<D, 256> k;
+        k.load(a.c.codes[0] + (size_t)unit * a.c.C * D, slot0, sees.held, tid);
+        k.store(smem + L::k, tid);
     }
     fence_proxy_async_smem();
     tc_fence_before();
@@ -608,7 +697,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_weights_kernel(const 
     const uint32_t tmem = *tmem_slot;
     float sum = 0.f;
 
-    if (warp == 11) {
+    if (warp == 9) {
         constexpr uint32_t id_s = idesc_f16(128, 128, false);
         const DescKind dk(smem_desc(0, 16, 1024));
         const uint32_t base16 = desc_addr16(smem_u32(smem));
@@ -624,101 +713,70 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_weights_kernel(const 
             commit_warp(&s_full[st]);
             commit_warp(&q_empty[st]);
         }
-    } else if (warp >= 8) {
+    } else if (warp == 8) {
         // =========================== queries and their rows' terms ===========================
-        const int t = tid - 256;
-        constexpr int kChunks = D / 8, kAll = 128 * kChunks;            // 16-byte pieces of a row, of a tile
-        constexpr int kAhead = 2;                                       // tiles on their way
-        for (int n = 0; n < N + kAhead; ++n) {
-            if (n < N) {
-                const int st = n % kSt;
-                if (n >= kSt) qp_wait(&q_empty[st], n / kSt - 1, abort_flag);
-                unsigned char* tile = smem + L::q + st * L::kTile;
-                const int64_t r0 = first + (int64_t)n * 128;
-                const uint16_t* from = pr.q16 + ((size_t)unit * a.R + r0) * D;
-                const int most = (int)min((int64_t)128, valid - r0) * kChunks;
-#pragma unroll 4
-                for (int piece = t; piece < kAll; piece += kQpMakers) {
-                    const bool real = piece < most;
-                    cp_async16_zfill(smem_u32(tile + operand_at(piece / kChunks, piece % kChunks)), from + (real ? piece * 8 : 0), real);
-                }
-                // the rows' terms; rows that add nothing have the logarithm infinity
-                float* rows = reinterpret_cast<float*>(smem + L::rows + st * L::kRowBytes);
-                for (int i = t; i < 128; i += kQpMakers) {
-                    const int64_t r = r0 + i;
-                    float f = 0.f, nl = -INFINITY;
-                    int lim = 0;
-                    if (r < valid) {
-                        const float2 ml = a.ml[(size_t)unit * a.R + r];
-                        f = pr.q_factor[(size_t)unit * a.R + r];
-                        lim = sees(r);
-                        if (ml.y != 0.f) nl = __log2f(ml.y) - ml.x;
-                    }
-                    rows[(i >> 1) * 4 + (i & 1)] = f;
-                    rows[(i >> 1) * 4 + 2 + (i & 1)] = nl;
-                    reinterpret_cast<int*>(rows + 256)[i] = lim;
-                }
+        const size_t tile0 = (size_t)unit * pr.tiles * 2 + (size_t)(first / 128);
+        for (int n = 0; n < N; ++n) {
+            const int st = n % kSt;
+            if (n >= kSt) qp_wait(&q_empty[st], n / kSt - 1, abort_flag);
+            if (lane == 0) {
+                mbar_arrive_expect_tx(&q_full[st], L::kTile + kQpRecord);
+                bulk_load(smem + L::q + st * L::kTile, pr.q_tiles + (tile0 + n) * L::kTile, L::kTile, &q_full[st]);
+                bulk_load(smem + L::rows + st * kQpRecord, pr.records + (tile0 + n) * kQpRecord, kQpRecord, &q_full[st]);
             }
-            cp_async_commit();
-            if (n >= kAhead) {
-                asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&q_full[(n - kAhead) % kSt]);
-            }
+            __syncwarp();
         }
+        // (the copies end before the CTA does: the products of the last tile wait for them)
     } else {
         // =========================== a slot to a thread; warps 0-3 and 4-7 take the row tiles in turn ===========================
         const int g = warp >> 2, my = (warp & 3) * 32 + lane, slot = slot0 + my;
         const int blk = slot / kQcBlock;
         const float ks = slot < sees.held ? a.c.scale[0][(size_t)unit * a.c.NB + blk] : 0.f;
-        const uint64_t k2 = f2(ks, ks), cl = f2(a.cap * kLog2e, a.cap * kLog2e);
-        uint64_t acc[2] = {0, 0};
+        const float cap = a.cap * kLog2e;
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
         for (int n = g; n < N; n += 2) {
             const int st = n % kSt;
-            const float* rows = reinterpret_cast<const float*>(smem + L::rows + st * L::kRowBytes);
+            const float* rows = reinterpret_cast<const float*>(smem + L::rows + st * kQpRecord);
             const int* lims = reinterpret_cast<const int*>(rows + 256);
-            const bool masked = slot0 + kQpSlots > sees(first + (int64_t)n * 128);
             qp_wait(&q_full[st], n / kSt, abort_flag);                  // (the rows' terms)
             qp_wait(&s_full[st], n / kSt, abort_flag);
             tc_fence_after();
-            auto add = [&](auto hide, int c, const uint32_t (&x)[32]) {
-                uint64_t s[16];
+            const bool masked = slot0 + kQpSlots > lims[0];             // (a tile's first row sees least of its valid ones)
+            by_chunks(tmem + ((uint32_t)(warp & 3) << 21) + st * 128, [&](int c, const uint32_t (&x)[32]) {
                 const float* row = rows + 64 * c;
+                float e[32];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const float4 t = *reinterpret_cast<const float4*>(row + 4 * j);
-                    s[j] = mul2(f2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), k2);
-                    s[j] = CAP ? mul2(s[j], f2(t.x, t.y)) : fma2(s[j], f2(t.x, t.y), f2(t.z, t.w));
+                    const float u = __uint_as_float(x[2 * j]) * ks, v = __uint_as_float(x[2 * j + 1]) * ks;
+                    e[2 * j] = CAP ? u * t.x : fmaf(u, t.x, t.z);
+                    e[2 * j + 1] = CAP ? v * t.y : fmaf(v, t.y, t.w);
                 }
-                if constexpr (CAP)
-                    capped(s, cl, [&](int j) {
-                        const float2 t = *reinterpret_cast<const float2*>(row + 4 * j + 2);
-                        return f2(t.x, t.y);
-                    });
+                if constexpr (CAP) {
+                    tanh32(e);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    float2 e = f2_of(s[j]);
-                    e.x = ex2(e.x);
-                    e.y = ex2(e.y);
-                    if (decltype(hide)::value) {
-                        if (slot >= lims[32 * c + 2 * j]) e.x = 0.f;
-                        if (slot >= lims[32 * c + 2 * j + 1]) e.y = 0.f;
+                    for (int j = 0; j < 16; ++j) {
+                        const float2 t = *reinterpret_cast<const float2*>(row + 4 * j + 2);
+                        e[2 * j] = fmaf(e[2 * j], cap, t.x);
+                        e[2 * j + 1] = fmaf(e[2 * j + 1], cap, t.y);
                     }
-                    acc[j & 1] = add2(acc[j & 1], f2(e.x, e.y));
                 }
-            };
-            const uint32_t s_col = tmem + ((uint32_t)(warp & 3) << 21) + st * 128;
-            if (masked) by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { add(std::true_type(), c, x); });
-            else by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) { add(std::false_type(), c, x); });
+#pragma unroll
+                for (int j = 0; j < 32; ++j) e[j] = ex2(e[j]);
+                if (masked) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) e[j] = slot < lims[32 * c + j] ? e[j] : 0.f;
+                }
+#pragma unroll
+                for (int j = 0; j < 32; ++j) acc[j & 3] += e[j];
+            });
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&s_empty[st]);
             __syncwarp();
             if (lane == 0) mbar_arrive(&q_empty[st]);
         }
-        const float2 x = f2_of(add2(acc[0], acc[1]));
-        sum = x.x + x.y;
+        sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
     }
     tc_fence_before();
     __syncthreads();
@@ -730,7 +788,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_weights_kernel(const 
         if (*abort_flag) sum = __uint_as_float(0x7fffffffu);
         a.c.weight[(size_t)unit * a.c.C + slot0 + tid] += sum;
     }
-    if (warp == 11) tmem_dealloc(tmem, 512);
+    if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
 template <int D, bool CAP>
@@ -745,7 +803,7 @@ cudaError_t prompt_with(const QcAttend& a, const QcPrompt& pr, cudaStream_t s) {
         return e;
     if (!a.accumulate) return cudaSuccess;
     if ((e = allow_smem(qc_prompt_weights_kernel<D, CAP>, QwtSmem<D>::total, &done[1])) != cudaSuccess) return e;
-    return pdl_launch(qc_prompt_weights_kernel<D, CAP>, (unsigned)(units * ((a.c.C + kQpSlots - 1) / kQpSlots)), kQpThreads,
+    return pdl_launch(qc_prompt_weights_kernel<D, CAP>, (unsigned)(units * ((a.c.C + kQpSlots - 1) / kQpSlots)), kQwtThreads,
                       QwtSmem<D>::total, s, a, pr);
 }
 

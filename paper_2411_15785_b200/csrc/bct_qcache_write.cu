@@ -136,12 +136,6 @@ __device__ __forceinline__ void store_codes(int8_t* p, uint32_t w) {
 }
 __device__ __forceinline__ float code_at(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
 
-// The larger one, or a NaN if either is one; an infinity becomes one at the end.
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float y;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-    return y;
-}
 // Largest magnitude of a plane's four warps; a NaN or an infinity in any of them makes it a NaN.
 __device__ __forceinline__ float plane_amax(float mine, float (*share)[4], int plane, int part) {
 #pragma unroll
