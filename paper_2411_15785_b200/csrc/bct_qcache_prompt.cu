@@ -253,8 +253,8 @@ struct RowWalk {
         G = a.G;
         head = (int)((unsigned)r - i * a.G);
         at = ((int64_t)b * a.T + i) * token + (int64_t)(h * a.G + head) * a.c.D;
-        const int tokens_on = step / G;
-        heads_on = step - tokens_on * G;
+        int tokens_on = 0;
+        for (heads_on = step; heads_on >= G; heads_on -= G) ++tokens_on;   // (step is a few rows)
         head_step = tokens_on * token + (int64_t)heads_on * a.c.D;
         token_step = token - (int64_t)G * a.c.D;       // a token on, and the heads of a group back
     }
@@ -282,9 +282,9 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(qp_smem_raw) + 1023) & ~uintptr_t(1023));
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bars);
     uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6;   // [2] by stages
-    uint64_t *s_full = bars + 8, *p_full = bars + 10, *o_full = bars + 12;                   // [2] by tiles of rows
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 14);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 15);
+    uint64_t *q_full = bars + 8, *s_full = bars + 10, *p_full = bars + 12, *o_full = bars + 14;   // [2] by tiles of rows
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 16);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 17);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     // (unit, rows, split): the rows that see most come first
@@ -312,6 +312,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
             mbar_init(&k_empty[i], 1);
             mbar_init(&v_full[i], kQpMakers / 32);
             mbar_init(&v_empty[i], 1);
+            mbar_init(&q_full[i], 4);
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 4);
             mbar_init(&o_full[i], 1);
@@ -321,52 +322,6 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
     }
     if (warp == 11) tmem_alloc(tmem_slot, 512);
 
-    const int sub = warp >> 2;                                          // of warps 0-7: the tile of rows
-    const int my_row = (warp & 3) * 32 + lane;
-    const int64_t r = r0 + sub * 128 + my_row;
-    const size_t tile128 = ((size_t)unit * pr.tiles + (size_t)(r0 / kQpRows)) * 2 + sub;
-    const bool keep_q = pr.q_tiles != nullptr && split == 0;            // for the pass that forms the weights
-    float factor = 0.f;                                                 // what the row's products are multiplied with
-    int lim = 0;
-    if (warp < 8) {
-        // The warp's rows, as an operand: kLanes lanes to a row, 16 bytes each.
-        constexpr int kLanes = D / 8, kEach = 32 / kLanes, kTurns = 32 / kEach;
-        const int part = lane % kLanes;
-        uint4 w[kTurns];
-        RowWalk walk(a, b, h, r - lane + lane / kLanes, kEach);
-#pragma unroll
-        for (int i = 0; i < kTurns; ++i) {
-            w[i] = make_uint4(0, 0, 0, 0);
-            if (r - lane + i * kEach + lane / kLanes < valid)
-                w[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + walk.at + 8 * part);
-            walk.next();
-        }
-#pragma unroll
-        for (int i = 0; i < kTurns; ++i) {
-            // (magnitudes in their order as 16-bit integers, two at a time)
-            uint32_t two = __vmaxu2(__vmaxu2(w[i].x & 0x7fff7fffu, w[i].y & 0x7fff7fffu), __vmaxu2(w[i].z & 0x7fff7fffu, w[i].w & 0x7fff7fffu));
-#pragma unroll
-            for (int o = 1; o < kLanes; o <<= 1) two = __vmaxu2(two, __shfl_xor_sync(0xffffffffu, two, o));
-            float by, back, x[8];
-            row_scale(__uint_as_float(max(two << 16, two & 0xffff0000u)), &by, &back);
-            Chunk<__nv_bfloat16>::unpack(w[i], x);
-            const uint4 o = make_uint4(half2_bits(x[0] * by, x[1] * by), half2_bits(x[2] * by, x[3] * by),
-                                       half2_bits(x[4] * by, x[5] * by), half2_bits(x[6] * by, x[7] * by));
-            const int at = operand_at((warp & 3) * 32 + i * kEach + lane / kLanes, part);
-            *reinterpret_cast<uint4*>(smem + L::q + sub * L::kTile + at) = o;
-            if (keep_q) *reinterpret_cast<uint4*>(pr.q_tiles + tile128 * L::kTile + at) = o;
-            back = __shfl_sync(0xffffffffu, back, lane % kEach * kLanes);
-            if (i == lane / kEach) factor = row_factor(a, back);
-        }
-        const bool real = r < valid;
-        lim = real ? sees(r) : 0;
-        if (keep_q) {
-            float* terms = terms_of(pr, tile128, my_row);
-            terms[0] = real ? factor : 0.f;
-            terms[2] = -INFINITY;
-            limits_of(pr, tile128)[my_row] = lim;
-        }
-    }
     fence_proxy_async_smem();
     tc_fence_before();
     __syncthreads();
@@ -389,8 +344,11 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
         };
         if (N > 0) {
             qp_wait(&k_full[0], 0, abort_flag);
-            tc_fence_after();
-            for (int g = 0; g < subs; ++g) scores(0, g);
+            for (int g = 0; g < subs; ++g) {
+                qp_wait(&q_full[g], 0, abort_flag);
+                tc_fence_after();
+                scores(0, g);
+            }
         }
         for (int n = 0; n < N; ++n) {
             const uint32_t va = base16 + (L::v + (n & 1) * L::kTile) / 16;
@@ -435,7 +393,69 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
             if (lane == 0) mbar_arrive(&v_full[st]);
         }
     } else {
-        // =========================== softmax ===========================
+        // =========================== queries, softmax ===========================
+        const int sub = warp >> 2;                                          // of warps 0-7: the tile of rows
+        const int my_row = (warp & 3) * 32 + lane;
+        const int64_t r = r0 + sub * 128 + my_row;
+        const size_t tile128 = ((size_t)unit * pr.tiles + (size_t)(r0 / kQpRows)) * 2 + sub;
+        const bool keep_q = pr.q_tiles != nullptr && split == 0;            // for the pass that forms the weights
+        float factor = 0.f;                                                 // what the row's products are multiplied with
+        int lim = 0;
+        // The warp's rows, as an operand: kLanes lanes to a row, 16 bytes each.
+        constexpr int kLanes = D / 8, kEach = 32 / kLanes, kTurns = 32 / kEach;
+        const int part = lane % kLanes;
+        uint4 w[kTurns];
+        RowWalk walk(a, b, h, r - lane + lane / kLanes, kEach);
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            w[i] = make_uint4(0, 0, 0, 0);
+            if (r - lane + i * kEach + lane / kLanes < valid)
+                w[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + walk.at + 8 * part);
+            walk.next();
+        }
+        // (magnitudes in their order as 16-bit integers, two at a time; all rows at once, since a row's shuffles wait for one
+        // another)
+        uint32_t two[kTurns];
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i)
+            two[i] = __vmaxu2(__vmaxu2(w[i].x & 0x7fff7fffu, w[i].y & 0x7fff7fffu), __vmaxu2(w[i].z & 0x7fff7fffu, w[i].w & 0x7fff7fffu));
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1)
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) two[i] = __vmaxu2(two[i], __shfl_xor_sync(0xffffffffu, two[i], o));
+        // the lane's own row
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const uint32_t t = __shfl_sync(0xffffffffu, two[i], lane % kEach * kLanes);
+            if (i == lane / kEach) top = t;
+        }
+        float unused;
+        row_scale(__uint_as_float(max(top << 16, top & 0xffff0000u)), &unused, &factor);
+        factor = row_factor(a, factor);
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            float by, back, x[8];
+            row_scale(__uint_as_float(max(two[i] << 16, two[i] & 0xffff0000u)), &by, &back);
+            Chunk<__nv_bfloat16>::unpack(w[i], x);
+            const uint4 o = make_uint4(half2_bits(x[0] * by, x[1] * by), half2_bits(x[2] * by, x[3] * by),
+                                       half2_bits(x[4] * by, x[5] * by), half2_bits(x[6] * by, x[7] * by));
+            const int at = operand_at((warp & 3) * 32 + i * kEach + lane / kLanes, part);
+            *reinterpret_cast<uint4*>(smem + L::q + sub * L::kTile + at) = o;
+            if (keep_q) *reinterpret_cast<uint4*>(pr.q_tiles + tile128 * L::kTile + at) = o;
+        }
+        const bool real = r < valid;
+        lim = real ? sees(r) : 0;
+        if (keep_q) {
+            float* terms = terms_of(pr, tile128, my_row);
+            terms[0] = real ? factor : 0.f;
+            terms[2] = -INFINITY;
+            limits_of(pr, tile128)[my_row] = lim;
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_full[sub]);
+
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);      // (32 lanes further in bits 16 and up)
         const uint32_t s_col = lanes + sub * 128, o_col = lanes + 256 + sub * D;
         const float* ksp = a.c.scale[0] + (size_t)unit * a.c.NB;
