@@ -62,8 +62,8 @@ struct QcAttend {
     float2* part_ml;       // [2 n_warps][rows of a group]: running maximum (in powers of two) and sum
     int2* spans;           // [units][row groups]: the first and last warp that have blocks of them
     float2* ml;            // [units][R]: maximum, 1 / sum
-    float* scores;         // [units][C][R2], powers of two; NULL where the weights are formed from the keys again
-    int R2;                // R, rounded up to an even number where it is not 1
+    float* scores;         // [units][R][Cs], powers of two; NULL where the weights are formed from the keys again
+    int Cs;                // C, rounded up to whole blocks
 };
 // The tensor path's share of such a call (bct_qcache_prompt.cu).
 struct QcPrompt {
@@ -81,7 +81,6 @@ struct QcPlan {
     bool by_scores;        // the weights come from stored scores
     int n_warps;
     int64_t n_groups;
-    int R2;
     size_t part_o, part_ml, spans, ml, scores, q_tiles, records, total;
 };
 cudaError_t qc_attend(const QcAttend& a, const QcPlan& p, int dtype, cudaStream_t s);

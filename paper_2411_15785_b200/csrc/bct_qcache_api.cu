@@ -130,12 +130,11 @@ bct_status_t plan_attend(const QcView& v, int64_t T, int32_t n_q_heads, int32_t 
     p->n_groups = (R + p->rows - 1) / p->rows;
     p->by_scores = accumulate != 0 && R <= bct::kQcScoredRows;
     p->n_warps = (int)std::min<int64_t>(bct::qc_attend_max_warps(), units * p->n_groups * v.NB);
-    p->R2 = R == 1 ? 1 : (int)((std::min<int64_t>(R, bct::kQcScoredRows) + 1) / 2 * 2);
     p->part_o = take((size_t)2 * p->n_warps * p->rows * v.D * 4);
     p->part_ml = take((size_t)2 * p->n_warps * p->rows * 8);
     p->spans = take((size_t)units * p->n_groups * 8);
     p->ml = take((size_t)units * R * 8);
-    p->scores = take(p->by_scores ? (size_t)units * v.C * p->R2 * 4 : 0);
+    p->scores = take(p->by_scores ? (size_t)units * R * v.NB * bct::kQcBlock * 4 : 0);
     p->total = at;
     return BCT_OK;
 }
@@ -230,7 +229,7 @@ extern "C" bct_status_t bct_qcache_attend(const bct_qcache_t* cache, int64_t T, 
     a.spans = reinterpret_cast<int2*>(base + p.spans);
     a.ml = reinterpret_cast<float2*>(base + p.ml);
     a.scores = p.by_scores ? reinterpret_cast<float*>(base + p.scores) : nullptr;
-    a.R2 = p.R2;
+    a.Cs = a.c.NB * bct::kQcBlock;
     cudaError_t e;
     if (p.prompt) {
         if (accumulate != 0) {

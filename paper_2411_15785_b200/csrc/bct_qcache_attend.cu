@@ -28,6 +28,8 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
+
 #include "bct_device.cuh"
 #include "bct_internal.h"
 #include "bct_qcache.h"
@@ -42,9 +44,11 @@ constexpr int kQaWarps = 8;
 constexpr int kQaThreads = kQaWarps * 32;
 constexpr int kQaStages = 3;
 constexpr int kQaScored = kQcScoredRows;
-constexpr int kQjThreads = 256;
-constexpr int kQjSlots = 1024;        // slots of a CTA of the joining kernel
-constexpr float kPScale = 32768.f;    // of a probability on its way into fp16
+constexpr int kQjThreads = 128;
+constexpr int kQjResident = 8;        // CTAs of the joining kernel on an SM
+constexpr int kQjSlots = 4 * kQjThreads;   // slots that one of them takes at a time
+constexpr float kPBack = 32768.f;     // 2^15
+constexpr float kPShift = 15.f;       // of a probability on its way into fp16, in powers of two
 
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -195,9 +199,10 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
     constexpr int kRows = 8 * NT;
     extern __shared__ __align__(128) unsigned char qa_smem[];
     __shared__ int64_t upto[kQaThreads];
+    __shared__ float2 scales_all[kQaWarps][kQaStages];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     unsigned char* ring = qa_smem + warp * (kQaStages * 2 * kTile);
-    const uint32_t ring32 = smem_u32(ring);
+    const float2* scales = scales_all[warp];
 
     pdl_wait();
     pdl_open();
@@ -229,20 +234,78 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
             ++b;
         }
     }
-    int nb = (min(max(a.c.state[b], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
-    int64_t unit_in = (x - before) / nb;           // h * n_groups + group
-    int blk = (int)((x - before) - unit_in * nb);
+    // Where the run stands: its blocks are fetched two ahead of those that are worked on, across units.
+    struct Place {
+        int b, nb, unit_in, blk;   // sequence, its blocks, h * n_groups + group, block
+    };
+    auto blocks_of = [&](int b_) { return (min(max(a.c.state[b_], 0), a.c.C) + kQcBlock - 1) / kQcBlock; };
+    auto next_unit = [&](Place& p, bool more) {
+        p.blk = 0;
+        if (++p.unit_in == (int)per_seq && more) {
+            p.unit_in = 0;
+            do p.nb = blocks_of(++p.b);
+            while (p.nb == 0);
+        }
+    };
+    Place now;
+    now.b = b;
+    now.nb = blocks_of(b);
+    now.unit_in = (int)((x - before) / now.nb);
+    now.blk = (int)((x - before) - (int64_t)now.unit_in * now.nb);
+
+    Place ahead = now;
+    int64_t fetched = x;
+    const int8_t *kp = nullptr, *vp = nullptr;      // the fetched unit's, for this lane
+    const float *ksp = nullptr, *vsp = nullptr;
+    constexpr int kChunks = D / 16, kPer = 32 / kChunks;   // chunks of a slot, slots of an instruction
+    auto unit_of = [&](const Place& p) { return (int64_t)p.b * a.c.Hkv + p.unit_in / (int)a.n_groups; };
+    auto at_unit = [&]() {
+        const int64_t u = unit_of(ahead);
+        kp = a.c.codes[0] + (size_t)u * a.c.C * D + lane * 16;
+        vp = a.c.codes[1] + (size_t)u * a.c.C * D + lane * 16;
+        ksp = a.c.scale[0] + (size_t)u * a.c.NB;
+        vsp = a.c.scale[1] + (size_t)u * a.c.NB;
+    };
+    at_unit();
+    const uint32_t lane_at = smem_u32(ring) + tile_at<D>(lane / kChunks, lane % kChunks);
+    auto fetch = [&](int stage) {
+        if (fetched < end) {
+            const uint32_t dst = lane_at + stage * 2 * kTile;
+            const int left = a.c.C - ahead.blk * kQcBlock - lane / kChunks;      // slots of the lane that exist
+            const size_t from = (size_t)ahead.blk * kTile;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const int8_t* src = (p ? vp : kp) + from;
+#pragma unroll
+                for (int i = 0; i < kQcBlock / kPer; ++i) {   // (the swizzle of slot i * kPer + .. is that of i * kPer, in bits 4..6)
+                    const uint32_t to = (dst ^ (uint32_t)(tile_at<D>(i * kPer, 0) & 0x70)) + (p * kTile + i * kPer * D);
+                    if ((ahead.blk + 1) * kQcBlock <= a.c.C) cp_async16_zfill(to, src + i * kPer * D, true);
+                    else cp_async16_zfill(to, i * kPer < left ? src + i * kPer * D : kp, i * kPer < left);
+                }
+            }
+            if (lane < 2)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;"
+                             ::"r"(smem_u32(scales + stage) + lane * 4), "l"((lane ? vsp : ksp) + ahead.blk) : "memory");
+            ++fetched;
+            if (++ahead.blk == ahead.nb && fetched < end) {
+                next_unit(ahead, true);
+                at_unit();
+            }
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kQaStages - 1; ++s) fetch(s);
+    int stage = 0;
 
     while (x < end) {
-        const int h = (int)(unit_in / a.n_groups);
-        const int64_t group = unit_in - h * a.n_groups;
+        const int nb = now.nb, unit_in = now.unit_in;
+        b = now.b;
+        const int h = unit_in / (int)a.n_groups;
+        const int64_t group = unit_in - h * (int)a.n_groups;
         const int64_t unit = (int64_t)b * a.c.Hkv + h, r0 = group * kRows;
-        const int first = blk, last = (int)min((int64_t)nb, first + (end - x));   // this piece's blocks
+        const int first = now.blk, last = (int)min((int64_t)nb, first + (end - x));   // this piece's blocks
         const Sees sees = sees_of(a, b);
-        const int8_t* kp = a.c.codes[0] + (size_t)unit * a.c.C * D;
-        const int8_t* vp = a.c.codes[1] + (size_t)unit * a.c.C * D;
-        const float* ksp = a.c.scale[0] + (size_t)unit * a.c.NB;
-        const float* vsp = a.c.scale[1] + (size_t)unit * a.c.NB;
 
         // rows 2t, 2t + 1 of each tile of eight are this lane's in the scores and outputs, row g in the queries
         uint32_t q[NT][TERMS][D / 16][2];
@@ -267,25 +330,6 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
         lim_min = __reduce_min_sync(0xffffffffu, lim_min);
         const int stop = min(last, (lim_max + kQcBlock - 1) / kQcBlock);   // blocks behind it are hidden from all rows
 
-        auto fetch = [&](int blk_, int stage) {
-            if (blk_ < stop) {
-                const uint32_t dst = ring32 + stage * 2 * kTile;
-                constexpr int kChunks = D / 16, kPer = 32 / kChunks;   // chunks of a slot, slots of an instruction
-                const int c = lane % kChunks;
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const int8_t* src = p ? vp : kp;
-#pragma unroll
-                    for (int i = 0; i < kQcBlock / kPer; ++i) {
-                        const int s = i * kPer + lane / kChunks, slot = blk_ * kQcBlock + s;
-                        const bool real = slot < lim_max;
-                        cp_async16_zfill(dst + p * kTile + tile_at<D>(s, c), src + (size_t)(real ? slot : 0) * D + c * 16, real);
-                    }
-                }
-            }
-            cp_async_commit();
-        };
-
         float o[NT][kMt][4], m_run[NT][2], l_run[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -294,19 +338,17 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
             m_run[nt][0] = m_run[nt][1] = -INFINITY;
             l_run[nt][0] = l_run[nt][1] = 0.f;
         }
-#pragma unroll
-        for (int s = 0; s < kQaStages - 1; ++s) fetch(first + s, s);
-        int stage = 0;
-        for (int i = first; i < stop; ++i) {
-            const float ks = ksp[i], vs = vsp[i];
+        for (int i = first; i < last; ++i) {
             cp_async_wait<kQaStages - 2>();
             __syncwarp();
-            {
-                int to = stage + kQaStages - 1;
-                fetch(i + kQaStages - 1, to >= kQaStages ? to - kQaStages : to);
-            }
+            fetch(stage == 0 ? kQaStages - 1 : stage - 1);
             const unsigned char* tile = ring + stage * 2 * kTile;
+            const float ks = scales[stage].x, vs = scales[stage].y;
             if (++stage == kQaStages) stage = 0;
+            if (i >= stop) {
+                __syncwarp();
+                continue;
+            }
 
             float s[NT][2][4];
             {
@@ -329,15 +371,13 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
                         if (!all && slot0 + j >= lim[nt][e]) v = -INFINITY;
                         top[e] = fmaxf(top[e], v);
                     }
-                if (a.scores != nullptr && r0 + nt * 8 + 2 * t < a.R) {
-                    float* to = a.scores + ((size_t)unit * a.c.C + slot0) * a.R2 + r0 + nt * 8 + 2 * t;
+                if (a.scores != nullptr) {                    // rows of whole blocks: a lane's four slots side by side
+                    float* to = a.scores + ((size_t)unit * a.R + r0 + nt * 8 + 2 * t) * a.Cs + slot0;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (slot0 + j >= lim_max) break;
-                        const float* v = &s[nt][j >> 1][2 * (j & 1)];
-                        if (a.R2 == 1) to[j] = v[0];
-                        else *reinterpret_cast<float2*>(to + (size_t)j * a.R2) = make_float2(v[0], v[1]);
-                    }
+                    for (int e = 0; e < 2; ++e)
+                        if (r0 + nt * 8 + 2 * t + e < a.R)
+                            *reinterpret_cast<float4*>(to + (size_t)e * a.Cs) =
+                                make_float4(s[nt][0][e], s[nt][0][2 + e], s[nt][1][e], s[nt][1][2 + e]);
                 }
                 bool higher = false;
 #pragma unroll
@@ -357,15 +397,17 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
                         for (int f = 0; f < kMt; ++f) o[nt][f][e] *= by, o[nt][f][2 + e] *= by;
                     }
                 }
+                // P, and its sum, times 2^15 until the piece is done
+                float less[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) less[e] = (m_run[nt][e] == -INFINITY ? 0.f : m_run[nt][e]) - kPShift;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     float p[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float m = m_run[nt][e] == -INFINITY ? 0.f : m_run[nt][e];
-                        p[e] = ex2(s[nt][j >> 1][2 * (j & 1) + e] - m);
+                        p[e] = ex2(s[nt][j >> 1][2 * (j & 1) + e] - less[e]);
                         l_run[nt][e] += p[e];
-                        p[e] *= kPScale;
                     }
                     const uint32_t hi = half2_bits(p[0], p[1]);
                     pf[nt][0][j] = transposed(hi);
@@ -378,7 +420,6 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
 
             // V: for the slots 8 t + i (e = 0) and 8 t + 4 + i (e = 1) the lane's D / 8 features, 16 or 8 from 16 g or 8 g on
             const unsigned char* vt = tile + kTile;
-            const float vmul = vs * (1.f / kPScale);
 #pragma unroll
             for (int half = 0; half < D / 64; ++half) {       // 8 bytes of each slot at a time
                 uint2 w[2][4];
@@ -419,16 +460,13 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
                                     mma16816(acc, A[2 * k2][0], A[2 * k2][1], A[2 * k2 + 1][0], A[2 * k2 + 1][1],
                                              pf[nt][term][2 * k2], pf[nt][term][2 * k2 + 1]);
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) o[nt][f][c] = fmaf(acc[c], vmul, o[nt][f][c]);
+                            for (int c = 0; c < 4; ++c) o[nt][f][c] = fmaf(acc[c], vs, o[nt][f][c]);
                         }
                     }
                 }
             }
             __syncwarp();   // the stage may be filled again
         }
-        cp_async_wait<0>();
-        __syncwarp();
-
         // the piece's sums; a whole unit is done, a part goes to scratch
         const bool whole = first == 0 && last == nb;
         if (first == 0 && lane == 0)    // for who joins them: the first and last run that have blocks of these rows
@@ -454,39 +492,34 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
 #pragma unroll
                     for (int c = 0; c < kE / Chunk<T>::kElems; ++c)
                         *reinterpret_cast<uint4*>(to + c * Chunk<T>::kElems) = Chunk<T>::pack(y + c * Chunk<T>::kElems);
-                    if (g == 0) a.ml[unit * a.R + r] = make_float2(m_run[nt][e], inv);
+                    if (g == 0) a.ml[unit * a.R + r] = make_float2(m_run[nt][e], inv * kPBack);
                 } else {
                     float* to = a.part_o + (slot_no * kRows + row) * D + g * kE;
 #pragma unroll
                     for (int f = 0; f < kMt; f += 2)
                         *reinterpret_cast<float4*>(to + 2 * f) = make_float4(o[nt][f][e], o[nt][f][2 + e], o[nt][f + 1][e], o[nt][f + 1][2 + e]);
-                    if (g == 0) a.part_ml[slot_no * kRows + row] = make_float2(m_run[nt][e], l);
+                    if (g == 0) a.part_ml[slot_no * kRows + row] = make_float2(m_run[nt][e], l);   // (both times 2^15)
                 }
             }
 
         x += last - first;
-        blk = 0;
-        if (last == nb && x < end) {
-            if (++unit_in == per_seq) {
-                unit_in = 0;
-                do ++b, nb = (min(max(a.c.state[b], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
-                while (nb == 0);
-            }
-        }
+        now.blk = last;
+        if (last == nb && x < end) next_unit(now, true);
     }
+    cp_async_wait<0>();
 }
 
 // Joins what several warps have of a unit, writes the zeros of an empty cache's rows, and adds the weights from the stored
-// scores (SCORED).  A CTA per unit and kQjSlots of its slots, or, without scores, per unit and 8 of its rows; the rows that
+// scores (SCORED).  A CTA for some of a unit's slots, or, without scores, per unit and 8 of its rows; the rows that
 // a unit's CTAs join are shared out among them, and a row's parts, up to two for each warp that the call has, among the
-// CTA's threads.
-template <typename T, int D, bool SCORED>
-__global__ void __launch_bounds__(kQjThreads) qc_join_kernel(const QcAttend a, int ctas, int group_rows) {
-    constexpr int kLanes = D / 4, kSlices = kQjThreads / kLanes;   // four features of a lane; slices of a row's parts
-    constexpr int kEach = kQjSlots / kQjThreads;
-    __shared__ float2 row_ml[SCORED ? kQaScored : 1];
+// CTA's threads.  ONE: one row to a unit.
+template <typename T, int D, bool SCORED, bool ONE>
+__global__ void __launch_bounds__(kQjThreads, kQjResident) qc_join_kernel(const QcAttend a, int ctas, int group_rows, int share) {
+    // outputs are joined by pieces of 32 features, four of a lane, whose parts are shared out among groups of lanes
+    constexpr int kLanes = 8, kGroups = kQjThreads / kLanes, kPieces = D / 32;
+    __shared__ float2 row_ml[SCORED ? kQaScored : 8];
     __shared__ int row_sees[SCORED ? kQaScored : 1];
-    __shared__ float4 sums[kSlices][kLanes];
+    __shared__ float4 sums[kGroups][kLanes];
     const unsigned unit = blockIdx.x / (unsigned)ctas;
     const int part = (int)(blockIdx.x - unit * ctas);
     const int b = (int)(unit / (unsigned)a.c.Hkv), h = (int)unit - b * a.c.Hkv, tid = threadIdx.x;
@@ -495,104 +528,183 @@ __global__ void __launch_bounds__(kQjThreads) qc_join_kernel(const QcAttend a, i
     pdl_open();
     const Sees sees = sees_of(a, b);
     const int nb = (sees.held + kQcBlock - 1) / kQcBlock;
-    const int slot0 = part * kQjSlots + tid, end = sees.n > 0 ? min((part + 1) * kQjSlots, sees.held) : 0;
+    // The CTA's slots, kQjSlots at a time.  What a CTA does takes a few steps that wait for one another, so everything that can
+    // be loaded before it is known to be needed is (it exists in any case).
+    const int seen = sees.n > 0 ? sees.held : 0, chunks = (a.c.C + kQjSlots - 1) / kQjSlots;
+    const int chunk0 = SCORED ? chunks * part / ctas : 0, chunk1 = SCORED ? chunks * (part + 1) / ctas : 0;
     float* weight = a.c.weight + (size_t)unit * a.c.C;
-    const float* scores = a.scores + (size_t)unit * a.c.C * a.R2;
-    // (on their way while the rows' sums are formed)
-    float before[kEach], single[kEach];
-    if constexpr (SCORED) {
+    const float* scores = a.scores + (size_t)unit * a.R * a.Cs;
+    const bool quads = (a.c.C & 3) == 0;                       // a thread has four slots side by side
+    auto load_weights = [&](int j, float (&w)[4]) {
+        if (quads && j < a.c.C) {
+            const float4 v = *reinterpret_cast<const float4*>(weight + j);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        } else {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int j = slot0 + i * kQjThreads;
-            before[i] = j < end ? weight[j] : 0.f;
-            single[i] = j < end && a.R2 == 1 ? scores[j] : 0.f;
+            for (int i = 0; i < 4; ++i) w[i] = j + i < a.c.C ? weight[j + i] : 0.f;
         }
-    }
+    };
+    auto load_scores = [&](int r, int j) {
+        return j < a.c.C ? *reinterpret_cast<const float4*>(scores + (size_t)r * a.Cs + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+    };
+    // A turn: a chunk with its first four rows, or four chunks of one row; all of it on its way at once, the first turn's
+    // while the rows' sums are formed.
+    constexpr int kDeep = ONE ? 4 : 1;
+    float before[kDeep][4];
+    float4 early[4];
+    auto load_turn = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i)
+            if (c + i < chunk1) load_weights((c + i) * kQjSlots + 4 * tid, before[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (ONE ? c + i < chunk1 : i < (int)a.R) early[i] = load_scores(ONE ? 0 : i, (c + (ONE ? i : 0)) * kQjSlots + 4 * tid);
+    };
+    if constexpr (SCORED)
+        if (chunk0 < chunk1) load_turn(chunk0);
 
-    // the runs that have a row's group; where its parts are: 2 first + 1, then 2 run
-    auto span_of = [&](int64_t r) { return nb > 0 ? a.spans[unit * a.n_groups + r / group_rows] : make_int2(0, 0); };
-    auto place = [&](int64_t r, int run, int first) { return (2 * (int64_t)run + (run == first)) * group_rows + r % group_rows; };
+    // A row's group, the runs that have it (2 first + 1, then 2 run are their places), and its place in theirs.
+    struct Row {
+        unsigned group, in;
+        int first, last;
+    };
+    auto row_at = [&](int64_t r) {
+        Row w;
+        w.group = (unsigned)r / (unsigned)group_rows;
+        w.in = (unsigned)r - w.group * group_rows;
+        const int2 span = a.spans[(size_t)unit * a.n_groups + w.group];
+        w.first = nb > 0 ? span.x : 0, w.last = nb > 0 ? span.y : 0;
+        return w;
+    };
+    auto place = [&](const Row& w, int run) { return (2u * run + (run == w.first)) * group_rows + w.in; };
     // maximum and 1 / sum of a row, by a warp
-    auto join = [&](int64_t r, int2 span) {
+    auto join = [&](int64_t r, const Row& w) {
+        const float2 whole = a.ml[(size_t)unit * a.R + r];
         if (nb == 0) return make_float2(-INFINITY, 0.f);
-        if (span.x == span.y) return a.ml[(size_t)unit * a.R + r];
+        if (w.first == w.last) return whole;
         float m = -INFINITY, l = 0.f;
-        for (int i = span.x + lane; i <= span.y; i += 32) {
-            const float2 p = a.part_ml[place(r, i, span.x)];
-            const float top = fmaxf(m, p.x);
-            l = top == -INFINITY ? l + p.y : l * ex2(m - top) + p.y * ex2(p.x - top);   // (p.y is 0, or a NaN)
+        constexpr int kAt = 6;                                       // parts of a lane on their way together
+        for (int i0 = w.first + lane; i0 <= w.last; i0 += 32 * kAt) {
+            float2 p[kAt];
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < kAt; ++i) p[i] = i0 + 32 * i <= w.last ? a.part_ml[place(w, i0 + 32 * i)] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int i = 0; i < kAt; ++i) top = fmaxf(top, p[i].x);
+            const float ref = top == -INFINITY ? 0.f : top;          // (a part without slots: minus infinity and 0, or a NaN)
+            l *= ex2(m - ref);
+#pragma unroll
+            for (int i = 0; i < kAt; ++i) l += p[i].x == -INFINITY ? p[i].y : p[i].y * ex2(p[i].x - ref);
             m = top;
         }
         const float top = warp_max(m);
-        l = warp_sum(top == -INFINITY ? l : l * ex2(m - top));
-        return make_float2(top, l > 0.f ? 1.f / l : (l == l ? 0.f : l));
+        l = warp_sum(top == -INFINITY || m == -INFINITY ? l : l * ex2(m - top));
+        return make_float2(top, l > 0.f ? kPBack / l : (l == l ? 0.f : l));
     };
 
     if constexpr (SCORED) {                        // every row's, for the weights (R <= kQaScored)
         for (int r = warp; r < (int)a.R; r += kQjThreads / 32) {
-            const float2 v = join(r, span_of(r));
+            const float2 v = join(r, row_at(r));
             if (lane == 0) {
                 row_ml[r] = v;
                 row_sees[r] = v.y == 0.f ? 0 : sees(r);
             }
         }
         __syncthreads();
+#pragma unroll 1
+        for (int c = chunk0; c < chunk1 && c * kQjSlots < seen; c += kDeep) {
+            if (c > chunk0) load_turn(c);
+            auto add = [&](float (&w)[4], const float4& v, int r, int j) {
+                const float2 ml = row_ml[r];
+                const int lim = row_sees[r] - j;
+                if (lim > 0) w[0] += ex2(v.x - ml.x) * ml.y;
+                if (lim > 1) w[1] += ex2(v.y - ml.x) * ml.y;
+                if (lim > 2) w[2] += ex2(v.z - ml.x) * ml.y;
+                if (lim > 3) w[3] += ex2(v.w - ml.x) * ml.y;
+            };
+            const int j0 = c * kQjSlots + 4 * tid;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int j = slot0 + i * kQjThreads;
-            if (j >= end) break;
-            float w = 0.f;
-            if (a.R2 == 1) {
-                if (j < row_sees[0]) w = ex2(single[i] - row_ml[0].x) * row_ml[0].y;
-            } else {
-                const float2* s = reinterpret_cast<const float2*>(scores + (size_t)j * a.R2);
-#pragma unroll 4
-                for (int r = 0; r < (int)a.R; r += 2) {
-                    const float2 v = s[r / 2];
-                    if (j < row_sees[r]) w += ex2(v.x - row_ml[r].x) * row_ml[r].y;
-                    if (r + 1 < (int)a.R && j < row_sees[r + 1]) w += ex2(v.y - row_ml[r + 1].x) * row_ml[r + 1].y;
+            for (int i = 0; i < 4; ++i)
+                if (ONE ? c + i < chunk1 : i < (int)a.R) add(before[ONE ? i : 0], early[i], ONE ? 0 : i, j0 + (ONE ? i * kQjSlots : 0));
+            if constexpr (!ONE) {
+                for (int r = 4; r < (int)a.R; r += 4) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (r + i < (int)a.R) early[i] = load_scores(r + i, j0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (r + i < (int)a.R) add(before[0], early[i], r + i, j0);
                 }
             }
-            weight[j] = before[i] + w;
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                const int j = j0 + i * kQjSlots;
+                if (c + i >= chunk1 || j >= seen) continue;
+                if (quads) {                                   // (what stands behind the slots held stays as it was)
+                    *reinterpret_cast<float4*>(weight + j) = make_float4(before[i][0], before[i][1], before[i][2], before[i][3]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (j + k < seen) weight[j + k] = before[i][k];
+                }
+            }
         }
     }
-    const int64_t r_step = SCORED ? ctas : 1, r_end = SCORED ? a.R : min(a.R, (int64_t)(part + 1) * 8);
-    for (int64_t r = SCORED ? part : (int64_t)part * 8; r < r_end; r += r_step) {
-        const int2 span = span_of(r);
-        if (nb > 0 && span.x == span.y) continue;              // whole: its warp wrote it
-        float2 ml;
-        if constexpr (SCORED) {
-            ml = row_ml[r];
-        } else {
-            if (warp == 0) {
-                ml = join(r, span);
-                if (lane == 0) row_ml[0] = a.ml[(size_t)unit * a.R + r] = ml;
-            }
-            __syncthreads();
-            ml = row_ml[0];
-        }
-        const int slice = tid / kLanes, f = tid % kLanes;
-        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (nb > 0) {
-#pragma unroll 4
-            for (int i = span.x + slice; i <= span.y; i += kSlices) {
-                const int64_t at = place(r, i, span.x);
-                const float m = a.part_ml[at].x;
-                const float by = m == -INFINITY ? 0.f : ex2(m - ml.x) * ml.y;
-                const float4 o = *reinterpret_cast<const float4*>(a.part_o + at * D + 4 * f);
-                y.x = fmaf(o.x, by, y.x), y.y = fmaf(o.y, by, y.y), y.z = fmaf(o.z, by, y.z), y.w = fmaf(o.w, by, y.w);
+    // Outputs.  The CTA's pieces of rows side by side, `share` groups of lanes to each.
+    const int64_t r_first = SCORED ? 0 : (int64_t)part * 8;
+    const int rows = SCORED ? (int)a.R : (int)min((int64_t)8, a.R - r_first), step = SCORED ? ctas : 1;
+    if constexpr (!SCORED) {
+        for (int i = warp; i < rows; i += kQjThreads / 32) {
+            const Row w = row_at(r_first + i);
+            const float2 v = join(r_first + i, w);
+            if (lane == 0) {
+                row_ml[i] = v;
+                if (nb == 0 || w.first != w.last) a.ml[(size_t)unit * a.R + r_first + i] = v;
             }
         }
-        sums[slice][f] = y;
         __syncthreads();
-        if (slice == 0) {
+    }
+    const int from = SCORED ? part : 0, pieces = (rows * kPieces - from + step - 1) / step;
+    const int group = tid / kLanes, f = tid % kLanes, slice = group % share;
+    for (int base = 0; base < pieces; base += kGroups / share) {
+        const int no = base + group / share, piece = from + no * step, row = piece / kPieces, at_f = piece % kPieces * 32 + 4 * f;
+        const int64_t r = r_first + row;
+        bool mine = no < pieces;
+        Row w = {};
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (mine) {
+            w = row_at(r);
+            ml = row_ml[row];
+            mine = nb == 0 || w.first != w.last;                // (a whole one was written by its warp)
+        }
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (mine && nb > 0) {
+            for (int i0 = w.first + slice; i0 <= w.last; i0 += 4 * share) {   // four parts on their way together
+                float m[4];
+                float4 o[4];
 #pragma unroll
-            for (int i = 1; i < kSlices; ++i) {
-                const float4 o = sums[i][f];
+                for (int i = 0; i < 4; ++i) {
+                    const unsigned at = place(w, i0 + i * share);
+                    const bool there = i0 + i * share <= w.last;
+                    m[i] = there ? a.part_ml[at].x : -INFINITY;
+                    o[i] = there ? *reinterpret_cast<const float4*>(a.part_o + (size_t)at * D + at_f) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float by = m[i] == -INFINITY ? 0.f : ex2(m[i] - ml.x - kPShift) * ml.y;
+                    y.x = fmaf(o[i].x, by, y.x), y.y = fmaf(o[i].y, by, y.y), y.z = fmaf(o[i].z, by, y.z), y.w = fmaf(o[i].w, by, y.w);
+                }
+            }
+        }
+        sums[group][f] = y;
+        __syncthreads();
+        if (mine && slice == 0) {
+            for (int i = 1; i < share; ++i) {
+                const float4 o = sums[group + i][f];
                 y.x += o.x, y.y += o.y, y.z += o.z, y.w += o.w;
             }
             if (ml.y != ml.y) y = make_float4(ml.y, ml.y, ml.y, ml.y);
-            T* to = const_cast<T*>(row_of<T>(a, a.out, b, h, r)) + 4 * f;
+            T* to = const_cast<T*>(row_of<T>(a, a.out, b, h, r)) + at_f;
             if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = y;
             else *reinterpret_cast<uint2*>(to) = make_uint2(Chunk<T>::pack2(y.x, y.y), Chunk<T>::pack2(y.z, y.w));
         }
@@ -687,9 +799,16 @@ cudaError_t attend_of(const QcAttend& a, const QcPlan& p, cudaStream_t s) {
     else if constexpr (TERMS == 1) e = attend_with<T, D, 3, TERMS>(a, s);
     if (e != cudaSuccess) return e;
     const int64_t units = (int64_t)a.c.B * a.c.Hkv;
-    const int ctas = (int)(p.by_scores ? (a.c.C + kQjSlots - 1) / kQjSlots : (a.R + 7) / 8);
-    e = p.by_scores ? pdl_launch(qc_join_kernel<T, D, true>, (unsigned)(units * ctas), kQjThreads, 0, s, a, ctas, p.rows)
-                    : pdl_launch(qc_join_kernel<T, D, false>, (unsigned)(units * ctas), kQjThreads, 0, s, a, ctas, p.rows);
+    // with scores: a CTA for each kQjSlots slots, and four at least where there are rows and pieces to join, but no more
+    // than run side by side
+    const int64_t most = std::max<int64_t>((a.c.C + kQjSlots - 1) / kQjSlots, std::min<int64_t>(4, a.R));
+    const int64_t even = (148 * kQjResident + units - 1) / units;
+    const int ctas = (int)(p.by_scores ? std::min(most, even) : (a.R + 7) / 8);
+    // groups of lanes for a row's parts, four to each: by the arguments alone, as is the order of their sums
+    int share = 1;
+    while (share < 16 && share * 4 < a.n_warps / (units * a.n_groups) + 1) share *= 2;
+    const auto kernel = !p.by_scores ? qc_join_kernel<T, D, false, false> : a.R == 1 ? qc_join_kernel<T, D, true, true> : qc_join_kernel<T, D, true, false>;
+    e = pdl_launch(kernel, (unsigned)(units * ctas), kQjThreads, 0, s, a, ctas, p.rows, share);
     if constexpr (TERMS == 2) {   // (many bfloat16 rows are the tensor path's)
         if (e == cudaSuccess && a.accumulate != 0 && !p.by_scores)
             e = pdl_launch(qc_weights_kernel<T, D, TERMS>, (unsigned)(units * a.c.NB), kQaThreads, 0, s, a);
