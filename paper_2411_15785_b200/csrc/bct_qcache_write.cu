@@ -14,6 +14,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
+
 #include "bct_device.cuh"
 #include "bct_internal.h"
 #include "bct_qcache.h"
@@ -37,40 +39,45 @@ __device__ __forceinline__ int exact_code(float x, float lo, float s, float inv)
     else if (down < 0.f || (down == 0.f && odd)) q -= 1.f;
     return static_cast<int>(fminf(fmaxf(q, -127.f), 127.f));
 }
-template <int N>
-__device__ __forceinline__ uint32_t packed(const uint32_t (&u)[N]) {   // the low bytes
-    if constexpr (N == 4) return __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
-    else return __byte_perm(u[0], u[1], 0x0040) & 0xffffu;
+__device__ __forceinline__ uint32_t packed(const uint32_t (&u)[4]) {   // the low bytes
+    return __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
 }
-// N codes as the bytes of a word.  Adding 1.5 2^23 rounds x / s to an integer, whose low byte is the code; *far is the
+// Four codes as the bytes of a word.  Adding 1.5 2^23 rounds x / s to an integer, whose low byte is the code; *far is the
 // largest distance from it: only next to a half can it be the wrong one (x inv is off by 127.5 2^-24 = 7.6e-6 at most).
-template <int N>
-__device__ __forceinline__ uint32_t codes_of(const float (&x)[N], float inv, float* far) {
+__device__ __forceinline__ uint32_t codes_of(const float* x, float inv, float* far) {
     constexpr float kMagic = 12582912.f;
-    uint32_t u[N];
+    uint32_t u[4];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < 4; ++i) {
         const float m = fmaf(x[i], inv, kMagic);
         u[i] = __float_as_uint(m);
         *far = fmaxf(*far, fabsf(fmaf(x[i], inv, kMagic - m)));
     }
     return packed(u);
 }
-template <int N>
-__device__ __forceinline__ uint32_t exact_codes(const float (&x)[N], const float (&lo)[N], float s, float inv) {
-    uint32_t u[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) u[i] = (uint32_t)exact_code(x[i], lo[i], s, inv);
+// The exact ones of x + lo (out of the way of the loops that rarely need them).
+__device__ __noinline__ uint32_t exact_codes(float4 x, float4 lo, float s, float inv) {
+    const uint32_t u[4] = {(uint32_t)exact_code(x.x, lo.x, s, inv), (uint32_t)exact_code(x.y, lo.y, s, inv),
+                           (uint32_t)exact_code(x.z, lo.z, s, inv), (uint32_t)exact_code(x.w, lo.w, s, inv)};
     return packed(u);
 }
 constexpr float kNextToHalf = 0.49999f;
-// N codes divided by a power of two, ties to the even one
-template <int N>
+// Code i of a word as a float (and no conversion, of which there are few to a clock): the byte + 128 under the exponent of 2^23
+__device__ __forceinline__ float code_at(uint32_t w, int i) {
+    return __uint_as_float(__byte_perm(w ^ 0x80808080u, 0x4b000000u, 0x7440 | i)) - 8388736.f;
+}
+// The largest magnitude of the codes of a word, -127..127.
+__device__ __forceinline__ unsigned top_code(uint32_t w) {
+    const uint32_t minus = (w >> 7) & 0x01010101u, a = (w ^ (minus * 0xffu)) + minus;
+    const uint32_t two = __vmaxu2(a & 0x00ff00ffu, (a >> 8) & 0x00ff00ffu);
+    return max(two & 0xffffu, two >> 16);
+}
+// Four codes divided by a power of two, ties to the even one.
 __device__ __forceinline__ uint32_t shrunk(uint32_t w, float by) {
-    uint32_t out = 0;
+    uint32_t u[4];
 #pragma unroll
-    for (int i = 0; i < N; ++i) out |= (uint32_t)(uint8_t)(int8_t)(int)rintf((float)(int8_t)(w >> (8 * i)) * by) << (8 * i);
-    return out;
+    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(fmaf(code_at(w, i), by, 12582912.f));
+    return packed(u);
 }
 
 // The scale of a block that takes values up to amax, and the factor by which the codes it holds are multiplied.  64 bits
@@ -89,61 +96,48 @@ __device__ __forceinline__ float grown(float s, F amax, bool fresh, float* shrin
     return ldexpf(s, e);
 }
 
-// N features of a lane, as loaded
-template <typename T, int N>
-struct Row {
-    static constexpr int kWords = N * (int)sizeof(T) / 4;
-    uint32_t w[kWords];
-    __device__ __forceinline__ void load(const T* p) {
-        if constexpr (kWords == 4) {
-            const uint4 u = *reinterpret_cast<const uint4*>(p);
-            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-        } else if constexpr (kWords == 2) {
-            const uint2 u = *reinterpret_cast<const uint2*>(p);
-            w[0] = u.x, w[1] = u.y;
-        } else {
-            w[0] = *reinterpret_cast<const uint32_t*>(p);
-        }
+// Eight lanes share a row.  Of the features of new tokens a lane has 16 bytes in each 128 of the row (kE of them, whose codes
+// it stores together); of a row of codes, D / 8.
+template <typename T>
+struct Piece {
+    static constexpr int kE = 16 / (int)sizeof(T);
+    uint4 w;
+    // the largest magnitude, as the bits of a float (which are in its order; a NaN's and an infinity's come last); of
+    // bfloat16 in both halves of the word
+    __device__ __forceinline__ uint32_t top(uint32_t so_far) const {
+        if constexpr (sizeof(T) == 4)
+            return max(max(so_far, w.x & 0x7fffffffu), max(w.y & 0x7fffffffu, max(w.z & 0x7fffffffu, w.w & 0x7fffffffu)));
+        else
+            return __vmaxu2(__vmaxu2(so_far, w.x & 0x7fff7fffu), __vmaxu2(w.y & 0x7fff7fffu, __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu)));
     }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) w[i] = 0;
-    }
-    __device__ __forceinline__ void values(float (&x)[N]) const {
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = __uint_as_float(w[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) {
-                x[2 * i] = __uint_as_float(w[i] << 16);
-                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            }
-        }
-    }
+    __device__ __forceinline__ static uint32_t top_of(uint32_t t) { return sizeof(T) == 4 ? t : max(t << 16, t & 0xffff0000u); }
 };
-
-// N codes of a lane, as the N bytes of a word
 template <int N>
-__device__ __forceinline__ uint32_t load_codes(const int8_t* p) {
-    if constexpr (N == 4) return *reinterpret_cast<const uint32_t*>(p);
-    else return *reinterpret_cast<const uint16_t*>(p);
+__device__ __forceinline__ void load_words(const int8_t* p, uint32_t (&w)[N]) {
+    if constexpr (N == 4) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    } else if constexpr (N == 2) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        w[0] = u.x, w[1] = u.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
 }
 template <int N>
-__device__ __forceinline__ void store_codes(int8_t* p, uint32_t w) {
-    if constexpr (N == 4) *reinterpret_cast<uint32_t*>(p) = w;
-    else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w;
+__device__ __forceinline__ void store_words(int8_t* p, const uint32_t (&w)[N]) {
+    if constexpr (N == 4) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else if constexpr (N == 2) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(p) = w[0];
 }
-__device__ __forceinline__ float code_at(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
 
-// Largest magnitude of a plane's four warps; a NaN or an infinity in any of them makes it a NaN.
-__device__ __forceinline__ float plane_amax(float mine, float (*share)[4], int plane, int part) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mine = max_nan(mine, __shfl_xor_sync(0xffffffffu, mine, o));
+// Largest magnitude (its bits) of a plane's four warps, as a float; a NaN or an infinity in any of them makes it a NaN.
+__device__ __forceinline__ float plane_amax(uint32_t mine, uint32_t (*share)[4], int plane, int part) {
+    mine = __reduce_max_sync(0xffffffffu, mine);
     if ((threadIdx.x & 31) == 0) share[plane][part] = mine;
     __syncthreads();
-    const float amax = max_nan(max_nan(share[plane][0], share[plane][1]), max_nan(share[plane][2], share[plane][3]));
-    return amax <= 3.402823466e38f ? amax : __uint_as_float(0x7fffffffu);
+    const uint32_t amax = max(max(share[plane][0], share[plane][1]), max(share[plane][2], share[plane][3]));
+    return __uint_as_float(amax < 0x7f800000u ? amax : 0x7fffffffu);
 }
 
 // ---- append -----------------------------------------------------------------------------------------------------
@@ -151,9 +145,11 @@ __device__ __forceinline__ float plane_amax(float mine, float (*share)[4], int p
 // length on: all of them have read it by then.
 template <typename T, int D>
 __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? 6 : 4) qc_append_kernel(const QcAppend a) {
-    constexpr int kN = D / 32;
-    __shared__ float share[2][4];
+    constexpr int kE = Piece<T>::kE, kC = D * (int)sizeof(T) / 128;   // pieces of a lane in a row
+    constexpr int kTurns = kQwRows / 4, kW = D / 32;                  // turns of four rows; words of a lane in a row of codes
+    __shared__ uint32_t share[2][4];
     pdl_wait();
+    pdl_open();
     // the heads of a block of tokens run side by side: they stand side by side in memory
     const int h = blockIdx.x % a.c.Hkv, bw = blockIdx.x / a.c.Hkv, w = bw % a.W, b = bw / a.W, unit = b * a.c.Hkv + h;
     const int C = a.c.C;
@@ -164,62 +160,58 @@ __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? 6 : 4) qc_append_
     if (lo < held + n && n > 0) {
         const int plane = threadIdx.x >> 7, part = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
         const int first = max(held, lo), last = min(held + n, lo + kQcBlock);   // the new slots of this block
-        int8_t* codes = a.c.codes[plane] + (size_t)unit * C * D;
+        // the lane's rows: row0, and 4 further on at each turn
+        const int row0 = lo + part * kQwRows + (lane >> 3), l8 = lane & 7;
+        int8_t* codes = a.c.codes[plane] + ((size_t)unit * C + row0) * D;
         float* scale = a.c.scale[plane] + (size_t)unit * a.c.NB + blk;
-        const T* x = static_cast<const T*>(a.x[plane]);
-        Row<T, kN> row[kQwRows];
-#pragma unroll
-        for (int i = 0; i < kQwRows; ++i) {
-            const int slot = lo + part * kQwRows + i;
-            if (slot >= first && slot < last) row[i].load(x + (((size_t)b * a.T + (slot - held)) * a.c.Hkv + h) * D + lane * kN);
-            else row[i].clear();
-        }
+        const int64_t step = 4 * (int64_t)a.c.Hkv * D;
+        const T* x = static_cast<const T*>(a.x[plane]) + (((int64_t)b * a.T + (row0 - held)) * a.c.Hkv + h) * D + l8 * kE;
+        auto is_new = [&](int i) { return row0 + 4 * i >= first && row0 + 4 * i < last; };
+        Piece<T> in[kTurns][kC];
+        uint32_t top = 0;
         const float old = *scale;
-        float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < kQwRows; ++i) {
-            float y[kN];
-            row[i].values(y);
+        for (int i = 0; i < kTurns; ++i) {
+            const bool there = is_new(i);
 #pragma unroll
-            for (int j = 0; j < kN; ++j) top = max_nan(top, fabsf(y[j]));
+            for (int c = 0; c < kC; ++c) in[i][c].w = there ? *reinterpret_cast<const uint4*>(x + i * step + c * 8 * kE) : make_uint4(0, 0, 0, 0);
         }
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+            for (int c = 0; c < kC; ++c) top = in[i][c].top(top);
         // (all have read the old scale when its barrier lets them go)
-        const float amax = plane_amax(top, share, plane, part);
+        const float amax = plane_amax(Piece<T>::top_of(top), share, plane, part);
         float shrink;
         const float s = grown(old, amax, first == lo, &shrink), inv = s > 0.f ? 1.f / s : 0.f;
-        unsigned again = 0;                                 // rows with a value next to a half
 #pragma unroll
-        for (int i = 0; i < kQwRows; ++i) {
-            const int slot = lo + part * kQwRows + i;
-            float y[kN], far = 0.f;
-            row[i].values(y);
-            const uint32_t c = s > 0.f ? codes_of(y, inv, &far) : 0;
-            if (far > kNextToHalf) again |= 1u << i;
-            if (slot >= first && slot < last) store_codes<kN>(codes + (size_t)slot * D + lane * kN, c);
-        }
-#pragma unroll 1
-        for (; again != 0; again &= again - 1) {
-            const int slot = lo + part * kQwRows + __ffs(again) - 1;
-            if (slot < first || slot >= last || !(s > 0.f)) continue;
-            Row<T, kN> one;
-            one.load(x + (((size_t)b * a.T + (slot - held)) * a.c.Hkv + h) * D + lane * kN);
-            float y[kN];
-            one.values(y);
-            const float none[kN] = {};
-            store_codes<kN>(codes + (size_t)slot * D + lane * kN, exact_codes(y, none, s, inv));
+        for (int i = 0; i < kTurns; ++i) {
+            if (!is_new(i)) continue;
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+                float y[kE];
+                Chunk<T>::unpack(in[i][c].w, y);
+                uint32_t out[kE / 4];
+#pragma unroll
+                for (int k = 0; k < kE / 4; ++k) {
+                    float far = 0.f;
+                    out[k] = s > 0.f ? codes_of(y + 4 * k, inv, &far) : 0;
+                    if (far > kNextToHalf)
+                        out[k] = exact_codes(make_float4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]), make_float4(0.f, 0.f, 0.f, 0.f), s, inv);
+                }
+                store_words(codes + i * 4 * D + (c * 8 + l8) * kE, out);
+            }
         }
         if (shrink != 1.f) {                                // (what stands behind the new end too: a block's codes have one scale)
-            uint32_t held_codes[kQwRows];
 #pragma unroll
-            for (int i = 0; i < kQwRows; ++i) {
-                const int slot = lo + part * kQwRows + i;
-                if (slot < C && (slot < first || slot >= last)) held_codes[i] = load_codes<kN>(codes + (size_t)slot * D + lane * kN);
-            }
+            for (int i = 0; i < kTurns; ++i) {
+                if (is_new(i) || row0 + 4 * i >= C) continue;
+                uint32_t w[kW];
+                int8_t* p = codes + i * 4 * D + l8 * (D / 8);
+                load_words(p, w);
 #pragma unroll
-            for (int i = 0; i < kQwRows; ++i) {
-                const int slot = lo + part * kQwRows + i;
-                if (slot < C && (slot < first || slot >= last))
-                    store_codes<kN>(codes + (size_t)slot * D + lane * kN, shrunk<kN>(held_codes[i], shrink));
+                for (int k = 0; k < kW; ++k) w[k] = shrunk(w[k], shrink);
+                store_words(p, w);
             }
         }
         if (part == 0 && lane == 0) *scale = s;
@@ -286,6 +278,7 @@ __global__ void __launch_bounds__(THREADS) qc_select_kernel(const QcEvict a) {
     __shared__ int found[3];
     const int unit = blockIdx.x, b = unit / a.c.Hkv, C = a.c.C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_wait();
+    pdl_open();
     const int held = min(max(a.c.state[b], 0), C), from = a.c.state[a.c.B + b] - a.recent;
     const int n = held - a.keep;
     if (n <= 0) {
@@ -404,104 +397,147 @@ __global__ void __launch_bounds__(THREADS) qc_select_kernel(const QcEvict a) {
     }
 }
 
-// A warp per block with holes and plane: the slots that move in come with the codes and scale of where they were, eight
-// rows in flight.  (Four warps to a block, as an append has, would be idle where a block has a few holes.)
-constexpr int kQmRows = 8;
+// A warp per block with holes and plane: the slots that move in come with the codes and scale of where they were, four
+// rows at a time.  (Four warps to a block, as an append has, would be idle where a block has a few holes.)  What a block
+// needs is found in steps that wait for one another, list, slots, codes, so a warp goes from block to block and looks up the
+// next one's slots while this one's codes are on their way.
+constexpr int kQmResident = 5;   // CTAs on an SM
 template <int D>
-__global__ void __launch_bounds__(kQwThreads) qc_move_kernel(const QcEvict a, int per_unit) {
-    constexpr int kN = D / 32;
+__global__ void __launch_bounds__(kQwThreads, kQmResident) qc_move_kernel(const QcEvict a, int per_unit, int64_t items) {
+    constexpr int kW = D / 32;   // words of a lane in a row of codes
     const int lane = threadIdx.x & 31, plane = (threadIdx.x >> 5) & 1, C = a.c.C;
-    const int64_t item = (int64_t)blockIdx.x * (kQwThreads / 64) + (threadIdx.x >> 6);
-    const int unit = (int)(item / per_unit), no = (int)(item - (int64_t)unit * per_unit);
-    if (unit >= a.c.B * a.c.Hkv) return;
+    const int64_t stride = (int64_t)gridDim.x * (kQwThreads / 64);
     pdl_wait();
-    const int n_blocks = a.n_blocks[unit];
-    const int4 e = a.max_blocks > 0 ? a.blocks[(size_t)unit * a.max_blocks + no] : make_int4(0, 0, 0, 0);
-    if (no == 0 && plane == 0 && unit % a.c.Hkv == 0 && lane == 0 && a.n_out[unit] > 0) a.c.state[unit / a.c.Hkv] = a.keep;
-    if (no >= n_blocks) return;
-    const int lo = e.x * kQcBlock;
-    const unsigned holes = (unsigned)e.z;
-    const int count = __popc(holes);
-    int8_t* codes = a.c.codes[plane] + (size_t)unit * C * D + lane * kN;
-    float* scales = a.c.scale[plane] + (size_t)unit * a.c.NB;
-    const int kept = min(kQcBlock, a.keep - lo);
-    const unsigned all = kept == kQcBlock ? 0xffffffffu : (1u << kept) - 1u;
-    const bool fresh = holes == all;
-
-    // lane i: the i-th hole, the slot that moves there and its scale (the block that the new end cuts takes slots in and
-    // gives some away: its scale is the one before)
-    const int src = lane < count ? a.movers[(size_t)unit * a.max_moves + e.y + lane] : 0;
-    int dst = lo;
-    for (unsigned m = holes, i = 0; m != 0; m &= m - 1, ++i)
-        if (i == (unsigned)lane) dst = lo + __ffs(m) - 1;
-    const float old = scales[e.x];
-    uint32_t word[kQmRows];
-    auto load = [&](int i0) {
-#pragma unroll
-        for (int i = 0; i < kQmRows; ++i)
-            if (i0 + i < count) word[i] = load_codes<kN>(codes + (size_t)__shfl_sync(0xffffffffu, src, i0 + i) * D);
+    pdl_open();
+    struct Item {
+        int unit;
+        bool some;               // a block with holes
+        int4 e;                  // block, first hole's number, mask of holes
+        int src;                 // lane i: the slot that moves into the i-th hole
+        float old;               // the block's scale
     };
-    load(0);
-    float from = 0.f;
-    if (lane < count) from = src / kQcBlock == a.keep / kQcBlock ? a.cut_scale[2 * unit + plane] : scales[src / kQcBlock];
-    double amax = 0.;
-    for (int i0 = 0;;) {
-        // row by row: the largest |code| times its scale, exact in 64 bits
-#pragma unroll
-        for (int i = 0; i < kQmRows; ++i) {
-            if (i0 + i < count) {
-                int top = 0;
-#pragma unroll
-                for (int j = 0; j < kN; ++j) top = max(top, abs((int)(int8_t)(word[i] >> (8 * j))));
-                amax = fmax(amax, (double)top * (double)__shfl_sync(0xffffffffu, from, i0 + i));
-            }
+    auto look = [&](int64_t at) {
+        Item t = {};
+        if (at >= items) return t;
+        t.unit = (int)((unsigned)at / (unsigned)per_unit);
+        const int no = (int)((unsigned)at - (unsigned)t.unit * per_unit);
+        const int n_blocks = a.n_blocks[t.unit];
+        if (a.max_blocks > 0) t.e = a.blocks[(size_t)t.unit * a.max_blocks + no];
+        if (no == 0 && plane == 0 && t.unit % a.c.Hkv == 0 && lane == 0 && a.n_out[t.unit] > 0) a.c.state[t.unit / a.c.Hkv] = a.keep;
+        t.some = no < n_blocks;
+        return t;
+    };
+    auto find = [&](Item& t) {
+        if (!t.some) return;
+        t.src = lane < __popc(t.e.z) ? a.movers[(size_t)t.unit * a.max_moves + t.e.y + lane] : 0;
+        t.old = a.c.scale[plane][(size_t)t.unit * a.c.NB + t.e.x];
+    };
+    int64_t at = (int64_t)blockIdx.x * (kQwThreads / 64) + (threadIdx.x >> 6);
+    Item next = look(at);
+    find(next);
+    for (; at < items; at += stride) {
+        const Item now = next;
+        next = look(at + stride);
+        if (!now.some) {
+            find(next);
+            continue;
         }
-        if ((i0 += kQmRows) >= count) break;
-        load(i0);
-    }
+        const int unit = now.unit, lo = now.e.x * kQcBlock, src = now.src;
+        const float old = now.old;
+        const unsigned holes = (unsigned)now.e.z;
+        const int count = __popc(holes);
+        int8_t* codes = a.c.codes[plane] + (size_t)unit * C * D + (lane & 7) * (D / 8);
+        float* scales = a.c.scale[plane] + (size_t)unit * a.c.NB;
+        const int kept = min(kQcBlock, a.keep - lo);
+        const unsigned all = kept == kQcBlock ? 0xffffffffu : (1u << kept) - 1u;
+        const bool fresh = holes == all;
+
+        // four rows at a time, eight lanes to each: the lane's is the (i0 + lane / 8)-th
+        uint32_t w[kW];
+        auto load = [&](int i0) {
+            const int no = i0 + (lane >> 3), slot = __shfl_sync(0xffffffffu, src, no & 31);
+            if (no < count) load_words(codes + (size_t)slot * D, w);
+        };
+        load(0);
+        // (the block that the new end cuts takes slots in and gives some away: its scale is the one before)
+        float from = 0.f;
+        if (lane < count) from = src / kQcBlock == a.keep / kQcBlock ? a.cut_scale[2 * unit + plane] : scales[src / kQcBlock];
+        find(next);
+        int dst = lo;            // lane i: the i-th hole
+        for (unsigned m = holes, i = 0; m != 0; m &= m - 1, ++i)
+            if (i == (unsigned)lane) dst = lo + __ffs(m) - 1;
+        // the largest |code| of a row: its product with the row's scale is exact in 64 bits
+        double amax = 0.;
+        for (int i0 = 0;;) {
+            const int no = i0 + (lane >> 3);
+            unsigned top = 0;
+            if (no < count) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) amax = fmax(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    if (__any_sync(0xffffffffu, !(fabsf(from) <= 3.402823466e38f))) amax = nan("");
-    float shrink;
-    const float s = grown(old, amax, fresh, &shrink), inv = s > 0.f ? 1.f / s : 0.f;
-    if (count > kQmRows) load(0);
-    for (int i0 = 0;;) {
+                for (int k = 0; k < kW; ++k) top = max(top, top_code(w[k]));
+            }
+            amax = fmax(amax, (double)top * (double)__shfl_sync(0xffffffffu, from, no & 31));
+            if ((i0 += 4) >= count) break;
+            load(i0);
+        }
+        if (__any_sync(0xffffffffu, !(fabsf(from) <= 3.402823466e38f))) amax = nan("");
+        const unsigned bits = __reduce_max_sync(0xffffffffu, __float_as_uint((float)amax) & 0x7fffffffu);
+        float s = old, shrink = 1.f;
+        if (fresh || old == 0.f || !(__uint_as_float(bits) < 127.4f * old)) {   // (or not a number)
 #pragma unroll
-        for (int i = 0; i < kQmRows; ++i) {
-            if (i0 + i < count) {
-                const float f = __shfl_sync(0xffffffffu, from, i0 + i);
-                const int to = __shfl_sync(0xffffffffu, dst, i0 + i);
-                float x[kN], rest[kN], far = 0.f;
+            for (int o = 16; o > 0; o >>= 1) amax = fmax(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            s = grown(old, bits < 0x7f800000u ? amax : nan(""), fresh, &shrink);
+        }
+        const float inv = s > 0.f ? 1.f / s : 0.f;
+        if (count > 4) load(0);
+        for (int i0 = 0;;) {
+            const int no = i0 + (lane >> 3);
+            const float f = __shfl_sync(0xffffffffu, from, no & 31);
+            const int to = __shfl_sync(0xffffffffu, dst, no & 31);
+            if (no < count) {
 #pragma unroll
-                for (int j = 0; j < kN; ++j) {
-                    const float code = code_at(word[i], j);
-                    x[j] = code * f;
-                    rest[j] = fmaf(code, f, -x[j]);
+                for (int k = 0; k < kW; ++k) {
+                    float x[4], far = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = code_at(w[k], j) * f;
+                    uint32_t c = s > 0.f ? codes_of(x, inv, &far) : 0;
+                    if (far > kNextToHalf) {
+                        float rest[4];                       // what the products lost
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) rest[j] = fmaf(code_at(w[k], j), f, -x[j]);
+                        c = exact_codes(make_float4(x[0], x[1], x[2], x[3]), make_float4(rest[0], rest[1], rest[2], rest[3]), s, inv);
+                    }
+                    w[k] = c;
                 }
-                uint32_t c = s > 0.f ? codes_of(x, inv, &far) : 0;
-                if (far > kNextToHalf && s > 0.f) c = exact_codes(x, rest, s, inv);
-                store_codes<kN>(codes + (size_t)to * D, c);
+                store_words(codes + (size_t)to * D, w);
+            }
+            if ((i0 += 4) >= count) break;
+            load(i0);
+        }
+        if (shrink != 1.f) {
+            const unsigned stay = all & ~holes;
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                uint32_t v[4][kW];
+                const unsigned mine = stay >> (16 * half + (lane >> 3));
+                int8_t* p = codes + (size_t)(lo + 16 * half + (lane >> 3)) * D;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if ((mine >> (4 * i)) & 1) load_words(p + 4 * i * D, v[i]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!((mine >> (4 * i)) & 1)) continue;
+#pragma unroll
+                    for (int k = 0; k < kW; ++k) v[i][k] = shrunk(v[i][k], shrink);
+                    store_words(p + 4 * i * D, v[i]);
+                }
             }
         }
-        if ((i0 += kQmRows) >= count) break;
-        load(i0);
-    }
-    if (shrink != 1.f) {
-        const unsigned stay = all & ~holes;
-        for (int i0 = 0; i0 < kept; i0 += kQmRows) {
-#pragma unroll
-            for (int i = 0; i < kQmRows; ++i)
-                if ((stay >> (i0 + i)) & 1) word[i] = load_codes<kN>(codes + (size_t)(lo + i0 + i) * D);
-#pragma unroll
-            for (int i = 0; i < kQmRows; ++i)
-                if ((stay >> (i0 + i)) & 1) store_codes<kN>(codes + (size_t)(lo + i0 + i) * D, shrunk<kN>(word[i], shrink));
+        if (lane == 0) scales[now.e.x] = s;
+        if (plane == 0 && lane < count) {
+            const size_t u = (size_t)unit * C;
+            a.c.weight[u + dst] = a.c.weight[u + src];
+            a.c.position[u + dst] = a.c.position[u + src];
         }
-    }
-    if (lane == 0) scales[e.x] = s;
-    if (plane == 0 && lane < count) {
-        const size_t u = (size_t)unit * C;
-        a.c.weight[u + dst] = a.c.weight[u + src];
-        a.c.position[u + dst] = a.c.position[u + src];
     }
 }
 
@@ -527,9 +563,10 @@ cudaError_t qc_evict(const QcEvict& a, cudaStream_t s) {
     if (smem > 32768 && (e = allow_smem(kernel, kQsKeys * 4, &done[small])) != cudaSuccess) return e;
     if ((e = pdl_launch(kernel, units, small ? 256 : 1024, smem, s, a)) != cudaSuccess) return e;
     const int per_unit = a.max_blocks > 0 ? a.max_blocks : 1;
-    const unsigned grid = (unsigned)(((int64_t)units * per_unit + kQwThreads / 64 - 1) / (kQwThreads / 64));
-    return a.c.D == 128 ? pdl_launch(qc_move_kernel<128>, grid, kQwThreads, 0, s, a, per_unit)
-                        : pdl_launch(qc_move_kernel<64>, grid, kQwThreads, 0, s, a, per_unit);
+    const int64_t items = (int64_t)units * per_unit, ctas = (items + kQwThreads / 64 - 1) / (kQwThreads / 64);
+    const unsigned grid = (unsigned)std::min<int64_t>(ctas, 148 * kQmResident);
+    return a.c.D == 128 ? pdl_launch(qc_move_kernel<128>, grid, kQwThreads, 0, s, a, per_unit, items)
+                        : pdl_launch(qc_move_kernel<64>, grid, kQwThreads, 0, s, a, per_unit, items);
 }
 
 }  // namespace bct
