@@ -27,6 +27,7 @@ struct QcAppend {
     const int32_t* lens;   // or NULL
     int64_t T;
     int W;                 // blocks of a cache that T tokens touch at most
+    int ctas;              // that share a unit's blocks (set by qc_append)
 };
 cudaError_t qc_append(const QcAppend& a, int dtype, cudaStream_t s);
 

@@ -175,8 +175,8 @@ extern "C" bct_status_t bct_qcache_append(const bct_qcache_t* cache, int64_t T, 
     s[kCacheSpans + 1] = {"new v", v, bytes};
     s[kCacheSpans + 2] = {"lens", lens, (size_t)a.c.B * 4};
     if (bct_status_t st = check_overlap(s, kCacheSpans + 3, kCacheSpans)) return st;
-    a.x[0] = k, a.x[1] = v, a.lens = lens, a.T = T;
-    a.W = (int)std::min<int64_t>((T + bct::kQcBlock - 1) / bct::kQcBlock + 1, a.c.NB);
+    a.x[0] = k, a.x[1] = v, a.lens = lens, a.T = T, a.ctas = 0;
+    a.W = (int)std::min<int64_t>((T + bct::kQcBlock - 2) / bct::kQcBlock + 1, a.c.NB);   // (one token touches one)
     if (!grid_fits((int64_t)a.c.B * a.c.Hkv, a.W)) return fail(BCT_ERR_INVALID_ARG, "batch, heads and T too large for one call");
     const cudaError_t e = bct::qc_append(a, dtype, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? BCT_OK : fail_cuda("bct_qcache_append", e);

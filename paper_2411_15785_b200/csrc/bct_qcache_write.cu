@@ -141,47 +141,66 @@ __device__ __forceinline__ float plane_amax(uint32_t mine, uint32_t (*share)[4],
 }
 
 // ---- append -----------------------------------------------------------------------------------------------------
-// A CTA per (sequence, head, block of the cache that the new tokens may touch).  The last CTA of a sequence moves its
-// length on: all of them have read it by then.
+// A few CTAs per (sequence, head) go through the blocks that its new tokens touch, the next block's tokens on their way while
+// this one's are worked on.  The last CTA of a sequence to have read its length moves it on.
+constexpr int kQwResident = 4;    // CTAs on an SM
 template <typename T, int D>
-__global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? 6 : 4) qc_append_kernel(const QcAppend a) {
+__global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? kQwResident : 2) qc_append_kernel(const QcAppend a) {
     constexpr int kE = Piece<T>::kE, kC = D * (int)sizeof(T) / 128;   // pieces of a lane in a row
     constexpr int kTurns = kQwRows / 4, kW = D / 32;                  // turns of four rows; words of a lane in a row of codes
-    __shared__ uint32_t share[2][4];
+    __shared__ uint32_t share[2][2][4];
     pdl_wait();
     pdl_open();
     // the heads of a block of tokens run side by side: they stand side by side in memory
-    const int h = blockIdx.x % a.c.Hkv, bw = blockIdx.x / a.c.Hkv, w = bw % a.W, b = bw / a.W, unit = b * a.c.Hkv + h;
+    const int h = blockIdx.x % a.c.Hkv, bw = blockIdx.x / a.c.Hkv, w0 = bw % a.ctas, b = bw / a.ctas, unit = b * a.c.Hkv + h;
     const int C = a.c.C;
     const int held = min(max(a.c.state[b], 0), C), seen = a.c.state[a.c.B + b];
     const int64_t want = a.lens == nullptr ? a.T : min((int64_t)max(a.lens[b], 0), a.T);
-    const int n = (int)min(want, (int64_t)(C - held));
-    const int blk = held / kQcBlock + w, lo = blk * kQcBlock;
-    if (lo < held + n && n > 0) {
-        const int plane = threadIdx.x >> 7, part = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
-        const int first = max(held, lo), last = min(held + n, lo + kQcBlock);   // the new slots of this block
-        // the lane's rows: row0, and 4 further on at each turn
-        const int row0 = lo + part * kQwRows + (lane >> 3), l8 = lane & 7;
+    const int n = (int)min(want, (int64_t)(C - held)), end = held + n;
+    const int plane = threadIdx.x >> 7, part = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, l8 = lane & 7;
+    const int blk_end = n > 0 ? (end - 1) / kQcBlock + 1 : 0;
+    __syncthreads();          // all of this CTA have the sequence's state (their bounds are made of it)
+    int ticket = 0;
+    if (threadIdx.x == 0) ticket = atomicAdd(reinterpret_cast<int*>(a.c.state + 2 * a.c.B + b), 1);
+
+    const int row_in = part * kQwRows + (lane >> 3);          // the lane's rows of a block: this one, and 4 further on at each turn
+    const int64_t step = 4 * (int64_t)a.c.Hkv * D;
+    const T* const x0 = static_cast<const T*>(a.x[plane]) + ((int64_t)b * a.T * a.c.Hkv + h) * D + l8 * kE;
+    float* const scales = a.c.scale[plane] + (size_t)unit * a.c.NB;
+    Piece<T> ahead[kTurns][kC];
+    float old_ahead = 0.f;
+    auto fetch = [&](int blk) {
+        if (blk >= blk_end) return;
+        const int row0 = blk * kQcBlock + row_in;
+        const T* x = x0 + (int64_t)(row0 - held) * a.c.Hkv * D;
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const bool there = row0 + 4 * i >= held && row0 + 4 * i < end;
+#pragma unroll
+            for (int c = 0; c < kC; ++c)
+                ahead[i][c].w = there ? *reinterpret_cast<const uint4*>(x + i * step + c * 8 * kE) : make_uint4(0, 0, 0, 0);
+        }
+        old_ahead = scales[blk];
+    };
+    int turn = 0;
+    int blk = held / kQcBlock + w0;
+    fetch(blk);
+    for (; blk < blk_end; blk += a.ctas, turn ^= 1) {
+        const int lo = blk * kQcBlock, first = max(held, lo), last = min(end, lo + kQcBlock), row0 = lo + row_in;
         int8_t* codes = a.c.codes[plane] + ((size_t)unit * C + row0) * D;
-        float* scale = a.c.scale[plane] + (size_t)unit * a.c.NB + blk;
-        const int64_t step = 4 * (int64_t)a.c.Hkv * D;
-        const T* x = static_cast<const T*>(a.x[plane]) + (((int64_t)b * a.T + (row0 - held)) * a.c.Hkv + h) * D + l8 * kE;
         auto is_new = [&](int i) { return row0 + 4 * i >= first && row0 + 4 * i < last; };
         Piece<T> in[kTurns][kC];
         uint32_t top = 0;
-        const float old = *scale;
-#pragma unroll
-        for (int i = 0; i < kTurns; ++i) {
-            const bool there = is_new(i);
-#pragma unroll
-            for (int c = 0; c < kC; ++c) in[i][c].w = there ? *reinterpret_cast<const uint4*>(x + i * step + c * 8 * kE) : make_uint4(0, 0, 0, 0);
-        }
 #pragma unroll
         for (int i = 0; i < kTurns; ++i)
 #pragma unroll
-            for (int c = 0; c < kC; ++c) top = in[i][c].top(top);
-        // (all have read the old scale when its barrier lets them go)
-        const float amax = plane_amax(Piece<T>::top_of(top), share, plane, part);
+            for (int c = 0; c < kC; ++c) {
+                in[i][c] = ahead[i][c];
+                top = in[i][c].top(top);
+            }
+        const float old = old_ahead;
+        fetch(blk + a.ctas);
+        const float amax = plane_amax(Piece<T>::top_of(top), share[turn], plane, part);
         float shrink;
         const float s = grown(old, amax, first == lo, &shrink), inv = s > 0.f ? 1.f / s : 0.f;
 #pragma unroll
@@ -214,7 +233,9 @@ __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? 6 : 4) qc_append_
                 store_words(p, w);
             }
         }
-        if (part == 0 && lane == 0) *scale = s;
+        // (the plane's warps have read the old scale: the barrier above came after their loads of it were used or not, and
+        // no other block of this loop has the same)
+        if (part == 0 && lane == 0) scales[blk] = s;
         if (plane == 0 && part == 0) {
             const int slot = lo + lane;
             if (slot >= first && slot < last) {
@@ -223,14 +244,10 @@ __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? 6 : 4) qc_append_
             }
         }
     }
-    __syncthreads();   // all of this CTA have read the sequence's state (have it: their branches went by it)
-    if (threadIdx.x == 0) {
-        int* done = reinterpret_cast<int*>(a.c.state + 2 * a.c.B + b);
-        if (atomicAdd(done, 1) == a.W * a.c.Hkv - 1) {
-            a.c.state[b] = held + n;
-            a.c.state[a.c.B + b] = seen + n;
-            *done = 0;
-        }
+    if (threadIdx.x == 0 && ticket == a.ctas * a.c.Hkv - 1) {
+        a.c.state[b] = end;
+        a.c.state[a.c.B + b] = seen + n;
+        a.c.state[2 * a.c.B + b] = 0;
     }
 }
 
@@ -543,8 +560,13 @@ __global__ void __launch_bounds__(kQwThreads, kQmResident) qc_move_kernel(const 
 
 }  // namespace
 
-cudaError_t qc_append(const QcAppend& a, int dtype, cudaStream_t s) {
-    const unsigned grid = (unsigned)((int64_t)a.c.B * a.c.Hkv * a.W);
+cudaError_t qc_append(const QcAppend& args, int dtype, cudaStream_t s) {
+    QcAppend a = args;
+    const int64_t units = (int64_t)a.c.B * a.c.Hkv;
+    // As many CTAs as run side by side, where there are as many blocks; four blocks to each at most, so that sequences of
+    // unlike lengths even out.
+    a.ctas = (int)std::max<int64_t>(std::min<int64_t>(a.W, 148 * kQwResident / units), (a.W + 3) / 4);
+    const unsigned grid = (unsigned)(units * a.ctas);
     if (dtype == BCT_BF16)
         return a.c.D == 128 ? pdl_launch(qc_append_kernel<__nv_bfloat16, 128>, grid, kQwThreads, 0, s, a)
                             : pdl_launch(qc_append_kernel<__nv_bfloat16, 64>, grid, kQwThreads, 0, s, a);
