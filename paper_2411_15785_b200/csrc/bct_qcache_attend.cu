@@ -74,28 +74,63 @@ __device__ __forceinline__ int tile_at(int slot, int chunk) {
     else return (slot >> 1) * 128 + (((((slot & 1) << 2) | chunk) ^ x) << 4);
 }
 
-// upto[thread]: the blocks of the sequences up to the end of its share of them, `chunk_out` sequences.  Returns all blocks.
-__device__ __forceinline__ int64_t count_blocks(const QcAttend& a, int64_t* upto, int* chunk_out) {
-    const int chunk = (a.c.B + blockDim.x - 1) / blockDim.x;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int64_t x = 0;
-    for (int i = 0; i < chunk; ++i) {
-        const int b = tid * chunk + i;
-        if (b < a.c.B) x += (min(max(a.c.state[b], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
+// Blocks of a sequence.
+__device__ __forceinline__ int blocks_of(const QcAttend& a, int b) {
+    return (min(max(a.c.state[b], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
+}
+// Block x of all sequences', per_seq times each: its sequence, the blocks (times per_seq) of those before, and of all.  x is
+// made of the total by `where`.  Up to 32 sequences are a warp's own affair; more are added up by the CTA, which then calls
+// this with all its threads (upto: a word for each).
+template <typename F>
+__device__ __forceinline__ int64_t find_block(const QcAttend& a, int64_t per_seq, int64_t* upto, F where, int64_t* x, int* seq,
+                                              int64_t* before) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = a.c.B;
+    if (B <= 32) {
+        int64_t sum = lane < B ? blocks_of(a, lane) : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += y;
+        }
+        const int64_t total = __shfl_sync(0xffffffffu, sum, 31) * per_seq;
+        *x = where(total);
+        const int behind = __popc(__ballot_sync(0xffffffffu, sum * per_seq <= *x));   // sequences that end before it
+        *seq = behind;
+        *before = behind ? __shfl_sync(0xffffffffu, sum, behind - 1 & 31) * per_seq : 0;
+        return total;
     }
+    const int chunk = (B + blockDim.x - 1) / blockDim.x;
+    int64_t sum = 0;
+    for (int i = 0; i < chunk; ++i)
+        if (tid * chunk + i < B) sum += blocks_of(a, tid * chunk + i);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
+        const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += y;
     }
     __shared__ int64_t warps[32];
-    if (lane == 31) warps[warp] = x;
+    if (lane == 31) warps[warp] = sum;
     __syncthreads();
-    for (int i = 0; i < warp; ++i) x += warps[i];
-    upto[tid] = x;
+    for (int i = 0; i < warp; ++i) sum += warps[i];
+    upto[tid] = sum;
     __syncthreads();
-    *chunk_out = chunk;
-    return upto[blockDim.x - 1];
+    const int64_t total = upto[blockDim.x - 1] * per_seq;
+    *x = where(total);
+    if (*x >= total) return total;
+    int lo = 0, hi = blockDim.x - 1;               // first thread's share that ends behind x
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (upto[mid] * per_seq > *x) hi = mid; else lo = mid + 1;
+    }
+    *seq = lo * chunk;
+    *before = (lo ? upto[lo - 1] : 0) * per_seq;
+    for (;;) {
+        const int64_t nb = blocks_of(a, *seq);
+        if (*before + nb * per_seq > *x) break;
+        *before += nb * per_seq;
+        ++*seq;
+    }
+    return total;
 }
 // The warp whose run has block x of `total` in all, of n runs (n <= total).
 __device__ __forceinline__ int run_of(int64_t x, int64_t total, int n) { return (int)(((x + 1) * n - 1) / total); }
@@ -206,50 +241,35 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
 
     pdl_wait();
     pdl_open();
-    int chunk;
+    // where the run begins: its sequence, then the unit and row group within
     const int64_t per_seq = (int64_t)a.c.Hkv * a.n_groups;
-    const int64_t total = count_blocks(a, upto, &chunk) * per_seq;
-    if (total == 0) return;
-    const int n_runs = (int)min((int64_t)a.n_warps, total);
     const int run = warp * gridDim.x + blockIdx.x;
+    int n_runs, b;
+    int64_t x, before;    // blocks of the sequences before b, times per_seq
+    const int64_t total = find_block(a, per_seq, upto,
+                                     [&](int64_t all) {
+                                         n_runs = (int)min((int64_t)a.n_warps, all);
+                                         return run < n_runs ? all * run / n_runs : all;
+                                     },
+                                     &x, &b, &before);
     if (run >= n_runs) return;
-    int64_t x = total * run / n_runs;
     const int64_t end = total * (run + 1) / n_runs;
 
-    // where the run begins: its sequence, then the unit and row group within
-    int b;
-    int64_t before;       // blocks of the sequences before b, times per_seq
-    {
-        int lo = 0, hi = kQaThreads - 1;           // first thread's share that ends behind x
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (upto[mid] * per_seq > x) hi = mid; else lo = mid + 1;
-        }
-        b = lo * chunk;
-        before = (lo ? upto[lo - 1] : 0) * per_seq;
-        for (;;) {
-            const int64_t nb = (min(max(a.c.state[b], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
-            if (before + nb * per_seq > x) break;
-            before += nb * per_seq;
-            ++b;
-        }
-    }
     // Where the run stands: its blocks are fetched two ahead of those that are worked on, across units.
     struct Place {
         int b, nb, unit_in, blk;   // sequence, its blocks, h * n_groups + group, block
     };
-    auto blocks_of = [&](int b_) { return (min(max(a.c.state[b_], 0), a.c.C) + kQcBlock - 1) / kQcBlock; };
     auto next_unit = [&](Place& p, bool more) {
         p.blk = 0;
         if (++p.unit_in == (int)per_seq && more) {
             p.unit_in = 0;
-            do p.nb = blocks_of(++p.b);
+            do p.nb = blocks_of(a, ++p.b);
             while (p.nb == 0);
         }
     };
     Place now;
     now.b = b;
-    now.nb = blocks_of(b);
+    now.nb = blocks_of(a, b);
     now.unit_in = (int)((x - before) / now.nb);
     now.blk = (int)((x - before) - (int64_t)now.unit_in * now.nb);
 
@@ -514,7 +534,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
 // a unit's CTAs join are shared out among them, and a row's parts, up to two for each warp that the call has, among the
 // CTA's threads.  ONE: one row to a unit.
 template <typename T, int D, bool SCORED, bool ONE>
-__global__ void __launch_bounds__(kQjThreads, kQjResident) qc_join_kernel(const QcAttend a, int ctas, int group_rows, int share) {
+__global__ void __launch_bounds__(kQjThreads, kQjResident) qc_join_kernel(const QcAttend a, int ctas, int group_rows, int share, int ml_lanes, int rows_each) {
     // outputs are joined by pieces of 32 features, four of a lane, whose parts are shared out among groups of lanes
     constexpr int kLanes = 8, kGroups = kQjThreads / kLanes, kPieces = D / 32;
     __shared__ float2 row_ml[SCORED ? kQaScored : 8];
@@ -577,18 +597,19 @@ __global__ void __launch_bounds__(kQjThreads, kQjResident) qc_join_kernel(const 
         return w;
     };
     auto place = [&](const Row& w, int run) { return (2u * run + (run == w.first)) * group_rows + w.in; };
-    // maximum and 1 / sum of a row, by a warp
-    auto join = [&](int64_t r, const Row& w) {
-        const float2 whole = a.ml[(size_t)unit * a.R + r];
-        if (nb == 0) return make_float2(-INFINITY, 0.f);
-        if (w.first == w.last) return whole;
+    // Maximum and 1 / sum of a row, by ml_lanes lanes (8, or 32 where a row has many parts).  All lanes of a warp call it.
+    const int ml_at = tid & (ml_lanes - 1), ml_group = tid / ml_lanes, ml_groups = kQjThreads / ml_lanes;
+    auto join = [&](bool real, int64_t r, const Row& w) {
+        const float2 whole = real ? a.ml[(size_t)unit * a.R + r] : make_float2(0.f, 0.f);
         float m = -INFINITY, l = 0.f;
         constexpr int kAt = 6;                                       // parts of a lane on their way together
-        for (int i0 = w.first + lane; i0 <= w.last; i0 += 32 * kAt) {
+        const int last = real && nb > 0 && w.first < w.last ? w.last : -1;
+        for (int i0 = w.first + ml_at; i0 <= last; i0 += ml_lanes * kAt) {
             float2 p[kAt];
             float top = m;
 #pragma unroll
-            for (int i = 0; i < kAt; ++i) p[i] = i0 + 32 * i <= w.last ? a.part_ml[place(w, i0 + 32 * i)] : make_float2(-INFINITY, 0.f);
+            for (int i = 0; i < kAt; ++i)
+                p[i] = i0 + ml_lanes * i <= last ? a.part_ml[place(w, i0 + ml_lanes * i)] : make_float2(-INFINITY, 0.f);
 #pragma unroll
             for (int i = 0; i < kAt; ++i) top = fmaxf(top, p[i].x);
             const float ref = top == -INFINITY ? 0.f : top;          // (a part without slots: minus infinity and 0, or a NaN)
@@ -597,15 +618,19 @@ __global__ void __launch_bounds__(kQjThreads, kQjResident) qc_join_kernel(const 
             for (int i = 0; i < kAt; ++i) l += p[i].x == -INFINITY ? p[i].y : p[i].y * ex2(p[i].x - ref);
             m = top;
         }
-        const float top = warp_max(m);
-        l = warp_sum(top == -INFINITY || m == -INFINITY ? l : l * ex2(m - top));
-        return make_float2(top, l > 0.f ? kPBack / l : (l == l ? 0.f : l));
+        float top = m;
+        for (int o = 1; o < ml_lanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (top != -INFINITY && m != -INFINITY) l *= ex2(m - top);
+        for (int o = 1; o < ml_lanes; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        if (nb == 0) return make_float2(-INFINITY, 0.f);
+        return last >= 0 ? make_float2(top, l > 0.f ? kPBack / l : (l == l ? 0.f : l)) : whole;
     };
 
     if constexpr (SCORED) {                        // every row's, for the weights (R <= kQaScored)
-        for (int r = warp; r < (int)a.R; r += kQjThreads / 32) {
-            const float2 v = join(r, row_at(r));
-            if (lane == 0) {
+        for (int r0 = 0; r0 < (int)a.R; r0 += ml_groups) {
+            const int r = r0 + ml_group;
+            const float2 v = join(r < (int)a.R, r, row_at(min(r, (int)a.R - 1)));
+            if (ml_at == 0 && r < (int)a.R) {
                 row_ml[r] = v;
                 row_sees[r] = v.y == 0.f ? 0 : sees(r);
             }
@@ -651,13 +676,14 @@ __global__ void __launch_bounds__(kQjThreads, kQjResident) qc_join_kernel(const 
         }
     }
     // Outputs.  The CTA's pieces of rows side by side, `share` groups of lanes to each.
-    const int64_t r_first = SCORED ? 0 : (int64_t)part * 8;
-    const int rows = SCORED ? (int)a.R : (int)min((int64_t)8, a.R - r_first), step = SCORED ? ctas : 1;
+    const int64_t r_first = SCORED ? 0 : (int64_t)part * rows_each;
+    const int rows = SCORED ? (int)a.R : (int)min((int64_t)rows_each, a.R - r_first), step = SCORED ? ctas : 1;
     if constexpr (!SCORED) {
-        for (int i = warp; i < rows; i += kQjThreads / 32) {
-            const Row w = row_at(r_first + i);
-            const float2 v = join(r_first + i, w);
-            if (lane == 0) {
+        for (int i0 = 0; i0 < rows; i0 += ml_groups) {
+            const int i = i0 + ml_group;
+            const Row w = row_at(r_first + min(i, rows - 1));
+            const float2 v = join(i < rows, r_first + i, w);
+            if (ml_at == 0 && i < rows) {
                 row_ml[i] = v;
                 if (nb == 0 || w.first != w.last) a.ml[(size_t)unit * a.R + r_first + i] = v;
             }
@@ -799,16 +825,20 @@ cudaError_t attend_of(const QcAttend& a, const QcPlan& p, cudaStream_t s) {
     else if constexpr (TERMS == 1) e = attend_with<T, D, 3, TERMS>(a, s);
     if (e != cudaSuccess) return e;
     const int64_t units = (int64_t)a.c.B * a.c.Hkv;
-    // with scores: a CTA for each kQjSlots slots, and four at least where there are rows and pieces to join, but no more
-    // than run side by side
-    const int64_t most = std::max<int64_t>((a.c.C + kQjSlots - 1) / kQjSlots, std::min<int64_t>(4, a.R));
+    // With scores: a CTA for each kQjSlots slots, or for each four pieces of the outputs, but no more than run side by side.
+    // Without: eight rows to a CTA, or one where they are few.
     const int64_t even = (148 * kQjResident + units - 1) / units;
-    const int ctas = (int)(p.by_scores ? std::min(most, even) : (a.R + 7) / 8);
-    // groups of lanes for a row's parts, four to each: by the arguments alone, as is the order of their sums
+    const int64_t most = std::max<int64_t>((a.c.C + kQjSlots - 1) / kQjSlots, a.R <= 4 ? a.R * (D / 32) : a.R * (D / 32) / 4);
+    const int rows_each = units * a.R <= 148 * kQjResident ? 1 : 8;
+    const int ctas = (int)(p.by_scores ? std::min(most, even) : (a.R + rows_each - 1) / rows_each);
+    // Groups of lanes for a row's parts, four parts to each, and lanes for their sums: by the arguments alone, as is the order
+    // of the sums then.
+    const int64_t parts = a.n_warps / (units * a.n_groups) + 1;
     int share = 1;
-    while (share < 16 && share * 4 < a.n_warps / (units * a.n_groups) + 1) share *= 2;
+    while (share < 16 && share * 4 < parts) share *= 2;
+    const int ml_lanes = parts > 48 ? 32 : 8;
     const auto kernel = !p.by_scores ? qc_join_kernel<T, D, false, false> : a.R == 1 ? qc_join_kernel<T, D, true, true> : qc_join_kernel<T, D, true, false>;
-    e = pdl_launch(kernel, (unsigned)(units * ctas), kQjThreads, 0, s, a, ctas, p.rows, share);
+    e = pdl_launch(kernel, (unsigned)(units * ctas), kQjThreads, 0, s, a, ctas, p.rows, share, ml_lanes, rows_each);
     if constexpr (TERMS == 2) {   // (many bfloat16 rows are the tensor path's)
         if (e == cudaSuccess && a.accumulate != 0 && !p.by_scores)
             e = pdl_launch(qc_weights_kernel<T, D, TERMS>, (unsigned)(units * a.c.NB), kQaThreads, 0, s, a);
