@@ -87,6 +87,33 @@ __device__ __forceinline__ float tanh_near(float x) {
     p = fmaf(y, p, -0.33332839608192444f);
     return x * fmaf(y, p, 0.9999999403953552f);
 }
+// two at a time (there are instructions for pairs of floats)
+__device__ __forceinline__ uint64_t f2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ void tanh_near2(float& a, float& b) {
+    auto both = [](float c) { return f2(c, c); };
+    const uint64_t x = f2(a, b), y = mul2(x, x);
+    uint64_t p = fma2(y, both(0.001041022245772183f), both(-0.006203378085047007f));
+    p = fma2(y, p, both(0.020289979875087738f));
+    p = fma2(y, p, both(-0.05345702916383743f));
+    p = fma2(y, p, both(0.13325203955173492f));
+    p = fma2(y, p, both(-0.33332839608192444f));
+    p = mul2(x, fma2(y, p, both(0.9999999403953552f)));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p));
+}
 __device__ __forceinline__ float tanh_any(float x) {
     if (!(fabsf(x) > 1.f)) return tanh_near(x);   // (a NaN too)
     const float e = ex2(fminf(fabsf(x), 16.f) * (2.f * kLog2e));

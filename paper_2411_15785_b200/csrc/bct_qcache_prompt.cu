@@ -157,7 +157,7 @@ __device__ __forceinline__ void tanh32(float (&s)[32]) {
         for (int j = 0; j < 32; ++j) s[j] = far[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) s[j] = tanh_near(s[j]);
+        for (int j = 0; j < 32; j += 2) tanh_near2(s[j], s[j + 1]);
     }
 }
 
