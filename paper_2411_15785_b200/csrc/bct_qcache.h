@@ -9,7 +9,7 @@
 namespace bct {
 
 constexpr int kQcBlock = BCT_QCACHE_BLOCK;   // slots that share a scale
-constexpr int kQcScoredRows = 32;            // rows of a unit up to which the weights come from stored scores
+constexpr int kQcScoredRows = 24;            // rows of a unit up to which the weights come from stored scores
 
 // The caller's cache, resolved: planes by (sequence, kv-head) unit, state by sequence.
 struct QcView {
@@ -70,6 +70,8 @@ struct QcAttend {
 struct QcPrompt {
     int tiles;             // of 256 rows, per unit
     int splits;            // CTAs that share the slots of a tile of rows
+    int by_slots;          // one tile of 128 rows to a unit: a CTA's two sets of accumulators share its slots
+    int parts;             // partial results of a row
     unsigned char* q_tiles;   // [units][2 tiles] of 128 rows: queries as operands; NULL without weights
     unsigned char* records;   // their rows' terms
 };

@@ -113,9 +113,11 @@ bct_status_t plan_attend(const QcView& v, int64_t T, int32_t n_q_heads, int32_t 
         // a CTA per SM, but four tiles of 128 slots to each at least
         p->pr.tiles = (int)tiles;
         p->pr.splits = (int)std::max<int64_t>(1, std::min<int64_t>(148 / (units * tiles), v.C / 512));
-        if (p->pr.splits > 1) {
-            p->part_o = take((size_t)units * R * p->pr.splits * v.D * 4);
-            p->part_ml = take((size_t)units * R * p->pr.splits * 8);
+        p->pr.by_slots = R <= 128;
+        p->pr.parts = p->pr.splits * (p->pr.by_slots ? 2 : 1);
+        if (p->pr.parts > 1) {
+            p->part_o = take((size_t)units * R * p->pr.parts * v.D * 4);
+            p->part_ml = take((size_t)units * R * p->pr.parts * 8);
         }
         if (accumulate) {
             p->q_tiles = take((size_t)units * tiles * 256 * v.D * 2);

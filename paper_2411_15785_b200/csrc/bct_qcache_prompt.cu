@@ -20,6 +20,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "bct_device.cuh"
@@ -211,6 +212,11 @@ struct Codes {
             for (int i = 0; i < kRaw; ++i) raw[i] = i * THREADS < most ? from[i * THREADS] : make_uint4(0, 0, 0, 0);
         }
     }
+    // asks for a tile that comes later to be brought into L2
+    __device__ __forceinline__ static void ahead(const int8_t* unit, int slot0, int end, int t) {
+        const int lines = min(128, end - slot0) * D / 128;
+        for (int i = t; i < lines; i += THREADS) asm volatile("prefetch.global.L2 [%0];" ::"l"(unit + (size_t)slot0 * D + i * 128));
+    }
     __device__ __forceinline__ void store(unsigned char* tile, int t) const {
         const int row = t / kPer, c = t % kPer * 2;
         // (the lanes of the second half of a row begin with the other chunk: no two lanes at the same banks)
@@ -302,6 +308,8 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
     const int lim_max = rows > 0 ? sees(r0 + rows - 1) : 0, lim_min = rows > 0 ? sees(r0) : 0;
     const int all_tiles = (lim_max + kQpSlots - 1) / kQpSlots;
     const int lo = (int)((int64_t)all_tiles * split / pr.splits), hi = (int)((int64_t)all_tiles * (split + 1) / pr.splits);
+    // Two tiles of rows, or, where a unit has one, its tiles of slots in turn to each of two sets of accumulators.
+    const bool by_slots = pr.by_slots != 0;
     const int N = hi - lo, subs = rows > 128 ? 2 : 1;
     const int8_t* kp = a.c.codes[0] + (size_t)unit * a.c.C * D;
     const int8_t* vp = a.c.codes[1] + (size_t)unit * a.c.C * D;
@@ -340,32 +348,52 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
             for (int hf = 0; hf < D / 64; ++hf)
                 umma4_kk(tmem + g * 128, dk.at(qa + hf * (kQpHalf / 16)), dk.at(ka + hf * (kQpHalf / 16)), id_s, hf > 0);
             commit_warp(&s_full[g]);
-            if (g == subs - 1) commit_warp(&k_empty[n & 1]);
+            if (by_slots || g == subs - 1) commit_warp(&k_empty[n & 1]);
         };
-        if (N > 0) {
-            qp_wait(&k_full[0], 0, abort_flag);
-            for (int g = 0; g < subs; ++g) {
-                qp_wait(&q_full[g], 0, abort_flag);
-                tc_fence_after();
-                scores(0, g);
-            }
-        }
-        for (int n = 0; n < N; ++n) {
+        auto outputs = [&](int n, int g, int turn) {
             const uint32_t va = base16 + (L::v + (n & 1) * L::kTile) / 16;
-            for (int g = 0; g < subs; ++g) {
-                if (g == 0) qp_wait(&v_full[n & 1], n >> 1, abort_flag);
-                qp_wait(&p_full[g], n, abort_flag);
-                tc_fence_after();
-                umma4_tm(tmem + 256 + g * D, tmem + g * 128, dmn.at(va), id_o, n > 0);
-                umma4_tm(tmem + 256 + g * D, tmem + g * 128 + 32, dmn.at(va + 512), id_o, true);
-                commit_warp(&o_full[g]);
-                if (g == subs - 1) commit_warp(&v_empty[n & 1]);
-                if (n + 1 < N) {
-                    if (g == 0) {
-                        qp_wait(&k_full[(n + 1) & 1], (n + 1) >> 1, abort_flag);
-                        tc_fence_after();
+            qp_wait(&p_full[g], turn, abort_flag);
+            tc_fence_after();
+            umma4_tm(tmem + 256 + g * D, tmem + g * 128, dmn.at(va), id_o, turn > 0);
+            umma4_tm(tmem + 256 + g * D, tmem + g * 128 + 32, dmn.at(va + 512), id_o, true);
+            commit_warp(&o_full[g]);
+            if (by_slots || g == subs - 1) commit_warp(&v_empty[n & 1]);
+        };
+        auto wait_k = [&](int n) {
+            qp_wait(&k_full[n & 1], n >> 1, abort_flag);
+            tc_fence_after();
+        };
+        if (by_slots) {
+            for (int n = 0; n < min(N, 2); ++n) {
+                qp_wait(&q_full[n], 0, abort_flag);
+                wait_k(n);
+                scores(n, n);
+            }
+            for (int n = 0; n < N; ++n) {
+                qp_wait(&v_full[n & 1], n >> 1, abort_flag);
+                outputs(n, n & 1, n >> 1);
+                if (n + 2 < N) {
+                    wait_k(n + 2);
+                    scores(n + 2, n & 1);          // (after the product that reads P from its place)
+                }
+            }
+        } else {
+            if (N > 0) {
+                wait_k(0);
+                for (int g = 0; g < subs; ++g) {
+                    qp_wait(&q_full[g], 0, abort_flag);
+                    tc_fence_after();
+                    scores(0, g);
+                }
+            }
+            for (int n = 0; n < N; ++n) {
+                for (int g = 0; g < subs; ++g) {
+                    if (g == 0) qp_wait(&v_full[n & 1], n >> 1, abort_flag);
+                    outputs(n, g, n);
+                    if (n + 1 < N) {
+                        if (g == 0) wait_k(n + 1);
+                        scores(n + 1, g);
                     }
-                    scores(n + 1, g);      // (after the product that reads P from its place)
                 }
             }
         }
@@ -377,8 +405,17 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
             k.load(kp, lo * kQpSlots, lim_max, t);
             v.load(vp, lo * kQpSlots, lim_max, t);
         }
+        constexpr int kAhead = 4;      // (a tile's loads are one tile ahead, which DRAM takes longer than)
+        for (int n = 1; n < min(N, kAhead); ++n) {
+            k.ahead(kp, (lo + n) * kQpSlots, lim_max, t);
+            v.ahead(vp, (lo + n) * kQpSlots, lim_max, t);
+        }
         for (int n = 0; n < N; ++n) {
             const int st = n & 1;
+            if (n + kAhead < N) {
+                k.ahead(kp, (lo + n + kAhead) * kQpSlots, lim_max, t);
+                v.ahead(vp, (lo + n + kAhead) * kQpSlots, lim_max, t);
+            }
             if (n >= 2) qp_wait(&k_empty[st], (n >> 1) - 1, abort_flag);
             k.store(smem + L::k + st * L::kTile, t);
             if (n + 1 < N) k.load(kp, (lo + n + 1) * kQpSlots, lim_max, t);
@@ -396,9 +433,9 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
         // =========================== queries, softmax ===========================
         const int sub = warp >> 2;                                          // of warps 0-7: the tile of rows
         const int my_row = (warp & 3) * 32 + lane;
-        const int64_t r = r0 + sub * 128 + my_row;
+        const int64_t r = r0 + (by_slots ? 0 : sub * 128) + my_row;
         const size_t tile128 = ((size_t)unit * pr.tiles + (size_t)(r0 / kQpRows)) * 2 + sub;
-        const bool keep_q = pr.q_tiles != nullptr && split == 0;            // for the pass that forms the weights
+        const bool keep_q = pr.q_tiles != nullptr && split == 0 && !(by_slots && sub == 1);            // for the pass that forms the weights
         float factor = 0.f;                                                 // what the row's products are multiplied with
         int lim = 0;
         // The warp's rows, as an operand: kLanes lanes to a row, 16 bytes each.
@@ -461,6 +498,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
         const float* ksp = a.c.scale[0] + (size_t)unit * a.c.NB;
         const float* vsp = a.c.scale[1] + (size_t)unit * a.c.NB;
         const int blocks = (lim_max + kQcBlock - 1) / kQcBlock;
+        const bool idle = (warp & 3) * 32 + (by_slots ? 0 : sub * 128) >= rows;   // none of the warp's rows is a valid token's
         float m = -INFINITY, vref = 0.f, vmost = 0.f;
         const float cap = a.cap * kLog2e;
         float l = 0.f;
@@ -471,13 +509,15 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
             ks_next = vs_next = 0.f;
             if (n < N && blk < blocks) ks_next = ksp[blk], vs_next = vsp[blk];
         };
-        load_scales(0);
-        if (sub < subs) {
-            auto tile = [&](int n, auto hide) {               // hide: some row does not see all of it
+        // the tiles of slots of this warp's accumulators: from n0 on, n_step apart
+        const int n0 = by_slots ? sub : 0, n_step = by_slots ? 2 : 1, turns = by_slots ? (N + 1 - sub) / 2 : sub < subs ? N : 0;
+        load_scales(n0);
+        if (turns > 0) {
+            auto tile = [&](int turn, auto hide) {               // hide: some row does not see all of it
                 constexpr bool kHide = decltype(hide)::value;
-                const int slot0 = (lo + n) * kQpSlots;
+                const int n = n0 + turn * n_step, slot0 = (lo + n) * kQpSlots;
                 const float ks = ks_next, vs = vs_next;
-                load_scales(n + 1);
+                load_scales(n + n_step);
                 float vt = fmaxf(vs, __shfl_xor_sync(0xffffffffu, vs, 1));
                 vt = fmaxf(0.f, fmaxf(vt, __shfl_xor_sync(0xffffffffu, vt, 2)));
                 // the scale that the values are relative to follows the loudest block (some way above it, so that it moves
@@ -492,8 +532,12 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
                 // P's factor of the lane's block, as a power of two and inverted; a block of zeros has any
                 const float v_rel = vs == 0.f ? kQpPScale : max_nan(__fdividef(vs, vref > 0.f ? vref : 1.f), 8.67361738e-19f) * kQpPScale;
                 const float v_log = __log2f(v_rel), v_inv = __fdividef(1.f, v_rel);
-                qp_wait(&s_full[sub], n, abort_flag);
+                qp_wait(&s_full[sub], turn, abort_flag);
                 tc_fence_after();
+                if (idle) {
+                    if (lane == 0) mbar_arrive(&p_full[sub]);
+                    return;
+                }
 
                 float top = -INFINITY;
                 by_chunks(s_col, [&](int c, const uint32_t (&x)[32]) {
@@ -520,8 +564,8 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
                     l *= keep;
                     m = top;
                 }
-                if (n > 0 && __any_sync(0xffffffffu, by != 1.f)) {
-                    qp_wait(&o_full[sub], n - 1, abort_flag);
+                if (turn > 0 && __any_sync(0xffffffffu, by != 1.f)) {
+                    qp_wait(&o_full[sub], turn - 1, abort_flag);
                     tc_fence_after();
 #pragma unroll 1
                     for (int c = 0; c < D; c += 32) {
@@ -567,23 +611,25 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
                 if (lane == 0) mbar_arrive(&p_full[sub]);
             };
             const int seen = min(max(lim_min / kQpSlots - lo, 0), N);   // tiles that every row sees
+            const int seen_turns = by_slots ? (seen + 1 - sub) / 2 : seen;
 #pragma unroll 1
-            for (int n = 0; n < seen; ++n) tile(n, std::false_type());
+            for (int t = 0; t < seen_turns; ++t) tile(t, std::false_type());
 #pragma unroll 1
-            for (int n = seen; n < N; ++n) tile(n, std::true_type());
+            for (int t = seen_turns; t < turns; ++t) tile(t, std::true_type());
         }
         // results: the accumulators are in units of vref / 2^9
-        if (N > 0 && sub < subs) {
-            qp_wait(&o_full[sub], N - 1, abort_flag);
+        const bool mine = turns > 0;
+        if (mine) {
+            qp_wait(&o_full[sub], turns - 1, abort_flag);
             tc_fence_after();
         }
         if (lim == 0) l = 0.f;                                // (a padding row in a tile that others see through)
         if (*abort_flag) l = __uint_as_float(0x7fffffffu);
         float mul = vref * (1.f / kQpPScale);
-        const bool there = r < a.R, mine = N > 0 && sub < subs;
+        const bool there = r < a.R;
         const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-        if (pr.splits == 1) mul = l == l ? mul * inv : l;
-        const int64_t at = ((int64_t)unit * a.R + r) * pr.splits + split;
+        if (pr.parts == 1) mul = l == l ? mul * inv : l;
+        const int64_t at = ((int64_t)unit * a.R + r) * pr.parts + (by_slots ? 2 * split + sub : split);
         // (through the warp's part of the queries' tile, which is free by now, so that rows are written in one piece)
         unsigned char* stage = smem + L::q + sub * L::kTile + (warp & 3) * (32 * D * 2);
 #pragma unroll 1
@@ -596,7 +642,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
             float y[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) y[j] = mine && (l != 0.f) ? __uint_as_float(x[j]) * mul : 0.f;
-            if (pr.splits == 1) {
+            if (pr.parts == 1) {
 #pragma unroll
                 for (int j = 0; j < 32; j += 8)
                     *reinterpret_cast<uint4*>(stage + lane * (D * 2) + ((((c + j) >> 3) ^ (lane & 7)) << 4)) = Chunk<__nv_bfloat16>::pack(y + j);
@@ -607,7 +653,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
             }
             __syncwarp();
         }
-        if (pr.splits == 1) {
+        if (pr.parts == 1) {
             constexpr int kLanes = D / 8, kEach = 32 / kLanes;
             RowWalk walk(a, b, h, r - lane + lane / kLanes, kEach);
 #pragma unroll 4
@@ -619,7 +665,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
             }
         }
         if (there) {
-            if (pr.splits > 1) a.part_ml[at] = make_float2(m, l);
+            if (pr.parts > 1) a.part_ml[at] = make_float2(m, l);
             else if (keep_q && inv != 0.f) terms_of(pr, tile128, my_row)[2] = log2f(inv) - m;
         }
     }
@@ -637,17 +683,17 @@ __global__ void __launch_bounds__(256) qc_prompt_join_kernel(const QcAttend a, c
     pdl_open();
     if (row >= rows) return;
     const int64_t unit = row / a.R, r = row - unit * a.R;
-    const float2* ml = a.part_ml + row * pr.splits;
+    const float2* ml = a.part_ml + row * pr.parts;
     float m = -INFINITY, l = 0.f;
-    for (int i = 0; i < pr.splits; ++i) m = fmaxf(m, ml[i].x);
-    for (int i = 0; i < pr.splits; ++i) l += m == -INFINITY ? ml[i].y : ml[i].y * ex2(ml[i].x - m);
+    for (int i = 0; i < pr.parts; ++i) m = fmaxf(m, ml[i].x);
+    for (int i = 0; i < pr.parts; ++i) l += m == -INFINITY ? ml[i].y : ml[i].y * ex2(ml[i].x - m);
     const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
     constexpr int kN = D / 32;
     float y[kN] = {};
-    for (int i = 0; i < pr.splits; ++i) {
+    for (int i = 0; i < pr.parts; ++i) {
         const float by = ml[i].x == -INFINITY ? 0.f : ex2(ml[i].x - m) * inv;
 #pragma unroll
-        for (int j = 0; j < kN; ++j) y[j] = fmaf(a.part_o[(row * pr.splits + i) * D + lane * kN + j], by, y[j]);
+        for (int j = 0; j < kN; ++j) y[j] = fmaf(a.part_o[(row * pr.parts + i) * D + lane * kN + j], by, y[j]);
     }
     const int b = (int)(unit / a.c.Hkv), h = (int)(unit - (int64_t)b * a.c.Hkv);
     __nv_bfloat16* to = const_cast<__nv_bfloat16*>(row_of<__nv_bfloat16>(a, a.out, b, h, r)) + lane * kN;
@@ -670,6 +716,37 @@ struct QwtSmem {
     static constexpr int bars = rows + kQwtStages * kQpRecord;
     static constexpr int total = bars + 256 + 1024;
 };
+
+// What 32 rows give a thread's slot, from their products with its key.
+template <bool CAP>
+__device__ __forceinline__ void add_weights(const uint32_t (&x)[32], const float* row, const int* lims, float ks, float cap, int slot,
+                                            bool masked, float (&acc)[4]) {
+    float e[32];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const float4 t = *reinterpret_cast<const float4*>(row + 4 * j);
+        const float u = __uint_as_float(x[2 * j]) * ks, v = __uint_as_float(x[2 * j + 1]) * ks;
+        e[2 * j] = CAP ? u * t.x : fmaf(u, t.x, t.z);
+        e[2 * j + 1] = CAP ? v * t.y : fmaf(v, t.y, t.w);
+    }
+    if constexpr (CAP) {
+        tanh32(e);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float2 t = *reinterpret_cast<const float2*>(row + 4 * j + 2);
+            e[2 * j] = fmaf(e[2 * j], cap, t.x);
+            e[2 * j + 1] = fmaf(e[2 * j + 1], cap, t.y);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) e[j] = ex2(e[j]);
+    if (masked) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) e[j] = slot < lims[j] ? e[j] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) acc[j & 3] += e[j];
+}
 
 template <int D, bool CAP>
 __global__ void __launch_bounds__(kQwtThreads, 1) qc_prompt_weights_kernel(const QcAttend a, const QcPrompt pr) {
@@ -763,32 +840,7 @@ __global__ void __launch_bounds__(kQwtThreads, 1) qc_prompt_weights_kernel(const
             tc_fence_after();
             const bool masked = slot0 + kQpSlots > lims[0];             // (a tile's first row sees least of its valid ones)
             by_chunks(tmem + ((uint32_t)(warp & 3) << 21) + st * 128, [&](int c, const uint32_t (&x)[32]) {
-                const float* row = rows + 64 * c;
-                float e[32];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float4 t = *reinterpret_cast<const float4*>(row + 4 * j);
-                    const float u = __uint_as_float(x[2 * j]) * ks, v = __uint_as_float(x[2 * j + 1]) * ks;
-                    e[2 * j] = CAP ? u * t.x : fmaf(u, t.x, t.z);
-                    e[2 * j + 1] = CAP ? v * t.y : fmaf(v, t.y, t.w);
-                }
-                if constexpr (CAP) {
-                    tanh32(e);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float2 t = *reinterpret_cast<const float2*>(row + 4 * j + 2);
-                        e[2 * j] = fmaf(e[2 * j], cap, t.x);
-                        e[2 * j + 1] = fmaf(e[2 * j + 1], cap, t.y);
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < 32; ++j) e[j] = ex2(e[j]);
-                if (masked) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) e[j] = slot < lims[32 * c + j] ? e[j] : 0.f;
-                }
-#pragma unroll
-                for (int j = 0; j < 32; ++j) acc[j & 3] += e[j];
+                add_weights<CAP>(x, rows + 64 * c, lims + 32 * c, ks, cap, slot, masked, acc);
             });
             tc_fence_before();
             __syncwarp();
@@ -811,17 +863,213 @@ __global__ void __launch_bounds__(kQwtThreads, 1) qc_prompt_weights_kernel(const
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
+// The same for few rows (R <= 256, two tiles of queries at most), where a tile of slots is little work: CTAs go through a run
+// of 256-slot pieces, the queries in place until the unit changes.  Warps 0-3 have a piece's first 128 slots, 4-7 its others;
+// warps 8-9 turn codes into operands, a piece ahead; warp 10 loads queries, warp 11 issues the products.
+constexpr int kQwfMakers = 64;
+template <int D>
+struct QwfSmem {
+    static constexpr int kTile = D / 64 * kQpHalf;
+    static constexpr int k = 0;                        // [2 stages][2 halves of a piece]
+    static constexpr int q = k + 4 * kTile;            // two
+    static constexpr int rows = q + 2 * kTile;         // their records
+    static constexpr int bars = rows + 2 * kQpRecord;
+    static constexpr int total = bars + 256 + 1024;
+};
+
+template <int D, bool CAP>
+__global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(const QcAttend a, const QcPrompt pr) {
+    using L = QwfSmem<D>;
+    extern __shared__ unsigned char qp_smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(qp_smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bars);
+    uint64_t *k_full = bars, *k_empty = bars + 4;      // [stage][half]
+    uint64_t *s_full = bars + 8, *s_empty = bars + 12; // [half][turn]
+    uint64_t *q_full = bars + 16, *q_empty = bars + 17;
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 18);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 19);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int per_unit = (a.c.C + 255) / 256;
+    const int64_t pieces = (int64_t)a.c.B * a.c.Hkv * per_unit;
+    const int64_t p0 = pieces * blockIdx.x / gridDim.x, p1 = pieces * (blockIdx.x + 1) / gridDim.x;
+    pdl_wait();
+
+    if (tid == 0) {
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&k_full[i], kQwfMakers / 32);
+            mbar_init(&k_empty[i], 1);
+            mbar_init(&s_full[i], 1);
+            mbar_init(&s_empty[i], 4);
+        }
+        mbar_init(q_full, 1);
+        mbar_init(q_empty, 9);                         // the products and the eight warps that read the rows' terms
+        *abort_flag = 0;
+        fence_mbar_init_cluster();
+    }
+    if (warp == 11) tmem_alloc(tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    // Every role walks through the run alike: walk(piece) for each piece with slots that some row sees, `fresh` where it is
+    // the first one of a unit.
+    auto walk = [&](auto&& visit) {
+        int64_t p = p0;
+        int done = 0, units = 0;
+        while (p < p1) {
+            const int unit = (int)(p / per_unit), b = unit / a.c.Hkv;
+            const Sees sees = sees_of(a, b);
+            const int end = sees.n > 0 ? sees.held : 0;                 // slots
+            const int64_t unit_end = min(p1, (int64_t)(unit + 1) * per_unit);
+            bool fresh = true;
+            for (; p < unit_end; ++p) {
+                const int slot0 = (int)(p - (int64_t)unit * per_unit) * 256;
+                if (slot0 >= end) break;
+                if (fresh) ++units;
+                visit(unit, slot0, sees, done++, units - 1, fresh);
+                fresh = false;
+            }
+            p = unit_end;
+        }
+        return units;
+    };
+
+    if (warp == 11) {
+        // =========================== products ===========================
+        constexpr uint32_t id_s = idesc_f16(128, 128, false);
+        const DescKind dk(smem_desc(0, 16, 1024));
+        const uint32_t base16 = desc_addr16(smem_u32(smem));
+        int turns = 0;                                                  // products of a half so far
+        walk([&](int, int, const Sees& sees, int no, int unit_no, bool fresh) {
+            const int N = (int)(((int64_t)sees.n * a.G + 127) / 128), st = no & 1;
+            if (fresh) {
+                if (unit_no > 0) commit_warp(q_empty);
+                qp_wait(q_full, unit_no, abort_flag);
+            }
+            for (int h = 0; h < 2; ++h) {
+                qp_wait(&k_full[2 * st + h], no >> 1, abort_flag);
+                for (int n = 0; n < N; ++n) {
+                    const int turn = turns + n;
+                    if (turn >= 2) qp_wait(&s_empty[2 * h + (turn & 1)], (turn >> 1) - 1, abort_flag);
+                    tc_fence_after();
+                    const uint32_t ka = base16 + (L::k + (2 * st + h) * L::kTile) / 16, qa = base16 + (L::q + n * L::kTile) / 16;
+#pragma unroll
+                    for (int hf = 0; hf < D / 64; ++hf)
+                        umma4_kk(tmem + (2 * h + (turn & 1)) * 128, dk.at(ka + hf * (kQpHalf / 16)), dk.at(qa + hf * (kQpHalf / 16)), id_s, hf > 0);
+                    commit_warp(&s_full[2 * h + (turn & 1)]);
+                }
+                commit_warp(&k_empty[2 * st + h]);
+            }
+            turns += N;
+        });
+    } else if (warp == 10) {
+        // =========================== queries and their rows' terms ===========================
+        walk([&](int unit, int, const Sees& sees, int, int unit_no, bool fresh) {
+            if (!fresh) return;
+            const int N = (int)(((int64_t)sees.n * a.G + 127) / 128);
+            if (unit_no > 0) qp_wait(q_empty, unit_no - 1, abort_flag);
+            if (lane == 0) {
+                mbar_arrive_expect_tx(q_full, N * (L::kTile + kQpRecord));
+                for (int n = 0; n < N; ++n) {
+                    const size_t tile = (size_t)unit * pr.tiles * 2 + n;
+                    bulk_load(smem + L::q + n * L::kTile, pr.q_tiles + tile * L::kTile, L::kTile, q_full);
+                    bulk_load(smem + L::rows + n * kQpRecord, pr.records + tile * kQpRecord, kQpRecord, q_full);
+                }
+            }
+            __syncwarp();
+        });
+    } else if (warp >= 8) {
+        // =========================== codes to operands ===========================
+        const int t = tid - 256;
+        Codes<D, kQwfMakers> raw;
+        int ready_unit = -1, ready_slot = -1;                           // what `raw` has: a half that was asked for ahead
+        walk([&](int unit, int slot0, const Sees& sees, int no, int, bool) {
+            const int8_t* kp = a.c.codes[0] + (size_t)unit * a.c.C * D;
+            const int st = no & 1;
+            for (int h = 0; h < 2; ++h) {
+                const int at = slot0 + 128 * h;
+                if (ready_unit != unit || ready_slot != at) raw.load(kp, at, max(sees.held, at), t);
+                if (no >= 2) qp_wait(&k_empty[2 * st + h], (no >> 1) - 1, abort_flag);
+                raw.store(smem + L::k + (2 * st + h) * L::kTile, t);
+                ready_unit = unit, ready_slot = at + 128;
+                if (at + 6 * 128 < sees.held) raw.ahead(kp, at + 6 * 128, sees.held, t);
+                if (at + 128 < sees.held) raw.load(kp, at + 128, sees.held, t);
+                else ready_unit = -1;
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&k_full[2 * st + h]);
+            }
+        });
+    } else {
+        // =========================== a slot to a thread ===========================
+        const int h = warp >> 2, my = h * 128 + (warp & 3) * 32 + lane;
+        const float cap = a.cap * kLog2e;
+        int turns = 0;
+        walk([&](int unit, int slot0, const Sees& sees, int, int unit_no, bool fresh) {
+            const int slot = slot0 + my;
+            const bool there = slot < sees.held;
+            const int64_t valid = (int64_t)sees.n * a.G;
+            const int N = (int)((valid + 127) / 128);
+            const float ks = there ? a.c.scale[0][(size_t)unit * a.c.NB + slot / kQcBlock] : 0.f;
+            float* weight = a.c.weight + (size_t)unit * a.c.C + slot;
+            const float before = there ? *weight : 0.f;
+            if (fresh) {
+                if (unit_no > 0) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(q_empty);
+                }
+                qp_wait(q_full, unit_no, abort_flag);
+            }
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int n = 0; n < N; ++n) {
+                const int turn = turns + n;
+                const float* rows = reinterpret_cast<const float*>(smem + L::rows + n * kQpRecord);
+                const int* lims = reinterpret_cast<const int*>(rows + 256);
+                qp_wait(&s_full[2 * h + (turn & 1)], turn >> 1, abort_flag);
+                tc_fence_after();
+                const bool masked = slot0 + 256 > lims[0];
+                const int chunks = (int)min((int64_t)4, (valid - (int64_t)n * 128 + 31) / 32);   // rows by 32
+                const uint32_t col = tmem + ((uint32_t)(warp & 3) << 21) + (2 * h + (turn & 1)) * 128;
+#pragma unroll 1
+                for (int c = 0; c < chunks; ++c) {
+                    uint32_t x[32];
+                    tmem_ld32_raw(col + 32 * c, x);
+                    tmem_wait_ld(x);
+                    add_weights<CAP>(x, rows + 64 * c, lims + 32 * c, ks, cap, slot, masked, acc);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_empty[2 * h + (turn & 1)]);
+            }
+            turns += N;
+            float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+            if (*abort_flag) sum = __uint_as_float(0x7fffffffu);
+            if (there) *weight = before + sum;
+        });
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 11) tmem_dealloc(tmem, 512);
+}
+
 template <int D, bool CAP>
 cudaError_t prompt_with(const QcAttend& a, const QcPrompt& pr, cudaStream_t s) {
-    static std::atomic<uint64_t> done[2];
+    static std::atomic<uint64_t> done[3];
     const int64_t units = (int64_t)a.c.B * a.c.Hkv;
     cudaError_t e = allow_smem(qc_prompt_kernel<D, CAP>, QpSmem<D>::total, &done[0]);
     if (e != cudaSuccess) return e;
     e = pdl_launch(qc_prompt_kernel<D, CAP>, (unsigned)(units * pr.tiles * pr.splits), kQpThreads, QpSmem<D>::total, s, a, pr);
     if (e != cudaSuccess) return e;
-    if (pr.splits > 1 && (e = pdl_launch(qc_prompt_join_kernel<D>, (unsigned)((units * a.R + 7) / 8), 256, 0, s, a, pr)) != cudaSuccess)
+    if (pr.parts > 1 && (e = pdl_launch(qc_prompt_join_kernel<D>, (unsigned)((units * a.R + 7) / 8), 256, 0, s, a, pr)) != cudaSuccess)
         return e;
     if (!a.accumulate) return cudaSuccess;
+    if (a.R <= 256) {
+        if ((e = allow_smem(qc_prompt_few_weights_kernel<D, CAP>, QwfSmem<D>::total, &done[2])) != cudaSuccess) return e;
+        const int64_t pieces = units * ((a.c.C + 255) / 256);
+        return pdl_launch(qc_prompt_few_weights_kernel<D, CAP>, (unsigned)std::min<int64_t>(148, pieces), kQpThreads,
+                          QwfSmem<D>::total, s, a, pr);
+    }
     if ((e = allow_smem(qc_prompt_weights_kernel<D, CAP>, QwtSmem<D>::total, &done[1])) != cudaSuccess) return e;
     return pdl_launch(qc_prompt_weights_kernel<D, CAP>, (unsigned)(units * ((a.c.C + kQpSlots - 1) / kQpSlots)), kQwtThreads,
                       QwtSmem<D>::total, s, a, pr);
