@@ -863,9 +863,10 @@ __global__ void __launch_bounds__(kQwtThreads, 1) qc_prompt_weights_kernel(const
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-// The same for few rows (R <= 256, two tiles of queries at most), where a tile of slots is little work: CTAs go through a run
-// of 256-slot pieces, the queries in place until the unit changes.  Warps 0-3 have a piece's first 128 slots, 4-7 its others;
-// warps 8-9 turn codes into operands, a piece ahead; warp 10 loads queries, warp 11 issues the products.
+// The same for few rows, where a tile of slots is little work: CTAs go through a run of 256-slot pieces, with the queries in
+// place until the unit changes (R <= 256, two tiles at most) or, STREAM, through two places in turn.  Warps 0-3 have a
+// piece's first 128 slots, 4-7 its others; warps 8-9 turn codes into operands, a piece ahead; warp 10 loads queries, warp 11
+// issues the products.
 constexpr int kQwfMakers = 64;
 template <int D>
 struct QwfSmem {
@@ -877,7 +878,7 @@ struct QwfSmem {
     static constexpr int total = bars + 256 + 1024;
 };
 
-template <int D, bool CAP>
+template <int D, bool CAP, bool STREAM>
 __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(const QcAttend a, const QcPrompt pr) {
     using L = QwfSmem<D>;
     extern __shared__ unsigned char qp_smem_raw[];
@@ -885,9 +886,9 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(co
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bars);
     uint64_t *k_full = bars, *k_empty = bars + 4;      // [stage][half]
     uint64_t *s_full = bars + 8, *s_empty = bars + 12; // [half][turn]
-    uint64_t *q_full = bars + 16, *q_empty = bars + 17;
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 18);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 19);
+    uint64_t *q_full = bars + 16, *q_empty = bars + 18;   // the units' queries, by turns; STREAM: [place]
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 20);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 21);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int per_unit = (a.c.C + 255) / 256;
     const int64_t pieces = (int64_t)a.c.B * a.c.Hkv * per_unit;
@@ -901,8 +902,10 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(co
             mbar_init(&s_full[i], 1);
             mbar_init(&s_empty[i], 4);
         }
-        mbar_init(q_full, 1);
-        mbar_init(q_empty, 9);                         // the products and the eight warps that read the rows' terms
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], 9);                 // the products and the eight warps that read the rows' terms
+        }
         *abort_flag = 0;
         fence_mbar_init_cluster();
     }
@@ -935,49 +938,75 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(co
         return units;
     };
 
+    // the first tile of rows that a piece's first slot is seen by (STREAM), and the tiles
+    auto first_tile = [&](const Sees& sees, int slot0) { return STREAM ? (int)((int64_t)max(0, slot0 - (sees.held - sees.n)) * a.G / 128) : 0; };
+    auto tiles_of = [&](const Sees& sees) { return (int)(((int64_t)sees.n * a.G + 127) / 128); };
+
     if (warp == 11) {
         // =========================== products ===========================
         constexpr uint32_t id_s = idesc_f16(128, 128, false);
         const DescKind dk(smem_desc(0, 16, 1024));
         const uint32_t base16 = desc_addr16(smem_u32(smem));
         int turns = 0;                                                  // products of a half so far
-        walk([&](int, int, const Sees& sees, int no, int unit_no, bool fresh) {
-            const int N = (int)(((int64_t)sees.n * a.G + 127) / 128), st = no & 1;
-            if (fresh) {
-                if (unit_no > 0) commit_warp(q_empty);
-                qp_wait(q_full, unit_no, abort_flag);
-            }
-            for (int h = 0; h < 2; ++h) {
-                qp_wait(&k_full[2 * st + h], no >> 1, abort_flag);
-                for (int n = 0; n < N; ++n) {
-                    const int turn = turns + n;
-                    if (turn >= 2) qp_wait(&s_empty[2 * h + (turn & 1)], (turn >> 1) - 1, abort_flag);
-                    tc_fence_after();
-                    const uint32_t ka = base16 + (L::k + (2 * st + h) * L::kTile) / 16, qa = base16 + (L::q + n * L::kTile) / 16;
+        auto product = [&](int st, int h, int place, int turn) {
+            if (turn >= 2) qp_wait(&s_empty[2 * h + (turn & 1)], (turn >> 1) - 1, abort_flag);
+            tc_fence_after();
+            const uint32_t ka = base16 + (L::k + (2 * st + h) * L::kTile) / 16, qa = base16 + (L::q + place * L::kTile) / 16;
 #pragma unroll
-                    for (int hf = 0; hf < D / 64; ++hf)
-                        umma4_kk(tmem + (2 * h + (turn & 1)) * 128, dk.at(ka + hf * (kQpHalf / 16)), dk.at(qa + hf * (kQpHalf / 16)), id_s, hf > 0);
-                    commit_warp(&s_full[2 * h + (turn & 1)]);
+            for (int hf = 0; hf < D / 64; ++hf)
+                umma4_kk(tmem + (2 * h + (turn & 1)) * 128, dk.at(ka + hf * (kQpHalf / 16)), dk.at(qa + hf * (kQpHalf / 16)), id_s, hf > 0);
+            commit_warp(&s_full[2 * h + (turn & 1)]);
+        };
+        walk([&](int, int slot0, const Sees& sees, int no, int unit_no, bool fresh) {
+            const int N = tiles_of(sees), st = no & 1;
+            if constexpr (STREAM) {
+                for (int h = 0; h < 2; ++h) qp_wait(&k_full[2 * st + h], no >> 1, abort_flag);
+                for (int n = first_tile(sees, slot0); n < N; ++n, ++turns) {
+                    qp_wait(&q_full[turns & 1], turns >> 1, abort_flag);
+                    for (int h = 0; h < 2; ++h) product(st, h, turns & 1, turns);
+                    commit_warp(&q_empty[turns & 1]);
                 }
-                commit_warp(&k_empty[2 * st + h]);
+                for (int h = 0; h < 2; ++h) commit_warp(&k_empty[2 * st + h]);
+            } else {
+                if (fresh) {
+                    if (unit_no > 0) commit_warp(q_empty);
+                    qp_wait(q_full, unit_no, abort_flag);
+                }
+                for (int h = 0; h < 2; ++h) {
+                    qp_wait(&k_full[2 * st + h], no >> 1, abort_flag);
+                    for (int n = 0; n < N; ++n) product(st, h, n, turns + n);
+                    commit_warp(&k_empty[2 * st + h]);
+                }
+                turns += N;
             }
-            turns += N;
         });
     } else if (warp == 10) {
         // =========================== queries and their rows' terms ===========================
-        walk([&](int unit, int, const Sees& sees, int, int unit_no, bool fresh) {
-            if (!fresh) return;
-            const int N = (int)(((int64_t)sees.n * a.G + 127) / 128);
-            if (unit_no > 0) qp_wait(q_empty, unit_no - 1, abort_flag);
-            if (lane == 0) {
-                mbar_arrive_expect_tx(q_full, N * (L::kTile + kQpRecord));
-                for (int n = 0; n < N; ++n) {
-                    const size_t tile = (size_t)unit * pr.tiles * 2 + n;
-                    bulk_load(smem + L::q + n * L::kTile, pr.q_tiles + tile * L::kTile, L::kTile, q_full);
-                    bulk_load(smem + L::rows + n * kQpRecord, pr.records + tile * kQpRecord, kQpRecord, q_full);
+        int turns = 0;
+        auto load = [&](int unit, int n, int place, uint64_t* bar) {
+            const size_t tile = (size_t)unit * pr.tiles * 2 + n;
+            bulk_load(smem + L::q + place * L::kTile, pr.q_tiles + tile * L::kTile, L::kTile, bar);
+            bulk_load(smem + L::rows + place * kQpRecord, pr.records + tile * kQpRecord, kQpRecord, bar);
+        };
+        walk([&](int unit, int slot0, const Sees& sees, int, int unit_no, bool fresh) {
+            const int N = tiles_of(sees);
+            if constexpr (STREAM) {
+                for (int n = first_tile(sees, slot0); n < N; ++n, ++turns) {
+                    if (turns >= 2) qp_wait(&q_empty[turns & 1], (turns >> 1) - 1, abort_flag);
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(&q_full[turns & 1], L::kTile + kQpRecord);
+                        load(unit, n, turns & 1, &q_full[turns & 1]);
+                    }
+                    __syncwarp();
                 }
+            } else if (fresh) {
+                if (unit_no > 0) qp_wait(q_empty, unit_no - 1, abort_flag);
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(q_full, N * (L::kTile + kQpRecord));
+                    for (int n = 0; n < N; ++n) load(unit, n, n, q_full);
+                }
+                __syncwarp();
             }
-            __syncwarp();
         });
     } else if (warp >= 8) {
         // =========================== codes to operands ===========================
@@ -1010,11 +1039,11 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(co
             const int slot = slot0 + my;
             const bool there = slot < sees.held;
             const int64_t valid = (int64_t)sees.n * a.G;
-            const int N = (int)((valid + 127) / 128);
+            const int N = tiles_of(sees);
             const float ks = there ? a.c.scale[0][(size_t)unit * a.c.NB + slot / kQcBlock] : 0.f;
             float* weight = a.c.weight + (size_t)unit * a.c.C + slot;
             const float before = there ? *weight : 0.f;
-            if (fresh) {
+            if (!STREAM && fresh) {
                 if (unit_no > 0) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(q_empty);
@@ -1022,9 +1051,10 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(co
                 qp_wait(q_full, unit_no, abort_flag);
             }
             float acc[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int n = 0; n < N; ++n) {
-                const int turn = turns + n;
-                const float* rows = reinterpret_cast<const float*>(smem + L::rows + n * kQpRecord);
+            for (int n = first_tile(sees, slot0); n < N; ++n) {
+                const int turn = turns++;
+                const float* rows = reinterpret_cast<const float*>(smem + L::rows + (STREAM ? turn & 1 : n) * kQpRecord);
+                if constexpr (STREAM) qp_wait(&q_full[turn & 1], turn >> 1, abort_flag);
                 const int* lims = reinterpret_cast<const int*>(rows + 256);
                 qp_wait(&s_full[2 * h + (turn & 1)], turn >> 1, abort_flag);
                 tc_fence_after();
@@ -1040,9 +1070,11 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(co
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&s_empty[2 * h + (turn & 1)]);
+                if (lane == 0) {
+                    mbar_arrive(&s_empty[2 * h + (turn & 1)]);
+                    if constexpr (STREAM) mbar_arrive(&q_empty[turn & 1]);
+                }
             }
-            turns += N;
             float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
             if (*abort_flag) sum = __uint_as_float(0x7fffffffu);
             if (there) *weight = before + sum;
@@ -1055,7 +1087,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(co
 
 template <int D, bool CAP>
 cudaError_t prompt_with(const QcAttend& a, const QcPrompt& pr, cudaStream_t s) {
-    static std::atomic<uint64_t> done[3];
+    static std::atomic<uint64_t> done[4];
     const int64_t units = (int64_t)a.c.B * a.c.Hkv;
     cudaError_t e = allow_smem(qc_prompt_kernel<D, CAP>, QpSmem<D>::total, &done[0]);
     if (e != cudaSuccess) return e;
@@ -1064,11 +1096,13 @@ cudaError_t prompt_with(const QcAttend& a, const QcPrompt& pr, cudaStream_t s) {
     if (pr.parts > 1 && (e = pdl_launch(qc_prompt_join_kernel<D>, (unsigned)((units * a.R + 7) / 8), 256, 0, s, a, pr)) != cudaSuccess)
         return e;
     if (!a.accumulate) return cudaSuccess;
-    if (a.R <= 256) {
-        if ((e = allow_smem(qc_prompt_few_weights_kernel<D, CAP>, QwfSmem<D>::total, &done[2])) != cudaSuccess) return e;
-        const int64_t pieces = units * ((a.c.C + 255) / 256);
-        return pdl_launch(qc_prompt_few_weights_kernel<D, CAP>, (unsigned)std::min<int64_t>(148, pieces), kQpThreads,
-                          QwfSmem<D>::total, s, a, pr);
+    // Runs of slots need pieces enough to even out; with many rows a tile of slots is work enough for a CTA of its own.
+    const int64_t pieces = units * ((a.c.C + 255) / 256);
+    if (a.R <= 256 || (a.R <= 2048 && pieces >= 4 * 148)) {
+        const bool stream = a.R > 256;
+        const auto kernel = stream ? qc_prompt_few_weights_kernel<D, CAP, true> : qc_prompt_few_weights_kernel<D, CAP, false>;
+        if ((e = allow_smem(kernel, QwfSmem<D>::total, &done[2 + stream])) != cudaSuccess) return e;
+        return pdl_launch(kernel, (unsigned)std::min<int64_t>(148, pieces), kQpThreads, QwfSmem<D>::total, s, a, pr);
     }
     if ((e = allow_smem(qc_prompt_weights_kernel<D, CAP>, QwtSmem<D>::total, &done[1])) != cudaSuccess) return e;
     return pdl_launch(qc_prompt_weights_kernel<D, CAP>, (unsigned)(units * ((a.c.C + kQpSlots - 1) / kQpSlots)), kQwtThreads,

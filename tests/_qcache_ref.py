@@ -23,9 +23,11 @@ class Ref:
     def _write(self, p, b, h, slots, x, end):
         """Rows x into `slots`, where no slot from `end` on holds anything."""
         codes, scale = getattr(self, p)[b, h], getattr(self, p + "_scale")[b, h]
-        for blk in sorted(set(int(s) // BLOCK for s in slots)):
-            mine = [i for i, s in enumerate(slots) if s // BLOCK == blk]
-            rows = [int(slots[i]) for i in mine]
+        slots = np.asarray(slots, dtype=np.int64)                     # ascending
+        assert (np.diff(slots) > 0).all()
+        for blk in np.unique(slots // BLOCK).tolist():
+            mine = slice(*np.searchsorted(slots, [blk * BLOCK, (blk + 1) * BLOCK]).tolist())
+            rows = slots[mine].tolist()
             stay = [j for j in range(blk * BLOCK, min(blk * BLOCK + BLOCK, end)) if j not in rows]
             new = x[mine]
             s = float(scale[blk])

@@ -236,6 +236,48 @@ def test_several_tokens_see_up_to_themselves(Bt, T, Hq, Hkv, d, dtype, C, held, 
             assert bool((out[b, n:] == 0).all())
 
 
+MANY = [  # the row counts where another kernel takes over, caches that are shared out, and batches that fill the device
+    (2, 3, 8, 1, 128, "bf16", 150, [150, 70], [3, 1]), (2, 25, 1, 1, 128, "bf16", 150, [150, 25], None),
+    (2, 24, 1, 1, 128, "f32", 150, [150, 25], None), (2, 16, 8, 1, 128, "bf16", 900, [900, 17], [16, 15]),
+    (2, 32, 8, 2, 64, "bf16", 600, [600, 300], [32, 1]), (1, 30, 8, 1, 128, "bf16", 20000, [19999], None),
+    (1, 3, 24, 3, 128, "bf16", 20000, [20000], None), (2, 300, 2, 1, 128, "bf16", 9000, [9000, 8191], [300, 299]),
+    (37, 20, 4, 2, 64, "bf16", 700, [(53 * i) % 701 for i in range(37)], [i % 21 for i in range(37)]),
+    (37, 9, 12, 4, 128, "bf16", 520, [(37 * i) % 521 for i in range(37)], [9 - i % 10 for i in range(37)]),
+    (40, 70, 16, 4, 128, "bf16", 1000, [(211 * i) % 1001 for i in range(40)], [(11 * i) % 71 for i in range(40)]),
+    (75, 512, 4, 1, 64, "bf16", 2048, [2048 - 29 * i for i in range(75)], [512 - 7 * i for i in range(75)]),
+    (40, 520, 8, 2, 64, "bf16", 1793, [1793 - 31 * i for i in range(40)], [520 - 13 * i for i in range(40)]),
+]
+
+
+@pytest.mark.parametrize("Bt,T,Hq,Hkv,d,dtype,C,held,lens", MANY)
+def test_several_tokens_at_the_counts_of_rows_where_kernels_change(Bt, T, Hq, Hkv, d, dtype, C, held, lens):
+    test_several_tokens_see_up_to_themselves(Bt, T, Hq, Hkv, d, dtype, C, held, lens, 0.0)
+
+
+def test_lengths_outside_the_call_count_as_its_ends():
+    got = []
+    for lens in ([-3, 9, 2], [0, 4, 2]):
+        cache, _ = _filled(3, 2, 128, 100, "bf16", [10, 60, 33], 8)
+        k, v, q = (_tokens(3, 4, h, 128, "bf16", 50 + i) for i, h in enumerate((2, 2, 8)))
+        cache.append(k, v, _i32(lens))
+        out = cache.attend(q, lens=_i32(lens))
+        torch.cuda.synchronize()
+        got.append([out, cache.weight] + list(_planes(cache)))
+    assert got[0][-1][0].tolist() == [10, 64, 35]
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("lens", [[1, 1], [0, 1], [-1, 7]])
+def test_single_tokens_of_a_padded_batch(lens):
+    cache, ref = _filled(2, 2, 128, 100, "bf16", [40, 63], 8)
+    out = _check_attend(cache, ref, _tokens(2, 1, 8, 128, "bf16", 9), lens)
+    assert bool((out[0] == 0).all()) == (lens[0] < 1)
+    before = cache.weight.clone()
+    cache.attend(_tokens(2, 1, 8, 128, "bf16", 10), lens=_i32([0, 0]))
+    assert torch.equal(cache.weight, before)
+
+
 @pytest.mark.parametrize("T", [1, 6, 140])
 @pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "f32")])
 def test_rows_that_see_nothing_are_zero(T, d, dtype):
