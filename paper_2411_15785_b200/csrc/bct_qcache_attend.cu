@@ -78,60 +78,6 @@ __device__ __forceinline__ int tile_at(int slot, int chunk) {
 __device__ __forceinline__ int blocks_of(const QcAttend& a, int b) {
     return (min(max(a.c.state[b], 0), a.c.C) + kQcBlock - 1) / kQcBlock;
 }
-// Block x of all sequences', per_seq times each: its sequence, the blocks (times per_seq) of those before, and of all.  x is
-// made of the total by `where`.  Up to 32 sequences are a warp's own affair; more are added up by the CTA, which then calls
-// this with all its threads (upto: a word for each).
-template <typename F>
-__device__ __forceinline__ int64_t find_block(const QcAttend& a, int64_t per_seq, int64_t* upto, F where, int64_t* x, int* seq,
-                                              int64_t* before) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = a.c.B;
-    if (B <= 32) {
-        int64_t sum = lane < B ? blocks_of(a, lane) : 0;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += y;
-        }
-        const int64_t total = __shfl_sync(0xffffffffu, sum, 31) * per_seq;
-        *x = where(total);
-        const int behind = __popc(__ballot_sync(0xffffffffu, sum * per_seq <= *x));   // sequences that end before it
-        *seq = behind;
-        *before = behind ? __shfl_sync(0xffffffffu, sum, behind - 1 & 31) * per_seq : 0;
-        return total;
-    }
-    const int chunk = (B + blockDim.x - 1) / blockDim.x;
-    int64_t sum = 0;
-    for (int i = 0; i < chunk; ++i)
-        if (tid * chunk + i < B) sum += blocks_of(a, tid * chunk + i);
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += y;
-    }
-    __shared__ int64_t warps[32];
-    if (lane == 31) warps[warp] = sum;
-    __syncthreads();
-    for (int i = 0; i < warp; ++i) sum += warps[i];
-    upto[tid] = sum;
-    __syncthreads();
-    const int64_t total = upto[blockDim.x - 1] * per_seq;
-    *x = where(total);
-    if (*x >= total) return total;
-    int lo = 0, hi = blockDim.x - 1;               // first thread's share that ends behind x
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (upto[mid] * per_seq > *x) hi = mid; else lo = mid + 1;
-    }
-    *seq = lo * chunk;
-    *before = (lo ? upto[lo - 1] : 0) * per_seq;
-    for (;;) {
-        const int64_t nb = blocks_of(a, *seq);
-        if (*before + nb * per_seq > *x) break;
-        *before += nb * per_seq;
-        ++*seq;
-    }
-    return total;
-}
 // The warp whose run has block x of `total` in all, of n runs (n <= total).
 __device__ __forceinline__ int run_of(int64_t x, int64_t total, int n) { return (int)(((x + 1) * n - 1) / total); }
 
@@ -246,7 +192,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
     const int run = warp * gridDim.x + blockIdx.x;
     int n_runs, b;
     int64_t x, before;    // blocks of the sequences before b, times per_seq
-    const int64_t total = find_block(a, per_seq, upto,
+    const int64_t total = find_share(a.c.B, [&](int i) { return blocks_of(a, i); }, per_seq, upto,
                                      [&](int64_t all) {
                                          n_runs = (int)min((int64_t)a.n_warps, all);
                                          return run < n_runs ? all * run / n_runs : all;
@@ -740,10 +686,12 @@ __global__ void __launch_bounds__(kQjThreads, kQjResident) qc_join_kernel(const 
 
 // The weights from the keys again, for calls with many rows: a CTA per block of slots, whose warps share the rows that see
 // it and add up in their order.
+template <int D>
+constexpr int kQwWarps = D == 64 ? 16 : 12;
 template <typename T, int D, int TERMS>
-__global__ void __launch_bounds__(kQaThreads) qc_weights_kernel(const QcAttend a) {
+__global__ void __launch_bounds__(32 * kQwWarps<D>) qc_weights_kernel(const QcAttend a) {
     __shared__ __align__(128) unsigned char tile[kQcBlock * D];
-    __shared__ float sums[kQaWarps][kQcBlock];
+    __shared__ float sums[kQwWarps<D>][kQcBlock];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const unsigned unit = blockIdx.x / (unsigned)a.c.NB;
     const int blk = (int)(blockIdx.x - unit * a.c.NB);
@@ -771,7 +719,7 @@ __global__ void __launch_bounds__(kQaThreads) qc_weights_kernel(const QcAttend a
     const int i0 = max(0, slot0 - (sees.held - sees.n));
     const int mine = 8 * (g >> 1) + 4 * (g & 1);
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t r0 = (int64_t)i0 * a.G / 8 * 8 + warp * 8; r0 < (int64_t)sees.n * a.G; r0 += 8 * kQaWarps) {
+    for (int64_t r0 = (int64_t)i0 * a.G / 8 * 8 + warp * 8; r0 < (int64_t)sees.n * a.G; r0 += 8 * kQwWarps<D>) {
         uint32_t q[1][TERMS][D / 16][2];
         float m;
         const int64_t r = r0 + g;
@@ -804,7 +752,7 @@ __global__ void __launch_bounds__(kQaThreads) qc_weights_kernel(const QcAttend a
     if (tid < kQcBlock && slot0 + tid < sees.held) {
         float x = 0.f;
 #pragma unroll
-        for (int i = 0; i < kQaWarps; ++i) x += sums[i][tid];
+        for (int i = 0; i < kQwWarps<D>; ++i) x += sums[i][tid];
         a.c.weight[(size_t)unit * a.c.C + slot0 + tid] += x;
     }
 }
@@ -841,7 +789,7 @@ cudaError_t attend_of(const QcAttend& a, const QcPlan& p, cudaStream_t s) {
     e = pdl_launch(kernel, (unsigned)(units * ctas), kQjThreads, 0, s, a, ctas, p.rows, share, ml_lanes, rows_each);
     if constexpr (TERMS == 2) {   // (many bfloat16 rows are the tensor path's)
         if (e == cudaSuccess && a.accumulate != 0 && !p.by_scores)
-            e = pdl_launch(qc_weights_kernel<T, D, TERMS>, (unsigned)(units * a.c.NB), kQaThreads, 0, s, a);
+            e = pdl_launch(qc_weights_kernel<T, D, TERMS>, (unsigned)(units * a.c.NB), 32 * kQwWarps<D>, 0, s, a);
     }
     return e;
 }

@@ -50,6 +50,60 @@ __device__ __forceinline__ Sees sees_of(const QcAttend& a, int b) {
     s.R = a.R;
     return s;
 }
+// B sequences have size_of(b) things each, per_seq times over.  Thing x of them all: its sequence, how many stand before that
+// one, and the total, which x is made of by `where`; x = total has no sequence.  Up to 32 sequences are a warp's own affair; more are added up by the CTA, which then calls
+// this with all its threads (upto: a word for each).
+template <typename S, typename F>
+__device__ __forceinline__ int64_t find_share(int B, S size_of, int64_t per_seq, int64_t* upto, F where, int64_t* x, int* seq,
+                                              int64_t* before) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (B <= 32) {
+        int64_t sum = lane < B ? size_of(lane) : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += y;
+        }
+        const int64_t total = __shfl_sync(0xffffffffu, sum, 31) * per_seq;
+        *x = where(total);
+        const int behind = __popc(__ballot_sync(0xffffffffu, sum * per_seq <= *x));   // sequences that end before it
+        *seq = behind;
+        *before = behind ? __shfl_sync(0xffffffffu, sum, behind - 1 & 31) * per_seq : 0;
+        return total;
+    }
+    const int chunk = (B + blockDim.x - 1) / blockDim.x;
+    int64_t sum = 0;
+    for (int i = 0; i < chunk; ++i)
+        if (tid * chunk + i < B) sum += size_of(tid * chunk + i);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += y;
+    }
+    __shared__ int64_t warps[32];
+    if (lane == 31) warps[warp] = sum;
+    __syncthreads();
+    for (int i = 0; i < warp; ++i) sum += warps[i];
+    upto[tid] = sum;
+    __syncthreads();
+    const int64_t total = upto[blockDim.x - 1] * per_seq;
+    *x = where(total);
+    if (*x >= total) return total;
+    int lo = 0, hi = blockDim.x - 1;               // first thread's share that ends behind x
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (upto[mid] * per_seq > *x) hi = mid; else lo = mid + 1;
+    }
+    *seq = lo * chunk;
+    *before = (lo ? upto[lo - 1] : 0) * per_seq;
+    for (;;) {
+        const int64_t nb = size_of(*seq);
+        if (*before + nb * per_seq > *x) break;
+        *before += nb * per_seq;
+        ++*seq;
+    }
+    return total;
+}
 template <typename T>
 __device__ __forceinline__ const T* row_of(const QcAttend& a, const void* base, int b, int h, int64_t r) {
     const unsigned i = (unsigned)r / (unsigned)a.G, head = (unsigned)h * a.G + ((unsigned)r - i * a.G);

@@ -863,8 +863,9 @@ __global__ void __launch_bounds__(kQwtThreads, 1) qc_prompt_weights_kernel(const
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-// The same for few rows, where a tile of slots is little work: CTAs go through a run of 256-slot pieces, with the queries in
-// place until the unit changes (R <= 256, two tiles at most) or, STREAM, through two places in turn.  Warps 0-3 have a
+// The same for few rows, where a tile of slots is little work: CTAs go through runs of 256-slot pieces that are of equal work,
+// whatever the sequences' lengths, with the queries in place until the unit changes (R <= 256, two tiles at most) or, STREAM,
+// through two places in turn.  Warps 0-3 have a
 // piece's first 128 slots, 4-7 its others; warps 8-9 turn codes into operands, a piece ahead; warp 10 loads queries, warp 11
 // issues the products.
 constexpr int kQwfMakers = 64;
@@ -890,9 +891,6 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(co
     volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 20);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 21);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int per_unit = (a.c.C + 255) / 256;
-    const int64_t pieces = (int64_t)a.c.B * a.c.Hkv * per_unit;
-    const int64_t p0 = pieces * blockIdx.x / gridDim.x, p1 = pieces * (blockIdx.x + 1) / gridDim.x;
     pdl_wait();
 
     if (tid == 0) {
@@ -915,32 +913,64 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_few_weights_kernel(co
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    // Every role walks through the run alike: walk(piece) for each piece with slots that some row sees, `fresh` where it is
-    // the first one of a unit.
-    auto walk = [&](auto&& visit) {
-        int64_t p = p0;
-        int done = 0, units = 0;
-        while (p < p1) {
-            const int unit = (int)(p / per_unit), b = unit / a.c.Hkv;
-            const Sees sees = sees_of(a, b);
-            const int end = sees.n > 0 ? sees.held : 0;                 // slots
-            const int64_t unit_end = min(p1, (int64_t)(unit + 1) * per_unit);
-            bool fresh = true;
-            for (; p < unit_end; ++p) {
-                const int slot0 = (int)(p - (int64_t)unit * per_unit) * 256;
-                if (slot0 >= end) break;
-                if (fresh) ++units;
-                visit(unit, slot0, sees, done++, units - 1, fresh);
-                fresh = false;
-            }
-            p = unit_end;
-        }
-        return units;
-    };
-
-    // the first tile of rows that a piece's first slot is seen by (STREAM), and the tiles
-    auto first_tile = [&](const Sees& sees, int slot0) { return STREAM ? (int)((int64_t)max(0, slot0 - (sees.held - sees.n)) * a.G / 128) : 0; };
+    // A piece's work is the tiles of rows that see its first slot (STREAM; all tiles otherwise), and one more for its slots.
     auto tiles_of = [&](const Sees& sees) { return (int)(((int64_t)sees.n * a.G + 127) / 128); };
+    auto first_tile = [&](const Sees& sees, int slot0) {
+        return STREAM ? (int)((int64_t)max(0, slot0 - (sees.held - sees.n)) * a.G / 128) : 0;
+    };
+    auto pieces_of = [&](const Sees& sees) { return sees.n > 0 ? (sees.held + 255) / 256 : 0; };
+    // pieces that all the tiles see: the first ones
+    auto full_of = [&](const Sees& sees) {
+        return !STREAM ? pieces_of(sees) : sees.held < sees.n ? 0 : min(pieces_of(sees), (sees.held - sees.n) / 256 + 1);
+    };
+    auto work_of = [&](int b) {
+        const Sees sees = sees_of(a, b);
+        const int N = tiles_of(sees), P = pieces_of(sees), full = full_of(sees);
+        int64_t work = (int64_t)full * (N + 1);
+        for (int p = full; p < P; ++p) work += N + 1 - first_tile(sees, p * 256);
+        return work;
+    };
+    // The run: from the first piece whose work starts at x0 or behind it, as work is counted through all units, to x1.
+    int64_t x0 = 0, x1 = 0, before = 0;
+    int seq = a.c.B;
+    find_share(a.c.B, work_of, a.c.Hkv, reinterpret_cast<int64_t*>(smem),
+               [&](int64_t all) {
+                   x1 = all * (blockIdx.x + 1) / gridDim.x;
+                   return all * blockIdx.x / gridDim.x;
+               },
+               &x0, &seq, &before);
+    __syncthreads();                                                    // (the words are the operands' place)
+    // Every role walks through the run alike: walk(visit) for each piece, `fresh` where it is the run's first of a unit.
+    auto walk = [&](auto&& visit) {
+        if (x0 >= x1) return 0;
+        int done = 0, units = 0, b = seq;
+        int64_t at = before;
+        for (;; ++b) {
+            if (b >= a.c.B) return units;
+            const Sees sees = sees_of(a, b);
+            const int N = tiles_of(sees), P = pieces_of(sees), full = full_of(sees);
+            if (P == 0) continue;
+            int h = 0, p = 0;
+            if (at < x0) {                                              // the run's first sequence
+                const int64_t work = work_of(b);
+                h = (int)((x0 - at) / work);
+                at += h * work;
+                p = (int)min((int64_t)full, (x0 - at + N) / (N + 1));
+                at += (int64_t)p * (N + 1);
+                for (; p < P && at < x0; ++p) at += N + 1 - first_tile(sees, p * 256);
+            }
+            for (; h < a.c.Hkv; ++h, p = 0) {
+                bool fresh = true;
+                for (; p < P; ++p) {
+                    if (at >= x1) return units;
+                    if (fresh) ++units;
+                    visit(b * a.c.Hkv + h, p * 256, sees, done++, units - 1, fresh);
+                    fresh = false;
+                    at += N + 1 - first_tile(sees, p * 256);
+                }
+            }
+        }
+    };
 
     if (warp == 11) {
         // =========================== products ===========================
@@ -1096,9 +1126,11 @@ cudaError_t prompt_with(const QcAttend& a, const QcPrompt& pr, cudaStream_t s) {
     if (pr.parts > 1 && (e = pdl_launch(qc_prompt_join_kernel<D>, (unsigned)((units * a.R + 7) / 8), 256, 0, s, a, pr)) != cudaSuccess)
         return e;
     if (!a.accumulate) return cudaSuccess;
-    // Runs of slots need pieces enough to even out; with many rows a tile of slots is work enough for a CTA of its own.
+    // Runs of slots even out when there are many pieces, each of little work; otherwise a tile of slots gets a CTA of its own.
+    // The whole call by runs / by tiles, 8 heads of 4 queries to a sequence: 4 x 8192, 512 rows 182 / 220 us; 16 x 4096, 4096
+    // rows 2030 / 2096; 4 x 2048, 2048 rows 178 / 177; 5 ragged sequences of up to 2500, 777 rows of 8 heads 147 / 140.
     const int64_t pieces = units * ((a.c.C + 255) / 256);
-    if (a.R <= 256 || (a.R <= 2048 && pieces >= 4 * 148)) {
+    if (a.R <= 256 || (pieces >= 4 * 148 && a.R <= 4 * pieces)) {
         const bool stream = a.R > 256;
         const auto kernel = stream ? qc_prompt_few_weights_kernel<D, CAP, true> : qc_prompt_few_weights_kernel<D, CAP, false>;
         if ((e = allow_smem(kernel, QwfSmem<D>::total, &done[2 + stream])) != cudaSuccess) return e;
