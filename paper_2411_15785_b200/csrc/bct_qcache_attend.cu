@@ -82,20 +82,22 @@ __device__ __forceinline__ int blocks_of(const QcAttend& a, int b) {
 __device__ __forceinline__ int run_of(int64_t x, int64_t total, int n) { return (int)(((x + 1) * n - 1) / total); }
 
 // The queries of eight rows as fragments: lane (g, t) has row g.  `mul`: what the row was divided by.
+template <typename T, int D>
+constexpr int kQueryWords = D / 4 / Chunk<T>::kElems;
+template <typename T, int D>
+__device__ __forceinline__ void fetch_queries(const T* row, bool real, uint4 (&w)[kQueryWords<T, D>]) {
+    constexpr int kE = Chunk<T>::kElems, kEach = 16 / kE;
+#pragma unroll
+    for (int i = 0; i < kQueryWords<T, D>; ++i) {
+        w[i] = make_uint4(0, 0, 0, 0);
+        if (real) w[i] = *reinterpret_cast<const uint4*>(row + 64 * (i / kEach) + 16 * (threadIdx.x & 3) + i % kEach * kE);
+    }
+}
 template <typename T, int D, int TERMS>
-__device__ __forceinline__ void load_queries(const T* row, bool real, uint32_t (&f)[TERMS][D / 16][2], float* mul) {
-    const int t = threadIdx.x & 3;
+__device__ __forceinline__ void make_queries(const uint4 (&w)[kQueryWords<T, D>], uint32_t (&f)[TERMS][D / 16][2], float* mul) {
     float x[D / 4];
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) {
-        constexpr int kE = Chunk<T>::kElems;
-#pragma unroll
-        for (int i = 0; i < 16 / kE; ++i) {
-            uint4 w = make_uint4(0, 0, 0, 0);
-            if (real) w = *reinterpret_cast<const uint4*>(row + 64 * j + 16 * t + i * kE);
-            Chunk<T>::unpack(w, x + 16 * j + i * kE);
-        }
-    }
+    for (int i = 0; i < kQueryWords<T, D>; ++i) Chunk<T>::unpack(w[i], x + i * Chunk<T>::kElems);
     float top = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 4; ++i) top = fmaxf(top, fabsf(x[i]));
@@ -115,6 +117,13 @@ __device__ __forceinline__ void load_queries(const T* row, bool real, uint32_t (
             }
         }
     }
+}
+
+template <typename T, int D, int TERMS>
+__device__ __forceinline__ void load_queries(const T* row, bool real, uint32_t (&f)[TERMS][D / 16][2], float* mul) {
+    uint4 w[kQueryWords<T, D>];
+    fetch_queries<T, D>(row, real, w);
+    make_queries<T, D, TERMS>(w, f, mul);
 }
 
 // The codes of a block's keys as fragments: [i][word] pairs, i the lane's slots, word four features.
@@ -719,18 +728,26 @@ __global__ void __launch_bounds__(32 * kQwWarps<D>) qc_weights_kernel(const QcAt
     const int i0 = max(0, slot0 - (sees.held - sees.n));
     const int mine = 8 * (g >> 1) + 4 * (g & 1);
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t r0 = (int64_t)i0 * a.G / 8 * 8 + warp * 8; r0 < (int64_t)sees.n * a.G; r0 += 8 * kQwWarps<D>) {
-        uint32_t q[1][TERMS][D / 16][2];
-        float m;
+    uint4 next[kQueryWords<T, D>];
+    float2 next_ml[2];
+    auto ask = [&](int64_t r0) {                     // eight rows, an iteration ahead
         const int64_t r = r0 + g;
-        load_queries<T, D, TERMS>(row_of<T>(a, a.q, b, h, r < a.R ? r : 0), r < a.R, q[0], &m);
-        m = row_factor(a, m);
-        float2 ml[2];
+        fetch_queries<T, D>(row_of<T>(a, a.q, b, h, r < a.R ? r : 0), r < a.R, next);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int64_t re = r0 + 2 * t + e;
-            ml[e] = re < a.R ? a.ml[(size_t)unit * a.R + re] : make_float2(0.f, 0.f);
+            next_ml[e] = re < a.R ? a.ml[(size_t)unit * a.R + re] : make_float2(0.f, 0.f);
         }
+    };
+    int64_t r0 = (int64_t)i0 * a.G / 8 * 8 + warp * 8;
+    ask(r0);
+    for (; r0 < (int64_t)sees.n * a.G; r0 += 8 * kQwWarps<D>) {
+        uint32_t q[1][TERMS][D / 16][2];
+        float m;
+        make_queries<T, D, TERMS>(next, q[0], &m);
+        m = row_factor(a, m);
+        const float2 ml[2] = {next_ml[0], next_ml[1]};
+        ask(r0 + 8 * kQwWarps<D>);
         float s[1][2][4];
         score_products<D, TERMS, 1>(w, q, s);
         to_scores(s[0], __shfl_sync(0xffffffffu, m, 8 * t) * ks, __shfl_sync(0xffffffffu, m, 8 * t + 4) * ks, a.cap);
