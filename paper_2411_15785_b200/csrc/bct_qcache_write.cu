@@ -55,6 +55,28 @@ __device__ __forceinline__ uint32_t codes_of(const float* x, float inv, float* f
     }
     return packed(u);
 }
+// Four codes of x itself.  With q the rounded x inv, r = x - q s is exact next to half a step (multiples of s's ulp or of half
+// of it): it decides whether the neighbour is right, which is one apart.
+__device__ __forceinline__ uint32_t new_codes(const float* x, float inv, float s, float half) {
+    constexpr float kMagic = 12582912.f;
+    float m[4], far = 0.f;
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        m[i] = fmaf(x[i], inv, kMagic);
+        u[i] = __float_as_uint(m[i]);
+        far = fmaxf(far, fabsf(fmaf(kMagic - m[i], s, x[i])));
+    }
+    if (far >= half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float r = fmaf(kMagic - m[i], s, x[i]), over = fabsf(r) - half;
+            if (over > 0.f || (over == 0.f && (u[i] & 1))) u[i] += r > 0.f ? 1 : -1;
+            u[i] = min(max(u[i], 0x4b400000u - 127u), 0x4b400000u + 127u);   // 127.5 s would be 128
+        }
+    }
+    return packed(u);
+}
 // The exact ones of x + lo (out of the way of the loops that rarely need them).
 __device__ __noinline__ uint32_t exact_codes(float4 x, float4 lo, float s, float inv) {
     const uint32_t u[4] = {(uint32_t)exact_code(x.x, lo.x, s, inv), (uint32_t)exact_code(x.y, lo.y, s, inv),
@@ -202,7 +224,7 @@ __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? kQwResident : 2) 
         fetch(blk + a.ctas);
         const float amax = plane_amax(Piece<T>::top_of(top), share[turn], plane, part);
         float shrink;
-        const float s = grown(old, amax, first == lo, &shrink), inv = s > 0.f ? 1.f / s : 0.f;
+        const float s = grown(old, amax, first == lo, &shrink), inv = s > 0.f ? 1.f / s : 0.f, half = s > 0.f ? 0.5f * s : INFINITY;
 #pragma unroll
         for (int i = 0; i < kTurns; ++i) {
             if (!is_new(i)) continue;
@@ -212,12 +234,7 @@ __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? kQwResident : 2) 
                 Chunk<T>::unpack(in[i][c].w, y);
                 uint32_t out[kE / 4];
 #pragma unroll
-                for (int k = 0; k < kE / 4; ++k) {
-                    float far = 0.f;
-                    out[k] = s > 0.f ? codes_of(y + 4 * k, inv, &far) : 0;
-                    if (far > kNextToHalf)
-                        out[k] = exact_codes(make_float4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]), make_float4(0.f, 0.f, 0.f, 0.f), s, inv);
-                }
+                for (int k = 0; k < kE / 4; ++k) out[k] = s > 0.f ? new_codes(y + 4 * k, inv, s, half) : 0;
                 store_words(codes + i * 4 * D + (c * 8 + l8) * kE, out);
             }
         }
