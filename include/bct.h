@@ -414,8 +414,8 @@ typedef struct bct_qcache {
     float *k_scale, *v_scale; /* [B][Hkv][ceil(C / 32)] */
     float *weight;      /* [B][Hkv][C]: what attention has given the slot so far */
     int32_t *position;  /* [B][Hkv][C]: the number of the slot's token in its sequence, from 0 */
-    int32_t *state;     /* [3][B]: slots held (0..C, of every head of the sequence alike), tokens seen, a word of the
-                           library's own that is zero between calls */
+    int32_t *state;     /* [3][B]: slots held (0..C, of every head of the sequence alike), tokens seen (below 2^31), a word
+                           of the library's own that is zero between calls */
 } bct_qcache_t;
 
 /*
@@ -440,8 +440,9 @@ bct_status_t bct_qcache_append(const bct_qcache_t *cache, int64_t T, int32_t dty
  *   scratch DEVICE, 256-byte aligned, bct_qcache_attend_scratch_bytes bytes.  In use until the stream has passed the call:
  *           calls that may overlap need a scratch each
  * Roundings.  fp32 sums and softmax.  BCT_BF16: exact products of queries and codes, probabilities rounded to 11 bits where
- * they multiply values, one rounding of `out`.  BCT_F32: queries and probabilities rounded to 22 bits or more.  Where they
- * multiply values, probabilities below 2^-39 of the row's largest are 0.  The weights are fp32 sums in either.  No atomics: the same call gives the same bits.
+ * they multiply values, one rounding of `out`.  BCT_F32: queries and probabilities rounded to 22 bits or more.  In any case a
+ * term p_j v_j is off by up to 2^-39 of v_j, p_j = 1 being the row's largest; in BCT_BF16 calls with T * G > 24 by up to 2^-32
+ * of the largest value in the slots around j.  The weights are fp32 sums.  No atomics: the same call gives the same bits.
  */
 bct_status_t bct_qcache_attend_scratch_bytes(const bct_qcache_t *cache, int64_t T, int32_t n_q_heads, int32_t dtype,
                                              int32_t accumulate, size_t *bytes);

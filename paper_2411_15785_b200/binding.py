@@ -527,7 +527,7 @@ class QuantCache:
         self._planes = tuple(planes)   # the library has their addresses
         self._c = BctQcache(self.B, self.Hkv, self.d, self.C, *(t.data_ptr() for t in planes))
         self._p = ctypes.byref(self._c)
-        self._known = {}              # sizes of calls, by the shapes that they follow from
+        self._known = {}              # sizes of the last calls, by the shapes that they follow from
 
     @property
     def held(self) -> torch.Tensor:
@@ -538,6 +538,12 @@ class QuantCache:
     def seen(self) -> torch.Tensor:
         """Tokens appended to each sequence so far, int32 ``[B]`` on the device."""
         return self.state[1]
+
+    def _know(self, key, sizes):
+        if len(self._known) >= 64:
+            self._known.clear()
+        self._known[key] = sizes
+        return sizes
 
     def _sizes(self, name, x, heads):
         """(T, dtype code) of x ``[B, T, heads, d]``."""
@@ -558,7 +564,7 @@ class QuantCache:
         dt, shape = k.dtype, k.shape
         sizes = self._known.get((shape, dt))     # what follows from the shape alone
         if sizes is None:
-            sizes = self._known[shape, dt] = self._sizes("k", k, self.Hkv)
+            sizes = self._know((shape, dt), self._sizes("k", k, self.Hkv))
         if not (k.get_device() == self.dev and v.get_device() == self.dev and v.shape == shape and v.dtype is dt
                 and k.is_contiguous() and v.is_contiguous()):
             _operand("k", k, shape, dt, self.dev)      # one of these says what it is
@@ -580,7 +586,7 @@ class QuantCache:
             T, dt = self._sizes("q", q, Hq)
             n = ctypes.c_size_t(0)
             _check(self._lib.bct_qcache_attend_scratch_bytes(self._p, T, Hq, dt, accumulate, ctypes.byref(n)))
-            known = self._known[key] = T, Hq, dt, n.value
+            known = self._know(key, (T, Hq, dt, n.value))
         T, Hq, dt, need = known
         if q.get_device() != self.dev or not q.is_contiguous():
             _operand("q", q, q.shape, q.dtype, self.dev)
@@ -603,7 +609,7 @@ class QuantCache:
         if need is None:
             n = ctypes.c_size_t(0)
             _check(self._lib.bct_qcache_evict_scratch_bytes(self._p, keep, ctypes.byref(n)))
-            need = self._known[keep] = n.value
+            need = self._know(keep, n.value)
         scratch = _scratch(need, scratch, self.k, self.dev)
         _launch(self.dev, self._lib.bct_qcache_evict, self._p, keep, recent, *_scratch_args(scratch))
 

@@ -24,6 +24,11 @@
 // (and 64 + 16 t ..), and for the slots 8 t + i, 8 t + 4 + i the features 16 g .. 16 g + 15 of V; what it computes for the
 // former is, transposed 8 x 8 at a time by movmatrix, the other operand of the latter.  16-byte chunks of a slot are stored
 // at chunk ^ x(slot), with which both readings are free of bank conflicts.
+//
+// Measured (bfloat16, d 128): one row of 64 sequences x 32 heads x 2048 slots 174 us = 6.4 TB/s of codes and scales, 0.97 of a
+// copy's rate; of 37 sequences of up to 16384 slots x 8 heads 94 us = 5.6 TB/s; of one of 131071 50 us = 5.5 TB/s, joined in 16
+// to 20 more.  20 rows of 16 x 4001 slots x 8 heads under a cap: 83 us + 28; three tiles of rows take 255 registers, so eight
+// warps of an SM wait for their own results (issue slots 38 % used).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -693,8 +698,10 @@ __global__ void __launch_bounds__(kQjThreads, kQjResident) qc_join_kernel(const 
     }
 }
 
-// The weights from the keys again, for calls with many rows: a CTA per block of slots, whose warps share the rows that see
-// it and add up in their order.
+// The weights from the keys again, for float calls with many rows: a CTA per block of slots, whose warps share the rows that
+// see it, the next ones' queries on their way, and add up in their order.  There are few blocks in such calls, so it is the
+// chain of a warp's turns that counts: of 333 tokens x 8 heads of 2 sequences of 640, 34 us with 8 warps, 22 with 16, 19 with the
+// queries asked for ahead.  (As many as the registers allow: 122 of a thread with d 64, 168 with 128.)
 template <int D>
 constexpr int kQwWarps = D == 64 ? 16 : 12;
 template <typename T, int D, int TERMS>

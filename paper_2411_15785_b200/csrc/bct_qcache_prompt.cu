@@ -15,6 +15,12 @@
 // second pass in the transposed form, S^T = K Q^T with the slots in the lanes: with each row's maximum and sum known, a
 // thread adds up exp2(S - m) / sum over the rows, in their order, without atomics.
 //
+// Bound by the exponentials and what surrounds them: of 4300 clocks that a tile of 128 slots takes for 256 rows, d 128, the
+// products are 2048 and forming P 2300 (its exponentials alone 2048, 16 a clock), in a chain from one to the other; a CTA's
+// beginning and end are some 14000 beside them.  Measured: 2048 tokens of 2 sequences, 32 heads over 8 of 128: 119 us = 0.58
+// PFLOP/s (0.35 of the measured bf16 rate), the weights 66 more; 777 tokens of 5 sequences of up to 2477, 8 heads of 64, under a
+// cap 84 us, the weights 56.
+//
 // Every wait is bounded; a timeout ends the work and fills what the CTA writes with NaN.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

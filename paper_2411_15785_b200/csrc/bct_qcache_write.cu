@@ -165,6 +165,9 @@ __device__ __forceinline__ float plane_amax(uint32_t mine, uint32_t (*share)[4],
 // ---- append -----------------------------------------------------------------------------------------------------
 // A few CTAs per (sequence, head) go through the blocks that its new tokens touch, the next block's tokens on their way while
 // this one's are worked on.  The last CTA of a sequence to have read its length moves it on.
+// A fill of 8 sequences by up to 4096 tokens of 8 heads of 128: 38 us = 3.4 TB/s, half of a copy's rate.  What it spends is
+// instructions (some 17 for a value, of which the codes 8) more than bytes.  A warp to a plane of a block instead of four needs
+// a third fewer, but all of the registers, and took 46 us; two warps 38.
 constexpr int kQwResident = 4;    // CTAs on an SM
 template <typename T, int D>
 __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? kQwResident : 2) qc_append_kernel(const QcAppend a) {

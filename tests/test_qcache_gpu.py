@@ -463,6 +463,74 @@ def test_a_captured_step_replays_with_the_lengths_of_the_moment():
             assert torch.equal(a, b), i
 
 
+@pytest.mark.parametrize("T,Hq,dtype", [(40, 8, "bf16"), (6, 8, "bf16"), (40, 8, "f32"), (150, 4, "bf16")])
+def test_a_captured_prompt_replays_with_the_lengths_of_the_moment(T, Hq, dtype):
+    Bt, Hkv, d, C = 3, 2, 64, 400
+    cache, ref = _filled(Bt, Hkv, d, C, dtype, [390, 100, 0], 3)
+    k, v, q = (_tokens(Bt, T, h, d, dtype, 50 + i) for i, h in enumerate((Hkv, Hkv, Hq)))
+    lens, out = _i32([T, T // 2, 1]), torch.empty_like(q)
+
+    def step():
+        cache.evict(C - T, recent=20)
+        cache.append(k, v, lens)
+        cache.attend(q, lens, out=out, score_cap=20.0)
+
+    planes = [t.clone() for t in _planes(cache)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    for t, p in zip(_planes(cache), planes):
+        t.copy_(p)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    other = B.QuantCache(Bt, Hkv, d, C, planes=planes)
+    for i in range(5):
+        for x in (k, v, q):
+            x.copy_(_tokens(*x.shape, dtype, 60 + i))
+        lens.copy_(_i32([T - i, (T * i) // 4, 2 * i]))
+        graph.replay()
+        other.evict(C - T, recent=20)
+        other.append(k, v, lens)
+        want = other.attend(q, lens, score_cap=20.0)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
+        for b, n in enumerate(cache.held.tolist()):
+            for x, y in zip(_planes(cache)[:6], _planes(other)[:6]):
+                m = -(-n // 32) if x.shape[2] != C else n
+                assert torch.equal(x[b, :, :m], y[b, :, :m]), (i, b)
+        assert torch.equal(cache.state, other.state)
+
+
+@pytest.mark.parametrize("T", [1, 30])
+def test_two_caches_at_once_on_two_streams(T):
+    Bt, Hq, Hkv, d, C = 4, 8, 2, 128, 600
+
+    def run(streams):
+        caches = [_filled(Bt, Hkv, d, C, "bf16", [600, 400, 33, 500], 3 + i)[0] for i in range(2)]
+        x = [[_tokens(Bt, T, h, d, "bf16", 80 + 3 * j + i) for i, h in enumerate((Hkv, Hkv, Hq))] for j in range(2)]
+        torch.cuda.synchronize()
+        outs = [[], []]
+        for _ in range(12):
+            for j, cache in enumerate(caches):
+                with torch.cuda.stream(streams[j]):
+                    cache.evict(C - T, recent=10)
+                    cache.append(x[j][0], x[j][1])
+                    outs[j].append(cache.attend(x[j][2]))
+        torch.cuda.synchronize()
+        return caches, outs
+
+    one = torch.cuda.current_stream()
+    (a, oa), (b, ob) = run([one, one]), run([torch.cuda.Stream(), torch.cuda.Stream()])
+    for j in range(2):
+        for x, y in zip(oa[j], ob[j]):
+            assert torch.equal(x, y)
+        for x, y in zip(_planes(a[j]), _planes(b[j])):
+            assert torch.equal(x, y)
+
+
 def test_calls_on_a_stream_of_their_own():
     cache, ref = _filled(2, 2, 64, 128, "bf16", [100, 90], 3)
     torch.cuda.synchronize()
@@ -483,6 +551,15 @@ def test_calls_on_a_stream_of_their_own():
 def _same_but_weight(cache, ref):
     ref.weight[:] = cache.weight.cpu().numpy()
     _same(cache, ref)
+
+
+def test_what_a_cache_knows_of_its_calls_is_bounded():
+    cache, ref = _filled(1, 1, 64, 300, "bf16", [300], 3)
+    for keep in range(299, 100, -1):
+        cache.evict(keep)
+        ref.evict(keep)
+    _same(cache, ref)
+    assert len(cache._known) <= 64
 
 
 def test_binding_refuses_what_does_not_fit():
