@@ -47,7 +47,13 @@ namespace {
 
 constexpr int kQaWarps = 8;
 constexpr int kQaThreads = kQaWarps * 32;
-constexpr int kQaStages = 3;
+// Three tiles of rows leave no registers for their queries: those stand in shared memory then, in place of a stage.
+template <int NT>
+constexpr bool kQueriesShared = NT == 3;
+template <int NT>
+constexpr int kQaStages = kQueriesShared<NT> ? 2 : 3;
+template <int D, int NT>
+constexpr int kQaQueries = kQueriesShared<NT> ? NT * (D / 16) * 32 * 8 : 0;   // bytes of a warp
 constexpr int kQaScored = kQcScoredRows;
 constexpr int kQjThreads = 128;
 constexpr int kQjResident = 8;        // CTAs of the joining kernel on an SM
@@ -147,9 +153,9 @@ __device__ __forceinline__ void load_keys(const unsigned char* tile, int g, int 
 }
 
 // Products of a block's keys with eight rows: s[mt][..] for the slots i = 2 mt (c0, c1: rows 2t, 2t + 1), 2 mt + 1 (c2, c3).
-template <int D, int TERMS, int NT>
-__device__ __forceinline__ void score_products(const uint32_t (&w)[4][D / 16], const uint32_t (&q)[NT][TERMS][D / 16][2],
-                                               float (&s)[NT][2][4]) {
+// q(tile, term, step) is a lane's fragment of the queries.
+template <int D, int TERMS, int NT, typename Q>
+__device__ __forceinline__ void score_products(const uint32_t (&w)[4][D / 16], Q q, float (&s)[NT][2][4]) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -163,8 +169,10 @@ __device__ __forceinline__ void score_products(const uint32_t (&w)[4][D / 16], c
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int term = 0; term < TERMS; ++term)
-                    mma16816(s[nt][mt], a0, a1, a2, a3, q[nt][term][ks][0], q[nt][term][ks][1]);
+                for (int term = 0; term < TERMS; ++term) {
+                    const uint2 f = q(nt, term, ks);
+                    mma16816(s[nt][mt], a0, a1, a2, a3, f.x, f.y);
+                }
         }
     }
 }
@@ -194,9 +202,13 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
     constexpr int kRows = 8 * NT;
     extern __shared__ __align__(128) unsigned char qa_smem[];
     __shared__ int64_t upto[kQaThreads];
-    __shared__ float2 scales_all[kQaWarps][kQaStages];
+    constexpr int kStages = kQaStages<NT>;
+    constexpr bool kShared = kQueriesShared<NT>;
+    static_assert(!kShared || TERMS == 1);
+    __shared__ float2 scales_all[kQaWarps][kStages];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    unsigned char* ring = qa_smem + warp * (kQaStages * 2 * kTile);
+    unsigned char* ring = qa_smem + warp * (kStages * 2 * kTile + kQaQueries<D, NT>);
+    uint2* shared_q = reinterpret_cast<uint2*>(ring + kStages * 2 * kTile) + lane;   // [tile][step][lane]
     const float2* scales = scales_all[warp];
 
     pdl_wait();
@@ -275,7 +287,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
         cp_async_commit();
     };
 #pragma unroll
-    for (int s = 0; s < kQaStages - 1; ++s) fetch(s);
+    for (int s = 0; s < kStages - 1; ++s) fetch(s);
     int stage = 0;
 
     while (x < end) {
@@ -288,7 +300,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
         const Sees sees = sees_of(a, b);
 
         // rows 2t, 2t + 1 of each tile of eight are this lane's in the scores and outputs, row g in the queries
-        uint32_t q[NT][TERMS][D / 16][2];
+        uint32_t q[kShared ? 1 : NT][TERMS][D / 16][2];
         float mul[NT][2];
         int lim[NT][2];
         int lim_max = 0, lim_min = 0x7fffffff;
@@ -296,7 +308,11 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
         for (int nt = 0; nt < NT; ++nt) {
             const int64_t r = r0 + nt * 8 + g;
             float m;
-            load_queries<T, D, TERMS>(row_of<T>(a, a.q, b, h, r < a.R ? r : 0), r < a.R && sees(r) > 0, q[nt], &m);
+            load_queries<T, D, TERMS>(row_of<T>(a, a.q, b, h, r < a.R ? r : 0), r < a.R && sees(r) > 0, q[kShared ? 0 : nt], &m);
+            if constexpr (kShared) {
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) shared_q[(nt * (D / 16) + ks) * 32] = make_uint2(q[0][0][ks][0], q[0][0][ks][1]);
+            }
             m = row_factor(a, m);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -319,12 +335,12 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
             l_run[nt][0] = l_run[nt][1] = 0.f;
         }
         for (int i = first; i < last; ++i) {
-            cp_async_wait<kQaStages - 2>();
+            cp_async_wait<kStages - 2>();
             __syncwarp();
-            fetch(stage == 0 ? kQaStages - 1 : stage - 1);
+            fetch(stage == 0 ? kStages - 1 : stage - 1);
             const unsigned char* tile = ring + stage * 2 * kTile;
             const float ks = scales[stage].x, vs = scales[stage].y;
-            if (++stage == kQaStages) stage = 0;
+            if (++stage == kStages) stage = 0;
             if (i >= stop) {
                 __syncwarp();
                 continue;
@@ -334,7 +350,10 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
             {
                 uint32_t w[4][D / 16];
                 load_keys<D>(tile, g, t, w);
-                score_products<D, TERMS, NT>(w, q, s);
+                score_products<D, TERMS, NT>(w, [&](int nt, int term, int ks) {
+                    if constexpr (kShared) return shared_q[(nt * (D / 16) + ks) * 32];
+                    else return make_uint2(q[nt][term][ks][0], q[nt][term][ks][1]);
+                }, s);
             }
             const int slot0 = i * kQcBlock + 8 * (g >> 1) + 4 * (g & 1);
             const bool all = (i + 1) * kQcBlock <= lim_min;
@@ -756,7 +775,7 @@ __global__ void __launch_bounds__(32 * kQwWarps<D>) qc_weights_kernel(const QcAt
         const float2 ml[2] = {next_ml[0], next_ml[1]};
         ask(r0 + 8 * kQwWarps<D>);
         float s[1][2][4];
-        score_products<D, TERMS, 1>(w, q, s);
+        score_products<D, TERMS, 1>(w, [&](int, int term, int ks) { return make_uint2(q[0][term][ks][0], q[0][term][ks][1]); }, s);
         to_scores(s[0], __shfl_sync(0xffffffffu, m, 8 * t) * ks, __shfl_sync(0xffffffffu, m, 8 * t + 4) * ks, a.cap);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -783,7 +802,7 @@ __global__ void __launch_bounds__(32 * kQwWarps<D>) qc_weights_kernel(const QcAt
 
 template <typename T, int D, int NT, int TERMS>
 cudaError_t attend_with(const QcAttend& a, cudaStream_t s) {
-    constexpr int smem = kQaWarps * kQaStages * 2 * kQcBlock * D;
+    constexpr int smem = kQaWarps * (kQaStages<NT> * 2 * kQcBlock * D + kQaQueries<D, NT>);
     static std::atomic<uint64_t> done{0};
     if (const cudaError_t e = allow_smem(qc_attend_kernel<T, D, NT, TERMS>, smem, &done)) return e;
     return pdl_launch(qc_attend_kernel<T, D, NT, TERMS>, (a.n_warps + kQaWarps - 1) / kQaWarps, kQaThreads, smem, s, a);
