@@ -27,7 +27,7 @@
 //
 // Measured (bfloat16, d 128): one row of 64 sequences x 32 heads x 2048 slots 174 us = 6.4 TB/s of codes and scales, 0.97 of a
 // copy's rate; of 37 sequences of up to 16384 slots x 8 heads 94 us = 5.6 TB/s; of one of 131071 50 us = 5.5 TB/s, joined in 16
-// to 20 more.  20 rows of 16 x 4001 slots x 8 heads under a cap: 83 us + 28; three tiles of rows take 255 registers, so eight
+// to 20 more.  20 rows of 16 x 4001 slots x 8 heads under a cap: 76 us + 28; three tiles of rows take 255 registers, so eight
 // warps of an SM wait for their own results (issue slots 38 % used).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -47,13 +47,14 @@ namespace {
 
 constexpr int kQaWarps = 8;
 constexpr int kQaThreads = kQaWarps * 32;
-// Three tiles of rows leave no registers for their queries: those stand in shared memory then, in place of a stage.
+// Two tiles of rows or more leave no registers for their queries: those stand in shared memory then, in place of a stage (16
+// rows of 64 x 2048 slots x 8 heads 124 -> 116 us, 24 rows 198 -> 181).
 template <int NT>
-constexpr bool kQueriesShared = NT == 3;
+constexpr bool kQueriesShared = NT >= 2;
 template <int NT>
 constexpr int kQaStages = kQueriesShared<NT> ? 2 : 3;
-template <int D, int NT>
-constexpr int kQaQueries = kQueriesShared<NT> ? NT * (D / 16) * 32 * 8 : 0;   // bytes of a warp
+template <int D, int NT, int TERMS>
+constexpr int kQaQueries = kQueriesShared<NT> ? NT * TERMS * (D / 16) * 32 * 8 : 0;   // bytes of a warp
 constexpr int kQaScored = kQcScoredRows;
 constexpr int kQjThreads = 128;
 constexpr int kQjResident = 8;        // CTAs of the joining kernel on an SM
@@ -204,11 +205,10 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
     __shared__ int64_t upto[kQaThreads];
     constexpr int kStages = kQaStages<NT>;
     constexpr bool kShared = kQueriesShared<NT>;
-    static_assert(!kShared || TERMS == 1);
     __shared__ float2 scales_all[kQaWarps][kStages];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    unsigned char* ring = qa_smem + warp * (kStages * 2 * kTile + kQaQueries<D, NT>);
-    uint2* shared_q = reinterpret_cast<uint2*>(ring + kStages * 2 * kTile) + lane;   // [tile][step][lane]
+    unsigned char* ring = qa_smem + warp * (kStages * 2 * kTile + kQaQueries<D, NT, TERMS>);
+    uint2* shared_q = reinterpret_cast<uint2*>(ring + kStages * 2 * kTile) + lane;   // [tile][term][step][lane]
     const float2* scales = scales_all[warp];
 
     pdl_wait();
@@ -311,7 +311,10 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
             load_queries<T, D, TERMS>(row_of<T>(a, a.q, b, h, r < a.R ? r : 0), r < a.R && sees(r) > 0, q[kShared ? 0 : nt], &m);
             if constexpr (kShared) {
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) shared_q[(nt * (D / 16) + ks) * 32] = make_uint2(q[0][0][ks][0], q[0][0][ks][1]);
+                for (int i = 0; i < TERMS * (D / 16); ++i) {
+                    const uint32_t(&f)[2] = q[0][i / (D / 16)][i % (D / 16)];
+                    shared_q[(nt * TERMS * (D / 16) + i) * 32] = make_uint2(f[0], f[1]);
+                }
             }
             m = row_factor(a, m);
 #pragma unroll
@@ -351,7 +354,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
                 uint32_t w[4][D / 16];
                 load_keys<D>(tile, g, t, w);
                 score_products<D, TERMS, NT>(w, [&](int nt, int term, int ks) {
-                    if constexpr (kShared) return shared_q[(nt * (D / 16) + ks) * 32];
+                    if constexpr (kShared) return shared_q[((nt * TERMS + term) * (D / 16) + ks) * 32];
                     else return make_uint2(q[nt][term][ks][0], q[nt][term][ks][1]);
                 }, s);
             }
@@ -802,7 +805,7 @@ __global__ void __launch_bounds__(32 * kQwWarps<D>) qc_weights_kernel(const QcAt
 
 template <typename T, int D, int NT, int TERMS>
 cudaError_t attend_with(const QcAttend& a, cudaStream_t s) {
-    constexpr int smem = kQaWarps * (kQaStages<NT> * 2 * kQcBlock * D + kQaQueries<D, NT>);
+    constexpr int smem = kQaWarps * (kQaStages<NT> * 2 * kQcBlock * D + kQaQueries<D, NT, TERMS>);
     static std::atomic<uint64_t> done{0};
     if (const cudaError_t e = allow_smem(qc_attend_kernel<T, D, NT, TERMS>, smem, &done)) return e;
     return pdl_launch(qc_attend_kernel<T, D, NT, TERMS>, (a.n_warps + kQaWarps - 1) / kQaWarps, kQaThreads, smem, s, a);
