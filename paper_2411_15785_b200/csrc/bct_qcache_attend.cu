@@ -342,7 +342,8 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
             __syncwarp();
             fetch(stage == 0 ? kStages - 1 : stage - 1);
             const unsigned char* tile = ring + stage * 2 * kTile;
-            const float ks = scales[stage].x, vs = scales[stage].y;
+            const float ks = scales[stage].x;
+            float vs = scales[stage].y;
             if (++stage == kStages) stage = 0;
             if (i >= stop) {
                 __syncwarp();
@@ -420,6 +421,17 @@ __global__ void __launch_bounds__(kQaThreads, 1) qc_attend_kernel(const QcAttend
                 }
             }
 
+            if (vs != vs) {                                   // spoilt values: the rows that see the block have them, no others
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (lim[nt][e] > i * kQcBlock) {
+#pragma unroll
+                            for (int f = 0; f < kMt; ++f) o[nt][f][e] = o[nt][f][2 + e] = vs;
+                        }
+                vs = 0.f;
+            }
             // V: for the slots 8 t + i (e = 0) and 8 t + 4 + i (e = 1) the lane's D / 8 features, 16 or 8 from 16 g or 8 g on
             const unsigned char* vt = tile + kTile;
 #pragma unroll

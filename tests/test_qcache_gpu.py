@@ -186,6 +186,21 @@ def test_a_value_that_is_not_finite_spoils_its_block_only(what):
     assert bool(torch.isfinite(out[0, 0, 0]).all()) and bool(torch.isnan(out[0, 0, 1]).all())
 
 
+@pytest.mark.parametrize("plane", ["k", "v"])
+@pytest.mark.parametrize("T,Hq,dtype", [(3, 2, "bf16"), (30, 1, "bf16"), (40, 4, "bf16"), (60, 16, "bf16"), (70, 2, "f32"), (6, 1, "f32"),
+                                        (180, 2, "bf16"), (200, 4, "bf16")])
+def test_rows_that_do_not_see_a_spoilt_block_stay_clean(T, Hq, dtype, plane):
+    held = 64 + min(T, 32) // 2                                # the last block is seen by the later half of the last tokens
+    cache, ref = _filled(1, 1, 64, 300, dtype, [held], 3)
+    clean = cache.attend(_tokens(1, T, Hq, 64, dtype, 7), accumulate=False)
+    getattr(cache, plane + "_scale")[0, 0, 2] = float("nan")
+    out = cache.attend(_tokens(1, T, Hq, 64, dtype, 7))
+    sees = torch.clamp(held - T + 1 + torch.arange(T), min=0)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(out[0, sees.cuda() > 64]).all())
+    assert torch.equal(out[0, sees.cuda() <= 64], clean[0, sees.cuda() <= 64])
+
+
 # ---- attention --------------------------------------------------------------------------------------------------
 
 STEPS = [  # Bt, Hq, Hkv, d, dtype, C, held
