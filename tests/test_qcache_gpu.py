@@ -519,6 +519,37 @@ def test_a_captured_prompt_replays_with_the_lengths_of_the_moment(T, Hq, dtype):
         assert torch.equal(cache.state, other.state)
 
 
+@pytest.mark.parametrize("T,Hq,dtype", [(1, 2, "bf16"), (5, 4, "bf16"), (40, 4, "bf16"), (150, 8, "bf16"), (1, 2, "f32"), (40, 4, "f32")])
+def test_what_memory_held_before_makes_no_difference(T, Hq, dtype):
+    """Planes full of NaN, infinities and odd codes (but for the state): the calls go by what they have written."""
+    Bt, Hkv, d, C = 3, 2, 64, 420
+    clean = B.QuantCache(Bt, Hkv, d, C)
+    planes = [t.clone() for t in _planes(clean)]
+    planes[0].fill_(-128), planes[1].fill_(-77)
+    planes[2].fill_(float("nan")), planes[3].fill_(float("inf")), planes[4].fill_(float("nan")), planes[5].fill_(0x7fffffff)
+    dirty = B.QuantCache(Bt, Hkv, d, C, planes=planes)
+    got = []
+    for cache in (clean, dirty):
+        outs = []
+        for i, (n, lens) in enumerate([(T, [T, 0, 1]), (200, [200, 3, 64]), (T, None), (150, [10, 150, 33]), (T, None)]):
+            k, v = (_tokens(Bt, n, Hkv, d, dtype, 90 + 3 * i + j, 0.4) for j in range(2))
+            cache.evict(C - n, recent=8)
+            cache.append(k, v, _i32(lens))
+            outs.append(cache.attend(_tokens(Bt, n, Hq, d, dtype, 70 + i), _i32(lens)))
+            outs.append(cache.attend(_tokens(Bt, T, Hq, d, dtype, 80 + i), accumulate=False))
+        cache.evict(97, recent=5)
+        outs.append(cache.attend(_tokens(Bt, T, Hq, d, dtype, 60)))
+        got.append(outs)
+    torch.cuda.synchronize()
+    for i, (x, y) in enumerate(zip(*got)):
+        assert bool(torch.isfinite(x).all()) and torch.equal(x, y), i
+    assert torch.equal(clean.state, dirty.state)
+    for b, n in enumerate(clean.held.tolist()):
+        for x, y in zip(_planes(clean)[:6], _planes(dirty)[:6]):
+            m = -(-n // 32) if x.shape[2] != C else n
+            assert torch.equal(x[b, :, :m], y[b, :, :m]), b
+
+
 @pytest.mark.parametrize("T", [1, 30])
 def test_two_caches_at_once_on_two_streams(T):
     Bt, Hq, Hkv, d, C = 4, 8, 2, 128, 600
@@ -566,6 +597,81 @@ def test_calls_on_a_stream_of_their_own():
 def _same_but_weight(cache, ref):
     ref.weight[:] = cache.weight.cpu().numpy()
     _same(cache, ref)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_cache_whose_offsets_pass_32_bits(dtype):
+    Hkv, d, C = 2, 128, (1 << 23) + 40                         # 2^31 codes and more to a plane
+    held = C - 7
+    cache = B.QuantCache(1, Hkv, d, C)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for x in (cache.k, cache.v):
+        x.view(-1).random_(-127, 128, generator=g)
+    for x in (cache.k_scale, cache.v_scale):
+        x.uniform_(0.01, 0.02, generator=g)
+    cache.position[:] = torch.arange(C, dtype=torch.int32, device="cuda")
+    cache.state[:2] = held
+    for T, Hq in ((1, 2), (3, 8), (20, 4)):
+        cache.weight.zero_()
+        q = 2.0 * _tokens(1, T, Hq, d, dtype, T)
+        out = cache.attend(q).double()
+        G = Hq // Hkv
+        for h in range(Hkv):
+            x = q[0, :, h * G:(h + 1) * G].double().reshape(T * G, d)
+            lim = torch.repeat_interleave(held - T + 1 + torch.arange(T, device="cuda"), G)[:, None]
+            n_at = 1 << 20
+
+            def scores(at):
+                n = min(n_at, held - at)
+                of = torch.arange(at, at + n, device="cuda")
+                s = x @ (cache.k[0, h, at:at + n].double() * cache.k_scale[0, h, of // 32].double()[:, None]).T * d ** -0.5
+                return s.masked_fill(of[None, :] >= lim, float("-inf")), of
+
+            m = torch.stack([scores(at)[0].amax(-1) for at in range(0, held, n_at)]).amax(0)[:, None]
+            total, want, mag, wmax = 0.0, 0.0, 0.0, 0.0
+            parts = []
+            for at in range(0, held, n_at):
+                s, of = scores(at)
+                p = torch.exp(s - m)
+                V = cache.v[0, h, at:at + len(of)].double() * cache.v_scale[0, h, of // 32].double()[:, None]
+                total, want, mag = total + p.sum(-1, keepdim=True), want + p @ V, mag + p @ V.abs()
+                parts.append((of, p))
+            want, mag = want / total, mag / total
+            got = out[0, :, h * G:(h + 1) * G].reshape(T * G, d)
+            # scores are below 64 here: 144 * 2^-24 of that each; sums over a warp's run of blocks and over the runs' parts;
+            # probabilities and the output as everywhere (the file's head)
+            e = 2 * 144 * 2.0 ** -24 * 64 + 2.0 ** -21 + 2 * (C / 1024 + 4096) * 2.0 ** -24
+            tol = (e + 2.0 ** -11) * mag + 2.0 ** -8 * want.abs() + C * 2.0 ** -40 * 2.6
+            assert bool(((got - want).abs() <= tol).all()), (T, h, float((got - want).abs().max()))
+            for of, p in parts[:1] + parts[-1:]:
+                added = (p / total).sum(0)
+                w = cache.weight[0, h, of].double()
+                assert bool(((w - added).abs() <= (e + 80 * 2.0 ** -24) * added + 1e-30).all()), (T, h)
+    cache.weight.uniform_(0, 1, generator=g)
+    keep, recent = C - 100, 50
+    gone = torch.sort(cache.weight[0, :, :held - recent], stable=True).indices[:, :held - keep].sort().values
+    codes = cache.k.clone()
+    cache.evict(keep, recent)
+    torch.cuda.synchronize()
+    for h in range(Hkv):
+        left = torch.ones(held, dtype=torch.bool, device="cuda")
+        left[gone[h]] = False
+        assert torch.equal(cache.position[0, h, :keep].sort().values, torch.arange(held, dtype=torch.int32, device="cuda")[left])
+        stay = left[:keep]
+        moved = torch.zeros((keep + 31) // 32 * 32, dtype=torch.bool, device="cuda")
+        moved[:keep] = ~stay
+        quiet = ~moved.view(-1, 32).any(-1)
+        of = torch.nonzero(quiet).flatten()[-3:]               # blocks without holes are as they were
+        for blk in of.tolist():
+            assert torch.equal(cache.k[0, h, 32 * blk:32 * blk + 32], codes[0, h, 32 * blk:32 * blk + 32])
+    k = _tokens(1, 60, Hkv, d, dtype, 9)
+    cache.append(k, k)
+    torch.cuda.synchronize()
+    assert cache.held.tolist() == [keep + 60] and cache.seen.tolist() == [held + 60]
+    of = torch.arange(keep, keep + 60, device="cuda")
+    for h in range(Hkv):
+        s = cache.k_scale[0, h, of // 32].double()[:, None]
+        assert bool(((cache.k[0, h, of].double() * s - k[0, :, h].double()).abs() <= 0.5 * s * (1 + 1e-6)).all())
 
 
 def test_what_a_cache_knows_of_its_calls_is_bounded():
