@@ -98,8 +98,8 @@ bct_status_t check_scratch(const void* scratch, size_t bytes, size_t need) {
 inline bool grid_fits(int64_t units, int64_t ctas) { return ctas <= 0x7fffffff / units; }
 
 // Many bfloat16 rows go to the tensor path, whose time does not depend on how many there are up to 128: 24 rows of 16 x 4096
-// slots x 8 heads take 106 us on the other and 116 on it, of 64 x 2048 181 / 229, of 4 x 32768 x 4 heads 104 / 122; 16 rows of
-// 64 x 2048 114 / 228.  (From 25 rows on the other one would read the codes twice.)  Otherwise rows are served in groups of 8, 16 or 24 (16 in float, whose
+// slots x 8 heads take 110 us on the other and 116 on it, of 64 x 2048 187 / 229, of 4 x 32768 x 4 heads 108 / 122; 16 rows of
+// 64 x 2048 118 / 228.  (From 25 rows on the other one would read the codes twice.)  Otherwise rows are served in groups of 8, 16 or 24 (16 in float, whose
 // queries and probabilities are two terms each).
 bct_status_t plan_attend(const QcView& v, int64_t T, int32_t n_q_heads, int32_t dtype, int32_t accumulate, bct::QcPlan* p) {
     if (n_q_heads < 1 || n_q_heads > (1 << 16) || n_q_heads % v.Hkv != 0)

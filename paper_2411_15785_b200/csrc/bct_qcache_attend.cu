@@ -27,8 +27,8 @@
 //
 // Measured (bfloat16, d 128): one row of 64 sequences x 32 heads x 2048 slots 174 us = 6.4 TB/s of codes and scales, 0.97 of a
 // copy's rate; of 37 sequences of up to 16384 slots x 8 heads 94 us = 5.6 TB/s; of one of 131071 50 us = 5.5 TB/s, joined in 16
-// to 20 more.  20 rows of 16 x 4001 slots x 8 heads under a cap: 76 us + 28; three tiles of rows take 255 registers, so eight
-// warps of an SM wait for their own results (issue slots 38 % used).
+// to 20 more.  20 rows of 16 x 4001 slots x 8 heads under a cap: 78 us + 28; three tiles of rows take 255 registers, so eight
+// warps of an SM wait for their own results (issue slots 42 % used).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -48,7 +48,7 @@ namespace {
 constexpr int kQaWarps = 8;
 constexpr int kQaThreads = kQaWarps * 32;
 // Two tiles of rows or more leave no registers for their queries: those stand in shared memory then, in place of a stage (16
-// rows of 64 x 2048 slots x 8 heads 124 -> 116 us, 24 rows 198 -> 181).
+// rows of 64 x 2048 slots x 8 heads 124 -> 118 us, 24 rows 198 -> 187).
 template <int NT>
 constexpr bool kQueriesShared = NT >= 2;
 template <int NT>
