@@ -402,7 +402,8 @@ bct_status_t bct_norm_rotate_backward(int64_t n_tokens, int32_t n_q_heads, int32
  * smallest power of two with which that holds, and the codes it keeps are divided by it.  Codes are rounded to the nearest,
  * ties to the even one, and limited to -127..127.  So a value is off by half a step when it is written, and by less than
  * one step of its block's scale at any time (a slot that an eviction moves is rounded once more, as a new one).  A NaN or an
- * infinity makes its block's scale a NaN, and every output that sees the block, until the block is written anew.
+ * infinity makes its block's scale a NaN, and every output that sees the block, until the block is written anew; in a key, also
+ * the weights that the rows which see it give.
  */
 #define BCT_QCACHE_BLOCK 32
 typedef struct bct_qcache {

@@ -29,12 +29,6 @@ cudaError_t pdl_launch(void (*kernel)(P...), unsigned grid, unsigned threads, si
     return cudaLaunchKernelEx(&c, kernel, args...);
 }
 
-// The larger one, or a NaN if either is one.
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float y;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-    return y;
-}
 // The opt-in for more than 48 KiB of shared memory, once for each device; done: a kernel's own, a bit per device.
 template <typename K>
 cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>* done) {

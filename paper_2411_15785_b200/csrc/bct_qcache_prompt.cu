@@ -508,6 +508,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
         float m = -INFINITY, vref = 0.f, vmost = 0.f;
         const float cap = a.cap * kLog2e;
         float l = 0.f;
+        bool spoilt = false;
         // lane c (of four) has the scales of a tile's block c, a tile ahead
         float ks_next = 0.f, vs_next = 0.f;
         auto load_scales = [&](int n) {
@@ -535,8 +536,10 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
                     if (vref > 0.f && to > 0.f) by_v = vref / to;
                     if (to > 0.f) vref = to;
                 }
-                // P's factor of the lane's block, as a power of two and inverted; a block of zeros has any
-                const float v_rel = vs == 0.f ? kQpPScale : max_nan(__fdividef(vs, vref > 0.f ? vref : 1.f), 8.67361738e-19f) * kQpPScale;
+                // P's factor of the lane's block, as a power of two and inverted; a block of zeros has any, and one of spoilt values,
+                // which the rows that see it are given at the end
+                const float v_rel = vs > 0.f ? fmaxf(__fdividef(vs, vref > 0.f ? vref : 1.f), 8.67361738e-19f) * kQpPScale : kQpPScale;
+                if (const unsigned bad = __ballot_sync(0xffffffffu, vs != vs) & 15u) spoilt |= lim > slot0 + 32 * (__ffs(bad) - 1);
                 const float v_log = __log2f(v_rel), v_inv = __fdividef(1.f, v_rel);
                 qp_wait(&s_full[sub], turn, abort_flag);
                 tc_fence_after();
@@ -635,6 +638,7 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
         const bool there = r < a.R;
         const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
         if (pr.parts == 1) mul = l == l ? mul * inv : l;
+        if (spoilt) mul = __uint_as_float(0x7fffffffu);
         const int64_t at = ((int64_t)unit * a.R + r) * pr.parts + (by_slots ? 2 * split + sub : split);
         // (through the warp's part of the queries' tile, which is free by now, so that rows are written in one piece)
         unsigned char* stage = smem + L::q + sub * L::kTile + (warp & 3) * (32 * D * 2);

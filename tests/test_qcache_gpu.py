@@ -199,6 +199,13 @@ def test_rows_that_do_not_see_a_spoilt_block_stay_clean(T, Hq, dtype, plane):
     torch.cuda.synchronize()
     assert bool(torch.isnan(out[0, sees.cuda() > 64]).all())
     assert torch.equal(out[0, sees.cuda() <= 64], clean[0, sees.cuda() <= 64])
+    if plane == "v":
+        # probabilities are of the keys alone: the weights are what they are without the spoilt block, within the file head's
+        # bounds (not bit by bit: a row's sum is taken relative to the blocks' value scales on the tensor path)
+        _, added, _, S, _ = ref.attend(_tokens(1, T, Hq, 64, dtype, 7), device="cuda")
+        p_off = 2 * ((64 + 16 + 4) * 2.0 ** -24 * S) + 2.0 ** -21 + 300 * 2.0 ** -24
+        w = cache.weight[0, 0, :held].double().cpu()
+        assert bool(((w - added[0, 0, :held]).abs() <= (p_off + T * Hq * 2.0 ** -24 + 2.0 ** -23) * added[0, 0, :held]).all())
 
 
 # ---- attention --------------------------------------------------------------------------------------------------
