@@ -442,7 +442,7 @@ bct_status_t bct_qcache_append(const bct_qcache_t *cache, int64_t T, int32_t dty
  *           calls that may overlap need a scratch each
  * Roundings.  fp32 sums and softmax.  BCT_BF16: exact products of queries and codes, probabilities rounded to 11 bits where
  * they multiply values, one rounding of `out`.  BCT_F32: queries and probabilities rounded to 22 bits or more.  In any case a
- * term p_j v_j is off by up to 2^-39 of v_j, p_j = 1 being the row's largest; in BCT_BF16 calls with T * G > 24 by up to 2^-32
+ * term p_j v_j is off by up to 2^-39 of v_j, p_j = 1 being the row's largest; in BCT_BF16 calls with T * G > 32 by up to 2^-32
  * of the largest value in the slots around j.  The weights are fp32 sums.  No atomics: the same call gives the same bits.
  */
 bct_status_t bct_qcache_attend_scratch_bytes(const bct_qcache_t *cache, int64_t T, int32_t n_q_heads, int32_t dtype,

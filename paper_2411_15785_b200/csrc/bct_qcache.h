@@ -9,7 +9,7 @@
 namespace bct {
 
 constexpr int kQcBlock = BCT_QCACHE_BLOCK;   // slots that share a scale
-constexpr int kQcScoredRows = 24;            // rows of a unit up to which the weights come from stored scores
+constexpr int kQcScoredRows = 32;            // rows of a unit up to which the weights come from stored scores
 
 // The caller's cache, resolved: planes by (sequence, kv-head) unit, state by sequence.
 struct QcView {

@@ -97,10 +97,10 @@ bct_status_t check_scratch(const void* scratch, size_t bytes, size_t need) {
 }
 inline bool grid_fits(int64_t units, int64_t ctas) { return ctas <= 0x7fffffff / units; }
 
-// Many bfloat16 rows go to the tensor path, whose time does not depend on how many there are up to 128: 24 rows of 16 x 4096
-// slots x 8 heads take 110 us on the other and 116 on it, of 64 x 2048 187 / 229, of 4 x 32768 x 4 heads 108 / 122; 16 rows of
-// 64 x 2048 118 / 228.  (From 25 rows on the other one would read the codes twice.)  Otherwise rows are served in groups of 8, 16 or 24 (16 in float, whose
-// queries and probabilities are two terms each).
+// Many bfloat16 rows go to the tensor path, whose time hardly depends on how many there are up to 128.  The other serves rows in
+// groups alike of 8, 16 or 24 (16 in float, whose queries and probabilities are two terms each), a reading of the codes for
+// each.  28 rows take 108 us there and 118 on the tensor path with 16 x 4096 slots x 8 heads, 202 / 233 with 64 x 2048, 79 / 112
+// with 64 x 512, 58 / 52 with one sequence of 8192; 48 rows 177 / 120, 325 / 243, 126 / 120, 87 / 54.
 bct_status_t plan_attend(const QcView& v, int64_t T, int32_t n_q_heads, int32_t dtype, int32_t accumulate, bct::QcPlan* p) {
     if (n_q_heads < 1 || n_q_heads > (1 << 16) || n_q_heads % v.Hkv != 0)
         return fail(BCT_ERR_INVALID_ARG, "n_q_heads (%d) must be a multiple of n_kv_heads (%d) in 1..65536", n_q_heads, v.Hkv);
@@ -129,7 +129,8 @@ bct_status_t plan_attend(const QcView& v, int64_t T, int32_t n_q_heads, int32_t 
         return BCT_OK;
     }
     const int most = dtype == BCT_BF16 ? 3 : 2;
-    p->tiles = (int)std::min<int64_t>(most, (R + 7) / 8);
+    const int64_t groups = (R + 8 * most - 1) / (8 * most);
+    p->tiles = (int)((R + 8 * groups - 1) / (8 * groups));        // (groups alike)
     p->rows = 8 * p->tiles;
     p->n_groups = (R + p->rows - 1) / p->rows;
     p->by_scores = accumulate != 0 && R <= bct::kQcScoredRows;

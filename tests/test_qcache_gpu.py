@@ -262,7 +262,9 @@ MANY = [  # the row counts where another kernel takes over, caches that are shar
     (2, 3, 8, 1, 128, "bf16", 150, [150, 70], [3, 1]), (2, 25, 1, 1, 128, "bf16", 150, [150, 25], None),
     (2, 24, 1, 1, 128, "f32", 150, [150, 25], None), (2, 16, 8, 1, 128, "bf16", 900, [900, 17], [16, 15]),
     (2, 32, 8, 2, 64, "bf16", 600, [600, 300], [32, 1]), (1, 30, 8, 1, 128, "bf16", 20000, [19999], None),
-    (1, 3, 24, 3, 128, "bf16", 20000, [20000], None), (2, 300, 2, 1, 128, "bf16", 9000, [9000, 8191], [300, 299]),
+    (1, 3, 24, 3, 128, "bf16", 20000, [20000], None), (2, 32, 1, 1, 64, "bf16", 170, [170, 32], None),
+    (2, 33, 1, 1, 64, "bf16", 170, [170, 33], [33, 9]), (3, 4, 16, 2, 128, "bf16", 300, [300, 129, 2], [4, 3, 1]),
+    (2, 33, 1, 1, 64, "f32", 170, [170, 33], None), (2, 32, 2, 2, 128, "f32", 400, [400, 32], [32, 20]), (2, 300, 2, 1, 128, "bf16", 9000, [9000, 8191], [300, 299]),
     (37, 20, 4, 2, 64, "bf16", 700, [(53 * i) % 701 for i in range(37)], [i % 21 for i in range(37)]),
     (37, 9, 12, 4, 128, "bf16", 520, [(37 * i) % 521 for i in range(37)], [9 - i % 10 for i in range(37)]),
     (40, 70, 16, 4, 128, "bf16", 1000, [(211 * i) % 1001 for i in range(40)], [(11 * i) % 71 for i in range(40)]),
