@@ -43,7 +43,9 @@ __device__ __forceinline__ uint32_t packed(const uint32_t (&u)[4]) {   // the lo
     return __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
 }
 // Four codes as the bytes of a word.  Adding 1.5 2^23 rounds x / s to an integer, whose low byte is the code; *far is the
-// largest distance from it: only next to a half can it be the wrong one (x inv is off by 127.5 2^-24 = 7.6e-6 at most).
+// largest distance from it: only next to a half can it be the wrong one.  x, a code times a scale, and inv are rounded, 2^-24 of
+// themselves each, so that x inv is off by 127.5 2^-23 = 1.52e-5 at most, and the distance by 2^-25 more: up to kNextToHalf =
+// 0.5 - 2e-5 the integer is the right one.  127 too is the largest then: a quotient is 127.5 at most, where 128 is further off.
 __device__ __forceinline__ uint32_t codes_of(const float* x, float inv, float* far) {
     constexpr float kMagic = 12582912.f;
     uint32_t u[4];
@@ -83,7 +85,7 @@ __device__ __noinline__ uint32_t exact_codes(float4 x, float4 lo, float s, float
                            (uint32_t)exact_code(x.z, lo.z, s, inv), (uint32_t)exact_code(x.w, lo.w, s, inv)};
     return packed(u);
 }
-constexpr float kNextToHalf = 0.49999f;
+constexpr float kNextToHalf = 0.49998f;
 // Code i of a word as a float (and no conversion, of which there are few to a clock): the byte + 128 under the exponent of 2^23
 __device__ __forceinline__ float code_at(uint32_t w, int i) {
     return __uint_as_float(__byte_perm(w ^ 0x80808080u, 0x4b000000u, 0x7440 | i)) - 8388736.f;

@@ -1,0 +1,82 @@
+"""GPU tests of the 8-bit cache where its arithmetic can go wrong: roundings next to a half.  Codes and scales are equal to the
+64-bit form."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2411_15785_b200 import binding as B
+from paper_2411_15785_b200 import build as bld
+
+import _qcache_ref as R
+from test_qcache_gpu import _same
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    bld.build()
+    B.load()
+
+
+def _near(x, steps):
+    """Floats `steps` representable numbers above x (positive, normal)."""
+    return (np.asarray(x, np.float32).view(np.int32) + np.asarray(steps, np.int32)).view(np.float32)
+
+
+# ---- moves: codes times a scale, rounded to another scale's codes ------------------------------------------------
+
+def _moved(d, holes, code, f, s, seed):
+    """A cache for each (code, f, s): an eviction leaves `holes` places in block 0, whose scale is s, and moves as many rows
+    of block 1 there, whose scale is f and whose largest code is `code`.  Equal to the 64-bit form, or fails."""
+    rng = np.random.default_rng(seed)
+    units = len(code)
+    held = 33 if holes == 1 else 64                      # (one slot alone is found in another way)
+    k = np.zeros((2, units, 1, 64, d), np.int8)
+    k[:, :, 0, :32] = rng.integers(-127, 128, (2, units, 32, d))
+    c = np.asarray(code)[None, :, None, None]
+    k[:, :, 0, 32:] = rng.integers(-c, c + 1, (2, units, 32, d))
+    at = rng.integers(0, d // 2, (2, units, 32, 1))      # each row has the code and its negative somewhere
+    np.put_along_axis(k[:, :, 0, 32:], at, np.broadcast_to(c, at.shape).astype(np.int8), -1)
+    np.put_along_axis(k[:, :, 0, 32:], at + d // 2, np.broadcast_to(-c, at.shape).astype(np.int8), -1)
+    scale = np.stack([np.asarray(s, np.float32), np.asarray(f, np.float32)], -1)[:, None]
+    weight = np.full((units, 1, 64), 1.0, np.float32)
+    for u in range(units):
+        weight[u, 0, rng.permutation(32)[:holes]] = 0
+        if held == 64:
+            weight[u, 0, 32 + rng.permutation(32)[:32 - holes]] = 0
+    state = np.stack([np.full(units, held), np.full(units, held), np.zeros(units)]).astype(np.int32)
+    position = np.broadcast_to(np.arange(64, dtype=np.int32), (units, 1, 64)).copy()
+    planes = [torch.from_numpy(x).cuda() for x in (k[0], k[1], scale, scale.copy(), weight, position, state)]
+    cache = B.QuantCache(units, 1, d, 64, planes=planes)
+    ref = R.Ref(planes)
+    cache.evict(32)
+    ref.evict(32)
+    _same(cache, ref)
+    assert int(cache.k[:, :, :32].min()) >= -127 and int(cache.v[:, :, :32].min()) >= -127
+
+
+# code, scale of the source, scale of the destination.  The quotients are 127.5 (twice), 122.5000005, 127.4999994 and 116.5;
+# fl(code f) fl(1 / s) is up to 127.5 2^-23 = 1.5e-5 away from them
+HALVES = [(119, "0x1.26ac0ep+0", "0x1.1306fcp+0"), (27, "0x1.405020p+2", "0x1.0f52eep+0"),
+          (101, "0x1.d00680p+0", "0x1.7e958ep+0"), (124, "0x1.1503ap+0", "0x1.0d68ecp+0"), (121, "0x1.ad238p+0", "0x1.bdb7p+0")]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("holes", [1, 2, 9, 31])
+@pytest.mark.parametrize("power", [0, -40, 90])
+def test_moved_codes_next_to_a_half_are_those_of_the_exact_quotient(d, holes, power):
+    _moved(d, holes, [c for c, _, _ in HALVES], [float.fromhex(f) * 2.0 ** power for _, f, _ in HALVES],
+           [float.fromhex(s) * 2.0 ** power for _, _, s in HALVES], 5 + holes)
+
+
+@pytest.mark.parametrize("d,holes", [(64, 1), (64, 3), (128, 5)])
+@pytest.mark.parametrize("power,most", [(0, 127)])
+def test_moved_codes_aimed_at_halves(d, holes, power, most):
+    rng = np.random.default_rng(17 + holes)
+    units = 1500
+    s = _near(np.float32(2.0 ** power), rng.integers(0, 1 << 23, units) | 1)
+    code = rng.integers(1, most + 1, units)
+    half = rng.integers(code, most + 1) + 0.5                               # (above the code: f is above s)
+    f = _near((half * s.astype(np.float64) / code).astype(np.float32), rng.integers(-1, 2, units))
+    _moved(d, holes, code, f, s, 23)
