@@ -187,8 +187,6 @@ __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? kQwResident : 2) 
     const int plane = threadIdx.x >> 7, part = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, l8 = lane & 7;
     const int blk_end = n > 0 ? (end - 1) / kQcBlock + 1 : 0;
     __syncthreads();          // all of this CTA have the sequence's state (their bounds are made of it)
-    int ticket = 0;
-    if (threadIdx.x == 0) ticket = atomicAdd(reinterpret_cast<int*>(a.c.state + 2 * a.c.B + b), 1);
 
     const int row_in = part * kQwRows + (lane >> 3);          // the lane's rows of a block: this one, and 4 further on at each turn
     const int64_t step = 4 * (int64_t)a.c.Hkv * D;
@@ -212,6 +210,13 @@ __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? kQwResident : 2) 
     int turn = 0;
     int blk = held / kQcBlock + w0;
     fetch(blk);
+    // (a ticket orders nothing by itself: the fences put every CTA's reading of the state before the last one's writing.  Taken
+    // while the first tokens are on their way: a fill of 8 x 4096 39 us, 40.5 in front of their loads)
+    int ticket = 0;
+    if (threadIdx.x == 0) {
+        __threadfence();
+        ticket = atomicAdd(reinterpret_cast<int*>(a.c.state + 2 * a.c.B + b), 1);
+    }
     for (; blk < blk_end; blk += a.ctas, turn ^= 1) {
         const int lo = blk * kQcBlock, first = max(held, lo), last = min(end, lo + kQcBlock), row0 = lo + row_in;
         int8_t* codes = a.c.codes[plane] + ((size_t)unit * C + row0) * D;
@@ -267,6 +272,7 @@ __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? kQwResident : 2) 
         }
     }
     if (threadIdx.x == 0 && ticket == a.ctas * a.c.Hkv - 1) {
+        __threadfence();
         a.c.state[b] = end;
         a.c.state[a.c.B + b] = seen + n;
         a.c.state[2 * a.c.B + b] = 0;

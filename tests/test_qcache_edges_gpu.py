@@ -80,3 +80,22 @@ def test_moved_codes_aimed_at_halves(d, holes, power, most):
     half = rng.integers(code, most + 1) + 0.5                               # (above the code: f is above s)
     f = _near((half * s.astype(np.float64) / code).astype(np.float32), rng.integers(-1, 2, units))
     _moved(d, holes, code, f, s, 23)
+
+
+# ---- append: the CTAs of a sequence hand its length over ---------------------------------------------------------
+
+def test_the_length_moves_on_once_whatever_the_ctas_of_a_sequence_have_to_do():
+    """Many CTAs to a sequence, most of them without a block of their own, which take their tickets at once."""
+    Bt, Hkv, d, T = 3, 64, 64, 640
+    cache = B.QuantCache(Bt, Hkv, d, 4000)
+    k = torch.ones((Bt, T, Hkv, d), dtype=torch.bfloat16, device="cuda")
+    held = torch.zeros(Bt, dtype=torch.int32, device="cuda")
+    for i in range(120):
+        lens = torch.tensor([1, i % 3, 40 * (i % 2)], dtype=torch.int32, device="cuda")
+        cache.append(k, k, lens)
+        held += lens
+    torch.cuda.synchronize()
+    assert torch.equal(cache.held, held) and torch.equal(cache.seen, held) and not bool(cache.state[2].any())
+    for b, n in enumerate(held.tolist()):
+        assert bool((cache.k[b, :, :n] == 127).all()) and bool((cache.k[b, :, n:] == 0).all())
+        assert torch.equal(cache.position[b, :, :n], torch.arange(n, dtype=torch.int32, device="cuda").expand(Hkv, n))
