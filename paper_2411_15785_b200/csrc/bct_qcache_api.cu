@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <utility>
 
 #include "bct_internal.h"
 #include "bct_qcache.h"
@@ -59,7 +60,7 @@ bct_status_t check_sizes(const bct_qcache_t* c, QcView* v) {
     v->NB = (v->C + bct::kQcBlock - 1) / bct::kQcBlock;
     return BCT_OK;
 }
-enum { kCacheSpans = 7 };
+enum { kWeightSpan = 4, kCacheSpans = 7 };
 bct_status_t check_cache(const bct_qcache_t* c, QcView* v, Span* spans) {
     if (const bct_status_t st = check_sizes(c, v)) return st;
     const size_t units = (size_t)v->B * v->Hkv, slots = units * v->C, nb = units * v->NB;
@@ -221,7 +222,8 @@ extern "C" bct_status_t bct_qcache_attend(const bct_qcache_t* cache, int64_t T, 
     s[1] = {"scratch", scratch, p.total};
     s[kCacheSpans + 2] = {"q", q, bytes};
     s[kCacheSpans + 3] = {"lens", lens, (size_t)a.c.B * 4};
-    if (bct_status_t st = check_overlap(s, kCacheSpans + 4, 2)) return st;
+    std::swap(s[2], s[2 + kWeightSpan]);   // written only if `accumulate`
+    if (bct_status_t st = check_overlap(s, kCacheSpans + 4, accumulate != 0 ? 3 : 2)) return st;
     a.q = q, a.out = out, a.lens = lens, a.T = T;
     a.G = n_q_heads / a.c.Hkv;
     a.R = T * a.G;
