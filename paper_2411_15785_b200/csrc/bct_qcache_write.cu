@@ -29,12 +29,12 @@ constexpr int kQwRows = kQcBlock / 4;
 
 // round((x + lo) / s) in -127..127, ties to the even code; |lo| is at most half an ulp of x.  q is off by one at most
 // where x / s is next to a half; r = x - q s is exact there (multiples of s's ulp, or of half of it where q is 0 or 1,
-// below s), and so are the differences from half a step that decide.
+// below s), and so are the differences of 2 r from s that decide (half of s is no float where s is among the smallest).
 __device__ __forceinline__ int exact_code(float x, float lo, float s, float inv) {
     float q = rintf(x * inv);
-    const float r = fmaf(-q, s, x), half = 0.5f * s;
+    const float r = fmaf(-q, s, x);
     const bool odd = (static_cast<int>(q) & 1) != 0;
-    const float up = (r - half) + lo, down = (r + half) + lo;
+    const float up = fmaf(2.f, lo, fmaf(2.f, r, -s)), down = fmaf(2.f, lo, fmaf(2.f, r, s));
     if (up > 0.f || (up == 0.f && odd)) q += 1.f;
     else if (down < 0.f || (down == 0.f && odd)) q -= 1.f;
     return static_cast<int>(fminf(fmaxf(q, -127.f), 127.f));
@@ -58,8 +58,8 @@ __device__ __forceinline__ uint32_t codes_of(const float* x, float inv, float* f
     return packed(u);
 }
 // Four codes of x itself.  With q the rounded x inv, r = x - q s is exact next to half a step (multiples of s's ulp or of half
-// of it): it decides whether the neighbour is right, which is one apart.
-__device__ __forceinline__ uint32_t new_codes(const float* x, float inv, float s, float half) {
+// of it): 2 r against s decides whether the neighbour is right, which is one apart.  `edge` is s, or infinity where it is 0.
+__device__ __forceinline__ uint32_t new_codes(const float* x, float inv, float s, float edge) {
     constexpr float kMagic = 12582912.f;
     float m[4], far = 0.f;
     uint32_t u[4];
@@ -69,10 +69,10 @@ __device__ __forceinline__ uint32_t new_codes(const float* x, float inv, float s
         u[i] = __float_as_uint(m[i]);
         far = fmaxf(far, fabsf(fmaf(kMagic - m[i], s, x[i])));
     }
-    if (far >= half) {
+    if (2.f * far >= edge) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float r = fmaf(kMagic - m[i], s, x[i]), over = fabsf(r) - half;
+            const float r = fmaf(kMagic - m[i], s, x[i]), over = fmaf(2.f, fabsf(r), -s);
             if (over > 0.f || (over == 0.f && (u[i] & 1))) u[i] += r > 0.f ? 1 : -1;
             u[i] = min(max(u[i], 0x4b400000u - 127u), 0x4b400000u + 127u);   // 127.5 s would be 128
         }
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? kQwResident : 2) 
         fetch(blk + a.ctas);
         const float amax = plane_amax(Piece<T>::top_of(top), share[turn], plane, part);
         float shrink;
-        const float s = grown(old, amax, first == lo, &shrink), inv = s > 0.f ? 1.f / s : 0.f, half = s > 0.f ? 0.5f * s : INFINITY;
+        const float s = grown(old, amax, first == lo, &shrink), inv = s > 0.f ? 1.f / s : 0.f, edge = s > 0.f ? s : INFINITY;
 #pragma unroll
         for (int i = 0; i < kTurns; ++i) {
             if (!is_new(i)) continue;
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kQwThreads, sizeof(T) == 2 ? kQwResident : 2) 
                 Chunk<T>::unpack(in[i][c].w, y);
                 uint32_t out[kE / 4];
 #pragma unroll
-                for (int k = 0; k < kE / 4; ++k) out[k] = s > 0.f ? new_codes(y + 4 * k, inv, s, half) : 0;
+                for (int k = 0; k < kE / 4; ++k) out[k] = s > 0.f ? new_codes(y + 4 * k, inv, s, edge) : 0;
                 store_words(codes + i * 4 * D + (c * 8 + l8) * kE, out);
             }
         }

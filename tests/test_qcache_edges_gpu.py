@@ -8,7 +8,7 @@ from paper_2411_15785_b200 import binding as B
 from paper_2411_15785_b200 import build as bld
 
 import _qcache_ref as R
-from test_qcache_gpu import _same
+from test_qcache_gpu import _planes, _same
 
 pytestmark = pytest.mark.gpu
 
@@ -71,7 +71,7 @@ def test_moved_codes_next_to_a_half_are_those_of_the_exact_quotient(d, holes, po
 
 
 @pytest.mark.parametrize("d,holes", [(64, 1), (64, 3), (128, 5)])
-@pytest.mark.parametrize("power,most", [(0, 127)])
+@pytest.mark.parametrize("power,most", [(0, 127), (-126, 6)])               # (the smallest scales, whose half is no float)
 def test_moved_codes_aimed_at_halves(d, holes, power, most):
     rng = np.random.default_rng(17 + holes)
     units = 1500
@@ -99,3 +99,25 @@ def test_the_length_moves_on_once_whatever_the_ctas_of_a_sequence_have_to_do():
     for b, n in enumerate(held.tolist()):
         assert bool((cache.k[b, :, :n] == 127).all()) and bool((cache.k[b, :, n:] == 0).all())
         assert torch.equal(cache.position[b, :, :n], torch.arange(n, dtype=torch.int32, device="cuda").expand(Hkv, n))
+
+
+# ---- append: the smallest scales, whose half is no float ---------------------------------------------------------
+
+@pytest.mark.parametrize("d,T", [(64, 32), (128, 20)])
+def test_appended_codes_at_halves_of_the_smallest_scales(d, T):
+    rng = np.random.default_rng(3)
+    heads = 40
+    s = _near(np.float32(2.0 ** -126), rng.integers(1, 1 << 23, heads) | 1)          # odd multiples of 2^-149
+    x = np.zeros((1, T, heads, d), np.float32)
+    for h in range(heads):
+        amax = np.float32(127 * s[h].astype(np.float64))
+        mine = np.float64(np.float32(np.float64(amax) / 127))
+        half = (rng.integers(0, 126, (T, d)) + 0.5) * mine                          # exact in 64 bits, no multiple of 2^-149
+        x[0, :, h] = (np.rint(half * 2.0 ** 149) + rng.integers(-1, 2, (T, d))) * 2.0 ** -149 * rng.choice([-1, 1], (T, d))
+        x[0, 0, h, 0] = amax
+    k = torch.from_numpy(x).cuda()
+    cache = B.QuantCache(1, heads, d, 96)
+    ref = R.Ref(_planes(cache))
+    cache.append(k, k.flip(1))
+    ref.append(k, k.flip(1))
+    _same(cache, ref)
