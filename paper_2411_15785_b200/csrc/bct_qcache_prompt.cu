@@ -527,11 +527,12 @@ __global__ void __launch_bounds__(kQpThreads, 1) qc_prompt_kernel(const QcAttend
                 load_scales(n + n_step);
                 float vt = fmaxf(vs, __shfl_xor_sync(0xffffffffu, vs, 1));
                 vt = fmaxf(0.f, fmaxf(vt, __shfl_xor_sync(0xffffffffu, vt, 2)));
-                // the scale that the values are relative to follows the loudest block (some way above it, so that it moves
-                // rarely), not below 2^-60 of the loudest so far
+                // the scale that the values are relative to follows the loudest block of the tile: above it, so that it moves rarely,
+                // by 8 at most, so that P's last place, 2^-25 of 2^9, is 2^-31 of the tile's largest value; but not below 2^-60 of
+                // the loudest so far
                 float by_v = 1.f;
                 vmost = fmaxf(vmost, vt);
-                if (vt > vref || vt < vref * 0.00390625f) {
+                if (vt > vref || vt < vref * 0.125f) {
                     const float to = 4.f * fmaxf(vt, vmost * 8.67361738e-19f);
                     if (vref > 0.f && to > 0.f) by_v = vref / to;
                     if (to > 0.f) vref = to;

@@ -1,5 +1,6 @@
-"""GPU tests of the 8-bit cache where its arithmetic can go wrong: roundings next to a half.  Codes and scales are equal to the
-64-bit form."""
+"""GPU tests of the 8-bit cache where its arithmetic can go wrong: roundings next to a half, scales at the end of float's
+range, values of very unlike blocks.  Codes and scales are equal to the 64-bit form; other tolerances are derived beside the
+tests."""
 import numpy as np
 import pytest
 import torch
@@ -121,3 +122,36 @@ def test_appended_codes_at_halves_of_the_smallest_scales(d, T):
     cache.append(k, k.flip(1))
     ref.append(k, k.flip(1))
     _same(cache, ref)
+
+
+# ---- attention: blocks that are far apart ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Bt,Hkv,T,G", [(10, 8, 130, 1), (2, 1, 40, 1), (1, 2, 64, 4)])
+def test_quiet_values_behind_a_loud_tile_keep_their_terms(Bt, Hkv, T, G, d):
+    """One slot has a row's largest probability, and no value; all others 2^-26 of it.  Slots 0..127 are 60 times as loud as the
+    rest, on other features.  A term is off by 2^-31 of the largest value that its tile's scales stand for at most, besides the
+    roundings that are relative to the terms: 2^-11 of a probability, 2^-8 of an output, (d + 16) 2^-24 of a score of 18 for
+    its own and the sum's, n 2^-24 for each of two sums and 2^-21 for the exponentials."""
+    C = 128 * 11 + 50
+    n = C - 3
+    cache = B.QuantCache(Bt, Hkv, d, C)
+    k, v = torch.zeros((2, Bt, n, Hkv, d), device="cuda")
+    k[:, 200, :, 0] = 18.0                               # the others' scores are 0, its own 18
+    v[:, :128, :, 1::2] = 60.0
+    v[:, 128:, :, 0::2] = 1.0
+    v[:, 200] = 0.0
+    cache.append(k, v)
+    q = torch.zeros((Bt, T, Hkv * G, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    ref = R.Ref(_planes(cache))
+    want, added, M, S, _ = ref.attend(q, scale=1.0, device="cuda")
+    out = cache.attend(q, scale=1.0).double().cpu()
+    blocks = -(-n // 32)
+    tile = torch.arange(n) // 32 // 4
+    s = torch.nn.functional.pad(cache.v_scale[0, 0, :blocks].double().cpu(), (0, -blocks % 4)).view(-1, 4).amax(-1) * 127
+    near = torch.cumsum(2.0 ** -31 * s[tile], 0)[n - T:n]            # of the slots that token i sees (1 / sum is below 1)
+    p_off = 2 * (d + 16) * 2.0 ** -24 * S + 2.0 ** -21 + 2 * n * 2.0 ** -24
+    tol = (p_off + 2.0 ** -11) * M + 2.0 ** -8 * want.abs() + near[None, :, None, None]
+    assert float(want[..., 0].min()) > 4 * float(near.max())         # (losing them all would show)
+    assert bool(((out - want).abs() <= tol).all()), float(((out - want).abs() / tol).max())
