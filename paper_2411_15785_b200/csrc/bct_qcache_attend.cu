@@ -773,7 +773,8 @@ __global__ void __launch_bounds__(32 * kQwWarps<D>) qc_weights_kernel(const QcAt
     float2 next_ml[2];
     auto ask = [&](int64_t r0) {                     // eight rows, an iteration ahead
         const int64_t r = r0 + g;
-        fetch_queries<T, D>(row_of<T>(a, a.q, b, h, r < a.R ? r : 0), r < a.R, next);
+        const bool valid = r < (int64_t)sees.n * a.G;             // (rows behind the lengths are not read)
+        fetch_queries<T, D>(row_of<T>(a, a.q, b, h, valid ? r : 0), valid, next);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int64_t re = r0 + 2 * t + e;
