@@ -437,6 +437,8 @@ bct_status_t bct_qcache_append(const bct_qcache_t *cache, int64_t T, int32_t dty
  *   q, out  DEVICE [B][T][Hq][d] in `dtype`; heads h*G .. h*G+G-1 read kv-head h, G = Hq / Hkv; Hq in 1..65536
  *   lens    as above: n of each sequence.  Rows behind them are not read, add nothing, and their `out` is zero; so is that of
  *           a row that sees no slot
+ * A NaN in a query makes its row's `out` NaN and, as p_j is, with `accumulate` the weight of every slot that the row sees, which then
+ * counts as more than any number (below); an infinity may.  Other rows, and slots that only others see, are as without it.
  *   scale   <= 0 selects 1/sqrt(head_dim)
  *   scratch DEVICE, 256-byte aligned, bct_qcache_attend_scratch_bytes bytes.  In use until the stream has passed the call:
  *           calls that may overlap need a scratch each

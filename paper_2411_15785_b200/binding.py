@@ -575,7 +575,8 @@ class QuantCache:
     def attend(self, q, lens=None, scale=0.0, score_cap=0.0, accumulate=True, out=None, scratch=None, stream=None):
         """Attention of the last T tokens appended to each sequence, q ``[B, T, Hq, d]``, each over the slots up to its
         own; lens as in append.  scale <= 0: 1/sqrt(d).  score_cap > 0: scores are ``score_cap tanh(s / score_cap)``.
-        accumulate: adds what each slot was given to ``weight``.  Returns out ``[B, T, Hq, d]``."""
+        accumulate: adds what each slot was given to ``weight`` (NaN, to all that a row sees, if the row's query has a NaN).
+        Returns out ``[B, T, Hq, d]``."""
         if stream is not None:
             return _on_stream(stream, lambda q_: self.attend(q_, lens, scale, score_cap, accumulate, out, scratch), q)
         accumulate = 1 if accumulate else 0

@@ -1,6 +1,6 @@
 """GPU tests of the 8-bit cache where its arithmetic can go wrong: roundings next to a half, scales at the end of float's
-range, values of very unlike blocks.  Codes and scales are equal to the 64-bit form; other tolerances are derived beside the
-tests."""
+range, values of very unlike blocks, spoilt queries and their accounts of weight.  Codes and scales are equal to the 64-bit
+form; other tolerances are derived beside the tests."""
 import numpy as np
 import pytest
 import torch
@@ -9,7 +9,7 @@ from paper_2411_15785_b200 import binding as B
 from paper_2411_15785_b200 import build as bld
 
 import _qcache_ref as R
-from test_qcache_gpu import _planes, _same
+from test_qcache_gpu import _filled, _planes, _same, _tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -155,3 +155,28 @@ def test_quiet_values_behind_a_loud_tile_keep_their_terms(Bt, Hkv, T, G, d):
     tol = (p_off + 2.0 ** -11) * M + 2.0 ** -8 * want.abs() + near[None, :, None, None]
     assert float(want[..., 0].min()) > 4 * float(near.max())         # (losing them all would show)
     assert bool(((out - want).abs() <= tol).all()), float(((out - want).abs() / tol).max())
+
+
+# ---- a query that is not finite, and the account of weight -------------------------------------------------------
+
+@pytest.mark.parametrize("Bt,T,Hq,Hkv,C,dtype", [
+    (2, 1, 8, 1, 300, "bf16"), (2, 1, 1, 1, 300, "f32"), (2, 6, 4, 1, 300, "bf16"), (2, 40, 2, 1, 300, "f32"),     # by stored scores / keys
+    (2, 40, 4, 2, 300, "bf16"), (2, 300, 4, 1, 700, "bf16"), (75, 300, 1, 1, 2048, "bf16"),          # the tensor path's three forms
+])
+@pytest.mark.parametrize("what,cap", [(float("nan"), 0.0), (float("inf"), 0.0), (float("nan"), 20.0)])
+def test_a_query_that_is_not_finite_gives_nan_to_the_slots_that_its_row_sees_and_no_others(Bt, T, Hq, Hkv, C, dtype, what, cap):
+    held = C - 5
+    q = _tokens(Bt, T, Hq, 64, dtype, 9)
+    bad_q = q.clone()
+    bad_q[0, T // 2, 0, 5] = what
+    got = []
+    for x in (q, bad_q):
+        cache, _ = _filled(Bt, Hkv, 64, C, dtype, [held] * Bt, 8)
+        cache.attend(x, score_cap=cap)
+        got.append(cache.weight[:, :, :held])
+    clean, bad = got
+    seen = held - T + T // 2 + 1
+    assert bool(torch.isnan(bad[0, 0, :seen]).all())
+    assert torch.equal(bad[0, 0, seen:], clean[0, 0, seen:])
+    assert torch.equal(bad[1:], clean[1:]) and torch.equal(bad[0, 1:], clean[0, 1:])
+    assert bool(torch.isfinite(clean).all())
