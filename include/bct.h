@@ -439,7 +439,7 @@ bct_status_t bct_qcache_append(const bct_qcache_t *cache, int64_t T, int32_t dty
  *           a row that sees no slot
  * A NaN in a query makes its row's `out` NaN and, as p_j is, with `accumulate` the weight of every slot that the row sees, which then
  * counts as more than any number (below); an infinity may.  Other rows, and slots that only others see, are as without it.
- *   scale   <= 0 selects 1/sqrt(head_dim)
+ *   scale   <= 0 selects 1/sqrt(head_dim).  scale log2(e), score_cap log2(e) and scale / score_cap are within fp32's range
  *   scratch DEVICE, 256-byte aligned, bct_qcache_attend_scratch_bytes bytes.  In use until the stream has passed the call:
  *           calls that may overlap need a scratch each
  * Roundings.  fp32 sums and softmax.  BCT_BF16: exact products of queries and codes, probabilities rounded to 11 bits where

@@ -216,6 +216,8 @@ extern "C" bct_status_t bct_qcache_attend(const bct_qcache_t* cache, int64_t T, 
     if (!(scale > 0.f)) scale = 1.0f / std::sqrt((float)a.c.D);
     if (score_cap > 0.f && (!std::isfinite(scale / score_cap) || scale / score_cap < 1.17549435e-38f))
         return fail(BCT_ERR_INVALID_ARG, "scale / score_cap is out of fp32's range");
+    if (!std::isfinite(scale * 1.4426950408889634f) || !std::isfinite(score_cap * 1.4426950408889634f))   // (scores are powers of two)
+        return fail(BCT_ERR_INVALID_ARG, "scale or score_cap, times log2(e), is out of fp32's range");
     if (bct_status_t st = check_scratch(scratch, scratch_bytes, p.total)) return st;
     const size_t bytes = (size_t)a.c.B * T * n_q_heads * a.c.D * (dtype == BCT_F32 ? 4 : 2);
     s[0] = {"out", out, bytes};
