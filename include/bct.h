@@ -449,6 +449,8 @@ bct_status_t bct_qcache_append(const bct_qcache_t *cache, int64_t T, int32_t dty
  * s the largest v_scale of the 128 slots (from a multiple of 128 on) that j is among, seen by the row or not, or, if that is more,
  * by 2^-92 of 127 times the largest v_scale in front of them.  The weights are fp32 sums.  No atomics: the same call gives the
  * same bits.
+ * Range.  `out` is that precise while the blocks' largest values are 0 or at least 2^-90, and at most 2^112 divided by the number of
+ * slots seen (the sums hold 2^15 times the probabilities); scores, in powers of two, have to be within fp32's range.
  */
 bct_status_t bct_qcache_attend_scratch_bytes(const bct_qcache_t *cache, int64_t T, int32_t n_q_heads, int32_t dtype,
                                              int32_t accumulate, size_t *bytes);

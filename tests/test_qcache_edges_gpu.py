@@ -157,6 +157,25 @@ def test_quiet_values_behind_a_loud_tile_keep_their_terms(Bt, Hkv, T, G, d):
     assert bool(((out - want).abs() <= tol).all()), float(((out - want).abs() / tol).max())
 
 
+@pytest.mark.parametrize("T,dtype", [(1, "bf16"), (6, "bf16"), (40, "bf16"), (150, "bf16"), (1, "f32"), (40, "f32")])
+@pytest.mark.parametrize("power", [-90, 103])
+def test_values_at_the_ends_of_the_range(T, dtype, power):
+    """Largest values of 2^-90, and of 2^112 by the 300 slots seen (with a little to spare)."""
+    cache = B.QuantCache(2, 2, 64, 320)
+    k, v = _tokens(2, 300, 2, 64, dtype, 1), _tokens(2, 300, 2, 64, "f32", 2)
+    v = (v / v.abs().amax() * 2.0 ** power).to(k.dtype)
+    cache.append(k, v)
+    ref = R.Ref(_planes(cache))
+    q = _tokens(2, T, 8, 64, dtype, 3)
+    want, _, M, S, V = ref.attend(q, device="cuda")
+    out = cache.attend(q).double().cpu()
+    f32 = dtype == "f32"
+    e = (64 + 16) * 2.0 ** -24 * S + (2.0 ** -22 * S if f32 else 0.0)
+    p_off = 2 * e + 2.0 ** -21 + 2 * 300 * 2.0 ** -24
+    tol = (p_off + (2.0 ** -22 if f32 else 2.0 ** -11)) * M + (2.0 ** -24 if f32 else 2.0 ** -8) * want.abs() + 300 * 2.0 ** -31 * V
+    assert bool(((out - want).abs() <= tol).all()), float(((out - want).abs() / tol).max())
+
+
 # ---- a query that is not finite, and the account of weight -------------------------------------------------------
 
 @pytest.mark.parametrize("Bt,T,Hq,Hkv,C,dtype", [
