@@ -604,8 +604,11 @@ cudaError_t qc_append(const QcAppend& args, int dtype, cudaStream_t s) {
 
 cudaError_t qc_evict(const QcEvict& a, cudaStream_t s) {
     const int units = a.c.B * a.c.Hkv;
-    // many units fill the SMs with small CTAs, whose barriers cost less; few units need their threads
-    const bool small = units >= 296;
+    // Many units fill the SMs with small CTAs, whose barriers cost less; few units need their threads, and so do long ones, of
+    // whose keys an SM holds few.  An eviction of C / 16 slots with 256 / 1024 threads to a CTA: 64 units of 4096 slots 23 / 18 us, 256
+    // 38 / 35, 320 45 / 46, 512 60 / 64, 1024 107 / 114; 512 of 8192 108 / 111, of 16384 259 / 207, of 32768 594 / 414.  Of one slot: 256 of
+    // 4096 8.2 / 9.2, 512 9.7 / 12.1; 512 of 8192 11.8 / 14.1, of 16384 18.8 / 17.9, of 32768 95 / 55.
+    const bool small = units >= 296 && a.c.C <= 8192;
     const auto kernel = small ? qc_select_kernel<256> : qc_select_kernel<1024>;
     const int smem = (a.c.C < kQsKeys ? a.c.C : kQsKeys) * 4;
     cudaError_t e;

@@ -102,6 +102,27 @@ def test_the_length_moves_on_once_whatever_the_ctas_of_a_sequence_have_to_do():
         assert torch.equal(cache.position[b, :, :n], torch.arange(n, dtype=torch.int32, device="cuda").expand(Hkv, n))
 
 
+# ---- evictions of many sequences ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("Bt,C,n,ties", [(295, 200, 40, False), (296, 200, 1, True), (296, 200, 40, True), (298, 8192, 1, True),
+                                         (298, 8193, 700, False)])
+def test_evictions_where_the_selection_takes_other_ctas(Bt, C, n, ties):
+    cache = B.QuantCache(Bt, 1, 64, C)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    cache.k.random_(-127, 128, generator=g), cache.v.random_(-127, 128, generator=g)
+    cache.k_scale.uniform_(0.5, 2.0, generator=g), cache.v_scale.uniform_(0.5, 2.0, generator=g)
+    cache.weight.uniform_(0.0, 3.0, generator=g)
+    if ties:
+        cache.weight.round_()
+    cache.position[:] = torch.arange(C, dtype=torch.int32, device="cuda").flip(0)
+    cache.state[:2] = C
+    cache.state[0, ::3] = C - n // 2
+    ref = R.Ref(_planes(cache))
+    cache.evict(C - n, recent=20)
+    ref.evict(C - n, recent=20)
+    _same(cache, ref)
+
+
 # ---- append: the smallest scales, whose half is no float ---------------------------------------------------------
 
 @pytest.mark.parametrize("d,T", [(64, 32), (128, 20)])
