@@ -101,7 +101,8 @@ inline bool grid_fits(int64_t units, int64_t ctas) { return ctas <= 0x7fffffff /
 // Many bfloat16 rows go to the tensor path, whose time hardly depends on how many there are up to 128.  The other serves rows in
 // groups alike of 8, 16 or 24 (16 in float, whose queries and probabilities are two terms each), a reading of the codes for
 // each.  28 rows take 108 us there and 118 on the tensor path with 16 x 4096 slots x 8 heads, 202 / 233 with 64 x 2048, 79 / 112
-// with 64 x 512, 58 / 52 with one sequence of 8192; 48 rows 177 / 120, 325 / 243, 126 / 120, 87 / 54.
+// with 64 x 512, 58 / 52 with one sequence of 8192; 48 rows 177 / 120, 325 / 243, 126 / 120, 87 / 54.  (So one sequence alone loses
+// 6 us at 28 rows; the rule goes by the rows, since batches lose more on the other side: 10 to 33 us.)
 bct_status_t plan_attend(const QcView& v, int64_t T, int32_t n_q_heads, int32_t dtype, int32_t accumulate, bct::QcPlan* p) {
     if (n_q_heads < 1 || n_q_heads > (1 << 16) || n_q_heads % v.Hkv != 0)
         return fail(BCT_ERR_INVALID_ARG, "n_q_heads (%d) must be a multiple of n_kv_heads (%d) in 1..65536", n_q_heads, v.Hkv);

@@ -15,8 +15,8 @@
 // tensor cores are idle most of the time here.  Codes become fp16 exactly (two instructions for a pair: the byte under the
 // exponent of 1024, less 1152).  A query is scaled by a power of two to below 2^15 and is fp16 as it is if it is bfloat16
 // (terms below 2^-39 of the row's largest apart); a float query is two such terms.  Scores are thus exact products with
-// fp32 sums.  The probabilities enter the second product as fp16 times 2^15 (2^-12 of each, below 2^-39 of the largest 0),
-// for float results as two terms (2^-23).  Each block's V product starts from zero and is added with the block's scale in
+// fp32 sums.  The probabilities enter the second product as fp16 times 2^15 (off by 2^-11 of each, and by 2^-40 in any case),
+// for float results as two terms (2^-22).  Each block's V product starts from zero and is added with the block's scale in
 // fp32, so scales may differ by any factor.
 //
 // Fragments need no shuffling of codes: the order of features in the first product's sum, and of slots in the second's, is

@@ -41,7 +41,7 @@ namespace {
 
 constexpr int kQpRows = 256;                 // rows of a CTA
 constexpr int kQpSlots = 128;                // slots of a tile
-constexpr int kQpThreads = 12 * 32;         // (three warps to a quarter of an SM: 168 registers, a row of S stays in them)
+constexpr int kQpThreads = 12 * 32;         // (three warps to a quarter of an SM: 168 registers, for 64 columns of S and P of 32)
 constexpr int kQpMakers = 96;               // threads that turn codes into operands
 constexpr int kQpHalf = 128 * 128;           // bytes of 128 rows x 64 fp16 columns
 constexpr float kQpPScale = 512.f;           // 2^9

@@ -167,7 +167,7 @@ __device__ __forceinline__ float plane_amax(uint32_t mine, uint32_t (*share)[4],
 // ---- append -----------------------------------------------------------------------------------------------------
 // A few CTAs per (sequence, head) go through the blocks that its new tokens touch, the next block's tokens on their way while
 // this one's are worked on.  The last CTA of a sequence to have read its length moves it on.
-// A fill of 8 sequences by up to 4096 tokens of 8 heads of 128: 38 us = 3.4 TB/s, half of a copy's rate.  What it spends is
+// A fill of 8 sequences by up to 4096 tokens of 8 heads of 128: 39 us = 3.3 TB/s, half of a copy's rate.  What it spends is
 // instructions (some 17 for a value, of which the codes 8) more than bytes.  A warp to a plane of a block instead of four needs
 // a third fewer, but all of the registers, and took 46 us; two warps 38.
 constexpr int kQwResident = 4;    // CTAs on an SM
