@@ -445,7 +445,7 @@ bct_status_t bct_qcache_append(const bct_qcache_t *cache, int64_t T, int32_t dty
  * Roundings.  fp32 sums and softmax.  BCT_BF16: exact products of queries and codes, probabilities rounded to 11 bits where
  * they multiply values, one rounding of `out`.  BCT_F32: queries and probabilities rounded to 22 bits or more.  In any case a
  * term p_j v_j is off by up to 2^-39 of v_j, p_j = 1 being the row's largest.  BCT_BF16 calls with T * G > 32 multiply p_j by ratios
- * of v_scales, in fp32 powers of two (2^-19 of p_j; 2^-17 where a ratio is below 2^-24): there a term is off by up to 2^-31 of 127 s,
+ * of v_scales, in fp32 powers of two (2^-19 of p_j; 2^-17 where a ratio is below 2^-21): there a term is off by up to 2^-31 of 127 s,
  * s the largest v_scale of the 128 slots (from a multiple of 128 on) that j is among, seen by the row or not, or, if that is more,
  * by 2^-92 of 127 times the largest v_scale in front of them.  The weights are fp32 sums.  No atomics: the same call gives the
  * same bits.
